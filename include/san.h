@@ -321,6 +321,124 @@ int32_t san_js_matrix(int32_t n_layers, const float* d_S, int64_t layer_stride, 
 int32_t san_block_similarity(const double* js, int32_t n_layers, int32_t m, int32_t n, double* sim);
 int32_t san_policy_search(const double* js, int32_t n_layers, double theta, int32_t* sizes, int32_t* n_blocks);
 
+/* ------------------------------------------------------------------------------------------
+ * Around the decode step of a beam decoder with long prompts.  None of these calls needs a
+ * context or allocates: workspaces are caller buffers (256-byte aligned, sized by the *_bytes
+ * functions, contents of no importance between calls; calls whose kernels may overlap on the
+ * device need a workspace each).  `d_status` is an optional device int32[8] that the caller has
+ * zeroed: the first item skipped because of its id, length or position is recorded there as
+ * [0] = SAN_ERR_DEVICE_CHECK, [1..4] = kernel tag, item, value, limit, and stays until the
+ * caller clears it.  The current device at the call is the one that owns the stream and the
+ * buffers.  All may be captured into a CUDA graph. */
+
+/* Beam search's selection (Section 4.1 decodes with beam 4, Figure 5 with 4 to 20): the `beam` best
+ * continuations of every sentence, chosen over all of its hypotheses and the vocabulary.
+ * Hypothesis b of sentence s is row s*beam + b of every array.
+ *   - a hypothesis that is not done offers every token v with the score
+ *         d_score[row] + log Softmax(d_logits[row])[v]          and the length d_len[row] + 1;
+ *   - one that is done (d_done != 0) offers itself alone, unchanged; its token counts as eos;
+ *   - one whose score is not finite (a beam slot not in use yet: -inf) offers nothing.
+ * Candidates are ranked by score / ((5 + length) / 6)^alpha (alpha = 0: by score), ties go to the
+ * lowest slot, then the lowest token.  A logit of -inf or NaN is a masked token: it is never
+ * chosen and adds nothing to the sum; logits of +inf share the row's probability among them.
+ * Outputs, best first:
+ *   d_parent[row]     the slot (0..beam-1) it descends from: what san_beam_reorder takes
+ *   d_next[row]       its newest token (eos for a hypothesis that was done)
+ *   d_score_out, d_len_out, d_done_out   its state (done: it was, or the new token is eos)
+ *   d_tokens_out      its history: the parent's first len tokens and, unless the parent was done,
+ *                     the new one; entries from the new length on are not written
+ * Where a sentence has fewer candidates than slots, the slots left over come out as done, with
+ * score -inf, parent = the slot itself, token eos (0 without eos) and the slot's old length and history.
+ * Outputs may be the inputs' own buffers (d_tokens_out = d_tokens with the same ld_tokens, ...).
+ * Scores are compared in double (sums of exponentials: float32 terms, double sums).
+ * A length outside 0..ld_tokens, or ld_tokens itself where a token has to be added, skips the sentence
+ * (its outputs are not written) and is reported. */
+typedef struct {
+    int32_t dtype;            /* of d_logits: SAN_F32 or SAN_BF16 */
+    int32_t n_sent, beam, vocab;      /* beam 1..SAN_MAX_BEAM */
+    const void* d_logits;     /* [n_sent*beam][ld_logits], any element-aligned address */
+    int64_t ld_logits;        /* >= vocab */
+    int32_t eos;              /* 0..vocab-1, or -1: no token ends a hypothesis */
+    float alpha;              /* length exponent, finite */
+    const float* d_score; const int32_t* d_len; const int32_t* d_done;       /* [n_sent*beam] */
+    const int32_t* d_tokens; int64_t ld_tokens;     /* [n_sent*beam][ld_tokens], or both token arrays NULL */
+    float* d_score_out; int32_t* d_len_out; int32_t* d_done_out; int32_t* d_tokens_out;
+    int32_t* d_parent; int32_t* d_next;
+    void* d_workspace; size_t workspace_bytes;
+    int32_t* d_status;        /* optional */
+} san_select_args;
+int32_t san_beam_select_bytes(int32_t n_sent, int32_t beam, int32_t vocab, size_t* workspace_bytes);
+int32_t san_beam_select(const san_select_args* args, void* stream);
+
+/* Where a context keeps the cached rows of a block: the key plane of the block's lowest layer, the value
+ * plane of the same layer, and the distance between the value planes of successive layers in elements
+ * (kind SAN_SELF: planes [sequence][head][max_tgt_len][64]; SAN_ENCDEC: [sentence][head][max_src_len][64]).
+ * SAN_ERR_UNSUPPORTED for SAN_SELF with self_is_aan.  The addresses stay valid until the policy changes. */
+int32_t san_cache_planes(const san_ctx* ctx, int32_t kind, int32_t block, void** d_k, void** d_v, int64_t* v_stride);
+
+/* Query rows of one decode step and the cached rows behind them, for san_window_attn and
+ * san_prefix_attn: item i is sequence d_ids[i] with d_lens[i] cached rows (this step's row among them).
+ * The planes have the context's layout (san_cache_planes; chunk-permuted bf16 rows).  n_heads is a
+ * multiple of n_kv_heads: query head h reads key head h / (n_heads / n_kv_heads). */
+typedef struct {
+    int32_t dtype, n_heads, n_kv_heads;
+    int32_t n_layers;         /* layers that share the weights (Eq. 4): value planes and outputs */
+    const void* d_q;          /* [n_items][n_heads][64], 16-byte aligned as all of these */
+    const void* d_k;          /* [max_ids][n_kv_heads][cap_len][64] */
+    const void* d_v;          /* [n_layers] planes like d_k, v_stride elements apart (a multiple of 64) */
+    int64_t v_stride;
+    int32_t max_ids, cap_len;
+    const int32_t* d_ids; const int32_t* d_lens;
+    int32_t n_items;
+    int32_t max_len;          /* host bound on d_lens (0 = cap_len) */
+    void* d_out;              /* [n_layers][n_items][n_heads][64] */
+    int32_t* d_status;        /* optional */
+} san_cached_rows;
+
+/* Prefixes shared by rows of the batch: prefix g stands in front of the items d_first[g] ..
+ * d_first[g+1]-1 (items before d_first[0] or from d_first[n_prefix] on have none).  Rows in the order a
+ * projection (and san_full_block, san_window_block) has them, so that a prompt's keys and values
+ * can be used where they are. */
+typedef struct {
+    const void* d_k;          /* [n_prefix][cap_len][n_kv_heads][64], 16-byte aligned */
+    const void* d_v;          /* [n_layers] arrays like d_k, v_stride elements apart (a multiple of 64) */
+    int64_t v_stride;
+    int32_t n_prefix, cap_len;
+    const int32_t* d_lens;    /* [n_prefix], 0..max_len */
+    int32_t max_len;          /* host bound on d_lens (0 = cap_len) */
+    const int32_t* d_first;   /* [n_prefix + 1], ascending */
+    int32_t max_group;        /* host bound on the items of a prefix (0 = n_items) */
+} san_shared_prefix;
+
+/* One decode step of attention over a sliding window with sinks: with len = d_lens[i], row j is seen if
+ *     j >= len - window   or   j < n_sink,
+ *     S = Softmax(q . K^T / 8) over the rows seen,   O_l = sum_j S[j] V_l[j]   for every layer l.
+ * Rows that are not seen are not read.  window >= 1, n_sink >= 0.  len = 0 gives zeros.  An id or length out
+ * of range leaves the item's output as it was and is reported. */
+int32_t san_window_attn_bytes(const san_cached_rows* rows, int32_t window, int32_t n_sink, size_t* workspace_bytes);
+int32_t san_window_attn(const san_cached_rows* rows, int32_t window, int32_t n_sink, void* d_workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* One decode step of attention for rows behind shared prefixes: softmax and outputs as above over the
+ * prefix's rows and all of the item's own ones together.  A prefix is read once for all of its items (up to
+ * 16 query rows at a time from the cache hierarchy; more with tensor-core tiles).  A row that sees nothing
+ * (no prefix rows, len 0) gives zeros.  A prefix whose length, first item or number of items is out of range
+ * leaves the outputs of its items as they were and is reported. */
+int32_t san_prefix_attn_bytes(const san_cached_rows* rows, const san_shared_prefix* prefix, size_t* workspace_bytes);
+int32_t san_prefix_attn(const san_cached_rows* rows, const san_shared_prefix* prefix, void* d_workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* The whole-sequence form of san_window_attn, for prompts: san_full_block with causal != 0 and a window. Query
+ * row a of a sequence sees key row b <= a if b > a - window or b < n_sink.
+ *   d_q, d_out  [n_seq][cap_len][n_heads][64] and [n_layers][n_seq][cap_len][n_heads][64]
+ *   d_k, d_v    [n_seq][cap_len][n_kv_heads][64] and [n_layers][n_seq][cap_len][n_kv_heads][64]
+ * (16-byte aligned).  Rows at or beyond d_lens[i] are neither read nor written; a length is cut to
+ * 0..max_len (0 = cap_len) as in san_full_block.  SAN_BF16 only (SAN_F32: SAN_ERR_UNSUPPORTED, for the reason
+ * given there).  What a row does not see does not reach it, infinities and NaN included. */
+int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int32_t n_layers, int32_t window,
+                         int32_t n_sink, const void* d_q, const void* d_k, const void* d_v, const int32_t* d_lens,
+                         int32_t n_seq, int32_t cap_len, int32_t max_len, void* d_out, void* stream);
+
 /* Reads (and clears) the device error word: *first_error = SAN_OK or the first
  * device-check error since the last read; detail[0..3] (optional) = kernel tag, item,
  * offending value, limit.  Synchronises `stream`. */

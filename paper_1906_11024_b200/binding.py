@@ -30,6 +30,8 @@ EXPORTS = (
     "san_cache_append", "san_attn_weights", "san_attn_apply", "san_aan_step", "san_seq_reset",
     "san_device_status", "san_status_string", "san_attn_weights_static", "san_decode_step",
     "san_decode_step_host", "san_step_kernel_select", "san_step_kernel_used", "san_full_block", "san_beam_reorder", "san_js_matrix", "san_block_similarity", "san_policy_search",
+    "san_beam_select", "san_beam_select_bytes", "san_cache_planes", "san_window_attn", "san_window_attn_bytes",
+    "san_prefix_attn", "san_prefix_attn_bytes", "san_window_block",
 )
 
 
@@ -48,6 +50,35 @@ class san_step_args(C.Structure):
         ("n_sent", C.c_int32), ("max_src", C.c_int32),
         ("d_S_enc", C.c_void_p), ("ld_s", C.c_int64), ("d_O_enc", C.c_void_p),
         ("d_x_aan", C.c_void_p), ("d_t", C.c_void_p),
+    ]
+
+
+class san_select_args(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int32), ("n_sent", C.c_int32), ("beam", C.c_int32), ("vocab", C.c_int32),
+        ("d_logits", C.c_void_p), ("ld_logits", C.c_int64), ("eos", C.c_int32), ("alpha", C.c_float),
+        ("d_score", C.c_void_p), ("d_len", C.c_void_p), ("d_done", C.c_void_p),
+        ("d_tokens", C.c_void_p), ("ld_tokens", C.c_int64),
+        ("d_score_out", C.c_void_p), ("d_len_out", C.c_void_p), ("d_done_out", C.c_void_p),
+        ("d_tokens_out", C.c_void_p), ("d_parent", C.c_void_p), ("d_next", C.c_void_p),
+        ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("d_status", C.c_void_p),
+    ]
+
+
+class san_cached_rows(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("n_layers", C.c_int32),
+        ("d_q", C.c_void_p), ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("v_stride", C.c_int64),
+        ("max_ids", C.c_int32), ("cap_len", C.c_int32), ("d_ids", C.c_void_p), ("d_lens", C.c_void_p),
+        ("n_items", C.c_int32), ("max_len", C.c_int32), ("d_out", C.c_void_p), ("d_status", C.c_void_p),
+    ]
+
+
+class san_shared_prefix(C.Structure):
+    _fields_ = [
+        ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("v_stride", C.c_int64), ("n_prefix", C.c_int32),
+        ("cap_len", C.c_int32), ("d_lens", C.c_void_p), ("max_len", C.c_int32), ("d_first", C.c_void_p),
+        ("max_group", C.c_int32),
     ]
 
 
@@ -93,6 +124,15 @@ def lib():
     L.san_js_matrix.argtypes = [i32, vp, i64, i64, i32, i32, vp, vp, vp]
     L.san_block_similarity.argtypes = [C.POINTER(C.c_double), i32, i32, i32, C.POINTER(C.c_double)]
     L.san_policy_search.argtypes = [C.POINTER(C.c_double), i32, C.c_double, _I32P, _I32P]
+    L.san_beam_select_bytes.argtypes = [i32, i32, i32, C.POINTER(sz)]
+    L.san_beam_select.argtypes = [C.POINTER(san_select_args), vp]
+    L.san_cache_planes.argtypes = [vp, i32, i32, C.POINTER(vp), C.POINTER(vp), C.POINTER(i64)]
+    rows, pre = C.POINTER(san_cached_rows), C.POINTER(san_shared_prefix)
+    L.san_window_attn_bytes.argtypes = [rows, i32, i32, C.POINTER(sz)]
+    L.san_window_attn.argtypes = [rows, i32, i32, vp, sz, vp]
+    L.san_prefix_attn_bytes.argtypes = [rows, pre, C.POINTER(sz)]
+    L.san_prefix_attn.argtypes = [rows, pre, vp, sz, vp]
+    L.san_window_block.argtypes = [i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, i32, i32, i32, vp, vp]
     L.san_status_string.argtypes = [i32]
     L.san_status_string.restype = C.c_char_p
     for name in EXPORTS:
@@ -300,3 +340,83 @@ def san_full_block(dtype, n_heads, n_layers, causal, d_q, d_k, d_v, d_lens, n_se
     """Full-sequence shared attention: S once per block, applied to every layer's values."""
     return lib().san_full_block(dtype, n_heads, n_layers, int(causal), _ptr(d_q), _ptr(d_k), _ptr(d_v), _ptr(d_lens),
                                 n_seq, cap_len, max_len, _ptr(d_S), ld_s, _ptr(d_out), _stream(stream))
+
+
+def _struct(cls, kw):
+    """A struct from keyword arguments named like its fields (tensors, addresses, numbers or None)."""
+    a = cls()
+    for name, kind in cls._fields_:
+        v = kw.pop(name, None)
+        if kind is C.c_void_p:
+            setattr(a, name, _ptr(v))
+        elif v is not None:
+            setattr(a, name, float(v) if kind is C.c_float else int(v))
+    if kw:
+        raise TypeError(f"unknown {cls.__name__} fields: {sorted(kw)}")
+    return a
+
+
+def select_args(**kw) -> san_select_args:
+    """A san_select_args block; the caller keeps the tensors alive for as long as it is used."""
+    return _struct(san_select_args, kw)
+
+
+def cached_rows(**kw) -> san_cached_rows:
+    """A san_cached_rows block (query rows of a step and their cached rows)."""
+    return _struct(san_cached_rows, kw)
+
+
+def shared_prefix(**kw) -> san_shared_prefix:
+    """A san_shared_prefix block (prefixes and the items behind them)."""
+    return _struct(san_shared_prefix, kw)
+
+
+def san_beam_select_bytes(n_sent, beam, vocab):
+    """Returns (status, workspace bytes)."""
+    n = C.c_size_t(0)
+    rc = lib().san_beam_select_bytes(n_sent, beam, vocab, C.byref(n))
+    return rc, n.value
+
+
+def san_beam_select(args: san_select_args, stream=None) -> int:
+    """The best continuations of every sentence over its hypotheses and the vocabulary."""
+    return lib().san_beam_select(C.byref(args), _stream(stream))
+
+
+def san_cache_planes(ctx, kind, block):
+    """Returns (status, address of the block's key plane, of its first layer's value plane, elements between
+    the value planes of successive layers)."""
+    k, v, stride = C.c_void_p(None), C.c_void_p(None), C.c_int64(0)
+    rc = lib().san_cache_planes(ctx, kind, block, C.byref(k), C.byref(v), C.byref(stride))
+    return rc, k.value, v.value, stride.value
+
+
+def san_window_attn_bytes(rows: san_cached_rows, window, n_sink):
+    """Returns (status, workspace bytes)."""
+    n = C.c_size_t(0)
+    rc = lib().san_window_attn_bytes(C.byref(rows), window, n_sink, C.byref(n))
+    return rc, n.value
+
+
+def san_window_attn(rows: san_cached_rows, window, n_sink, d_workspace, workspace_bytes, stream=None) -> int:
+    """One decode step of attention over a sliding window of the cache and its first rows."""
+    return lib().san_window_attn(C.byref(rows), window, n_sink, _ptr(d_workspace), workspace_bytes, _stream(stream))
+
+
+def san_prefix_attn_bytes(rows: san_cached_rows, prefix: san_shared_prefix):
+    """Returns (status, workspace bytes)."""
+    n = C.c_size_t(0)
+    rc = lib().san_prefix_attn_bytes(C.byref(rows), C.byref(prefix), C.byref(n))
+    return rc, n.value
+
+
+def san_prefix_attn(rows: san_cached_rows, prefix: san_shared_prefix, d_workspace, workspace_bytes, stream=None) -> int:
+    """One decode step of attention for rows behind shared prefixes."""
+    return lib().san_prefix_attn(C.byref(rows), C.byref(prefix), _ptr(d_workspace), workspace_bytes, _stream(stream))
+
+
+def san_window_block(dtype, n_heads, n_kv_heads, n_layers, window, n_sink, d_q, d_k, d_v, d_lens, n_seq, cap_len, max_len,
+                     d_out, stream=None) -> int:
+    """Causal attention of whole sequences over a sliding window and their first rows."""
+    return lib().san_window_block(dtype, n_heads, n_kv_heads, n_layers, window, n_sink, _ptr(d_q), _ptr(d_k), _ptr(d_v),
+                                  _ptr(d_lens), n_seq, cap_len, max_len, _ptr(d_out), _stream(stream))

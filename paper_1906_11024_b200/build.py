@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsan_b200.so")
-SOURCES = ["san_api.cu", "san_static.cu", "san_policy.cpp"]
+SOURCES = ["san_api.cu", "san_static.cu", "san_serve.cu", "san_policy.cpp"]
 
 
 def _inputs():
@@ -29,7 +29,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-Xcompiler", "-fPIC", "-shared", "-o", tmp]
+           "-Xcompiler", "-fPIC", "-shared", "--threads", "0", "-o", tmp]
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += [os.path.join(CSRC, s) for s in SOURCES]

@@ -1,0 +1,575 @@
+// One decode step of attention over cached rows, for one query position per sequence, in two forms:
+//   san_window_attn   a row sees the last `window` rows of its cache and the first `n_sink` ones;
+//   san_prefix_attn   a row sees all of its cache and, in front of it, a prefix that it shares with
+//                     other rows of the batch.
+// As everywhere in this library the weights of a block are computed once and applied to the values
+// of each of its layers (Eq. 3, Eq. 4):
+//     O_l = sum_j S_j V_l[j],   S = Softmax(q.K^T / 8) over the rows j that are seen.
+//
+// The call is bound by reading keys and values once: (1 + layers) * 128 bytes per position and
+// key head (bf16) against 4 * 64 * (1 + layers) operations per query row.  What is laid out for that:
+//   * A UNIT is (key head, up to 16 query rows that share its keys, layer group, a run of positions).  For a
+//     sequence's own rows the query rows are the query heads of the key head's group; for a prefix they
+//     are those of every sequence behind the prefix, so that the prefix is read once for all of them.
+//   * A unit is streamed by 1 or 4 warps.  Each warp has a ring of slots of its own in shared memory (32 rows
+//     of one plane each), filled by 16-byte cp.async five slots ahead: no barrier between warps until
+//     their partial results meet at the end of the unit.
+//   * One pass with the running maximum and sum of the softmax; scores never leave the registers.  bf16
+//     rows go through mma.sync.m16n8k16: D[16 queries x 8 positions], whose accumulators are, packed, the A operand
+//     of D[16 queries x 8 dims].  With one query row 15 of 16 rows are padding, and it is still the
+//     cheapest form: about 5 warp instructions per position against 12 on the CUDA cores.  float32 rows (tolerance
+//     1e-5) stay on the CUDA cores: a lane scores one position for up to 8 query rows, then owns two dims.
+//   * Units of the same row (runs of a long row; its prefix and its own rows) leave (max, sum, unnormalised
+//     outputs) in the workspace and attend_join_kernel adds them up, launched with programmatic stream
+//     serialisation.  Nothing there has to be cleared between calls, no unit waits for another one, and
+//     the order of the additions is fixed.  A row with a single unit is finished by it.
+// Positions that a row does not see are not read (their place in shared memory is filled with
+// zeros), so what lies behind the end of a sequence or between the sinks and the window does not matter.
+#pragma once
+
+#include "san_kernels.cuh"
+
+namespace san {
+
+constexpr int TAG_ATTEND = 9, TAG_PREFIX = 10;
+constexpr int kAtWarps = 4;                 // warps of a CTA
+constexpr int kAtTile = 32;                 // positions per slot
+constexpr int kAtMaxLayers = 4;             // layers whose outputs a warp accumulates at once
+
+template <typename T> struct AttendGeom;
+template <> struct AttendGeom<__nv_bfloat16> { static constexpr int kRows = 16, kSlots = 6, kRowBytes = 128; };
+template <> struct AttendGeom<float>         { static constexpr int kRows = 8,  kSlots = 3, kRowBytes = 256; };
+template <typename T> __host__ __device__ constexpr int attend_warp_bytes() {       // ring; float32: query rows and weights behind it
+    return AttendGeom<T>::kSlots * kAtTile * AttendGeom<T>::kRowBytes +
+           (sizeof(T) == 4 ? AttendGeom<T>::kRows * kDh * 4 + kAtTile * AttendGeom<T>::kRows * 4 : 0);
+}
+template <typename T> __host__ __device__ constexpr int attend_smem_bytes() { return kAtWarps * (attend_warp_bytes<T>() + 2 * AttendGeom<T>::kRows * 4); }
+
+struct AttendParams {
+    const char* q; char* out;
+    int H, Hk, group, n_layers, n_items;    // group = H / Hk query heads per key head
+    // the sequences' own rows: planes [max_ids][Hk][cap][64] as the context keeps them
+    const char* k; const char* v; long long v_stride;           // bytes between the layers' value planes
+    int max_ids, cap, max_len, window, n_sink;                  // window 0: all rows are seen
+    const int* ids; const int* lens;
+    // shared prefixes: [n_prefix][pcap][Hk][64], rows in natural order
+    const char* pk; const char* pv; long long pv_stride;
+    int n_prefix, pcap, max_prefix, max_group;
+    const int* plens; const int* first;
+    // how the work is cut
+    int lg, n_lg;                           // layers per unit
+    int p_units, p_row_tiles, p_splits, p_span, p_wpu;          // units, runs of p_span tiles, warps per unit
+    int o_units, o_row_tiles, o_splits, o_span, o_wpu;
+    int p_ctas;                             // CTAs of the prefix units; those of the own rows follow
+    int slots;                              // partial results per row; 1: units write the outputs
+    float* part_o;                          // [slot][layer][item * H + head][64]
+    float2* part_ml;                        // [slot][item * H + head]
+    int* status;
+    float scale_log2e;
+};
+
+__device__ __forceinline__ void attend_error(int* status, int tag, int item, int value, int limit) {
+    if (status) record_error(status, tag, item, value, limit);
+}
+
+// The prefix of an item: the g with first[g] <= item < first[g + 1], or -1.
+__device__ __forceinline__ int prefix_of(const AttendParams& p, int item) {
+    if (p.n_prefix == 0 || item < p.first[0] || item >= p.first[p.n_prefix]) return -1;
+    int lo = 0, hi = p.n_prefix;            // first[lo] <= item < first[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (p.first[mid] <= item) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+// A prefix whose description is in order.  An empty one (no rows behind it) is.
+__device__ __forceinline__ bool prefix_ok(const AttendParams& p, int g) {
+    const int a = p.first[g], b = p.first[g + 1], len = p.plens[g];
+    return a >= 0 && b >= a && b <= p.n_items && b - a <= p.max_group && len >= 0 && len <= p.max_prefix;
+}
+__device__ __forceinline__ bool own_ok(const AttendParams& p, int item) {
+    const int id = p.ids[item], len = p.lens[item];
+    return id >= 0 && id < p.max_ids && len >= 0 && len <= p.max_len;
+}
+
+// What a unit reads: `n` positions, the first n_sink of them at 0.., the others from `lo` on.
+struct AttendRun {
+    const char* k; const char* v;
+    long long row_bytes, v_stride;
+    bool permuted;                          // chunk c of the row at pos sits at c ^ (pos & 7)
+    int n_sink, lo, n;                      // visible rows (of the whole sequence)
+    int begin, end;                         // this unit's part of them
+    int item0, row0, rows, head0;           // query row i: item item0 + (row0 + i) / group, head head0 + (row0 + i) % group
+    int layer0, layers, slot;
+};
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool full) {
+    const int n = full ? 16 : 0;            // 0: the 16 bytes are filled with zeros and nothing is read
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
+
+__device__ __forceinline__ void ldsm4(uint32_t* r, uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t* r, uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma_bf16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Fills one slot with rows [begin, begin + 32) of the visible ones, layer `plane` (-1: keys).
+template <typename T>
+__device__ __forceinline__ void attend_fill(const AttendRun& u, int begin, int end, int plane, uint32_t slot, int lane) {
+    constexpr int RB = AttendGeom<T>::kRowBytes, CPR = RB / 16, RPI = 32 / CPR;     // chunks per row, rows per instruction
+    const char* base = plane < 0 ? u.k : u.v + plane * u.v_stride;
+    const int c_smem = lane % CPR;
+#pragma unroll
+    for (int j = 0; j < kAtTile / RPI; ++j) {
+        const int r = j * RPI + lane / CPR, at = begin + r;
+        const bool full = at < end;
+        const int pos = !full ? 0 : at < u.n_sink ? at : u.lo + (at - u.n_sink);
+        const int c = c_smem ^ (r & 7);
+        const char* src = base + pos * u.row_bytes + ((u.permuted ? c ^ (pos & 7) : c) << 4);
+        cp16(slot + r * RB + c_smem * 16, src, full);
+    }
+    cp_commit();
+}
+
+// Where a unit's row goes, and the meeting of the warps of a unit.  Every warp of the CTA calls this (it
+// holds CTA barriers).  In shared memory: per warp [layers][kRows][64] outputs at `own`, (max, sum) per row at
+// `ml`; warps of a unit are neighbours.
+template <typename T>
+__device__ __forceinline__ void attend_finish(const AttendParams& p, const AttendRun& u, bool active, int wpu, char* smem,
+                                              const float2* ml, int warp, int lane) {
+    constexpr int R = AttendGeom<T>::kRows;
+    __syncthreads();
+    if (!active) return;
+    const int w0 = warp / wpu * wpu;
+    const long long n_rows = (long long)p.n_items * p.H;
+    // a unit's warps share its rows: 16 lanes and float4 for a row's 64 outputs
+    const int threads = wpu * 32, t = (warp - w0) * 32 + lane;
+    for (int i = t >> 4; i < u.rows; i += threads >> 4) {
+        float m = -INFINITY;
+        for (int w = 0; w < wpu; ++w) m = fmaxf(m, ml[(w0 + w) * R + i].x);
+        float l = 0.f, weight[kAtWarps];
+#pragma unroll
+        for (int w = 0; w < kAtWarps; ++w) {
+            if (w >= wpu) { weight[w] = 0.f; continue; }
+            const float2 x = ml[(w0 + w) * R + i];
+            weight[w] = x.y > 0.f ? (x.x == m ? 1.f : exp2f(x.x - m)) : x.y;      // nothing seen: 0 (and NaN stays NaN)
+            l += weight[w] * x.y;
+        }
+        const int row = u.row0 + i, item = u.item0 + row / p.group, head = u.head0 + row % p.group;
+        const long long at = (long long)item * p.H + head;
+        const bool direct = p.slots == 1;
+        const float inv = direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+        if (!direct && (t & 15) == 0 && u.layer0 == 0) p.part_ml[u.slot * n_rows + at] = make_float2(m, l);
+        if (!direct && l == 0.f) continue;                                        // the join does not look at it
+        for (int y = 0; y < u.layers; ++y) {
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kAtWarps; ++w) {
+                if (w >= wpu || weight[w] == 0.f) continue;
+                const float4 x = *reinterpret_cast<const float4*>(smem + (w0 + w) * attend_warp_bytes<T>() + ((y * R + i) * kDh + (t & 15) * 4) * 4);
+                o.x += weight[w] * x.x; o.y += weight[w] * x.y; o.z += weight[w] * x.z; o.w += weight[w] * x.w;
+            }
+            const int layer = u.layer0 + y;
+            if (direct) {
+                T* dst = reinterpret_cast<T*>(p.out) + ((long long)layer * n_rows + at) * kDh + (t & 15) * 4;
+                if constexpr (sizeof(T) == 4) {
+                    *reinterpret_cast<float4*>(dst) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+                } else {
+                    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+                }
+            } else {
+                *reinterpret_cast<float4*>(p.part_o + (((long long)u.slot * p.n_layers + layer) * n_rows + at) * kDh + (t & 15) * 4) = o;
+            }
+        }
+    }
+}
+
+// Walks a warp's tiles: fill(slot index, ...) runs kSlots - 1 slots ahead of use.  The slots of a tile are its
+// keys and then the values of each layer.
+template <typename T> struct AttendRing {
+    static constexpr int N = AttendGeom<T>::kSlots, SB = kAtTile * AttendGeom<T>::kRowBytes;
+    const AttendRun& u; uint32_t ring; int lane, step;      // step: positions between this warp's tiles
+    int f_at, f_plane, f_slot, r_slot;
+    __device__ __forceinline__ AttendRing(const AttendRun& run, uint32_t smem, int ln, int first, int stp)
+        : u(run), ring(smem), lane(ln), step(stp), f_at(first), f_plane(-1), f_slot(0), r_slot(0) {
+        for (int i = 0; i < N - 1; ++i) fill();
+    }
+    __device__ __forceinline__ void fill() {
+        if (f_at < u.end) {
+            attend_fill<T>(u, f_at, u.end, f_plane, ring + f_slot * SB, lane);
+            if (++f_plane == u.layers) { f_plane = -1; f_at += step; }
+            f_slot = f_slot + 1 == N ? 0 : f_slot + 1;
+        } else {
+            cp_commit();                                     // an empty group keeps the count
+        }
+    }
+    // Offset of the next slot in order, arrived; every lane is done with the one before it, which is refilled.
+    __device__ __forceinline__ uint32_t next() {
+        cp_wait<N - 2>();
+        __syncwarp();
+        fill();
+        const uint32_t s = r_slot * SB;
+        r_slot = r_slot + 1 == N ? 0 : r_slot + 1;
+        return s;
+    }
+};
+
+// bf16, up to 16 query rows.  ROWS8: rows 8 to 15 are padding.
+template <int LG, bool ROWS8>
+__device__ __forceinline__ void attend_warp_bf16(const AttendParams& p, const AttendRun& u, int first, int step, char* smem, float2* ml, int lane) {
+    const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(smem);
+    AttendRing<__nv_bfloat16> ring(u, ring_addr, lane, first, step);
+    const int g = lane >> 2, t4 = lane & 3;
+    uint32_t qa[4][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = g + h * 8;
+        const bool real = i < u.rows && !(ROWS8 && h == 1);
+        const int row = u.row0 + (real ? i : 0), item = u.item0 + row / p.group, head = u.head0 + row % p.group;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q + ((long long)item * p.H + head) * 128) + t4;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            qa[c][h] = real ? src[c * 8] : 0u;
+            qa[c][h + 2] = real ? src[c * 8 + 4] : 0u;
+        }
+    }
+    float acc[LG][8][4];
+#pragma unroll
+    for (int y = 0; y < LG; ++y)
+#pragma unroll
+        for (int d = 0; d < 8; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[y][d][e] = 0.f;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+    const int r8 = lane & 7, mat = lane >> 3;
+    for (int at = first; at < u.end; at += step) {
+        const uint32_t ks = ring_addr + ring.next();
+        float s[4][4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+            uint32_t b[8];
+            const uint32_t row = ks + (n * 8 + r8) * 128;
+            ldsm4(b, row + ((mat ^ r8) << 4));
+            ldsm4(b + 4, row + (((mat + 4) ^ r8) << 4));
+#pragma unroll
+            for (int c = 0; c < 4; ++c) mma_bf16(s[n], qa[c], b[2 * c], b[2 * c + 1]);
+        }
+        float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[n][e] = at + n * 8 + t4 * 2 + (e & 1) < u.end ? s[n][e] * p.scale_log2e : -INFINITY;
+                top[e >> 1] = fmaxf(top[e >> 1], s[n][e]);
+            }
+        float alpha[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (ROWS8 && h == 1) { alpha[1] = 1.f; continue; }
+            top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
+            top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
+            const float m_new = fmaxf(m[h], top[h]);
+            const float base = m_new == -INFINITY ? 0.f : m_new;     // all scores -inf so far: weights 0
+            alpha[h] = m[h] == m_new ? 1.f : fast_exp2(m[h] - base);
+            m[h] = m_new;
+            float sum = 0.f;
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    s[n][2 * h + e] = fast_exp2(s[n][2 * h + e] - base);
+                    sum += s[n][2 * h + e];
+                }
+            l[h] = l[h] * alpha[h] + sum;
+        }
+        // The weights enter the second product in bf16 (at most half a step, 2^-8 relative, of independent sign); their
+        // sum is that of the float32 ones.
+        uint32_t pa[2][4];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            pa[c][0] = pack_bf16(s[2 * c][0], s[2 * c][1]);
+            pa[c][1] = ROWS8 ? 0u : pack_bf16(s[2 * c][2], s[2 * c][3]);
+            pa[c][2] = pack_bf16(s[2 * c + 1][0], s[2 * c + 1][1]);
+            pa[c][3] = ROWS8 ? 0u : pack_bf16(s[2 * c + 1][2], s[2 * c + 1][3]);
+        }
+        if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+#pragma unroll
+            for (int y = 0; y < LG; ++y)
+#pragma unroll
+                for (int d = 0; d < 8; ++d)
+#pragma unroll
+                    for (int e = 0; e < (ROWS8 ? 2 : 4); ++e) acc[y][d][e] *= alpha[e >> 1];
+        }
+#pragma unroll
+        for (int y = 0; y < LG; ++y) {
+            if (y >= u.layers) break;
+            const uint32_t vs = ring_addr + ring.next();
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int d = 0; d < 8; d += 2) {
+                    uint32_t b[4];
+                    ldsm4t(b, vs + (c * 16 + (mat & 1) * 8 + r8) * 128 + (((d + (mat >> 1)) ^ r8) << 4));
+                    mma_bf16(acc[y][d], pa[c], b[0], b[1]);
+                    mma_bf16(acc[y][d + 1], pa[c], b[2], b[3]);
+                }
+            }
+    }
+    cp_wait<0>();
+    __syncwarp();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (ROWS8 && h == 1) break;
+        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+        if (t4 == 0) ml[g + h * 8] = make_float2(m[h], l[h]);
+#pragma unroll
+        for (int y = 0; y < LG; ++y)
+#pragma unroll
+            for (int d = 0; d < 8; ++d)
+                *reinterpret_cast<float2*>(smem + ((y * 16 + g + h * 8) * kDh + d * 8 + t4 * 2) * 4) = make_float2(acc[y][d][2 * h], acc[y][d][2 * h + 1]);
+    }
+}
+
+// float32, up to R query rows on the CUDA cores.
+template <int LG, int R>
+__device__ __forceinline__ void attend_warp_f32(const AttendParams& p, const AttendRun& u, int first, int step, char* smem, float2* ml, int lane) {
+    constexpr int RMAX = AttendGeom<float>::kRows;
+    AttendRing<float> ring(u, (uint32_t)__cvta_generic_to_shared(smem), lane, first, step);
+    float* qs = reinterpret_cast<float*>(smem + AttendGeom<float>::kSlots * kAtTile * 256);      // [R][64]
+    float* ws = qs + RMAX * kDh;                                                                // [32][R] weights
+    for (int i = 0; i < R; ++i) {
+        const bool real = i < u.rows;
+        const int row = u.row0 + (real ? i : 0), item = u.item0 + row / p.group, head = u.head0 + row % p.group;
+        const float2* src = reinterpret_cast<const float2*>(p.q + ((long long)item * p.H + head) * 256);
+        reinterpret_cast<float2*>(qs + i * kDh)[lane] = real ? src[lane] : make_float2(0.f, 0.f);
+    }
+    float acc[LG][R][2], m[R], l[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        m[i] = -INFINITY; l[i] = 0.f;
+#pragma unroll
+        for (int y = 0; y < LG; ++y) acc[y][i][0] = acc[y][i][1] = 0.f;
+    }
+    __syncwarp();
+    for (int at = first; at < u.end; at += step) {
+        const uint32_t ks = ring.next();
+        float s[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+            const float4 k = *reinterpret_cast<const float4*>(smem + ks + lane * 256 + ((c ^ (lane & 7)) << 4));
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const float4 q = *reinterpret_cast<const float4*>(qs + i * kDh + c * 4);
+                s[i] = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, fmaf(q.w, k.w, s[i]))));
+            }
+        }
+        bool moved = false;
+        float alpha[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            s[i] = at + lane < u.end ? s[i] * p.scale_log2e : -INFINITY;
+            const float m_new = fmaxf(m[i], warp_max(s[i]));
+            const float b = m_new == -INFINITY ? 0.f : m_new;
+            alpha[i] = m[i] == m_new ? 1.f : exp2f(m[i] - b);
+            moved |= m[i] != m_new;
+            m[i] = m_new;
+            s[i] = exp2f(s[i] - b);
+            l[i] = l[i] * alpha[i] + s[i];                    // this lane's positions; joined at the end
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < R; ++i) ws[lane * R + i] = s[i];
+        __syncwarp();
+        if (moved)                                            // the same in all lanes
+#pragma unroll
+            for (int y = 0; y < LG; ++y)
+#pragma unroll
+                for (int i = 0; i < R; ++i) { acc[y][i][0] *= alpha[i]; acc[y][i][1] *= alpha[i]; }
+#pragma unroll
+        for (int y = 0; y < LG; ++y) {
+            if (y >= u.layers) break;
+            const uint32_t vs = ring.next();
+#pragma unroll 8
+            for (int j = 0; j < kAtTile; ++j) {
+                const float2 v = *reinterpret_cast<const float2*>(smem + vs + j * 256 + ((((lane >> 1) ^ (j & 7)) << 4) | ((lane & 1) << 3)));
+                float w[R];
+                if constexpr (R % 4 == 0) {
+#pragma unroll
+                    for (int i = 0; i < R; i += 4) *reinterpret_cast<float4*>(w + i) = *reinterpret_cast<const float4*>(ws + j * R + i);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < R; ++i) w[i] = ws[j * R + i];
+                }
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    acc[y][i][0] = fmaf(w[i], v.x, acc[y][i][0]);
+                    acc[y][i][1] = fmaf(w[i], v.y, acc[y][i][1]);
+                }
+            }
+            }
+    }
+    cp_wait<0>();
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        l[i] = warp_sum(l[i]);
+        if (lane == 0) ml[i] = make_float2(m[i], l[i]);
+#pragma unroll
+        for (int y = 0; y < LG; ++y)
+            *reinterpret_cast<float2*>(smem + ((y * RMAX + i) * kDh + lane * 2) * 4) = make_float2(acc[y][i][0], acc[y][i][1]);
+    }
+}
+
+// Unit `index` of the prefix units or of the sequences' own rows.  False: nothing to do (reported where the input
+// is at fault).
+template <typename T>
+__device__ __forceinline__ bool attend_unit(const AttendParams& p, bool prefix, int index, bool reporter, AttendRun* u) {
+    constexpr int R = AttendGeom<T>::kRows, RB = AttendGeom<T>::kRowBytes;
+    if (index >= (prefix ? p.p_units : p.o_units)) return false;
+    const int lg = index % p.n_lg; index /= p.n_lg;
+    const int splits = prefix ? p.p_splits : p.o_splits, span = (prefix ? p.p_span : p.o_span) * kAtTile;
+    const int split = index % splits; index /= splits;
+    const int hk = index % p.Hk; index /= p.Hk;
+    u->head0 = hk * p.group;
+    u->layer0 = lg * p.lg;
+    u->layers = min(p.lg, p.n_layers - u->layer0);
+    if (prefix) {
+        const int tile = index % p.p_row_tiles, g = index / p.p_row_tiles;
+        if (!prefix_ok(p, g)) {
+            if (reporter && tile == 0 && split == 0 && hk == 0 && lg == 0) {
+                const int count = p.first[g + 1] - p.first[g];
+                const bool by_len = p.plens[g] < 0 || p.plens[g] > p.max_prefix;
+                attend_error(p.status, TAG_PREFIX, g, by_len ? p.plens[g] : count, by_len ? p.max_prefix : p.max_group);
+            }
+            return false;
+        }
+        const int rows = (p.first[g + 1] - p.first[g]) * p.group;
+        u->item0 = p.first[g];
+        u->row0 = tile * R;
+        u->rows = min(R, rows - u->row0);
+        if (u->rows <= 0) return false;
+        u->n = p.plens[g]; u->n_sink = 0; u->lo = 0;
+        u->row_bytes = (long long)p.Hk * RB;
+        const long long at = ((long long)g * p.pcap * p.Hk + hk) * RB;
+        u->k = p.pk + at;
+        u->v = p.pv + at + u->layer0 * p.pv_stride;
+        u->v_stride = p.pv_stride;
+        u->permuted = false;
+        u->slot = split;
+    } else {
+        const int tile = index % p.o_row_tiles, item = index / p.o_row_tiles;
+        if (!own_ok(p, item)) {
+            if (reporter && tile == 0 && split == 0 && hk == 0 && lg == 0) {
+                const int id = p.ids[item];
+                const bool by_id = id < 0 || id >= p.max_ids;
+                attend_error(p.status, TAG_ATTEND, item, by_id ? id : p.lens[item], by_id ? p.max_ids : p.max_len);
+            }
+            return false;
+        }
+        u->item0 = item; u->row0 = tile * R; u->rows = min(R, p.group - u->row0);
+        const int len = p.lens[item];
+        u->lo = p.window > 0 ? max(0, len - p.window) : 0;
+        u->n_sink = min(p.n_sink, u->lo);
+        u->n = u->n_sink + len - u->lo;
+        u->row_bytes = RB;
+        const long long at = ((long long)p.ids[item] * p.Hk + hk) * p.cap * RB;
+        u->k = p.k + at;
+        u->v = p.v + at + u->layer0 * p.v_stride;
+        u->v_stride = p.v_stride;
+        u->permuted = sizeof(T) == 2;
+        u->slot = p.p_splits + split;
+    }
+    u->begin = min(split * span, u->n);
+    u->end = min(u->begin + span, u->n);
+    return true;
+}
+
+template <typename T, int LG>
+__global__ void __launch_bounds__(kAtWarps * 32) attend_kernel(const __grid_constant__ AttendParams p) {
+    extern __shared__ __align__(128) char attend_smem[];
+    asm volatile("griddepcontrol.launch_dependents;");
+    constexpr int R = AttendGeom<T>::kRows;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool prefix = (int)blockIdx.x < p.p_ctas;
+    const int wpu = prefix ? p.p_wpu : p.o_wpu;
+    const int cta = prefix ? (int)blockIdx.x : (int)blockIdx.x - p.p_ctas;
+    float2* ml = reinterpret_cast<float2*>(attend_smem + kAtWarps * attend_warp_bytes<T>());
+    AttendRun u;
+    const bool active = attend_unit<T>(p, prefix, cta * (kAtWarps / wpu) + warp / wpu, warp % wpu == 0 && lane == 0, &u);
+    if (active) {
+        char* smem = attend_smem + warp * attend_warp_bytes<T>();
+        const int first = u.begin + (warp % wpu) * kAtTile, step = wpu * kAtTile;
+        if constexpr (sizeof(T) == 2) {
+            if (u.rows <= 8) attend_warp_bf16<LG, true>(p, u, first, step, smem, ml + warp * R, lane);
+            else attend_warp_bf16<LG, false>(p, u, first, step, smem, ml + warp * R, lane);
+        } else {
+            if (u.rows <= 1) attend_warp_f32<LG, 1>(p, u, first, step, smem, ml + warp * R, lane);
+            else if (u.rows <= 4) attend_warp_f32<LG, 4>(p, u, first, step, smem, ml + warp * R, lane);
+            else attend_warp_f32<LG, 8>(p, u, first, step, smem, ml + warp * R, lane);
+        }
+    }
+    attend_finish<T>(p, u, active, wpu, attend_smem, ml, warp, lane);
+}
+
+// Adds up the partial results of a row: 16 threads per (item, head), four outputs each.
+template <typename T>
+__global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant__ AttendParams p) {
+    const long long n_rows = (long long)p.n_items * p.H;
+    const long long at = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const int c = threadIdx.x & 15;
+    if (at >= n_rows) return;
+    const int item = (int)(at / p.H);
+    if (!own_ok(p, item)) return;
+    const int g = prefix_of(p, item);
+    if (g >= 0 && !prefix_ok(p, g)) return;
+    const int begin = g >= 0 ? 0 : p.p_splits;          // no prefix in front of this row: its own partial results only
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    float m = -INFINITY;
+    for (int s = begin; s < p.slots; ++s) m = fmaxf(m, p.part_ml[s * n_rows + at].x);
+    float l = 0.f;
+    for (int s = begin; s < p.slots; ++s) {
+        const float2 x = p.part_ml[s * n_rows + at];
+        if (x.y != 0.f) l += x.y * (x.x == m ? 1.f : exp2f(x.x - m));
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    for (int y = 0; y < p.n_layers; ++y) {
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = begin; s < p.slots; ++s) {
+            const float2 x = p.part_ml[s * n_rows + at];
+            if (x.y == 0.f) continue;
+            const float w = (x.x == m ? 1.f : exp2f(x.x - m)) * inv;
+            const float4 v = *reinterpret_cast<const float4*>(p.part_o + (((long long)s * p.n_layers + y) * n_rows + at) * kDh + c * 4);
+            o.x = fmaf(w, v.x, o.x); o.y = fmaf(w, v.y, o.y); o.z = fmaf(w, v.z, o.z); o.w = fmaf(w, v.w, o.w);
+        }
+        T* dst = reinterpret_cast<T*>(p.out) + ((long long)y * n_rows + at) * kDh + c * 4;
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(dst) = o;
+        else *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
+    }
+}
+
+}  // namespace san

@@ -1,0 +1,319 @@
+// Host side of the calls around the decode step of a beam decoder with long prompts: beam selection,
+// step attention behind shared prefixes and over sliding windows, windowed prompts.  Argument checks
+// and how the work is cut; the arithmetic is in san_select.cuh, san_attend.cuh and san_window.cuh.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "san_ctx.h"
+#include "san_kernels.cuh"
+#include "san_select.cuh"
+#include "san_attend.cuh"
+#include "san_window.cuh"
+
+using namespace san;
+
+namespace {
+
+constexpr int kSms = 148;                   // the cuts are made for this GPU; any other number of SMs works
+inline long long div_up(long long a, long long b) { return (a + b - 1) / b; }
+inline int32_t cuda_status(cudaError_t e) { return e == cudaSuccess ? SAN_OK : SAN_ERR_CUDA; }
+inline bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+// Opt-in to dynamic shared memory above 48 KB, once per kernel and device.
+int32_t opt_in(const void* fn, int bytes) {
+    return cuda_status(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+}
+
+// Launches `fn` so that its CTAs may be set up while the kernel before it on the stream still runs
+// (it waits with griddepcontrol.wait before it reads what that one wrote).
+template <typename P>
+int32_t launch_after(void (*fn)(P), unsigned grid, unsigned block, cudaStream_t st, const P& p) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(block); cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    return cuda_status(cudaLaunchKernelEx(&cfg, fn, p));
+}
+
+// ------------------------------------------------------------------------------- beam selection
+// Logits per thread: 32 fill the registers and keep the parts few; 8 where a call has so few rows that
+// its chunks would leave SMs without one.
+int select_per_thread(long long rows, int vocab) { return rows * div_up(vocab, 32 * kSelThreads) < kSms ? 8 : 32; }
+int select_chunks(long long rows, int vocab) { return (int)div_up(vocab, select_per_thread(rows, vocab) * kSelThreads); }
+
+int32_t select_shape(int32_t n_sent, int32_t beam, int32_t vocab) {
+    if (n_sent < 0 || beam < 1 || beam > SAN_MAX_BEAM || vocab < 1 || vocab > (1 << 28)) return SAN_ERR_SHAPE;
+    if ((long long)n_sent * beam > (1 << 24)) return SAN_ERR_SHAPE;
+    if ((long long)n_sent * beam * select_chunks((long long)n_sent * beam, vocab) > 0x7fffffffLL) return SAN_ERR_SHAPE;
+    return SAN_OK;
+}
+
+template <typename T, int PER>
+int32_t launch_select(const SelectParams& p, bool vector, cudaStream_t st) {
+    const unsigned grid = (unsigned)((long long)p.n_sent * p.beam * p.chunks);
+    if (vector) select_rows_kernel<T, PER, true><<<grid, kSelThreads, 0, st>>>(p);
+    else select_rows_kernel<T, PER, false><<<grid, kSelThreads, 0, st>>>(p);
+    if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
+    return launch_after(&select_merge_kernel<T>, (unsigned)p.n_sent, kSelThreads, st, p);
+}
+
+// ------------------------------------------------------------------------------- step attention
+int32_t check_rows(const san_cached_rows* r) {
+    if (!r) return SAN_ERR_NULL;
+    if (r->dtype != SAN_F32 && r->dtype != SAN_BF16) return SAN_ERR_DTYPE;
+    if (r->n_heads < 1 || r->n_heads > 1024 || r->n_kv_heads < 1 || r->n_heads % r->n_kv_heads != 0) return SAN_ERR_SHAPE;
+    if (r->n_layers < 1 || r->n_layers > SAN_MAX_LAYERS) return SAN_ERR_SHAPE;
+    if (r->max_ids < 1 || r->cap_len < 1 || r->cap_len > (1 << 28)) return SAN_ERR_SHAPE;
+    if (r->n_items < 0 || r->n_items > (1 << 24)) return SAN_ERR_SHAPE;
+    if (r->max_len < 0 || r->max_len > r->cap_len) return SAN_ERR_SHAPE;
+    if (r->n_layers > 1 && (r->v_stride < 1 || r->v_stride % kDh != 0)) return SAN_ERR_SHAPE;
+    return SAN_OK;
+}
+int32_t check_prefix(const san_cached_rows* r, const san_shared_prefix* x) {
+    if (!x) return SAN_ERR_NULL;
+    if (x->n_prefix < 0 || x->n_prefix > (1 << 24) || x->cap_len < 1 || x->cap_len > (1 << 28)) return SAN_ERR_SHAPE;
+    if (x->max_len < 0 || x->max_len > x->cap_len || x->max_group < 0 || x->max_group > r->n_items) return SAN_ERR_SHAPE;
+    if (r->n_layers > 1 && (x->v_stride < 1 || x->v_stride % kDh != 0)) return SAN_ERR_SHAPE;
+    return SAN_OK;
+}
+
+// How one kind of units is cut: warps per unit and runs of tiles.
+// A warp takes a whole run where that gives every warp slot of the GPU two of them or the run is short;
+// otherwise the four warps of a CTA share a run, and a long one is cut into several until the SMs have
+// two CTAs each, but not below eight tiles (a run's partial results cost about as much as a tile).
+void cut_runs(long long units, int bound, int* wpu, int* splits, int* span) {
+    const int tiles = (int)div_up(std::max(bound, 1), kAtTile);
+    const long long warps = (long long)kSms * 2 * kAtWarps;
+    *wpu = 1; *splits = 1;
+    if (tiles > 2 && units < 2 * warps) {
+        *wpu = kAtWarps;
+        const long long want = div_up(2 * kSms, std::max<long long>(units, 1));
+        *splits = (int)std::max<long long>(1, std::min<long long>(want, div_up(tiles, 8)));
+    }
+    *span = (int)div_up(tiles, *splits);
+    *splits = (int)div_up(tiles, *span);
+}
+
+struct AttendPlan { AttendParams p; size_t ml_bytes, bytes; long long ctas; };
+
+// Everything but the addresses.
+int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int window, int n_sink, AttendPlan* out) {
+    std::memset(out, 0, sizeof(*out));
+    AttendParams& p = out->p;
+    const int R = r->dtype == SAN_BF16 ? AttendGeom<__nv_bfloat16>::kRows : AttendGeom<float>::kRows;
+    const long long e = r->dtype == SAN_BF16 ? 2 : 4;
+    p.H = r->n_heads; p.Hk = r->n_kv_heads; p.group = r->n_heads / r->n_kv_heads;
+    p.n_layers = r->n_layers; p.n_items = r->n_items;
+    p.max_ids = r->max_ids; p.cap = r->cap_len; p.max_len = r->max_len ? r->max_len : r->cap_len;
+    p.window = window; p.n_sink = n_sink;
+    p.v_stride = r->v_stride * e;
+    p.n_lg = (int)div_up(r->n_layers, kAtMaxLayers);
+    p.lg = (int)div_up(r->n_layers, p.n_lg);
+    p.n_lg = (int)div_up(r->n_layers, p.lg);
+    if (x && x->n_prefix > 0) {
+        p.n_prefix = x->n_prefix; p.pcap = x->cap_len; p.pv_stride = x->v_stride * e;
+        p.max_prefix = x->max_len ? x->max_len : x->cap_len;
+        p.max_group = x->max_group ? x->max_group : std::max(1, r->n_items);
+        p.p_row_tiles = (int)div_up((long long)p.max_group * p.group, R);
+        const long long units = (long long)p.n_prefix * p.p_row_tiles * p.Hk * p.n_lg;
+        cut_runs(units, p.max_prefix, &p.p_wpu, &p.p_splits, &p.p_span);
+        if (units * p.p_splits > 0x7fffffffLL) return SAN_ERR_SHAPE;
+        p.p_units = (int)(units * p.p_splits);
+        p.p_ctas = (int)div_up(p.p_units, kAtWarps / p.p_wpu);
+    }
+    p.o_row_tiles = (int)div_up(p.group, R);
+    const long long units = (long long)r->n_items * p.o_row_tiles * p.Hk * p.n_lg;
+    const long long bound = window > 0 ? std::min<long long>(p.max_len, (long long)window + n_sink) : p.max_len;
+    cut_runs(units, (int)bound, &p.o_wpu, &p.o_splits, &p.o_span);
+    if (units * p.o_splits > 0x7fffffffLL) return SAN_ERR_SHAPE;
+    p.o_units = (int)(units * p.o_splits);
+    p.slots = p.p_splits + p.o_splits;
+    const size_t rows = (size_t)r->n_items * r->n_heads;
+    if (p.slots > 1) {
+        out->ml_bytes = (size_t)div_up((long long)(p.slots * rows * sizeof(float2)), 256) * 256;
+        out->bytes = out->ml_bytes + p.slots * rows * r->n_layers * kDh * sizeof(float);
+    }
+    out->ctas = p.p_ctas + div_up(p.o_units, kAtWarps / p.o_wpu);
+    if (out->ctas > 0x7fffffffLL || div_up((long long)rows, 16) > 0x7fffffffLL) return SAN_ERR_SHAPE;
+    p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)kDh));
+    return SAN_OK;
+}
+
+template <typename T, int LG>
+int32_t launch_attend_as(const AttendPlan& a, cudaStream_t st) {
+    constexpr int smem = attend_smem_bytes<T>();
+    const int32_t rc = opt_in((const void*)attend_kernel<T, LG>, smem);
+    if (rc != SAN_OK) return rc;
+    attend_kernel<T, LG><<<(unsigned)a.ctas, kAtWarps * 32, smem, st>>>(a.p);
+    if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
+    if (a.p.slots == 1) return SAN_OK;
+    const long long rows = (long long)a.p.n_items * a.p.H;
+    return launch_after(&attend_join_kernel<T>, (unsigned)div_up(rows, 16), 256, st, a.p);
+}
+template <typename T>
+int32_t launch_attend(const AttendPlan& a, cudaStream_t st) {
+    return a.p.lg == 1 ? launch_attend_as<T, 1>(a, st) : a.p.lg == 2 ? launch_attend_as<T, 2>(a, st) : launch_attend_as<T, 4>(a, st);
+}
+
+int32_t run_attend(const san_cached_rows* r, const san_shared_prefix* x, int window, int n_sink, void* ws, size_t ws_bytes, void* stream) {
+    AttendPlan a;
+    int32_t rc = plan_attend(r, x, window, n_sink, &a);
+    if (rc != SAN_OK) return rc;
+    if (r->n_items == 0) return SAN_OK;
+    if (!r->d_q || !r->d_k || !r->d_v || !r->d_ids || !r->d_lens || !r->d_out) return SAN_ERR_NULL;
+    if (!aligned(r->d_q, 16) || !aligned(r->d_k, 16) || !aligned(r->d_v, 16) || !aligned(r->d_out, 16)) return SAN_ERR_SHAPE;
+    if (x && x->n_prefix > 0) {
+        if (!x->d_k || !x->d_v || !x->d_lens || !x->d_first) return SAN_ERR_NULL;
+        if (!aligned(x->d_k, 16) || !aligned(x->d_v, 16)) return SAN_ERR_SHAPE;
+        a.p.pk = static_cast<const char*>(x->d_k); a.p.pv = static_cast<const char*>(x->d_v);
+        a.p.plens = x->d_lens; a.p.first = x->d_first;
+    }
+    if (a.bytes > 0) {
+        if (!ws) return SAN_ERR_NULL;
+        if (!aligned(ws, 256)) return SAN_ERR_SHAPE;
+        if (ws_bytes < a.bytes) return SAN_ERR_CAPACITY;
+    }
+    a.p.q = static_cast<const char*>(r->d_q); a.p.out = static_cast<char*>(r->d_out);
+    a.p.k = static_cast<const char*>(r->d_k); a.p.v = static_cast<const char*>(r->d_v);
+    a.p.ids = r->d_ids; a.p.lens = r->d_lens; a.p.status = r->d_status;
+    a.p.part_ml = static_cast<float2*>(ws);
+    a.p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + a.ml_bytes);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return r->dtype == SAN_BF16 ? launch_attend<__nv_bfloat16>(a, st) : launch_attend<float>(a, st);
+}
+
+template <int LG>
+int32_t launch_window(const WindowParams& p, dim3 grid, cudaStream_t st) {
+    window_block_kernel<LG><<<grid, 128, 0, st>>>(p);
+    return cuda_status(cudaGetLastError());
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t san_beam_select_bytes(int32_t n_sent, int32_t beam, int32_t vocab, size_t* workspace_bytes) {
+    if (!workspace_bytes) return SAN_ERR_NULL;
+    const int32_t rc = select_shape(n_sent, beam, vocab);
+    if (rc != SAN_OK) return rc;
+    const long long rows = (long long)n_sent * beam;
+    *workspace_bytes = (size_t)rows * select_chunks(rows, vocab) * select_part_bytes(beam);
+    return SAN_OK;
+}
+
+int32_t san_beam_select(const san_select_args* a, void* stream) {
+    if (!a) return SAN_ERR_NULL;
+    if (a->dtype != SAN_F32 && a->dtype != SAN_BF16) return SAN_ERR_DTYPE;
+    size_t need = 0;
+    int32_t rc = san_beam_select_bytes(a->n_sent, a->beam, a->vocab, &need);
+    if (rc != SAN_OK) return rc;
+    if (a->ld_logits < a->vocab || a->eos < -1 || a->eos >= a->vocab || !std::isfinite(a->alpha)) return SAN_ERR_SHAPE;
+    if (a->n_sent == 0) return SAN_OK;
+    if (!a->d_logits || !a->d_score || !a->d_len || !a->d_done || !a->d_score_out || !a->d_len_out || !a->d_done_out ||
+        !a->d_parent || !a->d_next || !a->d_workspace) return SAN_ERR_NULL;
+    if ((a->d_tokens == nullptr) != (a->d_tokens_out == nullptr)) return SAN_ERR_NULL;
+    if (a->d_tokens && (a->ld_tokens < 1 || a->ld_tokens > 0x7ffffffe)) return SAN_ERR_SHAPE;
+    const size_t e = a->dtype == SAN_F32 ? 4 : 2;
+    if (!aligned(a->d_logits, e) || !aligned(a->d_workspace, 256)) return SAN_ERR_SHAPE;
+    if (a->workspace_bytes < need) return SAN_ERR_CAPACITY;
+    SelectParams p;
+    std::memset(&p, 0, sizeof(p));
+    const long long rows = (long long)a->n_sent * a->beam;
+    p.logits = a->d_logits; p.ld = a->ld_logits; p.vocab = a->vocab; p.n_sent = a->n_sent; p.beam = a->beam;
+    p.chunks = select_chunks(rows, a->vocab); p.eos = a->eos; p.alpha = (double)a->alpha;
+    p.score = a->d_score; p.len = a->d_len; p.done = a->d_done; p.tokens = a->d_tokens; p.ld_tokens = a->ld_tokens;
+    p.score_out = a->d_score_out; p.len_out = a->d_len_out; p.done_out = a->d_done_out; p.tokens_out = a->d_tokens_out;
+    p.parent = a->d_parent; p.next = a->d_next; p.ws = static_cast<char*>(a->d_workspace); p.status = a->d_status;
+    const bool vector = aligned(a->d_logits, 16) && a->ld_logits * (int64_t)e % 16 == 0;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool few = select_per_thread(rows, a->vocab) == 8;
+    if (a->dtype == SAN_F32) return few ? launch_select<float, 8>(p, vector, st) : launch_select<float, 32>(p, vector, st);
+    return few ? launch_select<__nv_bfloat16, 8>(p, vector, st) : launch_select<__nv_bfloat16, 32>(p, vector, st);
+}
+
+int32_t san_cache_planes(const san_ctx* ctx, int32_t kind, int32_t block, void** d_k, void** d_v, int64_t* v_stride) {
+    if (!ctx || !d_k || !d_v || !v_stride) return SAN_ERR_NULL;
+    if (kind != SAN_SELF && kind != SAN_ENCDEC) return SAN_ERR_RANGE;
+    const bool self = kind == SAN_SELF;
+    if (self && ctx->cfg.self_is_aan) return SAN_ERR_UNSUPPORTED;
+    const Policy& pol = self ? ctx->self_pol : ctx->enc_pol;
+    if (block < 0 || block >= pol.n_blocks) return SAN_ERR_RANGE;
+    const size_t plane = self ? ctx->self_plane_bytes : ctx->mem_plane_bytes;
+    const size_t v_plane = !self && ctx->cfg.encdec_shared_context ? (size_t)block : (size_t)pol.first_layer_of_block[block];
+    *d_k = ctx->cache + (self ? ctx->off_self_k : ctx->off_mem_k) + (size_t)block * plane;
+    *d_v = ctx->cache + (self ? ctx->off_self_v : ctx->off_mem_v) + v_plane * plane;
+    *v_stride = (int64_t)(plane / (size_t)ctx->elem_bytes);
+    return SAN_OK;
+}
+
+int32_t san_window_attn_bytes(const san_cached_rows* rows, int32_t window, int32_t n_sink, size_t* workspace_bytes) {
+    if (!workspace_bytes) return SAN_ERR_NULL;
+    int32_t rc = check_rows(rows);
+    if (rc != SAN_OK) return rc;
+    if (window < 1 || n_sink < 0) return SAN_ERR_SHAPE;
+    AttendPlan a;
+    if ((rc = plan_attend(rows, nullptr, window, n_sink, &a)) != SAN_OK) return rc;
+    *workspace_bytes = a.bytes;
+    return SAN_OK;
+}
+
+int32_t san_window_attn(const san_cached_rows* rows, int32_t window, int32_t n_sink, void* d_workspace, size_t workspace_bytes,
+                        void* stream) {
+    const int32_t rc = check_rows(rows);
+    if (rc != SAN_OK) return rc;
+    if (window < 1 || n_sink < 0) return SAN_ERR_SHAPE;
+    return run_attend(rows, nullptr, window, n_sink, d_workspace, workspace_bytes, stream);
+}
+
+int32_t san_prefix_attn_bytes(const san_cached_rows* rows, const san_shared_prefix* prefix, size_t* workspace_bytes) {
+    if (!workspace_bytes) return SAN_ERR_NULL;
+    int32_t rc = check_rows(rows);
+    if (rc == SAN_OK) rc = check_prefix(rows, prefix);
+    if (rc != SAN_OK) return rc;
+    AttendPlan a;
+    if ((rc = plan_attend(rows, prefix, 0, 0, &a)) != SAN_OK) return rc;
+    *workspace_bytes = a.bytes;
+    return SAN_OK;
+}
+
+int32_t san_prefix_attn(const san_cached_rows* rows, const san_shared_prefix* prefix, void* d_workspace, size_t workspace_bytes,
+                        void* stream) {
+    int32_t rc = check_rows(rows);
+    if (rc == SAN_OK) rc = check_prefix(rows, prefix);
+    if (rc != SAN_OK) return rc;
+    return run_attend(rows, prefix, 0, 0, d_workspace, workspace_bytes, stream);
+}
+
+int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int32_t n_layers, int32_t window, int32_t n_sink,
+                         const void* d_q, const void* d_k, const void* d_v, const int32_t* d_lens, int32_t n_seq, int32_t cap_len,
+                         int32_t max_len, void* d_out, void* stream) {
+    if (dtype != SAN_BF16) return dtype == SAN_F32 ? SAN_ERR_UNSUPPORTED : SAN_ERR_DTYPE;
+    if (n_heads < 1 || n_heads > 65535 || n_kv_heads < 1 || n_heads % n_kv_heads != 0) return SAN_ERR_SHAPE;
+    if (n_layers < 1 || n_layers > SAN_MAX_LAYERS || window < 1 || n_sink < 0) return SAN_ERR_SHAPE;
+    if (n_seq < 0 || cap_len < 1 || cap_len > (1 << 28) || max_len < 0 || max_len > cap_len) return SAN_ERR_SHAPE;
+    if (n_seq == 0) return SAN_OK;
+    if (!d_q || !d_k || !d_v || !d_lens || !d_out) return SAN_ERR_NULL;
+    if (!aligned(d_q, 16) || !aligned(d_k, 16) || !aligned(d_v, 16) || !aligned(d_out, 16)) return SAN_ERR_SHAPE;
+    if (max_len == 0) max_len = cap_len;
+    WindowParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.q = static_cast<const __nv_bfloat16*>(d_q); p.k = static_cast<const __nv_bfloat16*>(d_k);
+    p.v = static_cast<const __nv_bfloat16*>(d_v); p.out = static_cast<__nv_bfloat16*>(d_out);
+    p.lens = d_lens; p.n_seq = n_seq; p.cap = cap_len; p.H = n_heads; p.Hk = n_kv_heads; p.group = n_heads / n_kv_heads;
+    p.n_layers = n_layers; p.max_len = max_len; p.window = window; p.n_sink = n_sink;
+    p.v_layer = (long long)n_seq * cap_len * n_kv_heads * kDh;
+    p.out_layer = (long long)n_seq * cap_len * n_heads * kDh;
+    p.n_lg = (int)div_up(n_layers, 2);
+    p.lg = (int)div_up(n_layers, p.n_lg);
+    p.n_lg = (int)div_up(n_layers, p.lg);
+    p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)kDh));
+    if ((long long)n_seq * p.n_lg > 65535) return SAN_ERR_SHAPE;
+    const dim3 grid((unsigned)div_up(max_len, kWinQ), (unsigned)n_heads, (unsigned)(n_seq * p.n_lg));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return p.lg == 1 ? launch_window<1>(p, grid, st) : launch_window<2>(p, grid, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,236 @@
+// Whole sequences under a sliding window with sinks (san_window_block): query row a sees key row b <= a if
+// b > a - window or b < n_sink; S = Softmax(q.K^T / 8) over those, computed once and applied to
+// each layer of the block (Eq. 3, Eq. 4).
+//
+// window_block_kernel (mma.sync): CTA = 64 query rows of one (sequence, head, layer group), 16 per warp.  The CTA walks the
+// rows that any of its queries sees - the sinks, then the window of its first query up to its last query -
+// in tiles of 64 through a ring of shared-memory slots that cp.async fills three slots ahead (keys, then each
+// layer's values), with the running maximum and sum of the softmax; scores stay in registers.
+// A value that a row does not see has weight zero, and zero times an infinity or NaN is NaN: a row whose
+// output came out as NaN is computed again over just the rows it sees (window_row_again).
+#pragma once
+
+#include "san_attend.cuh"
+
+namespace san {
+
+struct WindowParams {
+    const __nv_bfloat16* q; const __nv_bfloat16* k; const __nv_bfloat16* v; __nv_bfloat16* out;
+    const int* lens;
+    long long v_layer, out_layer;           // elements between layers
+    int n_seq, cap, H, Hk, group, n_layers, lg, n_lg, max_len, window, n_sink;
+    float scale_log2e;
+};
+
+constexpr int kWinQ = 64, kWinTile = 64, kWinSlots = 4;
+
+// Row a of (sequence, head), one layer, by one warp: the definition, over the rows that are seen.
+__device__ __noinline__ void window_row_again(const WindowParams& p, int seq, int head, int layer, int a, int lane) {
+    const long long kv = ((long long)seq * p.cap * p.Hk + head / p.group) * kDh + lane * 2;
+    const long long at = (((long long)seq * p.cap + a) * p.H + head) * kDh + lane * 2;
+    const long long step = (long long)p.Hk * kDh;
+    auto two = [](const __nv_bfloat16* x) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(x)); };
+    const float2 q = two(p.q + at);
+    const int lo = max(0, a - p.window + 1), ns = min(p.n_sink, lo), n = ns + a + 1 - lo;
+    float m = -INFINITY, l = 0.f, ox = 0.f, oy = 0.f;
+    for (int pass = 0; pass < 2; ++pass)
+        for (int i = 0; i < n; ++i) {
+            const long long b = i < ns ? i : lo + i - ns;
+            const float2 k = two(p.k + kv + b * step);
+            const float z = warp_sum(q.x * k.x + q.y * k.y) * p.scale_log2e;
+            if (pass == 0) { m = fmaxf(m, z); continue; }
+            const float w = exp2f(z - (m == -INFINITY ? 0.f : m));
+            if (w == 0.f) continue;
+            const float2 v = two(p.v + layer * p.v_layer + kv + b * step);
+            l += w;
+            ox = fmaf(w, v.x, ox); oy = fmaf(w, v.y, oy);
+        }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    *reinterpret_cast<uint32_t*>(p.out + layer * p.out_layer + at) = pack_bf16(ox * inv, oy * inv);
+}
+
+template <int LG>
+__global__ void __launch_bounds__(128) window_block_kernel(const __grid_constant__ WindowParams p) {
+    __shared__ __align__(128) char ring[kWinSlots * kWinTile * 128];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int head = blockIdx.y, seq = blockIdx.z / p.n_lg, layer0 = blockIdx.z % p.n_lg * p.lg;
+    const int layers = min(p.lg, p.n_layers - layer0);
+    const int len = max(0, min(p.lens[seq], p.max_len));
+    const int a0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kWinQ;        // the longest rows first
+    if (a0 >= len) return;
+    const int a1 = min(a0 + kWinQ, len);
+    const int lo = max(0, a0 - p.window + 1), ns = min(p.n_sink, lo), n = ns + a1 - lo;
+    const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(ring);
+    const char* kbase = reinterpret_cast<const char*>(p.k + ((long long)seq * p.cap * p.Hk + head / p.group) * kDh);
+    const char* vbase = reinterpret_cast<const char*>(p.v + layer0 * p.v_layer + ((long long)seq * p.cap * p.Hk + head / p.group) * kDh);
+    const long long row_bytes = (long long)p.Hk * 128;
+
+    int f_at = 0, f_plane = -1, f_slot = 0;
+    auto fill = [&]() {
+        if (f_at < n) {
+            const char* src = f_plane < 0 ? kbase : vbase + f_plane * p.v_layer * 2;
+            const uint32_t slot = ring_addr + f_slot * (kWinTile * 128);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = j * 16 + (threadIdx.x >> 3), c = threadIdx.x & 7, at = f_at + r;
+                const bool full = at < n;
+                const int pos = !full ? 0 : at < ns ? at : lo + at - ns;
+                cp16(slot + r * 128 + ((c ^ (r & 7)) << 4), src + pos * row_bytes + (c << 4), full);
+            }
+            if (++f_plane == layers) { f_plane = -1; f_at += kWinTile; }
+            f_slot = f_slot + 1 == kWinSlots ? 0 : f_slot + 1;
+        }
+        cp_commit();
+    };
+    for (int i = 0; i < kWinSlots - 1; ++i) fill();
+
+    const int g = lane >> 2, t4 = lane & 3, r8 = lane & 7, mat = lane >> 3;
+    const int qa0 = a0 + warp * 16;                                       // the warp's first query
+    uint32_t qa[4][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int a = qa0 + g + h * 8;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q + (((long long)seq * p.cap + a) * p.H + head) * kDh) + t4;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            qa[c][h] = a < a1 ? src[c * 8] : 0u;
+            qa[c][h + 2] = a < a1 ? src[c * 8 + 4] : 0u;
+        }
+    }
+    float acc[LG][8][4];
+#pragma unroll
+    for (int y = 0; y < LG; ++y)
+#pragma unroll
+        for (int d = 0; d < 8; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[y][d][e] = 0.f;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+    int slot = 0;
+    auto next = [&]() -> uint32_t {
+        cp_wait<kWinSlots - 2>();
+        __syncthreads();                                                  // arrived for all; the slot before it is free
+        fill();
+        const uint32_t s = ring_addr + slot * (kWinTile * 128);
+        slot = slot + 1 == kWinSlots ? 0 : slot + 1;
+        return s;
+    };
+    for (int at = 0; at < n; at += kWinTile) {
+        const uint32_t ks = next();
+        const int b_first = at < ns ? 0 : lo + at - ns, b_last = lo + at + kWinTile - 1 - ns;
+        // every one of the warp's queries sees the whole tile: nothing to mask
+        const bool whole = at >= ns && at + kWinTile <= n && b_last <= qa0 && b_first > qa0 + 15 - p.window;
+        const bool none = at >= ns && b_first > qa0 + 15;                 // behind the warp's last query
+        uint32_t pa[4][4];
+        if (!none) {
+            float s[8][4];
+#pragma unroll
+            for (int c8 = 0; c8 < 8; ++c8) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[c8][e] = 0.f;
+                uint32_t b[8];
+                const uint32_t row = ks + (c8 * 8 + r8) * 128;
+                ldsm4(b, row + ((mat ^ r8) << 4));
+                ldsm4(b + 4, row + (((mat + 4) ^ r8) << 4));
+#pragma unroll
+                for (int c = 0; c < 4; ++c) mma_bf16(s[c8], qa[c], b[2 * c], b[2 * c + 1]);
+            }
+            float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int c8 = 0; c8 < 8; ++c8)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    bool seen = true;
+                    if (!whole) {
+                        const int at1 = at + c8 * 8 + t4 * 2 + (e & 1), a = qa0 + g + (e >> 1) * 8;
+                        const int b = at1 < ns ? at1 : lo + at1 - ns;
+                        seen = at1 < n && b <= a && (b > a - p.window || b < p.n_sink);
+                    }
+                    s[c8][e] = seen ? s[c8][e] * p.scale_log2e : -INFINITY;
+                    top[e >> 1] = fmaxf(top[e >> 1], s[c8][e]);
+                }
+            float alpha[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
+                top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
+                const float m_new = fmaxf(m[h], top[h]);
+                const float base = m_new == -INFINITY ? 0.f : m_new;
+                alpha[h] = m[h] == m_new ? 1.f : fast_exp2(m[h] - base);
+                m[h] = m_new;
+                float sum = 0.f;
+#pragma unroll
+                for (int c8 = 0; c8 < 8; ++c8)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        s[c8][2 * h + e] = fast_exp2(s[c8][2 * h + e] - base);
+                        sum += s[c8][2 * h + e];
+                    }
+                l[h] = l[h] * alpha[h] + sum;
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                pa[c][0] = pack_bf16(s[2 * c][0], s[2 * c][1]);
+                pa[c][1] = pack_bf16(s[2 * c][2], s[2 * c][3]);
+                pa[c][2] = pack_bf16(s[2 * c + 1][0], s[2 * c + 1][1]);
+                pa[c][3] = pack_bf16(s[2 * c + 1][2], s[2 * c + 1][3]);
+            }
+            if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+#pragma unroll
+                for (int y = 0; y < LG; ++y)
+#pragma unroll
+                    for (int d = 0; d < 8; ++d)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[y][d][e] *= alpha[e >> 1];
+            }
+        }
+#pragma unroll
+        for (int y = 0; y < LG; ++y) {
+            if (y >= layers) break;
+            const uint32_t vs = next();
+            if (none) continue;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int d = 0; d < 8; d += 2) {
+                    uint32_t b[4];
+                    ldsm4t(b, vs + (c * 16 + (mat & 1) * 8 + r8) * 128 + (((d + (mat >> 1)) ^ r8) << 4));
+                    mma_bf16(acc[y][d], pa[c], b[0], b[1]);
+                    mma_bf16(acc[y][d + 1], pa[c], b[2], b[3]);
+                }
+        }
+    }
+    cp_wait<0>();
+    bool odd[2] = {false, false};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+        const float inv = l[h] == 0.f ? 0.f : 1.f / l[h];
+        const int a = qa0 + g + h * 8;
+        if (a < a1) {
+#pragma unroll
+            for (int y = 0; y < LG; ++y) {
+                if (y >= layers) break;
+                __nv_bfloat16* dst = p.out + (layer0 + y) * p.out_layer + (((long long)seq * p.cap + a) * p.H + head) * kDh + t4 * 2;
+#pragma unroll
+                for (int d = 0; d < 8; ++d) {
+                    const float x = acc[y][d][2 * h] * inv, z = acc[y][d][2 * h + 1] * inv;
+                    odd[h] |= x != x || z != z;
+                    *reinterpret_cast<uint32_t*>(dst + d * 8) = pack_bf16(x, z);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        unsigned again = __ballot_sync(0xffffffffu, odd[h]);
+        while (again) {
+            const int gg = (__ffs(again) - 1) >> 2;
+            again &= ~(0xfu << (gg * 4));
+            for (int y = 0; y < layers; ++y) window_row_again(p, seq, head, layer0 + y, qa0 + gg + h * 8, lane);
+        }
+    }
+}
+
+}  // namespace san

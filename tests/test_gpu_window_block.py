@@ -1,0 +1,142 @@
+"""Windowed attention of whole sequences (san_window_block) against the rows that each query sees, in 64 bits."""
+import pytest
+import torch
+
+from paper_1906_11024_b200 import binding as B
+from paper_1906_11024_b200 import build as san_build
+from tests.serve_helpers import DH, check_outputs, randn
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    san_build.build()
+    B.lib()
+
+
+def _reference(q, k, v, window, sink):
+    """q [l][64], k [l][64], v [L][l][64] in 64 bits -> outputs, slack and weighted sizes [L][l][64]."""
+    l = q.shape[0]
+    a, b = torch.arange(l)[:, None], torch.arange(l)[None, :]
+    seen = (b <= a) & ((b > a - window) | (b < sink))
+    z = (q @ k.T / 8.0).masked_fill(~seen, -float("inf"))
+    p = torch.softmax(z, -1)
+    size = p @ v.abs()
+    # as in serve_helpers.attend, the largest score error of any pair
+    dz = 70 * 2.0 ** -24 * float((q.abs() @ k.abs().T).max()) / 8.0
+    return p @ v, size * (4 * dz + 2.0 ** -20 + 2 * l * 2.0 ** -24), size
+
+
+def _run(lens, cap, H, Hk, L, window, sink, max_len=0, seed=0, spoil=None, scale=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    n = len(lens)
+    q, k = randn(gen, n, cap, H, DH, dtype=torch.bfloat16), randn(gen, n, cap, Hk, DH, dtype=torch.bfloat16)
+    v = randn(gen, L, n, cap, Hk, DH, dtype=torch.bfloat16)
+    q *= scale
+    dq, dk, dv = (x.clone() for x in (q, k, v))
+    for i, t in enumerate(lens):                                # behind the end of a sequence: NaN
+        dq[i, t:], dk[i, t:] = float("nan"), float("nan")
+        dv[:, i, t:] = float("nan")
+    if spoil:
+        spoil(dk, dv)
+    dq, dk, dv = (x.to(DEV) for x in (dq, dk, dv))
+    out = torch.full((L, n, cap, H, DH), -7.0, dtype=torch.bfloat16, device=DEV)
+    dl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    B.check(B.san_window_block(B.SAN_BF16, H, Hk, L, window, sink, dq, dk, dv, dl, n, cap, max_len, out))
+    torch.cuda.synchronize()
+    got = out.cpu()
+    return q, k, v, got
+
+
+def _check(q, k, v, got, lens, window, sink, skip=lambda i: ()):
+    L, n, cap, H = got.shape[:4]
+    r = H // k.shape[2]
+    for i, t in enumerate(lens):
+        assert (got[:, i, t:] == -7.0).all(), i
+        rows = [a for a in range(t) if a not in set(skip(i))]
+        if not rows:
+            continue
+        for h in range(H):
+            want, slack, size = _reference(q[i, :t, h].double(), k[i, :t, h // r].double(), v[:, i, :t, h // r].double(), window, sink)
+            check_outputs(got[:, i, rows, h], want[:, rows], slack[:, rows], size[:, rows], torch.bfloat16, (i, h))
+
+
+@pytest.mark.parametrize("lens,cap,H,Hk,L,window,sink", [
+    ([1], 1, 1, 1, 1, 1, 0),
+    ([1, 2, 15, 16, 17, 63, 64, 65, 0, 80, 33], 80, 2, 2, 3, 16, 1),
+    ([130, 128, 127, 1], 131, 2, 1, 2, 1, 0),                   # a window of one row
+    ([200, 190], 200, 3, 3, 1, 64, 4),
+    ([200, 190], 200, 4, 2, 2, 65, 5),
+    ([300, 129], 300, 2, 2, 2, 1000000000, 0),                    # causal
+    ([513, 400], 520, 1, 1, 5, 100, 130),                       # more sinks than a tile
+    ([1000], 1000, 2, 1, 1, 257, 3),
+    ([700], 700, 1, 1, 2, 33, 64),
+])
+def test_lengths_windows_sinks(lens, cap, H, Hk, L, window, sink):
+    q, k, v, got = _run(lens, cap, H, Hk, L, window, sink, seed=cap)
+    _check(q, k, v, got, lens, window, sink)
+
+
+def test_equals_the_causal_full_sequence_call():
+    """A window over everything is san_full_block's causal form."""
+    lens, cap, H, L = [150, 77], 150, 2, 2
+    q, k, v, got = _run(lens, cap, H, H, L, cap, 0)
+    dq, dk, dv = (x.to(DEV) for x in (q, k, v))
+    out = torch.full_like(got, -7.0).to(DEV)
+    dl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    B.check(B.san_full_block(B.SAN_BF16, H, L, 1, dq, dk, dv, dl, 2, cap, 0, None, 0, out))
+    torch.cuda.synchronize()
+    a, b = got.double(), out.cpu().double()
+    assert (a - b).norm() <= 2.0 ** -7 * b.norm()               # each within half a step twice
+
+
+def test_host_bound_cuts_longer_sequences():
+    lens, cap = [96, 50], 96
+    q, k, v, got = _run(lens, cap, 2, 2, 2, 20, 2, max_len=64)
+    _check(q, k, v, got, [64, 50], 20, 2)
+
+
+@pytest.mark.parametrize("what", ["nan", "inf"])
+def test_what_a_row_does_not_see_does_not_reach_it(what):
+    """One spoilt key and value row: rows that see it come out as its values demand, the others as if it were not there."""
+    bad, window, sink, lens = 70, 40, 2, [200]
+
+    def spoil(dk, dv):
+        dv[:, 0, bad] = float(what)
+        if what == "nan":
+            dk[0, bad] = float("nan")
+
+    q, k, v, got = _run(lens, 200, 2, 2, 2, window, sink, spoil=spoil)
+    sees = list(range(bad, bad + window))
+    _check(q, k, v, got, lens, window, sink, skip=lambda i: sees)
+    assert not torch.isfinite(got[:, 0, sees]).any()
+
+
+def test_scores_in_the_thousands():
+    lens = [140]
+    q, k, v, got = _run(lens, 140, 1, 1, 1, 50, 4, scale=512.0)
+    _check(q, k, v, got, lens, 50, 4)
+
+
+def test_captured_and_replayed():
+    lens, cap, H = [100, 64], 100, 2
+    gen = torch.Generator().manual_seed(1)
+    mk = lambda *s: randn(gen, *s, dtype=torch.bfloat16)        # noqa: E731
+    k, v = mk(2, cap, H, DH), mk(1, 2, cap, H, DH)
+    dq, dk, dv = torch.zeros(2, cap, H, DH, dtype=torch.bfloat16, device=DEV), k.to(DEV), v.to(DEV)
+    out = torch.full((1, 2, cap, H, DH), -7.0, dtype=torch.bfloat16, device=DEV)
+    dl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    call = lambda: B.check(B.san_window_block(B.SAN_BF16, H, H, 1, 30, 3, dq, dk, dv, dl, 2, cap, 0, out))     # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for _ in range(2):
+        q = mk(2, cap, H, DH)
+        dq.copy_(q)
+        g.replay()
+        torch.cuda.synchronize()
+        _check(q, k, v, out.cpu(), lens, 30, 3)
