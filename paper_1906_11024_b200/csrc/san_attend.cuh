@@ -536,40 +536,52 @@ __global__ void __launch_bounds__(kAtWarps * 32) attend_kernel(const __grid_cons
     attend_finish<T>(p, u, active, wpu, attend_smem, ml, warp, lane);
 }
 
-// Adds up the partial results of a row: 16 threads per (item, head), four outputs each.
-template <typename T>
+// Adds up the partial results of a row and layer: 16 threads for its outputs, four each, times G groups that
+// take every G-th partial result (the loads of a row with many of them are a chain of G times fewer round
+// trips).  grid = (rows / (16 / G), layers).
+template <typename T, int G>
 __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant__ AttendParams p) {
+    __shared__ float4 s_o[G > 1 ? 256 : 1];
+    __shared__ float2 s_ml[G > 1 ? 256 : 1];
     const long long n_rows = (long long)p.n_items * p.H;
-    const long long at = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
-    const int c = threadIdx.x & 15;
-    if (at >= n_rows) return;
-    const int item = (int)(at / p.H);
-    if (!own_ok(p, item)) return;
-    const int g = prefix_of(p, item);
-    if (g >= 0 && !prefix_ok(p, g)) return;
-    const int begin = g >= 0 ? 0 : p.p_splits;          // no prefix in front of this row: its own partial results only
+    const int c = threadIdx.x & 15, grp = threadIdx.x / 16 % G, layer = blockIdx.y;
+    const long long at = (long long)blockIdx.x * (16 / G) + threadIdx.x / (16 * G);
+    bool mine = at < n_rows;
+    int begin = 0;
+    if (mine) {
+        const int item = (int)(at / p.H), g = prefix_of(p, item);
+        mine = own_ok(p, item) && (g < 0 || prefix_ok(p, g));
+        begin = g >= 0 ? 0 : p.p_splits;                // no prefix in front of this row: its own partial results only
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    float m = -INFINITY;
-    for (int s = begin; s < p.slots; ++s) m = fmaxf(m, p.part_ml[s * n_rows + at].x);
-    float l = 0.f;
-    for (int s = begin; s < p.slots; ++s) {
-        const float2 x = p.part_ml[s * n_rows + at];
-        if (x.y != 0.f) l += x.y * (x.x == m ? 1.f : exp2f(x.x - m));
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float2 x, float4 v) {
+        if (x.y == 0.f) return;                         // nothing seen there: its outputs were not written
+        const float m_new = fmaxf(m, x.x);
+        const float a = m == m_new ? 1.f : exp2f(m - m_new), b = x.x == m_new ? 1.f : exp2f(x.x - m_new);
+        l = l * a + x.y * b;
+        o.x = o.x * a + v.x * b; o.y = o.y * a + v.y * b; o.z = o.z * a + v.z * b; o.w = o.w * a + v.w * b;
+        m = m_new;
+    };
+    if (mine) {
+#pragma unroll 4
+        for (int s = begin + grp; s < p.slots; s += G)
+            add(p.part_ml[s * n_rows + at],
+                *reinterpret_cast<const float4*>(p.part_o + (((long long)s * p.n_layers + layer) * n_rows + at) * kDh + c * 4));
     }
+    if constexpr (G > 1) {
+        s_o[threadIdx.x] = o;
+        s_ml[threadIdx.x] = make_float2(m, l);
+        __syncthreads();
+        if (grp != 0) return;
+        for (int k = 1; k < G; ++k) add(s_ml[threadIdx.x + k * 16], s_o[threadIdx.x + k * 16]);
+    }
+    if (!mine) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    for (int y = 0; y < p.n_layers; ++y) {
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int s = begin; s < p.slots; ++s) {
-            const float2 x = p.part_ml[s * n_rows + at];
-            if (x.y == 0.f) continue;
-            const float w = (x.x == m ? 1.f : exp2f(x.x - m)) * inv;
-            const float4 v = *reinterpret_cast<const float4*>(p.part_o + (((long long)s * p.n_layers + y) * n_rows + at) * kDh + c * 4);
-            o.x = fmaf(w, v.x, o.x); o.y = fmaf(w, v.y, o.y); o.z = fmaf(w, v.z, o.z); o.w = fmaf(w, v.w, o.w);
-        }
-        T* dst = reinterpret_cast<T*>(p.out) + ((long long)y * n_rows + at) * kDh + c * 4;
-        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(dst) = o;
-        else *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
-    }
+    T* dst = reinterpret_cast<T*>(p.out) + ((long long)layer * n_rows + at) * kDh + c * 4;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(dst) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    else *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
 }
 
 }  // namespace san

@@ -6,17 +6,19 @@
 // ranked by score / ((5 + length) / 6)^alpha, ties to the lowest (slot, token).
 //
 // The logits are read once and that is what bounds the call; everything else is a few KB:
-//   select_rows_kernel   CTA = (hypothesis, chunk of the vocabulary).  A thread loads its 8 or 32 logits
-//     into registers (all loads in flight at once), keeps their maximum, and adds exp(x - max) over
-//     them in float32 (32 terms at most), the threads' sums in double.  The chunk's best `beam` logits come out without sorting it:
-//     the beam-th largest of the 256 threads' maxima is a lower bound T that at most 32 x beam logits
-//     reach and about beam do; those go to a list in shared memory, and each finds its own place in it
-//     by counting the ones above it.  Keys are (logit, index) pairs and therefore all different, so ties
-//     cost nothing and fall to the lowest index.
-//   select_merge_kernel  CTA = sentence.  Joins the chunks' maxima and sums to the log-sum-exp of each row
-//     (double: scores of different hypotheses are compared with one another), ranks the beam x chunks
+//   select_rows_kernel   CTA = (hypothesis, part of the vocabulary), in steps of 16 KB, the next step's logits on their way
+//     into registers while a step is worked on.  A thread keeps the maximum and the sum of 2^(x log2(e) - M) of
+//     its logits, three instructions a logit (float32, rescaled when the maximum moves; the threads' sums are joined
+//     in double).  The part's best `beam` logits come out without sorting it: the beam-th largest of the 256
+//     threads' maxima in the first step is a lower bound T of the beam-th best logit, which hardly more than
+//     `beam` logits of a step reach; those go to a list in shared memory, T is raised when the list fills up, and
+//     at the end each key finds its own place by counting the ones above it.
+//   select_merge_kernel  CTA = sentence.  Joins the parts' maxima and sums to the log-sum-exp of each row
+//     (double: scores of different hypotheses are compared with one another), ranks the beam x parts
 //     x beam candidates the same way, and carries scores, lengths and token histories over.  It is launched
 //     with programmatic stream serialisation: its CTAs are in place when the last logits arrive.
+// Where more candidates reach the bound than the list holds (rows that are alike nearly everywhere: a mask of
+// the type's lowest value) the best ones are taken one by one, each the largest below the one before.
 // A finished hypothesis, or one without a score, has its logits skipped.
 #pragma once
 
@@ -26,12 +28,14 @@ namespace san {
 
 constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
-constexpr int kSelList = 2048;                 // most candidates that can pass the bound (see below)
+constexpr int kSelWords = 16;                  // 32-bit words of logits per thread and step
+constexpr int kSelList = 1024;                 // keys that may reach the bound between two checks; more: one by one
+constexpr int kSelTight = 64;                  // what the list is cut down to (equal logits aside)
 constexpr int TAG_SELECT = 8;
 
 struct SelectParams {
     const void* logits; long long ld;          // elements between rows
-    int vocab, n_sent, beam, chunks, eos;
+    int vocab, n_sent, beam, chunks, steps, eos;     // steps of a chunk (a part of a row)
     double alpha;
     const float* score; const int* len; const int* done;
     const int* tokens; long long ld_tokens;
@@ -56,6 +60,9 @@ __device__ __forceinline__ unsigned order_f32(float x) {
 __device__ __forceinline__ float unorder_f32(unsigned u) {
     return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
 }
+__device__ __forceinline__ double unorder_f64(unsigned long long u) {
+    return __longlong_as_double((long long)(u >> 63 ? u & ~(1ull << 63) : ~u));
+}
 __device__ __forceinline__ unsigned long long order_f64(double x) {
     const unsigned long long u = (unsigned long long)__double_as_longlong(x + 0.0);
     return u >> 63 ? ~u : u | (1ull << 63);
@@ -65,67 +72,51 @@ __device__ __forceinline__ unsigned long long order_f64(double x) {
 struct Key64 {
     unsigned long long a;
     __device__ __forceinline__ bool over(const Key64& o) const { return a > o.a; }
-    __device__ __forceinline__ bool any() const { return a != 0; }
     __device__ __forceinline__ Key64 swapped(int mask) const { return {__shfl_xor_sync(0xffffffffu, a, mask)}; }
-    __device__ __forceinline__ Key64 from(int lane) const { return {__shfl_sync(0xffffffffu, a, lane)}; }
 };
 struct Key128 {
     unsigned long long a, b;
     __device__ __forceinline__ bool over(const Key128& o) const { return a > o.a || (a == o.a && b > o.b); }
-    __device__ __forceinline__ bool any() const { return a != 0; }
     __device__ __forceinline__ Key128 swapped(int mask) const {
         return {__shfl_xor_sync(0xffffffffu, a, mask), __shfl_xor_sync(0xffffffffu, b, mask)};
     }
-    __device__ __forceinline__ Key128 from(int lane) const {
-        return {__shfl_sync(0xffffffffu, a, lane), __shfl_sync(0xffffffffu, b, lane)};
-    }
 };
+template <typename K> __device__ __forceinline__ K larger(const K& x, const K& y) { return y.over(x) ? y : x; }
 
-template <typename K> __device__ __forceinline__ K keep(const K& mine, const K& other, bool larger) {
-    return other.over(mine) == larger ? other : mine;
-}
-// The warp's 32 keys in descending order over the lanes (bitonic network).
-template <typename K> __device__ __forceinline__ K warp_sort(K k, int lane) {
+// The CTA's largest key, in all threads.  `slots`: kSelWarps keys of shared memory, free again after the next barrier.
+template <typename K> __device__ __forceinline__ K block_largest(K k, K* slots) {
 #pragma unroll
-    for (int size = 2; size <= 32; size <<= 1)
-#pragma unroll
-        for (int step = size >> 1; step > 0; step >>= 1)
-            k = keep(k, k.swapped(step), ((lane & step) == 0) == ((lane & size) == 0));
-    return k;
-}
-// The 32 largest of two descending runs of 32, descending.
-template <typename K> __device__ __forceinline__ K warp_merge(K k, const K& other, int lane) {
-    k = keep(k, other.from(31 - lane), true);
-#pragma unroll
-    for (int step = 16; step > 0; step >>= 1) k = keep(k, k.swapped(step), (lane & step) == 0);
-    return k;
-}
-
-// A lower bound of the CTA's n-th largest key (n <= 32) from one key per thread, the thread's largest; a key
-// that n threads reach.  Up to eight wanted keys the warps' own n-th largest serve: the largest of them is
-// reached by at most n threads of each warp (n * 8 * 32 <= kSelList keys); beyond that the warps' runs
-// are merged and exactly n threads reach the bound.  `runs`: kSelWarps * 32 keys of shared memory.
-template <typename K> __device__ __forceinline__ K nth_bound(K mine, int n, K* runs) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    mine = warp_sort(mine, lane);
-    if (n <= 8) {
-        if (lane == n - 1) runs[warp] = mine;
-        __syncthreads();
-        K best = runs[0];
-#pragma unroll
-        for (int w = 1; w < kSelWarps; ++w) best = keep(best, runs[w], true);
-        return best;
-    }
-    runs[threadIdx.x] = mine;
-    for (int half = kSelWarps / 2; half > 0; half >>= 1) {
-        __syncthreads();
-        if (warp < half) {
-            mine = warp_merge(mine, runs[(warp + half) * 32 + lane], lane);
-            runs[threadIdx.x] = mine;
-        }
-    }
+    for (int o = 16; o > 0; o >>= 1) k = larger(k, k.swapped(o));
     __syncthreads();
-    return runs[n - 1];
+    if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = k;
+    __syncthreads();
+    k = slots[0];
+#pragma unroll
+    for (int w = 1; w < kSelWarps; ++w) k = larger(k, slots[w]);
+    return k;
+}
+
+// From one value per thread, the thread's largest: its warp's largest, and what the warp adds to a lower bound of the
+// CTA's n-th largest value.  Up to n = 8 each warp has at least n groups of lanes of its own, and the largest of the
+// warps' least maxima serves; beyond that all warps together have 16 or 32 groups and the least maximum serves.
+template <typename V> __device__ __forceinline__ void group_bounds(V top, int n, V* warp_top, V* warp_least) {
+    const int groups = n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : n <= 8 ? 8 : n <= 16 ? 2 : 4;     // of this warp
+    const int width = 32 / groups;
+    V least = top;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const V other = __shfl_xor_sync(0xffffffffu, top, o);
+        const V other_least = __shfl_xor_sync(0xffffffffu, least, o);
+        top = other > top ? other : top;
+        least = o < width ? top : other_least < least ? other_least : least;
+    }
+    *warp_top = top; *warp_least = least;
+}
+template <typename V> __device__ __forceinline__ V join_bounds(const V* warp_least, int n) {
+    V t = warp_least[0];
+#pragma unroll
+    for (int w = 1; w < kSelWarps; ++w) t = (warp_least[w] > t) == (n <= 8) ? warp_least[w] : t;
+    return t;
 }
 
 // Writes the n largest of `count` different keys to out(place, key); the list is in shared memory.
@@ -133,106 +124,268 @@ template <typename K, typename F> __device__ __forceinline__ void rank_list(cons
     for (int i = threadIdx.x; i < count; i += kSelThreads) {
         const K mine = list[i];
         int above = 0;
+#pragma unroll 4
         for (int j = 0; j < count; ++j) above += list[j].over(mine) ? 1 : 0;
         if (above < n) out(above, mine);
     }
 }
 
-// 32-bit view of the logits a thread holds.
 template <typename T> __device__ __forceinline__ float as_f32(T x);
 template <> __device__ __forceinline__ float as_f32<float>(float x) { return x; }
 template <> __device__ __forceinline__ float as_f32<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// grid = rows * chunks.  PER logits per thread; VECTOR: every row starts on a 16-byte boundary and a thread
-// holds runs of 16 bytes, else single logits 256 apart (one mapping for all rows of a call, so that equal
-// rows get equal sums whatever their addresses).
-template <typename T, int PER, bool VECTOR>
-__global__ void __launch_bounds__(kSelThreads) select_rows_kernel(const SelectParams p) {
+// The logits of a thread in one step: kSelWords registers, eight logits at a time.
+template <typename T> struct SelectHeld;
+template <> struct SelectHeld<float> {
+    static constexpr int N = kSelWords;
+    float x[kSelWords];
+    __device__ __forceinline__ void set(int i, float v) { x[i] = v; }
+    __device__ __forceinline__ void set16(int j, const uint4& v) {
+        x[4 * j] = __uint_as_float(v.x); x[4 * j + 1] = __uint_as_float(v.y);
+        x[4 * j + 2] = __uint_as_float(v.z); x[4 * j + 3] = __uint_as_float(v.w);
+    }
+    __device__ __forceinline__ float get(int i) const { return x[i]; }
+    __device__ __forceinline__ void mask_nan() {
+#pragma unroll
+        for (int i = 0; i < kSelWords; ++i) x[i] = fmaxf(x[i], -INFINITY);
+    }
+    __device__ __forceinline__ float top8(int g) const {              // the largest of logits 8 g .. 8 g + 7
+        float t = x[8 * g];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) t = fmaxf(t, x[8 * g + i]);
+        return t;
+    }
+};
+template <> struct SelectHeld<__nv_bfloat16> {
+    static constexpr int N = 2 * kSelWords;
+    uint32_t x[kSelWords];                                            // logit 2 i low, 2 i + 1 high
+    __device__ __forceinline__ void set(int i, float v) {
+        const uint32_t b = __float_as_uint(v) >> 16;                  // v is a bf16 number
+        x[i >> 1] = i & 1 ? (x[i >> 1] & 0xffffu) | b << 16 : b;
+    }
+    __device__ __forceinline__ void set16(int j, const uint4& v) { x[4 * j] = v.x; x[4 * j + 1] = v.y; x[4 * j + 2] = v.z; x[4 * j + 3] = v.w; }
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16); }
+    __device__ __forceinline__ static __nv_bfloat162 two(uint32_t w) { return *reinterpret_cast<__nv_bfloat162*>(&w); }
+    __device__ __forceinline__ void mask_nan() {
+#pragma unroll
+        for (int i = 0; i < kSelWords; ++i) {
+            const __nv_bfloat162 v = __hmax2(two(x[i]), two(0xff80ff80u));
+            x[i] = *reinterpret_cast<const uint32_t*>(&v);
+        }
+    }
+    __device__ __forceinline__ float top8(int g) const {
+        const __nv_bfloat162 t = __hmax2(__hmax2(two(x[4 * g]), two(x[4 * g + 1])), __hmax2(two(x[4 * g + 2]), two(x[4 * g + 3])));
+        return fmaxf(__low2float(t), __high2float(t));
+    }
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ unsigned long long select_key(float x, int index) {       // x > -inf
+    return ((unsigned long long)order_f32(x) << 32) | (unsigned)~index;
+}
+
+// One warp: of the `count` keys of the list keeps those that reach a bound raised, from `lo` on, until at most
+// kSelTight do (never fewer than n).  Returns the bound; *left: keys left, packed together.
+__device__ __forceinline__ uint32_t tighten(Key64* list, int count, int n, uint32_t lo, int* left, int lane) {
+    uint32_t hi = 0;
+    for (int j = lane; j < count; j += 32) hi = max(hi, (uint32_t)(list[j].a >> 32));
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    int have = count;
+    while (have > kSelTight && hi > lo) {
+        const uint32_t mid = lo + (hi - lo + 1) / 2;
+        int k = 0;
+        for (int j = lane; j < count; j += 32) k += (uint32_t)(list[j].a >> 32) >= mid ? 1 : 0;
+        k = __reduce_add_sync(0xffffffffu, k);
+        if (k >= n) { lo = mid; have = k; } else hi = mid - 1;
+    }
+    int at = 0;
+    for (int j = 0; j < count; j += 32) {
+        const Key64 k = list[min(j + lane, count - 1)];
+        const unsigned keeps = __ballot_sync(0xffffffffu, j + lane < count && (uint32_t)(k.a >> 32) >= lo);
+        if (keeps >> lane & 1) list[at + __popc(keeps & ((1u << lane) - 1))] = k;      // at or before what was just read
+        at += __popc(keeps);
+        __syncwarp();
+    }
+    *left = at;
+    return lo;
+}
+
+// grid = rows * chunks.  VECTOR: every row starts on a 16-byte boundary and a thread holds runs of 16 bytes, else
+// single logits 256 apart (one mapping for all rows of a call, so that equal rows get equal sums whatever
+// their addresses).
+template <typename T, bool VECTOR>
+__global__ void __launch_bounds__(kSelThreads, 4) select_rows_kernel(const SelectParams p) {
     asm volatile("griddepcontrol.launch_dependents;");
-    constexpr int VEC = VECTOR ? 16 / (int)sizeof(T) : 1;
-    constexpr int NV = PER / VEC;
-    __shared__ unsigned long long s_list[kSelList];
-    __shared__ Key64 s_runs[kSelWarps * 32];
-    __shared__ float s_max[kSelWarps];
+    using Held = SelectHeld<T>;
+    constexpr int N = Held::N, VEC = VECTOR ? 16 / (int)sizeof(T) : 1, STEP = N * kSelThreads;
+    __shared__ Key64 s_list[kSelList];
+    __shared__ Key64 s_slots[kSelWarps];
+    __shared__ float s_max[kSelWarps], s_least[kSelWarps];
     __shared__ double s_sum[kSelWarps];
     __shared__ int s_count;
+    __shared__ uint32_t s_bound;
     const int row = (int)(blockIdx.x / (unsigned)p.chunks), chunk = (int)(blockIdx.x % (unsigned)p.chunks);
     if (select_dead(p.score[row]) || p.done[row] != 0) return;        // uniform over the CTA
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const T* x = static_cast<const T*>(p.logits) + (long long)row * p.ld;
-    const int base = chunk * (PER * kSelThreads);
+    const int begin = min(chunk * p.steps * STEP, p.vocab), end = (int)min((long long)begin + (long long)p.steps * STEP, (long long)p.vocab);
 
-    float v[PER];
+    auto load = [&](Held& v, int base) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int at = base + (j * kSelThreads + (int)threadIdx.x) * VEC;
-        if constexpr (VECTOR) {
-            if (at + VEC <= p.vocab) {
-                unpack16<T>(ld16_stream(x + at), v + j * VEC);
+        for (int j = 0; j < N / VEC; ++j) {
+            const int at = base + (j * kSelThreads + (int)threadIdx.x) * VEC;
+            if constexpr (VECTOR) {
+                if (at + VEC <= end) {
+                    v.set16(j, ld16_stream(x + at));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) v.set(j * VEC + e, at + e < end ? as_f32<T>(x[at + e]) : -INFINITY);
+                }
             } else {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) v[j * VEC + e] = at + e < p.vocab ? as_f32<T>(x[at + e]) : -INFINITY;
+                v.set(j, at < end ? as_f32<T>(x[at]) : -INFINITY);
             }
-        } else {
-            v[j] = at < p.vocab ? as_f32<T>(x[at]) : -INFINITY;
+        }
+    };
+    // Sum of e^(x - top).  With M = fl(c top), c = fl(log2 e): the arguments c x - M are rounded once, relative to
+    // themselves (the product is exact inside the FMA), and M - c top, the same for all, is put right at the
+    // end.  A maximum so large that c x could be infinite, or infinite itself: only logits equal to it count.
+    constexpr float c = 1.4426950408889634f;
+    float top = -INFINITY, m = 0.f, part[4] = {0.f, 0.f, 0.f, 0.f};
+    float bound = -INFINITY;
+    if (threadIdx.x == 0) s_count = 0;
+    Held next;
+    load(next, begin);
+    for (int base = begin; base < end; base += STEP) {
+        Held v = next;
+        if (base + STEP < end) load(next, base + STEP);
+        v.mask_nan();
+        float t8[N / 8], t = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < N / 8; ++g) { t8[g] = v.top8(g); t = fmaxf(t, t8[g]); }
+        if (t > top) {
+            const float m_new = t * c, scale = fabsf(top) < 1e30f && fabsf(t) < 1e30f ? exp2_fast(m - m_new) : 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[i] *= scale;
+            top = t; m = m_new;
+        }
+        if (fabsf(top) < 1e30f) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) part[i & 3] += exp2_fast(fmaf(v.get(i), c, -m));
+        } else if (top > -INFINITY) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) part[i & 3] += v.get(i) == top ? 1.f : 0.f;
+        }
+        if (base == begin) {
+            // The first bound: the beam-th largest of the threads' maxima, or a little below it, found by halving the
+            // way from the groups' bound to the largest; hardly more than `beam` logits of the step reach it.
+            float wtop, least;
+            group_bounds(t, p.beam, &wtop, &least);
+            if (lane == 0) { s_least[warp] = least; s_max[warp] = wtop; }
+            __syncthreads();
+            float most = s_max[0];
+#pragma unroll
+            for (int w = 1; w < kSelWarps; ++w) most = fmaxf(most, s_max[w]);
+            const uint32_t mine = order_f32(t);
+            uint32_t lo = order_f32(join_bounds(s_least, p.beam)), hi = order_f32(most);
+            for (int count = kSelThreads; count > p.beam + p.beam / 4 + 1 && hi > lo; ) {
+                const uint32_t mid = lo + (hi - lo + 1) / 2;
+                const int n = __syncthreads_count(mine >= mid);
+                if (n >= p.beam) { lo = mid; count = n; } else hi = mid - 1;
+            }
+            bound = unorder_f32(lo);
+        }
+        if (t >= bound && t > -INFINITY) {
+#pragma unroll
+            for (int g = 0; g < N / 8; ++g) {
+                if (!(t8[g] >= bound)) continue;
+#pragma unroll
+                for (int i = 8 * g; i < 8 * g + 8; ++i)
+                    if (v.get(i) >= bound && v.get(i) > -INFINITY) {
+                        const int at = atomicAdd(&s_count, 1);
+                        if (at < kSelList) s_list[at].a = select_key(v.get(i), base + ((i / VEC) * kSelThreads + (int)threadIdx.x) * VEC + i % VEC);
+                    }
+            }
+        }
+        __syncthreads();
+        const int count = s_count;
+        if (count > kSelList) {                                       // keys were lost: only the sums go on
+            bound = INFINITY;
+        } else if (count > kSelList / 2 && base + STEP < end) {
+            if (warp == 0) {
+                int left;
+                const uint32_t b = tighten(s_list, count, p.beam, order_f32(bound), &left, lane);
+                if (lane == 0) { s_count = left; s_bound = b; }
+            }
+            __syncthreads();
+            bound = unorder_f32(s_bound);
         }
     }
-    if (threadIdx.x == 0) s_count = 0;
-    auto index_of = [&](int i) { return base + ((i / VEC) * kSelThreads + (int)threadIdx.x) * VEC + i % VEC; };
-    float top = -INFINITY;
-    int top_i = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        v[i] = v[i] == v[i] ? v[i] : -INFINITY;                       // NaN: masked
-        if (v[i] > top) { top = v[i]; top_i = i; }
-    }
-    // exp2 of differences to the thread's own maximum; equal values (two infinities too) differ by nothing
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) sum += v[i] == top ? 1.0f : exp2f((v[i] - top) * 1.4426950408889634f);
-    if (top == -INFINITY) sum = 0.f;
-
+    float sum = (part[0] + part[1]) + (part[2] + part[3]);
+    if (fabsf(top) < 1e30f) sum *= exp2_fast(-fmaf(top, c, -m));      // 2^(M - c top)
     const float wtop = warp_max(top);
-    double wsum = top == wtop ? (double)sum : (double)sum * (double)exp2f((top - wtop) * 1.4426950408889634f);
-    if (wtop == -INFINITY) wsum = 0.0;
+    double wsum = sum == 0.f ? 0.0 : top == wtop ? (double)sum : (double)sum * (double)exp2_fast((top - wtop) * c);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) wsum += __shfl_xor_sync(0xffffffffu, wsum, o);
     if (lane == 0) { s_max[warp] = wtop; s_sum[warp] = wsum; }
-
-    auto key_of = [](float f, int index) -> Key64 {
-        return {f == -INFINITY ? 0ull : ((unsigned long long)order_f32(f) << 32) | (unsigned)~index};
-    };
-    const Key64 mine = key_of(top, index_of(top_i));
-    const Key64 bound = nth_bound<Key64>(mine, p.beam, s_runs);       // s_max, s_sum, s_count: behind its barrier
-    if (mine.any() && !bound.over(mine)) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const Key64 k = key_of(v[i], index_of(i));
-            if (k.any() && !bound.over(k)) s_list[atomicAdd(&s_count, 1)] = k.a;
-        }
-    }
-    char* part = p.ws + (size_t)blockIdx.x * select_part_bytes(p.beam);
-    if (threadIdx.x == 0) {
-        float m = s_max[0];
-        for (int w = 1; w < kSelWarps; ++w) m = fmaxf(m, s_max[w]);
-        double s = 0.0;
-        for (int w = 0; w < kSelWarps; ++w)
-            if (s_max[w] > -INFINITY) s += s_max[w] == m ? s_sum[w] : s_sum[w] * (double)exp2f((s_max[w] - m) * 1.4426950408889634f);
-        *reinterpret_cast<float*>(part) = m;
-        *reinterpret_cast<double*>(part + 8) = s;
+    int count = s_count;
+    if (count > kSelTight && count <= kSelList && warp == 0) {
+        int left;
+        tighten(s_list, count, p.beam, order_f32(bound), &left, lane);
+        if (lane == 0) s_count = left;
     }
     __syncthreads();
-    const int count = s_count;
-    unsigned long long* best = reinterpret_cast<unsigned long long*>(part + 16);
-    rank_list(reinterpret_cast<const Key64*>(s_list), count, p.beam, [&](int place, const Key64& k) { best[place] = k.a; });
-    for (int i = count + (int)threadIdx.x; i < p.beam; i += kSelThreads) best[i] = 0;
+    char* out = p.ws + (size_t)blockIdx.x * select_part_bytes(p.beam);
+    if (threadIdx.x == 0) {
+        float all = s_max[0];
+        for (int w = 1; w < kSelWarps; ++w) all = fmaxf(all, s_max[w]);
+        double s = 0.0;
+        for (int w = 0; w < kSelWarps; ++w)
+            if (s_sum[w] > 0.0) s += s_max[w] == all ? s_sum[w] : s_sum[w] * (double)exp2_fast((s_max[w] - all) * c);
+        *reinterpret_cast<float*>(out) = all;
+        *reinterpret_cast<double*>(out + 8) = s;
+    }
+    Key64* best = reinterpret_cast<Key64*>(out + 16);
+    if (count <= kSelList) {
+        count = s_count;
+        for (int i0 = 0; i0 < count; i0 += kSelThreads / 4) {         // four threads count for one key
+            const int i = i0 + (int)(threadIdx.x >> 2);
+            const Key64 mine = s_list[min(i, count - 1)];
+            int above = 0;
+            for (int j = threadIdx.x & 3; j < count; j += 4) above += s_list[j].over(mine) ? 1 : 0;
+            above += __shfl_xor_sync(0xffffffffu, above, 1);
+            above += __shfl_xor_sync(0xffffffffu, above, 2);
+            if (i < count && above < p.beam && (threadIdx.x & 3) == 0) best[above] = mine;
+        }
+        for (int i = count + (int)threadIdx.x; i < p.beam; i += kSelThreads) best[i] = Key64{0};
+        return;
+    }
+    Key64 last{~0ull};
+    for (int k = 0; k < p.beam; ++k) {                                // read once more for every place (from L2)
+        Key64 mine{0};
+#pragma unroll 8
+        for (int at = begin + (int)threadIdx.x; at < end; at += kSelThreads) {
+            const float f = as_f32<T>(x[at]);
+            const Key64 y{f > -INFINITY ? select_key(f, at) : 0ull};
+            if (last.over(y)) mine = larger(mine, y);
+        }
+        last = block_largest(mine, s_slots);
+        if (threadIdx.x == 0) best[k] = last;
+    }
 }
 
+constexpr int kMergeHeld = 8;                  // candidates per thread and round
+
 // grid = sentences.
-template <typename T>
-__global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const SelectParams p) {
-    __shared__ Key128 s_list[kSelList];        // 32 KB; the histories' columns after the ranking
-    __shared__ Key128 s_runs[kSelWarps * 32];
+static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const SelectParams p) {
+    __shared__ Key128 s_list[kSelThreads * kMergeHeld];      // 32 KB; the histories' columns after the ranking
+    __shared__ Key128 s_best[2][SAN_MAX_BEAM];
+    __shared__ unsigned long long s_least[kSelWarps], s_most[kSelWarps], s_rank[SAN_MAX_BEAM];
+    __shared__ int s_counts[2][kSelWarps];
+    __shared__ Key128 s_slots[kSelWarps];
     __shared__ float s_score[SAN_MAX_BEAM], s_top[SAN_MAX_BEAM];
     __shared__ double s_logsum[SAN_MAX_BEAM], s_norm[SAN_MAX_BEAM];
     __shared__ int s_len[SAN_MAX_BEAM], s_done[SAN_MAX_BEAM], s_parent[SAN_MAX_BEAM], s_token[SAN_MAX_BEAM];
@@ -247,7 +400,7 @@ __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const SelectP
         const int len = p.len[row], done = p.done[row] != 0;
         const bool dead = select_dead(score);
         s_score[b] = dead ? -INFINITY : score; s_len[b] = len; s_done[b] = done;
-        s_norm[b] = pow((5.0 + (double)(len + (done ? 0 : 1))) / 6.0, p.alpha);
+        s_norm[b] = p.alpha == 0.0 ? 1.0 : pow((5.0 + (double)(len + (done ? 0 : 1))) / 6.0, p.alpha);
         s_parent[b] = b; s_token[b] = -1;
         const long long limit = p.tokens ? p.ld_tokens : 0x7ffffffe;
         if (len < 0 || len > limit || (len == limit && !done && !dead)) {
@@ -261,104 +414,128 @@ __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const SelectP
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const size_t part_bytes = select_part_bytes(beam);
     const char* parts = p.ws + (size_t)sent * beam * p.chunks * part_bytes;
+    // candidate i of the sentence: (slot, chunk, place); a finished hypothesis stands at its first one
+    const int per_row = p.chunks * beam, total = beam * per_row;
+    unsigned long long held[kMergeHeld];
+    auto load = [&](int first) {
+#pragma unroll
+        for (int j = 0; j < kMergeHeld; ++j) {
+            const int i = first + j * kSelThreads + (int)threadIdx.x;
+            held[j] = 0;
+            if (i >= total) continue;
+            const int part = i / beam, b = part / p.chunks;           // part: (slot, chunk)
+            if (s_score[b] == -INFINITY) continue;
+            if (s_done[b]) held[j] = i == b * per_row ? 1 : 0;        // itself
+            else held[j] = *reinterpret_cast<const unsigned long long*>(parts + (size_t)part * part_bytes + 16 + 8 * (size_t)(i - part * beam));
+        }
+    };
+    load(0);
     for (int b = warp; b < beam; b += kSelWarps) {                    // log of each row's sum of exponentials
         if (s_done[b] || s_score[b] == -INFINITY) continue;
         const char* part = parts + (size_t)b * p.chunks * part_bytes;
         float m = -INFINITY;
-        for (int c = lane; c < p.chunks; c += 32) m = fmaxf(m, *reinterpret_cast<const float*>(part + c * part_bytes));
-        m = warp_max(m);
         double s = 0.0;
-        for (int c = lane; c < p.chunks; c += 32) {
-            const float mc = *reinterpret_cast<const float*>(part + c * part_bytes);
-            const double sc = *reinterpret_cast<const double*>(part + c * part_bytes + 8);
-            if (mc > -INFINITY) s += mc == m ? sc : sc * exp((double)mc - (double)m);
-        }
+        for (int c0 = 0; c0 < p.chunks; c0 += 32) {
+            const bool have = c0 + lane < p.chunks;
+            const float mc = have ? *reinterpret_cast<const float*>(part + (c0 + lane) * part_bytes) : -INFINITY;
+            const double sc = have ? *reinterpret_cast<const double*>(part + (c0 + lane) * part_bytes + 8) : 0.0;
+            const float m_new = fmaxf(m, warp_max(mc));
+            double t = mc == -INFINITY ? 0.0 : mc == m_new ? sc : sc * exp((double)mc - (double)m_new);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+            s = (m == -INFINITY ? 0.0 : m == m_new ? s : s * exp((double)m - (double)m_new)) + t;
+            m = m_new;
+        }
         if (lane == 0) { s_top[b] = m; s_logsum[b] = log(s); }
     }
     __syncthreads();
-    // candidate i of the sentence: (slot, chunk, place); a finished hypothesis stands at its first one
-    const int per_row = p.chunks * beam, total = beam * per_row;
     auto score_of = [&](int b, float x) {
         const double d = x == s_top[b] ? 0.0 : (double)x - (double)s_top[b];
         return (double)s_score[b] + (d - s_logsum[b]);
     };
-    auto key_at = [&](int i) -> Key128 {
-        const int b = i / per_row, k = i - b * per_row;
-        if (s_score[b] == -INFINITY) return {0, 0};
-        double rank;
-        int token;
-        if (s_done[b]) {
-            if (k != 0) return {0, 0};
-            token = max(p.eos, 0);
-            rank = (double)s_score[b] / s_norm[b];
+    int kept = 0;                                                     // candidates kept from the rounds before
+    for (int first = 0, round = 0; first < total; first += kSelThreads * kMergeHeld, round ^= 1) {
+        if (first > 0) load(first);
+        Key128 key[kMergeHeld];
+        unsigned long long top = 0;
+#pragma unroll
+        for (int j = 0; j < kMergeHeld; ++j) {
+            key[j] = Key128{0, 0};
+            if (held[j] == 0) continue;
+            const int b = (first + j * kSelThreads + (int)threadIdx.x) / per_row;
+            const int token = s_done[b] ? max(p.eos, 0) : (int)~(unsigned)held[j];
+            const double rank = (s_done[b] ? (double)s_score[b] : score_of(b, unorder_f32((unsigned)(held[j] >> 32)))) / s_norm[b];
+            if (rank > -INFINITY) key[j] = Key128{order_f64(rank), ~(((unsigned long long)(unsigned)b << 32) | (unsigned)token)};
+            top = key[j].a > top ? key[j].a : top;
+        }
+        unsigned long long warp_top, least;
+        group_bounds(top, beam, &warp_top, &least);
+        if (lane == 0) { s_least[warp] = least; s_most[warp] = warp_top; }
+        __syncthreads();
+        unsigned long long bound = join_bounds(s_least, beam), most = s_most[0];
+#pragma unroll
+        for (int w = 1; w < kSelWarps; ++w) most = s_most[w] > most ? s_most[w] : most;
+        if (kept == beam && s_best[round][beam - 1].a > bound) bound = s_best[round][beam - 1].a;
+        if (bound == 0) bound = 1;
+        // Candidates are not mixed over the threads as logits are (hypotheses differ in score, places in rank), so the
+        // bound may be low: halve the way to the largest until at most 128 reach it, never fewer than `beam` of this round
+        // unless the bound is that of the rounds before.
+        int count = 0;
+        for (int step = 0; step < 64; ++step) {
+            const unsigned long long mid = step == 0 ? bound : bound + (most - bound + 1) / 2;
+            int n = 0;
+#pragma unroll
+            for (int j = 0; j < kMergeHeld; ++j) n += key[j].a >= mid ? 1 : 0;
+            n = __reduce_add_sync(0xffffffffu, n);
+            if (lane == 0) s_counts[step & 1][warp] = n;
+            __syncthreads();
+            n = 0;
+#pragma unroll
+            for (int w = 0; w < kSelWarps; ++w) n += s_counts[step & 1][w];
+            if (step == 0 || n >= beam) { bound = mid; count = n; }
+            else most = mid - 1;                                      // fewer than `beam` reach mid
+            if (count <= 128 || most <= bound) break;
+        }
+#pragma unroll
+        for (int j = 0; j < kMergeHeld; ++j)
+            if (key[j].a >= bound) s_list[atomicAdd(&s_count, 1)] = key[j];
+        __syncthreads();
+        const bool long_list = count > 256;                           // counting would take longer than picking them out
+        if (!long_list && (int)threadIdx.x < kept) s_list[count + threadIdx.x] = s_best[round][threadIdx.x];
+        __syncthreads();
+        if (threadIdx.x == 0) s_count = 0;
+        if (!long_list) {
+            count += kept;
+            rank_list(s_list, count, beam, [&](int place, const Key128& k) { s_best[round ^ 1][place] = k; });
+            kept = min(count, beam);
         } else {
-            const int c = k / beam;
-            const unsigned long long key = *reinterpret_cast<const unsigned long long*>(parts + ((size_t)b * p.chunks + c) * part_bytes + 16 + 8 * (size_t)(k - c * beam));
-            if (key == 0) return {0, 0};
-            token = (int)~(unsigned)key;
-            rank = score_of(b, unorder_f32((unsigned)(key >> 32))) / s_norm[b];
-        }
-        if (!(rank > -INFINITY)) return {0, 0};
-        return {order_f64(rank), ~(((unsigned long long)(unsigned)b << 32) | (unsigned)token)};
-    };
-    int count;
-    if (total <= kSelThreads) {                                       // all of them fit the list
-        if ((int)threadIdx.x < total) {
-            const Key128 k = key_at(threadIdx.x);
-            if (k.any()) s_list[atomicAdd(&s_count, 1)] = k;
-        }
-    } else {
-        Key128 mine{0, 0};
-        for (int i = threadIdx.x; i < total; i += kSelThreads) mine = keep(mine, key_at(i), true);
-        const Key128 bound = nth_bound<Key128>(mine, beam, s_runs);
-        if (mine.any() && !bound.over(mine))
-            for (int i = threadIdx.x; i < total; i += kSelThreads) {
-                const Key128 k = key_at(i);
-                if (k.any() && !bound.over(k)) {
-                    const int at = atomicAdd(&s_count, 1);
-                    if (at < kSelList) s_list[at] = k;
-                }
+            Key128 last{~0ull, ~0ull};
+            for (int k = 0; k < beam; ++k) {
+                Key128 mine{0, 0};
+#pragma unroll
+                for (int j = 0; j < kMergeHeld; ++j)
+                    if (last.over(key[j])) mine = larger(mine, key[j]);
+                if ((int)threadIdx.x < kept && last.over(s_best[round][threadIdx.x])) mine = larger(mine, s_best[round][threadIdx.x]);
+                last = block_largest(mine, s_slots);
+                if (threadIdx.x == 0) s_best[round ^ 1][k] = last;    // more than 256 candidates: there are `beam`
             }
-    }
-    __syncthreads();
-    count = s_count;
-    if (count > kSelList) {
-        // more candidates at or above the bound than the list holds (a few threads hold most of the best
-        // ones): one after the other, the largest below the last
-        Key128 last{~0ull, ~0ull};
-        count = 0;
-        for (int k = 0; k < beam; ++k) {
-            Key128 mine{0, 0};
-            for (int i = threadIdx.x; i < total; i += kSelThreads) {
-                const Key128 c = key_at(i);
-                if (last.over(c)) mine = keep(mine, c, true);
-            }
-            mine = warp_sort(mine, lane);
-            __syncthreads();
-            if (lane == 0) s_runs[warp] = mine;
-            __syncthreads();
-            last = s_runs[0];
-            for (int w = 1; w < kSelWarps; ++w) last = keep(last, s_runs[w], true);
-            if (!last.any()) break;
-            if (threadIdx.x == 0) s_list[k] = last;
-            count = k + 1;
+            kept = beam;
         }
         __syncthreads();
+        if ((int)threadIdx.x < kept) {
+            const unsigned long long id = ~s_best[round ^ 1][threadIdx.x].b;
+            s_parent[threadIdx.x] = (int)(id >> 32);
+            s_token[threadIdx.x] = (int)(unsigned)id;
+            s_rank[threadIdx.x] = s_best[round ^ 1][threadIdx.x].a;
+        }
     }
-    rank_list(s_list, count, beam, [&](int place, const Key128& k) {
-        const unsigned long long id = ~k.b;
-        s_parent[place] = (int)(id >> 32);
-        s_token[place] = (int)(unsigned)id;
-    });
     __syncthreads();
     if (threadIdx.x < beam) {
         const int s = threadIdx.x, b = s_parent[s], row = sent * beam + s;
         const bool none = s_token[s] < 0, keeps = none || s_done[b];
         const int token = none ? max(p.eos, 0) : s_token[s];
         float score = none ? -INFINITY : s_score[b];
-        if (!keeps) score = (float)score_of(b, as_f32<T>(static_cast<const T*>(p.logits)[(long long)(sent * beam + b) * p.ld + token]));
+        if (!keeps) score = (float)(unorder_f64(s_rank[s]) * s_norm[b]);     // the candidate's score again, within 2^-53
         p.score_out[row] = score;
         p.len_out[row] = s_len[b] + (keeps ? 0 : 1);
         p.done_out[row] = keeps || token == p.eos;

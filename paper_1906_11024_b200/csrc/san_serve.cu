@@ -28,9 +28,9 @@ int32_t opt_in(const void* fn, int bytes) {
 // Launches `fn` so that its CTAs may be set up while the kernel before it on the stream still runs
 // (it waits with griddepcontrol.wait before it reads what that one wrote).
 template <typename P>
-int32_t launch_after(void (*fn)(P), unsigned grid, unsigned block, cudaStream_t st, const P& p) {
+int32_t launch_after(void (*fn)(P), dim3 grid, unsigned block, cudaStream_t st, const P& p) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(block); cfg.stream = st;
+    cfg.gridDim = grid; cfg.blockDim = dim3(block); cfg.stream = st;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
@@ -39,25 +39,30 @@ int32_t launch_after(void (*fn)(P), unsigned grid, unsigned block, cudaStream_t 
 }
 
 // ------------------------------------------------------------------------------- beam selection
-// Logits per thread: 32 fill the registers and keep the parts few; 8 where a call has so few rows that
-// its chunks would leave SMs without one.
-int select_per_thread(long long rows, int vocab) { return rows * div_up(vocab, 32 * kSelThreads) < kSms ? 8 : 32; }
-int select_chunks(long long rows, int vocab) { return (int)div_up(vocab, select_per_thread(rows, vocab) * kSelThreads); }
+// Parts of a row: enough that the SMs (four CTAs each) have four waves of them, each of whole steps.
+struct SelectCut { int chunks, steps; };
+SelectCut select_cut(int32_t dtype, long long rows, int vocab) {
+    const int step = kSelWords * (dtype == SAN_BF16 ? 2 : 1) * kSelThreads;
+    const long long all = div_up(vocab, step);
+    const long long want = std::min(all, std::max<long long>(1, div_up(16 * kSms, std::max<long long>(rows, 1))));
+    const long long steps = div_up(all, want);
+    return {(int)div_up(all, steps), (int)steps};
+}
 
 int32_t select_shape(int32_t n_sent, int32_t beam, int32_t vocab) {
     if (n_sent < 0 || beam < 1 || beam > SAN_MAX_BEAM || vocab < 1 || vocab > (1 << 28)) return SAN_ERR_SHAPE;
     if ((long long)n_sent * beam > (1 << 24)) return SAN_ERR_SHAPE;
-    if ((long long)n_sent * beam * select_chunks((long long)n_sent * beam, vocab) > 0x7fffffffLL) return SAN_ERR_SHAPE;
+    if ((long long)n_sent * beam * div_up(vocab, kSelWords * kSelThreads) > 0x7fffffffLL) return SAN_ERR_SHAPE;
     return SAN_OK;
 }
 
-template <typename T, int PER>
+template <typename T>
 int32_t launch_select(const SelectParams& p, bool vector, cudaStream_t st) {
     const unsigned grid = (unsigned)((long long)p.n_sent * p.beam * p.chunks);
-    if (vector) select_rows_kernel<T, PER, true><<<grid, kSelThreads, 0, st>>>(p);
-    else select_rows_kernel<T, PER, false><<<grid, kSelThreads, 0, st>>>(p);
+    if (vector) select_rows_kernel<T, true><<<grid, kSelThreads, 0, st>>>(p);
+    else select_rows_kernel<T, false><<<grid, kSelThreads, 0, st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
-    return launch_after(&select_merge_kernel<T>, (unsigned)p.n_sent, kSelThreads, st, p);
+    return launch_after(&select_merge_kernel, dim3((unsigned)p.n_sent), kSelThreads, st, p);
 }
 
 // ------------------------------------------------------------------------------- step attention
@@ -137,7 +142,7 @@ int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int wi
         out->bytes = out->ml_bytes + p.slots * rows * r->n_layers * kDh * sizeof(float);
     }
     out->ctas = p.p_ctas + div_up(p.o_units, kAtWarps / p.o_wpu);
-    if (out->ctas > 0x7fffffffLL || div_up((long long)rows, 16) > 0x7fffffffLL) return SAN_ERR_SHAPE;
+    if (out->ctas > 0x7fffffffLL || (long long)rows > 0x7fffffffLL) return SAN_ERR_SHAPE;
     p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)kDh));
     return SAN_OK;
 }
@@ -151,7 +156,10 @@ int32_t launch_attend_as(const AttendPlan& a, cudaStream_t st) {
     if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
     if (a.p.slots == 1) return SAN_OK;
     const long long rows = (long long)a.p.n_items * a.p.H;
-    return launch_after(&attend_join_kernel<T>, (unsigned)div_up(rows, 16), 256, st, a.p);
+    const int groups = a.p.slots <= 3 ? 1 : a.p.slots <= 12 ? 4 : 16;
+    const dim3 grid((unsigned)div_up(rows, 16 / groups), (unsigned)a.p.n_layers);
+    return launch_after(groups == 1 ? &attend_join_kernel<T, 1> : groups == 4 ? &attend_join_kernel<T, 4> : &attend_join_kernel<T, 16>,
+                        grid, 256, st, a.p);
 }
 template <typename T>
 int32_t launch_attend(const AttendPlan& a, cudaStream_t st) {
@@ -200,7 +208,8 @@ int32_t san_beam_select_bytes(int32_t n_sent, int32_t beam, int32_t vocab, size_
     const int32_t rc = select_shape(n_sent, beam, vocab);
     if (rc != SAN_OK) return rc;
     const long long rows = (long long)n_sent * beam;
-    *workspace_bytes = (size_t)rows * select_chunks(rows, vocab) * select_part_bytes(beam);
+    const int chunks = std::max(select_cut(SAN_F32, rows, vocab).chunks, select_cut(SAN_BF16, rows, vocab).chunks);
+    *workspace_bytes = (size_t)rows * chunks * select_part_bytes(beam);
     return SAN_OK;
 }
 
@@ -223,15 +232,15 @@ int32_t san_beam_select(const san_select_args* a, void* stream) {
     std::memset(&p, 0, sizeof(p));
     const long long rows = (long long)a->n_sent * a->beam;
     p.logits = a->d_logits; p.ld = a->ld_logits; p.vocab = a->vocab; p.n_sent = a->n_sent; p.beam = a->beam;
-    p.chunks = select_chunks(rows, a->vocab); p.eos = a->eos; p.alpha = (double)a->alpha;
+    const SelectCut cut = select_cut(a->dtype, rows, a->vocab);
+    p.chunks = cut.chunks; p.steps = cut.steps;
+    p.eos = a->eos; p.alpha = (double)a->alpha;
     p.score = a->d_score; p.len = a->d_len; p.done = a->d_done; p.tokens = a->d_tokens; p.ld_tokens = a->ld_tokens;
     p.score_out = a->d_score_out; p.len_out = a->d_len_out; p.done_out = a->d_done_out; p.tokens_out = a->d_tokens_out;
     p.parent = a->d_parent; p.next = a->d_next; p.ws = static_cast<char*>(a->d_workspace); p.status = a->d_status;
     const bool vector = aligned(a->d_logits, 16) && a->ld_logits * (int64_t)e % 16 == 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool few = select_per_thread(rows, a->vocab) == 8;
-    if (a->dtype == SAN_F32) return few ? launch_select<float, 8>(p, vector, st) : launch_select<float, 32>(p, vector, st);
-    return few ? launch_select<__nv_bfloat16, 8>(p, vector, st) : launch_select<__nv_bfloat16, 32>(p, vector, st);
+    return a->dtype == SAN_F32 ? launch_select<float>(p, vector, st) : launch_select<__nv_bfloat16>(p, vector, st);
 }
 
 int32_t san_cache_planes(const san_ctx* ctx, int32_t kind, int32_t block, void** d_k, void** d_v, int64_t* v_stride) {
