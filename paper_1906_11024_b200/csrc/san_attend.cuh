@@ -61,6 +61,7 @@ struct AttendParams {
     int p_units, p_row_tiles, p_splits, p_span, p_wpu;          // units, runs of p_span tiles, warps per unit
     int o_units, o_row_tiles, o_splits, o_span, o_wpu;
     int p_ctas;                             // CTAs of the prefix units; those of the own rows follow
+    int t_lg, t_n_lg;                       // layers per unit of the tensor-core tiles (0: the prefixes are not theirs)
     int slots;                              // partial results per row; 1: units write the outputs
     float* part_o;                          // [slot][layer][item * H + head][64]
     float2* part_ml;                        // [slot][item * H + head]
@@ -86,6 +87,11 @@ __device__ __forceinline__ int prefix_of(const AttendParams& p, int item) {
 __device__ __forceinline__ bool prefix_ok(const AttendParams& p, int g) {
     const int a = p.first[g], b = p.first[g + 1], len = p.plens[g];
     return a >= 0 && b >= a && b <= p.n_items && b - a <= p.max_group && len >= 0 && len <= p.max_prefix;
+}
+__device__ __forceinline__ void prefix_report(const AttendParams& p, int g) {
+    const int count = p.first[g + 1] - p.first[g];
+    const bool by_len = p.plens[g] < 0 || p.plens[g] > p.max_prefix;
+    attend_error(p.status, TAG_PREFIX, g, by_len ? p.plens[g] : count, by_len ? p.max_prefix : p.max_group);
 }
 __device__ __forceinline__ bool own_ok(const AttendParams& p, int item) {
     const int id = p.ids[item], len = p.lens[item];
@@ -461,11 +467,7 @@ __device__ __forceinline__ bool attend_unit(const AttendParams& p, bool prefix, 
     if (prefix) {
         const int tile = index % p.p_row_tiles, g = index / p.p_row_tiles;
         if (!prefix_ok(p, g)) {
-            if (reporter && tile == 0 && split == 0 && hk == 0 && lg == 0) {
-                const int count = p.first[g + 1] - p.first[g];
-                const bool by_len = p.plens[g] < 0 || p.plens[g] > p.max_prefix;
-                attend_error(p.status, TAG_PREFIX, g, by_len ? p.plens[g] : count, by_len ? p.max_prefix : p.max_group);
-            }
+            if (reporter && tile == 0 && split == 0 && hk == 0 && lg == 0) prefix_report(p, g);
             return false;
         }
         const int rows = (p.first[g + 1] - p.first[g]) * p.group;

@@ -10,11 +10,13 @@
 #include "san_select.cuh"
 #include "san_attend.cuh"
 #include "san_window.cuh"
+#include "san_tile.cuh"
 
 using namespace san;
 
 namespace {
 
+constexpr int kTileRows = 32;               // query rows behind a prefix from which on it goes to the tensor-core tiles
 constexpr int kSms = 148;                   // the cuts are made for this GPU; any other number of SMs works
 inline long long div_up(long long a, long long b) { return (a + b - 1) / b; }
 inline int32_t cuda_status(cudaError_t e) { return e == cudaSuccess ? SAN_OK : SAN_ERR_CUDA; }
@@ -102,7 +104,7 @@ void cut_runs(long long units, int bound, int* wpu, int* splits, int* span) {
     *splits = (int)div_up(tiles, *span);
 }
 
-struct AttendPlan { AttendParams p; size_t ml_bytes, bytes; long long ctas; };
+struct AttendPlan { AttendParams p; size_t ml_bytes, bytes; long long ctas, tiles; };
 
 // Everything but the addresses.
 int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int window, int n_sink, AttendPlan* out) {
@@ -122,6 +124,22 @@ int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int wi
         p.n_prefix = x->n_prefix; p.pcap = x->cap_len; p.pv_stride = x->v_stride * e;
         p.max_prefix = x->max_len ? x->max_len : x->cap_len;
         p.max_group = x->max_group ? x->max_group : std::max(1, r->n_items);
+        const long long rows = (long long)p.max_group * p.group;
+        if (r->dtype == SAN_BF16 && rows > kTileRows) {
+            p.t_n_lg = (int)div_up(r->n_layers, kTileMaxLayers);
+            p.t_lg = (int)div_up(r->n_layers, p.t_n_lg);
+            p.t_n_lg = (int)div_up(r->n_layers, p.t_lg);
+            p.p_row_tiles = (int)div_up(rows, kTileQ);
+            // runs of chunks: as many as fill the SMs' two CTAs once, of four chunks or more
+            const long long units = (long long)p.n_prefix * p.p_row_tiles * p.Hk * p.t_n_lg, chunks = div_up(p.max_prefix, kTileK);
+            const long long want = std::max<long long>(1, std::min<long long>(2 * kSms / std::max<long long>(units, 1), div_up(chunks, 4)));
+            p.p_span = (int)div_up(chunks, want);
+            p.p_splits = (int)div_up(chunks, p.p_span);
+            out->tiles = units * p.p_splits;
+            if (out->tiles > 0x7fffffffLL) return SAN_ERR_SHAPE;
+        }
+    }
+    if (p.n_prefix > 0 && p.t_lg == 0) {
         p.p_row_tiles = (int)div_up((long long)p.max_group * p.group, R);
         const long long units = (long long)p.n_prefix * p.p_row_tiles * p.Hk * p.n_lg;
         cut_runs(units, p.max_prefix, &p.p_wpu, &p.p_splits, &p.p_span);
@@ -161,8 +179,22 @@ int32_t launch_attend_as(const AttendPlan& a, cudaStream_t st) {
     return launch_after(groups == 1 ? &attend_join_kernel<T, 1> : groups == 4 ? &attend_join_kernel<T, 4> : &attend_join_kernel<T, 16>,
                         grid, 256, st, a.p);
 }
+template <class Mode, int LG, class P>
+int32_t launch_tiles(const P& p, dim3 grid, cudaStream_t st) {
+    constexpr int smem = tile_smem_bytes(LG);
+    const int32_t rc = opt_in((const void*)tile_kernel<Mode, LG, P>, smem);
+    if (rc != SAN_OK) return rc;
+    tile_kernel<Mode, LG, P><<<grid, kTileThreads, smem, st>>>(p);
+    return cuda_status(cudaGetLastError());
+}
+
 template <typename T>
 int32_t launch_attend(const AttendPlan& a, cudaStream_t st) {
+    if (a.tiles > 0) {
+        const dim3 grid((unsigned)a.tiles);
+        const int32_t rc = a.p.t_lg == 1 ? launch_tiles<TilePrefix, 1>(a.p, grid, st) : launch_tiles<TilePrefix, 2>(a.p, grid, st);
+        if (rc != SAN_OK) return rc;
+    }
     return a.p.lg == 1 ? launch_attend_as<T, 1>(a, st) : a.p.lg == 2 ? launch_attend_as<T, 2>(a, st) : launch_attend_as<T, 4>(a, st);
 }
 
@@ -320,6 +352,11 @@ int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int
     p.n_lg = (int)div_up(n_layers, p.lg);
     p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)kDh));
     if ((long long)n_seq * p.n_lg > 65535) return SAN_ERR_SHAPE;
+    if (max_len >= kTileQ) {
+        const dim3 tiles((unsigned)div_up(max_len, kTileQ), (unsigned)n_heads, (unsigned)(n_seq * p.n_lg));
+        cudaStream_t st = static_cast<cudaStream_t>(stream);
+        return p.lg == 1 ? launch_tiles<TileWindow, 1>(p, tiles, st) : launch_tiles<TileWindow, 2>(p, tiles, st);
+    }
     const dim3 grid((unsigned)div_up(max_len, kWinQ), (unsigned)n_heads, (unsigned)(n_seq * p.n_lg));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return p.lg == 1 ? launch_window<1>(p, grid, st) : launch_window<2>(p, grid, st);

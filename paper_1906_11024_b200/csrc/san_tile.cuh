@@ -1,0 +1,440 @@
+// Attention of 128 query rows at a time on the fifth-generation tensor cores: long windowed prompts
+// (san_window_block) and prefixes with many rows behind them (san_prefix_attn).  S = Softmax(q.K^T / 8) over the
+// keys that a row sees, once per block (Eq. 1, Eq. 3), O_l = S.V_l for each layer (Eq. 2, Eq. 4), in one pass with a
+// running maximum.
+//
+// CTA = 128 query rows x (key head, up to kTileMaxLayers layers, a run of keys).  Keys come in chunks of 64; per chunk one
+// tcgen05.mma chain writes the scores (M 128, N 64, K 64) into one of two score buffers in tensor memory, and
+// one adds weights x values (N = 64 x layers) to the outputs, which stay in tensor memory.  Roles:
+//   warps 0-3  softmax: thread = query row = tensor-memory lane, so maxima and sums need no shuffles.  Weights go to
+//              shared memory in bf16 as the A operand of the second product.  The maximum that the weights are
+//              taken against moves only when a row's own has grown by more than 2^8, since then the
+//              outputs have to be read, scaled and written back; the sum uses the same one, so nothing is lost.
+//   warps 4-6  copies: 16-byte cp.async into operand tiles (rows of 128 bytes, chunks XOR-swizzled by row & 7, what
+//              the matrix descriptors name), keys up to three chunks ahead, values two; rows past the end are zeros.
+//   warp 7     one thread issues the MMAs: scores of chunk t + 1 before outputs of chunk t, so that the tensor cores
+//              work on them while the softmax warps work on chunk t.
+// What bounds it: the exponentials, 64 per row and chunk at 16 per clock and SM (512 clocks a chunk against 384
+// of tensor core with two layers); two CTAs share an SM (up to two layers each) and fill each other's waits.
+// Every wait is bounded: one that runs out raises a flag that ends the CTA's other waits, the CTA frees its tensor
+// memory and leaves its rows unwritten (reported where there is a status word).
+#pragma once
+
+#include "san_attend.cuh"
+#include "san_window.cuh"
+
+namespace san {
+
+constexpr int kTileQ = 128, kTileK = 64, kTileThreads = 256, kTileLoaders = 96;
+constexpr int kTileKSlots = 3, kTileMaxLayers = 2;
+constexpr int TAG_TILE = 11;
+__host__ __device__ constexpr int tile_smem_bytes(int layers) {
+    return 1024 + kTileQ * 128 * 3 + (kTileKSlots + 2 * layers) * kTileK * 128;
+}
+
+__device__ __forceinline__ uint32_t tile_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void tile_bar_init(uint64_t* bar, int count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(tile_u32(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void tile_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tile_u32(bar)) : "memory");
+}
+// Bounded wait for the phase of that parity: false once it has lasted about a second or another wait has given up.
+__device__ __forceinline__ bool tile_wait(uint64_t* bar, uint32_t parity, volatile int* dead) {
+    const uint32_t addr = tile_u32(bar);
+    uint32_t ok;
+    long long t0 = 0;
+    for (uint32_t turn = 0;; ++turn) {
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(ok) : "r"(addr), "r"(parity), "r"(1000000u) : "memory");
+        if (ok) return true;
+        if ((turn & 63u) != 63u) continue;
+        if (*dead) return false;
+        const long long now = clock64();
+        if (t0 == 0) t0 = now;
+        else if (now - t0 > 2000000000LL) { *dead = 1; return false; }
+    }
+}
+// Shared-memory matrix descriptor: 128-byte swizzle, groups of 8 rows 1024 bytes apart; `lead`: bytes between the 64-element
+// column blocks of an MN-major operand wider than 64.
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr, uint32_t lead = 16) {
+    return (uint64_t)((addr >> 4) & 0x3fffu) | ((uint64_t)((lead >> 4) & 0x3fffu) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+// Instruction descriptor: float32 accumulator, bf16 operands, M 128, N n; b_mn: B is MN-major.
+__device__ __forceinline__ uint32_t tile_idesc(bool b_mn, int n) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+__device__ __forceinline__ void tile_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u) : "memory");
+}
+__device__ __forceinline__ void tile_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(tile_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tile_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tile_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tile_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// 32 columns of this thread's lane, without the wait.
+__device__ __forceinline__ void tile_ld32(uint32_t addr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+                   "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tile_ld16(uint32_t addr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tile_st16(uint32_t addr, const float* v) {
+    const uint32_t* r = reinterpret_cast<const uint32_t*>(v);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+                 :: "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                    "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tile_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tile_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// What a CTA works on.  Visible keys are numbered 0 .. end - 1: the first ns of them are rows 0.., the others rows lo...
+struct TileWork {
+    const char* k; const char* v;
+    long long row_bytes, v_stride;          // bytes between rows, between layers
+    int ns, lo, begin, end;
+    int rows, layer0, layers;
+};
+
+// ---- windowed prompts: grid (query tiles, heads, sequences x layer groups)
+struct TileWindow {
+    const WindowParams& p;
+    int seq, head, a0, len;
+    __device__ __forceinline__ bool work(TileWork* w) {
+        head = blockIdx.y; seq = blockIdx.z / p.n_lg;
+        w->layer0 = blockIdx.z % p.n_lg * p.lg;
+        w->layers = min(p.lg, p.n_layers - w->layer0);
+        len = max(0, min(p.lens[seq], p.max_len));
+        a0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kTileQ;
+        if (a0 >= len) return false;
+        w->rows = min(kTileQ, len - a0);
+        w->lo = max(0, a0 - p.window + 1);
+        w->ns = min(p.n_sink, w->lo);
+        w->begin = 0;
+        w->end = w->ns + a0 + w->rows - w->lo;
+        const long long at = ((long long)seq * p.cap * p.Hk + head / p.group) * 128;
+        w->row_bytes = (long long)p.Hk * 128;
+        w->v_stride = p.v_layer * 2;
+        w->k = reinterpret_cast<const char*>(p.k) + at;
+        w->v = reinterpret_cast<const char*>(p.v) + at + w->layer0 * w->v_stride;
+        return true;
+    }
+    __device__ __forceinline__ const uint4* query(int i) const {
+        return reinterpret_cast<const uint4*>(p.q + (((long long)seq * p.cap + a0 + i) * p.H + head) * kDh);
+    }
+    // Of chunk [c0, c0 + 64) of the visible keys, those that row i sees: bit j for number c0 + j.
+    __device__ __forceinline__ bool all_seen(const TileWork& w, int c0) const {
+        return c0 >= w.ns && c0 + kTileK <= w.end && w.lo + c0 - w.ns + kTileK - 1 <= a0 && w.lo + c0 - w.ns > a0 + kTileQ - 1 - p.window;
+    }
+    __device__ __forceinline__ unsigned long long seen(const TileWork& w, int c0, int i) const {
+        auto below = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };      // bits 0 .. n - 1
+        const int a = a0 + i, self = w.ns + a - w.lo;                   // the row's own number
+        const int sinks = w.ns + max(0, p.n_sink - w.lo);               // numbers below it are sinks (or behind the row)
+        const unsigned long long recent = ~below(w.ns + max(a - p.window + 1, w.lo) - w.lo - c0);
+        return (recent | below(sinks - c0)) & below(min(self + 1, w.end) - c0);
+    }
+    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, int i, float m, float l, bool ok) const {
+        const bool mine = ok && i < w.rows;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        bool odd = false;
+#pragma unroll
+        for (int y = 0; y < LG; ++y) {
+            if (y >= w.layers) break;
+            uint4* dst = reinterpret_cast<uint4*>(p.out + (w.layer0 + y) * p.out_layer + (((long long)seq * p.cap + a0 + i) * p.H + head) * kDh);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float o[32];
+                __syncwarp();
+                tile_ld32(t_out + y * 64 + h * 32, o);
+                tile_wait_ld();
+#pragma unroll
+                for (int c = 0; c < 32; ++c) { o[c] *= inv; odd |= o[c] != o[c]; }
+                if (mine)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        dst[h * 4 + c] = make_uint4(pack_bf16(o[8 * c], o[8 * c + 1]), pack_bf16(o[8 * c + 2], o[8 * c + 3]),
+                                                    pack_bf16(o[8 * c + 4], o[8 * c + 5]), pack_bf16(o[8 * c + 6], o[8 * c + 7]));
+            }
+        }
+        unsigned again = __ballot_sync(0xffffffffu, odd && mine);       // see san_window.cuh
+        while (again) {
+            const int r = __ffs(again) - 1;
+            again &= again - 1;
+            for (int y = 0; y < w.layers; ++y) window_row_again(p, seq, head, w.layer0 + y, a0 + (i & ~31) + r, threadIdx.x & 31);
+        }
+    }
+    __device__ __forceinline__ void failed() const {}
+};
+
+// ---- shared prefixes: units as in attend_unit, 128 query rows and runs of p_span chunks
+struct TilePrefix {
+    const AttendParams& p;
+    int g, hk, row0, slot;
+    __device__ __forceinline__ bool work(TileWork* w) {
+        int index = blockIdx.x;
+        const int lg = index % p.t_n_lg; index /= p.t_n_lg;
+        const int split = index % p.p_splits; index /= p.p_splits;
+        hk = index % p.Hk; index /= p.Hk;
+        const int tile = index % p.p_row_tiles;
+        g = index / p.p_row_tiles;
+        if (!prefix_ok(p, g)) {
+            if (threadIdx.x == 0 && tile == 0 && split == 0 && hk == 0 && lg == 0) prefix_report(p, g);
+            return false;
+        }
+        row0 = tile * kTileQ;
+        w->rows = min(kTileQ, (p.first[g + 1] - p.first[g]) * p.group - row0);
+        if (w->rows <= 0) return false;
+        w->layer0 = lg * p.t_lg;
+        w->layers = min(p.t_lg, p.n_layers - w->layer0);
+        w->ns = 0; w->lo = 0;
+        w->begin = min(split * p.p_span * kTileK, p.plens[g]);
+        w->end = min(w->begin + p.p_span * kTileK, p.plens[g]);
+        const long long at = ((long long)g * p.pcap * p.Hk + hk) * 128;
+        w->row_bytes = (long long)p.Hk * 128;
+        w->v_stride = p.pv_stride;
+        w->k = p.pk + at;
+        w->v = p.pv + at + w->layer0 * p.pv_stride;
+        slot = split;
+        return true;
+    }
+    __device__ __forceinline__ long long place(int i) const {
+        const int row = row0 + i;
+        return (long long)(p.first[g] + row / p.group) * p.H + hk * p.group + row % p.group;
+    }
+    __device__ __forceinline__ const uint4* query(int i) const { return reinterpret_cast<const uint4*>(p.q + place(i) * 128); }
+    __device__ __forceinline__ bool all_seen(const TileWork& w, int c0) const { return c0 + kTileK <= w.end; }
+    __device__ __forceinline__ unsigned long long seen(const TileWork& w, int c0, int) const {
+        return w.end - c0 >= 64 ? ~0ull : (1ull << (w.end - c0)) - 1;
+    }
+    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, int i, float m, float l, bool ok) const {
+        const long long n_rows = (long long)p.n_items * p.H, at = i < w.rows ? place(i) : 0;
+        const bool mine = ok && i < w.rows;
+        if (mine && w.layer0 == 0) p.part_ml[slot * n_rows + at] = make_float2(m, l);
+        if (w.begin == w.end) return;                                   // nothing there: the join does not look at the outputs
+#pragma unroll
+        for (int y = 0; y < LG; ++y) {
+            if (y >= w.layers) break;
+            float4* dst = reinterpret_cast<float4*>(p.part_o + (((long long)slot * p.n_layers + w.layer0 + y) * n_rows + at) * kDh);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float o[32];
+                __syncwarp();
+                tile_ld32(t_out + y * 64 + h * 32, o);
+                tile_wait_ld();
+                if (mine)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) dst[h * 8 + c] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+            }
+        }
+    }
+    __device__ __forceinline__ void failed() const {
+        if (p.status && atomicCAS(&p.status[0], 0, (int)SAN_ERR_TIMEOUT) == 0) { p.status[1] = TAG_TILE; p.status[2] = g; }
+    }
+};
+
+template <class Mode, int LG, class Params>
+__global__ void __launch_bounds__(kTileThreads, 2) tile_kernel(const __grid_constant__ Params params) {
+    constexpr uint32_t kCols = 256;                                     // scores 2 x 64, outputs 64 x LG
+    static_assert(128 + 64 * LG <= (int)kCols, "tensor memory");
+    extern __shared__ __align__(1024) char tile_smem[];
+    __shared__ __align__(8) uint64_t k_full[kTileKSlots], k_free[kTileKSlots], v_full[2], s_full[2], s_free[2], p_full[2], pv_done[2];
+    __shared__ uint32_t tmem_s;
+    __shared__ int dead_s;
+    asm volatile("griddepcontrol.launch_dependents;");
+    Mode mode{params};
+    TileWork w;
+    if (!mode.work(&w)) return;                                         // uniform over the CTA, before anything is allocated
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int* dead = &dead_s;
+    char* base = tile_smem + ((1024u - (tile_u32(tile_smem) & 1023u)) & 1023u);
+    char* sQ = base;
+    char* sP = sQ + kTileQ * 128;                                       // two weight tiles
+    const uint32_t aK = tile_u32(sP + 2 * kTileQ * 128);
+    const uint32_t aV = aK + kTileKSlots * kTileK * 128;                // two slots of LG value tiles
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kTileKSlots; ++i) { tile_bar_init(&k_full[i], kTileLoaders); tile_bar_init(&k_free[i], 1); }
+        for (int i = 0; i < 2; ++i) {
+            tile_bar_init(&v_full[i], kTileLoaders); tile_bar_init(&s_full[i], 1); tile_bar_init(&s_free[i], 128);
+            tile_bar_init(&p_full[i], 128); tile_bar_init(&pv_done[i], 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        dead_s = 0;
+    }
+    if (warp == 7) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(tile_u32(&tmem_s)), "r"(kCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (threadIdx.x < 128) {
+        const int i = threadIdx.x;
+        const uint4* src = i < w.rows ? mode.query(i) : nullptr;
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+            *reinterpret_cast<uint4*>(sQ + i * 128 + ((c ^ (i & 7)) << 4)) = src ? src[c] : make_uint4(0, 0, 0, 0);
+    }
+    tile_proxy_fence();
+    tile_before_sync();
+    __syncthreads();
+    tile_after_sync();
+    const uint32_t tmem = tmem_s;
+    const int chunks = (w.end - w.begin + kTileK - 1) / kTileK;
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+
+    if (warp == 7) {
+        if (lane == 0) {
+            const uint64_t dQ = tile_desc(tile_u32(sQ));
+            const uint32_t id_s = tile_idesc(false, kTileK), id_o = tile_idesc(true, w.layers * kDh);
+            auto scores = [&](int t) -> bool {
+                if (!tile_wait(&k_full[t % kTileKSlots], (uint32_t)(t / kTileKSlots) & 1u, dead)) return false;
+                if (t >= 2 && !tile_wait(&s_free[t & 1], (uint32_t)((t - 2) >> 1) & 1u, dead)) return false;
+                tile_after_sync();
+                const uint64_t dK = tile_desc(aK + (uint32_t)(t % kTileKSlots) * (kTileK * 128));
+#pragma unroll
+                for (int s = 0; s < 4; ++s) tile_mma(tmem + (t & 1) * 64, dQ + 2 * s, dK + 2 * s, id_s, s > 0);
+                tile_commit(&s_full[t & 1]);
+                tile_commit(&k_free[t % kTileKSlots]);
+                return true;
+            };
+            auto outputs = [&](int t) -> bool {
+                if (!tile_wait(&v_full[t & 1], (uint32_t)(t >> 1) & 1u, dead)) return false;
+                if (!tile_wait(&p_full[t & 1], (uint32_t)(t >> 1) & 1u, dead)) return false;
+                tile_after_sync();
+                const uint64_t dP = tile_desc(tile_u32(sP) + (uint32_t)(t & 1) * (kTileQ * 128));
+                const uint64_t dV = tile_desc(aV + (uint32_t)(t & 1) * (LG * kTileK * 128), kTileK * 128);
+#pragma unroll
+                for (int s = 0; s < 4; ++s) tile_mma(tmem + 128, dP + 2 * s, dV + 128 * s, id_o, t > 0 || s > 0);
+                tile_commit(&pv_done[t & 1]);
+                return true;
+            };
+            bool go = chunks == 0 || scores(0);
+            for (int t = 0; t < chunks && go; ++t) go = (t + 1 >= chunks || scores(t + 1)) && outputs(t);
+        }
+    } else if (warp >= 4) {
+        const int tid = threadIdx.x - 128;
+        auto copy = [&](const char* src, uint32_t dst, int c0) {
+#pragma unroll
+            for (int j = 0; j < (kTileK * 8 + kTileLoaders - 1) / kTileLoaders; ++j) {
+                const int u = tid + j * kTileLoaders, r = u >> 3, c = u & 7, at = c0 + r;
+                if (r >= kTileK) break;
+                const bool full = at < w.end;
+                const int pos = !full ? 0 : at < w.ns ? at : w.lo + at - w.ns;
+                cp16(dst + r * 128 + ((c ^ (r & 7)) << 4), src + pos * w.row_bytes + (c << 4), full);
+            }
+        };
+        auto arrived = [&](uint64_t* bar) { tile_proxy_fence(); tile_arrive(bar); };
+        bool go = true;
+        for (int t = 0; t < chunks && go; ++t) {
+            const int c0 = w.begin + t * kTileK;
+            if (t >= kTileKSlots && !(go = tile_wait(&k_free[t % kTileKSlots], (uint32_t)(t / kTileKSlots - 1) & 1u, dead))) break;
+            copy(w.k, aK + (uint32_t)(t % kTileKSlots) * (kTileK * 128), c0);
+            cp_commit();
+            if (t > 0) { cp_wait<2>(); arrived(&k_full[(t - 1) % kTileKSlots]); }       // in flight behind it: values t - 1, keys t
+            if (t >= 2 && !(go = tile_wait(&pv_done[t & 1], (uint32_t)((t - 2) >> 1) & 1u, dead))) break;
+            for (int y = 0; y < w.layers; ++y) copy(w.v + y * w.v_stride, aV + (uint32_t)((t & 1) * LG + y) * (kTileK * 128), c0);
+            cp_commit();
+            if (t > 0) { cp_wait<2>(); arrived(&v_full[(t - 1) & 1]); }                 // keys t, values t
+        }
+        cp_wait<0>();
+        if (go && chunks > 0) {
+            arrived(&k_full[(chunks - 1) % kTileKSlots]);
+            arrived(&v_full[(chunks - 1) & 1]);
+        }
+    } else {
+        const int i = threadIdx.x;
+        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+        const float sc = params.scale_log2e;
+        for (int t = 0; t < chunks; ++t) {
+            const int c0 = w.begin + t * kTileK;
+            ok = __all_sync(0xffffffffu, tile_wait(&s_full[t & 1], (uint32_t)(t >> 1) & 1u, dead));
+            if (!ok) break;
+            tile_after_sync();
+            float z[64];
+            tile_ld32(lanes + (t & 1) * 64, z);
+            tile_ld32(lanes + (t & 1) * 64 + 32, z + 32);
+            tile_wait_ld();
+            tile_before_sync();
+            tile_arrive(&s_free[t & 1]);
+            if (!mode.all_seen(w, c0)) {                                // uniform over the CTA
+                const unsigned long long seen = mode.seen(w, c0, i);
+                const uint32_t s0 = (uint32_t)seen, s1 = (uint32_t)(seen >> 32);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    z[j] = s0 >> j & 1u ? z[j] : -INFINITY;
+                    z[32 + j] = s1 >> j & 1u ? z[32 + j] : -INFINITY;
+                }
+            }
+            float top[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+            for (int j = 4; j < 64; ++j) top[j & 3] = fmaxf(top[j & 3], z[j]);
+            const float m_chunk = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sc;
+            // A row that has seen nothing yet has outputs and a sum of zero: its maximum starts here.
+            const bool grown = m_chunk > m + 8.f && m > -INFINITY;
+            if (m == -INFINITY) m = m_chunk;
+            if (__any_sync(0xffffffffu, grown)) {
+                // (t > 0.)  The outputs of the chunk before are complete, those of this one wait for its weights.
+                ok = __all_sync(0xffffffffu, tile_wait(&pv_done[(t - 1) & 1], (uint32_t)((t - 1) >> 1) & 1u, dead));
+                if (!ok) break;
+                tile_after_sync();
+                const float f = grown ? fast_exp2(m - m_chunk) : 1.f;
+                if (grown) { m = m_chunk; l *= f; }
+                for (int y = 0; y < 4 * w.layers; ++y) {                // 16 columns at a time: the scores are still held
+                    float o[16];
+                    tile_ld16(lanes + 128 + y * 16, o);
+                    tile_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[j] *= f;
+                    tile_st16(lanes + 128 + y * 16, o);
+                }
+                tile_wait_st();
+                tile_before_sync();
+            }
+            const float base_m = m == -INFINITY ? 0.f : m;
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 64; ++j) {
+                z[j] = fast_exp2(fmaf(z[j], sc, -base_m));
+                sum[j & 3] += z[j];
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            if (t >= 2) {                                               // the weight tile is free
+                ok = __all_sync(0xffffffffu, tile_wait(&pv_done[t & 1], (uint32_t)((t - 2) >> 1) & 1u, dead));
+                if (!ok) break;
+            }
+            char* row = sP + (t & 1) * (kTileQ * 128) + i * 128;
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                *reinterpret_cast<uint4*>(row + ((c ^ (i & 7)) << 4)) =
+                    make_uint4(pack_bf16(z[8 * c], z[8 * c + 1]), pack_bf16(z[8 * c + 2], z[8 * c + 3]),
+                               pack_bf16(z[8 * c + 4], z[8 * c + 5]), pack_bf16(z[8 * c + 6], z[8 * c + 7]));
+            tile_proxy_fence();
+            tile_arrive(&p_full[t & 1]);
+        }
+        if (ok && chunks > 0) ok = tile_wait(&pv_done[(chunks - 1) & 1], (uint32_t)((chunks - 1) >> 1) & 1u, dead);
+        ok = __all_sync(0xffffffffu, ok);
+        tile_after_sync();
+        if (ok) mode.template finish<LG>(w, lanes + 128, i, m, l, true);
+        else if (threadIdx.x == 0) mode.failed();
+    }
+    tile_before_sync();
+    __syncthreads();
+    if (warp == 7) {
+        __syncwarp();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kCols) : "memory");
+    }
+}
+
+}  // namespace san
