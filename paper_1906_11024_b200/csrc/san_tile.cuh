@@ -11,7 +11,7 @@
 //              taken against moves only when a row's own has grown by more than 2^8, since then the
 //              outputs have to be read, scaled and written back; the sum uses the same one, so nothing is lost.
 //   warps 4-6  copies: 16-byte cp.async into operand tiles (rows of 128 bytes, chunks XOR-swizzled by row & 7, what
-//              the matrix descriptors name), keys up to three chunks ahead, values two; rows past the end are zeros.
+//              the matrix descriptors name), up to three chunks ahead; rows past the end are zeros.
 //   warp 7     one thread issues the MMAs: scores of chunk t + 1 before outputs of chunk t, so that the tensor cores
 //              work on them while the softmax warps work on chunk t.
 // What bounds it: the exponentials, 64 per row and chunk at 16 per clock and SM (512 clocks a chunk against 384
@@ -26,10 +26,10 @@
 namespace san {
 
 constexpr int kTileQ = 128, kTileK = 64, kTileThreads = 256, kTileLoaders = 96;
-constexpr int kTileKSlots = 3, kTileMaxLayers = 2;
+constexpr int kTileSlots = 3, kTileMaxLayers = 2;     // slots of the key ring and of the value ring
 constexpr int TAG_TILE = 11;
 __host__ __device__ constexpr int tile_smem_bytes(int layers) {
-    return 1024 + kTileQ * 128 * 3 + (kTileKSlots + 2 * layers) * kTileK * 128;
+    return 1024 + kTileQ * 128 * 2 + kTileSlots * (1 + layers) * kTileK * 128;
 }
 
 __device__ __forceinline__ uint32_t tile_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -101,6 +101,29 @@ __device__ __forceinline__ void tile_st16(uint32_t addr, const float* v) {
 }
 __device__ __forceinline__ void tile_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tile_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Two float32 numbers in one instruction, and the largest of three.
+__device__ __forceinline__ unsigned long long tile_pair(float x, float y) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void tile_unpair(unsigned long long r, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(r)); }
+__device__ __forceinline__ unsigned long long tile_fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ unsigned long long tile_add2(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float tile_max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 
 // What a CTA works on.  Visible keys are numbered 0 .. end - 1: the first ns of them are rows 0.., the others rows lo...
 struct TileWork {
@@ -251,7 +274,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) tile_kernel(const __grid_cons
     constexpr uint32_t kCols = 256;                                     // scores 2 x 64, outputs 64 x LG
     static_assert(128 + 64 * LG <= (int)kCols, "tensor memory");
     extern __shared__ __align__(1024) char tile_smem[];
-    __shared__ __align__(8) uint64_t k_full[kTileKSlots], k_free[kTileKSlots], v_full[2], s_full[2], s_free[2], p_full[2], pv_done[2];
+    __shared__ __align__(8) uint64_t k_full[kTileSlots], k_free[kTileSlots], v_full[kTileSlots], pv_done[kTileSlots], s_full[2], s_free[2], p_full[1];
     __shared__ uint32_t tmem_s;
     __shared__ int dead_s;
     asm volatile("griddepcontrol.launch_dependents;");
@@ -262,15 +285,16 @@ __global__ void __launch_bounds__(kTileThreads, 2) tile_kernel(const __grid_cons
     volatile int* dead = &dead_s;
     char* base = tile_smem + ((1024u - (tile_u32(tile_smem) & 1023u)) & 1023u);
     char* sQ = base;
-    char* sP = sQ + kTileQ * 128;                                       // two weight tiles
-    const uint32_t aK = tile_u32(sP + 2 * kTileQ * 128);
-    const uint32_t aV = aK + kTileKSlots * kTileK * 128;                // two slots of LG value tiles
+    char* sP = sQ + kTileQ * 128;                                       // weights
+    const uint32_t aK = tile_u32(sP + kTileQ * 128);
+    const uint32_t aV = aK + kTileSlots * kTileK * 128;                 // slots of LG value tiles
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kTileKSlots; ++i) { tile_bar_init(&k_full[i], kTileLoaders); tile_bar_init(&k_free[i], 1); }
-        for (int i = 0; i < 2; ++i) {
-            tile_bar_init(&v_full[i], kTileLoaders); tile_bar_init(&s_full[i], 1); tile_bar_init(&s_free[i], 128);
-            tile_bar_init(&p_full[i], 128); tile_bar_init(&pv_done[i], 1);
+        for (int i = 0; i < kTileSlots; ++i) {
+            tile_bar_init(&k_full[i], kTileLoaders); tile_bar_init(&k_free[i], 1);
+            tile_bar_init(&v_full[i], kTileLoaders); tile_bar_init(&pv_done[i], 1);
         }
+        for (int i = 0; i < 2; ++i) { tile_bar_init(&s_full[i], 1); tile_bar_init(&s_free[i], 128); }
+        tile_bar_init(&p_full[0], 128);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         dead_s = 0;
     }
@@ -299,60 +323,70 @@ __global__ void __launch_bounds__(kTileThreads, 2) tile_kernel(const __grid_cons
             const uint64_t dQ = tile_desc(tile_u32(sQ));
             const uint32_t id_s = tile_idesc(false, kTileK), id_o = tile_idesc(true, w.layers * kDh);
             auto scores = [&](int t) -> bool {
-                if (!tile_wait(&k_full[t % kTileKSlots], (uint32_t)(t / kTileKSlots) & 1u, dead)) return false;
+                if (!tile_wait(&k_full[t % kTileSlots], (uint32_t)(t / kTileSlots) & 1u, dead)) return false;
                 if (t >= 2 && !tile_wait(&s_free[t & 1], (uint32_t)((t - 2) >> 1) & 1u, dead)) return false;
+                tile_proxy_fence();                                     // the copies are writes of the generic proxy
                 tile_after_sync();
-                const uint64_t dK = tile_desc(aK + (uint32_t)(t % kTileKSlots) * (kTileK * 128));
+                const uint64_t dK = tile_desc(aK + (uint32_t)(t % kTileSlots) * (kTileK * 128));
 #pragma unroll
                 for (int s = 0; s < 4; ++s) tile_mma(tmem + (t & 1) * 64, dQ + 2 * s, dK + 2 * s, id_s, s > 0);
                 tile_commit(&s_full[t & 1]);
-                tile_commit(&k_free[t % kTileKSlots]);
+                tile_commit(&k_free[t % kTileSlots]);
                 return true;
             };
+            const uint64_t dP = tile_desc(tile_u32(sP));
             auto outputs = [&](int t) -> bool {
-                if (!tile_wait(&v_full[t & 1], (uint32_t)(t >> 1) & 1u, dead)) return false;
-                if (!tile_wait(&p_full[t & 1], (uint32_t)(t >> 1) & 1u, dead)) return false;
+                if (!tile_wait(&v_full[t % kTileSlots], (uint32_t)(t / kTileSlots) & 1u, dead)) return false;
+                if (!tile_wait(&p_full[0], (uint32_t)t & 1u, dead)) return false;
+                tile_proxy_fence();
                 tile_after_sync();
-                const uint64_t dP = tile_desc(tile_u32(sP) + (uint32_t)(t & 1) * (kTileQ * 128));
-                const uint64_t dV = tile_desc(aV + (uint32_t)(t & 1) * (LG * kTileK * 128), kTileK * 128);
+                const uint64_t dV = tile_desc(aV + (uint32_t)(t % kTileSlots) * (LG * kTileK * 128), kTileK * 128);
 #pragma unroll
                 for (int s = 0; s < 4; ++s) tile_mma(tmem + 128, dP + 2 * s, dV + 128 * s, id_o, t > 0 || s > 0);
-                tile_commit(&pv_done[t & 1]);
+                tile_commit(&pv_done[t % kTileSlots]);
                 return true;
             };
             bool go = chunks == 0 || scores(0);
             for (int t = 0; t < chunks && go; ++t) go = (t + 1 >= chunks || scores(t + 1)) && outputs(t);
         }
     } else if (warp >= 4) {
-        const int tid = threadIdx.x - 128;
+        // thread: 16-byte piece c of rows r0, r0 + 12, ...
+        static_assert(kTileLoaders == 96 && kTileK == 64, "rows of a thread");
+        const int r0 = (threadIdx.x - 128) >> 3, c = threadIdx.x & 7;
+        const uint32_t sw0 = (uint32_t)(r0 * 128 + ((c ^ (r0 & 7)) << 4)), sw1 = (uint32_t)(r0 * 128 + ((c ^ ((r0 + 4) & 7)) << 4));
+        const long long step = 12 * w.row_bytes;
         auto copy = [&](const char* src, uint32_t dst, int c0) {
+            const int first = c0 + r0;
+            if (c0 >= w.ns && c0 + kTileK <= w.end) {                   // 64 rows on end
+                const char* at = src + (long long)(w.lo + first - w.ns) * w.row_bytes + (c << 4);
 #pragma unroll
-            for (int j = 0; j < (kTileK * 8 + kTileLoaders - 1) / kTileLoaders; ++j) {
-                const int u = tid + j * kTileLoaders, r = u >> 3, c = u & 7, at = c0 + r;
-                if (r >= kTileK) break;
-                const bool full = at < w.end;
-                const int pos = !full ? 0 : at < w.ns ? at : w.lo + at - w.ns;
-                cp16(dst + r * 128 + ((c ^ (r & 7)) << 4), src + pos * w.row_bytes + (c << 4), full);
+                for (int j = 0; j < 6; ++j, at += step)
+                    if (j < 5 || r0 < 4) cp16(dst + (uint32_t)(j * 12 * 128) + (j & 1 ? sw1 : sw0), at, true);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 6; ++j) {
+                    const int n = first + j * 12;
+                    const bool full = n < w.end;
+                    const int pos = !full ? 0 : n < w.ns ? n : w.lo + n - w.ns;
+                    if (j < 5 || r0 < 4) cp16(dst + (uint32_t)(j * 12 * 128) + (j & 1 ? sw1 : sw0), src + pos * w.row_bytes + (c << 4), full);
+                }
             }
         };
-        auto arrived = [&](uint64_t* bar) { tile_proxy_fence(); tile_arrive(bar); };
-        bool go = true;
-        for (int t = 0; t < chunks && go; ++t) {
-            const int c0 = w.begin + t * kTileK;
-            if (t >= kTileKSlots && !(go = tile_wait(&k_free[t % kTileKSlots], (uint32_t)(t / kTileKSlots - 1) & 1u, dead))) break;
-            copy(w.k, aK + (uint32_t)(t % kTileKSlots) * (kTileK * 128), c0);
-            cp_commit();
-            if (t > 0) { cp_wait<2>(); arrived(&k_full[(t - 1) % kTileKSlots]); }       // in flight behind it: values t - 1, keys t
-            if (t >= 2 && !(go = tile_wait(&pv_done[t & 1], (uint32_t)((t - 2) >> 1) & 1u, dead))) break;
-            for (int y = 0; y < w.layers; ++y) copy(w.v + y * w.v_stride, aV + (uint32_t)((t & 1) * LG + y) * (kTileK * 128), c0);
-            cp_commit();
-            if (t > 0) { cp_wait<2>(); arrived(&v_full[(t - 1) & 1]); }                 // keys t, values t
+        // the barrier hears of a thread's copies when they have landed; the thread does not wait for them
+        auto landed = [](uint64_t* bar) {
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tile_u32(bar)) : "memory");
+        };
+        for (int t = 0; t < chunks; ++t) {
+            const int c0 = w.begin + t * kTileK, slot = t % kTileSlots;
+            const uint32_t before = (uint32_t)(t / kTileSlots - 1) & 1u;
+            if (t >= kTileSlots && !tile_wait(&k_free[slot], before, dead)) break;
+            copy(w.k, aK + (uint32_t)slot * (kTileK * 128), c0);
+            landed(&k_full[slot]);
+            if (t >= kTileSlots && !tile_wait(&pv_done[slot], before, dead)) break;
+            for (int y = 0; y < w.layers; ++y) copy(w.v + y * w.v_stride, aV + (uint32_t)(slot * LG + y) * (kTileK * 128), c0);
+            landed(&v_full[slot]);
         }
-        cp_wait<0>();
-        if (go && chunks > 0) {
-            arrived(&k_full[(chunks - 1) % kTileKSlots]);
-            arrived(&v_full[(chunks - 1) & 1]);
-        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
         const int i = threadIdx.x;
         const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
@@ -379,14 +413,18 @@ __global__ void __launch_bounds__(kTileThreads, 2) tile_kernel(const __grid_cons
             }
             float top[4] = {z[0], z[1], z[2], z[3]};
 #pragma unroll
-            for (int j = 4; j < 64; ++j) top[j & 3] = fmaxf(top[j & 3], z[j]);
+            for (int j = 4; j < 60; j += 8)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top[e] = tile_max3(top[e], z[j + 2 * e], z[j + 2 * e + 1]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top[e] = fmaxf(top[e], z[60 + e]);
             const float m_chunk = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sc;
             // A row that has seen nothing yet has outputs and a sum of zero: its maximum starts here.
             const bool grown = m_chunk > m + 8.f && m > -INFINITY;
             if (m == -INFINITY) m = m_chunk;
             if (__any_sync(0xffffffffu, grown)) {
                 // (t > 0.)  The outputs of the chunk before are complete, those of this one wait for its weights.
-                ok = __all_sync(0xffffffffu, tile_wait(&pv_done[(t - 1) & 1], (uint32_t)((t - 1) >> 1) & 1u, dead));
+                ok = __all_sync(0xffffffffu, tile_wait(&pv_done[(t - 1) % kTileSlots], (uint32_t)((t - 1) / kTileSlots) & 1u, dead));
                 if (!ok) break;
                 tile_after_sync();
                 const float f = grown ? fast_exp2(m - m_chunk) : 1.f;
@@ -403,27 +441,32 @@ __global__ void __launch_bounds__(kTileThreads, 2) tile_kernel(const __grid_cons
                 tile_before_sync();
             }
             const float base_m = m == -INFINITY ? 0.f : m;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            unsigned long long sum[2] = {0ull, 0ull};
+            const unsigned long long sc2 = tile_pair(sc, sc), m2 = tile_pair(-base_m, -base_m);
 #pragma unroll
-            for (int j = 0; j < 64; ++j) {
-                z[j] = fast_exp2(fmaf(z[j], sc, -base_m));
-                sum[j & 3] += z[j];
+            for (int j = 0; j < 64; j += 2) {
+                tile_unpair(tile_fma2(tile_pair(z[j], z[j + 1]), sc2, m2), z[j], z[j + 1]);
+                z[j] = fast_exp2(z[j]);
+                z[j + 1] = fast_exp2(z[j + 1]);
+                sum[(j >> 1) & 1] = tile_add2(sum[(j >> 1) & 1], tile_pair(z[j], z[j + 1]));
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            if (t >= 2) {                                               // the weight tile is free
-                ok = __all_sync(0xffffffffu, tile_wait(&pv_done[t & 1], (uint32_t)((t - 2) >> 1) & 1u, dead));
+            float sa, sb;
+            tile_unpair(tile_add2(sum[0], sum[1]), sa, sb);
+            l += sa + sb;
+            if (t >= 1) {                                               // the weight tile is free
+                ok = __all_sync(0xffffffffu, tile_wait(&pv_done[(t - 1) % kTileSlots], (uint32_t)((t - 1) / kTileSlots) & 1u, dead));
                 if (!ok) break;
             }
-            char* row = sP + (t & 1) * (kTileQ * 128) + i * 128;
+            char* row = sP + i * 128;
 #pragma unroll
             for (int c = 0; c < 8; ++c)
                 *reinterpret_cast<uint4*>(row + ((c ^ (i & 7)) << 4)) =
                     make_uint4(pack_bf16(z[8 * c], z[8 * c + 1]), pack_bf16(z[8 * c + 2], z[8 * c + 3]),
                                pack_bf16(z[8 * c + 4], z[8 * c + 5]), pack_bf16(z[8 * c + 6], z[8 * c + 7]));
             tile_proxy_fence();
-            tile_arrive(&p_full[t & 1]);
+            tile_arrive(&p_full[0]);
         }
-        if (ok && chunks > 0) ok = tile_wait(&pv_done[(chunks - 1) & 1], (uint32_t)((chunks - 1) >> 1) & 1u, dead);
+        if (ok && chunks > 0) ok = tile_wait(&pv_done[(chunks - 1) % kTileSlots], (uint32_t)((chunks - 1) / kTileSlots) & 1u, dead);
         ok = __all_sync(0xffffffffu, ok);
         tile_after_sync();
         if (ok) mode.template finish<LG>(w, lanes + 128, i, m, l, true);
