@@ -12,12 +12,11 @@
 //     sequence's own rows the query rows are the query heads of the key head's group; for a prefix they
 //     are those of every sequence behind the prefix, so that the prefix is read once for all of them.
 //   * A unit is streamed by 1 or 4 warps.  Each warp has a ring of slots of its own in shared memory (32 rows
-//     of one plane each), filled by 16-byte cp.async five slots ahead: no barrier between warps until
+//     of one plane each), filled by 16-byte cp.async two slots ahead: no barrier between warps until
 //     their partial results meet at the end of the unit.
 //   * One pass with the running maximum and sum of the softmax; scores never leave the registers.  bf16
-//     rows go through mma.sync.m16n8k16: D[16 queries x 8 positions], whose accumulators are, packed, the A operand
-//     of D[16 queries x 8 dims].  With one query row 15 of 16 rows are padding, and it is still the
-//     cheapest form: about 5 warp instructions per position against 12 on the CUDA cores.  float32 rows (tolerance
+//     rows go through mma.sync.m16n8k16 with the queries as N.  With one query row seven of eight columns are padding,
+//     and it is still the cheapest form: about 5 warp instructions per position against 12 on the CUDA cores.  float32 rows (tolerance
 //     1e-5) stay on the CUDA cores: a lane scores one position for up to 8 query rows, then owns two dims.
 //   * Units of the same row (runs of a long row; its prefix and its own rows) leave (max, sum, unnormalised
 //     outputs) in the workspace and attend_join_kernel adds them up, launched with programmatic stream
@@ -37,13 +36,15 @@ constexpr int kAtTile = 32;                 // positions per slot
 constexpr int kAtMaxLayers = 4;             // layers whose outputs a warp accumulates at once
 
 template <typename T> struct AttendGeom;
-template <> struct AttendGeom<__nv_bfloat16> { static constexpr int kRows = 16, kSlots = 6, kRowBytes = 128; };
-template <> struct AttendGeom<float>         { static constexpr int kRows = 8,  kSlots = 3, kRowBytes = 256; };
+constexpr int kAtRows = 8;                  // query rows of a unit: one N of mma.sync
+constexpr int kAtOutLd = 68;                // floats between the rows of outputs in shared memory (no bank conflicts)
+template <> struct AttendGeom<__nv_bfloat16> { static constexpr int kSlots = 3, kRowBytes = 128; };
+template <> struct AttendGeom<float>         { static constexpr int kSlots = 3, kRowBytes = 256; };
 template <typename T> __host__ __device__ constexpr int attend_warp_bytes() {       // ring; float32: query rows and weights behind it
     return AttendGeom<T>::kSlots * kAtTile * AttendGeom<T>::kRowBytes +
-           (sizeof(T) == 4 ? AttendGeom<T>::kRows * kDh * 4 + kAtTile * AttendGeom<T>::kRows * 4 : 0);
+           (sizeof(T) == 4 ? kAtRows * kDh * 4 + kAtTile * kAtRows * 4 : 0);
 }
-template <typename T> __host__ __device__ constexpr int attend_smem_bytes() { return kAtWarps * (attend_warp_bytes<T>() + 2 * AttendGeom<T>::kRows * 4); }
+template <typename T> __host__ __device__ constexpr int attend_smem_bytes() { return kAtWarps * (attend_warp_bytes<T>() + 2 * kAtRows * 4); }
 
 struct AttendParams {
     const char* q; char* out;
@@ -143,15 +144,30 @@ template <typename T>
 __device__ __forceinline__ void attend_fill(const AttendRun& u, int begin, int end, int plane, uint32_t slot, int lane) {
     constexpr int RB = AttendGeom<T>::kRowBytes, CPR = RB / 16, RPI = 32 / CPR;     // chunks per row, rows per instruction
     const char* base = plane < 0 ? u.k : u.v + plane * u.v_stride;
-    const int c_smem = lane % CPR;
+    const int c_smem = lane % CPR, q = lane / CPR;
+    const uint32_t dst = slot + q * RB + c_smem * 16;
+    if (begin >= u.n_sink && begin + kAtTile <= end) {       // 32 rows on end
+        const int pos = u.lo + begin - u.n_sink + q;
+        const char* src = base + pos * u.row_bytes;
+        const long long step = RPI * u.row_bytes;
+        int off[8 / RPI];                                    // the chunk to fetch: row j * RPI + q has 8 / RPI swizzles
 #pragma unroll
-    for (int j = 0; j < kAtTile / RPI; ++j) {
-        const int r = j * RPI + lane / CPR, at = begin + r;
-        const bool full = at < end;
-        const int pos = !full ? 0 : at < u.n_sink ? at : u.lo + (at - u.n_sink);
-        const int c = c_smem ^ (r & 7);
-        const char* src = base + pos * u.row_bytes + ((u.permuted ? c ^ (pos & 7) : c) << 4);
-        cp16(slot + r * RB + c_smem * 16, src, full);
+        for (int j = 0; j < 8 / RPI; ++j) {
+            const int c = c_smem ^ ((j * RPI + q) & 7);
+            off[j] = (u.permuted ? c ^ ((pos + j * RPI) & 7) : c) << 4;
+        }
+#pragma unroll
+        for (int j = 0; j < kAtTile / RPI; ++j, src += step) cp16(dst + j * RPI * RB, src + off[j % (8 / RPI)], true);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kAtTile / RPI; ++j) {
+            const int r = j * RPI + q, at = begin + r;
+            const bool full = at < end;
+            const int pos = !full ? 0 : at < u.n_sink ? at : u.lo + (at - u.n_sink);
+            const int c = c_smem ^ (r & 7);
+            const char* src = base + pos * u.row_bytes + ((u.permuted ? c ^ (pos & 7) : c) << 4);
+            cp16(dst + j * RPI * RB, src, full);
+        }
     }
     cp_commit();
 }
@@ -162,7 +178,7 @@ __device__ __forceinline__ void attend_fill(const AttendRun& u, int begin, int e
 template <typename T>
 __device__ __forceinline__ void attend_finish(const AttendParams& p, const AttendRun& u, bool active, int wpu, char* smem,
                                               const float2* ml, int warp, int lane) {
-    constexpr int R = AttendGeom<T>::kRows;
+    constexpr int R = kAtRows;
     __syncthreads();
     if (!active) return;
     const int w0 = warp / wpu * wpu;
@@ -191,7 +207,7 @@ __device__ __forceinline__ void attend_finish(const AttendParams& p, const Atten
 #pragma unroll
             for (int w = 0; w < kAtWarps; ++w) {
                 if (w >= wpu || weight[w] == 0.f) continue;
-                const float4 x = *reinterpret_cast<const float4*>(smem + (w0 + w) * attend_warp_bytes<T>() + ((y * R + i) * kDh + (t & 15) * 4) * 4);
+                const float4 x = *reinterpret_cast<const float4*>(smem + (w0 + w) * attend_warp_bytes<T>() + ((y * R + i) * kAtOutLd + (t & 15) * 4) * 4);
                 o.x += weight[w] * x.x; o.y += weight[w] * x.y; o.z += weight[w] * x.z; o.w += weight[w] * x.w;
             }
             const int layer = u.layer0 + y;
@@ -239,130 +255,138 @@ template <typename T> struct AttendRing {
     }
 };
 
-// bf16, up to 16 query rows.  ROWS8: rows 8 to 15 are padding.
-template <int LG, bool ROWS8>
+// bf16, up to eight query rows, which are the N side of both products: scores D[16 positions x 8 queries] with
+// the key rows as A, outputs D[16 dims x 8 queries] with the value rows, transposed by ldmatrix, as A.
+template <int LG>
 __device__ __forceinline__ void attend_warp_bf16(const AttendParams& p, const AttendRun& u, int first, int step, char* smem, float2* ml, int lane) {
     const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(smem);
     AttendRing<__nv_bfloat16> ring(u, ring_addr, lane, first, step);
     const int g = lane >> 2, t4 = lane & 3;
-    uint32_t qa[4][4];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int i = g + h * 8;
-        const bool real = i < u.rows && !(ROWS8 && h == 1);
-        const int row = u.row0 + (real ? i : 0), item = u.item0 + row / p.group, head = u.head0 + row % p.group;
+    uint32_t qb[4][2];                                       // B: query g, dims 16 c + 2 t4 .. and 8 further on
+    {
+        const bool real = g < u.rows;
+        const int row = u.row0 + (real ? g : 0), item = u.item0 + row / p.group, head = u.head0 + row % p.group;
         const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q + ((long long)item * p.H + head) * 128) + t4;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            qa[c][h] = real ? src[c * 8] : 0u;
-            qa[c][h + 2] = real ? src[c * 8 + 4] : 0u;
+            qb[c][0] = real ? src[c * 8] : 0u;
+            qb[c][1] = real ? src[c * 8 + 4] : 0u;
         }
     }
-    float acc[LG][8][4];
+    float acc[LG][4][4];                                     // [layer][16 dims]: dims g and g + 8, queries 2 t4 and 2 t4 + 1
 #pragma unroll
     for (int y = 0; y < LG; ++y)
 #pragma unroll
-        for (int d = 0; d < 8; ++d)
+        for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[y][d][e] = 0.f;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
     const int r8 = lane & 7, mat = lane >> 3;
-    for (int at = first; at < u.end; at += step) {
-        const uint32_t ks = ring_addr + ring.next();
-        float s[4][4];
+    const uint32_t k_row = ((mat & 1) * 8 + r8) * 128, v_row = ((mat >> 1) * 8 + r8) * 128;
+    uint32_t k_chunk[4], v_chunk[4];
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
+    for (int c = 0; c < 4; ++c) {
+        k_chunk[c] = (uint32_t)((2 * c + (mat >> 1)) ^ r8) << 4;
+        v_chunk[c] = (uint32_t)((2 * c + (mat & 1)) ^ r8) << 4;
+    }
+    for (int at = first; at < u.end; at += step) {
+        const uint32_t ks = ring_addr + ring.next() + k_row;
+        float s[2][4];                                       // positions 16 n + g and + 8, queries 2 t4 and 2 t4 + 1
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
-            uint32_t b[8];
-            const uint32_t row = ks + (n * 8 + r8) * 128;
-            ldsm4(b, row + ((mat ^ r8) << 4));
-            ldsm4(b + 4, row + (((mat + 4) ^ r8) << 4));
 #pragma unroll
-            for (int c = 0; c < 4; ++c) mma_bf16(s[n], qa[c], b[2 * c], b[2 * c + 1]);
+            for (int c = 0; c < 4; ++c) {
+                uint32_t a[4];
+                ldsm4(a, ks + n * 16 * 128 + k_chunk[c]);
+                mma_bf16(s[n], a, qb[c][0], qb[c][1]);
+            }
         }
         float top[2] = {-INFINITY, -INFINITY};
+        const bool part = at + kAtTile > u.end;
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                s[n][e] = at + n * 8 + t4 * 2 + (e & 1) < u.end ? s[n][e] * p.scale_log2e : -INFINITY;
-                top[e >> 1] = fmaxf(top[e >> 1], s[n][e]);
+                s[n][e] = part && at + n * 16 + (e >> 1) * 8 + g >= u.end ? -INFINITY : s[n][e] * p.scale_log2e;
+                top[e & 1] = fmaxf(top[e & 1], s[n][e]);
             }
         float alpha[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if (ROWS8 && h == 1) { alpha[1] = 1.f; continue; }
-            top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
-            top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
-            const float m_new = fmaxf(m[h], top[h]);
-            const float base = m_new == -INFINITY ? 0.f : m_new;     // all scores -inf so far: weights 0
-            alpha[h] = m[h] == m_new ? 1.f : fast_exp2(m[h] - base);
-            m[h] = m_new;
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], o));
+            const float m_new = fmaxf(m[j], top[j]);
+            const float base = m_new == -INFINITY ? 0.f : m_new;         // all scores -inf so far: weights 0
+            alpha[j] = m[j] == m_new ? 1.f : fast_exp2(m[j] - base);
+            m[j] = m_new;
             float sum = 0.f;
 #pragma unroll
-            for (int n = 0; n < 4; ++n)
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    s[n][2 * h + e] = fast_exp2(s[n][2 * h + e] - base);
-                    sum += s[n][2 * h + e];
+                    s[n][2 * e + j] = fast_exp2(s[n][2 * e + j] - base);
+                    sum += s[n][2 * e + j];
                 }
-            l[h] = l[h] * alpha[h] + sum;
+            l[j] = l[j] * alpha[j] + sum;
         }
         // The weights enter the second product in bf16 (at most half a step, 2^-8 relative, of independent sign); their
-        // sum is that of the float32 ones.
-        uint32_t pa[2][4];
+        // sum is that of the float32 ones.  As B they have to hold neighbouring positions: an 8 x 8 transpose.
+        uint32_t pb[2][2];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            pa[c][0] = pack_bf16(s[2 * c][0], s[2 * c][1]);
-            pa[c][1] = ROWS8 ? 0u : pack_bf16(s[2 * c][2], s[2 * c][3]);
-            pa[c][2] = pack_bf16(s[2 * c + 1][0], s[2 * c + 1][1]);
-            pa[c][3] = ROWS8 ? 0u : pack_bf16(s[2 * c + 1][2], s[2 * c + 1][3]);
-        }
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(pb[n][e]) : "r"(pack_bf16(s[n][2 * e], s[n][2 * e + 1])));
         if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
 #pragma unroll
             for (int y = 0; y < LG; ++y)
 #pragma unroll
-                for (int d = 0; d < 8; ++d)
+                for (int d = 0; d < 4; ++d)
 #pragma unroll
-                    for (int e = 0; e < (ROWS8 ? 2 : 4); ++e) acc[y][d][e] *= alpha[e >> 1];
+                    for (int e = 0; e < 4; ++e) acc[y][d][e] *= alpha[e & 1];
         }
 #pragma unroll
         for (int y = 0; y < LG; ++y) {
             if (y >= u.layers) break;
-            const uint32_t vs = ring_addr + ring.next();
+            const uint32_t vs = ring_addr + ring.next() + v_row;
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
-                for (int d = 0; d < 8; d += 2) {
-                    uint32_t b[4];
-                    ldsm4t(b, vs + (c * 16 + (mat & 1) * 8 + r8) * 128 + (((d + (mat >> 1)) ^ r8) << 4));
-                    mma_bf16(acc[y][d], pa[c], b[0], b[1]);
-                    mma_bf16(acc[y][d + 1], pa[c], b[2], b[3]);
+                for (int d = 0; d < 4; ++d) {
+                    uint32_t a[4];
+                    ldsm4t(a, vs + n * 16 * 128 + v_chunk[d]);
+                    mma_bf16(acc[y][d], a, pb[n][0], pb[n][1]);
                 }
-            }
+        }
     }
     cp_wait<0>();
     __syncwarp();
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        if (ROWS8 && h == 1) break;
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-        if (t4 == 0) ml[g + h * 8] = make_float2(m[h], l[h]);
+    for (int j = 0; j < 2; ++j) {
 #pragma unroll
-        for (int y = 0; y < LG; ++y)
+        for (int o = 4; o < 32; o <<= 1) l[j] += __shfl_xor_sync(0xffffffffu, l[j], o);
+        const int row = 2 * t4 + j;
+        if (g == 0) ml[row] = make_float2(m[j], l[j]);
+        if (row < u.rows) {
+            float* out = reinterpret_cast<float*>(smem) + row * kAtOutLd + g;
 #pragma unroll
-            for (int d = 0; d < 8; ++d)
-                *reinterpret_cast<float2*>(smem + ((y * 16 + g + h * 8) * kDh + d * 8 + t4 * 2) * 4) = make_float2(acc[y][d][2 * h], acc[y][d][2 * h + 1]);
+            for (int y = 0; y < LG; ++y)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    out[y * kAtRows * kAtOutLd + d * 16] = acc[y][d][j];
+                    out[y * kAtRows * kAtOutLd + d * 16 + 8] = acc[y][d][2 + j];
+                }
+        }
     }
 }
 
 // float32, up to R query rows on the CUDA cores.
 template <int LG, int R>
 __device__ __forceinline__ void attend_warp_f32(const AttendParams& p, const AttendRun& u, int first, int step, char* smem, float2* ml, int lane) {
-    constexpr int RMAX = AttendGeom<float>::kRows;
+    constexpr int RMAX = kAtRows;
     AttendRing<float> ring(u, (uint32_t)__cvta_generic_to_shared(smem), lane, first, step);
     float* qs = reinterpret_cast<float*>(smem + AttendGeom<float>::kSlots * kAtTile * 256);      // [R][64]
     float* ws = qs + RMAX * kDh;                                                                // [32][R] weights
@@ -447,7 +471,7 @@ __device__ __forceinline__ void attend_warp_f32(const AttendParams& p, const Att
         if (lane == 0) ml[i] = make_float2(m[i], l[i]);
 #pragma unroll
         for (int y = 0; y < LG; ++y)
-            *reinterpret_cast<float2*>(smem + ((y * RMAX + i) * kDh + lane * 2) * 4) = make_float2(acc[y][i][0], acc[y][i][1]);
+            *reinterpret_cast<float2*>(smem + ((y * RMAX + i) * kAtOutLd + lane * 2) * 4) = make_float2(acc[y][i][0], acc[y][i][1]);
     }
 }
 
@@ -455,7 +479,7 @@ __device__ __forceinline__ void attend_warp_f32(const AttendParams& p, const Att
 // is at fault).
 template <typename T>
 __device__ __forceinline__ bool attend_unit(const AttendParams& p, bool prefix, int index, bool reporter, AttendRun* u) {
-    constexpr int R = AttendGeom<T>::kRows, RB = AttendGeom<T>::kRowBytes;
+    constexpr int R = kAtRows, RB = AttendGeom<T>::kRowBytes;
     if (index >= (prefix ? p.p_units : p.o_units)) return false;
     const int lg = index % p.n_lg; index /= p.n_lg;
     const int splits = prefix ? p.p_splits : p.o_splits, span = (prefix ? p.p_span : p.o_span) * kAtTile;
@@ -515,7 +539,7 @@ template <typename T, int LG>
 __global__ void __launch_bounds__(kAtWarps * 32) attend_kernel(const __grid_constant__ AttendParams p) {
     extern __shared__ __align__(128) char attend_smem[];
     asm volatile("griddepcontrol.launch_dependents;");
-    constexpr int R = AttendGeom<T>::kRows;
+    constexpr int R = kAtRows;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const bool prefix = (int)blockIdx.x < p.p_ctas;
     const int wpu = prefix ? p.p_wpu : p.o_wpu;
@@ -527,8 +551,7 @@ __global__ void __launch_bounds__(kAtWarps * 32) attend_kernel(const __grid_cons
         char* smem = attend_smem + warp * attend_warp_bytes<T>();
         const int first = u.begin + (warp % wpu) * kAtTile, step = wpu * kAtTile;
         if constexpr (sizeof(T) == 2) {
-            if (u.rows <= 8) attend_warp_bf16<LG, true>(p, u, first, step, smem, ml + warp * R, lane);
-            else attend_warp_bf16<LG, false>(p, u, first, step, smem, ml + warp * R, lane);
+            attend_warp_bf16<LG>(p, u, first, step, smem, ml + warp * R, lane);
         } else {
             if (u.rows <= 1) attend_warp_f32<LG, 1>(p, u, first, step, smem, ml + warp * R, lane);
             else if (u.rows <= 4) attend_warp_f32<LG, 4>(p, u, first, step, smem, ml + warp * R, lane);

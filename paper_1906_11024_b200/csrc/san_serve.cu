@@ -88,14 +88,15 @@ int32_t check_prefix(const san_cached_rows* r, const san_shared_prefix* x) {
 }
 
 // How one kind of units is cut: warps per unit and runs of tiles.
-// A warp takes a whole run where that gives every warp slot of the GPU two of them or the run is short;
+// A warp takes a whole run where the runs are short or no longer than twice a warp's share of the work;
 // otherwise the four warps of a CTA share a run, and a long one is cut into several until the SMs have
 // two CTAs each, but not below eight tiles (a run's partial results cost about as much as a tile).
 void cut_runs(long long units, int bound, int* wpu, int* splits, int* span) {
     const int tiles = (int)div_up(std::max(bound, 1), kAtTile);
     const long long warps = (long long)kSms * 2 * kAtWarps;
     *wpu = 1; *splits = 1;
-    if (tiles > 2 && units < 2 * warps) {
+    const long long share = units * tiles / warps;
+    if (tiles > std::max<long long>(2 * share, units * 10 >= warps ? 16 : 2)) {
         *wpu = kAtWarps;
         const long long want = div_up(2 * kSms, std::max<long long>(units, 1));
         *splits = (int)std::max<long long>(1, std::min<long long>(want, div_up(tiles, 8)));
@@ -110,7 +111,7 @@ struct AttendPlan { AttendParams p; size_t ml_bytes, bytes; long long ctas, tile
 int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int window, int n_sink, AttendPlan* out) {
     std::memset(out, 0, sizeof(*out));
     AttendParams& p = out->p;
-    const int R = r->dtype == SAN_BF16 ? AttendGeom<__nv_bfloat16>::kRows : AttendGeom<float>::kRows;
+    const int R = kAtRows;
     const long long e = r->dtype == SAN_BF16 ? 2 : 4;
     p.H = r->n_heads; p.Hk = r->n_kv_heads; p.group = r->n_heads / r->n_kv_heads;
     p.n_layers = r->n_layers; p.n_items = r->n_items;
