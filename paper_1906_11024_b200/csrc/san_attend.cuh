@@ -12,7 +12,7 @@
 //     sequence's own rows the query rows are the query heads of the key head's group; for a prefix they
 //     are those of every sequence behind the prefix, so that the prefix is read once for all of them.
 //   * A unit is streamed by 1 or 4 warps.  Each warp has a ring of slots of its own in shared memory (32 rows
-//     of one plane each), filled by 16-byte cp.async two slots ahead: no barrier between warps until
+//     of one plane each), filled by 16-byte cp.async all but one of the slots ahead: no barrier between warps until
 //     their partial results meet at the end of the unit.
 //   * One pass with the running maximum and sum of the softmax; scores never leave the registers.  bf16
 //     rows go through mma.sync.m16n8k16 with the queries as N.  With one query row seven of eight columns are padding,
@@ -38,13 +38,14 @@ constexpr int kAtMaxLayers = 4;             // layers whose outputs a warp accum
 template <typename T> struct AttendGeom;
 constexpr int kAtRows = 8;                  // query rows of a unit: one N of mma.sync
 constexpr int kAtOutLd = 68;                // floats between the rows of outputs in shared memory (no bank conflicts)
-template <> struct AttendGeom<__nv_bfloat16> { static constexpr int kSlots = 3, kRowBytes = 128; };
-template <> struct AttendGeom<float>         { static constexpr int kSlots = 3, kRowBytes = 256; };
-template <typename T> __host__ __device__ constexpr int attend_warp_bytes() {       // ring; float32: query rows and weights behind it
-    return AttendGeom<T>::kSlots * kAtTile * AttendGeom<T>::kRowBytes +
+template <> struct AttendGeom<__nv_bfloat16> { static constexpr int kRowBytes = 128; };
+template <> struct AttendGeom<float>         { static constexpr int kRowBytes = 256; };
+// N: slots of a warp's ring.
+template <typename T, int N> __host__ __device__ constexpr int attend_warp_bytes() {       // ring; float32: query rows and weights behind it
+    return N * kAtTile * AttendGeom<T>::kRowBytes +
            (sizeof(T) == 4 ? kAtRows * kDh * 4 + kAtTile * kAtRows * 4 : 0);
 }
-template <typename T> __host__ __device__ constexpr int attend_smem_bytes() { return kAtWarps * (attend_warp_bytes<T>() + 2 * kAtRows * 4); }
+template <typename T, int N> __host__ __device__ constexpr int attend_smem_bytes() { return kAtWarps * (attend_warp_bytes<T, N>() + 2 * kAtRows * 4); }
 
 struct AttendParams {
     const char* q; char* out;
@@ -175,7 +176,7 @@ __device__ __forceinline__ void attend_fill(const AttendRun& u, int begin, int e
 // Where a unit's row goes, and the meeting of the warps of a unit.  Every warp of the CTA calls this (it
 // holds CTA barriers).  In shared memory: per warp [layers][kRows][64] outputs at `own`, (max, sum) per row at
 // `ml`; warps of a unit are neighbours.
-template <typename T>
+template <typename T, int N>
 __device__ __forceinline__ void attend_finish(const AttendParams& p, const AttendRun& u, bool active, int wpu, char* smem,
                                               const float2* ml, int warp, int lane) {
     constexpr int R = kAtRows;
@@ -207,7 +208,7 @@ __device__ __forceinline__ void attend_finish(const AttendParams& p, const Atten
 #pragma unroll
             for (int w = 0; w < kAtWarps; ++w) {
                 if (w >= wpu || weight[w] == 0.f) continue;
-                const float4 x = *reinterpret_cast<const float4*>(smem + (w0 + w) * attend_warp_bytes<T>() + ((y * R + i) * kAtOutLd + (t & 15) * 4) * 4);
+                const float4 x = *reinterpret_cast<const float4*>(smem + (w0 + w) * attend_warp_bytes<T, N>() + ((y * R + i) * kAtOutLd + (t & 15) * 4) * 4);
                 o.x += weight[w] * x.x; o.y += weight[w] * x.y; o.z += weight[w] * x.z; o.w += weight[w] * x.w;
             }
             const int layer = u.layer0 + y;
@@ -225,10 +226,10 @@ __device__ __forceinline__ void attend_finish(const AttendParams& p, const Atten
     }
 }
 
-// Walks a warp's tiles: fill(slot index, ...) runs kSlots - 1 slots ahead of use.  The slots of a tile are its
-// keys and then the values of each layer.
-template <typename T> struct AttendRing {
-    static constexpr int N = AttendGeom<T>::kSlots, SB = kAtTile * AttendGeom<T>::kRowBytes;
+// Walks a warp's tiles: fill() runs N - 1 slots ahead of use.  The slots of a tile are its keys and then the
+// values of each layer.
+template <typename T, int N> struct AttendRing {
+    static constexpr int SB = kAtTile * AttendGeom<T>::kRowBytes;
     const AttendRun& u; uint32_t ring; int lane, step;      // step: positions between this warp's tiles
     int f_at, f_plane, f_slot, r_slot;
     __device__ __forceinline__ AttendRing(const AttendRun& run, uint32_t smem, int ln, int first, int stp)
@@ -257,10 +258,10 @@ template <typename T> struct AttendRing {
 
 // bf16, up to eight query rows, which are the N side of both products: scores D[16 positions x 8 queries] with
 // the key rows as A, outputs D[16 dims x 8 queries] with the value rows, transposed by ldmatrix, as A.
-template <int LG>
+template <int LG, int N>
 __device__ __forceinline__ void attend_warp_bf16(const AttendParams& p, const AttendRun& u, int first, int step, char* smem, float2* ml, int lane) {
     const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(smem);
-    AttendRing<__nv_bfloat16> ring(u, ring_addr, lane, first, step);
+    AttendRing<__nv_bfloat16, N> ring(u, ring_addr, lane, first, step);
     const int g = lane >> 2, t4 = lane & 3;
     uint32_t qb[4][2];                                       // B: query g, dims 16 c + 2 t4 .. and 8 further on
     {
@@ -384,11 +385,11 @@ __device__ __forceinline__ void attend_warp_bf16(const AttendParams& p, const At
 }
 
 // float32, up to R query rows on the CUDA cores.
-template <int LG, int R>
+template <int LG, int R, int N>
 __device__ __forceinline__ void attend_warp_f32(const AttendParams& p, const AttendRun& u, int first, int step, char* smem, float2* ml, int lane) {
     constexpr int RMAX = kAtRows;
-    AttendRing<float> ring(u, (uint32_t)__cvta_generic_to_shared(smem), lane, first, step);
-    float* qs = reinterpret_cast<float*>(smem + AttendGeom<float>::kSlots * kAtTile * 256);      // [R][64]
+    AttendRing<float, N> ring(u, (uint32_t)__cvta_generic_to_shared(smem), lane, first, step);
+    float* qs = reinterpret_cast<float*>(smem + N * kAtTile * 256);      // [R][64]
     float* ws = qs + RMAX * kDh;                                                                // [32][R] weights
     for (int i = 0; i < R; ++i) {
         const bool real = i < u.rows;
@@ -535,7 +536,7 @@ __device__ __forceinline__ bool attend_unit(const AttendParams& p, bool prefix, 
     return true;
 }
 
-template <typename T, int LG>
+template <typename T, int LG, int N>
 __global__ void __launch_bounds__(kAtWarps * 32) attend_kernel(const __grid_constant__ AttendParams p) {
     extern __shared__ __align__(128) char attend_smem[];
     asm volatile("griddepcontrol.launch_dependents;");
@@ -544,21 +545,21 @@ __global__ void __launch_bounds__(kAtWarps * 32) attend_kernel(const __grid_cons
     const bool prefix = (int)blockIdx.x < p.p_ctas;
     const int wpu = prefix ? p.p_wpu : p.o_wpu;
     const int cta = prefix ? (int)blockIdx.x : (int)blockIdx.x - p.p_ctas;
-    float2* ml = reinterpret_cast<float2*>(attend_smem + kAtWarps * attend_warp_bytes<T>());
+    float2* ml = reinterpret_cast<float2*>(attend_smem + kAtWarps * attend_warp_bytes<T, N>());
     AttendRun u;
     const bool active = attend_unit<T>(p, prefix, cta * (kAtWarps / wpu) + warp / wpu, warp % wpu == 0 && lane == 0, &u);
     if (active) {
-        char* smem = attend_smem + warp * attend_warp_bytes<T>();
+        char* smem = attend_smem + warp * attend_warp_bytes<T, N>();
         const int first = u.begin + (warp % wpu) * kAtTile, step = wpu * kAtTile;
         if constexpr (sizeof(T) == 2) {
-            attend_warp_bf16<LG>(p, u, first, step, smem, ml + warp * R, lane);
+            attend_warp_bf16<LG, N>(p, u, first, step, smem, ml + warp * R, lane);
         } else {
-            if (u.rows <= 1) attend_warp_f32<LG, 1>(p, u, first, step, smem, ml + warp * R, lane);
-            else if (u.rows <= 4) attend_warp_f32<LG, 4>(p, u, first, step, smem, ml + warp * R, lane);
-            else attend_warp_f32<LG, 8>(p, u, first, step, smem, ml + warp * R, lane);
+            if (u.rows <= 1) attend_warp_f32<LG, 1, N>(p, u, first, step, smem, ml + warp * R, lane);
+            else if (u.rows <= 4) attend_warp_f32<LG, 4, N>(p, u, first, step, smem, ml + warp * R, lane);
+            else attend_warp_f32<LG, 8, N>(p, u, first, step, smem, ml + warp * R, lane);
         }
     }
-    attend_finish<T>(p, u, active, wpu, attend_smem, ml, warp, lane);
+    attend_finish<T, N>(p, u, active, wpu, attend_smem, ml, warp, lane);
 }
 
 // Adds up the partial results of a row and layer: 16 threads for its outputs, four each, times G groups that

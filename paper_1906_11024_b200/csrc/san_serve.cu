@@ -87,20 +87,18 @@ int32_t check_prefix(const san_cached_rows* r, const san_shared_prefix* x) {
     return SAN_OK;
 }
 
-// How one kind of units is cut: warps per unit and runs of tiles.
-// A warp takes a whole run where the runs are short or no longer than twice a warp's share of the work;
-// otherwise the four warps of a CTA share a run, and a long one is cut into several until the SMs have
-// two CTAs each, but not below eight tiles (a run's partial results cost about as much as a tile).
-void cut_runs(long long units, int bound, int* wpu, int* splits, int* span) {
-    const int tiles = (int)div_up(std::max(bound, 1), kAtTile);
-    const long long warps = (long long)kSms * 2 * kAtWarps;
-    *wpu = 1; *splits = 1;
-    const long long share = units * tiles / warps;
-    if (tiles > std::max<long long>(2 * share, units * 10 >= warps ? 16 : 2)) {
-        *wpu = kAtWarps;
-        const long long want = div_up(2 * kSms, std::max<long long>(units, 1));
-        *splits = (int)std::max<long long>(1, std::min<long long>(want, div_up(tiles, 8)));
-    }
+// How one kind of units (`units` runs of up to `tiles` tiles) is cut where a warp's share of the whole call is
+// `share` tiles: warps per unit and runs of tiles.  A run of no more than 1.25 shares (or `least` tiles) is one warp's.  A longer
+// one is cut into up to four runs for a warp each, so that the warps finish together; beyond that the four
+// warps of a CTA take a run together, which leaves a quarter of the partial results.  Measured (device time): 32 prefixes of 16
+// tiles beside 1024 rows of up to 8, share 10: 48.6 us uncut, 35.9 in two runs each; 1024 runs of 17 tiles, share 15: 53.4 us
+// uncut, 58.7 by four warps each; 8 runs of 513 tiles: 13.0 us by four warps, 17.7 by one.
+// `least`: tiles below which a cut costs more than it gives (a float32 tile of eight rows is several bf16 ones' work).
+void cut_runs(int tiles, double share, int least, int* wpu, int* splits, int* span) {
+    const int most = std::max(least, (int)std::ceil(1.25 * share));
+    const int pieces = (int)div_up(tiles, most);
+    *wpu = pieces > 4 ? kAtWarps : 1;
+    *splits = pieces > 4 ? (int)div_up(pieces, kAtWarps) : pieces;
     *span = (int)div_up(tiles, *splits);
     *splits = (int)div_up(tiles, *span);
 }
@@ -130,30 +128,35 @@ int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int wi
             p.t_n_lg = (int)div_up(r->n_layers, kTileMaxLayers);
             p.t_lg = (int)div_up(r->n_layers, p.t_n_lg);
             p.t_n_lg = (int)div_up(r->n_layers, p.t_lg);
-            p.p_row_tiles = (int)div_up(rows, kTileQ);
-            // runs of chunks: as many as fill the SMs' two CTAs once, of four chunks or more
+            p.p_row_tiles = (int)div_up(rows, 2 * kTileQ);
+            // runs of chunks: as many as fill the SMs once, of two chunks or more
             const long long units = (long long)p.n_prefix * p.p_row_tiles * p.Hk * p.t_n_lg, chunks = div_up(p.max_prefix, kTileK);
-            const long long want = std::max<long long>(1, std::min<long long>(2 * kSms / std::max<long long>(units, 1), div_up(chunks, 4)));
+            const long long want = std::max<long long>(1, std::min<long long>(kSms / std::max<long long>(units, 1), div_up(chunks, 2)));
             p.p_span = (int)div_up(chunks, want);
             p.p_splits = (int)div_up(chunks, p.p_span);
             out->tiles = units * p.p_splits;
             if (out->tiles > 0x7fffffffLL) return SAN_ERR_SHAPE;
         }
     }
+    p.o_row_tiles = (int)div_up(p.group, R);
+    const long long bound = window > 0 ? std::min<long long>(p.max_len, (long long)window + n_sink) : p.max_len;
+    const long long o_runs = (long long)r->n_items * p.o_row_tiles * p.Hk * p.n_lg, o_tiles = std::max<long long>(1, div_up(bound, kAtTile));
+    long long p_runs = 0, p_tiles = 0;
     if (p.n_prefix > 0 && p.t_lg == 0) {
         p.p_row_tiles = (int)div_up((long long)p.max_group * p.group, R);
-        const long long units = (long long)p.n_prefix * p.p_row_tiles * p.Hk * p.n_lg;
-        cut_runs(units, p.max_prefix, &p.p_wpu, &p.p_splits, &p.p_span);
-        if (units * p.p_splits > 0x7fffffffLL) return SAN_ERR_SHAPE;
-        p.p_units = (int)(units * p.p_splits);
+        p_runs = (long long)p.n_prefix * p.p_row_tiles * p.Hk * p.n_lg;
+        p_tiles = div_up(p.max_prefix, kAtTile);
+    }
+    const double share = ((double)o_runs * o_tiles + (double)p_runs * p_tiles) / ((double)kSms * 2 * kAtWarps);
+    if (p_runs > 0) {
+        cut_runs((int)p_tiles, share, e == 4 ? 2 : 4, &p.p_wpu, &p.p_splits, &p.p_span);
+        if (p_runs * p.p_splits > 0x7fffffffLL) return SAN_ERR_SHAPE;
+        p.p_units = (int)(p_runs * p.p_splits);
         p.p_ctas = (int)div_up(p.p_units, kAtWarps / p.p_wpu);
     }
-    p.o_row_tiles = (int)div_up(p.group, R);
-    const long long units = (long long)r->n_items * p.o_row_tiles * p.Hk * p.n_lg;
-    const long long bound = window > 0 ? std::min<long long>(p.max_len, (long long)window + n_sink) : p.max_len;
-    cut_runs(units, (int)bound, &p.o_wpu, &p.o_splits, &p.o_span);
-    if (units * p.o_splits > 0x7fffffffLL) return SAN_ERR_SHAPE;
-    p.o_units = (int)(units * p.o_splits);
+    cut_runs((int)o_tiles, share, 4, &p.o_wpu, &p.o_splits, &p.o_span);
+    if (o_runs * p.o_splits > 0x7fffffffLL) return SAN_ERR_SHAPE;
+    p.o_units = (int)(o_runs * p.o_splits);
     p.slots = p.p_splits + p.o_splits;
     const size_t rows = (size_t)r->n_items * r->n_heads;
     if (p.slots > 1) {
@@ -166,19 +169,26 @@ int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int wi
     return SAN_OK;
 }
 
-template <typename T, int LG>
+template <typename T, int LG, int N>
 int32_t launch_attend_as(const AttendPlan& a, cudaStream_t st) {
-    constexpr int smem = attend_smem_bytes<T>();
-    const int32_t rc = opt_in((const void*)attend_kernel<T, LG>, smem);
+    constexpr int smem = attend_smem_bytes<T, N>();
+    const int32_t rc = opt_in((const void*)attend_kernel<T, LG, N>, smem);
     if (rc != SAN_OK) return rc;
-    attend_kernel<T, LG><<<(unsigned)a.ctas, kAtWarps * 32, smem, st>>>(a.p);
+    attend_kernel<T, LG, N><<<(unsigned)a.ctas, kAtWarps * 32, smem, st>>>(a.p);
     if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
     if (a.p.slots == 1) return SAN_OK;
     const long long rows = (long long)a.p.n_items * a.p.H;
-    const int groups = a.p.slots <= 3 ? 1 : a.p.slots <= 12 ? 4 : 16;
+    const int groups = a.p.slots <= 6 ? 1 : a.p.slots <= 12 ? 4 : 16;
     const dim3 grid((unsigned)div_up(rows, 16 / groups), (unsigned)a.p.n_layers);
     return launch_after(groups == 1 ? &attend_join_kernel<T, 1> : groups == 4 ? &attend_join_kernel<T, 4> : &attend_join_kernel<T, 16>,
                         grid, 256, st, a.p);
+}
+// Slots of a warp's ring: what fits the shared memory of an SM (14 slots of a CTA's four warps) with the CTAs that it
+// will hold; a warp's chain of slots is the faster the more of them are on their way.
+template <typename T, int LG>
+int32_t launch_attend_with(const AttendPlan& a, cudaStream_t st) {
+    if constexpr (sizeof(T) == 4) return launch_attend_as<T, LG, 3>(a, st);
+    else return a.ctas <= 2 * kSms ? launch_attend_as<T, LG, 6>(a, st) : a.ctas <= 3 * kSms ? launch_attend_as<T, LG, 4>(a, st) : launch_attend_as<T, LG, 3>(a, st);
 }
 template <class Mode, int LG, class P>
 int32_t launch_tiles(const P& p, dim3 grid, cudaStream_t st) {
@@ -196,7 +206,7 @@ int32_t launch_attend(const AttendPlan& a, cudaStream_t st) {
         const int32_t rc = a.p.t_lg == 1 ? launch_tiles<TilePrefix, 1>(a.p, grid, st) : launch_tiles<TilePrefix, 2>(a.p, grid, st);
         if (rc != SAN_OK) return rc;
     }
-    return a.p.lg == 1 ? launch_attend_as<T, 1>(a, st) : a.p.lg == 2 ? launch_attend_as<T, 2>(a, st) : launch_attend_as<T, 4>(a, st);
+    return a.p.lg == 1 ? launch_attend_with<T, 1>(a, st) : a.p.lg == 2 ? launch_attend_with<T, 2>(a, st) : launch_attend_with<T, 4>(a, st);
 }
 
 int32_t run_attend(const san_cached_rows* r, const san_shared_prefix* x, int window, int n_sink, void* ws, size_t ws_bytes, void* stream) {
@@ -354,7 +364,7 @@ int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int
     p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)kDh));
     if ((long long)n_seq * p.n_lg > 65535) return SAN_ERR_SHAPE;
     if (max_len >= kTileQ) {
-        const dim3 tiles((unsigned)div_up(max_len, kTileQ), (unsigned)n_heads, (unsigned)(n_seq * p.n_lg));
+        const dim3 tiles((unsigned)div_up(max_len, 2 * kTileQ), (unsigned)n_heads, (unsigned)(n_seq * p.n_lg));
         cudaStream_t st = static_cast<cudaStream_t>(stream);
         return p.lg == 1 ? launch_tiles<TileWindow, 1>(p, tiles, st) : launch_tiles<TileWindow, 2>(p, tiles, st);
     }

@@ -3,19 +3,24 @@
 // keys that a row sees, once per block (Eq. 1, Eq. 3), O_l = S.V_l for each layer (Eq. 2, Eq. 4), in one pass with a
 // running maximum.
 //
-// CTA = 128 query rows x (key head, up to kTileMaxLayers layers, a run of keys).  Keys come in chunks of 64; per chunk one
-// tcgen05.mma chain writes the scores (M 128, N 64, K 64) into one of two score buffers in tensor memory, and
-// one adds weights x values (N = 64 x layers) to the outputs, which stay in tensor memory.  Roles:
-//   warps 0-3  softmax: thread = query row = tensor-memory lane, so maxima and sums need no shuffles.  Weights go to
-//              shared memory in bf16 as the A operand of the second product.  The maximum that the weights are
-//              taken against moves only when a row's own has grown by more than 2^8, since then the
-//              outputs have to be read, scaled and written back; the sum uses the same one, so nothing is lost.
-//   warps 4-6  copies: 16-byte cp.async into operand tiles (rows of 128 bytes, chunks XOR-swizzled by row & 7, what
-//              the matrix descriptors name), up to three chunks ahead; rows past the end are zeros.
-//   warp 7     one thread issues the MMAs: scores of chunk t + 1 before outputs of chunk t, so that the tensor cores
-//              work on them while the softmax warps work on chunk t.
-// What bounds it: the exponentials, 64 per row and chunk at 16 per clock and SM (512 clocks a chunk against 384
-// of tensor core with two layers); two CTAs share an SM (up to two layers each) and fill each other's waits.
+// CTA = two tiles of 128 query rows x (key head, up to kTileMaxLayers layers, a run of keys).  Keys come in chunks of 128
+// that both tiles use; per tile and chunk one tcgen05.mma chain writes the scores (M 128, N 128, K 64) into tensor
+// memory, and one adds weights x values (N = 64 x layers, K 128) to the outputs, which stay there.  Roles:
+//   warps 0-3, 4-7  softmax of one tile each: thread = query row = tensor-memory lane, so maxima and sums need no shuffles.
+//              The weights go back to tensor memory in bf16, over the scores, as the A operand of the second
+//              product.  The maximum that the weights are taken against moves only when a row's own has grown by
+//              more than 2^8, since then the outputs have to be read, scaled and written back; the sum uses the
+//              same one, so nothing is lost.
+//   warps 8-10 copies: 16-byte cp.async into operand tiles (rows of 128 bytes, chunks XOR-swizzled by row & 7, what
+//              the matrix descriptors name), keys up to three chunks ahead, values two; rows past the end are zeros.
+//   warp 11    one thread issues the MMAs, the tiles in turn: outputs of a tile's last chunk, then its next scores, so
+//              that the tensor cores work for one tile while the other one's softmax runs.  MMAs of a thread
+//              complete in order: scores that have arrived mean that the outputs before them are complete
+//              and that the weights they replace have been read.
+// What bounds it: the exponentials, 2048 clocks for 256 rows x 128 keys at 16 per clock and SM, against 1536 of tensor
+// core with two layers.  With 64-key chunks and weights in shared memory (two CTAs per SM) operand reads, weight
+// writes and copies took 96 KB of shared-memory traffic per 64 keys and 128 rows, 750 clocks, and two prompts
+// of 8192 positions with a window of 1024 took 111 us.
 // Every wait is bounded: one that runs out raises a flag that ends the CTA's other waits, the CTA frees its tensor
 // memory and leaves its rows unwritten (reported where there is a status word).
 #pragma once
@@ -25,11 +30,11 @@
 
 namespace san {
 
-constexpr int kTileQ = 128, kTileK = 64, kTileThreads = 256, kTileLoaders = 96;
-constexpr int kTileSlots = 3, kTileMaxLayers = 2;     // slots of the key ring and of the value ring
+constexpr int kTileQ = 128, kTileK = 128, kTileThreads = 384, kTileLoaders = 96;
+constexpr int kTileKSlots = 3, kTileVSlots = 2, kTileMaxLayers = 2;
 constexpr int TAG_TILE = 11;
 __host__ __device__ constexpr int tile_smem_bytes(int layers) {
-    return 1024 + kTileQ * 128 * 2 + kTileSlots * (1 + layers) * kTileK * 128;
+    return 1024 + 2 * kTileQ * 128 + (kTileKSlots + kTileVSlots * layers) * kTileK * 128;
 }
 
 __device__ __forceinline__ uint32_t tile_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -68,6 +73,11 @@ __device__ __forceinline__ uint32_t tile_idesc(bool b_mn, int n) {
 __device__ __forceinline__ void tile_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
                  :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u) : "memory");
+}
+// A in tensor memory: lane = row, a column holds two neighbouring elements of K.
+__device__ __forceinline__ void tile_mma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u) : "memory");
 }
 __device__ __forceinline__ void tile_commit(uint64_t* bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(tile_u32(bar)) : "memory");
@@ -130,7 +140,7 @@ struct TileWork {
     const char* k; const char* v;
     long long row_bytes, v_stride;          // bytes between rows, between layers
     int ns, lo, begin, end;
-    int rows, layer0, layers;
+    int rows, layer0, layers;               // query rows, up to two tiles of them
 };
 
 // ---- windowed prompts: grid (query tiles, heads, sequences x layer groups)
@@ -142,9 +152,9 @@ struct TileWindow {
         w->layer0 = blockIdx.z % p.n_lg * p.lg;
         w->layers = min(p.lg, p.n_layers - w->layer0);
         len = max(0, min(p.lens[seq], p.max_len));
-        a0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kTileQ;
+        a0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * 2 * kTileQ;
         if (a0 >= len) return false;
-        w->rows = min(kTileQ, len - a0);
+        w->rows = min(2 * kTileQ, len - a0);
         w->lo = max(0, a0 - p.window + 1);
         w->ns = min(p.n_sink, w->lo);
         w->begin = 0;
@@ -159,19 +169,25 @@ struct TileWindow {
     __device__ __forceinline__ const uint4* query(int i) const {
         return reinterpret_cast<const uint4*>(p.q + (((long long)seq * p.cap + a0 + i) * p.H + head) * kDh);
     }
-    // Of chunk [c0, c0 + 64) of the visible keys, those that row i sees: bit j for number c0 + j.
-    __device__ __forceinline__ bool all_seen(const TileWork& w, int c0) const {
-        return c0 >= w.ns && c0 + kTileK <= w.end && w.lo + c0 - w.ns + kTileK - 1 <= a0 && w.lo + c0 - w.ns > a0 + kTileQ - 1 - p.window;
+    // Of chunk [c0, c0 + 128) of the visible keys: whether any row of tile x sees a part of it, whether all see all of
+    // it, and those of columns 32 q .. 32 q + 31 that row i sees.
+    __device__ __forceinline__ bool any_seen(const TileWork& w, int c0, int x) const {
+        const int first = a0 + x * kTileQ, last = min(first + kTileQ, a0 + w.rows) - 1;
+        if (last < first || c0 > w.ns + last - w.lo) return false;
+        return c0 < w.ns + max(0, p.n_sink - w.lo) || c0 + kTileK > w.ns + max(first - p.window + 1, w.lo) - w.lo;
     }
-    __device__ __forceinline__ unsigned long long seen(const TileWork& w, int c0, int i) const {
-        auto below = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };      // bits 0 .. n - 1
+    __device__ __forceinline__ bool all_seen(const TileWork& w, int c0, int x) const {
+        const int first = a0 + x * kTileQ, key = w.lo + c0 - w.ns;
+        return c0 >= w.ns && c0 + kTileK <= w.end && key + kTileK - 1 <= first && key > first + kTileQ - 1 - p.window;
+    }
+    __device__ __forceinline__ uint32_t seen(const TileWork& w, int c0, int i, int q) const {
+        auto below = [&](int n) { n -= c0 + 32 * q; return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; };      // of numbers below n
         const int a = a0 + i, self = w.ns + a - w.lo;                   // the row's own number
-        const int sinks = w.ns + max(0, p.n_sink - w.lo);               // numbers below it are sinks (or behind the row)
-        const unsigned long long recent = ~below(w.ns + max(a - p.window + 1, w.lo) - w.lo - c0);
-        return (recent | below(sinks - c0)) & below(min(self + 1, w.end) - c0);
+        const uint32_t recent = ~below(w.ns + max(a - p.window + 1, w.lo) - w.lo);
+        return (recent | below(w.ns + max(0, p.n_sink - w.lo))) & below(min(self + 1, w.end));
     }
-    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, int i, float m, float l, bool ok) const {
-        const bool mine = ok && i < w.rows;
+    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, int i, float m, float l) const {
+        const bool mine = i < w.rows;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         bool odd = false;
 #pragma unroll
@@ -218,8 +234,8 @@ struct TilePrefix {
             if (threadIdx.x == 0 && tile == 0 && split == 0 && hk == 0 && lg == 0) prefix_report(p, g);
             return false;
         }
-        row0 = tile * kTileQ;
-        w->rows = min(kTileQ, (p.first[g + 1] - p.first[g]) * p.group - row0);
+        row0 = tile * 2 * kTileQ;
+        w->rows = min(2 * kTileQ, (p.first[g + 1] - p.first[g]) * p.group - row0);
         if (w->rows <= 0) return false;
         w->layer0 = lg * p.t_lg;
         w->layers = min(p.t_lg, p.n_layers - w->layer0);
@@ -239,13 +255,15 @@ struct TilePrefix {
         return (long long)(p.first[g] + row / p.group) * p.H + hk * p.group + row % p.group;
     }
     __device__ __forceinline__ const uint4* query(int i) const { return reinterpret_cast<const uint4*>(p.q + place(i) * 128); }
-    __device__ __forceinline__ bool all_seen(const TileWork& w, int c0) const { return c0 + kTileK <= w.end; }
-    __device__ __forceinline__ unsigned long long seen(const TileWork& w, int c0, int) const {
-        return w.end - c0 >= 64 ? ~0ull : (1ull << (w.end - c0)) - 1;
+    __device__ __forceinline__ bool any_seen(const TileWork& w, int, int x) const { return x * kTileQ < w.rows; }
+    __device__ __forceinline__ bool all_seen(const TileWork& w, int c0, int) const { return c0 + kTileK <= w.end; }
+    __device__ __forceinline__ uint32_t seen(const TileWork& w, int c0, int, int q) const {
+        const int n = w.end - c0 - 32 * q;
+        return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1;
     }
-    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, int i, float m, float l, bool ok) const {
+    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, int i, float m, float l) const {
         const long long n_rows = (long long)p.n_items * p.H, at = i < w.rows ? place(i) : 0;
-        const bool mine = ok && i < w.rows;
+        const bool mine = i < w.rows;
         if (mine && w.layer0 == 0) p.part_ml[slot * n_rows + at] = make_float2(m, l);
         if (w.begin == w.end) return;                                   // nothing there: the join does not look at the outputs
 #pragma unroll
@@ -270,11 +288,11 @@ struct TilePrefix {
 };
 
 template <class Mode, int LG, class Params>
-__global__ void __launch_bounds__(kTileThreads, 2) tile_kernel(const __grid_constant__ Params params) {
-    constexpr uint32_t kCols = 256;                                     // scores 2 x 64, outputs 64 x LG
-    static_assert(128 + 64 * LG <= (int)kCols, "tensor memory");
+__global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_constant__ Params params) {
+    constexpr uint32_t kCols = 512, kTileCols = 256, kOut = 128;        // a tile's columns: scores (weights over them), outputs
+    static_assert(kOut + 64 * LG <= kTileCols, "tensor memory");
     extern __shared__ __align__(1024) char tile_smem[];
-    __shared__ __align__(8) uint64_t k_full[kTileSlots], k_free[kTileSlots], v_full[kTileSlots], pv_done[kTileSlots], s_full[2], s_free[2], p_full[1];
+    __shared__ __align__(8) uint64_t k_full[kTileKSlots], k_free[kTileKSlots], v_full[kTileVSlots], v_free[kTileVSlots], s_full[2], p_full[2], done[2];
     __shared__ uint32_t tmem_s;
     __shared__ int dead_s;
     asm volatile("griddepcontrol.launch_dependents;");
@@ -283,26 +301,21 @@ __global__ void __launch_bounds__(kTileThreads, 2) tile_kernel(const __grid_cons
     if (!mode.work(&w)) return;                                         // uniform over the CTA, before anything is allocated
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int* dead = &dead_s;
-    char* base = tile_smem + ((1024u - (tile_u32(tile_smem) & 1023u)) & 1023u);
-    char* sQ = base;
-    char* sP = sQ + kTileQ * 128;                                       // weights
-    const uint32_t aK = tile_u32(sP + kTileQ * 128);
-    const uint32_t aV = aK + kTileSlots * kTileK * 128;                 // slots of LG value tiles
+    char* sQ = tile_smem + ((1024u - (tile_u32(tile_smem) & 1023u)) & 1023u);
+    const uint32_t aK = tile_u32(sQ) + 2 * kTileQ * 128;
+    const uint32_t aV = aK + kTileKSlots * kTileK * 128;                // slots of LG value tiles
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kTileSlots; ++i) {
-            tile_bar_init(&k_full[i], kTileLoaders); tile_bar_init(&k_free[i], 1);
-            tile_bar_init(&v_full[i], kTileLoaders); tile_bar_init(&pv_done[i], 1);
-        }
-        for (int i = 0; i < 2; ++i) { tile_bar_init(&s_full[i], 1); tile_bar_init(&s_free[i], 128); }
-        tile_bar_init(&p_full[0], 128);
+        for (int i = 0; i < kTileKSlots; ++i) { tile_bar_init(&k_full[i], kTileLoaders); tile_bar_init(&k_free[i], 1); }
+        for (int i = 0; i < kTileVSlots; ++i) { tile_bar_init(&v_full[i], kTileLoaders); tile_bar_init(&v_free[i], 1); }
+        for (int i = 0; i < 2; ++i) { tile_bar_init(&s_full[i], 1); tile_bar_init(&p_full[i], kTileQ); tile_bar_init(&done[i], 1); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         dead_s = 0;
     }
-    if (warp == 7) {
+    if (warp == 11) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(tile_u32(&tmem_s)), "r"(kCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    if (threadIdx.x < 128) {
+    if (threadIdx.x < 2 * kTileQ) {
         const int i = threadIdx.x;
         const uint4* src = i < w.rows ? mode.query(i) : nullptr;
 #pragma unroll
@@ -315,60 +328,71 @@ __global__ void __launch_bounds__(kTileThreads, 2) tile_kernel(const __grid_cons
     tile_after_sync();
     const uint32_t tmem = tmem_s;
     const int chunks = (w.end - w.begin + kTileK - 1) / kTileK;
-    float m = -INFINITY, l = 0.f;
-    bool ok = true;
 
-    if (warp == 7) {
+    if (warp == 11) {
         if (lane == 0) {
-            const uint64_t dQ = tile_desc(tile_u32(sQ));
             const uint32_t id_s = tile_idesc(false, kTileK), id_o = tile_idesc(true, w.layers * kDh);
-            auto scores = [&](int t) -> bool {
-                if (!tile_wait(&k_full[t % kTileSlots], (uint32_t)(t / kTileSlots) & 1u, dead)) return false;
-                if (t >= 2 && !tile_wait(&s_free[t & 1], (uint32_t)((t - 2) >> 1) & 1u, dead)) return false;
+            int count[2] = {0, 0}, pending[2] = {-1, -1};               // chunks whose weights a tile has delivered; the one that it works on
+            auto outputs = [&](int x) -> bool {
+                const int t = pending[x], slot = t % kTileVSlots;
+                if (!tile_wait(&v_full[slot], (uint32_t)(t / kTileVSlots) & 1u, dead)) return false;
+                if (!tile_wait(&p_full[x], (uint32_t)count[x] & 1u, dead)) return false;
                 tile_proxy_fence();                                     // the copies are writes of the generic proxy
                 tile_after_sync();
-                const uint64_t dK = tile_desc(aK + (uint32_t)(t % kTileSlots) * (kTileK * 128));
+                const uint64_t dV = tile_desc(aV + (uint32_t)(slot * LG) * (kTileK * 128), kTileK * 128);
+                const uint32_t base = tmem + (uint32_t)x * kTileCols;
 #pragma unroll
-                for (int s = 0; s < 4; ++s) tile_mma(tmem + (t & 1) * 64, dQ + 2 * s, dK + 2 * s, id_s, s > 0);
-                tile_commit(&s_full[t & 1]);
-                tile_commit(&k_free[t % kTileSlots]);
+                for (int s = 0; s < kTileK / 16; ++s) tile_mma_ta(base + kOut, base + 8 * s, dV + 128 * s, id_o, count[x] > 0 || s > 0);
+                ++count[x];
+                pending[x] = -1;
                 return true;
             };
-            const uint64_t dP = tile_desc(tile_u32(sP));
-            auto outputs = [&](int t) -> bool {
-                if (!tile_wait(&v_full[t % kTileSlots], (uint32_t)(t / kTileSlots) & 1u, dead)) return false;
-                if (!tile_wait(&p_full[0], (uint32_t)t & 1u, dead)) return false;
+            bool go = true;
+            for (int t = 0; t < chunks && go; ++t) {
+                const int slot = t % kTileKSlots;
+                go = tile_wait(&k_full[slot], (uint32_t)(t / kTileKSlots) & 1u, dead);
                 tile_proxy_fence();
                 tile_after_sync();
-                const uint64_t dV = tile_desc(aV + (uint32_t)(t % kTileSlots) * (LG * kTileK * 128), kTileK * 128);
+                const uint64_t dK = tile_desc(aK + (uint32_t)slot * (kTileK * 128));
+                for (int x = 0; x < 2 && go; ++x) {
+                    if (pending[x] >= 0) go = outputs(x);
+                    if (!go || !mode.any_seen(w, w.begin + t * kTileK, x)) continue;
+                    const uint64_t dQ = tile_desc(tile_u32(sQ) + (uint32_t)x * (kTileQ * 128));
 #pragma unroll
-                for (int s = 0; s < 4; ++s) tile_mma(tmem + 128, dP + 2 * s, dV + 128 * s, id_o, t > 0 || s > 0);
-                tile_commit(&pv_done[t % kTileSlots]);
-                return true;
-            };
-            bool go = chunks == 0 || scores(0);
-            for (int t = 0; t < chunks && go; ++t) go = (t + 1 >= chunks || scores(t + 1)) && outputs(t);
+                    for (int s = 0; s < 4; ++s) tile_mma(tmem + (uint32_t)x * kTileCols, dQ + 2 * s, dK + 2 * s, id_s, s > 0);
+                    tile_commit(&s_full[x]);
+                    pending[x] = t;
+                }
+                if (!go) break;
+                tile_commit(&k_free[slot]);                             // both tiles' scores of chunk t
+                if (t > 0) tile_commit(&v_free[(t - 1) % kTileVSlots]); // and their outputs of chunk t - 1
+            }
+            for (int x = 0; x < 2 && go; ++x) {
+                if (pending[x] >= 0) go = outputs(x);
+                if (go) tile_commit(&done[x]);
+            }
         }
-    } else if (warp >= 4) {
+    } else if (warp >= 8) {
         // thread: 16-byte piece c of rows r0, r0 + 12, ...
-        static_assert(kTileLoaders == 96 && kTileK == 64, "rows of a thread");
-        const int r0 = (threadIdx.x - 128) >> 3, c = threadIdx.x & 7;
+        constexpr int kRows = (kTileK + 11) / 12;
+        static_assert(kTileLoaders == 96, "rows of a thread");
+        const int r0 = (threadIdx.x - 2 * kTileQ) >> 3, c = threadIdx.x & 7;
         const uint32_t sw0 = (uint32_t)(r0 * 128 + ((c ^ (r0 & 7)) << 4)), sw1 = (uint32_t)(r0 * 128 + ((c ^ ((r0 + 4) & 7)) << 4));
         const long long step = 12 * w.row_bytes;
         auto copy = [&](const char* src, uint32_t dst, int c0) {
             const int first = c0 + r0;
-            if (c0 >= w.ns && c0 + kTileK <= w.end) {                   // 64 rows on end
+            if (c0 >= w.ns && c0 + kTileK <= w.end) {                   // rows on end
                 const char* at = src + (long long)(w.lo + first - w.ns) * w.row_bytes + (c << 4);
 #pragma unroll
-                for (int j = 0; j < 6; ++j, at += step)
-                    if (j < 5 || r0 < 4) cp16(dst + (uint32_t)(j * 12 * 128) + (j & 1 ? sw1 : sw0), at, true);
+                for (int j = 0; j < kRows; ++j, at += step)
+                    if (r0 + 12 * j < kTileK) cp16(dst + (uint32_t)(j * 12 * 128) + (j & 1 ? sw1 : sw0), at, true);
             } else {
 #pragma unroll
-                for (int j = 0; j < 6; ++j) {
+                for (int j = 0; j < kRows; ++j) {
                     const int n = first + j * 12;
                     const bool full = n < w.end;
                     const int pos = !full ? 0 : n < w.ns ? n : w.lo + n - w.ns;
-                    if (j < 5 || r0 < 4) cp16(dst + (uint32_t)(j * 12 * 128) + (j & 1 ? sw1 : sw0), src + pos * w.row_bytes + (c << 4), full);
+                    if (r0 + 12 * j < kTileK) cp16(dst + (uint32_t)(j * 12 * 128) + (j & 1 ? sw1 : sw0), src + pos * w.row_bytes + (c << 4), full);
                 }
             }
         };
@@ -377,104 +401,99 @@ __global__ void __launch_bounds__(kTileThreads, 2) tile_kernel(const __grid_cons
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tile_u32(bar)) : "memory");
         };
         for (int t = 0; t < chunks; ++t) {
-            const int c0 = w.begin + t * kTileK, slot = t % kTileSlots;
-            const uint32_t before = (uint32_t)(t / kTileSlots - 1) & 1u;
-            if (t >= kTileSlots && !tile_wait(&k_free[slot], before, dead)) break;
-            copy(w.k, aK + (uint32_t)slot * (kTileK * 128), c0);
-            landed(&k_full[slot]);
-            if (t >= kTileSlots && !tile_wait(&pv_done[slot], before, dead)) break;
-            for (int y = 0; y < w.layers; ++y) copy(w.v + y * w.v_stride, aV + (uint32_t)(slot * LG + y) * (kTileK * 128), c0);
-            landed(&v_full[slot]);
+            const int c0 = w.begin + t * kTileK, ks = t % kTileKSlots, vs = t % kTileVSlots;
+            if (t >= kTileKSlots && !tile_wait(&k_free[ks], (uint32_t)(t / kTileKSlots - 1) & 1u, dead)) break;
+            copy(w.k, aK + (uint32_t)ks * (kTileK * 128), c0);
+            landed(&k_full[ks]);
+            if (t >= kTileVSlots && !tile_wait(&v_free[vs], (uint32_t)(t / kTileVSlots - 1) & 1u, dead)) break;
+            for (int y = 0; y < w.layers; ++y) copy(w.v + y * w.v_stride, aV + (uint32_t)(vs * LG + y) * (kTileK * 128), c0);
+            landed(&v_full[vs]);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
-        const int i = threadIdx.x;
-        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+        const int x = warp >> 2, i = threadIdx.x;                       // tile; query row of the CTA
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)x * kTileCols;
         const float sc = params.scale_log2e;
+        const unsigned long long sc2 = tile_pair(sc, sc);
+        float m = -INFINITY, l = 0.f;
+        bool ok = true;
+        int count = 0;
         for (int t = 0; t < chunks; ++t) {
             const int c0 = w.begin + t * kTileK;
-            ok = __all_sync(0xffffffffu, tile_wait(&s_full[t & 1], (uint32_t)(t >> 1) & 1u, dead));
+            if (!mode.any_seen(w, c0, x)) continue;
+            ok = __all_sync(0xffffffffu, tile_wait(&s_full[x], (uint32_t)count & 1u, dead));
             if (!ok) break;
             tile_after_sync();
-            float z[64];
-            tile_ld32(lanes + (t & 1) * 64, z);
-            tile_ld32(lanes + (t & 1) * 64 + 32, z + 32);
-            tile_wait_ld();
-            tile_before_sync();
-            tile_arrive(&s_free[t & 1]);
-            if (!mode.all_seen(w, c0)) {                                // uniform over the CTA
-                const unsigned long long seen = mode.seen(w, c0, i);
-                const uint32_t s0 = (uint32_t)seen, s1 = (uint32_t)(seen >> 32);
+            const bool whole = mode.all_seen(w, c0, x);                 // uniform over the CTA
+            float z[128];
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    z[j] = s0 >> j & 1u ? z[j] : -INFINITY;
-                    z[32 + j] = s1 >> j & 1u ? z[32 + j] : -INFINITY;
+            for (int q = 0; q < 4; ++q) tile_ld32(lanes + 32 * q, z + 32 * q);
+            tile_wait_ld();
+            if (!whole) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t seen = mode.seen(w, c0, i, q);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) z[32 * q + j] = seen >> j & 1u ? z[32 * q + j] : -INFINITY;
                 }
             }
             float top[4] = {z[0], z[1], z[2], z[3]};
 #pragma unroll
-            for (int j = 4; j < 60; j += 8)
+            for (int j = 4; j < 124; j += 8)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top[e] = tile_max3(top[e], z[j + 2 * e], z[j + 2 * e + 1]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) top[e] = fmaxf(top[e], z[60 + e]);
+            for (int e = 0; e < 4; ++e) top[e] = fmaxf(top[e], z[124 + e]);
             const float m_chunk = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sc;
             // A row that has seen nothing yet has outputs and a sum of zero: its maximum starts here.
             const bool grown = m_chunk > m + 8.f && m > -INFINITY;
             if (m == -INFINITY) m = m_chunk;
-            if (__any_sync(0xffffffffu, grown)) {
-                // (t > 0.)  The outputs of the chunk before are complete, those of this one wait for its weights.
-                ok = __all_sync(0xffffffffu, tile_wait(&pv_done[(t - 1) % kTileSlots], (uint32_t)((t - 1) / kTileSlots) & 1u, dead));
-                if (!ok) break;
-                tile_after_sync();
+            if (__any_sync(0xffffffffu, grown)) {                       // (count > 0)
                 const float f = grown ? fast_exp2(m - m_chunk) : 1.f;
                 if (grown) { m = m_chunk; l *= f; }
                 for (int y = 0; y < 4 * w.layers; ++y) {                // 16 columns at a time: the scores are still held
                     float o[16];
-                    tile_ld16(lanes + 128 + y * 16, o);
+                    tile_ld16(lanes + kOut + y * 16, o);
                     tile_wait_ld();
 #pragma unroll
                     for (int j = 0; j < 16; ++j) o[j] *= f;
-                    tile_st16(lanes + 128 + y * 16, o);
+                    tile_st16(lanes + kOut + y * 16, o);
                 }
-                tile_wait_st();
-                tile_before_sync();
             }
             const float base_m = m == -INFINITY ? 0.f : m;
             unsigned long long sum[2] = {0ull, 0ull};
-            const unsigned long long sc2 = tile_pair(sc, sc), m2 = tile_pair(-base_m, -base_m);
+            const unsigned long long m2 = tile_pair(-base_m, -base_m);
 #pragma unroll
-            for (int j = 0; j < 64; j += 2) {
-                tile_unpair(tile_fma2(tile_pair(z[j], z[j + 1]), sc2, m2), z[j], z[j + 1]);
-                z[j] = fast_exp2(z[j]);
-                z[j + 1] = fast_exp2(z[j + 1]);
-                sum[(j >> 1) & 1] = tile_add2(sum[(j >> 1) & 1], tile_pair(z[j], z[j + 1]));
+            for (int q = 0; q < 4; ++q) {
+                float packed[16];
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) {
+                    float u, v;
+                    tile_unpair(tile_fma2(tile_pair(z[32 * q + j], z[32 * q + j + 1]), sc2, m2), u, v);
+                    u = fast_exp2(u);
+                    v = fast_exp2(v);
+                    sum[(j >> 1) & 1] = tile_add2(sum[(j >> 1) & 1], tile_pair(u, v));
+                    packed[j >> 1] = __uint_as_float(pack_bf16(u, v));
+                }
+                tile_st16(lanes + 16 * q, packed);                      // over scores that have been read
             }
             float sa, sb;
             tile_unpair(tile_add2(sum[0], sum[1]), sa, sb);
             l += sa + sb;
-            if (t >= 1) {                                               // the weight tile is free
-                ok = __all_sync(0xffffffffu, tile_wait(&pv_done[(t - 1) % kTileSlots], (uint32_t)((t - 1) / kTileSlots) & 1u, dead));
-                if (!ok) break;
-            }
-            char* row = sP + i * 128;
-#pragma unroll
-            for (int c = 0; c < 8; ++c)
-                *reinterpret_cast<uint4*>(row + ((c ^ (i & 7)) << 4)) =
-                    make_uint4(pack_bf16(z[8 * c], z[8 * c + 1]), pack_bf16(z[8 * c + 2], z[8 * c + 3]),
-                               pack_bf16(z[8 * c + 4], z[8 * c + 5]), pack_bf16(z[8 * c + 6], z[8 * c + 7]));
-            tile_proxy_fence();
-            tile_arrive(&p_full[0]);
+            tile_wait_st();
+            tile_before_sync();
+            tile_arrive(&p_full[x]);
+            ++count;
         }
-        if (ok && chunks > 0) ok = tile_wait(&pv_done[(chunks - 1) % kTileSlots], (uint32_t)((chunks - 1) / kTileSlots) & 1u, dead);
+        if (ok) ok = tile_wait(&done[x], 0u, dead);
         ok = __all_sync(0xffffffffu, ok);
         tile_after_sync();
-        if (ok) mode.template finish<LG>(w, lanes + 128, i, m, l, true);
+        if (ok) mode.template finish<LG>(w, lanes + kOut, i, m, l);
         else if (threadIdx.x == 0) mode.failed();
     }
     tile_before_sync();
     __syncthreads();
-    if (warp == 7) {
+    if (warp == 11) {
         __syncwarp();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kCols) : "memory");
     }
