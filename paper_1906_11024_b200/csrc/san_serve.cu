@@ -129,9 +129,9 @@ int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int wi
             p.t_lg = (int)div_up(r->n_layers, p.t_n_lg);
             p.t_n_lg = (int)div_up(r->n_layers, p.t_lg);
             p.p_row_tiles = (int)div_up(rows, 2 * kTileQ);
-            // runs of chunks: as many as fill the SMs once, of two chunks or more
+            // runs of chunks: as many as fill the SMs once, of four chunks or more
             const long long units = (long long)p.n_prefix * p.p_row_tiles * p.Hk * p.t_n_lg, chunks = div_up(p.max_prefix, kTileK);
-            const long long want = std::max<long long>(1, std::min<long long>(kSms / std::max<long long>(units, 1), div_up(chunks, 2)));
+            const long long want = std::max<long long>(1, std::min<long long>(kSms / std::max<long long>(units, 1), div_up(chunks, 4)));
             p.p_span = (int)div_up(chunks, want);
             p.p_splits = (int)div_up(chunks, p.p_span);
             out->tiles = units * p.p_splits;

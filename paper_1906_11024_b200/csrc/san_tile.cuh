@@ -3,24 +3,29 @@
 // keys that a row sees, once per block (Eq. 1, Eq. 3), O_l = S.V_l for each layer (Eq. 2, Eq. 4), in one pass with a
 // running maximum.
 //
-// CTA = two tiles of 128 query rows x (key head, up to kTileMaxLayers layers, a run of keys).  Keys come in chunks of 128
-// that both tiles use; per tile and chunk one tcgen05.mma chain writes the scores (M 128, N 128, K 64) into tensor
-// memory, and one adds weights x values (N = 64 x layers, K 128) to the outputs, which stay there.  Roles:
+// CTA = two tiles of 128 query rows x (key head, up to kTileMaxLayers layers, a run of keys).  Keys come in chunks of 64 that
+// both tiles use; per tile and chunk one tcgen05.mma chain writes the scores (M 128, N 64, K 64) into one of
+// the tile's two score buffers in tensor memory, and one adds weights x values (N = 64 x layers, K 64) to the outputs,
+// which stay there.  Roles:
 //   warps 0-3, 4-7  softmax of one tile each: thread = query row = tensor-memory lane, so maxima and sums need no shuffles.
 //              The weights go back to tensor memory in bf16, over the scores, as the A operand of the second
 //              product.  The maximum that the weights are taken against moves only when a row's own has grown by
 //              more than 2^8, since then the outputs have to be read, scaled and written back; the sum uses the
 //              same one, so nothing is lost.
 //   warps 8-10 copies: 16-byte cp.async into operand tiles (rows of 128 bytes, chunks XOR-swizzled by row & 7, what
-//              the matrix descriptors name), keys up to three chunks ahead, values two; rows past the end are zeros.
-//   warp 11    one thread issues the MMAs, the tiles in turn: outputs of a tile's last chunk, then its next scores, so
-//              that the tensor cores work for one tile while the other one's softmax runs.  MMAs of a thread
-//              complete in order: scores that have arrived mean that the outputs before them are complete
-//              and that the weights they replace have been read.
-// What bounds it: the exponentials, 2048 clocks for 256 rows x 128 keys at 16 per clock and SM, against 1536 of tensor
-// core with two layers.  With 64-key chunks and weights in shared memory (two CTAs per SM) operand reads, weight
-// writes and copies took 96 KB of shared-memory traffic per 64 keys and 128 rows, 750 clocks, and two prompts
-// of 8192 positions with a window of 1024 took 111 us.
+//              the matrix descriptors name), keys up to four chunks ahead, values three; rows past the end are zeros.
+//   warp 11    issues the MMAs: both tiles' scores of chunk t + 1, then their outputs of chunk t, so that scores
+//              are there when a softmax warp comes for them.  MMAs of a thread complete in order: scores never
+//              replace weights that have not been read.  All its lanes take the same path and one elected lane
+//              issues, which leaves descriptors and addresses in uniform registers: with a single lane in a
+//              branch the issue alone took 1700 clocks a chunk (now 1000) and bounded the kernel.
+// What bounds it: the softmax warps, one of each tile per SM quarter: 1800 clocks per chunk measured, of which the
+// exponentials of both tiles take 1170 (1024 at 16 per clock and SM), maxima 250, waiting for scores 220; the tensor cores
+// are busy for a third of it.  Tried on top and not faster: taking turns with the exponentials (1690 to 1880),
+// a quarter of them as polynomials on the FMA pipe (1770).  Two prompts of 8192 positions, window 1024, 8
+// heads, 2 layers: 111 us with one tile per CTA (two CTAs per SM) and weights in shared memory, whose writes, operand reads and
+// copies took 750 clocks of shared memory per chunk and tile; 117 us with 128-key chunks and one score buffer
+// per tile, where a tile's next scores waited for its outputs.
 // Every wait is bounded: one that runs out raises a flag that ends the CTA's other waits, the CTA frees its tensor
 // memory and leaves its rows unwritten (reported where there is a status word).
 #pragma once
@@ -30,8 +35,8 @@
 
 namespace san {
 
-constexpr int kTileQ = 128, kTileK = 128, kTileThreads = 384, kTileLoaders = 96;
-constexpr int kTileKSlots = 3, kTileVSlots = 2, kTileMaxLayers = 2;
+constexpr int kTileQ = 128, kTileK = 64, kTileThreads = 384, kTileLoaders = 96;
+constexpr int kTileKSlots = 4, kTileVSlots = 3, kTileMaxLayers = 2;
 constexpr int TAG_TILE = 11;
 __host__ __device__ constexpr int tile_smem_bytes(int layers) {
     return 1024 + 2 * kTileQ * 128 + (kTileKSlots + kTileVSlots * layers) * kTileK * 128;
@@ -59,6 +64,11 @@ __device__ __forceinline__ bool tile_wait(uint64_t* bar, uint32_t parity, volati
         if (t0 == 0) t0 = now;
         else if (now - t0 > 2000000000LL) { *dead = 1; return false; }
     }
+}
+// The same for a whole warp, which goes on together: a lane left behind could meet the barrier two phases later, when
+// the parity it waits for means another phase.
+__device__ __forceinline__ bool tile_wait_warp(uint64_t* bar, uint32_t parity, volatile int* dead) {
+    return __all_sync(0xffffffffu, tile_wait(bar, parity, dead));
 }
 // Shared-memory matrix descriptor: 128-byte swizzle, groups of 8 rows 1024 bytes apart; `lead`: bytes between the 64-element
 // column blocks of an MN-major operand wider than 64.
@@ -169,7 +179,7 @@ struct TileWindow {
     __device__ __forceinline__ const uint4* query(int i) const {
         return reinterpret_cast<const uint4*>(p.q + (((long long)seq * p.cap + a0 + i) * p.H + head) * kDh);
     }
-    // Of chunk [c0, c0 + 128) of the visible keys: whether any row of tile x sees a part of it, whether all see all of
+    // Of chunk [c0, c0 + 64) of the visible keys: whether any row of tile x sees a part of it, whether all see all of
     // it, and those of columns 32 q .. 32 q + 31 that row i sees.
     __device__ __forceinline__ bool any_seen(const TileWork& w, int c0, int x) const {
         const int first = a0 + x * kTileQ, last = min(first + kTileQ, a0 + w.rows) - 1;
@@ -289,17 +299,17 @@ struct TilePrefix {
 
 template <class Mode, int LG, class Params>
 __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_constant__ Params params) {
-    constexpr uint32_t kCols = 512, kTileCols = 256, kOut = 128;        // a tile's columns: scores (weights over them), outputs
+    constexpr uint32_t kCols = 512, kTileCols = 256, kOut = 128;        // a tile's columns: scores twice (weights over them), outputs
     static_assert(kOut + 64 * LG <= kTileCols, "tensor memory");
     extern __shared__ __align__(1024) char tile_smem[];
-    __shared__ __align__(8) uint64_t k_full[kTileKSlots], k_free[kTileKSlots], v_full[kTileVSlots], v_free[kTileVSlots], s_full[2], p_full[2], done[2];
+    __shared__ __align__(8) uint64_t k_full[kTileKSlots], k_free[kTileKSlots], v_full[kTileVSlots], v_free[kTileVSlots], s_full[2][2], p_full[2][2], pv_done[2][2];
     __shared__ uint32_t tmem_s;
     __shared__ int dead_s;
     asm volatile("griddepcontrol.launch_dependents;");
     Mode mode{params};
     TileWork w;
     if (!mode.work(&w)) return;                                         // uniform over the CTA, before anything is allocated
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5;
     volatile int* dead = &dead_s;
     char* sQ = tile_smem + ((1024u - (tile_u32(tile_smem) & 1023u)) & 1023u);
     const uint32_t aK = tile_u32(sQ) + 2 * kTileQ * 128;
@@ -307,7 +317,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     if (threadIdx.x == 0) {
         for (int i = 0; i < kTileKSlots; ++i) { tile_bar_init(&k_full[i], kTileLoaders); tile_bar_init(&k_free[i], 1); }
         for (int i = 0; i < kTileVSlots; ++i) { tile_bar_init(&v_full[i], kTileLoaders); tile_bar_init(&v_free[i], 1); }
-        for (int i = 0; i < 2; ++i) { tile_bar_init(&s_full[i], 1); tile_bar_init(&p_full[i], kTileQ); tile_bar_init(&done[i], 1); }
+        for (int i = 0; i < 2; ++i) {
+            tile_bar_init(&s_full[i][0], 1); tile_bar_init(&s_full[i][1], 1);
+            tile_bar_init(&p_full[i][0], kTileQ); tile_bar_init(&p_full[i][1], kTileQ); tile_bar_init(&pv_done[i][0], 1); tile_bar_init(&pv_done[i][1], 1);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         dead_s = 0;
     }
@@ -330,48 +343,53 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     const int chunks = (w.end - w.begin + kTileK - 1) / kTileK;
 
     if (warp == 11) {
-        if (lane == 0) {
-            const uint32_t id_s = tile_idesc(false, kTileK), id_o = tile_idesc(true, w.layers * kDh);
-            int count[2] = {0, 0}, pending[2] = {-1, -1};               // chunks whose weights a tile has delivered; the one that it works on
-            auto outputs = [&](int x) -> bool {
-                const int t = pending[x], slot = t % kTileVSlots;
-                if (!tile_wait(&v_full[slot], (uint32_t)(t / kTileVSlots) & 1u, dead)) return false;
-                if (!tile_wait(&p_full[x], (uint32_t)count[x] & 1u, dead)) return false;
-                tile_proxy_fence();                                     // the copies are writes of the generic proxy
-                tile_after_sync();
-                const uint64_t dV = tile_desc(aV + (uint32_t)(slot * LG) * (kTileK * 128), kTileK * 128);
-                const uint32_t base = tmem + (uint32_t)x * kTileCols;
+        uint32_t elected;                                           // 1 in one lane
+        asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(elected));
+        const uint32_t id_s = tile_idesc(false, kTileK), id_o = tile_idesc(true, w.layers * kDh);
+        int scored[2] = {0, 0}, applied[2] = {0, 0};                // chunks of a tile whose MMAs have been issued
+        auto scores = [&](int t) -> bool {
+            const int slot = t % kTileKSlots;
+            if (!tile_wait_warp(&k_full[slot], (uint32_t)(t / kTileKSlots) & 1u, dead)) return false;
+            tile_proxy_fence();                                     // the copies are writes of the generic proxy
+            tile_after_sync();
+            const uint64_t dK = tile_desc(aK + (uint32_t)slot * (kTileK * 128));
+            for (int x = 0; x < 2; ++x) {
+                if (!mode.any_seen(w, w.begin + t * kTileK, x)) continue;
+                const uint64_t dQ = tile_desc(tile_u32(sQ) + (uint32_t)x * (kTileQ * 128));
+                const int buf = scored[x] & 1;                      // its weights of two chunks ago have been applied (in order)
+                if (elected) {
 #pragma unroll
-                for (int s = 0; s < kTileK / 16; ++s) tile_mma_ta(base + kOut, base + 8 * s, dV + 128 * s, id_o, count[x] > 0 || s > 0);
-                ++count[x];
-                pending[x] = -1;
-                return true;
-            };
-            bool go = true;
-            for (int t = 0; t < chunks && go; ++t) {
-                const int slot = t % kTileKSlots;
-                go = tile_wait(&k_full[slot], (uint32_t)(t / kTileKSlots) & 1u, dead);
-                tile_proxy_fence();
-                tile_after_sync();
-                const uint64_t dK = tile_desc(aK + (uint32_t)slot * (kTileK * 128));
-                for (int x = 0; x < 2 && go; ++x) {
-                    if (pending[x] >= 0) go = outputs(x);
-                    if (!go || !mode.any_seen(w, w.begin + t * kTileK, x)) continue;
-                    const uint64_t dQ = tile_desc(tile_u32(sQ) + (uint32_t)x * (kTileQ * 128));
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) tile_mma(tmem + (uint32_t)x * kTileCols, dQ + 2 * s, dK + 2 * s, id_s, s > 0);
-                    tile_commit(&s_full[x]);
-                    pending[x] = t;
+                    for (int s = 0; s < 4; ++s) tile_mma(tmem + (uint32_t)x * kTileCols + buf * kTileK, dQ + 2 * s, dK + 2 * s, id_s, s > 0);
+                    tile_commit(&s_full[x][buf]);
                 }
-                if (!go) break;
-                tile_commit(&k_free[slot]);                             // both tiles' scores of chunk t
-                if (t > 0) tile_commit(&v_free[(t - 1) % kTileVSlots]); // and their outputs of chunk t - 1
+                ++scored[x];
             }
-            for (int x = 0; x < 2 && go; ++x) {
-                if (pending[x] >= 0) go = outputs(x);
-                if (go) tile_commit(&done[x]);
+            if (elected) tile_commit(&k_free[slot]);
+            return true;
+        };
+        auto outputs = [&](int t) -> bool {
+            const int slot = t % kTileVSlots;
+            if (!tile_wait_warp(&v_full[slot], (uint32_t)(t / kTileVSlots) & 1u, dead)) return false;
+            tile_proxy_fence();
+            const uint64_t dV = tile_desc(aV + (uint32_t)(slot * LG) * (kTileK * 128), kTileK * 128);
+            for (int x = 0; x < 2; ++x) {
+                if (!mode.any_seen(w, w.begin + t * kTileK, x)) continue;
+                if (!tile_wait_warp(&p_full[x][applied[x] & 1], (uint32_t)(applied[x] >> 1) & 1u, dead)) return false;
+                tile_after_sync();
+                const uint32_t base = tmem + (uint32_t)x * kTileCols;
+                if (elected) {
+#pragma unroll
+                    for (int s = 0; s < kTileK / 16; ++s)
+                        tile_mma_ta(base + kOut, base + (applied[x] & 1) * kTileK + 8 * s, dV + 128 * s, id_o, applied[x] > 0 || s > 0);
+                    tile_commit(&pv_done[x][applied[x] & 1]);
+                }
+                ++applied[x];
             }
-        }
+            if (elected) tile_commit(&v_free[slot]);
+            return true;
+        };
+        bool go = chunks == 0 || scores(0);
+        for (int t = 0; t < chunks && go; ++t) go = (t + 1 >= chunks || scores(t + 1)) && outputs(t);
     } else if (warp >= 8) {
         // thread: 16-byte piece c of rows r0, r0 + 12, ...
         constexpr int kRows = (kTileK + 11) / 12;
@@ -417,38 +435,50 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         const unsigned long long sc2 = tile_pair(sc, sc);
         float m = -INFINITY, l = 0.f;
         bool ok = true;
-        int count = 0;
+        int count = 0, outputs = 0;
+        // Outputs of the tile's chunks below n are complete.  A wait names a phase by its parity, so every phase is waited
+        // for, and chunks alternate between two barriers (as with scores and weights): the softmax is up to two
+        // chunks behind the outputs, and a barrier may not move on by two phases under a wait.
+        auto outputs_until = [&](int n) -> bool {
+            for (; outputs < n; ++outputs)
+                if (!tile_wait_warp(&pv_done[x][outputs & 1], (uint32_t)(outputs >> 1) & 1u, dead)) return false;
+            return true;
+        };
         for (int t = 0; t < chunks; ++t) {
             const int c0 = w.begin + t * kTileK;
             if (!mode.any_seen(w, c0, x)) continue;
-            ok = __all_sync(0xffffffffu, tile_wait(&s_full[x], (uint32_t)count & 1u, dead));
+            const uint32_t buf = lanes + (count & 1) * kTileK;
+            ok = tile_wait_warp(&s_full[x][count & 1], (uint32_t)(count >> 1) & 1u, dead);
+            ok = ok && outputs_until(count - 1);                        // (long complete: the scores were issued behind them)
             if (!ok) break;
             tile_after_sync();
-            const bool whole = mode.all_seen(w, c0, x);                 // uniform over the CTA
-            float z[128];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) tile_ld32(lanes + 32 * q, z + 32 * q);
+            float z[64];
+            tile_ld32(buf, z);
+            tile_ld32(buf + 32, z + 32);
             tile_wait_ld();
-            if (!whole) {
+            if (!mode.all_seen(w, c0, x)) {                             // uniform over the tile's warps
+                const uint32_t s0 = mode.seen(w, c0, i, 0), s1 = mode.seen(w, c0, i, 1);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t seen = mode.seen(w, c0, i, q);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) z[32 * q + j] = seen >> j & 1u ? z[32 * q + j] : -INFINITY;
+                for (int j = 0; j < 32; ++j) {
+                    z[j] = s0 >> j & 1u ? z[j] : -INFINITY;
+                    z[32 + j] = s1 >> j & 1u ? z[32 + j] : -INFINITY;
                 }
             }
             float top[4] = {z[0], z[1], z[2], z[3]};
 #pragma unroll
-            for (int j = 4; j < 124; j += 8)
+            for (int j = 4; j < 60; j += 8)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top[e] = tile_max3(top[e], z[j + 2 * e], z[j + 2 * e + 1]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) top[e] = fmaxf(top[e], z[124 + e]);
+            for (int e = 0; e < 4; ++e) top[e] = fmaxf(top[e], z[60 + e]);
             const float m_chunk = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sc;
             // A row that has seen nothing yet has outputs and a sum of zero: its maximum starts here.
             const bool grown = m_chunk > m + 8.f && m > -INFINITY;
             if (m == -INFINITY) m = m_chunk;
             if (__any_sync(0xffffffffu, grown)) {                       // (count > 0)
+                ok = outputs_until(count);                              // those of this chunk wait for its weights
+                if (!ok) break;
+                tile_after_sync();
                 const float f = grown ? fast_exp2(m - m_chunk) : 1.f;
                 if (grown) { m = m_chunk; l *= f; }
                 for (int y = 0; y < 4 * w.layers; ++y) {                // 16 columns at a time: the scores are still held
@@ -463,30 +493,27 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             const float base_m = m == -INFINITY ? 0.f : m;
             unsigned long long sum[2] = {0ull, 0ull};
             const unsigned long long m2 = tile_pair(-base_m, -base_m);
+            float packed[32];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float packed[16];
-#pragma unroll
-                for (int j = 0; j < 32; j += 2) {
-                    float u, v;
-                    tile_unpair(tile_fma2(tile_pair(z[32 * q + j], z[32 * q + j + 1]), sc2, m2), u, v);
-                    u = fast_exp2(u);
-                    v = fast_exp2(v);
-                    sum[(j >> 1) & 1] = tile_add2(sum[(j >> 1) & 1], tile_pair(u, v));
-                    packed[j >> 1] = __uint_as_float(pack_bf16(u, v));
-                }
-                tile_st16(lanes + 16 * q, packed);                      // over scores that have been read
+            for (int j = 0; j < 64; j += 2) {
+                float u, v;
+                tile_unpair(tile_fma2(tile_pair(z[j], z[j + 1]), sc2, m2), u, v);
+                u = fast_exp2(u);
+                v = fast_exp2(v);
+                sum[(j >> 1) & 1] = tile_add2(sum[(j >> 1) & 1], tile_pair(u, v));
+                packed[j >> 1] = __uint_as_float(pack_bf16(u, v));
             }
+            tile_st16(buf, packed);                                     // over the scores, which have been read
+            tile_st16(buf + 16, packed + 16);
             float sa, sb;
             tile_unpair(tile_add2(sum[0], sum[1]), sa, sb);
             l += sa + sb;
             tile_wait_st();
             tile_before_sync();
-            tile_arrive(&p_full[x]);
+            tile_arrive(&p_full[x][count & 1]);
             ++count;
         }
-        if (ok) ok = tile_wait(&done[x], 0u, dead);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = ok && outputs_until(count);
         tile_after_sync();
         if (ok) mode.template finish<LG>(w, lanes + kOut, i, m, l);
         else if (threadIdx.x == 0) mode.failed();
