@@ -30,6 +30,7 @@ constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelWords = 16;                  // 32-bit words of logits per thread and step
 constexpr int kSelList = 1024;                 // keys that may reach the bound between two checks; more: one by one
+constexpr int kSelLong = 96;                   // list length at which the bound is raised
 constexpr int kSelTight = 64;                  // what the list is cut down to (equal logits aside)
 constexpr int TAG_SELECT = 8;
 
@@ -76,7 +77,7 @@ struct Key64 {
 };
 struct Key128 {
     unsigned long long a, b;
-    __device__ __forceinline__ bool over(const Key128& o) const { return a > o.a || (a == o.a && b > o.b); }
+    __device__ __forceinline__ bool over(const Key128& o) const { return (a > o.a) | ((a == o.a) & (b > o.b)); }
     __device__ __forceinline__ Key128 swapped(int mask) const {
         return {__shfl_xor_sync(0xffffffffu, a, mask), __shfl_xor_sync(0xffffffffu, b, mask)};
     }
@@ -119,14 +120,20 @@ template <typename V> __device__ __forceinline__ V join_bounds(const V* warp_lea
     return t;
 }
 
-// Writes the n largest of `count` different keys to out(place, key); the list is in shared memory.
+// Gives the n largest of `count` different keys to out(place, key); the list is in shared memory.  Up to 32 threads
+// count the keys above one, as many as there are for each.
 template <typename K, typename F> __device__ __forceinline__ void rank_list(const K* list, int count, int n, F out) {
-    for (int i = threadIdx.x; i < count; i += kSelThreads) {
-        const K mine = list[i];
+    int per = kSelThreads;
+    while (per > 1 && (per > 32 || per * count > kSelThreads)) per >>= 1;
+    const int part = threadIdx.x & (per - 1);
+    for (int first = 0; first < count; first += kSelThreads / per) {
+        const int i = first + (int)threadIdx.x / per;
+        const K mine = list[min(i, count - 1)];
         int above = 0;
 #pragma unroll 4
-        for (int j = 0; j < count; ++j) above += list[j].over(mine) ? 1 : 0;
-        if (above < n) out(above, mine);
+        for (int j = part; j < count; j += per) above += list[j].over(mine) ? 1 : 0;
+        for (int o = 1; o < per; o <<= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
+        if (i < count && above < n && part == 0) out(above, mine);
     }
 }
 
@@ -149,10 +156,11 @@ template <> struct SelectHeld<float> {
 #pragma unroll
         for (int i = 0; i < kSelWords; ++i) x[i] = fmaxf(x[i], -INFINITY);
     }
-    __device__ __forceinline__ float top8(int g) const {              // the largest of logits 8 g .. 8 g + 7
+    // The largest of logits 8 g .. 8 g + 7, NaN if one of them is.
+    __device__ __forceinline__ float top8(int g) const {
         float t = x[8 * g];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) t = fmaxf(t, x[8 * g + i]);
+        for (int i = 1; i < 8; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(t) : "f"(x[8 * g + i]));
         return t;
     }
 };
@@ -174,11 +182,30 @@ template <> struct SelectHeld<__nv_bfloat16> {
         }
     }
     __device__ __forceinline__ float top8(int g) const {
-        const __nv_bfloat162 t = __hmax2(__hmax2(two(x[4 * g]), two(x[4 * g + 1])), __hmax2(two(x[4 * g + 2]), two(x[4 * g + 3])));
-        return fmaxf(__low2float(t), __high2float(t));
+        const __nv_bfloat162 t = __hmax2_nan(__hmax2_nan(two(x[4 * g]), two(x[4 * g + 1])), __hmax2_nan(two(x[4 * g + 2]), two(x[4 * g + 3])));
+        float r = __low2float(t);
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(r) : "f"(__high2float(t)));
+        return r;
     }
 };
 
+// Two float32 numbers in one instruction.
+__device__ __forceinline__ unsigned long long pair_f32(float x, float y) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void unpair_f32(unsigned long long r, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(r)); }
+__device__ __forceinline__ unsigned long long fma_f32x2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ unsigned long long add_f32x2(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -235,6 +262,15 @@ __global__ void __launch_bounds__(kSelThreads, 4) select_rows_kernel(const Selec
     const int begin = min(chunk * p.steps * STEP, p.vocab), end = (int)min((long long)begin + (long long)p.steps * STEP, (long long)p.vocab);
 
     auto load = [&](Held& v, int base) {
+        if (base + STEP <= end) {                                     // a whole step: no bounds
+            const T* at = x + base + (int)threadIdx.x * VEC;
+#pragma unroll
+            for (int j = 0; j < N / VEC; ++j) {
+                if constexpr (VECTOR) v.set16(j, ld16_stream(at + j * kSelThreads * VEC));
+                else v.set(j, as_f32<T>(at[j * kSelThreads]));
+            }
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < N / VEC; ++j) {
             const int at = base + (j * kSelThreads + (int)threadIdx.x) * VEC;
@@ -254,7 +290,7 @@ __global__ void __launch_bounds__(kSelThreads, 4) select_rows_kernel(const Selec
     // themselves (the product is exact inside the FMA), and M - c top, the same for all, is put right at the
     // end.  A maximum so large that c x could be infinite, or infinite itself: only logits equal to it count.
     constexpr float c = 1.4426950408889634f;
-    float top = -INFINITY, m = 0.f, part[4] = {0.f, 0.f, 0.f, 0.f};
+    float top = -INFINITY, m = 0.f, part[4] = {0.f, 0.f, 0.f, 0.f};      // two pairs of partial sums
     float bound = -INFINITY;
     if (threadIdx.x == 0) s_count = 0;
     Held next;
@@ -262,10 +298,17 @@ __global__ void __launch_bounds__(kSelThreads, 4) select_rows_kernel(const Selec
     for (int base = begin; base < end; base += STEP) {
         Held v = next;
         if (base + STEP < end) load(next, base + STEP);
-        v.mask_nan();
         float t8[N / 8], t = -INFINITY;
+        auto largest = [&]() {
+            t = -INFINITY;
 #pragma unroll
-        for (int g = 0; g < N / 8; ++g) { t8[g] = v.top8(g); t = fmaxf(t, t8[g]); }
+            for (int g = 0; g < N / 8; ++g) { t8[g] = v.top8(g); asm("max.NaN.f32 %0, %0, %1;" : "+f"(t) : "f"(t8[g])); }
+        };
+        largest();
+        if (t != t) {                                                 // masked tokens among them: -inf from here on
+            v.mask_nan();
+            largest();
+        }
         if (t > top) {
             const float m_new = t * c, scale = fabsf(top) < 1e30f && fabsf(t) < 1e30f ? exp2_fast(m - m_new) : 0.f;
 #pragma unroll
@@ -273,8 +316,16 @@ __global__ void __launch_bounds__(kSelThreads, 4) select_rows_kernel(const Selec
             top = t; m = m_new;
         }
         if (fabsf(top) < 1e30f) {
+            unsigned long long sum[2] = {pair_f32(part[0], part[1]), pair_f32(part[2], part[3])};
+            const unsigned long long c2 = pair_f32(c, c), m2 = pair_f32(-m, -m);
 #pragma unroll
-            for (int i = 0; i < N; ++i) part[i & 3] += exp2_fast(fmaf(v.get(i), c, -m));
+            for (int i = 0; i < N; i += 2) {
+                float y, z;
+                unpair_f32(fma_f32x2(pair_f32(v.get(i), v.get(i + 1)), c2, m2), y, z);
+                sum[(i >> 1) & 1] = add_f32x2(sum[(i >> 1) & 1], pair_f32(exp2_fast(y), exp2_fast(z)));
+            }
+            unpair_f32(sum[0], part[0], part[1]);
+            unpair_f32(sum[1], part[2], part[3]);
         } else if (top > -INFINITY) {
 #pragma unroll
             for (int i = 0; i < N; ++i) part[i & 3] += v.get(i) == top ? 1.f : 0.f;
@@ -314,7 +365,7 @@ __global__ void __launch_bounds__(kSelThreads, 4) select_rows_kernel(const Selec
         const int count = s_count;
         if (count > kSelList) {                                       // keys were lost: only the sums go on
             bound = INFINITY;
-        } else if (count > kSelList / 2 && base + STEP < end) {
+        } else if (count > kSelLong && base + STEP < end) {
             if (warp == 0) {
                 int left;
                 const uint32_t b = tighten(s_list, count, p.beam, order_f32(bound), &left, lane);
@@ -339,27 +390,22 @@ __global__ void __launch_bounds__(kSelThreads, 4) select_rows_kernel(const Selec
     }
     __syncthreads();
     char* out = p.ws + (size_t)blockIdx.x * select_part_bytes(p.beam);
-    if (threadIdx.x == 0) {
-        float all = s_max[0];
-        for (int w = 1; w < kSelWarps; ++w) all = fmaxf(all, s_max[w]);
-        double s = 0.0;
-        for (int w = 0; w < kSelWarps; ++w)
-            if (s_sum[w] > 0.0) s += s_max[w] == all ? s_sum[w] : s_sum[w] * (double)exp2_fast((s_max[w] - all) * c);
-        *reinterpret_cast<float*>(out) = all;
-        *reinterpret_cast<double*>(out + 8) = s;
+    if (warp == kSelWarps - 1) {
+        float t = lane < kSelWarps ? s_max[lane] : -INFINITY;
+        double s = lane < kSelWarps ? s_sum[lane] : 0.0;
+        const float all = warp_max(t);
+        s = s == 0.0 || t == all ? s : s * (double)exp2_fast((t - all) * c);
+#pragma unroll
+        for (int o = kSelWarps / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (lane == 0) {
+            *reinterpret_cast<float*>(out) = all;
+            *reinterpret_cast<double*>(out + 8) = s;
+        }
     }
     Key64* best = reinterpret_cast<Key64*>(out + 16);
     if (count <= kSelList) {
         count = s_count;
-        for (int i0 = 0; i0 < count; i0 += kSelThreads / 4) {         // four threads count for one key
-            const int i = i0 + (int)(threadIdx.x >> 2);
-            const Key64 mine = s_list[min(i, count - 1)];
-            int above = 0;
-            for (int j = threadIdx.x & 3; j < count; j += 4) above += s_list[j].over(mine) ? 1 : 0;
-            above += __shfl_xor_sync(0xffffffffu, above, 1);
-            above += __shfl_xor_sync(0xffffffffu, above, 2);
-            if (i < count && above < p.beam && (threadIdx.x & 3) == 0) best[above] = mine;
-        }
+        rank_list(s_list, count, p.beam, [&](int place, const Key64& k) { best[place] = k; });
         for (int i = count + (int)threadIdx.x; i < p.beam; i += kSelThreads) best[i] = Key64{0};
         return;
     }
@@ -387,7 +433,7 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
     __shared__ int s_counts[2][kSelWarps];
     __shared__ Key128 s_slots[kSelWarps];
     __shared__ float s_score[SAN_MAX_BEAM], s_top[SAN_MAX_BEAM];
-    __shared__ double s_logsum[SAN_MAX_BEAM], s_norm[SAN_MAX_BEAM];
+    __shared__ double s_logsum[SAN_MAX_BEAM], s_norm[SAN_MAX_BEAM], s_inverse[SAN_MAX_BEAM];
     __shared__ int s_len[SAN_MAX_BEAM], s_done[SAN_MAX_BEAM], s_parent[SAN_MAX_BEAM], s_token[SAN_MAX_BEAM];
     __shared__ int s_count, s_bad, s_longest;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -401,6 +447,7 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
         const bool dead = select_dead(score);
         s_score[b] = dead ? -INFINITY : score; s_len[b] = len; s_done[b] = done;
         s_norm[b] = p.alpha == 0.0 ? 1.0 : pow((5.0 + (double)(len + (done ? 0 : 1))) / 6.0, p.alpha);
+        s_inverse[b] = 1.0 / s_norm[b];
         s_parent[b] = b; s_token[b] = -1;
         const long long limit = p.tokens ? p.ld_tokens : 0x7ffffffe;
         if (len < 0 || len > limit || (len == limit && !done && !dead)) {
@@ -430,23 +477,28 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
         }
     };
     load(0);
-    for (int b = warp; b < beam; b += kSelWarps) {                    // log of each row's sum of exponentials
-        if (s_done[b] || s_score[b] == -INFINITY) continue;
-        const char* part = parts + (size_t)b * p.chunks * part_bytes;
+    // log of each row's sum of exponentials: as many lanes for a row as it has parts (32 at most)
+    int width = 1;
+    while (width < 32 && width < p.chunks) width <<= 1;
+    for (int b0 = warp * (32 / width); b0 < beam; b0 += kSelWarps * (32 / width)) {
+        const int b = b0 + lane / width, c = lane & (width - 1);
+        const bool row = b < beam && !s_done[min(b, beam - 1)] && s_score[min(b, beam - 1)] > -INFINITY;
+        const char* part = parts + (size_t)min(b, beam - 1) * p.chunks * part_bytes;
         float m = -INFINITY;
         double s = 0.0;
-        for (int c0 = 0; c0 < p.chunks; c0 += 32) {
-            const bool have = c0 + lane < p.chunks;
-            const float mc = have ? *reinterpret_cast<const float*>(part + (c0 + lane) * part_bytes) : -INFINITY;
-            const double sc = have ? *reinterpret_cast<const double*>(part + (c0 + lane) * part_bytes + 8) : 0.0;
-            const float m_new = fmaxf(m, warp_max(mc));
+        for (int c0 = 0; c0 < p.chunks; c0 += width) {
+            const bool have = row && c0 + c < p.chunks;
+            const float mc = have ? *reinterpret_cast<const float*>(part + (c0 + c) * part_bytes) : -INFINITY;
+            const double sc = have ? *reinterpret_cast<const double*>(part + (c0 + c) * part_bytes + 8) : 0.0;
+            float m_new = mc;
+            for (int o = 1; o < width; o <<= 1) m_new = fmaxf(m_new, __shfl_xor_sync(0xffffffffu, m_new, o));
+            m_new = fmaxf(m, m_new);
             double t = mc == -INFINITY ? 0.0 : mc == m_new ? sc : sc * exp((double)mc - (double)m_new);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+            for (int o = 1; o < width; o <<= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
             s = (m == -INFINITY ? 0.0 : m == m_new ? s : s * exp((double)m - (double)m_new)) + t;
             m = m_new;
         }
-        if (lane == 0) { s_top[b] = m; s_logsum[b] = log(s); }
+        if (row && c == 0) { s_top[b] = m; s_logsum[b] = log(s); }
     }
     __syncthreads();
     auto score_of = [&](int b, float x) {
@@ -456,17 +508,17 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
     int kept = 0;                                                     // candidates kept from the rounds before
     for (int first = 0, round = 0; first < total; first += kSelThreads * kMergeHeld, round ^= 1) {
         if (first > 0) load(first);
-        Key128 key[kMergeHeld];
-        unsigned long long top = 0;
+        // ranks by a multiplication, within 2^-51 of the ones by the division: good enough for a bound
+        unsigned long long key[kMergeHeld], top = 0;
+        auto score_at = [&](int b, unsigned long long h) { return s_done[b] ? (double)s_score[b] : score_of(b, unorder_f32((unsigned)(h >> 32))); };
 #pragma unroll
         for (int j = 0; j < kMergeHeld; ++j) {
-            key[j] = Key128{0, 0};
+            key[j] = 0;
             if (held[j] == 0) continue;
             const int b = (first + j * kSelThreads + (int)threadIdx.x) / per_row;
-            const int token = s_done[b] ? max(p.eos, 0) : (int)~(unsigned)held[j];
-            const double rank = (s_done[b] ? (double)s_score[b] : score_of(b, unorder_f32((unsigned)(held[j] >> 32)))) / s_norm[b];
-            if (rank > -INFINITY) key[j] = Key128{order_f64(rank), ~(((unsigned long long)(unsigned)b << 32) | (unsigned)token)};
-            top = key[j].a > top ? key[j].a : top;
+            const double rank = score_at(b, held[j]) * s_inverse[b];
+            if (rank > -INFINITY) key[j] = order_f64(rank);
+            top = key[j] > top ? key[j] : top;
         }
         unsigned long long warp_top, least;
         group_bounds(top, beam, &warp_top, &least);
@@ -475,7 +527,7 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
         unsigned long long bound = join_bounds(s_least, beam), most = s_most[0];
 #pragma unroll
         for (int w = 1; w < kSelWarps; ++w) most = s_most[w] > most ? s_most[w] : most;
-        if (kept == beam && s_best[round][beam - 1].a > bound) bound = s_best[round][beam - 1].a;
+        if (kept == beam && s_best[round][beam - 1].a > bound) bound = s_best[round][beam - 1].a - 16;     // an exact rank
         if (bound == 0) bound = 1;
         // Candidates are not mixed over the threads as logits are (hypotheses differ in score, places in rank), so the
         // bound may be low: halve the way to the largest until at most 128 reach it, never fewer than `beam` of this round
@@ -485,7 +537,7 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
             const unsigned long long mid = step == 0 ? bound : bound + (most - bound + 1) / 2;
             int n = 0;
 #pragma unroll
-            for (int j = 0; j < kMergeHeld; ++j) n += key[j].a >= mid ? 1 : 0;
+            for (int j = 0; j < kMergeHeld; ++j) n += key[j] >= mid ? 1 : 0;
             n = __reduce_add_sync(0xffffffffu, n);
             if (lane == 0) s_counts[step & 1][warp] = n;
             __syncthreads();
@@ -496,10 +548,18 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
             else most = mid - 1;                                      // fewer than `beam` reach mid
             if (count <= 128 || most <= bound) break;
         }
+        bound = bound > 16 ? bound - 16 : 1;                          // further down than the two ranks can differ
 #pragma unroll
         for (int j = 0; j < kMergeHeld; ++j)
-            if (key[j].a >= bound) s_list[atomicAdd(&s_count, 1)] = key[j];
+            if (key[j] >= bound) s_list[atomicAdd(&s_count, 1)] = Key128{held[j], (unsigned long long)(first + j * kSelThreads + (int)threadIdx.x)};
         __syncthreads();
+        for (int i = threadIdx.x; i < s_count; i += kSelThreads) {    // their exact ranks
+            const unsigned long long h = s_list[i].a;
+            const int b = (int)s_list[i].b / per_row, token = s_done[b] ? max(p.eos, 0) : (int)~(unsigned)h;
+            s_list[i] = Key128{order_f64(score_at(b, h) / s_norm[b]), ~(((unsigned long long)(unsigned)b << 32) | (unsigned)token)};
+        }
+        __syncthreads();
+        count = s_count;
         const bool long_list = count > 256;                           // counting would take longer than picking them out
         if (!long_list && (int)threadIdx.x < kept) s_list[count + threadIdx.x] = s_best[round][threadIdx.x];
         __syncthreads();
@@ -512,9 +572,8 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
             Key128 last{~0ull, ~0ull};
             for (int k = 0; k < beam; ++k) {
                 Key128 mine{0, 0};
-#pragma unroll
-                for (int j = 0; j < kMergeHeld; ++j)
-                    if (last.over(key[j])) mine = larger(mine, key[j]);
+                for (int i = threadIdx.x; i < count; i += kSelThreads)
+                    if (last.over(s_list[i])) mine = larger(mine, s_list[i]);
                 if ((int)threadIdx.x < kept && last.over(s_best[round][threadIdx.x])) mine = larger(mine, s_best[round][threadIdx.x]);
                 last = block_largest(mine, s_slots);
                 if (threadIdx.x == 0) s_best[round ^ 1][k] = last;    // more than 256 candidates: there are `beam`
@@ -551,6 +610,7 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
     const int longest = min((long long)s_longest + 1, p.ld_tokens);
     for (int pos = threadIdx.x; pos < longest; pos += kSelThreads) {
         const long long first = (long long)sent * beam * p.ld_tokens + pos;
+#pragma unroll 8
         for (int b = 0; b < beam; ++b) column[b * kSelThreads] = p.tokens[first + b * p.ld_tokens];
         for (int s = 0; s < beam; ++s) {
             const int b = s_parent[s], len = s_len[b], token = s_token[s];

@@ -22,9 +22,15 @@ inline long long div_up(long long a, long long b) { return (a + b - 1) / b; }
 inline int32_t cuda_status(cudaError_t e) { return e == cudaSuccess ? SAN_OK : SAN_ERR_CUDA; }
 inline bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
-// Opt-in to dynamic shared memory above 48 KB, once per kernel and device.
-int32_t opt_in(const void* fn, int bytes) {
-    return cuda_status(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+// Opt-in to dynamic shared memory above 48 KB, an attribute of a kernel on a device: done once for each (`set`, one
+// entry per device, belongs to the kernel).
+int32_t opt_in(const void* fn, int bytes, bool* set) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return SAN_ERR_CUDA;
+    if (dev >= 0 && dev < 64 && set[dev]) return SAN_OK;
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return SAN_ERR_CUDA;
+    if (dev >= 0 && dev < 64) set[dev] = true;
+    return SAN_OK;
 }
 
 // Launches `fn` so that its CTAs may be set up while the kernel before it on the stream still runs
@@ -41,14 +47,20 @@ int32_t launch_after(void (*fn)(P), dim3 grid, unsigned block, cudaStream_t st, 
 }
 
 // ------------------------------------------------------------------------------- beam selection
-// Parts of a row: enough that the SMs (four CTAs each) have four waves of them, each of whole steps.
+// Parts of a row, each of whole steps: the cut with the shortest estimate of (waves of CTAs, four per SM) x (steps of a part
+// + the 2.5 steps that the bound, the list and the hand-over of a part take).
 struct SelectCut { int chunks, steps; };
 SelectCut select_cut(int32_t dtype, long long rows, int vocab) {
     const int step = kSelWords * (dtype == SAN_BF16 ? 2 : 1) * kSelThreads;
     const long long all = div_up(vocab, step);
-    const long long want = std::min(all, std::max<long long>(1, div_up(16 * kSms, std::max<long long>(rows, 1))));
-    const long long steps = div_up(all, want);
-    return {(int)div_up(all, steps), (int)steps};
+    SelectCut best{1, (int)all};
+    double least = 1e30;
+    for (long long parts = 1; parts <= std::min<long long>(all, 64); ++parts) {
+        const long long steps = div_up(all, parts);
+        const double cost = (double)std::max<long long>(1, div_up(rows * div_up(all, steps), 4 * kSms)) * ((double)steps + 2.5);
+        if (cost < least) { least = cost; best = {(int)div_up(all, steps), (int)steps}; }
+    }
+    return best;
 }
 
 int32_t select_shape(int32_t n_sent, int32_t beam, int32_t vocab) {
@@ -172,7 +184,8 @@ int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int wi
 template <typename T, int LG, int N>
 int32_t launch_attend_as(const AttendPlan& a, cudaStream_t st) {
     constexpr int smem = attend_smem_bytes<T, N>();
-    const int32_t rc = opt_in((const void*)attend_kernel<T, LG, N>, smem);
+    static bool set[64] = {};
+    const int32_t rc = opt_in((const void*)attend_kernel<T, LG, N>, smem, set);
     if (rc != SAN_OK) return rc;
     attend_kernel<T, LG, N><<<(unsigned)a.ctas, kAtWarps * 32, smem, st>>>(a.p);
     if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
@@ -193,7 +206,8 @@ int32_t launch_attend_with(const AttendPlan& a, cudaStream_t st) {
 template <class Mode, int LG, class P>
 int32_t launch_tiles(const P& p, dim3 grid, cudaStream_t st) {
     constexpr int smem = tile_smem_bytes(LG);
-    const int32_t rc = opt_in((const void*)tile_kernel<Mode, LG, P>, smem);
+    static bool set[64] = {};
+    const int32_t rc = opt_in((const void*)tile_kernel<Mode, LG, P>, smem, set);
     if (rc != SAN_OK) return rc;
     tile_kernel<Mode, LG, P><<<grid, kTileThreads, smem, st>>>(p);
     return cuda_status(cudaGetLastError());

@@ -50,20 +50,23 @@ __device__ __forceinline__ void tile_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tile_u32(bar)) : "memory");
 }
 // Bounded wait for the phase of that parity: false once it has lasted about a second or another wait has given up.
-__device__ __forceinline__ bool tile_wait(uint64_t* bar, uint32_t parity, volatile int* dead) {
-    const uint32_t addr = tile_u32(bar);
+__device__ __noinline__ bool tile_wait_slow(uint32_t addr, uint32_t parity, volatile int* dead) {
     uint32_t ok;
-    long long t0 = 0;
+    const long long t0 = clock64();
     for (uint32_t turn = 0;; ++turn) {
         asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
                      : "=r"(ok) : "r"(addr), "r"(parity), "r"(1000000u) : "memory");
         if (ok) return true;
         if ((turn & 63u) != 63u) continue;
         if (*dead) return false;
-        const long long now = clock64();
-        if (t0 == 0) t0 = now;
-        else if (now - t0 > 2000000000LL) { *dead = 1; return false; }
+        if (clock64() - t0 > 2000000000LL) { *dead = 1; return false; }
     }
+}
+__device__ __forceinline__ bool tile_wait(uint64_t* bar, uint32_t parity, volatile int* dead) {
+    const uint32_t addr = tile_u32(bar);
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(addr), "r"(parity) : "memory");
+    return ok ? true : tile_wait_slow(addr, parity, dead);
 }
 // The same for a whole warp, which goes on together: a lane left behind could meet the barrier two phases later, when
 // the parity it waits for means another phase.
@@ -153,6 +156,14 @@ struct TileWork {
     int rows, layer0, layers;               // query rows, up to two tiles of them
 };
 
+// Which chunks (numbers t of a CTA's run) a tile takes part in: t < sinks or first <= t < end; and from which to which all
+// of its rows see all of the chunk.
+struct TileRange {
+    int sinks, first, end, whole_first, whole_end;
+    __device__ __forceinline__ bool any(int t) const { return t < sinks || (t >= first && t < end); }
+    __device__ __forceinline__ bool whole(int t) const { return t >= whole_first && t < whole_end; }
+};
+
 // ---- windowed prompts: grid (query tiles, heads, sequences x layer groups)
 struct TileWindow {
     const WindowParams& p;
@@ -179,17 +190,19 @@ struct TileWindow {
     __device__ __forceinline__ const uint4* query(int i) const {
         return reinterpret_cast<const uint4*>(p.q + (((long long)seq * p.cap + a0 + i) * p.H + head) * kDh);
     }
-    // Of chunk [c0, c0 + 64) of the visible keys: whether any row of tile x sees a part of it, whether all see all of
-    // it, and those of columns 32 q .. 32 q + 31 that row i sees.
-    __device__ __forceinline__ bool any_seen(const TileWork& w, int c0, int x) const {
-        const int first = a0 + x * kTileQ, last = min(first + kTileQ, a0 + w.rows) - 1;
-        if (last < first || c0 > w.ns + last - w.lo) return false;
-        return c0 < w.ns + max(0, p.n_sink - w.lo) || c0 + kTileK > w.ns + max(first - p.window + 1, w.lo) - w.lo;
+    __device__ __forceinline__ TileRange range(const TileWork& w, int x) const {
+        const int first = a0 + x * kTileQ, last = min(first + kTileQ, a0 + w.rows) - 1;      // rows of the tile
+        if (last < first) return {0, 0, 0, 0, 0};
+        auto number = [&](int key) { return key - w.lo + w.ns; };
+        TileRange r;
+        r.end = number(last) / kTileK + 1;
+        r.first = number(max(first - p.window + 1, w.lo)) / kTileK;
+        r.sinks = min((number(max(p.n_sink, w.lo)) + kTileK - 1) / kTileK, r.end);           // numbers below it are sinks
+        r.whole_first = (number(max(first + kTileQ - p.window, w.lo)) + kTileK - 1) / kTileK;
+        r.whole_end = min(number(first) + 1, w.end) / kTileK;
+        return r;
     }
-    __device__ __forceinline__ bool all_seen(const TileWork& w, int c0, int x) const {
-        const int first = a0 + x * kTileQ, key = w.lo + c0 - w.ns;
-        return c0 >= w.ns && c0 + kTileK <= w.end && key + kTileK - 1 <= first && key > first + kTileQ - 1 - p.window;
-    }
+    // Of columns 32 q .. 32 q + 31 of chunk [c0, c0 + 64) of the visible keys, those that row i sees.
     __device__ __forceinline__ uint32_t seen(const TileWork& w, int c0, int i, int q) const {
         auto below = [&](int n) { n -= c0 + 32 * q; return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; };      // of numbers below n
         const int a = a0 + i, self = w.ns + a - w.lo;                   // the row's own number
@@ -265,8 +278,10 @@ struct TilePrefix {
         return (long long)(p.first[g] + row / p.group) * p.H + hk * p.group + row % p.group;
     }
     __device__ __forceinline__ const uint4* query(int i) const { return reinterpret_cast<const uint4*>(p.q + place(i) * 128); }
-    __device__ __forceinline__ bool any_seen(const TileWork& w, int, int x) const { return x * kTileQ < w.rows; }
-    __device__ __forceinline__ bool all_seen(const TileWork& w, int c0, int) const { return c0 + kTileK <= w.end; }
+    __device__ __forceinline__ TileRange range(const TileWork& w, int x) const {
+        if (x * kTileQ >= w.rows) return {0, 0, 0, 0, 0};
+        return {0, 0, (w.end - w.begin + kTileK - 1) / kTileK, 0, (w.end - w.begin) / kTileK};
+    }
     __device__ __forceinline__ uint32_t seen(const TileWork& w, int c0, int, int q) const {
         const int n = w.end - c0 - 32 * q;
         return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1;
@@ -346,6 +361,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         uint32_t elected;                                           // 1 in one lane
         asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(elected));
         const uint32_t id_s = tile_idesc(false, kTileK), id_o = tile_idesc(true, w.layers * kDh);
+        const TileRange range[2] = {mode.range(w, 0), mode.range(w, 1)};
         int scored[2] = {0, 0}, applied[2] = {0, 0};                // chunks of a tile whose MMAs have been issued
         auto scores = [&](int t) -> bool {
             const int slot = t % kTileKSlots;
@@ -353,8 +369,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             tile_proxy_fence();                                     // the copies are writes of the generic proxy
             tile_after_sync();
             const uint64_t dK = tile_desc(aK + (uint32_t)slot * (kTileK * 128));
+#pragma unroll
             for (int x = 0; x < 2; ++x) {
-                if (!mode.any_seen(w, w.begin + t * kTileK, x)) continue;
+                if (!range[x].any(t)) continue;
                 const uint64_t dQ = tile_desc(tile_u32(sQ) + (uint32_t)x * (kTileQ * 128));
                 const int buf = scored[x] & 1;                      // its weights of two chunks ago have been applied (in order)
                 if (elected) {
@@ -372,8 +389,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             if (!tile_wait_warp(&v_full[slot], (uint32_t)(t / kTileVSlots) & 1u, dead)) return false;
             tile_proxy_fence();
             const uint64_t dV = tile_desc(aV + (uint32_t)(slot * LG) * (kTileK * 128), kTileK * 128);
+#pragma unroll
             for (int x = 0; x < 2; ++x) {
-                if (!mode.any_seen(w, w.begin + t * kTileK, x)) continue;
+                if (!range[x].any(t)) continue;
                 if (!tile_wait_warp(&p_full[x][applied[x] & 1], (uint32_t)(applied[x] >> 1) & 1u, dead)) return false;
                 tile_after_sync();
                 const uint32_t base = tmem + (uint32_t)x * kTileCols;
@@ -435,28 +453,23 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         const unsigned long long sc2 = tile_pair(sc, sc);
         float m = -INFINITY, l = 0.f;
         bool ok = true;
-        int count = 0, outputs = 0;
-        // Outputs of the tile's chunks below n are complete.  A wait names a phase by its parity, so every phase is waited
-        // for, and chunks alternate between two barriers (as with scores and weights): the softmax is up to two
-        // chunks behind the outputs, and a barrier may not move on by two phases under a wait.
-        auto outputs_until = [&](int n) -> bool {
-            for (; outputs < n; ++outputs)
-                if (!tile_wait_warp(&pv_done[x][outputs & 1], (uint32_t)(outputs >> 1) & 1u, dead)) return false;
-            return true;
-        };
+        int count = 0;
+        const TileRange range = mode.range(w, x);
+        // The outputs of the tile's chunk n are complete.  Two barriers in turn, as for scores and weights, because a wait
+        // names a phase by its parity: the outputs of chunk n - 2 were complete before the scores of chunk n.
+        auto outputs = [&](int n) -> bool { return tile_wait_warp(&pv_done[x][n & 1], (uint32_t)(n >> 1) & 1u, dead); };
         for (int t = 0; t < chunks; ++t) {
             const int c0 = w.begin + t * kTileK;
-            if (!mode.any_seen(w, c0, x)) continue;
+            if (!range.any(t)) continue;
             const uint32_t buf = lanes + (count & 1) * kTileK;
             ok = tile_wait_warp(&s_full[x][count & 1], (uint32_t)(count >> 1) & 1u, dead);
-            ok = ok && outputs_until(count - 1);                        // (long complete: the scores were issued behind them)
             if (!ok) break;
             tile_after_sync();
             float z[64];
             tile_ld32(buf, z);
             tile_ld32(buf + 32, z + 32);
             tile_wait_ld();
-            if (!mode.all_seen(w, c0, x)) {                             // uniform over the tile's warps
+            if (!range.whole(t)) {                                      // uniform over the tile's warps
                 const uint32_t s0 = mode.seen(w, c0, i, 0), s1 = mode.seen(w, c0, i, 1);
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
@@ -476,7 +489,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             const bool grown = m_chunk > m + 8.f && m > -INFINITY;
             if (m == -INFINITY) m = m_chunk;
             if (__any_sync(0xffffffffu, grown)) {                       // (count > 0)
-                ok = outputs_until(count);                              // those of this chunk wait for its weights
+                ok = outputs(count - 1);                                // those of this chunk wait for its weights
                 if (!ok) break;
                 tile_after_sync();
                 const float f = grown ? fast_exp2(m - m_chunk) : 1.f;
@@ -513,7 +526,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             tile_arrive(&p_full[x][count & 1]);
             ++count;
         }
-        ok = ok && outputs_until(count);
+        if (ok && count > 0) ok = outputs(count - 1);
         tile_after_sync();
         if (ok) mode.template finish<LG>(w, lanes + kOut, i, m, l);
         else if (threadIdx.x == 0) mode.failed();
