@@ -539,7 +539,7 @@ __device__ __forceinline__ bool attend_unit(const AttendParams& p, bool prefix, 
 template <typename T, int LG, int N>
 __global__ void __launch_bounds__(kAtWarps * 32) attend_kernel(const __grid_constant__ AttendParams p) {
     extern __shared__ __align__(128) char attend_smem[];
-    asm volatile("griddepcontrol.launch_dependents;");
+    if (p.slots > 1) asm volatile("griddepcontrol.launch_dependents;");       // the join may take its place (and wait there)
     constexpr int R = kAtRows;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const bool prefix = (int)blockIdx.x < p.p_ctas;
@@ -560,6 +560,9 @@ __global__ void __launch_bounds__(kAtWarps * 32) attend_kernel(const __grid_cons
         }
     }
     attend_finish<T, N>(p, u, active, wpu, attend_smem, ml, warp, lane);
+    // Beside the tensor-core tiles of the prefixes, launched before: this kernel is not over before they are, so that the
+    // join, which waits for this kernel, finds both.
+    if (p.t_lg > 0 && blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // Adds up the partial results of a row and layer: 16 threads for its outputs, four each, times G groups that
@@ -593,8 +596,8 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
     if (mine) {
 #pragma unroll 4
         for (int s = begin + grp; s < p.slots; s += G)
-            add(p.part_ml[s * n_rows + at],
-                *reinterpret_cast<const float4*>(p.part_o + (((long long)s * p.n_layers + layer) * n_rows + at) * kDh + c * 4));
+            add(__ldcg(p.part_ml + s * n_rows + at),
+                __ldcg(reinterpret_cast<const float4*>(p.part_o + (((long long)s * p.n_layers + layer) * n_rows + at) * kDh + c * 4)));
     }
     if constexpr (G > 1) {
         s_o[threadIdx.x] = o;

@@ -16,7 +16,6 @@ using namespace san;
 
 namespace {
 
-constexpr int kTileRows = 32;               // query rows behind a prefix from which on it goes to the tensor-core tiles
 constexpr int kSms = 148;                   // the cuts are made for this GPU; any other number of SMs works
 inline long long div_up(long long a, long long b) { return (a + b - 1) / b; }
 inline int32_t cuda_status(cudaError_t e) { return e == cudaSuccess ? SAN_OK : SAN_ERR_CUDA; }
@@ -36,9 +35,9 @@ int32_t opt_in(const void* fn, int bytes, bool* set) {
 // Launches `fn` so that its CTAs may be set up while the kernel before it on the stream still runs
 // (it waits with griddepcontrol.wait before it reads what that one wrote).
 template <typename P>
-int32_t launch_after(void (*fn)(P), dim3 grid, unsigned block, cudaStream_t st, const P& p) {
+int32_t launch_after(void (*fn)(P), dim3 grid, unsigned block, cudaStream_t st, const P& p, size_t smem = 0) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid; cfg.blockDim = dim3(block); cfg.stream = st;
+    cfg.gridDim = grid; cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
@@ -156,8 +155,14 @@ int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int wi
         p.n_prefix = x->n_prefix; p.pcap = x->cap_len; p.pv_stride = x->v_stride * e;
         p.max_prefix = x->max_len ? x->max_len : x->cap_len;
         p.max_group = x->max_group ? x->max_group : std::max(1, r->n_items);
-        const long long rows = (long long)p.max_group * p.group;
-        if (r->dtype == SAN_BF16 && rows > kTileRows) {
+        // Prefixes go to the tensor-core tiles where that is estimated to be faster.  Both measured: the streams of
+        // eight query rows get through 2900 slots (32 positions of one plane) a microsecond, the tiles through
+        // a chunk of 64 positions for 256 rows and up to two layers per SM and microsecond, after 9 us of set-up
+        // and hand-over.
+        const long long rows = (long long)p.max_group * p.group, tile_runs = (long long)p.n_prefix * p.Hk * div_up(rows, 2 * kTileQ) * div_up(r->n_layers, kTileMaxLayers);
+        const double streams_us = (double)p.n_prefix * p.Hk * div_up(rows, R) * div_up(p.max_prefix, kAtTile) * (p.n_layers + p.n_lg) / 2900.0;
+        const double tiles_us = (double)div_up(tile_runs * div_up(p.max_prefix, kTileK), kSms) + 9.0;
+        if (r->dtype == SAN_BF16 && tiles_us < streams_us) {
             p.t_n_lg = (int)div_up(r->n_layers, kTileMaxLayers);
             p.t_lg = (int)div_up(r->n_layers, p.t_n_lg);
             p.t_n_lg = (int)div_up(r->n_layers, p.t_lg);
@@ -208,8 +213,13 @@ int32_t launch_attend_as(const AttendPlan& a, cudaStream_t st) {
     static bool set[64] = {};
     const int32_t rc = opt_in((const void*)attend_kernel<T, LG, N>, smem, set);
     if (rc != SAN_OK) return rc;
-    attend_kernel<T, LG, N><<<(unsigned)a.ctas, kAtWarps * 32, smem, st>>>(a.p);
-    if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
+    if (a.tiles > 0) {                              // beside the tiles, which it does not depend on
+        const int32_t rc2 = launch_after(&attend_kernel<T, LG, N>, dim3((unsigned)a.ctas), kAtWarps * 32, st, a.p, smem);
+        if (rc2 != SAN_OK) return rc2;
+    } else {
+        attend_kernel<T, LG, N><<<(unsigned)a.ctas, kAtWarps * 32, smem, st>>>(a.p);
+        if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
+    }
     if (a.p.slots == 1) return SAN_OK;
     const long long rows = (long long)a.p.n_items * a.p.H;
     const int groups = a.p.slots <= 6 ? 1 : a.p.slots <= 12 ? 4 : 16;
@@ -400,7 +410,14 @@ int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int
     p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)kDh));
     if ((long long)n_seq * p.n_lg > 65535) return SAN_ERR_SHAPE;
     if (max_len >= kTileQ) {
-        const dim3 tiles((unsigned)div_up(max_len, 2 * kTileQ), (unsigned)n_heads, (unsigned)(n_seq * p.n_lg));
+        // A CTA takes a pair of tiles.  Where the last wave would hold less than half of the SMs' CTAs, its pairs are dealt as
+        // single tiles, which take about two thirds of a pair's time: 8192 positions x 16 sequences and heads are
+        // 3.35 waves of pairs, or three waves and 104 single tiles.
+        const long long pairs = div_up(max_len, 2 * kTileQ), all = pairs * n_heads * n_seq * p.n_lg, rest = all % kSms;
+        if (2 * all > 0x7fffffffLL) return SAN_ERR_SHAPE;
+        p.pairs = (int)pairs;
+        p.whole = (int)(2 * rest <= kSms ? all - rest : all);
+        const dim3 tiles((unsigned)(2 * all - p.whole));
         cudaStream_t st = static_cast<cudaStream_t>(stream);
         return p.lg == 1 ? launch_tiles<TileWindow, 1>(p, tiles, st) : launch_tiles<TileWindow, 2>(p, tiles, st);
     }

@@ -156,6 +156,24 @@ struct TileWork {
     int rows, layer0, layers;               // query rows, up to two tiles of them
 };
 
+// A warp writes 128 bytes of each of its lanes' rows (`piece`, to `dst`, if `mine`) by way of shared memory, so that eight lanes
+// write a row's 128 bytes side by side.  `rows`: the warp's own 32 rows of 128 bytes.
+__device__ __forceinline__ void tile_write_rows(char* rows, const uint4 (&piece)[8], char* dst, bool mine) {
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(rows + lane * 128 + ((c ^ (lane & 7)) << 4)) = piece[c];
+    __syncwarp();
+    const unsigned long long to = mine ? reinterpret_cast<unsigned long long>(dst) : 0ull;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int r = j * 4 + (lane >> 3), c = lane & 7;
+        const unsigned long long at = __shfl_sync(0xffffffffu, to, r);
+        const uint4 v = *reinterpret_cast<const uint4*>(rows + r * 128 + ((c ^ (r & 7)) << 4));
+        if (at) *reinterpret_cast<uint4*>(at + (c << 4)) = v;
+    }
+}
+
 // Which chunks (numbers t of a CTA's run) a tile takes part in: t < sinks or first <= t < end; and from which to which all
 // of its rows see all of the chunk.
 struct TileRange {
@@ -164,18 +182,28 @@ struct TileRange {
     __device__ __forceinline__ bool whole(int t) const { return t >= whole_first && t < whole_end; }
 };
 
-// ---- windowed prompts: grid (query tiles, heads, sequences x layer groups)
+// ---- windowed prompts: CTA = (query tiles, head, sequence, layer group), longest prompts' ends first; CTAs from
+// `whole` on take one tile each of the pairs that are left (see launch_tiles of the host side)
 struct TileWindow {
+    static constexpr int kRegs = 168;
     const WindowParams& p;
     int seq, head, a0, len;
     __device__ __forceinline__ bool work(TileWork* w) {
-        head = blockIdx.y; seq = blockIdx.z / p.n_lg;
-        w->layer0 = blockIdx.z % p.n_lg * p.lg;
+        int index = blockIdx.x, half = -1;
+        if (index >= p.whole) {
+            half = (index - p.whole) & 1;
+            index = p.whole + (index - p.whole) / 2;
+        }
+        const int layer_group = index % p.n_lg; index /= p.n_lg;
+        head = index % p.H; index /= p.H;
+        seq = index % p.n_seq;
+        const int pair = p.pairs - 1 - index / p.n_seq;
+        w->layer0 = layer_group * p.lg;
         w->layers = min(p.lg, p.n_layers - w->layer0);
         len = max(0, min(p.lens[seq], p.max_len));
-        a0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * 2 * kTileQ;
+        a0 = pair * 2 * kTileQ + (half > 0 ? kTileQ : 0);
         if (a0 >= len) return false;
-        w->rows = min(2 * kTileQ, len - a0);
+        w->rows = min(half < 0 ? 2 * kTileQ : kTileQ, len - a0);
         w->lo = max(0, a0 - p.window + 1);
         w->ns = min(p.n_sink, w->lo);
         w->begin = 0;
@@ -209,14 +237,15 @@ struct TileWindow {
         const uint32_t recent = ~below(w.ns + max(a - p.window + 1, w.lo) - w.lo);
         return (recent | below(w.ns + max(0, p.n_sink - w.lo))) & below(min(self + 1, w.end));
     }
-    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, int i, float m, float l) const {
+    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, char* rows, int i, float m, float l) const {
         const bool mine = i < w.rows;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         bool odd = false;
+        __nv_bfloat16* dst = p.out + (((long long)seq * p.cap + a0 + i) * p.H + head) * kDh;
 #pragma unroll
         for (int y = 0; y < LG; ++y) {
             if (y >= w.layers) break;
-            uint4* dst = reinterpret_cast<uint4*>(p.out + (w.layer0 + y) * p.out_layer + (((long long)seq * p.cap + a0 + i) * p.H + head) * kDh);
+            uint4 piece[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 float o[32];
@@ -225,12 +254,12 @@ struct TileWindow {
                 tile_wait_ld();
 #pragma unroll
                 for (int c = 0; c < 32; ++c) { o[c] *= inv; odd |= o[c] != o[c]; }
-                if (mine)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        dst[h * 4 + c] = make_uint4(pack_bf16(o[8 * c], o[8 * c + 1]), pack_bf16(o[8 * c + 2], o[8 * c + 3]),
-                                                    pack_bf16(o[8 * c + 4], o[8 * c + 5]), pack_bf16(o[8 * c + 6], o[8 * c + 7]));
+                for (int c = 0; c < 4; ++c)
+                    piece[h * 4 + c] = make_uint4(pack_bf16(o[8 * c], o[8 * c + 1]), pack_bf16(o[8 * c + 2], o[8 * c + 3]),
+                                                  pack_bf16(o[8 * c + 4], o[8 * c + 5]), pack_bf16(o[8 * c + 6], o[8 * c + 7]));
             }
+            tile_write_rows(rows, piece, reinterpret_cast<char*>(dst + (w.layer0 + y) * p.out_layer), mine);
         }
         unsigned again = __ballot_sync(0xffffffffu, odd && mine);       // see san_window.cuh
         while (again) {
@@ -244,9 +273,11 @@ struct TileWindow {
 
 // ---- shared prefixes: units as in attend_unit, 128 query rows and runs of p_span chunks
 struct TilePrefix {
+    static constexpr int kRegs = 136;       // leaves registers for a CTA of attend_kernel beside it on the SM
     const AttendParams& p;
     int g, hk, row0, slot;
     __device__ __forceinline__ bool work(TileWork* w) {
+        asm volatile("griddepcontrol.launch_dependents;");              // the sequences' own rows may be worked on meanwhile
         int index = blockIdx.x;
         const int lg = index % p.t_n_lg; index /= p.t_n_lg;
         const int split = index % p.p_splits; index /= p.p_splits;
@@ -286,7 +317,7 @@ struct TilePrefix {
         const int n = w.end - c0 - 32 * q;
         return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1;
     }
-    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, int i, float m, float l) const {
+    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, char* rows, int i, float m, float l) const {
         const long long n_rows = (long long)p.n_items * p.H, at = i < w.rows ? place(i) : 0;
         const bool mine = i < w.rows;
         if (mine && w.layer0 == 0) p.part_ml[slot * n_rows + at] = make_float2(m, l);
@@ -294,16 +325,14 @@ struct TilePrefix {
 #pragma unroll
         for (int y = 0; y < LG; ++y) {
             if (y >= w.layers) break;
-            float4* dst = reinterpret_cast<float4*>(p.part_o + (((long long)slot * p.n_layers + w.layer0 + y) * n_rows + at) * kDh);
+            float* dst = p.part_o + (((long long)slot * p.n_layers + w.layer0 + y) * n_rows + at) * kDh;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                float o[32];
+                uint4 piece[8];
                 __syncwarp();
-                tile_ld32(t_out + y * 64 + h * 32, o);
+                tile_ld32(t_out + y * 64 + h * 32, reinterpret_cast<float*>(piece));
                 tile_wait_ld();
-                if (mine)
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) dst[h * 8 + c] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+                tile_write_rows(rows, piece, reinterpret_cast<char*>(dst + h * 32), mine);
             }
         }
     }
@@ -313,14 +342,13 @@ struct TilePrefix {
 };
 
 template <class Mode, int LG, class Params>
-__global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_constant__ Params params) {
+__global__ void __maxnreg__(Mode::kRegs) tile_kernel(const __grid_constant__ Params params) {
     constexpr uint32_t kCols = 512, kTileCols = 256, kOut = 128;        // a tile's columns: scores twice (weights over them), outputs
     static_assert(kOut + 64 * LG <= kTileCols, "tensor memory");
     extern __shared__ __align__(1024) char tile_smem[];
-    __shared__ __align__(8) uint64_t k_full[kTileKSlots], k_free[kTileKSlots], v_full[kTileVSlots], v_free[kTileVSlots], s_full[2][2], p_full[2][2], pv_done[2][2];
+    __shared__ __align__(8) uint64_t k_full[kTileKSlots], k_free[kTileKSlots], v_full[kTileVSlots], v_free[kTileVSlots], s_full[2][2], p_full[2][2], pv_done[2][2], q_full[2];
     __shared__ uint32_t tmem_s;
     __shared__ int dead_s;
-    asm volatile("griddepcontrol.launch_dependents;");
     Mode mode{params};
     TileWork w;
     if (!mode.work(&w)) return;                                         // uniform over the CTA, before anything is allocated
@@ -334,6 +362,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         for (int i = 0; i < kTileVSlots; ++i) { tile_bar_init(&v_full[i], kTileLoaders); tile_bar_init(&v_free[i], 1); }
         for (int i = 0; i < 2; ++i) {
             tile_bar_init(&s_full[i][0], 1); tile_bar_init(&s_full[i][1], 1);
+            tile_bar_init(&q_full[i], kTileQ);
             tile_bar_init(&p_full[i][0], kTileQ); tile_bar_init(&p_full[i][1], kTileQ); tile_bar_init(&pv_done[i][0], 1); tile_bar_init(&pv_done[i][1], 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -343,14 +372,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(tile_u32(&tmem_s)), "r"(kCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    if (threadIdx.x < 2 * kTileQ) {
-        const int i = threadIdx.x;
-        const uint4* src = i < w.rows ? mode.query(i) : nullptr;
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-            *reinterpret_cast<uint4*>(sQ + i * 128 + ((c ^ (i & 7)) << 4)) = src ? src[c] : make_uint4(0, 0, 0, 0);
-    }
-    tile_proxy_fence();
     tile_before_sync();
     __syncthreads();
     tile_after_sync();
@@ -406,7 +427,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
             if (elected) tile_commit(&v_free[slot]);
             return true;
         };
-        bool go = chunks == 0 || scores(0);
+        bool go = tile_wait_warp(&q_full[0], 0u, dead) && tile_wait_warp(&q_full[1], 0u, dead) && (chunks == 0 || scores(0));
         for (int t = 0; t < chunks && go; ++t) go = (t + 1 >= chunks || scores(t + 1)) && outputs(t);
     } else if (warp >= 8) {
         // thread: 16-byte piece c of rows r0, r0 + 12, ...
@@ -451,6 +472,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)x * kTileCols;
         const float sc = params.scale_log2e;
         const unsigned long long sc2 = tile_pair(sc, sc);
+        {
+            const uint4* src = i < w.rows ? mode.query(i) : nullptr;
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                *reinterpret_cast<uint4*>(sQ + i * 128 + ((c ^ (i & 7)) << 4)) = src ? src[c] : make_uint4(0, 0, 0, 0);
+            tile_proxy_fence();
+            tile_arrive(&q_full[x]);
+        }
         float m = -INFINITY, l = 0.f;
         bool ok = true;
         int count = 0;
@@ -528,7 +557,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         }
         if (ok && count > 0) ok = outputs(count - 1);
         tile_after_sync();
-        if (ok) mode.template finish<LG>(w, lanes + kOut, i, m, l);
+        if (ok) mode.template finish<LG>(w, lanes + kOut, sQ + (i & ~31) * 128, i, m, l);       // (the queries have been read)
         else if (threadIdx.x == 0) mode.failed();
     }
     tile_before_sync();

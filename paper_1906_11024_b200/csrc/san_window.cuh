@@ -19,12 +19,14 @@ struct WindowParams {
     const int* lens;
     long long v_layer, out_layer;           // elements between layers
     int n_seq, cap, H, Hk, group, n_layers, lg, n_lg, max_len, window, n_sink;
+    int pairs, whole;                       // tensor-core tiles: pairs of tiles of a sequence, CTAs that take a pair
     float scale_log2e;
 };
 
 constexpr int kWinQ = 64, kWinTile = 64, kWinSlots = 4;
 
-// Row a of (sequence, head), one layer, by one warp: the definition, over the rows that are seen.
+// Row a of (sequence, head), one layer, by one warp: the definition, over the rows that are seen.  Leaves as soon as the
+// row is known to be NaN, so that inputs full of NaN cost next to nothing.
 __device__ __noinline__ void window_row_again(const WindowParams& p, int seq, int head, int layer, int a, int lane) {
     const long long kv = ((long long)seq * p.cap * p.Hk + head / p.group) * kDh + lane * 2;
     const long long at = (((long long)seq * p.cap + a) * p.H + head) * kDh + lane * 2;
@@ -38,12 +40,19 @@ __device__ __noinline__ void window_row_again(const WindowParams& p, int seq, in
             const long long b = i < ns ? i : lo + i - ns;
             const float2 k = two(p.k + kv + b * step);
             const float z = warp_sum(q.x * k.x + q.y * k.y) * p.scale_log2e;
-            if (pass == 0) { m = fmaxf(m, z); continue; }
+            if (pass == 0) {
+                m = fmaxf(m, z);
+                if (z == z) continue;
+                l = z;                       // a score that is seen is NaN: so is the row
+                pass = 2;
+                break;
+            }
             const float w = exp2f(z - (m == -INFINITY ? 0.f : m));
             if (w == 0.f) continue;
             const float2 v = two(p.v + layer * p.v_layer + kv + b * step);
             l += w;
             ox = fmaf(w, v.x, ox); oy = fmaf(w, v.y, oy);
+            if (__all_sync(0xffffffffu, ox != ox && oy != oy)) break;        // it cannot become anything else
         }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     *reinterpret_cast<uint32_t*>(p.out + layer * p.out_layer + at) = pack_bf16(ox * inv, oy * inv);

@@ -174,17 +174,37 @@ def _prefix(r, plens, groups, pcap, max_len=0, max_prefix=0, max_group=0, skip=(
 @pytest.mark.parametrize("lens,cap,plens,groups,pcap,H,Hk,L", [
     ([0], 1, [1], [0, 1], 1, 1, 1, 1),                                     # nothing of its own
     ([9, 3, 1, 7], 10, [33], [0, 4], 40, 2, 2, 1),                         # one beam behind one prompt
-    ([5, 0, 12, 40, 40, 3, 0], 40, [65, 0, 31], [0, 2, 5, 7], 70, 2, 2, 3),    # an empty prefix, an empty row behind it
+    ([5, 0, 12, 40, 40, 3, 0], 40, [65, 0, 31], [0, 2, 5, 7], 70, 2, 2, 3),    # an empty prefix
+    ([0, 3, 0], 4, [0, 9], [0, 2, 3], 9, 2, 1, 2),                         # a row that sees nothing at all
     ([5, 6, 7, 8, 9], 10, [64, 10], [1, 1, 4], 64, 3, 3, 2),               # a prefix without rows; rows without a prefix
     ([4] * 37, 6, [130], [0, 37], 130, 2, 1, 2),                           # more query rows than a unit holds
     ([4] * 70, 4, [100, 90], [0, 50, 70], 100, 4, 4, 1),
-    ([4] * 130, 4, [300], [0, 130], 300, 1, 1, 1),                         # a whole tensor-core tile and two rows
+    ([4] * 130, 4, [300], [0, 130], 300, 1, 1, 1),
     ([3] * 100, 4, [257, 511], [0, 71, 100], 512, 2, 1, 2),                # 142 and 58 query rows, odd prefixes
+    ([2] * 300, 4, [9, 4000, 3999], [0, 3, 3, 300], 4000, 2, 2, 1),        # tensor-core tiles: three rows, none, two tiles and 41 rows
+    ([2] * 257, 4, [2500], [0, 257], 2500, 4, 2, 3),                       # the same, query heads in pairs, two layer groups
     ([17, 2], 20, [2000], [0, 2], 2000, 2, 2, 5),                          # one prefix over several units
 ])
 def test_prefix_lengths_groups_heads(dtype, lens, cap, plens, groups, pcap, H, Hk, L):
     r = Rows(dtype, lens, H, Hk, L, cap, seed=len(lens))
     _prefix(r, plens, groups, pcap)
+
+
+def test_tensor_core_tiles_with_scores_that_keep_growing():
+    """Scores that rise along the prefix by more than 2^8 between chunks: the running maximum moves, outputs are scaled."""
+    n, P = 300, 4096
+    r = Rows("bf16", [1] * n, 2, 2, 2, 2, seed=3)
+    gen = torch.Generator().manual_seed(2)
+    pk, pv = randn(gen, 1, P, 2, DH, dtype=r.dt), randn(gen, 2, 1, P, 2, DH, dtype=r.dt)
+    pk *= torch.linspace(0.1, 40.0, P)[None, :, None, None].to(r.dt)
+    dev = [x.to(DEV) for x in (pk, pv, torch.tensor([P], dtype=torch.int32), torch.tensor([0, n], dtype=torch.int32))]
+    a = r.args()
+    x = B.shared_prefix(d_k=dev[0], d_v=dev[1], v_stride=dev[1][0].numel(), n_prefix=1, cap_len=P, d_lens=dev[2], d_first=dev[3])
+    rc, nb = B.san_prefix_attn_bytes(a, x)
+    ws = torch.empty(nb, dtype=torch.uint8, device=DEV)
+    B.check(B.san_prefix_attn(a, x, ws, nb))
+    torch.cuda.synchronize()
+    r.check(lambda i: range(1), lambda i, hk: (pk[0, :, hk].double(), pv[:, 0, :, hk].double()))
 
 
 def test_prefix_bounds_from_the_host_and_a_stream():

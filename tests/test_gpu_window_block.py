@@ -114,6 +114,34 @@ def test_what_a_row_does_not_see_does_not_reach_it(what):
     assert not torch.isfinite(got[:, 0, sees]).any()
 
 
+def test_inputs_full_of_nan():
+    """Every row comes out as NaN, and soon: 2000 rows of a causal prompt."""
+    n, cap, H = 1, 2000, 2
+    x = torch.full((n, cap, H, DH), float("nan"), dtype=torch.bfloat16, device=DEV)
+    out = torch.zeros(1, n, cap, H, DH, dtype=torch.bfloat16, device=DEV)
+    dl = torch.tensor([cap], dtype=torch.int32, device=DEV)
+    ok = torch.randn(n, cap, H, DH, device=DEV).to(torch.bfloat16)
+    for q, k, v in ((x, ok, ok), (ok, x, ok), (ok, ok, x)):
+        B.check(B.san_window_block(B.SAN_BF16, H, H, 1, cap, 0, q, k, v[None].contiguous(), dl, n, cap, 0, out))
+        torch.cuda.synchronize()
+        assert torch.isnan(out).all()
+
+
+def test_scores_that_keep_growing():
+    """The running maximum moves by more than 2^8 from chunk to chunk: outputs are scaled."""
+    gen = torch.Generator().manual_seed(8)
+    l, H = 700, 2
+    q, k, v = (randn(gen, 1, l, H, DH, dtype=torch.bfloat16) for _ in range(3))
+    k *= torch.linspace(0.1, 60.0, l)[None, :, None, None].to(torch.bfloat16)
+    out = torch.full((2, 1, l, H, DH), -7.0, dtype=torch.bfloat16, device=DEV)
+    vv = torch.stack([v, -v])
+    dq, dk, dv = q.to(DEV), k.to(DEV), vv.to(DEV)
+    dl = torch.tensor([l], dtype=torch.int32, device=DEV)
+    B.check(B.san_window_block(B.SAN_BF16, H, H, 2, 400, 2, dq, dk, dv, dl, 1, l, 0, out))
+    torch.cuda.synchronize()
+    _check(q, k, vv, out.cpu(), [l], 400, 2)
+
+
 def test_scores_in_the_thousands():
     lens = [140]
     q, k, v, got = _run(lens, 140, 1, 1, 1, 50, 4, scale=512.0)
