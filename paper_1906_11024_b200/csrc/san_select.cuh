@@ -294,6 +294,7 @@ __device__ __forceinline__ void select_rows(const SelectParams& p) {
     float top = -INFINITY, m = 0.f, part[4] = {0.f, 0.f, 0.f, 0.f};      // two pairs of partial sums
     float bound = -INFINITY;
     if (threadIdx.x == 0) s_count = 0;
+    int step = 0;
     Held next;
     load(next, begin);
     for (int base = begin; base < end; base += STEP) {
@@ -362,11 +363,14 @@ __device__ __forceinline__ void select_rows(const SelectParams& p) {
                     }
             }
         }
+        // The list is looked at every fourth step: some hundred keys come in between.
+        if ((++step & 3) != 0 || base + STEP >= end) continue;
         __syncthreads();
         const int count = s_count;
+        __syncthreads();
         if (count > kSelList) {                                       // keys were lost: only the sums go on
             bound = INFINITY;
-        } else if (count > kSelLong && base + STEP < end) {
+        } else if (count > kSelLong) {
             if (warp == 0) {
                 int left;
                 const uint32_t b = tighten(s_list, count, p.beam, order_f32(bound), &left, lane);
@@ -376,6 +380,7 @@ __device__ __forceinline__ void select_rows(const SelectParams& p) {
             bound = unorder_f32(s_bound);
         }
     }
+    __syncthreads();
     float sum = (part[0] + part[1]) + (part[2] + part[3]);
     if (fabsf(top) < 1e30f) sum *= exp2_fast(-fmaf(top, c, -m));      // 2^(M - c top)
     const float wtop = warp_max(top);
