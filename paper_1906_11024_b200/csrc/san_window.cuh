@@ -2,10 +2,15 @@
 // b > a - window or b < n_sink; S = Softmax(q.K^T / 8) over those, computed once and applied to
 // each layer of the block (Eq. 3, Eq. 4).
 //
-// window_block_kernel (mma.sync): CTA = 64 query rows of one (sequence, head, layer group), 16 per warp.  The CTA walks the
+// window_block_kernel (mma.sync; sequences below 128 positions, longer ones go to the tiles of san_tile.cuh): CTA = 32 query
+// rows of one (sequence, head, layer group), 8 per warp, which are the N side of both products as in attend_kernel: 16
+// accumulator registers a layer, so that four CTAs fit an SM with three layers each.  The CTA walks the
 // rows that any of its queries sees - the sinks, then the window of its first query up to its last query -
 // in tiles of 64 through a ring of shared-memory slots that cp.async fills three slots ahead (keys, then each
-// layer's values), with the running maximum and sum of the softmax; scores stay in registers.
+// layer's values), with the running maximum and sum of the softmax; scores stay in registers.  Bound by the
+// chain of one CTA (length, copies, products: some 4 us) and the number of CTAs: 64 sentences of up to 60 positions, 8 heads,
+// 3 layers: 16.7 us with 16 queries per warp and layers in groups of two (each recomputing the scores), 14.6 in one
+// group (236 registers, two CTAs per SM).
 // A value that a row does not see has weight zero, and zero times an infinity or NaN is NaN: a row whose
 // output came out as NaN is computed again over just the rows it sees (window_row_again).
 #pragma once
@@ -23,7 +28,7 @@ struct WindowParams {
     float scale_log2e;
 };
 
-constexpr int kWinQ = 64, kWinTile = 64, kWinSlots = 4;
+constexpr int kWinQ = 32, kWinTile = 64, kWinSlots = 4;
 
 // Row a of (sequence, head), one layer, by one warp: the definition, over the rows that are seen.  Leaves as soon as the
 // row is known to be NaN, so that inputs full of NaN cost next to nothing.
@@ -94,26 +99,32 @@ __global__ void __launch_bounds__(128) window_block_kernel(const __grid_constant
     for (int i = 0; i < kWinSlots - 1; ++i) fill();
 
     const int g = lane >> 2, t4 = lane & 3, r8 = lane & 7, mat = lane >> 3;
-    const int qa0 = a0 + warp * 16;                                       // the warp's first query
-    uint32_t qa[4][4];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int a = qa0 + g + h * 8;
+    const int qa0 = a0 + warp * 8;                                        // the warp's first query
+    uint32_t qb[4][2];                                                    // B: query g, dims 16 c + 2 t4 .. and 8 further on
+    {
+        const int a = qa0 + g;
         const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q + (((long long)seq * p.cap + a) * p.H + head) * kDh) + t4;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            qa[c][h] = a < a1 ? src[c * 8] : 0u;
-            qa[c][h + 2] = a < a1 ? src[c * 8 + 4] : 0u;
+            qb[c][0] = a < a1 ? src[c * 8] : 0u;
+            qb[c][1] = a < a1 ? src[c * 8 + 4] : 0u;
         }
     }
-    float acc[LG][8][4];
+    float acc[LG][4][4];                                                  // [layer][16 dims]: dims g and g + 8, queries 2 t4 and 2 t4 + 1
 #pragma unroll
     for (int y = 0; y < LG; ++y)
 #pragma unroll
-        for (int d = 0; d < 8; ++d)
+        for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[y][d][e] = 0.f;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    const uint32_t k_row = ((mat & 1) * 8 + r8) * 128, v_row = ((mat >> 1) * 8 + r8) * 128;
+    uint32_t k_chunk[4], v_chunk[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        k_chunk[c] = (uint32_t)((2 * c + (mat >> 1)) ^ r8) << 4;
+        v_chunk[c] = (uint32_t)((2 * c + (mat & 1)) ^ r8) << 4;
+    }
 
     int slot = 0;
     auto next = [&]() -> uint32_t {
@@ -125,120 +136,126 @@ __global__ void __launch_bounds__(128) window_block_kernel(const __grid_constant
         return s;
     };
     for (int at = 0; at < n; at += kWinTile) {
-        const uint32_t ks = next();
+        const uint32_t ks = next() + k_row;
         const int b_first = at < ns ? 0 : lo + at - ns, b_last = lo + at + kWinTile - 1 - ns;
         // every one of the warp's queries sees the whole tile: nothing to mask
-        const bool whole = at >= ns && at + kWinTile <= n && b_last <= qa0 && b_first > qa0 + 15 - p.window;
-        const bool none = at >= ns && b_first > qa0 + 15;                 // behind the warp's last query
-        uint32_t pa[4][4];
+        const bool whole = at >= ns && at + kWinTile <= n && b_last <= qa0 && b_first > qa0 + 7 - p.window;
+        const bool none = at >= ns && b_first > qa0 + 7;                  // behind the warp's last query
+        uint32_t pb[4][2];
         if (!none) {
-            float s[8][4];
+            float s[4][4];                                                // positions 16 c + g and + 8, queries 2 t4 and 2 t4 + 1
 #pragma unroll
-            for (int c8 = 0; c8 < 8; ++c8) {
+            for (int c = 0; c < 4; ++c) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[c8][e] = 0.f;
-                uint32_t b[8];
-                const uint32_t row = ks + (c8 * 8 + r8) * 128;
-                ldsm4(b, row + ((mat ^ r8) << 4));
-                ldsm4(b + 4, row + (((mat + 4) ^ r8) << 4));
+                for (int e = 0; e < 4; ++e) s[c][e] = 0.f;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) mma_bf16(s[c8], qa[c], b[2 * c], b[2 * c + 1]);
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t a[4];
+                    ldsm4(a, ks + c * 16 * 128 + k_chunk[k]);
+                    mma_bf16(s[c], a, qb[k][0], qb[k][1]);
+                }
             }
             float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-            for (int c8 = 0; c8 < 8; ++c8)
+            for (int c = 0; c < 4; ++c)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     bool seen = true;
                     if (!whole) {
-                        const int at1 = at + c8 * 8 + t4 * 2 + (e & 1), a = qa0 + g + (e >> 1) * 8;
+                        const int at1 = at + c * 16 + (e >> 1) * 8 + g, a = qa0 + t4 * 2 + (e & 1);
                         const int b = at1 < ns ? at1 : lo + at1 - ns;
                         seen = at1 < n && b <= a && (b > a - p.window || b < p.n_sink);
                     }
-                    s[c8][e] = seen ? s[c8][e] * p.scale_log2e : -INFINITY;
-                    top[e >> 1] = fmaxf(top[e >> 1], s[c8][e]);
+                    s[c][e] = seen ? s[c][e] * p.scale_log2e : -INFINITY;
+                    top[e & 1] = fmaxf(top[e & 1], s[c][e]);
                 }
             float alpha[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
-                top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
-                const float m_new = fmaxf(m[h], top[h]);
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], o));
+                const float m_new = fmaxf(m[j], top[j]);
                 const float base = m_new == -INFINITY ? 0.f : m_new;
-                alpha[h] = m[h] == m_new ? 1.f : fast_exp2(m[h] - base);
-                m[h] = m_new;
+                alpha[j] = m[j] == m_new ? 1.f : fast_exp2(m[j] - base);
+                m[j] = m_new;
                 float sum = 0.f;
 #pragma unroll
-                for (int c8 = 0; c8 < 8; ++c8)
+                for (int c = 0; c < 4; ++c)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        s[c8][2 * h + e] = fast_exp2(s[c8][2 * h + e] - base);
-                        sum += s[c8][2 * h + e];
+                        s[c][2 * e + j] = fast_exp2(s[c][2 * e + j] - base);
+                        sum += s[c][2 * e + j];
                     }
-                l[h] = l[h] * alpha[h] + sum;
+                l[j] = l[j] * alpha[j] + sum;
             }
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                pa[c][0] = pack_bf16(s[2 * c][0], s[2 * c][1]);
-                pa[c][1] = pack_bf16(s[2 * c][2], s[2 * c][3]);
-                pa[c][2] = pack_bf16(s[2 * c + 1][0], s[2 * c + 1][1]);
-                pa[c][3] = pack_bf16(s[2 * c + 1][2], s[2 * c + 1][3]);
-            }
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(pb[c][e]) : "r"(pack_bf16(s[c][2 * e], s[c][2 * e + 1])));
             if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
 #pragma unroll
                 for (int y = 0; y < LG; ++y)
 #pragma unroll
-                    for (int d = 0; d < 8; ++d)
+                    for (int d = 0; d < 4; ++d)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[y][d][e] *= alpha[e >> 1];
+                        for (int e = 0; e < 4; ++e) acc[y][d][e] *= alpha[e & 1];
             }
         }
 #pragma unroll
         for (int y = 0; y < LG; ++y) {
             if (y >= layers) break;
-            const uint32_t vs = next();
+            const uint32_t vs = next() + v_row;
             if (none) continue;
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int d = 0; d < 8; d += 2) {
-                    uint32_t b[4];
-                    ldsm4t(b, vs + (c * 16 + (mat & 1) * 8 + r8) * 128 + (((d + (mat >> 1)) ^ r8) << 4));
-                    mma_bf16(acc[y][d], pa[c], b[0], b[1]);
-                    mma_bf16(acc[y][d + 1], pa[c], b[2], b[3]);
+                for (int d = 0; d < 4; ++d) {
+                    uint32_t a[4];
+                    ldsm4t(a, vs + c * 16 * 128 + v_chunk[d]);
+                    mma_bf16(acc[y][d], a, pb[c][0], pb[c][1]);
                 }
         }
     }
     cp_wait<0>();
+    __syncthreads();                                                      // the ring is free: outputs go through it, a warp's 8 rows at a time
+    char* rows = ring + warp * (8 * 128);
     bool odd[2] = {false, false};
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-        const float inv = l[h] == 0.f ? 0.f : 1.f / l[h];
-        const int a = qa0 + g + h * 8;
-        if (a < a1) {
+    for (int j = 0; j < 2; ++j) {
 #pragma unroll
-            for (int y = 0; y < LG; ++y) {
-                if (y >= layers) break;
-                __nv_bfloat16* dst = p.out + (layer0 + y) * p.out_layer + (((long long)seq * p.cap + a) * p.H + head) * kDh + t4 * 2;
-#pragma unroll
-                for (int d = 0; d < 8; ++d) {
-                    const float x = acc[y][d][2 * h] * inv, z = acc[y][d][2 * h + 1] * inv;
-                    odd[h] |= x != x || z != z;
-                    *reinterpret_cast<uint32_t*>(dst + d * 8) = pack_bf16(x, z);
-                }
-            }
-        }
+        for (int o = 4; o < 32; o <<= 1) l[j] += __shfl_xor_sync(0xffffffffu, l[j], o);
     }
+    const float inv[2] = {l[0] == 0.f ? 0.f : 1.f / l[0], l[1] == 0.f ? 0.f : 1.f / l[1]};
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        unsigned again = __ballot_sync(0xffffffffu, odd[h]);
-        while (again) {
-            const int gg = (__ffs(again) - 1) >> 2;
-            again &= ~(0xfu << (gg * 4));
-            for (int y = 0; y < layers; ++y) window_row_again(p, seq, head, layer0 + y, qa0 + gg + h * 8, lane);
+    for (int y = 0; y < LG; ++y) {
+        if (y >= layers) break;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int r = 2 * t4 + j;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float x = acc[y][d][2 * e + j] * inv[j];
+                    odd[j] |= x != x;
+                    *reinterpret_cast<__nv_bfloat16*>(rows + r * 128 + (((2 * d + e) ^ r) << 4) + 2 * g) = __float2bfloat16_rn(x);
+                }
         }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int r = k * 4 + (lane >> 3), c = lane & 7, a = qa0 + r;
+            if (a < a1)
+                *reinterpret_cast<uint4*>(p.out + (layer0 + y) * p.out_layer + (((long long)seq * p.cap + a) * p.H + head) * kDh + c * 8) =
+                    *reinterpret_cast<const uint4*>(rows + r * 128 + ((c ^ r) << 4));
+        }
+        __syncwarp();
+    }
+    for (int r = 0; r < 8; ++r) {
+        const bool again = __any_sync(0xffffffffu, (2 * t4 == r && odd[0]) || (2 * t4 + 1 == r && odd[1]));
+        if (again && qa0 + r < a1)
+            for (int y = 0; y < layers; ++y) window_row_again(p, seq, head, layer0 + y, qa0 + r, lane);
     }
 }
 
