@@ -13,13 +13,16 @@
  *
  * General rules
  *  - Every function returns a status (SAN_OK = 0).  Nothing throws or traps, and no kernel
- *    waits on another kernel, CTA or rank.  The only device-side waits are a CTA's waits for
+ *    spins on another kernel, CTA or rank.  The only device-side waits are a CTA's waits for
  *    its OWN asynchronous copies or tensor-core operations (mbarrier waits in the kernels
- *    behind san_decode_step and san_full_block); each gives up after about a second, makes
+ *    behind san_decode_step, san_full_block, san_window_block and san_prefix_attn), the hardware
+ *    barrier of a thread-block cluster (san_beam_select) and the end of the kernel before on the
+ *    same stream; an mbarrier wait gives up after about a second and makes
  *    the kernel stop early.  san_decode_step reports it as SAN_ERR_TIMEOUT through
  *    san_device_status, which then also clears the context's split-row tickets so that later
- *    steps start clean; san_full_block has no status word, and a tile whose wait ran out
- *    leaves its output rows unwritten.
+ *    steps start clean; san_prefix_attn reports it in its status words (its rows' outputs are then
+ *    undefined); san_full_block and san_window_block have no status word, and a tile whose wait
+ *    ran out leaves its output rows unwritten.
  *  - All `d_` pointers are DEVICE pointers owned by the caller; all others are HOST
  *    pointers.  The library allocates no device memory: the cache arena and the
  *    workspace are caller buffers handed to san_create.
@@ -420,8 +423,8 @@ int32_t san_window_attn(const san_cached_rows* rows, int32_t window, int32_t n_s
                         size_t workspace_bytes, void* stream);
 
 /* One decode step of attention for rows behind shared prefixes: softmax and outputs as above over the
- * prefix's rows and all of the item's own ones together.  A prefix is read once for all of its items (up to
- * 16 query rows at a time from the cache hierarchy; more with tensor-core tiles).  A row that sees nothing
+ * prefix's rows and all of the item's own ones together.  A prefix is read from memory once for all of its
+ * items (eight query rows at a time, from L2 after the first; 256 with tensor-core tiles).  A row that sees nothing
  * (no prefix rows, len 0) gives zeros.  A prefix whose length, first item or number of items is out of range
  * leaves the outputs of its items as they were and is reported. */
 int32_t san_prefix_attn_bytes(const san_cached_rows* rows, const san_shared_prefix* prefix, size_t* workspace_bytes);

@@ -433,7 +433,7 @@ __device__ __forceinline__ void select_rows(const SelectParams& p) {
     }
 }
 
-constexpr int kMergeHeld = 8;                  // candidates per thread and round
+constexpr int kMergeHeld = 8;                  // candidates per thread and pass
 
 // One sentence by one CTA; ready() returns when the rows' partial results can be read.
 template <typename F>
@@ -523,8 +523,8 @@ __device__ __forceinline__ void select_merge(const SelectParams& p, const int se
         const double d = x == s_top[b] ? 0.0 : (double)x - (double)s_top[b];
         return (double)s_score[b] + (d - s_logsum[b]);
     };
-    int kept = 0;                                                     // candidates kept from the rounds before
-    for (int first = 0, round = 0; first < total; first += kSelThreads * kMergeHeld, round ^= 1) {
+    int kept = 0;                                                     // candidates kept from the passes before
+    for (int first = 0, turn = 0; first < total; first += kSelThreads * kMergeHeld, turn ^= 1) {
         if (first > 0) load(first);
         // ranks by a multiplication, within 2^-51 of the ones by the division: good enough for a bound
         unsigned long long key[kMergeHeld], top = 0;
@@ -549,11 +549,11 @@ __device__ __forceinline__ void select_merge(const SelectParams& p, const int se
             bound = join_bounds(s_least, beam);
 #pragma unroll
             for (int w = 1; w < kSelWarps; ++w) most = s_most[w] > most ? s_most[w] : most;
-            if (kept == beam && s_best[round][beam - 1].a > bound) bound = s_best[round][beam - 1].a - 16;     // an exact rank
+            if (kept == beam && s_best[turn][beam - 1].a > bound) bound = s_best[turn][beam - 1].a - 16;     // an exact rank
             if (bound == 0) bound = 1;
             // Candidates are not mixed over the threads as logits are (hypotheses differ in score, places in rank), so the
-            // bound may be low: halve the way to the largest until at most 128 reach it, never fewer than `beam` of this round
-            // unless the bound is that of the rounds before.
+            // bound may be low: halve the way to the largest until at most 128 reach it, never fewer than `beam` of this pass
+            // unless the bound is that of the passes before.
             for (int step = 0; step < 64; ++step) {
                 const unsigned long long mid = step == 0 ? bound : bound + (most - bound + 1) / 2;
                 int n = 0;
@@ -583,12 +583,12 @@ __device__ __forceinline__ void select_merge(const SelectParams& p, const int se
         __syncthreads();
         count = s_count;
         const bool long_list = count > 256;                           // counting would take longer than picking them out
-        if (!long_list && (int)threadIdx.x < kept) s_list[count + threadIdx.x] = s_best[round][threadIdx.x];
+        if (!long_list && (int)threadIdx.x < kept) s_list[count + threadIdx.x] = s_best[turn][threadIdx.x];
         __syncthreads();
         if (threadIdx.x == 0) s_count = 0;
         if (!long_list) {
             count += kept;
-            rank_list(s_list, count, beam, [&](int place, const Key128& k) { s_best[round ^ 1][place] = k; });
+            rank_list(s_list, count, beam, [&](int place, const Key128& k) { s_best[turn ^ 1][place] = k; });
             kept = min(count, beam);
         } else {
             Key128 last{~0ull, ~0ull};
@@ -596,18 +596,18 @@ __device__ __forceinline__ void select_merge(const SelectParams& p, const int se
                 Key128 mine{0, 0};
                 for (int i = threadIdx.x; i < count; i += kSelThreads)
                     if (last.over(s_list[i])) mine = larger(mine, s_list[i]);
-                if ((int)threadIdx.x < kept && last.over(s_best[round][threadIdx.x])) mine = larger(mine, s_best[round][threadIdx.x]);
+                if ((int)threadIdx.x < kept && last.over(s_best[turn][threadIdx.x])) mine = larger(mine, s_best[turn][threadIdx.x]);
                 last = block_largest(mine, s_slots);
-                if (threadIdx.x == 0) s_best[round ^ 1][k] = last;    // more than 256 candidates: there are `beam`
+                if (threadIdx.x == 0) s_best[turn ^ 1][k] = last;    // more than 256 candidates: there are `beam`
             }
             kept = beam;
         }
         __syncthreads();
         if ((int)threadIdx.x < kept) {
-            const unsigned long long id = ~s_best[round ^ 1][threadIdx.x].b;
+            const unsigned long long id = ~s_best[turn ^ 1][threadIdx.x].b;
             s_parent[threadIdx.x] = (int)(id >> 32);
             s_token[threadIdx.x] = (int)(unsigned)id;
-            s_rank[threadIdx.x] = s_best[round ^ 1][threadIdx.x].a;
+            s_rank[threadIdx.x] = s_best[turn ^ 1][threadIdx.x].a;
         }
     }
     __syncthreads();

@@ -259,6 +259,33 @@ def test_captured_twice_in_a_row_with_one_workspace():
         r.out = first
 
 
+def test_tensor_core_tiles_captured_and_replayed():
+    """Tiles, own rows beside them and the join, replayed back to back with new queries and lengths."""
+    n, P = 300, 4100
+    r = Rows("bf16", [3] * n, 2, 2, 1, 6, seed=21)
+    gen = torch.Generator().manual_seed(12)
+    pk, pv = randn(gen, 1, P, 2, DH, dtype=r.dt), randn(gen, 1, 1, P, 2, DH, dtype=r.dt)
+    dev = [x.to(DEV) for x in (pk, pv, torch.tensor([P], dtype=torch.int32), torch.tensor([0, n], dtype=torch.int32))]
+    a = r.args()
+    x = B.shared_prefix(d_k=dev[0], d_v=dev[1], v_stride=dev[1][0].numel(), n_prefix=1, cap_len=P, d_lens=dev[2], d_first=dev[3])
+    rc, nb = B.san_prefix_attn_bytes(a, x)
+    ws = torch.empty(nb, dtype=torch.uint8, device=DEV)
+    B.check(B.san_prefix_attn(a, x, ws, nb))
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        for _ in range(3):                                      # the same workspace, call after call
+            B.check(B.san_prefix_attn(a, x, ws, nb))
+    for seed, p in ((5, P), (6, 2049)):
+        r.q = randn(torch.Generator().manual_seed(seed), *r.q.shape, dtype=r.dt)
+        r.d[0].copy_(r.q)
+        dev[2].fill_(p)
+        r.out.fill_(-7)
+        g.replay()
+        torch.cuda.synchronize()
+        r.check(lambda i: range(3), lambda i, hk: (pk[0, :p, hk].double(), pv[:, 0, :p, hk].double()))
+
+
 def test_far_rows_of_a_large_plane():
     """Byte offsets beyond 32 bits inside one key plane: the rows that are read are the last ones."""
     H, cap, n = 2, 70000, 260                       # 260 * 2 * 70000 * 128 B = 4.66 GB a plane
