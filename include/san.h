@@ -15,9 +15,8 @@
  *  - Every function returns a status (SAN_OK = 0).  Nothing throws or traps, and no kernel
  *    spins on another kernel, CTA or rank.  The only device-side waits are a CTA's waits for
  *    its OWN asynchronous copies or tensor-core operations (mbarrier waits in the kernels
- *    behind san_decode_step, san_full_block, san_window_block and san_prefix_attn), the hardware
- *    barrier of a thread-block cluster (san_beam_select) and the end of the kernel before on the
- *    same stream; an mbarrier wait gives up after about a second and makes
+ *    behind san_decode_step, san_full_block, san_window_block and san_prefix_attn) and the end of
+ *    the kernel before on the same stream; an mbarrier wait gives up after about a second and makes
  *    the kernel stop early.  san_decode_step reports it as SAN_ERR_TIMEOUT through
  *    san_device_status, which then also clears the context's split-row tickets so that later
  *    steps start clean; san_prefix_attn reports it in its status words (its rows' outputs are then

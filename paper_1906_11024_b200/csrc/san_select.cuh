@@ -6,7 +6,7 @@
 // ranked by score / ((5 + length) / 6)^alpha, ties to the lowest (slot, token).
 //
 // The logits are read once and that is what bounds the call; everything else is a few KB:
-//   select_rows_kernel   CTA = (hypothesis, part of the vocabulary), in steps of 16 KB, the next step's logits on their way
+//   select_rows_kernel   CTA = (hypothesis, part of the vocabulary), in steps of 8 or 16 KB, the next step's logits on their way
 //     into registers while a step is worked on.  A thread keeps the maximum and the sum of 2^(x log2(e) - M) of
 //     its logits, three instructions a logit (float32, rescaled when the maximum moves; the threads' sums are joined
 //     in double).  The part's best `beam` logits come out without sorting it: the beam-th largest of the 256
@@ -17,9 +17,10 @@
 //     (double: scores of different hypotheses are compared with one another), ranks the beam x parts
 //     x beam candidates the same way, and carries scores, lengths and token histories over.  It is launched
 //     with programmatic stream serialisation: its CTAs are in place when the last logits arrive.
-//   select_cluster_kernel  both in one launch, the CTAs of a sentence as a cluster (see there).
-// Measured (device time of the whole call): 512 rows of 128000 bf16 logits 47.6 us, of which issue and exponentials fill
-// half; 740 rows of 50257 float32 ones off 16-byte boundaries 63.6; 4 rows of 32000 10.3, the chain of one sentence.  The first
+//     Both in one launch, a sentence's CTAs as a cluster whose first CTA went on behind the cluster's barrier, was slower
+//     (device time: 4 rows of 32000 float32 10.3 us against 8.8, 256 of bf16 16.0 against 14.9, 512 of 128000 47.6 against 42.4).
+// Measured (device time of the whole call): 512 rows of 128000 bf16 logits 42.4 us, of which issue and exponentials fill
+// half; 740 rows of 50257 float32 ones off 16-byte boundaries 59.3; 4 rows of 32000 8.8, the chain of one sentence.  The first
 // version, which sorted a key per thread and held 32 logits in float32, took 162, 133 and 12.3.  A ring of cp.async stages in
 // shared memory in place of the registers measured the same: loads are not what is waited for.
 // Where more candidates reach the bound than the list holds (rows that are alike nearly everywhere: a mask of
@@ -33,11 +34,15 @@ namespace san {
 
 constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
-constexpr int kSelWords = 16;                  // 32-bit words of logits per thread and step
+// 32-bit words of logits per thread and step, and CTAs of the rows' kernels that an SM holds (their registers are limited for
+// that).  Measured, 8 words and 5 CTAs against 16 and 4: 740 rows of 50257 float32 59.3 us against 64.0, 512 rows of 128000
+// bf16 71 against 47.6.
+template <typename T> struct SelectGeom;
+template <> struct SelectGeom<float> { static constexpr int kWords = 8, kCtas = 5; };
+template <> struct SelectGeom<__nv_bfloat16> { static constexpr int kWords = 16, kCtas = 4; };
 constexpr int kSelList = 1024;                 // keys that may reach the bound between two checks; more: one by one
 constexpr int kSelLong = 96;                   // list length at which the bound is raised
 constexpr int kSelTight = 64;                  // what the list is cut down to (equal logits aside)
-constexpr int kSelCluster = 16;                // CTAs of a cluster at most
 constexpr int TAG_SELECT = 8;
 
 struct SelectParams {
@@ -147,11 +152,11 @@ template <typename T> __device__ __forceinline__ float as_f32(T x);
 template <> __device__ __forceinline__ float as_f32<float>(float x) { return x; }
 template <> __device__ __forceinline__ float as_f32<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// The logits of a thread in one step: kSelWords registers, eight logits at a time.
+// The logits of a thread in one step: kWords registers, eight logits at a time.
 template <typename T> struct SelectHeld;
 template <> struct SelectHeld<float> {
-    static constexpr int N = kSelWords;
-    float x[kSelWords];
+    static constexpr int kWords = SelectGeom<float>::kWords, N = kWords;
+    float x[kWords];
     __device__ __forceinline__ void set(int i, float v) { x[i] = v; }
     __device__ __forceinline__ void set16(int j, const uint4& v) {
         x[4 * j] = __uint_as_float(v.x); x[4 * j + 1] = __uint_as_float(v.y);
@@ -160,7 +165,7 @@ template <> struct SelectHeld<float> {
     __device__ __forceinline__ float get(int i) const { return x[i]; }
     __device__ __forceinline__ void mask_nan() {
 #pragma unroll
-        for (int i = 0; i < kSelWords; ++i) x[i] = fmaxf(x[i], -INFINITY);
+        for (int i = 0; i < kWords; ++i) x[i] = fmaxf(x[i], -INFINITY);
     }
     // The largest of logits 8 g .. 8 g + 7, NaN if one of them is.
     __device__ __forceinline__ float top8(int g) const {
@@ -171,8 +176,8 @@ template <> struct SelectHeld<float> {
     }
 };
 template <> struct SelectHeld<__nv_bfloat16> {
-    static constexpr int N = 2 * kSelWords;
-    uint32_t x[kSelWords];                                            // logit 2 i low, 2 i + 1 high
+    static constexpr int kWords = SelectGeom<__nv_bfloat16>::kWords, N = 2 * kWords;
+    uint32_t x[kWords];                                            // logit 2 i low, 2 i + 1 high
     __device__ __forceinline__ void set(int i, float v) {
         const uint32_t b = __float_as_uint(v) >> 16;                  // v is a bf16 number
         x[i >> 1] = i & 1 ? (x[i >> 1] & 0xffffu) | b << 16 : b;
@@ -182,7 +187,7 @@ template <> struct SelectHeld<__nv_bfloat16> {
     __device__ __forceinline__ static __nv_bfloat162 two(uint32_t w) { return *reinterpret_cast<__nv_bfloat162*>(&w); }
     __device__ __forceinline__ void mask_nan() {
 #pragma unroll
-        for (int i = 0; i < kSelWords; ++i) {
+        for (int i = 0; i < kWords; ++i) {
             const __nv_bfloat162 v = __hmax2(two(x[i]), two(0xff80ff80u));
             x[i] = *reinterpret_cast<const uint32_t*>(&v);
         }
@@ -247,11 +252,12 @@ __device__ __forceinline__ uint32_t tighten(Key64* list, int count, int n, uint3
     return lo;
 }
 
-// CTA blockIdx.x of rows * chunks.  VECTOR: every row starts on a 16-byte boundary and a thread holds runs of 16 bytes, else
+// grid = rows * chunks, then select_merge_kernel.  VECTOR: every row starts on a 16-byte boundary and a thread holds runs of 16 bytes, else
 // single logits 256 apart (one mapping for all rows of a call, so that equal rows get equal sums whatever
 // their addresses).
 template <typename T, bool VECTOR>
-__device__ __forceinline__ void select_rows(const SelectParams& p) {
+__global__ void __launch_bounds__(kSelThreads, SelectGeom<T>::kCtas) select_rows_kernel(const SelectParams p) {
+    asm volatile("griddepcontrol.launch_dependents;");
     using Held = SelectHeld<T>;
     constexpr int N = Held::N, VEC = VECTOR ? 16 / (int)sizeof(T) : 1, STEP = N * kSelThreads;
     __shared__ Key64 s_list[kSelList];
@@ -435,9 +441,8 @@ __device__ __forceinline__ void select_rows(const SelectParams& p) {
 
 constexpr int kMergeHeld = 8;                  // candidates per thread and pass
 
-// One sentence by one CTA; ready() returns when the rows' partial results can be read.
-template <typename F>
-__device__ __forceinline__ void select_merge(const SelectParams& p, const int sent, F ready) {
+// grid = sentences.
+static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const SelectParams p) {
     __shared__ Key128 s_list[kSelThreads * kMergeHeld];      // 32 KB; the histories' columns after the ranking
     __shared__ Key128 s_best[2][SAN_MAX_BEAM];
     __shared__ unsigned long long s_least[kSelWarps], s_most[kSelWarps], s_rank[SAN_MAX_BEAM];
@@ -448,7 +453,7 @@ __device__ __forceinline__ void select_merge(const SelectParams& p, const int se
     __shared__ int s_len[SAN_MAX_BEAM], s_done[SAN_MAX_BEAM], s_parent[SAN_MAX_BEAM], s_token[SAN_MAX_BEAM];
     __shared__ int s_count, s_bad, s_longest;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int beam = p.beam;
+    const int sent = blockIdx.x, beam = p.beam;
     if (threadIdx.x == 0) { s_count = 0; s_bad = 0; s_longest = 0; }
     __syncthreads();
     if (threadIdx.x < beam) {
@@ -475,7 +480,7 @@ __device__ __forceinline__ void select_merge(const SelectParams& p, const int se
 #pragma unroll
     for (int b = 0; b < kEarly; ++b)
         early[b] = beam <= kEarly && b < beam && (int)threadIdx.x < longest && !s_bad ? p.tokens[((long long)sent * beam + b) * p.ld_tokens + threadIdx.x] : 0;
-    ready();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (s_bad) return;                                                // the sentence keeps its old state
     const size_t part_bytes = select_part_bytes(beam);
     const char* parts = p.ws + (size_t)sent * beam * p.chunks * part_bytes;
@@ -645,29 +650,6 @@ __device__ __forceinline__ void select_merge(const SelectParams& p, const int se
             else if (pos == len && token >= 0) p.tokens_out[first + s * p.ld_tokens] = token;
         }
     }
-}
-
-// grid = rows * chunks, then select_merge_kernel.
-template <typename T, bool VECTOR>
-__global__ void __launch_bounds__(kSelThreads, 4) select_rows_kernel(const SelectParams p) {
-    asm volatile("griddepcontrol.launch_dependents;");
-    select_rows<T, VECTOR>(p);
-}
-// grid = sentences.
-static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const SelectParams p) {
-    select_merge(p, blockIdx.x, [] { asm volatile("griddepcontrol.wait;" ::: "memory"); });
-}
-// Both in one launch, where a sentence's rows and parts are at most kSelCluster CTAs: they form a cluster, and its first
-// CTA goes on with the sentence when all have arrived at the cluster's barrier.  grid = rows * chunks.
-template <typename T, bool VECTOR>
-__global__ void __launch_bounds__(kSelThreads, 4) select_cluster_kernel(const SelectParams p) {
-    select_rows<T, VECTOR>(p);
-    __syncthreads();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    const unsigned per_sentence = (unsigned)(p.beam * p.chunks);
-    auto ready = [] { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); };
-    if (blockIdx.x % per_sentence == 0) select_merge(p, (int)(blockIdx.x / per_sentence), ready);
-    else ready();
 }
 
 }  // namespace san

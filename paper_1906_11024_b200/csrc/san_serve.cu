@@ -46,18 +46,19 @@ int32_t launch_after(void (*fn)(P), dim3 grid, unsigned block, cudaStream_t st, 
 }
 
 // ------------------------------------------------------------------------------- beam selection
-// Parts of a row, each of whole steps: the cut with the shortest estimate of (waves of CTAs, four per SM) x (steps of a part
-// + the 2.5 steps that the bound, the list and the hand-over of a part take), where a second launch counts as two
-// more steps (a sentence of at most kSelCluster CTAs needs none).
+// Parts of a row, each of whole steps: the cut with the shortest estimate of (waves of CTAs, four or five per SM) x (steps of a part
+// + the 2.5 steps that the bound, the list and the hand-over of a part take).
 struct SelectCut { int chunks, steps; };
-SelectCut select_cut(int32_t dtype, long long rows, int beam, int vocab) {
-    const int step = kSelWords * (dtype == SAN_BF16 ? 2 : 1) * kSelThreads;
+SelectCut select_cut(int32_t dtype, long long rows, int vocab) {
+    const bool bf16 = dtype == SAN_BF16;
+    const int step = (bf16 ? 2 * SelectGeom<__nv_bfloat16>::kWords : SelectGeom<float>::kWords) * kSelThreads;
+    const int ctas = kSms * (bf16 ? SelectGeom<__nv_bfloat16>::kCtas : SelectGeom<float>::kCtas);
     const long long all = div_up(vocab, step);
     SelectCut best{1, (int)all};
     double least = 1e30;
     for (long long parts = 1; parts <= std::min<long long>(all, 64); ++parts) {
         const long long steps = div_up(all, parts), chunks = div_up(all, steps);
-        const double cost = (double)std::max<long long>(1, div_up(rows * chunks, 4 * kSms)) * ((double)steps + 2.5) + (beam * chunks > kSelCluster ? 2.0 : 0.0);
+        const double cost = (double)std::max<long long>(1, div_up(rows * chunks, ctas)) * ((double)steps + 2.5);
         if (cost < least) { least = cost; best = {(int)chunks, (int)steps}; }
     }
     return best;
@@ -66,33 +67,16 @@ SelectCut select_cut(int32_t dtype, long long rows, int beam, int vocab) {
 int32_t select_shape(int32_t n_sent, int32_t beam, int32_t vocab) {
     if (n_sent < 0 || beam < 1 || beam > SAN_MAX_BEAM || vocab < 1 || vocab > (1 << 28)) return SAN_ERR_SHAPE;
     if ((long long)n_sent * beam > (1 << 24)) return SAN_ERR_SHAPE;
-    if ((long long)n_sent * beam * div_up(vocab, kSelWords * kSelThreads) > 0x7fffffffLL) return SAN_ERR_SHAPE;
+    if ((long long)n_sent * beam * std::min<long long>(64, div_up(vocab, SelectGeom<float>::kWords * kSelThreads)) > 0x7fffffffLL) return SAN_ERR_SHAPE;
     return SAN_OK;
 }
 
 template <typename T, bool VECTOR>
 int32_t launch_select_as(const SelectParams& p, cudaStream_t st) {
     const unsigned grid = (unsigned)((long long)p.n_sent * p.beam * p.chunks);
-    const int cluster = p.beam * p.chunks;
-    if (cluster > kSelCluster) {
-        select_rows_kernel<T, VECTOR><<<grid, kSelThreads, 0, st>>>(p);
-        if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
-        return launch_after(&select_merge_kernel, dim3((unsigned)p.n_sent), kSelThreads, st, p);
-    }
-    static bool set[64] = {};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return SAN_ERR_CUDA;
-    if (dev < 0 || dev >= 64 || !set[dev]) {       // clusters of more than eight CTAs have to be asked for
-        if (cudaFuncSetAttribute(select_cluster_kernel<T, VECTOR>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return SAN_ERR_CUDA;
-        if (dev >= 0 && dev < 64) set[dev] = true;
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(kSelThreads); cfg.stream = st;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)cluster; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr; cfg.numAttrs = 1;
-    return cuda_status(cudaLaunchKernelEx(&cfg, select_cluster_kernel<T, VECTOR>, p));
+    select_rows_kernel<T, VECTOR><<<grid, kSelThreads, 0, st>>>(p);
+    if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
+    return launch_after(&select_merge_kernel, dim3((unsigned)p.n_sent), kSelThreads, st, p);
 }
 template <typename T>
 int32_t launch_select(const SelectParams& p, bool vector, cudaStream_t st) {
@@ -296,7 +280,7 @@ int32_t san_beam_select_bytes(int32_t n_sent, int32_t beam, int32_t vocab, size_
     const int32_t rc = select_shape(n_sent, beam, vocab);
     if (rc != SAN_OK) return rc;
     const long long rows = (long long)n_sent * beam;
-    const int chunks = std::max(select_cut(SAN_F32, rows, beam, vocab).chunks, select_cut(SAN_BF16, rows, beam, vocab).chunks);
+    const int chunks = std::max(select_cut(SAN_F32, rows, vocab).chunks, select_cut(SAN_BF16, rows, vocab).chunks);
     *workspace_bytes = (size_t)rows * chunks * select_part_bytes(beam);
     return SAN_OK;
 }
@@ -320,7 +304,7 @@ int32_t san_beam_select(const san_select_args* a, void* stream) {
     std::memset(&p, 0, sizeof(p));
     const long long rows = (long long)a->n_sent * a->beam;
     p.logits = a->d_logits; p.ld = a->ld_logits; p.vocab = a->vocab; p.n_sent = a->n_sent; p.beam = a->beam;
-    const SelectCut cut = select_cut(a->dtype, rows, a->beam, a->vocab);
+    const SelectCut cut = select_cut(a->dtype, rows, a->vocab);
     p.chunks = cut.chunks; p.steps = cut.steps;
     p.eos = a->eos; p.alpha = (double)a->alpha;
     p.score = a->d_score; p.len = a->d_len; p.done = a->d_done; p.tokens = a->d_tokens; p.ld_tokens = a->ld_tokens;
