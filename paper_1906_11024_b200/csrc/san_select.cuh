@@ -15,12 +15,14 @@
 //     at the end each key finds its own place by counting the ones above it.
 //   select_merge_kernel  CTA = sentence.  Joins the parts' maxima and sums to the log-sum-exp of each row
 //     (double: scores of different hypotheses are compared with one another), ranks the beam x parts
-//     x beam candidates the same way, and carries scores, lengths and token histories over.  It is launched
-//     with programmatic stream serialisation: its CTAs are in place when the last logits arrive.
+//     x beam candidates, 1024 at a time, the best of every part first, until the parts' next ones cannot matter, and carries
+//     scores, lengths and token histories over.  It is launched with programmatic stream serialisation: its
+//     CTAs are in place, and the histories in shared memory, when the last logits arrive.
+//     Part after part in place of the best first took every pass: one sentence of 32 rows of 128000 float32 86 us, now 29.
 //     Both in one launch, a sentence's CTAs as a cluster whose first CTA went on behind the cluster's barrier, was slower
 //     (device time: 4 rows of 32000 float32 10.3 us against 8.8, 256 of bf16 16.0 against 14.9, 512 of 128000 47.6 against 42.4).
-// Measured (device time of the whole call): 512 rows of 128000 bf16 logits 42.4 us, of which issue and exponentials fill
-// half; 740 rows of 50257 float32 ones off 16-byte boundaries 59.3; 4 rows of 32000 8.8, the chain of one sentence.  The first
+// Measured (device time of the whole call): 512 rows of 128000 bf16 logits 41.0 us, of which issue and exponentials fill
+// half; 740 rows of 50257 float32 ones off 16-byte boundaries 51.3; 4 rows of 32000 8.0, the chain of one sentence.  The first
 // version, which sorted a key per thread and held 32 logits in float32, took 162, 133 and 12.3.  A ring of cp.async stages in
 // shared memory in place of the registers measured the same: loads are not what is waited for.
 // Where more candidates reach the bound than the list holds (rows that are alike nearly everywhere: a mask of
@@ -36,7 +38,7 @@ constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
 // 32-bit words of logits per thread and step, and CTAs of the rows' kernels that an SM holds (their registers are limited for
 // that).  Measured, 8 words and 5 CTAs against 16 and 4: 740 rows of 50257 float32 59.3 us against 64.0, 512 rows of 128000
-// bf16 71 against 47.6.
+// bf16 48.5 against 42.4 (before the merge took what it takes now).
 template <typename T> struct SelectGeom;
 template <> struct SelectGeom<float> { static constexpr int kWords = 8, kCtas = 5; };
 template <> struct SelectGeom<__nv_bfloat16> { static constexpr int kWords = 16, kCtas = 4; };
@@ -252,9 +254,9 @@ __device__ __forceinline__ uint32_t tighten(Key64* list, int count, int n, uint3
     return lo;
 }
 
-// grid = rows * chunks, then select_merge_kernel.  VECTOR: every row starts on a 16-byte boundary and a thread holds runs of 16 bytes, else
-// single logits 256 apart (one mapping for all rows of a call, so that equal rows get equal sums whatever
-// their addresses).
+// grid = rows * chunks, then select_merge_kernel.  VECTOR: every row starts on a 16-byte boundary and a thread holds runs
+// of 16 bytes, else single logits 256 apart (one mapping for all rows of a call, so that equal rows get equal sums
+// whatever their addresses).
 template <typename T, bool VECTOR>
 __global__ void __launch_bounds__(kSelThreads, SelectGeom<T>::kCtas) select_rows_kernel(const SelectParams p) {
     asm volatile("griddepcontrol.launch_dependents;");
@@ -439,11 +441,17 @@ __global__ void __launch_bounds__(kSelThreads, SelectGeom<T>::kCtas) select_rows
     }
 }
 
-constexpr int kMergeHeld = 8;                  // candidates per thread and pass
+constexpr int kMergeHeld = 4;                  // candidates per thread and pass
+constexpr int kMergeHistory = 4096;            // tokens of the histories in shared memory at once
+
+__device__ __forceinline__ void copy4_async(int* dst, const int* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((unsigned)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
 
 // grid = sentences.
 static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const SelectParams p) {
-    __shared__ Key128 s_list[kSelThreads * kMergeHeld];      // 32 KB; the histories' columns after the ranking
+    __shared__ Key128 s_list[kSelThreads * kMergeHeld];
+    __shared__ int s_history[kMergeHistory];
     __shared__ Key128 s_best[2][SAN_MAX_BEAM];
     __shared__ unsigned long long s_least[kSelWarps], s_most[kSelWarps], s_rank[SAN_MAX_BEAM];
     __shared__ int s_counts[2][kSelWarps];
@@ -473,19 +481,23 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
         atomicMax(&s_longest, len);
     }
     __syncthreads();
-    // histories, first positions: on their way while the rows are worked on
-    constexpr int kEarly = 8;
-    const int longest = p.tokens ? (int)min((long long)s_longest + 1, p.ld_tokens) : 0;
-    int early[kEarly];
-#pragma unroll
-    for (int b = 0; b < kEarly; ++b)
-        early[b] = beam <= kEarly && b < beam && (int)threadIdx.x < longest && !s_bad ? p.tokens[((long long)sent * beam + b) * p.ld_tokens + threadIdx.x] : 0;
+    // Histories, `span` positions at a time; the first ones are on their way while the rows are worked on.
+    const int span = kMergeHistory / beam & ~31, longest = p.tokens ? (int)min((long long)s_longest + 1, p.ld_tokens) : 0;
+    auto fetch = [&](int first) {
+        for (int b = warp; b < beam; b += kSelWarps) {
+            const int* from = p.tokens + ((long long)sent * beam + b) * p.ld_tokens;
+            for (int pos = first + lane; pos < min(first + span, s_len[b]); pos += 32) copy4_async(s_history + b * span + pos - first, from + pos);
+        }
+    };
+    if (longest > 0 && !s_bad) fetch(0);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (s_bad) return;                                                // the sentence keeps its old state
     const size_t part_bytes = select_part_bytes(beam);
     const char* parts = p.ws + (size_t)sent * beam * p.chunks * part_bytes;
-    // candidate i of the sentence: (slot, chunk, place); a finished hypothesis stands at its first one
-    const int per_row = p.chunks * beam, total = beam * per_row;
+    // candidate i of the sentence: (place, slot, chunk), so that the best ones of every part come first; a finished
+    // hypothesis stands at its first one
+    const int n_parts = p.chunks * beam, total = beam * n_parts;
+    auto slot_of = [&](int i) { return (int)((unsigned)i % (unsigned)n_parts / (unsigned)p.chunks); };
     unsigned long long held[kMergeHeld];
     auto load = [&](int first) {
 #pragma unroll
@@ -493,10 +505,10 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
             const int i = first + j * kSelThreads + (int)threadIdx.x;
             held[j] = 0;
             if (i >= total) continue;
-            const int part = i / beam, b = part / p.chunks;           // part: (slot, chunk)
+            const int place = (unsigned)i / (unsigned)n_parts, part = i - place * n_parts, b = (unsigned)part / (unsigned)p.chunks;
             if (s_score[b] == -INFINITY) continue;
-            if (s_done[b]) held[j] = i == b * per_row ? 1 : 0;        // itself
-            else held[j] = *reinterpret_cast<const unsigned long long*>(parts + (size_t)part * part_bytes + 16 + 8 * (size_t)(i - part * beam));
+            if (s_done[b]) held[j] = i == b * p.chunks ? 1 : 0;       // itself
+            else held[j] = *reinterpret_cast<const unsigned long long*>(parts + (size_t)part * part_bytes + 16 + 8 * (size_t)place);
         }
     };
     load(0);
@@ -529,29 +541,44 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
         return (double)s_score[b] + (d - s_logsum[b]);
     };
     int kept = 0;                                                     // candidates kept from the passes before
+    int idle = 0;                                                     // candidates in a row, the last ones, that are below the ones kept
     for (int first = 0, turn = 0; first < total; first += kSelThreads * kMergeHeld, turn ^= 1) {
         if (first > 0) load(first);
-        // ranks by a multiplication, within 2^-51 of the ones by the division: good enough for a bound
-        unsigned long long key[kMergeHeld], top = 0;
         auto score_at = [&](int b, unsigned long long h) { return s_done[b] ? (double)s_score[b] : score_of(b, unorder_f32((unsigned)(h >> 32))); };
+        auto exact = [&](int b, unsigned long long h) {                   // the key that orders the sentence's candidates
+            const double rank = score_at(b, h) / s_norm[b];
+            const int token = s_done[b] ? max(p.eos, 0) : (int)~(unsigned)h;
+            return Key128{rank > -INFINITY ? order_f64(rank) : 0, ~(((unsigned long long)(unsigned)b << 32) | (unsigned)token)};
+        };
+        auto list = [&](bool in, const Key128& k) {
+            const unsigned all = __ballot_sync(0xffffffffu, in);
+            int at = 0;
+            if (lane == 0 && all) at = atomicAdd(&s_count, __popc(all));
+            at = __shfl_sync(0xffffffffu, at, 0) + __popc(all & ((1u << lane) - 1));
+            if (in) s_list[at] = k;
+        };
+        unsigned long long key[kMergeHeld];
+        if (total <= kSelThreads) {                                   // few enough to look at them all
+            Key128 k{0, 0};
+            if (held[0] != 0) k = exact(slot_of((int)threadIdx.x), held[0]);
+            list(k.a != 0, k);
+        } else {
+            // ranks by a multiplication, within 2^-51 of the ones by the division: good enough for a bound
+            unsigned long long top = 0;
 #pragma unroll
-        for (int j = 0; j < kMergeHeld; ++j) {
-            key[j] = 0;
-            if (first + j * kSelThreads >= total || held[j] == 0) continue;
-            const int b = (first + j * kSelThreads + (int)threadIdx.x) / per_row;
-            const double rank = score_at(b, held[j]) * s_inverse[b];
-            if (rank > -INFINITY) key[j] = order_f64(rank);
-            top = key[j] > top ? key[j] : top;
-        }
-        int count = 0;
-        unsigned long long bound = 1;
-        if (total > kSelThreads) {
+            for (int j = 0; j < kMergeHeld; ++j) {
+                key[j] = 0;
+                if (first + j * kSelThreads >= total || held[j] == 0) continue;
+                const int b = slot_of(first + j * kSelThreads + (int)threadIdx.x);
+                const double rank = score_at(b, held[j]) * s_inverse[b];
+                if (rank > -INFINITY) key[j] = order_f64(rank);
+                top = key[j] > top ? key[j] : top;
+            }
             unsigned long long warp_top, least;
             group_bounds(top, beam, &warp_top, &least);
             if (lane == 0) { s_least[warp] = least; s_most[warp] = warp_top; }
             __syncthreads();
-            unsigned long long most = s_most[0];
-            bound = join_bounds(s_least, beam);
+            unsigned long long most = s_most[0], bound = join_bounds(s_least, beam);
 #pragma unroll
             for (int w = 1; w < kSelWarps; ++w) most = s_most[w] > most ? s_most[w] : most;
             if (kept == beam && s_best[turn][beam - 1].a > bound) bound = s_best[turn][beam - 1].a - 16;     // an exact rank
@@ -559,7 +586,7 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
             // Candidates are not mixed over the threads as logits are (hypotheses differ in score, places in rank), so the
             // bound may be low: halve the way to the largest until at most 128 reach it, never fewer than `beam` of this pass
             // unless the bound is that of the passes before.
-            for (int step = 0; step < 64; ++step) {
+            for (int step = 0, count = 0; step < 64; ++step) {
                 const unsigned long long mid = step == 0 ? bound : bound + (most - bound + 1) / 2;
                 int n = 0;
 #pragma unroll
@@ -571,22 +598,18 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
 #pragma unroll
                 for (int w = 0; w < kSelWarps; ++w) n += s_counts[step & 1][w];
                 if (step == 0 || n >= beam) { bound = mid; count = n; }
-                else most = mid - 1;                                      // fewer than `beam` reach mid
+                else most = mid - 1;                                  // fewer than `beam` reach mid
                 if (count <= 128 || most <= bound) break;
             }
-            bound = bound > 16 ? bound - 16 : 1;                          // further down than the two ranks can differ
-        }
+            bound = bound > 16 ? bound - 16 : 1;                      // further down than the two ranks can differ
 #pragma unroll
-        for (int j = 0; j < kMergeHeld; ++j)
-            if (key[j] >= bound) s_list[atomicAdd(&s_count, 1)] = Key128{held[j], (unsigned long long)(first + j * kSelThreads + (int)threadIdx.x)};
-        __syncthreads();
-        for (int i = threadIdx.x; i < s_count; i += kSelThreads) {    // their exact ranks
-            const unsigned long long h = s_list[i].a;
-            const int b = (int)s_list[i].b / per_row, token = s_done[b] ? max(p.eos, 0) : (int)~(unsigned)h;
-            s_list[i] = Key128{order_f64(score_at(b, h) / s_norm[b]), ~(((unsigned long long)(unsigned)b << 32) | (unsigned)token)};
+            for (int j = 0; j < kMergeHeld; ++j)
+                list(key[j] >= bound, Key128{held[j], (unsigned long long)slot_of(first + j * kSelThreads + (int)threadIdx.x)});
+            __syncthreads();
+            for (int i = threadIdx.x; i < s_count; i += kSelThreads) s_list[i] = exact((int)s_list[i].b, s_list[i].a);
         }
         __syncthreads();
-        count = s_count;
+        int count = s_count;
         const bool long_list = count > 256;                           // counting would take longer than picking them out
         if (!long_list && (int)threadIdx.x < kept) s_list[count + threadIdx.x] = s_best[turn][threadIdx.x];
         __syncthreads();
@@ -608,12 +631,22 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
             kept = beam;
         }
         __syncthreads();
-        if ((int)threadIdx.x < kept) {
+        if ((int)threadIdx.x < kept && s_best[turn ^ 1][threadIdx.x].a != 0) {
             const unsigned long long id = ~s_best[turn ^ 1][threadIdx.x].b;
             s_parent[threadIdx.x] = (int)(id >> 32);
             s_token[threadIdx.x] = (int)(unsigned)id;
             s_rank[threadIdx.x] = s_best[turn ^ 1][threadIdx.x].a;
         }
+        // A part's candidates are in order, and so are their ranks: once as many candidates in a row as there are parts are
+        // below the ones kept, all that come after are.
+        const int end = first + kSelThreads * kMergeHeld, from = max(first, end - n_parts);
+        if (end >= total) break;
+        const unsigned long long least = s_best[turn ^ 1][beam - 1].a;
+        bool over = kept < beam || least <= 16;
+#pragma unroll
+        for (int j = 0; j < kMergeHeld; ++j) over |= first + j * kSelThreads + (int)threadIdx.x >= from && key[j] >= least - 16;
+        idle = __syncthreads_or(over) ? 0 : idle + (end - from);
+        if (idle >= n_parts) break;
     }
     __syncthreads();
     if (threadIdx.x < beam) {
@@ -629,25 +662,19 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
         p.next[row] = token;
         s_token[s] = keeps ? -1 : token;                              // the token that joins the history
     }
-    if (!p.tokens) return;
-    __syncthreads();
-    // Histories: a thread owns positions, reads each of them in every hypothesis and then writes it, so
-    // that the new histories may take the old ones' place.
-    int* column = reinterpret_cast<int*>(s_list) + threadIdx.x;       // kSelThreads ints per hypothesis
-    for (int pos = threadIdx.x; pos < longest; pos += kSelThreads) {
-        const long long first = (long long)sent * beam * p.ld_tokens + pos;
-        if (beam <= kEarly && pos < kSelThreads) {
-#pragma unroll
-            for (int b = 0; b < kEarly; ++b)
-                if (b < beam) column[b * kSelThreads] = early[b];
-        } else {
-#pragma unroll 8
-            for (int b = 0; b < beam; ++b) column[b * kSelThreads] = p.tokens[first + b * p.ld_tokens];
+    // Histories: each position is read in every hypothesis before it is written, so that the new histories may take
+    // the old ones' place.
+    for (int first = 0; first < longest; first += span) {
+        if (first > 0) {
+            __syncthreads();                                          // the positions before have been written
+            fetch(first);
         }
-        for (int s = 0; s < beam; ++s) {
-            const int b = s_parent[s], len = s_len[b], token = s_token[s];
-            if (pos < len) p.tokens_out[first + s * p.ld_tokens] = column[b * kSelThreads];
-            else if (pos == len && token >= 0) p.tokens_out[first + s * p.ld_tokens] = token;
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+        for (int s = warp; s < beam; s += kSelWarps) {
+            const int b = s_parent[s], len = s_len[b], token = s_token[s], end = min(first + span, token < 0 ? len : len + 1);
+            int* to = p.tokens_out + ((long long)sent * beam + s) * p.ld_tokens;
+            for (int pos = first + lane; pos < end; pos += 32) to[pos] = pos < len ? s_history[b * span + pos - first] : token;
         }
     }
 }

@@ -128,6 +128,35 @@ def test_many_candidates_above_the_bound():
     _compare(_call(x, V, V, st, S, beam, 2, 0.0), want, st)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ties", [False, True])
+def test_all_winners_in_one_part(dtype, ties):
+    """Every winner of the first sentence is the best, second best, ... of the same part of one row, down to its last
+    place; the merge, which takes the parts' best ones first, must not stop before."""
+    S, beam, V = 2, 32, 50257
+    rng = np.random.default_rng(6)
+    x = torch.from_numpy(rng.standard_normal((S * beam, V), dtype=np.float32))
+    x[7, 30001:30041] = 20.0 if ties else torch.arange(40, dtype=torch.float32) / 4 + 20.0
+    x = x.to(dtype_of(dtype)[0])
+    st = _state(rng, S, beam, V, 4, 6, done_share=0.0)
+    st["score"][:beam] -= 40.0
+    st["score"][7] = -1.0
+    for ld in (V, V + 7):
+        want = select(x, st["score"], st["len"], st["done"], st["tokens"], 2, 0.0, beam)
+        assert (want["parent"][:beam] == 7).all()
+        _compare(_call(x, ld, V, st, S, beam, 2, 0.0), want, st)
+
+
+def test_long_histories_in_place():
+    """Histories of several windows of the merge's shared memory, taking the old ones' place."""
+    S, beam, V, cap = 2, 32, 70, 420
+    rng = np.random.default_rng(13)
+    st = _state(rng, S, beam, V, 400, cap, done_share=0.3)
+    x = torch.from_numpy(rng.standard_normal((S * beam, V), dtype=np.float32) * 3)
+    want = select(x, st["score"], st["len"], st["done"], st["tokens"], 2, 0.6, beam)
+    _compare(_call(x, V, V, st, S, beam, 2, 0.6, in_place=True), want, st, in_place=True)
+
+
 def test_first_step_masks_and_too_few_candidates():
     """One live slot; masked tokens of every kind; rows with fewer candidates than slots, or none."""
     beam, V, S = 4, 300, 5
