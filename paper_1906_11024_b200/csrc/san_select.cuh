@@ -21,14 +21,16 @@
 //     Part after part in place of the best first took every pass: one sentence of 32 rows of 128000 float32 86 us, now 29.
 //     Both in one launch, a sentence's CTAs as a cluster whose first CTA went on behind the cluster's barrier, was slower
 //     (device time: 4 rows of 32000 float32 10.3 us against 8.8, 256 of bf16 16.0 against 14.9, 512 of 128000 47.6 against 42.4).
-// Measured (device time of the whole call): 512 rows of 128000 bf16 logits 41.0 us, of which issue and exponentials fill
-// half; 740 rows of 50257 float32 ones off 16-byte boundaries 51.3; 4 rows of 32000 8.0, the chain of one sentence.  The first
+// Measured (device time of the whole call): 512 rows of 128000 bf16 logits 40.0 us, of which issue and exponentials fill
+// half; 740 rows of 50257 float32 ones off 16-byte boundaries 49.2; 4 rows of 32000 7.8, the chain of one sentence.  The first
 // version, which sorted a key per thread and held 32 logits in float32, took 162, 133 and 12.3.  A ring of cp.async stages in
 // shared memory in place of the registers measured the same: loads are not what is waited for.
 // Where more candidates reach the bound than the list holds (rows that are alike nearly everywhere: a mask of
 // the type's lowest value) the best ones are taken one by one, each the largest below the one before.
 // A finished hypothesis, or one without a score, has its logits skipped.
 #pragma once
+
+#include <cfloat>
 
 #include "san_kernels.cuh"
 
@@ -169,6 +171,11 @@ template <> struct SelectHeld<float> {
 #pragma unroll
         for (int i = 0; i < kWords; ++i) x[i] = fmaxf(x[i], -INFINITY);
     }
+    __device__ __forceinline__ float pick8(int g, int e) const {      // logit 8 g + e
+        const float a = e & 1 ? x[8 * g + 1] : x[8 * g], b = e & 1 ? x[8 * g + 3] : x[8 * g + 2];
+        const float c = e & 1 ? x[8 * g + 5] : x[8 * g + 4], d = e & 1 ? x[8 * g + 7] : x[8 * g + 6];
+        return e & 4 ? (e & 2 ? d : c) : (e & 2 ? b : a);
+    }
     // The largest of logits 8 g .. 8 g + 7, NaN if one of them is.
     __device__ __forceinline__ float top8(int g) const {
         float t = x[8 * g];
@@ -193,6 +200,10 @@ template <> struct SelectHeld<__nv_bfloat16> {
             const __nv_bfloat162 v = __hmax2(two(x[i]), two(0xff80ff80u));
             x[i] = *reinterpret_cast<const uint32_t*>(&v);
         }
+    }
+    __device__ __forceinline__ float pick8(int g, int e) const {
+        const uint32_t a = e & 2 ? x[4 * g + 1] : x[4 * g], b = e & 2 ? x[4 * g + 3] : x[4 * g + 2], w = e & 4 ? b : a;
+        return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
     }
     __device__ __forceinline__ float top8(int g) const {
         const __nv_bfloat162 t = __hmax2_nan(__hmax2_nan(two(x[4 * g]), two(x[4 * g + 1])), __hmax2_nan(two(x[4 * g + 2]), two(x[4 * g + 3])));
@@ -363,16 +374,20 @@ __global__ void __launch_bounds__(kSelThreads, SelectGeom<T>::kCtas) select_rows
             }
             bound = unorder_f32(lo);
         }
-        if (t >= bound && t > -INFINITY) {
+        const float least = fmaxf(bound, -FLT_MAX);                   // -inf offers nothing
+        if (t >= least) {
 #pragma unroll
             for (int g = 0; g < N / 8; ++g) {
-                if (!(t8[g] >= bound)) continue;
+                if (!(t8[g] >= least)) continue;
+                // A warp's lanes list their hits together, one each in turn: a branch per logit would take the hits of
+                // different places one after another.
+                unsigned hits = 0;
 #pragma unroll
-                for (int i = 8 * g; i < 8 * g + 8; ++i)
-                    if (v.get(i) >= bound && v.get(i) > -INFINITY) {
-                        const int at = atomicAdd(&s_count, 1);
-                        if (at < kSelList) s_list[at].a = select_key(v.get(i), base + ((i / VEC) * kSelThreads + (int)threadIdx.x) * VEC + i % VEC);
-                    }
+                for (int i = 0; i < 8; ++i) hits |= v.get(8 * g + i) >= least ? 1u << i : 0u;
+                for (; hits; hits &= hits - 1) {
+                    const int e = __ffs((int)hits) - 1, i = 8 * g + e, at = atomicAdd(&s_count, 1);
+                    if (at < kSelList) s_list[at].a = select_key(v.pick8(g, e), base + ((i / VEC) * kSelThreads + (int)threadIdx.x) * VEC + i % VEC);
+                }
             }
         }
         // The list is looked at every fourth step: some hundred keys come in between.
