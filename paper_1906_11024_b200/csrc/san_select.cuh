@@ -21,8 +21,8 @@
 //     Part after part in place of the best first took every pass: one sentence of 32 rows of 128000 float32 86 us, now 29.
 //     Both in one launch, a sentence's CTAs as a cluster whose first CTA went on behind the cluster's barrier, was slower
 //     (device time: 4 rows of 32000 float32 10.3 us against 8.8, 256 of bf16 16.0 against 14.9, 512 of 128000 47.6 against 42.4).
-// Measured (device time of the whole call): 512 rows of 128000 bf16 logits 40.0 us, of which issue and exponentials fill
-// half; 740 rows of 50257 float32 ones off 16-byte boundaries 49.2; 4 rows of 32000 7.8, the chain of one sentence.  The first
+// Measured (device time of the whole call): 512 rows of 128000 bf16 logits 39.7 us, of which issue and exponentials fill
+// half; 740 rows of 50257 float32 ones off 16-byte boundaries 46.0; 4 rows of 32000 7.6, the chain of one sentence.  The first
 // version, which sorted a key per thread and held 32 logits in float32, took 162, 133 and 12.3.  A ring of cp.async stages in
 // shared memory in place of the registers measured the same: loads are not what is waited for.
 // Where more candidates reach the bound than the list holds (rows that are alike nearly everywhere: a mask of
@@ -149,6 +149,28 @@ template <typename K, typename F> __device__ __forceinline__ void rank_list(cons
         for (int j = part; j < count; j += per) above += list[j].over(mine) ? 1 : 0;
         for (int o = 1; o < per; o <<= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
         if (i < count && above < n && part == 0) out(above, mine);
+    }
+}
+// The same for longer lists: eight threads count for four keys at a time, so that a key read serves four.  (144 keys: 8000
+// clocks with a thread a key.)
+template <typename K, typename F> __device__ __forceinline__ void rank_long_list(const K* list, int count, int n, F out) {
+    const int part = threadIdx.x & 7, group = threadIdx.x >> 3, groups = kSelThreads / 8;
+    for (int first = 0; first < count; first += 4 * groups) {
+        K mine[4];
+        int above[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine[e] = list[min(first + group + e * groups, count - 1)];
+#pragma unroll 2
+        for (int j = part; j < count; j += 8) {
+            const K other = list[j];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) above[e] += other.over(mine[e]) ? 1 : 0;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            for (int o = 1; o < 8; o <<= 1) above[e] += __shfl_xor_sync(0xffffffffu, above[e], o);
+            if (part == e && first + group + e * groups < count && above[e] < n) out(above[e], mine[e]);
+        }
     }
 }
 
@@ -457,6 +479,7 @@ __global__ void __launch_bounds__(kSelThreads, SelectGeom<T>::kCtas) select_rows
 }
 
 constexpr int kMergeHeld = 4;                  // candidates per thread and pass
+constexpr int kMergeShort = 64;                // candidates up to which a few threads count for each
 constexpr int kMergeHistory = 4096;            // tokens of the histories in shared memory at once
 
 __device__ __forceinline__ void copy4_async(int* dst, const int* src) {
@@ -573,10 +596,30 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
             if (in) s_list[at] = k;
         };
         unsigned long long key[kMergeHeld];
-        if (total <= kSelThreads) {                                   // few enough to look at them all
+        if (total <= kSelThreads) {                                   // one a thread
             Key128 k{0, 0};
             if (held[0] != 0) k = exact(slot_of((int)threadIdx.x), held[0]);
-            list(k.a != 0, k);
+            // Only the best ones are listed, found by the upper halves of their ranks: ordering 144 takes 6000 clocks, this 600.
+            const unsigned upper = (unsigned)(k.a >> 32);
+            unsigned bound = 1;
+            int have = __syncthreads_count(upper >= bound);
+            if (have > kMergeShort) {
+                unsigned warp_top, least;
+                group_bounds(upper, beam, &warp_top, &least);
+                if (lane == 0) { s_least[warp] = least; s_most[warp] = warp_top; }
+                __syncthreads();
+                unsigned long long most = s_most[0];
+#pragma unroll
+                for (int w = 1; w < kSelWarps; ++w) most = s_most[w] > most ? s_most[w] : most;
+                bound = max((unsigned)join_bounds(s_least, beam), 1u);
+                have = __syncthreads_count(upper >= bound);
+                for (unsigned hi = (unsigned)most; have > kMergeShort && hi > bound; ) {
+                    const unsigned mid = bound + (hi - bound + 1) / 2;
+                    const int n = __syncthreads_count(upper >= mid);
+                    if (n >= beam) { bound = mid; have = n; } else hi = mid - 1;
+                }
+            }
+            list(upper >= bound, k);
         } else {
             // ranks by a multiplication, within 2^-51 of the ones by the division: good enough for a bound
             unsigned long long top = 0;
@@ -599,7 +642,7 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
             if (kept == beam && s_best[turn][beam - 1].a > bound) bound = s_best[turn][beam - 1].a - 16;     // an exact rank
             if (bound == 0) bound = 1;
             // Candidates are not mixed over the threads as logits are (hypotheses differ in score, places in rank), so the
-            // bound may be low: halve the way to the largest until at most 128 reach it, never fewer than `beam` of this pass
+            // bound may be low: halve the way to the largest until at most kMergeShort reach it, never fewer than `beam` of this pass
             // unless the bound is that of the passes before.
             for (int step = 0, count = 0; step < 64; ++step) {
                 const unsigned long long mid = step == 0 ? bound : bound + (most - bound + 1) / 2;
@@ -614,7 +657,7 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
                 for (int w = 0; w < kSelWarps; ++w) n += s_counts[step & 1][w];
                 if (step == 0 || n >= beam) { bound = mid; count = n; }
                 else most = mid - 1;                                  // fewer than `beam` reach mid
-                if (count <= 128 || most <= bound) break;
+                if (count <= kMergeShort || most <= bound) break;
             }
             bound = bound > 16 ? bound - 16 : 1;                      // further down than the two ranks can differ
 #pragma unroll
@@ -631,7 +674,9 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
         if (threadIdx.x == 0) s_count = 0;
         if (!long_list) {
             count += kept;
-            rank_list(s_list, count, beam, [&](int place, const Key128& k) { s_best[turn ^ 1][place] = k; });
+            auto out = [&](int place, const Key128& k) { s_best[turn ^ 1][place] = k; };
+            if (count <= kMergeShort) rank_list(s_list, count, beam, out);
+            else rank_long_list(s_list, count, beam, out);
             kept = min(count, beam);
         } else {
             Key128 last{~0ull, ~0ull};
