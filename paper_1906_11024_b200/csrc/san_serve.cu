@@ -387,13 +387,17 @@ int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int
     p.n_layers = n_layers; p.max_len = max_len; p.window = window; p.n_sink = n_sink;
     p.v_layer = (long long)n_seq * cap_len * n_kv_heads * kDh;
     p.out_layer = (long long)n_seq * cap_len * n_heads * kDh;
-    const int at_once = max_len >= kTileQ ? kTileMaxLayers : 4;
+    // The tensor-core tiles take sequences of a tile and more, unless the rows that a CTA of window_block_kernel walks are
+    // one slot of its ring.  Measured, tiles and window_block_kernel: 4 x 4096 positions, 8 heads, 4 sinks, window 4: 32.4 and
+    // 24.4 us, 32: 32.2 and 31.8, 96: 35.9 and 43.3; 4 layers and window 4: 65.3 and 47.7.
+    const bool use_tiles = max_len >= kTileQ && (long long)window + n_sink + kWinQ - 1 > kWinTile;
+    const int at_once = use_tiles ? kTileMaxLayers : 4;
     p.n_lg = (int)div_up(n_layers, at_once);
     p.lg = (int)div_up(n_layers, p.n_lg);
     p.n_lg = (int)div_up(n_layers, p.lg);
     p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)kDh));
     if ((long long)n_seq * p.n_lg > 65535) return SAN_ERR_SHAPE;
-    if (max_len >= kTileQ) {
+    if (use_tiles) {
         // A CTA takes a pair of tiles.  Where the last wave would hold less than half of the SMs' CTAs, its pairs are dealt as
         // single tiles, which take about two thirds of a pair's time: 8192 positions x 16 sequences and heads are
         // 3.35 waves of pairs, or three waves and 104 single tiles.

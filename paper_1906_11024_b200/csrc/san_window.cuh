@@ -2,7 +2,7 @@
 // b > a - window or b < n_sink; S = Softmax(q.K^T / 8) over those, computed once and applied to
 // each layer of the block (Eq. 3, Eq. 4).
 //
-// window_block_kernel (mma.sync; sequences below 128 positions, longer ones go to the tiles of san_tile.cuh): CTA = 32 query
+// window_block_kernel (mma.sync; sequences below 128 positions or windows of some 30, others go to the tiles of san_tile.cuh): CTA = 32 query
 // rows of one (sequence, head, layer group), 8 per warp, which are the N side of both products as in attend_kernel: 16
 // accumulator registers a layer, so that four CTAs fit an SM with three layers each.  The CTA walks the
 // rows that any of its queries sees - the sinks, then the window of its first query up to its last query -

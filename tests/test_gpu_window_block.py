@@ -79,6 +79,15 @@ def test_lengths_windows_sinks(lens, cap, H, Hk, L, window, sink):
     _check(q, k, v, got, lens, window, sink)
 
 
+@pytest.mark.parametrize("L", [1, 5])
+@pytest.mark.parametrize("window,sink", [(1, 32), (7, 3), (29, 4), (30, 4), (33, 0), (34, 0)])
+def test_small_windows_of_long_sequences(window, sink, L):
+    """Both sides of the size from which a window's rows no longer fit one slot."""
+    lens, cap, H, Hk = [700, 1, 333], 705, 4, 2
+    q, k, v, got = _run(lens, cap, H, Hk, L, window, sink, seed=window)
+    _check(q, k, v, got, lens, window, sink)
+
+
 def test_equals_the_causal_full_sequence_call():
     """A window over everything is san_full_block's causal form."""
     lens, cap, H, L = [150, 77], 150, 2, 2
