@@ -599,7 +599,8 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
         if (total <= kSelThreads) {                                   // one a thread
             Key128 k{0, 0};
             if (held[0] != 0) k = exact(slot_of((int)threadIdx.x), held[0]);
-            // Only the best ones are listed, found by the upper halves of their ranks: ordering 144 takes 6000 clocks, this 600.
+            // Only the best ones are listed, found by the upper halves of their ranks: 87 sentences x 12
+            // rows of 1549, 144 candidates each, take 22.9 us so and 26.9 with all of them ordered.
             const unsigned upper = (unsigned)(k.a >> 32);
             unsigned bound = 1;
             int have = __syncthreads_count(upper >= bound);
