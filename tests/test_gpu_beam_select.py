@@ -104,6 +104,18 @@ def test_ties_go_to_the_lowest_slot_and_token(beam):
             _compare(_call(x, ld, V, st, S, beam, 2, 0.0), want, st)
 
 
+@pytest.mark.parametrize("beam,V", [(12, 1500), (15, 300), (16, 40), (5, 12000)])
+def test_ties_among_a_few_hundred_candidates(beam, V):
+    """More candidates than are ordered at once, all of the same rank, or of two."""
+    st = dict(score=np.full(beam, -1.5, np.float32), len=np.full(beam, 3, np.int32), done=np.zeros(beam, np.int32),
+              tokens=np.arange(beam * 5).reshape(beam, 5).astype(np.int32))
+    two = torch.zeros(beam, V)
+    two[:, 1::7] = 1.0
+    for x in (torch.zeros(beam, V), two):
+        want = select(x, st["score"], st["len"], st["done"], st["tokens"], 2, 0.6, beam)
+        _compare(_call(x, V, V, st, 1, beam, 2, 0.6), want, st)
+
+
 def test_rising_logits_one_thread_holds_the_best():
     """The best candidates sit next to one another (all in one thread's share), and in the last chunk."""
     for beam in (4, 8, 32):
