@@ -352,7 +352,8 @@ int32_t san_policy_search(const double* js, int32_t n_layers, double theta, int3
  * Where a sentence has fewer candidates than slots, the slots left over come out as done, with
  * score -inf, parent = the slot itself, token eos (0 without eos) and the slot's old length and history.
  * Outputs may be the inputs' own buffers (d_tokens_out = d_tokens with the same ld_tokens, ...).
- * Scores are compared in double (sums of exponentials: float32 terms, double sums).
+ * Scores are compared in double (sums of exponentials: float32 terms, double sums; rows that hold the
+ * same logits in another order may differ by their rounding and then do not tie).
  * A length outside 0..ld_tokens, or ld_tokens itself where a token has to be added, skips the sentence
  * (its outputs are not written) and is reported. */
 typedef struct {
