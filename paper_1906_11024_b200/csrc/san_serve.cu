@@ -379,6 +379,10 @@ int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int
     if (!d_q || !d_k || !d_v || !d_lens || !d_out) return SAN_ERR_NULL;
     if (!aligned(d_q, 16) || !aligned(d_k, 16) || !aligned(d_v, 16) || !aligned(d_out, 16)) return SAN_ERR_SHAPE;
     if (max_len == 0) max_len = cap_len;
+    // No row has more rows before it than that: what "all of them" is written as (2^31 - 1, say) does not reach the index
+    // arithmetic of the kernels, which adds to both.
+    window = std::min(window, max_len);
+    n_sink = std::min(n_sink, max_len);
     WindowParams p;
     std::memset(&p, 0, sizeof(p));
     p.q = static_cast<const __nv_bfloat16*>(d_q); p.k = static_cast<const __nv_bfloat16*>(d_k);

@@ -88,6 +88,14 @@ def test_small_windows_of_long_sequences(window, sink, L):
     _check(q, k, v, got, lens, window, sink)
 
 
+@pytest.mark.parametrize("window,sink", [(100, 2 ** 31 - 1), (1, 2 ** 31 - 63), (100, 2 ** 31 - 64), (2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1)])
+@pytest.mark.parametrize("lens,cap", [([100, 1, 37], 100), ([700, 128, 513, 1], 703)])
+def test_sinks_and_windows_up_to_the_largest_number(lens, cap, window, sink):
+    """More sinks, or a longer window, than there are rows: all of them are seen, by the tiles and below their length."""
+    q, k, v, got = _run(lens, cap, 2, 1, 2, window, sink, seed=cap)
+    _check(q, k, v, got, lens, window, sink)
+
+
 def test_equals_the_causal_full_sequence_call():
     """A window over everything is san_full_block's causal form."""
     lens, cap, H, L = [150, 77], 150, 2, 2
