@@ -376,6 +376,8 @@ int32_t san_beam_select(const san_select_args* args, void* stream);
 /* Where a context keeps the cached rows of a block: the key plane of the block's lowest layer, the value
  * plane of the same layer, and the distance between the value planes of successive layers in elements
  * (kind SAN_SELF: planes [sequence][head][max_tgt_len][64]; SAN_ENCDEC: [sentence][head][max_src_len][64]).
+ * With encdec_shared_context (Eq. 5) an encoder-decoder block has a single value plane and a single output: the distance
+ * is 0, and the calls below take such a block with n_layers = 1 alone (SAN_ERR_SHAPE otherwise).
  * SAN_ERR_UNSUPPORTED for SAN_SELF with self_is_aan.  The addresses stay valid until the policy changes. */
 int32_t san_cache_planes(const san_ctx* ctx, int32_t kind, int32_t block, void** d_k, void** d_v, int64_t* v_stride);
 

@@ -326,7 +326,8 @@ int32_t san_cache_planes(const san_ctx* ctx, int32_t kind, int32_t block, void**
     const size_t v_plane = !self && ctx->cfg.encdec_shared_context ? (size_t)block : (size_t)pol.first_layer_of_block[block];
     *d_k = ctx->cache + (self ? ctx->off_self_k : ctx->off_mem_k) + (size_t)block * plane;
     *d_v = ctx->cache + (self ? ctx->off_self_v : ctx->off_mem_v) + v_plane * plane;
-    *v_stride = (int64_t)(plane / (size_t)ctx->elem_bytes);
+    // One plane for the whole block: no distance that a call over several layers would take.
+    *v_stride = !self && ctx->cfg.encdec_shared_context ? 0 : (int64_t)(plane / (size_t)ctx->elem_bytes);
     return SAN_OK;
 }
 

@@ -147,3 +147,52 @@ def test_cache_planes_of_every_block():
     assert B.san_cache_planes(ctx, B.SAN_SELF, -1)[0] == B.SAN_ERR_RANGE
     assert B.san_cache_planes(ctx, 7, 0)[0] == B.SAN_ERR_RANGE
     B.san_destroy(ctx)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_blocks_that_share_one_context(dtype):
+    """Eq. 5: an encoder-decoder block has one value plane.  No distance to a second one is given, so that a call over the
+    block's layers is refused; one over that plane answers with its values, the last block's too."""
+    san_build.build()
+    dt, code = dtype_of(dtype)
+    L, H, S, src, enc = 4, 2, 3, 9, [1, 3]
+    cfg = B.san_config(n_layers=L, n_heads=H, d_head=DH, max_sent=S, beam=2, max_tgt_len=4, max_src_len=src, dtype=code,
+                       self_is_aan=0, encdec_shared_context=1)
+    rc, cb, wb = B.san_query_bytes(cfg, 1, len(enc))
+    B.check(rc)
+    cache, ws = torch.zeros(cb, dtype=torch.uint8, device=DEV), torch.empty(wb, dtype=torch.uint8, device=DEV)
+    rc, ctx = B.san_create(cfg, [L], enc, cache, cb, ws, wb)
+    B.check(rc)
+    gen = torch.Generator().manual_seed(3)
+    lens, first = [9, 1, 4], [0, 1]
+    k, v, q = (randn(gen, len(enc), *s, dtype=dt) for s in ((S, src, H, DH), (S, src, H, DH), (S, H, DH)))
+    sent, pos = torch.arange(S, dtype=torch.int32, device=DEV), torch.zeros(S, dtype=torch.int32, device=DEV)
+    dl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    dk, dv, dq = k.to(DEV), v.to(DEV), q.to(DEV)
+    for b in range(len(enc)):
+        B.check(B.san_cache_append(ctx, B.SAN_ENCDEC, first[b], first[b] + 1, dk[b], dv[b], sent, pos, dl, S, src))
+    for b, size in enumerate(enc):
+        rc, kp, vp, stride = B.san_cache_planes(ctx, B.SAN_ENCDEC, b)
+        assert (rc, stride) == (B.SAN_OK, 0)
+        make = lambda layers, out: B.cached_rows(                                                # noqa: E731
+            dtype=code, n_heads=H, n_kv_heads=H, n_layers=layers, d_q=dq[b], d_k=kp, d_v=vp, v_stride=stride, max_ids=S,
+            cap_len=src, d_ids=sent, d_lens=dl, n_items=S, d_out=out)
+        if size > 1:
+            out = torch.full((size, S, H, DH), -7.0, dtype=dt, device=DEV)
+            assert B.san_window_attn_bytes(make(size, out), src, 0)[0] == B.SAN_ERR_SHAPE
+            assert B.san_window_attn(make(size, out), src, 0, None, 0) == B.SAN_ERR_SHAPE
+            x = B.shared_prefix(d_k=dk, d_v=dk, v_stride=64, n_prefix=0, cap_len=1, d_lens=dl, d_first=dl)
+            assert B.san_prefix_attn(make(size, out), x, None, 0) == B.SAN_ERR_SHAPE
+        out = torch.full((1, S, H, DH), -7.0, dtype=dt, device=DEV)
+        rows = make(1, out)
+        assert B.san_window_attn_bytes(rows, src, 0) == (B.SAN_OK, 0)
+        B.check(B.san_window_attn(rows, src, 0, None, 0))
+        torch.cuda.synchronize()
+        for i in range(S):
+            for h in range(H):
+                qq, kk, vv = q[b, i, h].double(), k[b, i, :lens[i], h].double(), v[b, None, i, :lens[i], h].double()
+                want, slack = attend(qq, kk, vv)
+                check_outputs(out.cpu()[:, i, h], want, slack, weighted_size(qq, kk, vv), dt, (b, i, h))
+    rc, err, detail = B.san_device_status(ctx)
+    assert (rc, err) == (B.SAN_OK, 0), detail
+    B.san_destroy(ctx)
