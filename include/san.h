@@ -354,8 +354,8 @@ int32_t san_policy_search(const double* js, int32_t n_layers, double theta, int3
  * Outputs may be the inputs' own buffers (d_tokens_out = d_tokens with the same ld_tokens, ...).
  * Scores are compared in double (sums of exponentials: float32 terms, double sums; rows that hold the
  * same logits in another order may differ by their rounding and then do not tie).
- * A length outside 0..ld_tokens, or ld_tokens itself where a token has to be added, skips the sentence
- * (its outputs are not written) and is reported. */
+ * A length outside 0..ld_tokens, ld_tokens itself where a token has to be added, or a length whose ((5 + length) / 6)^alpha
+ * is not within 10^-250 .. 10^250 (an alpha far from 0), skips the sentence (its outputs are not written) and is reported. */
 typedef struct {
     int32_t dtype;            /* of d_logits: SAN_F32 or SAN_BF16 */
     int32_t n_sent, beam, vocab;      /* beam 1..SAN_MAX_BEAM */

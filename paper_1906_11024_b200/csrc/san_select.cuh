@@ -512,7 +512,10 @@ static __global__ void __launch_bounds__(kSelThreads) select_merge_kernel(const 
         s_inverse[b] = 1.0 / s_norm[b];
         s_parent[b] = b; s_token[b] = -1;
         const long long limit = p.tokens ? p.ld_tokens : 0x7ffffffe;
-        if (len < 0 || len > limit || (len == limit && !done && !dead)) {
+        // Scores come back out of ranks by a product with the norm: neither a float32 score over it nor one of its ranks may
+        // leave the normal numbers (2^-149 / 10^250 = 10^-295; 2^128 * 10^250 = 10^289).
+        const bool scale = dead || (s_norm[b] >= 1e-250 && s_norm[b] <= 1e250);
+        if (len < 0 || len > limit || (len == limit && !done && !dead) || !scale) {
             s_bad = 1;
             select_error(p.status, row, len, (int)limit);
         }

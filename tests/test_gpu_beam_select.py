@@ -265,3 +265,34 @@ def test_a_bad_length_skips_its_sentence_and_is_reported():
             assert np.array_equal(got[k][rows], good[k][rows]), k
             assert (got[k][beam:2 * beam] == (-9 if k in ("parent", "next") else -7)).all()
         assert (got["tokens"][beam:2 * beam] == -7).all()
+
+
+@pytest.mark.parametrize("alpha", [32.0, -32.0, 130.0, -130.0])
+def test_large_length_exponents(alpha):
+    """Ranks far from 1 (down to (405 / 6)^-130 = 10^-238): the choice and the scores are those of the definition."""
+    S, beam, V = 2, 4, 50
+    rng = np.random.default_rng(31)
+    st = _state(rng, S, beam, V, 400, 410, done_share=0.3)
+    x = torch.from_numpy(rng.standard_normal((S * beam, V), dtype=np.float32) * 2)
+    want = select(x, st["score"], st["len"], st["done"], st["tokens"], 2, alpha, beam)
+    _compare(_call(x, V, V, st, S, beam, 2, alpha), want, st)
+
+
+@pytest.mark.parametrize("alpha", [300.0, -300.0, 1e38])
+def test_an_exponent_beyond_the_range_of_ranks_is_reported(alpha):
+    """(405 / 6)^300 is no number of 64 bits: the sentence is skipped; one of length 0 (5 / 6, 6 / 6) is answered at 300."""
+    S, beam, V, cap = 2, 4, 50, 410
+    rng = np.random.default_rng(32)
+    st = _state(rng, S, beam, V, 400, cap, done_share=0.0)
+    st["len"][beam:] = 0
+    x = torch.from_numpy(rng.standard_normal((S * beam, V), dtype=np.float32))
+    want = select(x, st["score"], st["len"] * 0, st["done"], st["tokens"], 2, 1.0, beam)
+    status = torch.zeros(8, dtype=torch.int32, device=DEV)
+    got = _call(x, V, V, st, S, beam, 2, alpha, status=status)
+    found = status.cpu().tolist()
+    assert found[:2] == [B.SAN_ERR_DEVICE_CHECK, 8] and 0 <= found[2] < beam and found[3] == 400
+    for k in ("parent", "next", "len", "done"):
+        assert (got[k][:beam] == (-9 if k in ("parent", "next") else -7)).all(), k
+        assert np.array_equal(got[k][beam:], want[k][beam:]), k        # ((5 + 1) / 6)^alpha = 1 for every alpha
+    live = np.abs(got["score"][beam:] - want["score"][beam:])
+    assert (live <= 2.0 ** -20 + 2.0 ** -23 * np.abs(want["score"][beam:])).all()
