@@ -364,7 +364,7 @@ typedef struct {
     int32_t eos;              /* 0..vocab-1, or -1: no token ends a hypothesis */
     float alpha;              /* length exponent, finite */
     const float* d_score; const int32_t* d_len; const int32_t* d_done;       /* [n_sent*beam] */
-    const int32_t* d_tokens; int64_t ld_tokens;     /* [n_sent*beam][ld_tokens], or both token arrays NULL */
+    const int32_t* d_tokens; int64_t ld_tokens;     /* [n_sent*beam][ld_tokens], or both token arrays NULL; 1..0x7fff0000 */
     float* d_score_out; int32_t* d_len_out; int32_t* d_done_out; int32_t* d_tokens_out;
     int32_t* d_parent; int32_t* d_next;
     void* d_workspace; size_t workspace_bytes;

@@ -47,6 +47,7 @@ template <> struct SelectGeom<__nv_bfloat16> { static constexpr int kWords = 16,
 constexpr int kSelList = 1024;                 // keys that may reach the bound between two checks; more: one by one
 constexpr int kSelLong = 96;                   // list length at which the bound is raised
 constexpr int kSelTight = 64;                  // what the list is cut down to (equal logits aside)
+constexpr int kSelMaxTokens = 0x7fff0000;      // of a history: a window of the merge behind it is still within 32 bits
 constexpr int TAG_SELECT = 8;
 
 struct SelectParams {

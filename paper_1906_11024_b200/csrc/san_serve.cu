@@ -296,7 +296,7 @@ int32_t san_beam_select(const san_select_args* a, void* stream) {
     if (!a->d_logits || !a->d_score || !a->d_len || !a->d_done || !a->d_score_out || !a->d_len_out || !a->d_done_out ||
         !a->d_parent || !a->d_next || !a->d_workspace) return SAN_ERR_NULL;
     if ((a->d_tokens == nullptr) != (a->d_tokens_out == nullptr)) return SAN_ERR_NULL;
-    if (a->d_tokens && (a->ld_tokens < 1 || a->ld_tokens > 0x7ffffffe)) return SAN_ERR_SHAPE;
+    if (a->d_tokens && (a->ld_tokens < 1 || a->ld_tokens > kSelMaxTokens)) return SAN_ERR_SHAPE;
     const size_t e = a->dtype == SAN_F32 ? 4 : 2;
     if (!aligned(a->d_logits, e) || !aligned(a->d_workspace, 256)) return SAN_ERR_SHAPE;
     if (a->workspace_bytes < need) return SAN_ERR_CAPACITY;

@@ -35,6 +35,11 @@ def test_select_refusals(kw, status):
     assert _select(**kw) == status
 
 
+def test_select_refuses_histories_past_its_indices():
+    assert _select(ld_tokens=0x7fff0001) == B.SAN_ERR_SHAPE and _select(ld_tokens=0x7ffffffe) == B.SAN_ERR_SHAPE
+    assert _select(ld_tokens=0x7fff0000, workspace_bytes=16) == B.SAN_ERR_CAPACITY      # taken, and refused for the next reason
+
+
 def test_select_workspace():
     rc, n = B.san_beam_select_bytes(64, 4, 32000)
     assert rc == B.SAN_OK and n % (256 * (16 + 8 * 4)) == 0      # whole parts of rows: a maximum, a sum and four keys each
