@@ -261,8 +261,8 @@ template <typename T, int N> struct AttendRing {
 
 // bf16, up to eight query rows, which are the N side of both products: scores D[16 positions x 8 queries] with
 // the key rows as A, outputs D[16 dims x 8 queries] with the value rows, transposed by ldmatrix, as A.
-template <int LG, int N>
-__device__ __forceinline__ void attend_warp_bf16(const AttendParams& p, const AttendRun& u, int first, int step, char* smem, float2* ml, int lane) {
+template <int LG, int N, class Params>
+__device__ __forceinline__ void attend_warp_bf16(const Params& p, const AttendRun& u, int first, int step, char* smem, float2* ml, int lane) {
     const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(smem);
     AttendRing<__nv_bfloat16, N> ring(u, ring_addr, lane, first, step);
     const int g = lane >> 2, t4 = lane & 3;

@@ -182,6 +182,8 @@ struct TileRange {
     __device__ __forceinline__ bool whole(int t) const { return t >= whole_first && t < whole_end; }
 };
 
+template <int WARPS> __device__ __noinline__ void tile_rows_again(const WindowParams& p, char* smem, const uint32_t* again_s);
+
 // ---- windowed prompts: CTA = (query tiles, head, sequence, layer group), longest prompts' ends first; CTAs from
 // `whole` on take one tile each of the pairs that are left (see launch_tiles of the host side)
 struct TileWindow {
@@ -237,7 +239,7 @@ struct TileWindow {
         const uint32_t recent = ~below(w.ns + max(a - p.window + 1, w.lo) - w.lo);
         return (recent | below(w.ns + max(0, p.n_sink - w.lo))) & below(min(self + 1, w.end));
     }
-    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, char* rows, int i, float m, float l) const {
+    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, char* rows, uint32_t* again_s, int i, float m, float l) const {
         const bool mine = i < w.rows;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         bool odd = false;
@@ -261,15 +263,77 @@ struct TileWindow {
             }
             tile_write_rows(rows, piece, reinterpret_cast<char*>(dst + (w.layer0 + y) * p.out_layer), mine);
         }
-        unsigned again = __ballot_sync(0xffffffffu, odd && mine);       // see san_window.cuh
-        while (again) {
-            const int r = __ffs(again) - 1;
-            again &= again - 1;
-            for (int y = 0; y < w.layers; ++y) window_row_again(p, seq, head, w.layer0 + y, a0 + (i & ~31) + r, threadIdx.x & 31);
-        }
+        const unsigned rows_odd = __ballot_sync(0xffffffffu, odd && mine);
+        if ((threadIdx.x & 31) == 0) again_s[threadIdx.x >> 5] = rows_odd;
+    }
+    template <int WARPS> __device__ __forceinline__ void again(char* smem, const uint32_t* again_s) const {
+        uint32_t any = 0;
+        for (int k = 0; k < 2 * kTileQ / 32; ++k) any |= again_s[k];
+        if (any) tile_rows_again<WARPS>(p, smem, again_s);
     }
     __device__ __forceinline__ void failed() const {}
 };
+
+// Row a of (sequence, head), one layer, by one warp: over the rows that are seen and no others, as a row of a decode step.
+constexpr int kAgainBytes = 2 * kAtTile * 128;                          // of shared memory for a warp
+__device__ __forceinline__ void tile_row_again(const WindowParams& p, int seq, int head, int layer, int a, char* smem, int lane) {
+    struct { const char* q; int H, group; float scale_log2e; } rows;
+    rows.q = reinterpret_cast<const char*>(p.q + (long long)seq * p.cap * p.H * kDh);
+    rows.H = p.H; rows.group = 1; rows.scale_log2e = p.scale_log2e;
+    const long long kv = ((long long)seq * p.cap * p.Hk + head / p.group) * kDh;
+    AttendRun u;
+    u.k = reinterpret_cast<const char*>(p.k + kv);
+    u.v = reinterpret_cast<const char*>(p.v + layer * p.v_layer + kv);
+    u.row_bytes = (long long)p.Hk * 128; u.v_stride = 0; u.permuted = false;
+    u.lo = max(0, a - p.window + 1);
+    u.n_sink = min(p.n_sink, u.lo);
+    u.n = u.n_sink + a + 1 - u.lo;
+    u.begin = 0; u.end = u.n;
+    u.item0 = a; u.row0 = 0; u.rows = 1; u.head0 = head;
+    u.layer0 = layer; u.layers = 1; u.slot = 0;
+    float2* ml = reinterpret_cast<float2*>(smem + kAtTile * 128);
+    __syncwarp();                                                       // the row before has been written
+    attend_warp_bf16<1, 2>(rows, u, 0, kAtTile, smem, ml, lane);
+    __syncwarp();
+    const float l = ml[0].y, inv = l == 0.f ? 0.f : 1.f / l;
+    const float2 o = *reinterpret_cast<const float2*>(smem + lane * 8);
+    *reinterpret_cast<uint32_t*>(p.out + layer * p.out_layer + (((long long)seq * p.cap + a) * p.H + head) * kDh + lane * 2) = pack_bf16(o.x * inv, o.y * inv);
+}
+
+// All threads of a CTA that is done: rows that came out as NaN (again_s, a bit for each) are computed again where a value that
+// was multiplied by a weight of zero can be the cause, which chunks that not all of the tile's rows see may hold.  Rows that
+// are NaN by what they see stay: with one NaN among the sinks those are all rows of a prompt.  2 x 8192 positions, window 1024, 8
+// heads, 2 layers: 105 us; with a NaN value among the sinks 0.16 ms, in the middle 1.4, in every row 4.5 (one position
+// after the other for every row that is NaN took 198, 52 and 198).
+template <int WARPS> __device__ __noinline__ void tile_rows_again(const WindowParams& p, char* smem, const uint32_t* again_s) {
+    static_assert(WARPS <= kTileThreads / 32, "warps");
+    TileWindow mode{p};
+    TileWork w;
+    mode.work(&w);
+    bool spoiled = false;
+    for (int x = 0; x < 2; ++x) {
+        if ((again_s[4 * x] | again_s[4 * x + 1] | again_s[4 * x + 2] | again_s[4 * x + 3]) == 0) continue;
+        const TileRange r = mode.range(w, x);
+        const int first = mode.a0 + x * kTileQ, last = min(first + kTileQ, mode.a0 + w.rows) - 1;      // rows of the tile
+        for (int t = 0; t * kTileK < w.end; ++t) {
+            if (!r.any(t) || r.whole(t)) continue;
+            for (int i = threadIdx.x; i < w.layers * kTileK * 8; i += kTileThreads) {
+                const int n = t * kTileK + (i >> 3) % kTileK, y = i / (kTileK * 8), b = n < w.ns ? n : w.lo + n - w.ns;
+                if (n >= w.end || (b <= first && (b < p.n_sink || b > last - p.window))) continue;      // none, or seen by all
+                const uint4 v = *reinterpret_cast<const uint4*>(w.v + y * w.v_stride + b * w.row_bytes + (i & 7) * 16);
+                const uint32_t e = 0x7f80u;                             // an exponent of all ones: no finite number
+                for (const uint32_t z : {v.x, v.y, v.z, v.w}) spoiled |= (z & e) == e || (z >> 16 & e) == e;
+            }
+        }
+    }
+    if (!__syncthreads_or(spoiled)) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int n = 0;
+    for (int k = 0; k < 2 * kTileQ / 32; ++k)
+        for (uint32_t rows = again_s[k]; rows; rows &= rows - 1, ++n)
+            for (int y = 0; y < w.layers && n % WARPS == warp; ++y)
+                tile_row_again(p, mode.seq, mode.head, w.layer0 + y, mode.a0 + 32 * k + __ffs(rows) - 1, smem + warp * kAgainBytes, lane);
+}
 
 // ---- shared prefixes: units as in attend_unit, 128 query rows and runs of p_span chunks
 struct TilePrefix {
@@ -317,7 +381,7 @@ struct TilePrefix {
         const int n = w.end - c0 - 32 * q;
         return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1;
     }
-    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, char* rows, int i, float m, float l) const {
+    template <int LG> __device__ __forceinline__ void finish(const TileWork& w, uint32_t t_out, char* rows, uint32_t*, int i, float m, float l) const {
         const long long n_rows = (long long)p.n_items * p.H, at = i < w.rows ? place(i) : 0;
         const bool mine = i < w.rows;
         if (mine && w.layer0 == 0) p.part_ml[slot * n_rows + at] = make_float2(m, l);
@@ -336,6 +400,7 @@ struct TilePrefix {
             }
         }
     }
+    template <int WARPS> __device__ __forceinline__ void again(char*, const uint32_t*) const {}      // all rows see all there is
     __device__ __forceinline__ void failed() const {
         if (p.status && atomicCAS(&p.status[0], 0, (int)SAN_ERR_TIMEOUT) == 0) { p.status[1] = TAG_TILE; p.status[2] = g; }
     }
@@ -349,6 +414,7 @@ __global__ void __maxnreg__(Mode::kRegs) tile_kernel(const __grid_constant__ Par
     __shared__ __align__(8) uint64_t k_full[kTileKSlots], k_free[kTileKSlots], v_full[kTileVSlots], v_free[kTileVSlots], s_full[2][2], p_full[2][2], pv_done[2][2], q_full[2];
     __shared__ uint32_t tmem_s;
     __shared__ int dead_s;
+    __shared__ uint32_t again_s[2 * kTileQ / 32];
     Mode mode{params};
     TileWork w;
     if (!mode.work(&w)) return;                                         // uniform over the CTA, before anything is allocated
@@ -367,6 +433,7 @@ __global__ void __maxnreg__(Mode::kRegs) tile_kernel(const __grid_constant__ Par
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         dead_s = 0;
+        for (int i = 0; i < 2 * kTileQ / 32; ++i) again_s[i] = 0;
     }
     if (warp == 11) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(tile_u32(&tmem_s)), "r"(kCols) : "memory");
@@ -557,7 +624,7 @@ __global__ void __maxnreg__(Mode::kRegs) tile_kernel(const __grid_constant__ Par
         }
         if (ok && count > 0) ok = outputs(count - 1);
         tile_after_sync();
-        if (ok) mode.template finish<LG>(w, lanes + kOut, sQ + (i & ~31) * 128, i, m, l);       // (the queries have been read)
+        if (ok) mode.template finish<LG>(w, lanes + kOut, sQ + (i & ~31) * 128, again_s, i, m, l);       // (the queries have been read)
         else if (threadIdx.x == 0) mode.failed();
     }
     tile_before_sync();
@@ -566,6 +633,8 @@ __global__ void __maxnreg__(Mode::kRegs) tile_kernel(const __grid_constant__ Par
         __syncwarp();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kCols) : "memory");
     }
+    constexpr int kAgainWarps = (tile_smem_bytes(LG) - 1024) / kAgainBytes;      // as many as find room in the operands' place
+    if (*dead == 0) mode.template again<kAgainWarps < kTileThreads / 32 ? kAgainWarps : kTileThreads / 32>(sQ, again_s);
 }
 
 }  // namespace san

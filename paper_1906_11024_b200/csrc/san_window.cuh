@@ -12,7 +12,8 @@
 // 3 layers: 16.7 us with 16 queries per warp and layers in groups of two (each recomputing the scores), 14.6 in one
 // group (236 registers, two CTAs per SM).
 // A value that a row does not see has weight zero, and zero times an infinity or NaN is NaN: a row whose
-// output came out as NaN is computed again over just the rows it sees (window_row_again).
+// output came out as NaN is computed again over just the rows it sees (window_row_again: one position after the other, in few
+// registers, and they are 128 at most; the tiles of san_tile.cuh, whose rows see more, do it their own way).
 #pragma once
 
 #include "san_attend.cuh"

@@ -131,6 +131,62 @@ def test_what_a_row_does_not_see_does_not_reach_it(what):
     assert not torch.isfinite(got[:, 0, sees]).any()
 
 
+@pytest.mark.parametrize("what", ["nan", "inf", "-inf"])
+@pytest.mark.parametrize("lens,H,Hk,L,window,sink,bad", [
+    ([700, 300], 2, 1, 2, 100, 4, [1]),                         # a sink: every row behind it sees it
+    ([700, 300], 2, 2, 3, 100, 4, [2, 290, 299]),
+    ([1100], 1, 1, 1, 300, 0, [0, 129, 640, 1099]),
+    ([600], 4, 2, 2, 600, 0, [255, 256]),                       # causal
+    ([520], 1, 1, 1, 40, 70, [69, 70, 480]),                    # sinks that end inside a chunk
+    ([100, 60], 2, 1, 3, 20, 2, [1, 50]),                       # below the tiles
+])
+def test_single_bad_values(what, lens, H, Hk, L, window, sink, bad):
+    """One element of some value rows of the last layer: its column alone, of the rows that see it alone, is no number."""
+    cap, col = max(lens), 5
+
+    def spoil(dk, dv):
+        dv[L - 1, :, bad, :, col] = float(what)
+        for i, t in enumerate(lens):
+            dv[:, i, t:] = float("nan")
+
+    q, k, v, got = _run(lens, cap, H, Hk, L, window, sink, spoil=spoil)
+    v[L - 1, :, bad, :, col] = 0.0
+    for i, t in enumerate(lens):
+        hit = [a for a in range(t) if any(b <= a and (b > a - window or b < sink) for b in bad)]
+        rest = torch.ones(t, dtype=torch.bool)
+        rest[hit] = False
+        assert not torch.isfinite(got[L - 1, i, hit][..., col]).any() and torch.isfinite(got[L - 1, i, :t][rest][..., col]).all()
+        got[L - 1, i, hit, :, col] = 0.0
+        r = H // Hk
+        for h in range(H):
+            want, slack, size = _reference(q[i, :t, h].double(), k[i, :t, h // r].double(), v[:, i, :t, h // r].double(), window, sink)
+            want[L - 1, hit, col] = 0.0
+            check_outputs(got[:, i, :t, h], want, slack, size, torch.bfloat16, (i, h))
+
+
+@pytest.mark.parametrize("row", [0, 3000])
+def test_one_bad_value_costs_little(row):
+    """A NaN in one value of a long prompt, seen by thousands of rows: some 1 ms at most (0.1 without), a hundred of them are
+    allowed here."""
+    n, cap, H = 1, 8192, 8
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    mk = lambda *s: torch.randn(*s, generator=gen, device=DEV).to(torch.bfloat16)        # noqa: E731
+    q, k, v = mk(n, cap, H, DH), mk(n, cap, H, DH), mk(1, n, cap, H, DH)
+    v[:, :, row, :, 9] = float("nan")
+    out = torch.zeros(1, n, cap, H, DH, dtype=torch.bfloat16, device=DEV)
+    dl = torch.tensor([cap], dtype=torch.int32, device=DEV)
+    call = lambda: B.check(B.san_window_block(B.SAN_BF16, H, H, 1, cap, 0, q, k, v, dl, n, cap, 0, out))     # noqa: E731
+    call()
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    call()
+    end.record()
+    torch.cuda.synchronize()
+    bad = torch.isnan(out)
+    assert bad[:, :, row:, :, 9].all() and int(bad.sum()) == (cap - row) * H
+    assert begin.elapsed_time(end) < 100
+
+
 def test_inputs_full_of_nan():
     """Every row comes out as NaN, and soon: 2000 rows of a causal prompt."""
     n, cap, H = 1, 2000, 2
