@@ -325,9 +325,12 @@ int32_t san_policy_search(const double* js, int32_t n_layers, double theta, int3
 
 /* ------------------------------------------------------------------------------------------
  * Around the decode step of a beam decoder with long prompts.  None of these calls needs a
- * context or allocates: workspaces are caller buffers (256-byte aligned, sized by the *_bytes
- * functions, contents of no importance between calls; calls whose kernels may overlap on the
- * device need a workspace each).  `d_status` is an optional device int32[8] that the caller has
+ * context or allocates: workspaces are caller buffers (256-byte aligned, contents of no importance between calls; calls
+ * whose kernels may overlap on the device need a workspace each).  The *_bytes functions give the size that a call with
+ * these arguments makes full use of.  A workspace sized for the largest batch serves smaller ones: san_beam_select needs no
+ * more for fewer sentences, beams or tokens; the attention calls take any size from two partial results a query
+ * row (one for a prefix and one for own rows; none for san_window_attn) on and cut rows into fewer runs where it is less than
+ * they would use.  `d_status` is an optional device int32[8] that the caller has
  * zeroed: the first item skipped because of its id, length or position is recorded there as
  * [0] = SAN_ERR_DEVICE_CHECK, [1..4] = kernel tag, item, value, limit, and stays until the
  * caller clears it.  The current device at the call is the one that owns the stream and the

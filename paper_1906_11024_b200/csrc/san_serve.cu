@@ -49,6 +49,11 @@ int32_t launch_after(void (*fn)(P), dim3 grid, unsigned block, cudaStream_t st, 
 // Parts of a row, each of whole steps: the cut with the shortest estimate of (waves of CTAs, four or five per SM) x (steps of a part
 // + the 2.5 steps that the bound, the list and the hand-over of a part take).
 struct SelectCut { int chunks, steps; };
+constexpr int kSelectParts = 64;            // of a row at most
+long long select_most_parts(int vocab) {    // with the shorter steps of the two types
+    return std::min<long long>(kSelectParts, div_up(vocab, SelectGeom<float>::kWords * kSelThreads));
+}
+static_assert(SelectGeom<float>::kWords <= 2 * SelectGeom<__nv_bfloat16>::kWords, "float32 steps are the shorter ones");
 SelectCut select_cut(int32_t dtype, long long rows, int vocab) {
     const bool bf16 = dtype == SAN_BF16;
     const int step = (bf16 ? 2 * SelectGeom<__nv_bfloat16>::kWords : SelectGeom<float>::kWords) * kSelThreads;
@@ -56,7 +61,7 @@ SelectCut select_cut(int32_t dtype, long long rows, int vocab) {
     const long long all = div_up(vocab, step);
     SelectCut best{1, (int)all};
     double least = 1e30;
-    for (long long parts = 1; parts <= std::min<long long>(all, 64); ++parts) {
+    for (long long parts = 1; parts <= std::min<long long>(all, kSelectParts); ++parts) {
         const long long steps = div_up(all, parts), chunks = div_up(all, steps);
         const double cost = (double)std::max<long long>(1, div_up(rows * chunks, ctas)) * ((double)steps + 2.5);
         if (cost < least) { least = cost; best = {(int)chunks, (int)steps}; }
@@ -67,7 +72,7 @@ SelectCut select_cut(int32_t dtype, long long rows, int vocab) {
 int32_t select_shape(int32_t n_sent, int32_t beam, int32_t vocab) {
     if (n_sent < 0 || beam < 1 || beam > SAN_MAX_BEAM || vocab < 1 || vocab > (1 << 28)) return SAN_ERR_SHAPE;
     if ((long long)n_sent * beam > (1 << 24)) return SAN_ERR_SHAPE;
-    if ((long long)n_sent * beam * std::min<long long>(64, div_up(vocab, SelectGeom<float>::kWords * kSelThreads)) > 0x7fffffffLL) return SAN_ERR_SHAPE;
+    if ((long long)n_sent * beam * select_most_parts(vocab) > 0x7fffffffLL) return SAN_ERR_SHAPE;
     return SAN_OK;
 }
 
@@ -103,6 +108,7 @@ int32_t check_prefix(const san_cached_rows* r, const san_shared_prefix* x) {
     return SAN_OK;
 }
 
+constexpr int kOwnLeast = 4;                // tiles of own rows that are not cut
 // How one kind of units (`units` runs of up to `tiles` tiles) is cut where a warp's share of the whole call is
 // `share` tiles: warps per unit and runs of tiles.  A run of no more than 1.25 shares (or `least` tiles) is one warp's.  A longer
 // one is cut into up to four runs for a warp each, so that the warps finish together; beyond that the four
@@ -119,10 +125,15 @@ void cut_runs(int tiles, double share, int least, int* wpu, int* splits, int* sp
     *splits = (int)div_up(tiles, *span);
 }
 
-struct AttendPlan { AttendParams p; size_t ml_bytes, bytes; long long ctas, tiles; };
+struct AttendPlan { AttendParams p; size_t ml_bytes, bytes; long long ctas, tiles, tiles_own; };
 
-// Everything but the addresses.
-int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int window, int n_sink, AttendPlan* out) {
+// Workspace of `rows` partial results: (max, sum) and the layers' outputs of each.
+size_t partial_ml_bytes(size_t rows) { return (rows * sizeof(float2) + 255) / 256 * 256; }
+size_t partial_bytes(size_t rows, int layers) { return partial_ml_bytes(rows) + rows * layers * kDh * sizeof(float); }
+
+// Everything but the addresses.  Rows are cut into no more runs than find room in `room` bytes of workspace (a prefix's result and
+// its row's own one always stay two): a workspace made for a larger batch, which needs fewer runs, serves a smaller one.
+int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int window, int n_sink, size_t room, AttendPlan* out) {
     std::memset(out, 0, sizeof(*out));
     AttendParams& p = out->p;
     const int R = kAtRows;
@@ -135,6 +146,7 @@ int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int wi
     p.n_lg = (int)div_up(r->n_layers, kAtMaxLayers);
     p.lg = (int)div_up(r->n_layers, p.n_lg);
     p.n_lg = (int)div_up(r->n_layers, p.lg);
+    long long p_runs = 0, p_tiles = 0;          // runs of a prefix's rows before they are cut, and tiles (chunks of 64) of one
     if (x && x->n_prefix > 0) {
         p.n_prefix = x->n_prefix; p.pcap = x->cap_len; p.pv_stride = x->v_stride * e;
         p.max_prefix = x->max_len ? x->max_len : x->cap_len;
@@ -152,41 +164,56 @@ int32_t plan_attend(const san_cached_rows* r, const san_shared_prefix* x, int wi
             p.t_n_lg = (int)div_up(r->n_layers, p.t_lg);
             p.p_row_tiles = (int)div_up(rows, 2 * kTileQ);
             // runs of chunks: as many as fill the SMs once, of four chunks or more
-            const long long units = (long long)p.n_prefix * p.p_row_tiles * p.Hk * p.t_n_lg, chunks = div_up(p.max_prefix, kTileK);
-            const long long want = std::max<long long>(1, std::min<long long>(kSms / std::max<long long>(units, 1), div_up(chunks, 4)));
-            p.p_span = (int)div_up(chunks, want);
-            p.p_splits = (int)div_up(chunks, p.p_span);
-            out->tiles = units * p.p_splits;
-            if (out->tiles > 0x7fffffffLL) return SAN_ERR_SHAPE;
+            const long long units = (long long)p.n_prefix * p.p_row_tiles * p.Hk * p.t_n_lg;
+            p_tiles = div_up(p.max_prefix, kTileK);
+            const long long want = std::max<long long>(1, std::min<long long>(kSms / std::max<long long>(units, 1), div_up(p_tiles, 4)));
+            p.p_span = (int)div_up(p_tiles, want);
+            p.p_splits = (int)div_up(p_tiles, p.p_span);
         }
     }
     p.o_row_tiles = (int)div_up(p.group, R);
     const long long bound = window > 0 ? std::min<long long>(p.max_len, (long long)window + n_sink) : p.max_len;
     const long long o_runs = (long long)r->n_items * p.o_row_tiles * p.Hk * p.n_lg, o_tiles = std::max<long long>(1, div_up(bound, kAtTile));
-    long long p_runs = 0, p_tiles = 0;
     if (p.n_prefix > 0 && p.t_lg == 0) {
         p.p_row_tiles = (int)div_up((long long)p.max_group * p.group, R);
         p_runs = (long long)p.n_prefix * p.p_row_tiles * p.Hk * p.n_lg;
         p_tiles = div_up(p.max_prefix, kAtTile);
     }
-    const double share = ((double)o_runs * o_tiles + (double)p_runs * p_tiles) / ((double)kSms * 2 * kAtWarps);
-    if (p_runs > 0) {
-        cut_runs((int)p_tiles, share, e == 4 ? 2 : 4, &p.p_wpu, &p.p_splits, &p.p_span);
+    out->tiles_own = o_tiles;
+    const double share = ((double)o_runs * o_tiles + (double)p_runs * (p.t_lg ? 0 : p_tiles)) / ((double)kSms * 2 * kAtWarps);
+    if (p_runs > 0) cut_runs((int)p_tiles, share, e == 4 ? 2 : 4, &p.p_wpu, &p.p_splits, &p.p_span);
+    cut_runs((int)o_tiles, share, kOwnLeast, &p.o_wpu, &p.o_splits, &p.o_span);
+    const size_t rows = (size_t)r->n_items * r->n_heads;
+    if (rows > 0x7fffffff) return SAN_ERR_SHAPE;
+    if (p.p_splits + p.o_splits > 1 && partial_bytes((p.p_splits + p.o_splits) * rows, r->n_layers) > room) {
+        const int least = p.p_splits > 0 ? 2 : 1, all = p.p_splits + p.o_splits;
+        int most = (int)std::max<size_t>(least, std::min<size_t>(all - 1, room / partial_bytes(rows, r->n_layers) + 1));
+        while (most > least && partial_bytes(most * rows, r->n_layers) > room) --most;
+        const int own = least == 1 ? most : std::max(1, (int)((long long)most * p.o_splits / all));
+        p.o_span = (int)div_up(o_tiles, own);
+        p.o_splits = (int)div_up(o_tiles, p.o_span);
+        if (least > 1) {
+            p.p_span = (int)div_up(p_tiles, most - own);
+            p.p_splits = (int)div_up(p_tiles, p.p_span);
+        }
+    }
+    if (p.t_lg > 0) {
+        out->tiles = (long long)p.n_prefix * p.p_row_tiles * p.Hk * p.t_n_lg * p.p_splits;
+        if (out->tiles > 0x7fffffffLL) return SAN_ERR_SHAPE;
+    } else if (p_runs > 0) {
         if (p_runs * p.p_splits > 0x7fffffffLL) return SAN_ERR_SHAPE;
         p.p_units = (int)(p_runs * p.p_splits);
         p.p_ctas = (int)div_up(p.p_units, kAtWarps / p.p_wpu);
     }
-    cut_runs((int)o_tiles, share, 4, &p.o_wpu, &p.o_splits, &p.o_span);
     if (o_runs * p.o_splits > 0x7fffffffLL) return SAN_ERR_SHAPE;
     p.o_units = (int)(o_runs * p.o_splits);
     p.slots = p.p_splits + p.o_splits;
-    const size_t rows = (size_t)r->n_items * r->n_heads;
     if (p.slots > 1) {
-        out->ml_bytes = (size_t)div_up((long long)(p.slots * rows * sizeof(float2)), 256) * 256;
-        out->bytes = out->ml_bytes + p.slots * rows * r->n_layers * kDh * sizeof(float);
+        out->ml_bytes = partial_ml_bytes(p.slots * rows);
+        out->bytes = partial_bytes(p.slots * rows, r->n_layers);
     }
     out->ctas = p.p_ctas + div_up(p.o_units, kAtWarps / p.o_wpu);
-    if (out->ctas > 0x7fffffffLL || (long long)rows > 0x7fffffffLL) return SAN_ERR_SHAPE;
+    if (out->ctas > 0x7fffffffLL) return SAN_ERR_SHAPE;
     p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)kDh));
     return SAN_OK;
 }
@@ -240,7 +267,7 @@ int32_t launch_attend(const AttendPlan& a, cudaStream_t st) {
 
 int32_t run_attend(const san_cached_rows* r, const san_shared_prefix* x, int window, int n_sink, void* ws, size_t ws_bytes, void* stream) {
     AttendPlan a;
-    int32_t rc = plan_attend(r, x, window, n_sink, &a);
+    int32_t rc = plan_attend(r, x, window, n_sink, ws_bytes, &a);
     if (rc != SAN_OK) return rc;
     if (r->n_items == 0) return SAN_OK;
     if (!r->d_q || !r->d_k || !r->d_v || !r->d_ids || !r->d_lens || !r->d_out) return SAN_ERR_NULL;
@@ -279,17 +306,15 @@ int32_t san_beam_select_bytes(int32_t n_sent, int32_t beam, int32_t vocab, size_
     if (!workspace_bytes) return SAN_ERR_NULL;
     const int32_t rc = select_shape(n_sent, beam, vocab);
     if (rc != SAN_OK) return rc;
-    const long long rows = (long long)n_sent * beam;
-    const int chunks = std::max(select_cut(SAN_F32, rows, vocab).chunks, select_cut(SAN_BF16, rows, vocab).chunks);
-    *workspace_bytes = (size_t)rows * chunks * select_part_bytes(beam);
+    // As many parts as a row can be cut into, not as many as this call's rows are: fewer sentences are cut into more.
+    *workspace_bytes = (size_t)n_sent * beam * select_most_parts(vocab) * select_part_bytes(beam);
     return SAN_OK;
 }
 
 int32_t san_beam_select(const san_select_args* a, void* stream) {
     if (!a) return SAN_ERR_NULL;
     if (a->dtype != SAN_F32 && a->dtype != SAN_BF16) return SAN_ERR_DTYPE;
-    size_t need = 0;
-    int32_t rc = san_beam_select_bytes(a->n_sent, a->beam, a->vocab, &need);
+    const int32_t rc = select_shape(a->n_sent, a->beam, a->vocab);
     if (rc != SAN_OK) return rc;
     if (a->ld_logits < a->vocab || a->eos < -1 || a->eos >= a->vocab || !std::isfinite(a->alpha)) return SAN_ERR_SHAPE;
     if (a->n_sent == 0) return SAN_OK;
@@ -299,12 +324,12 @@ int32_t san_beam_select(const san_select_args* a, void* stream) {
     if (a->d_tokens && (a->ld_tokens < 1 || a->ld_tokens > kSelMaxTokens)) return SAN_ERR_SHAPE;
     const size_t e = a->dtype == SAN_F32 ? 4 : 2;
     if (!aligned(a->d_logits, e) || !aligned(a->d_workspace, 256)) return SAN_ERR_SHAPE;
-    if (a->workspace_bytes < need) return SAN_ERR_CAPACITY;
+    const long long rows = (long long)a->n_sent * a->beam;
+    const SelectCut cut = select_cut(a->dtype, rows, a->vocab);
+    if (a->workspace_bytes < (size_t)rows * cut.chunks * select_part_bytes(a->beam)) return SAN_ERR_CAPACITY;
     SelectParams p;
     std::memset(&p, 0, sizeof(p));
-    const long long rows = (long long)a->n_sent * a->beam;
     p.logits = a->d_logits; p.ld = a->ld_logits; p.vocab = a->vocab; p.n_sent = a->n_sent; p.beam = a->beam;
-    const SelectCut cut = select_cut(a->dtype, rows, a->vocab);
     p.chunks = cut.chunks; p.steps = cut.steps;
     p.eos = a->eos; p.alpha = (double)a->alpha;
     p.score = a->d_score; p.len = a->d_len; p.done = a->d_done; p.tokens = a->d_tokens; p.ld_tokens = a->ld_tokens;
@@ -337,8 +362,13 @@ int32_t san_window_attn_bytes(const san_cached_rows* rows, int32_t window, int32
     if (rc != SAN_OK) return rc;
     if (window < 1 || n_sink < 0) return SAN_ERR_SHAPE;
     AttendPlan a;
-    if ((rc = plan_attend(rows, nullptr, window, n_sink, &a)) != SAN_OK) return rc;
-    *workspace_bytes = a.bytes;
+    if ((rc = plan_attend(rows, nullptr, window, n_sink, SIZE_MAX, &a)) != SAN_OK) return rc;
+    // What any smaller batch or bound needs as well.  n items of c runs and t tiles each have a share of n c t / W tiles a warp (W
+    // warps), so that a run is at most ceil(W / (1.25 n c)) pieces and all items together at most W / (1.25 c) + n.
+    const long long pieces = div_up(a.tiles_own, kOwnLeast), n = rows->n_items, c = (long long)a.p.o_row_tiles * a.p.Hk * a.p.n_lg;
+    const long long most = std::max(std::min<long long>(pieces, 4), div_up(pieces, kAtWarps));
+    const long long partial = std::min(n * most, n + div_up(kSms * 2 * kAtWarps * 4 / 5 + 1, c));
+    *workspace_bytes = most > 1 ? partial_bytes((size_t)partial * rows->n_heads, rows->n_layers) : 0;
     return SAN_OK;
 }
 
@@ -356,7 +386,7 @@ int32_t san_prefix_attn_bytes(const san_cached_rows* rows, const san_shared_pref
     if (rc == SAN_OK) rc = check_prefix(rows, prefix);
     if (rc != SAN_OK) return rc;
     AttendPlan a;
-    if ((rc = plan_attend(rows, prefix, 0, 0, &a)) != SAN_OK) return rc;
+    if ((rc = plan_attend(rows, prefix, 0, 0, SIZE_MAX, &a)) != SAN_OK) return rc;
     *workspace_bytes = a.bytes;
     return SAN_OK;
 }

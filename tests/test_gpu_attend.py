@@ -316,3 +316,66 @@ def test_far_rows_of_a_large_plane():
         kk = small[h].double()
         want, slack = attend(q[0, h].double(), kk, kk[None])
         check_outputs(got[:, 0, h], want, slack, weighted_size(q[0, h].double(), kk, kk[None]), torch.bfloat16, h)
+
+
+def _least(r, room, call):
+    """`call` with a workspace of exactly `room` bytes; what lies behind it stays as it was."""
+    ws = torch.full((room + 512,), 0x5A, dtype=torch.uint8, device=DEV)
+    ws[:room] = 0xFF
+    r.out.fill_(-7)
+    B.check(call(ws, room))
+    torch.cuda.synchronize()
+    assert (ws[room:] == 0x5A).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_window_with_the_workspace_of_a_larger_batch(dtype):
+    """Rows that are cut into several runs, into as many as find room, and into one."""
+    window, sink, H, L = 900, 3, 2, 2
+    lens = [1500, 1024, 7, 0, 1499]
+    r = Rows(dtype, lens, H, 1, L, 1500, seed=2)
+    a = r.args()
+    full = B.san_window_attn_bytes(a, window, sink)[1]
+    one = (len(lens) * H * 8 + 255) // 256 * 256 + len(lens) * H * L * DH * 4
+    assert full > 3 * one
+    for room in (full, 4 * one + 300, 2 * one + 5, 2 * one - 300, 5, 0):
+        _least(r, room, lambda ws, n: B.san_window_attn(a, window, sink, ws, n))
+        r.check(_sees(lens, window, sink))
+    B.check(B.san_window_attn(a, window, sink, None, 0))
+    # the batch shrinks, the workspace is that of its beginning
+    for n in range(len(lens), 0, -1):
+        b = r.args(n_items=n)
+        out = torch.full_like(r.out, -7.0)
+        ws = torch.empty(max(full, 1), dtype=torch.uint8, device=DEV)
+        b.d_out = out.data_ptr()
+        B.check(B.san_window_attn(b, window, sink, ws, full))
+        torch.cuda.synchronize()
+        got = out.flatten()[:L * n * H * DH].view(L, n, H, DH)
+        keep, r.out = r.out, torch.full_like(r.out, -7.0)
+        r.out[:, :n] = got
+        r.check(_sees(lens, window, sink), skip=range(n, len(lens)))
+        r.out = keep
+
+
+@pytest.mark.parametrize("dtype,n,P,H,Hk,L", [
+    ("bf16", 3, 4000, 2, 2, 2),           # one long prefix in many runs
+    ("f32", 3, 900, 2, 1, 2),
+    ("bf16", 257, 2500, 2, 2, 3),         # tensor-core tiles
+])
+def test_prefix_with_the_least_workspace(dtype, n, P, H, Hk, L):
+    """Two partial results a row are enough; less than that is refused."""
+    own = 300
+    lens = [own if i == 1 else 2 + i % 3 for i in range(n)]
+    r = Rows(dtype, lens, H, Hk, L, own, seed=n)
+    pk, pv, dev = _prefixes(r, [P], [0, n], P)
+    a = r.args()
+    x = B.shared_prefix(d_k=dev[0], d_v=dev[1], v_stride=dev[1][0].numel(), n_prefix=1, cap_len=P, d_lens=dev[2], d_first=dev[3])
+    full = B.san_prefix_attn_bytes(a, x)[1]
+    need = lambda k: (k * n * H * 8 + 255) // 256 * 256 + k * n * H * L * DH * 4          # noqa: E731
+    assert full > need(2)
+    for room in sorted({need(2), need(3), need(4) + 100, full - 1}):
+        _least(r, room, lambda ws, b: B.san_prefix_attn(a, x, ws, b))
+        r.check(lambda i: range(lens[i]), lambda i, hk: (pk[0, :, hk].double(), pv[:, 0, :, hk].double()))
+    ws = torch.empty(full, dtype=torch.uint8, device=DEV)
+    assert B.san_prefix_attn(a, x, ws, need(2) - 1) == B.SAN_ERR_CAPACITY
+    assert B.san_prefix_attn(a, x, None, 0) == B.SAN_ERR_NULL

@@ -296,3 +296,28 @@ def test_an_exponent_beyond_the_range_of_ranks_is_reported(alpha):
         assert np.array_equal(got[k][beam:], want[k][beam:]), k        # ((5 + 1) / 6)^alpha = 1 for every alpha
     live = np.abs(got["score"][beam:] - want["score"][beam:])
     assert (live <= 2.0 ** -20 + 2.0 ** -23 * np.abs(want["score"][beam:])).all()
+
+
+def test_a_batch_that_shrinks_in_the_workspace_of_its_beginning():
+    beam, V, S = 4, 9000, 60
+    rng = np.random.default_rng(41)
+    x = torch.from_numpy(rng.standard_normal((S * beam, V), dtype=np.float32) * 2)
+    st = _state(rng, S, beam, V, 5, 8)
+    dx, d = x.to(DEV), {k: torch.from_numpy(np.array(v)).to(DEV) for k, v in st.items()}
+    rc, size = B.san_beam_select_bytes(S, beam, V)
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    for n in (60, 37, 9, 1):
+        o = {k: torch.full_like(v, -7) for k, v in d.items()}
+        parent, nxt = torch.full_like(d["len"], -9), torch.full_like(d["len"], -9)
+        a = B.select_args(dtype=B.SAN_F32, n_sent=n, beam=beam, vocab=V, d_logits=dx, ld_logits=V, eos=2, alpha=0.6, d_score=d["score"],
+                          d_len=d["len"], d_done=d["done"], d_tokens=d["tokens"], ld_tokens=8, d_score_out=o["score"],
+                          d_len_out=o["len"], d_done_out=o["done"], d_tokens_out=o["tokens"], d_parent=parent, d_next=nxt,
+                          d_workspace=ws, workspace_bytes=size)
+        B.check(B.san_beam_select(a))
+        torch.cuda.synchronize()
+        rows = n * beam
+        part = {k: v[:rows] for k, v in st.items()}
+        want = select(x[:rows], part["score"], part["len"], part["done"], part["tokens"], 2, float(np.float32(0.6)), beam)
+        got = {k: v.cpu().numpy()[:rows] for k, v in o.items()} | {"parent": parent.cpu().numpy()[:rows], "next": nxt.cpu().numpy()[:rows]}
+        _compare(got, want, part)
+        assert (parent[rows:] == -9).all() and (o["tokens"][rows:] == -7).all()

@@ -110,5 +110,34 @@ def test_window_block_refusals():
         assert f(**kw) == status, kw
 
 
+def test_select_workspace_holds_for_everything_smaller():
+    """A decoder's batch shrinks while its workspace stays."""
+    for beam in (1, 4, 20, 32):
+        for vocab in (1, 2048, 2049, 32000, 50257, 128000, 1 << 22):
+            sizes = [B.san_beam_select_bytes(n, beam, vocab)[1] for n in range(0, 300)]
+            assert sizes == sorted(sizes)
+    for n in (1, 64, 129):
+        sizes = [B.san_beam_select_bytes(n, beam, 32000)[1] for beam in range(1, 33)]
+        assert sizes == sorted(sizes)
+        sizes = [B.san_beam_select_bytes(n, 4, v)[1] for v in range(1, 140000, 777)]
+        assert sizes == sorted(sizes)
+
+
+@pytest.mark.parametrize("dtype", [B.SAN_F32, B.SAN_BF16])
+@pytest.mark.parametrize("H,Hk,L", [(8, 8, 4), (16, 4, 1), (20, 1, 9)])
+def test_window_workspace_holds_for_everything_smaller(dtype, H, Hk, L):
+    def size(n, cap, window, sink):
+        rc, b = B.san_window_attn_bytes(_rows(dtype=dtype, n_heads=H, n_kv_heads=Hk, n_layers=L, n_items=n, cap_len=cap, v_stride=64 * cap), window, sink)
+        assert rc == B.SAN_OK
+        return b
+
+    for window, sink in ((16, 1), (512, 4), (16384, 5), (1 << 30, 0)):
+        for cap in (100, 4096, 131072):
+            sizes = [size(n, cap, window, sink) for n in list(range(0, 200)) + [256, 500, 1000, 5000]]
+            assert sizes == sorted(sizes)
+        sizes = [size(64, cap, window, sink) for cap in range(1, 70000, 331)]
+        assert sizes == sorted(sizes)
+
+
 def test_cache_planes_needs_a_context():
     assert B.san_cache_planes(None, B.SAN_SELF, 0)[0] == B.SAN_ERR_NULL
