@@ -355,8 +355,9 @@ int32_t san_policy_search(const double* js, int32_t n_layers, double theta, int3
  * Where a sentence has fewer candidates than slots, the slots left over come out as done, with
  * score -inf, parent = the slot itself, token eos (0 without eos) and the slot's old length and history.
  * Outputs may be the inputs' own buffers (d_tokens_out = d_tokens with the same ld_tokens, ...).
- * Scores are compared in double (sums of exponentials: float32 terms, double sums; rows that hold the
- * same logits in another order may differ by their rounding and then do not tie).
+ * Scores are compared in double.  A row's sum of exponentials has float32 terms, added in float32 within
+ * a thread's 8 (float32) or 32 (bf16) logits of a step and in double beyond: within 3e-6 relative at worst, whatever the vocabulary.
+ * Rows that hold the same logits in another order may differ by that and then do not tie.
  * A length outside 0..ld_tokens, ld_tokens itself where a token has to be added, or a length whose ((5 + length) / 6)^alpha
  * is not within 10^-250 .. 10^250 (an alpha far from 0), skips the sentence (its outputs are not written) and is reported. */
 typedef struct {

@@ -8,8 +8,7 @@
 // The logits are read once and that is what bounds the call; everything else is a few KB:
 //   select_rows_kernel   CTA = (hypothesis, part of the vocabulary), in steps of 8 or 16 KB, the next step's logits on their way
 //     into registers while a step is worked on.  A thread keeps the maximum and the sum of 2^(x log2(e) - M) of
-//     its logits, three instructions a logit (float32, rescaled when the maximum moves; the threads' sums are joined
-//     in double).  The part's best `beam` logits come out without sorting it: the beam-th largest of the 256
+//     its logits (float32 within a step, double across steps and threads).  The part's best `beam` logits come out without sorting it: the beam-th largest of the 256
 //     threads' maxima in the first step is a lower bound T of the beam-th best logit, which hardly more than
 //     `beam` logits of a step reach; those go to a list in shared memory, T is raised when the list fills up, and
 //     at the end each key finds its own place by counting the ones above it.
@@ -21,8 +20,8 @@
 //     Part after part in place of the best first took every pass: one sentence of 32 rows of 128000 float32 86 us, now 29.
 //     Both in one launch, a sentence's CTAs as a cluster whose first CTA went on behind the cluster's barrier, was slower
 //     (device time: 4 rows of 32000 float32 10.3 us against 8.8, 256 of bf16 16.0 against 14.9, 512 of 128000 47.6 against 42.4).
-// Measured (device time of the whole call): 512 rows of 128000 bf16 logits 39.7 us, of which issue and exponentials fill
-// half; 740 rows of 50257 float32 ones off 16-byte boundaries 46.0; 4 rows of 32000 7.6, the chain of one sentence.  The first
+// Measured (device time of the whole call): 512 rows of 128000 bf16 logits 41.1 us, of which issue and exponentials fill
+// half; 740 rows of 50257 float32 ones off 16-byte boundaries 47.1; 4 rows of 32000 7.6, the chain of one sentence.  The first
 // version, which sorted a key per thread and held 32 logits in float32, took 162, 133 and 12.3.  A ring of cp.async stages in
 // shared memory in place of the registers measured the same: loads are not what is waited for.
 // Where more candidates reach the bound than the list holds (rows that are alike nearly everywhere: a mask of
@@ -333,11 +332,17 @@ __global__ void __launch_bounds__(kSelThreads, SelectGeom<T>::kCtas) select_rows
             }
         }
     };
-    // Sum of e^(x - top).  With M = fl(c top), c = fl(log2 e): the arguments c x - M are rounded once, relative to
-    // themselves (the product is exact inside the FMA), and M - c top, the same for all, is put right at the
-    // end.  A maximum so large that c x could be infinite, or infinite itself: only logits equal to it count.
+    // Sum of e^(x - top): the terms of a step in float32 (8 or 32 of them, four partial sums), the steps in double, so that
+    // the additions' roundings do not grow with the row (in float32 throughout: 512 rows of 128000 bf16 logits off by up
+    // to 7e-6, 592 of 2^20 by 5e-5, but 1.3 us less
+    // for either measured case).  Terms are 2^(c x - M), c = fl(log2 e): the arguments are rounded once,
+    // relative to themselves (the product is exact inside the FMA), and 2^(M - c top) is put right at the end.  M is the
+    // rounded c top of some step before and moves when the maximum has grown by 2^4 since, so that what a
+    // rescaling is off by shrinks faster than rescalings come.  A maximum so large that c x could be infinite, or infinite
+    // itself: only logits equal to it count.
     constexpr float c = 1.4426950408889634f;
-    float top = -INFINITY, m = 0.f, part[4] = {0.f, 0.f, 0.f, 0.f};      // two pairs of partial sums
+    float top = -INFINITY, m = 0.f;
+    double part = 0.0;
     float bound = -INFINITY;
     if (threadIdx.x == 0) s_count = 0;
     int step = 0;
@@ -358,13 +363,18 @@ __global__ void __launch_bounds__(kSelThreads, SelectGeom<T>::kCtas) select_rows
             largest();
         }
         if (t > top) {
-            const float m_new = t * c, scale = fabsf(top) < 1e30f && fabsf(t) < 1e30f ? exp2_fast(m - m_new) : 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) part[i] *= scale;
-            top = t; m = m_new;
+            if (!(fabsf(top) < 1e30f && fabsf(t) < 1e30f)) {
+                part = 0.0;
+                m = t * c;
+            } else if (fmaf(t, c, -m) > 4.f) {
+                const float m_new = t * c;
+                part *= (double)exp2_fast(m - m_new);
+                m = m_new;
+            }
+            top = t;
         }
         if (fabsf(top) < 1e30f) {
-            unsigned long long sum[2] = {pair_f32(part[0], part[1]), pair_f32(part[2], part[3])};
+            unsigned long long sum[2] = {0ull, 0ull};
             const unsigned long long c2 = pair_f32(c, c), m2 = pair_f32(-m, -m);
 #pragma unroll
             for (int i = 0; i < N; i += 2) {
@@ -372,11 +382,14 @@ __global__ void __launch_bounds__(kSelThreads, SelectGeom<T>::kCtas) select_rows
                 unpair_f32(fma_f32x2(pair_f32(v.get(i), v.get(i + 1)), c2, m2), y, z);
                 sum[(i >> 1) & 1] = add_f32x2(sum[(i >> 1) & 1], pair_f32(exp2_fast(y), exp2_fast(z)));
             }
-            unpair_f32(sum[0], part[0], part[1]);
-            unpair_f32(sum[1], part[2], part[3]);
+            float y, z;
+            unpair_f32(add_f32x2(sum[0], sum[1]), y, z);
+            part += (double)(y + z);
         } else if (top > -INFINITY) {
+            float equal = 0.f;
 #pragma unroll
-            for (int i = 0; i < N; ++i) part[i & 3] += v.get(i) == top ? 1.f : 0.f;
+            for (int i = 0; i < N; ++i) equal += v.get(i) == top ? 1.f : 0.f;
+            part += (double)equal;
         }
         if (base == begin) {
             // The first bound: the beam-th largest of the threads' maxima, or a little below it, found by halving the
@@ -431,10 +444,9 @@ __global__ void __launch_bounds__(kSelThreads, SelectGeom<T>::kCtas) select_rows
         }
     }
     __syncthreads();
-    float sum = (part[0] + part[1]) + (part[2] + part[3]);
-    if (fabsf(top) < 1e30f) sum *= exp2_fast(-fmaf(top, c, -m));      // 2^(M - c top)
+    if (fabsf(top) < 1e30f) part *= (double)exp2_fast(-fmaf(top, c, -m));      // 2^(M - c top)
     const float wtop = warp_max(top);
-    double wsum = sum == 0.f ? 0.0 : top == wtop ? (double)sum : (double)sum * (double)exp2_fast((top - wtop) * c);
+    double wsum = part == 0.0 || top == wtop ? part : part * (double)exp2_fast((top - wtop) * c);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) wsum += __shfl_xor_sync(0xffffffffu, wsum, o);
     if (lane == 0) { s_max[warp] = wtop; s_sum[warp] = wsum; }

@@ -321,3 +321,40 @@ def test_a_batch_that_shrinks_in_the_workspace_of_its_beginning():
         got = {k: v.cpu().numpy()[:rows] for k, v in o.items()} | {"parent": parent.cpu().numpy()[:rows], "next": nxt.cpu().numpy()[:rows]}
         _compare(got, want, part)
         assert (parent[rows:] == -9).all() and (o["tokens"][rows:] == -7).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("S,V", [(512, 128000), (592, 1 << 20)])
+def test_sums_of_long_rows_do_not_drift(dtype, S, V):
+    """One long part a row, with terms that are all alike: what each addition rounds off has the same sign.  Beam 1, so that the
+    scores are the sums."""
+    dt, code = dtype_of(dtype)
+    val = (-0.05 - torch.arange(S, device=DEV) % 512 * 0.0137).to(dt)
+    x = val[:, None].repeat(1, V)
+    x[:, :8192] = 0.0                                       # every thread's maximum
+    i32 = lambda n: torch.full((S,), n, dtype=torch.int32, device=DEV)       # noqa: E731
+    d = dict(d_score=torch.full((S,), -1.0, device=DEV), d_len=i32(3), d_done=i32(0))
+    o = dict(d_score_out=torch.zeros(S, device=DEV), d_len_out=i32(-7), d_done_out=i32(-7), d_parent=i32(-9), d_next=i32(-9))
+    rc, n = B.san_beam_select_bytes(S, 1, V)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    B.check(B.san_beam_select(B.select_args(dtype=code, n_sent=S, beam=1, vocab=V, d_logits=x, ld_logits=V, eos=-1, alpha=0.0,
+                                            d_workspace=ws, workspace_bytes=n, **d, **o)))
+    torch.cuda.synchronize()
+    z = val.double()
+    want = -1.0 - (8192 + (V - 8192) * z.exp()).log()
+    # a term: the exponential within 2^-22, its argument z log2(e) rounded by half a step (|z| 2^-24 of the term); up to nine
+    # additions within a step; the sum's relative error is the logarithm's absolute one; the score is rounded once
+    bound = 2.0 ** -22 + z.abs() * 2.0 ** -24 + 9 * 2.0 ** -24 + 2.0 ** -24 * want.abs()
+    assert (o["d_next"] == 0).all()
+    assert ((o["d_score_out"].double() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sums_of_rising_rows(dtype):
+    """The maximum moves with every step, by little: sums are not rescaled each time."""
+    beam, V, rows = 1, 128000, 3
+    x = torch.stack([torch.arange(V) * s for s in (1e-5, 1e-4, 1e-3)]).to(dtype_of(dtype)[0])
+    st = dict(score=np.full(rows, -1.0, np.float32), len=np.full(rows, 3, np.int32), done=np.zeros(rows, np.int32),
+              tokens=np.zeros((rows, 5), np.int32))
+    want = select(x, st["score"], st["len"], st["done"], st["tokens"], -1, 0.0, beam)
+    _compare(_call(x, V, V, st, rows, beam, -1, 0.0), want, st)
