@@ -625,7 +625,6 @@ __global__ void __maxnreg__(Mode::kRegs) tile_kernel(const __grid_constant__ Par
         if (ok && count > 0) ok = outputs(count - 1);
         tile_after_sync();
         if (ok) mode.template finish<LG>(w, lanes + kOut, sQ + (i & ~31) * 128, again_s, i, m, l);       // (the queries have been read)
-        else if (threadIdx.x == 0) mode.failed();
     }
     tile_before_sync();
     __syncthreads();
@@ -633,8 +632,13 @@ __global__ void __maxnreg__(Mode::kRegs) tile_kernel(const __grid_constant__ Par
         __syncwarp();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kCols) : "memory");
     }
+    // Whichever warp's wait ran out: the other tile may have finished by then.
+    if (*dead != 0) {
+        if (threadIdx.x == 0) mode.failed();
+        return;
+    }
     constexpr int kAgainWarps = (tile_smem_bytes(LG) - 1024) / kAgainBytes;      // as many as find room in the operands' place
-    if (*dead == 0) mode.template again<kAgainWarps < kTileThreads / 32 ? kAgainWarps : kTileThreads / 32>(sQ, again_s);
+    mode.template again<kAgainWarps < kTileThreads / 32 ? kAgainWarps : kTileThreads / 32>(sQ, again_s);
 }
 
 }  // namespace san
