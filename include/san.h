@@ -357,7 +357,8 @@ int32_t san_policy_search(const double* js, int32_t n_layers, double theta, int3
  * Outputs may be the inputs' own buffers (d_tokens_out = d_tokens with the same ld_tokens, ...).
  * Scores are compared in double.  A row's sum of exponentials has float32 terms, added in float32 within
  * a thread's 8 (float32) or 32 (bf16) logits of a step and in double beyond: within 3e-6 relative at worst, whatever the vocabulary.
- * Rows that hold the same logits in another order may differ by that and then do not tie.
+ * Rows that hold the same logits in another order, or all of them moved by a constant, may differ by that and then do
+ * not tie; a row of one token (the others masked) offers it at the hypothesis' score, exactly.
  * A length outside 0..ld_tokens, ld_tokens itself where a token has to be added, or a length whose ((5 + length) / 6)^alpha
  * is not within 10^-250 .. 10^250 (an alpha far from 0), skips the sentence (its outputs are not written) and is reported. */
 typedef struct {

@@ -444,7 +444,13 @@ __global__ void __launch_bounds__(kSelThreads, SelectGeom<T>::kCtas) select_rows
         }
     }
     __syncthreads();
-    if (fabsf(top) < 1e30f) part *= (double)exp2_fast(-fmaf(top, c, -m));      // 2^(M - c top)
+    // 2^(M - c top).  The maximum's own term alone counts as 1 whatever it was rounded to (a row of one token has the sum 1), and
+    // rounding to float32 once lets the two exponentials' errors cancel where they are one another's reverse: rows with the same
+    // terms under another maximum mostly have the same sum.  (A division by that term: 3 to 15 us more for the cases above.)
+    if (fabsf(top) < 1e30f) {
+        const float rest = fmaf(top, c, -m);
+        part = part == (double)exp2_fast(rest) ? 1.0 : (double)((float)part * exp2_fast(-rest));
+    }
     const float wtop = warp_max(top);
     double wsum = part == 0.0 || top == wtop ? part : part * (double)exp2_fast((top - wtop) * c);
 #pragma unroll

@@ -358,3 +358,23 @@ def test_sums_of_rising_rows(dtype):
               tokens=np.zeros((rows, 5), np.int32))
     want = select(x, st["score"], st["len"], st["done"], st["tokens"], -1, 0.0, beam)
     _compare(_call(x, V, V, st, rows, beam, -1, 0.0), want, st)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_token_alone_has_all_of_the_probability(dtype):
+    """Rows with one token, or one that is not masked, offer it at the hypothesis' own score: they tie with one another and with
+    finished hypotheses, whatever the logit."""
+    S, beam = 40, 16
+    rng = np.random.default_rng(51)
+    for V in (1, 3000):
+        x = torch.full((S * beam, V), -float("inf"))
+        at = torch.from_numpy(rng.integers(0, V, S * beam))
+        x[torch.arange(S * beam), at] = torch.from_numpy(rng.standard_normal(S * beam, dtype=np.float32) * 10)
+        x = x.to(dtype_of(dtype)[0])
+        st = _state(rng, S, beam, V, 6, 9, done_share=0.3)
+        st["score"][:] = -1.5
+        st["len"][st["done"] == 0] = 5
+        want = select(x, st["score"], st["len"], st["done"], st["tokens"], -1, 0.0, beam)
+        got = _call(x, V, V, st, S, beam, -1, 0.0)
+        _compare(got, want, st)
+        assert (got["score"] == -1.5).all() and np.array_equal(got["parent"], np.tile(np.arange(beam), S))
