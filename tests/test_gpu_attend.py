@@ -379,3 +379,102 @@ def test_prefix_with_the_least_workspace(dtype, n, P, H, Hk, L):
     ws = torch.empty(full, dtype=torch.uint8, device=DEV)
     assert B.san_prefix_attn(a, x, ws, need(2) - 1) == B.SAN_ERR_CAPACITY
     assert B.san_prefix_attn(a, x, None, 0) == B.SAN_ERR_NULL
+
+
+def test_many_small_prefixes_without_a_bound_on_groups():
+    """max_group left at 0: any prefix may have all items, by the host's knowledge; their kernel is the tiles' then."""
+    G, own = 24, 5
+    groups = [0]
+    for g in range(G):
+        groups.append(groups[-1] + (g * 5) % 9)                # 0 to 8 items each
+    lens = [(i * 3) % (own + 1) for i in range(groups[-1])]
+    plens = [(g * 37) % 65 for g in range(G)]
+    for bound in (0, 8):
+        r = Rows("bf16", lens, 2, 2, 2, own, seed=bound)
+        _prefix(r, plens, groups, 64, max_group=bound)
+
+
+@pytest.mark.parametrize("n,P,H,Hk,L", [(100, 2500, 16, 1, 2), (400, 3000, 8, 2, 1), (130, 2100, 12, 3, 3)])
+def test_tensor_core_tiles_with_grouped_heads(n, P, H, Hk, L):
+    """4 and 16 query heads a key head: 256 rows of a tile pair are several items' heads."""
+    r = Rows("bf16", [i % 4 for i in range(n)], H, Hk, L, 4, seed=n)
+    _prefix(r, [P], [0, n], P)
+
+
+@pytest.mark.parametrize("what", ["inf", "-inf", "nan"])
+@pytest.mark.parametrize("n", [3, 300])
+def test_bad_values_in_a_prefix(what, n):
+    """One element of one value row of a prefix, by the streams and by the tiles: its column is no number for the rows behind
+    that prefix, all other outputs are as they are without it."""
+    P, L, col, bad = 2500, 2, 11, 1777
+    r = Rows("bf16", [2] * (n + 2), 2, 2, L, 4, seed=n)
+    pk, pv, dev = _prefixes(r, [P, 30], [0, n, n + 2], P)
+    pv[1, 0, bad, :, col] = 0.0
+    dev[1][1, 0, bad, :, col] = float(what)
+    a = r.args()
+    x = B.shared_prefix(d_k=dev[0], d_v=dev[1], v_stride=dev[1][0].numel(), n_prefix=2, cap_len=P, d_lens=dev[2], d_first=dev[3])
+    size = B.san_prefix_attn_bytes(a, x)[1]
+    ws = torch.full((size,), 0xFF, dtype=torch.uint8, device=DEV)
+    B.check(B.san_prefix_attn(a, x, ws, size))
+    torch.cuda.synchronize()
+    assert not torch.isfinite(r.out[1, :n, :, col]).any()
+    r.out[1, :n, :, col] = 0.0
+    got = r.out.cpu()
+    assert torch.isfinite(got).all()
+    for i in list(range(0, n, max(1, n // 20))) + [n, n + 1]:
+        g, plen = (0, P) if i < n else (1, 30)
+        for h in range(2):
+            q = r.q[i, h].double()
+            k = torch.cat([pk[g, :plen, h].double(), r.k[r.ids[i], h, :2].double()])
+            v = torch.cat([pv[:, g, :plen, h].double(), r.v[:, r.ids[i], h, :2].double()], 1)
+            want, slack = attend(q, k, v)
+            if i < n:
+                want[1, col] = 0.0
+            check_outputs(got[:, i, h], want, slack, weighted_size(q, k, v), r.dt, (i, h))
+
+
+@pytest.mark.parametrize("n,own", [(2, 3), (200, 3)])
+def test_far_rows_of_large_prefixes(n, own):
+    """Byte offsets beyond 32 bits in the arrays of a prefix, by the streams and by the tiles."""
+    P, H, G = 70000, 64, 4                                          # 2.3 GB of keys, and of values
+    r = Rows("bf16", [own] * n, H, H, 1, 4, seed=n)
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    pk, pv = (torch.randn(*s, G, P, H, DH, generator=gen, device=DEV, dtype=torch.bfloat16) for s in ((), (1,)))
+    plens, first = [5, 0, 9, P], [0, 0, 0, 1, n]                    # item 0 behind the third prefix, the others behind the last
+    dev = [torch.tensor(x, dtype=torch.int32, device=DEV) for x in (plens, first)]
+    a = r.args()
+    x = B.shared_prefix(d_k=pk, d_v=pv, v_stride=pv.numel(), n_prefix=G, cap_len=P, d_lens=dev[0], d_first=dev[1], max_group=max(1, n - 1))
+    size = B.san_prefix_attn_bytes(a, x)[1]
+    ws = torch.full((size,), 0xFF, dtype=torch.uint8, device=DEV)
+    B.check(B.san_prefix_attn(a, x, ws, size))
+    torch.cuda.synchronize()
+    assert int(r.status[0]) == 0
+    for i, h in ((0, 63), (1, 0), (1, 63), (n - 1, 31)):
+        g = 2 if i == 0 else 3
+        q = r.q[i, h].double()
+        k = torch.cat([pk[g, :plens[g], h].cpu().double(), r.k[r.ids[i], h, :own].double()])
+        v = torch.cat([pv[:, g, :plens[g], h].cpu().double(), r.v[:, r.ids[i], h, :own].double()], 1)
+        want, slack = attend(q, k, v)
+        check_outputs(r.out[:, i, h].cpu(), want, slack, weighted_size(q, k, v), r.dt, (i, h))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_two_streams_at_once_behind_their_inputs(dtype):
+    """Two calls that may overlap, a workspace each, both behind what wrote their inputs."""
+    r = Rows(dtype, [1500, 1024, 700], 2, 1, 2, 1500, seed=3)
+    pk, pv, dev = _prefixes(r, [900], [0, 3], 900)
+    other = torch.full_like(r.out, -7.0)
+    a, b = r.args(), r.args(d_out=other)
+    x = B.shared_prefix(d_k=dev[0], d_v=dev[1], v_stride=dev[1][0].numel(), n_prefix=1, cap_len=900, d_lens=dev[2], d_first=dev[3])
+    na, nb = B.san_prefix_attn_bytes(a, x)[1], B.san_window_attn_bytes(b, 1200, 2)[1]
+    wa, wb = (torch.full((max(s, 1),), 0xFF, dtype=torch.uint8, device=DEV) for s in (na, nb))
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    for s in (one, two):
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        B.check(B.san_prefix_attn(a, x, wa, na, one))
+        B.check(B.san_window_attn(b, 1200, 2, wb, nb, two))
+    torch.cuda.synchronize()
+    r.check(lambda i: range(r.lens[i]), lambda i, hk: (pk[0, :, hk].double(), pv[:, 0, :, hk].double()))
+    r.out = other
+    r.check(_sees(r.lens, 1200, 2))

@@ -378,3 +378,27 @@ def test_a_token_alone_has_all_of_the_probability(dtype):
         got = _call(x, V, V, st, S, beam, -1, 0.0)
         _compare(got, want, st)
         assert (got["score"] == -1.5).all() and np.array_equal(got["parent"], np.tile(np.arange(beam), S))
+
+
+def test_on_another_stream_behind_its_inputs():
+    """As test_in_place_over_several_steps_and_another_stream, the side stream waiting for what fills the buffers."""
+    S, beam, V = 6, 5, 900
+    rng = np.random.default_rng(61)
+    st = _state(rng, S, beam, V, 30, 40, done_share=0.1)
+    x = torch.from_numpy(rng.standard_normal((S * beam, V), dtype=np.float32) * 3)
+    want = select(x, st["score"], st["len"], st["done"], st["tokens"], 2, float(np.float32(0.6)), beam)
+    side = torch.cuda.Stream()
+    dx, d = torch.empty(S * beam, V, device=DEV), {k: torch.from_numpy(np.array(v)).to(DEV) for k, v in st.items()}
+    dx.copy_(x)
+    o = {k: torch.full_like(v, -7) for k, v in d.items()}
+    parent, nxt = torch.full_like(d["len"], -9), torch.full_like(d["len"], -9)
+    rc, n = B.san_beam_select_bytes(S, beam, V)
+    ws = torch.full((n,), 0xA5, dtype=torch.uint8, device=DEV)
+    a = B.select_args(dtype=B.SAN_F32, n_sent=S, beam=beam, vocab=V, d_logits=dx, ld_logits=V, eos=2, alpha=0.6, d_score=d["score"],
+                      d_len=d["len"], d_done=d["done"], d_tokens=d["tokens"], ld_tokens=40, d_score_out=o["score"], d_len_out=o["len"],
+                      d_done_out=o["done"], d_tokens_out=o["tokens"], d_parent=parent, d_next=nxt, d_workspace=ws, workspace_bytes=n)
+    side.wait_stream(torch.cuda.current_stream())
+    B.check(B.san_beam_select(a, side))
+    side.synchronize()
+    got = {k: v.cpu().numpy() for k, v in o.items()} | {"parent": parent.cpu().numpy(), "next": nxt.cpu().numpy()}
+    _compare(got, want, st)

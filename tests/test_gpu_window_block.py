@@ -4,7 +4,7 @@ import torch
 
 from paper_1906_11024_b200 import binding as B
 from paper_1906_11024_b200 import build as san_build
-from tests.serve_helpers import DH, check_outputs, randn
+from tests.serve_helpers import DH, attend, check_outputs, randn, weighted_size
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -241,3 +241,43 @@ def test_captured_and_replayed():
         g.replay()
         torch.cuda.synchronize()
         _check(q, k, v, out.cpu(), lens, 30, 3)
+
+
+@pytest.mark.parametrize("window,sink", [(100, 3), (20, 2)])
+def test_far_rows_of_large_arrays(window, sink):
+    """Byte offsets beyond 32 bits in every array, by the tiles and by the kernel for small windows: the last sequence's last
+    rows, of the last layer too."""
+    n, cap, H, Hk, L = 3, 100000, 64, 32, 2             # queries and outputs 2.5 GB a layer, keys and values 1.2
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    mk = lambda *s: torch.randn(*s, generator=gen, device=DEV, dtype=torch.bfloat16)        # noqa: E731
+    q, k, v = mk(n, cap, H, DH), mk(n, cap, Hk, DH), mk(L, n, cap, Hk, DH)
+    out = torch.full((L, n, cap, H, DH), -7.0, dtype=torch.bfloat16, device=DEV)
+    lens = [1, 0, cap]
+    B.check(B.san_window_block(B.SAN_BF16, H, Hk, L, window, sink, q, k, v, torch.tensor(lens, dtype=torch.int32, device=DEV), n, cap, 0, out))
+    torch.cuda.synchronize()
+    assert (out[:, 1] == -7.0).all() and (out[:, 0, 1:] == -7.0).all()
+    begin = cap - window - 200                          # rows whose windows are within the copied part
+    part = torch.cat([torch.arange(sink), torch.arange(begin, cap)])
+    kk, vv = k[2, part].cpu().double(), v[:, 2, part].cpu().double()
+    for a in (cap - 1, cap - 2, cap - 64, cap - 200):
+        for h in (0, 31, 63):
+            pos = [i for i in range(len(part)) if part[i] <= a and (part[i] > a - window or part[i] < sink)]
+            assert len(pos) == window + sink
+            qq = q[2, a, h].cpu().double()
+            want, slack = attend(qq, kk[pos, h // 2], vv[:, pos, h // 2])
+            check_outputs(out[:, 2, a, h].cpu(), want, slack, weighted_size(qq, kk[pos, h // 2], vv[:, pos, h // 2]), torch.bfloat16, (a, h))
+
+
+def test_on_another_stream_behind_its_inputs():
+    lens, cap, H, window, sink = [300, 41], 300, 2, 90, 2
+    gen = torch.Generator().manual_seed(6)
+    q, k, v = (randn(gen, *s, cap, H, DH, dtype=torch.bfloat16) for s in ((2,), (2,), (1, 2)))
+    side = torch.cuda.Stream()
+    dq, dk, dv = (x.to(DEV) for x in (q, k, v))
+    out = torch.full((1, 2, cap, H, DH), -7.0, dtype=torch.bfloat16, device=DEV)
+    dl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):                       # the current stream is the one that is taken
+        B.check(B.san_window_block(B.SAN_BF16, H, H, 1, window, sink, dq, dk, dv, dl, 2, cap, 0, out))
+    side.synchronize()
+    _check(q, k, v, out.cpu(), lens, window, sink)
