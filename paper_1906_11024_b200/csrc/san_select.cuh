@@ -17,7 +17,7 @@
 //     x beam candidates, 1024 at a time, the best of every part first, until the parts' next ones cannot matter, and carries
 //     scores, lengths and token histories over.  It is launched with programmatic stream serialisation: its
 //     CTAs are in place, and the histories in shared memory, when the last logits arrive.
-//     Part after part in place of the best first took every pass: one sentence of 32 rows of 128000 float32 86 us, now 29.
+//     Part after part in place of the best first took every pass: one sentence of 32 rows of 128000 float32 86 us, 29 so (24 with the longer steps that it has now).
 //     Both in one launch, a sentence's CTAs as a cluster whose first CTA went on behind the cluster's barrier, was slower
 //     (device time: 4 rows of 32000 float32 10.3 us against 8.8, 256 of bf16 16.0 against 14.9, 512 of 128000 47.6 against 42.4).
 // Measured (device time of the whole call): 512 rows of 128000 bf16 logits 41.1 us, of which issue and exponentials fill
@@ -37,12 +37,14 @@ namespace san {
 
 constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
-// 32-bit words of logits per thread and step, and CTAs of the rows' kernels that an SM holds (their registers are limited for
-// that).  Measured, 8 words and 5 CTAs against 16 and 4: 740 rows of 50257 float32 59.3 us against 64.0, 512 rows of 128000
-// bf16 48.5 against 42.4 (before the merge took what it takes now).
-template <typename T> struct SelectGeom;
-template <> struct SelectGeom<float> { static constexpr int kWords = 8, kCtas = 5; };
-template <> struct SelectGeom<__nv_bfloat16> { static constexpr int kWords = 16, kCtas = 4; };
+// 32-bit words of logits per thread and step (W), and the CTAs of the rows' kernel that an SM holds with so many (registers are
+// limited for that).  Steps of 16 words are the faster ones but where one wave of CTAs with 8 takes rows that need two with 16.
+// Measured for float32, time with 8 words over time with 16, rows of 32000 to 50257 (beam 1): 200 rows 1.05 to 1.12,
+// 400 1.21 to 1.26, 592 1.08 to 1.12, 600 0.96 to 0.99, 740 0.92 to 0.94, 741 1.07 to 1.17, 888 1.09 to 1.23, 1184 1.13 to 1.15,
+// 1480 0.99 to 1.01, 2220 1.04 to 1.05; 740 rows of beam 20 47.3 us against 53.3.  bf16: 512 rows of 128000 48.5 us with 8 words, 42.4
+// with 16 (before the merge took what it takes now).
+constexpr int kSelWordsLong = 16, kSelWordsShort = 8;
+constexpr int select_ctas(int words) { return words == kSelWordsLong ? 4 : 5; }
 constexpr int kSelList = 1024;                 // keys that may reach the bound between two checks; more: one by one
 constexpr int kSelLong = 96;                   // list length at which the bound is raised
 constexpr int kSelTight = 64;                  // what the list is cut down to (equal logits aside)
@@ -178,10 +180,10 @@ template <typename T> __device__ __forceinline__ float as_f32(T x);
 template <> __device__ __forceinline__ float as_f32<float>(float x) { return x; }
 template <> __device__ __forceinline__ float as_f32<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// The logits of a thread in one step: kWords registers, eight logits at a time.
-template <typename T> struct SelectHeld;
-template <> struct SelectHeld<float> {
-    static constexpr int kWords = SelectGeom<float>::kWords, N = kWords;
+// The logits of a thread in one step: W registers, eight logits at a time.
+template <typename T, int W> struct SelectHeld;
+template <int W> struct SelectHeld<float, W> {
+    static constexpr int kWords = W, N = kWords;
     float x[kWords];
     __device__ __forceinline__ void set(int i, float v) { x[i] = v; }
     __device__ __forceinline__ void set16(int j, const uint4& v) {
@@ -206,8 +208,8 @@ template <> struct SelectHeld<float> {
         return t;
     }
 };
-template <> struct SelectHeld<__nv_bfloat16> {
-    static constexpr int kWords = SelectGeom<__nv_bfloat16>::kWords, N = 2 * kWords;
+template <int W> struct SelectHeld<__nv_bfloat16, W> {
+    static constexpr int kWords = W, N = 2 * kWords;
     uint32_t x[kWords];                                            // logit 2 i low, 2 i + 1 high
     __device__ __forceinline__ void set(int i, float v) {
         const uint32_t b = __float_as_uint(v) >> 16;                  // v is a bf16 number
@@ -290,10 +292,10 @@ __device__ __forceinline__ uint32_t tighten(Key64* list, int count, int n, uint3
 // grid = rows * chunks, then select_merge_kernel.  VECTOR: every row starts on a 16-byte boundary and a thread holds runs
 // of 16 bytes, else single logits 256 apart (one mapping for all rows of a call, so that equal rows get equal sums
 // whatever their addresses).
-template <typename T, bool VECTOR>
-__global__ void __launch_bounds__(kSelThreads, SelectGeom<T>::kCtas) select_rows_kernel(const SelectParams p) {
+template <typename T, bool VECTOR, int W>
+__global__ void __launch_bounds__(kSelThreads, select_ctas(W)) select_rows_kernel(const SelectParams p) {
     asm volatile("griddepcontrol.launch_dependents;");
-    using Held = SelectHeld<T>;
+    using Held = SelectHeld<T, W>;
     constexpr int N = Held::N, VEC = VECTOR ? 16 / (int)sizeof(T) : 1, STEP = N * kSelThreads;
     __shared__ Key64 s_list[kSelList];
     __shared__ Key64 s_slots[kSelWarps];
@@ -332,7 +334,7 @@ __global__ void __launch_bounds__(kSelThreads, SelectGeom<T>::kCtas) select_rows
             }
         }
     };
-    // Sum of e^(x - top): the terms of a step in float32 (8 or 32 of them, four partial sums), the steps in double, so that
+    // Sum of e^(x - top): the terms of a step in float32 (8 to 32 of them, four partial sums), the steps in double, so that
     // the additions' roundings do not grow with the row (in float32 throughout: 512 rows of 128000 bf16 logits off by up
     // to 7e-6, 592 of 2^20 by 5e-5, but 1.3 us less
     // for either measured case).  Terms are 2^(c x - M), c = fl(log2 e): the arguments are rounded once,

@@ -46,25 +46,24 @@ int32_t launch_after(void (*fn)(P), dim3 grid, unsigned block, cudaStream_t st, 
 }
 
 // ------------------------------------------------------------------------------- beam selection
-// Parts of a row, each of whole steps: the cut with the shortest estimate of (waves of CTAs, four or five per SM) x (steps of a part
-// + the 2.5 steps that the bound, the list and the hand-over of a part take).
-struct SelectCut { int chunks, steps; };
+// Steps of 8 words where that makes one wave of two (see san_select.cuh).  Parts of a row, each of whole steps: the cut with the
+// shortest estimate of (waves of CTAs) x (steps of a part + the 2.5 steps that the bound, the list and the hand-over of a part take).
+struct SelectCut { int words, chunks, steps; };
 constexpr int kSelectParts = 64;            // of a row at most
-long long select_most_parts(int vocab) {    // with the shorter steps of the two types
-    return std::min<long long>(kSelectParts, div_up(vocab, SelectGeom<float>::kWords * kSelThreads));
+long long select_most_parts(int vocab) {    // with the shortest steps
+    return std::min<long long>(kSelectParts, div_up(vocab, kSelWordsShort * kSelThreads));
 }
-static_assert(SelectGeom<float>::kWords <= 2 * SelectGeom<__nv_bfloat16>::kWords, "float32 steps are the shorter ones");
 SelectCut select_cut(int32_t dtype, long long rows, int vocab) {
-    const bool bf16 = dtype == SAN_BF16;
-    const int step = (bf16 ? 2 * SelectGeom<__nv_bfloat16>::kWords : SelectGeom<float>::kWords) * kSelThreads;
-    const int ctas = kSms * (bf16 ? SelectGeom<__nv_bfloat16>::kCtas : SelectGeom<float>::kCtas);
+    const bool f32 = dtype == SAN_F32;
+    const int words = f32 && rows > kSms * select_ctas(kSelWordsLong) && rows <= kSms * select_ctas(kSelWordsShort) ? kSelWordsShort : kSelWordsLong;
+    const int step = (f32 ? words : 2 * words) * kSelThreads, ctas = kSms * select_ctas(words);
     const long long all = div_up(vocab, step);
-    SelectCut best{1, (int)all};
+    SelectCut best{words, 1, (int)all};
     double least = 1e30;
     for (long long parts = 1; parts <= std::min<long long>(all, kSelectParts); ++parts) {
         const long long steps = div_up(all, parts), chunks = div_up(all, steps);
         const double cost = (double)std::max<long long>(1, div_up(rows * chunks, ctas)) * ((double)steps + 2.5);
-        if (cost < least) { least = cost; best = {(int)chunks, (int)steps}; }
+        if (cost < least) { least = cost; best = {words, (int)chunks, (int)steps}; }
     }
     return best;
 }
@@ -76,16 +75,16 @@ int32_t select_shape(int32_t n_sent, int32_t beam, int32_t vocab) {
     return SAN_OK;
 }
 
-template <typename T, bool VECTOR>
+template <typename T, bool VECTOR, int W>
 int32_t launch_select_as(const SelectParams& p, cudaStream_t st) {
     const unsigned grid = (unsigned)((long long)p.n_sent * p.beam * p.chunks);
-    select_rows_kernel<T, VECTOR><<<grid, kSelThreads, 0, st>>>(p);
+    select_rows_kernel<T, VECTOR, W><<<grid, kSelThreads, 0, st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
     return launch_after(&select_merge_kernel, dim3((unsigned)p.n_sent), kSelThreads, st, p);
 }
-template <typename T>
+template <typename T, int W>
 int32_t launch_select(const SelectParams& p, bool vector, cudaStream_t st) {
-    return vector ? launch_select_as<T, true>(p, st) : launch_select_as<T, false>(p, st);
+    return vector ? launch_select_as<T, true, W>(p, st) : launch_select_as<T, false, W>(p, st);
 }
 
 // ------------------------------------------------------------------------------- step attention
@@ -337,7 +336,8 @@ int32_t san_beam_select(const san_select_args* a, void* stream) {
     p.parent = a->d_parent; p.next = a->d_next; p.ws = static_cast<char*>(a->d_workspace); p.status = a->d_status;
     const bool vector = aligned(a->d_logits, 16) && a->ld_logits * (int64_t)e % 16 == 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return a->dtype == SAN_F32 ? launch_select<float>(p, vector, st) : launch_select<__nv_bfloat16>(p, vector, st);
+    if (a->dtype == SAN_BF16) return launch_select<__nv_bfloat16, kSelWordsLong>(p, vector, st);
+    return cut.words == kSelWordsShort ? launch_select<float, kSelWordsShort>(p, vector, st) : launch_select<float, kSelWordsLong>(p, vector, st);
 }
 
 int32_t san_cache_planes(const san_ctx* ctx, int32_t kind, int32_t block, void** d_k, void** d_v, int64_t* v_stride) {
