@@ -33,8 +33,13 @@
  *    only on the device (an id out of range, a length < 1 or beyond capacity) make the
  *    kernel skip that item and record the first such error in a device word, read back
  *    with san_device_status.
- *  - Element type is SAN_F32 or SAN_BF16 for q/k/v/x/outputs; S is always float32;
- *    products, sums and the softmax are float32.  d_head must be 64.
+ *  - Element type is SAN_F32 or SAN_BF16 for q/k/v/x/outputs; S, where it is given or taken, is
+ *    always float32; products, sums and the softmax are float32.  d_head must be 64.  Of bf16 inputs the
+ *    weights enter their product with the values in bf16 (at most half a step off, 2^-8 relative; their sum is that of
+ *    the float32 ones) in san_window_block, san_window_attn, san_prefix_attn, the 128-query tiles of
+ *    san_full_block and kernels 2 and 3 of san_decode_step (san_step_kernel_select): outputs are off by 1.2 to 1.4
+ *    times what their own rounding alone is.  The per-warp step kernel and the 64-query tiles of san_full_block
+ *    add what the rounding of a weight left as a second bf16 number.
  *  - Sequences are numbered 0 .. max_sent*beam-1; sequence s belongs to sentence
  *    s / beam (the beams of a sentence read the same encoder memory, Section 2).
  *
@@ -356,7 +361,7 @@ int32_t san_policy_search(const double* js, int32_t n_layers, double theta, int3
  * score -inf, parent = the slot itself, token eos (0 without eos) and the slot's old length and history.
  * Outputs may be the inputs' own buffers (d_tokens_out = d_tokens with the same ld_tokens, ...).
  * Scores are compared in double.  A row's sum of exponentials has float32 terms, added in float32 within
- * a thread's 8 (float32) or 32 (bf16) logits of a step and in double beyond: within 3e-6 relative at worst, whatever the vocabulary.
+ * a thread's 8 to 32 logits of a step and in double beyond: within 3e-6 relative at worst, whatever the vocabulary.
  * Rows that hold the same logits in another order, or all of them moved by a constant, may differ by that and then do
  * not tie; a row of one token (the others masked) offers it at the hypothesis' score, exactly.
  * A length outside 0..ld_tokens, ld_tokens itself where a token has to be added, or a length whose ((5 + length) / 6)^alpha
@@ -417,13 +422,15 @@ typedef struct {
     const int32_t* d_lens;    /* [n_prefix], 0..max_len */
     int32_t max_len;          /* host bound on d_lens (0 = cap_len) */
     const int32_t* d_first;   /* [n_prefix + 1], ascending */
-    int32_t max_group;        /* host bound on the items of a prefix (0 = n_items) */
+    int32_t max_group;        /* host bound on the items of a prefix (0 = n_items).  Kernels and cuts are chosen by it, so that a
+                                 close one is worth giving where there are several prefixes: results do not depend on it */
 } san_shared_prefix;
 
 /* One decode step of attention over a sliding window with sinks: with len = d_lens[i], row j is seen if
  *     j >= len - window   or   j < n_sink,
  *     S = Softmax(q . K^T / 8) over the rows seen,   O_l = sum_j S[j] V_l[j]   for every layer l.
- * Rows that are not seen are not read.  window >= 1, n_sink >= 0.  len = 0 gives zeros.  An id or length out
+ * Rows that are not seen are not read.  window >= 1, n_sink >= 0.  len = 0 gives zeros, and so does a row whose scores
+ * are all -infinity (here and in the two calls below).  An id or length out
  * of range leaves the item's output as it was and is reported. */
 int32_t san_window_attn_bytes(const san_cached_rows* rows, int32_t window, int32_t n_sink, size_t* workspace_bytes);
 int32_t san_window_attn(const san_cached_rows* rows, int32_t window, int32_t n_sink, void* d_workspace,

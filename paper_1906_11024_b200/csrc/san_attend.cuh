@@ -8,7 +8,7 @@
 //
 // The call is bound by reading keys and values once: (1 + layers) * 128 bytes per position and
 // key head (bf16) against 4 * 64 * (1 + layers) operations per query row.  What is laid out for that:
-//   * A UNIT is (key head, up to 16 query rows that share its keys, layer group, a run of positions).  For a
+//   * A UNIT is (key head, up to 8 query rows that share its keys, layer group, a run of positions).  For a
 //     sequence's own rows the query rows are the query heads of the key head's group; for a prefix they
 //     are those of every sequence behind the prefix, so that the prefix is read once for all of them.
 //   * A unit is streamed by 1 or 4 warps.  Each warp has a ring of slots of its own in shared memory (32 rows
@@ -177,8 +177,8 @@ __device__ __forceinline__ void attend_fill(const AttendRun& u, int begin, int e
 }
 
 // Where a unit's row goes, and the meeting of the warps of a unit.  Every warp of the CTA calls this (it
-// holds CTA barriers).  In shared memory: per warp [layers][kRows][64] outputs at `own`, (max, sum) per row at
-// `ml`; warps of a unit are neighbours.
+// holds CTA barriers).  In shared memory: per warp [layers][kAtRows] rows of 64 outputs, kAtOutLd floats
+// apart, at the start of its part, (max, sum) per row at `ml`; warps of a unit are neighbours.
 template <typename T, int N>
 __device__ __forceinline__ void attend_finish(const AttendParams& p, const AttendRun& u, bool active, int wpu, char* smem,
                                               const float2* ml, int warp, int lane) {

@@ -20,8 +20,11 @@
 //     Part after part in place of the best first took every pass: one sentence of 32 rows of 128000 float32 86 us, 29 so (24 with the longer steps that it has now).
 //     Both in one launch, a sentence's CTAs as a cluster whose first CTA went on behind the cluster's barrier, was slower
 //     (device time: 4 rows of 32000 float32 10.3 us against 8.8, 256 of bf16 16.0 against 14.9, 512 of 128000 47.6 against 42.4).
-// Measured (device time of the whole call): 512 rows of 128000 bf16 logits 41.1 us, of which issue and exponentials fill
-// half; 740 rows of 50257 float32 ones off 16-byte boundaries 47.1; 4 rows of 32000 7.6, the chain of one sentence.  The first
+// Measured (device time of the whole call): 512 rows of 128000 bf16 logits 41.2 us, issue slots and the
+// units of the exponentials half full each (ten thread instructions a logit, of which the sum and the maximum need some four; what the
+// others do has not been measured part by part); 740 rows of 50257 float32 ones off 16-byte boundaries 47.2 (twenty-two a logit:
+// single loads, short steps, more listing), of bf16 ones 59.8 (two-byte loads, 104 bytes of registers spilled); 4 rows of
+// 32000 7.6, the chain of one sentence.  The first
 // version, which sorted a key per thread and held 32 logits in float32, took 162, 133 and 12.3.  A ring of cp.async stages in
 // shared memory in place of the registers measured the same: loads are not what is waited for.
 // Where more candidates reach the bound than the list holds (rows that are alike nearly everywhere: a mask of

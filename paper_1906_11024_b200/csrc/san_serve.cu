@@ -434,8 +434,8 @@ int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int
     if ((long long)n_seq * p.n_lg > 65535) return SAN_ERR_SHAPE;
     if (use_tiles) {
         // A CTA takes a pair of tiles.  Where the last wave would hold less than half of the SMs' CTAs, its pairs are dealt as
-        // single tiles, which take about two thirds of a pair's time: 8192 positions x 16 sequences and heads are
-        // 3.35 waves of pairs, or three waves and 104 single tiles.
+        // single tiles, which take about two thirds of a pair's time: 7805 positions x 16 sequences and heads are 31 x 16 = 496
+        // pairs, 3.35 waves, or three waves of pairs and 104 single tiles.
         const long long pairs = div_up(max_len, 2 * kTileQ), all = pairs * n_heads * n_seq * p.n_lg, rest = all % kSms;
         if (2 * all > 0x7fffffffLL) return SAN_ERR_SHAPE;
         p.pairs = (int)pairs;

@@ -22,8 +22,8 @@
 // What bounds it: the softmax warps, one of each tile per SM quarter: 1800 clocks per chunk measured, of which the
 // exponentials of both tiles take 1170 (1024 at 16 per clock and SM), maxima 250, waiting for scores 220; the tensor cores
 // are busy for a third of it.  Tried on top and not faster: taking turns with the exponentials (1690 to 1880),
-// a quarter of them as polynomials on the FMA pipe (1770).  Two prompts of 8192 positions, window 1024, 8
-// heads, 2 layers: 111 us with one tile per CTA (two CTAs per SM) and weights in shared memory, whose writes, operand reads and
+// a quarter of them as polynomials on the FMA pipe (1770).  Two prompts of some 7800 positions, window 1024, 8
+// heads, 2 layers (97.7 us now): 111 us with one tile per CTA (two CTAs per SM) and weights in shared memory, whose writes, operand reads and
 // copies took 750 clocks of shared memory per chunk and tile; 117 us with 128-key chunks and one score buffer
 // per tile, where a tile's next scores waited for its outputs.
 // Every wait is bounded: one that runs out raises a flag that ends the CTA's other waits, the CTA frees its tensor
