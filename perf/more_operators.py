@@ -1,8 +1,8 @@
 """Measured cases of the calls for long prompts and a cache that is kept small.
 
   packed   san_packed_block: causal attention of whole prompts laid end to end, without padding, query heads in groups
-  store    san_q4_append, san_q4_read: rows into a cache of four bits a number, and back as numbers
-  attn     san_q4_attn: one decode step of attention over such a cache, with the weights where they are wanted
+  store    san_quant_append, san_quant_read: rows into a cache of four bits a number, and back as numbers
+  attn     san_quant_attn: one decode step of attention over such a cache, with the weights where they are wanted
   mass     san_weight_mass: what the cached rows have received of the weights so far
   evict    san_cache_evict: the rows that received most, the first and the last ones stay, in every layer of a block
 
@@ -245,17 +245,17 @@ def _plan(st):
         p = planes(st["codes"], B.SAN_Q4, st["scales"])
 
         def store():
-            rc = B.san_q4_append(p, code, st["k"], st["v"], st["ids"], st["pos"], None, n, case["rows"])
-            return rc or B.san_q4_read(p, code, st["k_back"], st["v_back"], st["ids"], st["pos"], None, n, case["rows"])
+            rc = B.san_quant_append(p, code, st["k"], st["v"], st["ids"], st["pos"], None, n, case["rows"])
+            return rc or B.san_quant_read(p, code, st["k_back"], st["v_back"], st["ids"], st["pos"], None, n, case["rows"])
         return store
     if op == "attn":
         p = planes(st["codes"], B.SAN_Q4, st["scales"])
         a = B.step_rows(dtype=code, n_heads=case["heads"], d_q=st["q"], d_ids=st["ids"], d_lens=st["lens"], n_items=n, max_len=st["max_len"],
                         d_S=st["S"], ld_s=st["max_len"], d_out=st["out"])
-        rc, b = B.san_q4_attn_bytes(p, a)
+        rc, b = B.san_quant_attn_bytes(p, a)
         B.check(rc)
         ws = room(b)
-        return lambda: B.san_q4_attn(p, a, ws, b)
+        return lambda: B.san_quant_attn(p, a, ws, b)
     if op == "mass":
         a = B.mass_args(n_heads=case["heads"], n_kv_heads=case["kv_heads"], d_S=st["S"], item_stride=st["strides"][0], row_stride=st["strides"][1],
                         head_stride=st["strides"][2], n_rows=case["rows"], d_rows=st["rows"], d_ids=st["ids"], d_lens=st["lens"], d_begin=st["begin"],
@@ -274,7 +274,7 @@ def _plan(st):
         rc = B.san_cache_evict(p, a, ws, b)
         if rc or not q4:
             return rc
-        return B.san_q4_read(p, B.SAN_F32, st["back"][0], st["back"][1:], st["ids"], st["back_pos"], st["back_rows"], n, case["keep"])
+        return B.san_quant_read(p, B.SAN_F32, st["back"][0], st["back"][1:], st["ids"], st["back_pos"], st["back_rows"], n, case["keep"])
     return evict
 
 
