@@ -81,7 +81,7 @@ enum {
     SAN_ERR_TIMEOUT = 9,      /* a kernel's bounded wait for its own copies ran out (see General rules) */
     SAN_ERR_UNSUPPORTED = 10
 };
-enum { SAN_F32 = 0, SAN_BF16 = 1 };
+enum { SAN_F32 = 0, SAN_BF16 = 1, SAN_Q4 = 2 }; /* SAN_Q4: cached rows in four bits, see san_planes; no call takes it elsewhere */
 enum { SAN_SELF = 0, SAN_ENCDEC = 1 };
 
 #define SAN_MAX_LAYERS 64
@@ -455,6 +455,124 @@ int32_t san_prefix_attn(const san_cached_rows* rows, const san_shared_prefix* pr
 int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int32_t n_layers, int32_t window,
                          int32_t n_sink, const void* d_q, const void* d_k, const void* d_v, const int32_t* d_lens,
                          int32_t n_seq, int32_t cap_len, int32_t max_len, void* d_out, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Long prompts, and a cache that is kept small: prompts without padding, cached rows in four bits a number, and the rows that
+ * receive least attention given up.  The rules of the calls above hold for these too: no context, nothing allocated, caller's
+ * workspaces (256-byte aligned, contents of no importance between calls, one for each call that may overlap another; sized by the *_bytes
+ * functions, and one sized for the largest batch serves smaller ones), optional d_status, all may be captured into a CUDA graph.  An id is named by one item of a call at most,
+ * except where rows are only read. */
+
+/* Causal attention of whole prompts laid end to end: sequence s is the tokens d_first[s] .. d_first[s+1]-1, and token a sees the
+ * tokens b <= a of its sequence,
+ *     S = Softmax(Q . K^T / 8) over those,   O_l = S . V_l   for every layer l of the block (Eq. 1 - 4).
+ * Query head h reads key head h / (n_heads / n_kv_heads).  Tokens may lie further apart than their numbers are long (q, k and v of
+ * one fused projection): ld_q, ld_k, ld_v are elements between tokens, multiples of 8.  Sequences may be empty.  Tokens that belong to no
+ * sequence keep their outputs as they were.  What a token does not see does not reach it, infinities and NaN included.
+ * SAN_BF16 only (SAN_F32: SAN_ERR_UNSUPPORTED, for the reason given for san_full_block).  A sequence that does not lie within the
+ * tokens or is longer than max_len is skipped and reported, and so is a tile of sequences that overlap in more tokens than there are. */
+typedef struct {
+    int32_t dtype, n_heads, n_kv_heads, n_layers;
+    const void* d_q; int64_t ld_q;        /* [n_tokens][n_heads][64], ld_q elements between tokens; 16-byte aligned as all of these */
+    const void* d_k; int64_t ld_k;        /* [n_tokens][n_kv_heads][64] */
+    const void* d_v; int64_t ld_v; int64_t v_stride;        /* [n_layers] of those, v_stride elements apart (a multiple of 8) */
+    const int32_t* d_first;               /* [n_seq + 1], ascending */
+    int32_t n_seq, n_tokens;
+    int32_t max_len;                      /* host bound on the lengths (0 = n_tokens); kernels are chosen by it */
+    void* d_out;                          /* [n_layers][n_tokens][n_heads][64] */
+    int32_t* d_status;                    /* optional */
+} san_packed_args;
+int32_t san_packed_block_bytes(const san_packed_args* args, size_t* workspace_bytes);
+int32_t san_packed_block(const san_packed_args* args, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Planes of cached rows of a block: its keys and each layer's values.
+ *   SAN_F32, SAN_BF16   [max_ids][n_kv_heads][cap_len][64], as a context keeps them (san_cache_planes)
+ *   SAN_Q4              codes [max_ids][n_kv_heads][cap_len][32 bytes] and scales [max_ids][n_kv_heads][cap_len][2] bf16, in the
+ *                       caller's own buffers: 36 bytes a row.  Dim d is in byte d / 2, even ones in its low half.  A row reads as
+ *                           low + step * n,   n its codes 0..15, (step, low) its scales.
+ * v_stride: elements between the layers' value planes, 64 a row in every format (a multiple of 64). */
+typedef struct {
+    int32_t dtype, n_kv_heads, n_layers;
+    void* d_k; void* d_v; int64_t v_stride;         /* 16-byte aligned */
+    void* d_k_scale; void* d_v_scale;               /* SAN_Q4 alone: [n_layers] of the latter, v_stride / 64 rows apart */
+    int32_t max_ids, cap_len;
+} san_planes;
+
+/* Rows into a cache of four bits, and back as numbers.  Item i's rows are n = d_nrows[i] (rows_per_item where d_nrows is NULL) from
+ * row d_pos[i] (0 where it is NULL) of id d_ids[i] on; the other side is in the order a projection writes it,
+ *     keys [n_items][rows_per_item][n_kv_heads][64],   values [n_layers][n_items][rows_per_item][n_kv_heads][64]   of `dtype`
+ * (SAN_F32 or SAN_BF16; rows beyond n are neither read nor written).
+ * Of a row x:  low = min x rounded down to bf16, step = (max x - low) / 15 rounded up to bf16, n = (x - low) / step rounded to the
+ * nearest, half to even (0 where step is 0), decided in 64 bits: no number is off by more than step / 2.  A row with an infinity or
+ * NaN, or whose low or step no bf16 number holds, reads as NaN.  san_quant_read rounds low + step * n to `dtype`.
+ * An id, a number of rows or a place out of range skips the item and is reported. */
+int32_t san_quant_append(const san_planes* cache, int32_t dtype, const void* d_k_new, const void* d_v_new, const int32_t* d_ids,
+                         const int32_t* d_pos, const int32_t* d_nrows, int32_t n_items, int32_t rows_per_item,
+                         int32_t* d_status, void* stream);
+int32_t san_quant_read(const san_planes* cache, int32_t dtype, void* d_k, void* d_v, const int32_t* d_ids, const int32_t* d_pos,
+                       const int32_t* d_nrows, int32_t n_items, int32_t rows_per_item, int32_t* d_status, void* stream);
+
+/* One decode step of attention over a cache of four bits: item i is one query position over the first d_lens[i] rows of id d_ids[i]
+ * (this step's row among them; several items may read one id),
+ *     S = Softmax(q . K^T / 8),   O_l = S . V_l   for every layer l of the block,
+ * K and V being what the rows read as.  len = 0 gives zeros, and so does a row whose scores are all -infinity; rows behind the length are not
+ * read.  A query row with an infinity or NaN gives NaN.  d_S, where it is given, receives the weights as san_attn_weights writes
+ * them (entries behind a row's length are left as they were): what san_weight_mass takes.
+ * float32 queries are answered in float32's accuracy: the cache's codes are whole numbers, nothing else is rounded. */
+typedef struct {
+    int32_t dtype, n_heads;               /* SAN_F32 or SAN_BF16; n_heads a multiple of the planes' n_kv_heads */
+    const void* d_q;                      /* [n_items][n_heads][64], 16-byte aligned */
+    const int32_t* d_ids; const int32_t* d_lens;
+    int32_t n_items;
+    int32_t max_len;                      /* host bound on d_lens (0 = cap_len) */
+    float* d_S; int64_t ld_s;             /* optional: [n_items][n_heads][ld_s], ld_s >= max_len */
+    void* d_out;                          /* [n_layers][n_items][n_heads][64], 16-byte aligned */
+    int32_t* d_status;                    /* optional */
+} san_step_rows;
+int32_t san_quant_attn_bytes(const san_planes* cache, const san_step_rows* rows, size_t* workspace_bytes);
+int32_t san_quant_attn(const san_planes* cache, const san_step_rows* rows, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* The mass of cached rows: what they have received of the weights.  For item i with len = d_lens[i], key head k and j < len
+ *     m[j] = (decay * m[j] where j < d_begin[i], else 0) + sum over r < rows and the query heads h of k of S[i][r][h][j],
+ * m = d_mass[d_ids[i]][k]; entries behind len are left as they were.  d_begin (0 .. len; NULL: len) is where rows begin that the mass does
+ * not know yet.  S is what any call of this library writes, by its strides in elements:
+ *     san_attn_weights, san_decode_step, san_quant_attn    item_stride H * ld_s, head_stride ld_s, n_rows 1
+ *     the same for encoder memory, rows = beam             item_stride beam * H * ld_s, row_stride H * ld_s, head_stride ld_s
+ *     san_full_block, rows = positions                     item_stride H * cap_len * ld_s, head_stride cap_len * ld_s, row_stride ld_s
+ * S[i][r][h][j] is read for j < len alone.  d_rows: rows of each item, 0 .. n_rows (NULL: n_rows).  Sums are float32, in an order that
+ * depends on n_rows alone.  An id, length, number of rows or begin out of range skips the item and is reported. */
+typedef struct {
+    int32_t n_heads, n_kv_heads;
+    const float* d_S; int64_t item_stride, row_stride, head_stride;
+    int32_t n_rows; const int32_t* d_rows;
+    const int32_t* d_ids; const int32_t* d_lens; const int32_t* d_begin;
+    int32_t n_items;                      /* at most 65535 */
+    int32_t max_len;                      /* host bound on d_lens */
+    float decay;                          /* finite */
+    float* d_mass; int64_t ld_mass;       /* [max_ids][n_kv_heads][ld_mass], ld_mass >= max_len */
+    int32_t max_ids;
+    int32_t* d_status;                    /* optional */
+} san_mass_args;
+int32_t san_weight_mass(const san_mass_args* args, void* stream);
+
+/* A cache cut back to its heaviest rows, in place.  Of an item with len = d_lens[i] > n_keep rows, each key head keeps n_keep: the
+ * first n_sink, the last n_recent, and of those between the ones of the largest mass (ties: the lowest row; NaN counts as -infinity).  They
+ * move to the front in their order, in the key plane, every layer's value plane and the mass; what lies behind them is left as it
+ * was.  Shorter items stay as they are.  d_lens_out[i] = min(len, n_keep) (may be d_lens).  d_kept, where it is given, receives
+ * the rows that were kept, min(len, n_keep) of them in ascending order.  Key heads choose for themselves, layers of a block share their
+ * weights and so the choice.  An id or length out of range skips the item (d_lens_out too) and is reported. */
+typedef struct {
+    const int32_t* d_ids; const int32_t* d_lens;
+    int32_t n_items;                      /* at most 65535 */
+    int32_t max_len;                      /* host bound on d_lens (0 = cap_len) */
+    int32_t n_keep, n_sink, n_recent;     /* n_keep >= 1, n_sink + n_recent <= n_keep <= 2^26 */
+    float* d_mass; int64_t ld_mass;       /* [max_ids][n_kv_heads][ld_mass], ld_mass >= max_len */
+    int32_t* d_kept; int64_t ld_kept;     /* optional: [n_items][n_kv_heads][ld_kept], ld_kept >= n_keep */
+    int32_t* d_lens_out;                  /* [n_items] */
+    int32_t* d_status;                    /* optional */
+} san_evict_args;
+int32_t san_cache_evict_bytes(const san_planes* cache, const san_evict_args* args, size_t* workspace_bytes);
+int32_t san_cache_evict(const san_planes* cache, const san_evict_args* args, void* d_workspace, size_t workspace_bytes, void* stream);
 
 /* Reads (and clears) the device error word: *first_error = SAN_OK or the first
  * device-check error since the last read; detail[0..3] (optional) = kernel tag, item,

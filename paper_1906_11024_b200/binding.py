@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(HERE, "libsan_b200.so")
 SAN_OK = 0
 SAN_ERR_NULL, SAN_ERR_SHAPE, SAN_ERR_POLICY, SAN_ERR_CAPACITY, SAN_ERR_DTYPE = 1, 2, 3, 4, 5
 SAN_ERR_RANGE, SAN_ERR_CUDA, SAN_ERR_DEVICE_CHECK, SAN_ERR_TIMEOUT, SAN_ERR_UNSUPPORTED = 6, 7, 8, 9, 10
-SAN_F32, SAN_BF16 = 0, 1
+SAN_F32, SAN_BF16, SAN_Q4 = 0, 1, 2
 SAN_SELF, SAN_ENCDEC = 0, 1
 SAN_MAX_LAYERS, SAN_MAX_BEAM = 64, 32
 
@@ -32,6 +32,8 @@ EXPORTS = (
     "san_decode_step_host", "san_step_kernel_select", "san_step_kernel_used", "san_full_block", "san_beam_reorder", "san_js_matrix", "san_block_similarity", "san_policy_search",
     "san_beam_select", "san_beam_select_bytes", "san_cache_planes", "san_window_attn", "san_window_attn_bytes",
     "san_prefix_attn", "san_prefix_attn_bytes", "san_window_block",
+    "san_packed_block", "san_packed_block_bytes", "san_quant_append", "san_quant_read", "san_quant_attn", "san_quant_attn_bytes",
+    "san_weight_mass", "san_cache_evict", "san_cache_evict_bytes",
 )
 
 
@@ -79,6 +81,48 @@ class san_shared_prefix(C.Structure):
         ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("v_stride", C.c_int64), ("n_prefix", C.c_int32),
         ("cap_len", C.c_int32), ("d_lens", C.c_void_p), ("max_len", C.c_int32), ("d_first", C.c_void_p),
         ("max_group", C.c_int32),
+    ]
+
+
+class san_packed_args(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("n_layers", C.c_int32),
+        ("d_q", C.c_void_p), ("ld_q", C.c_int64), ("d_k", C.c_void_p), ("ld_k", C.c_int64),
+        ("d_v", C.c_void_p), ("ld_v", C.c_int64), ("v_stride", C.c_int64), ("d_first", C.c_void_p),
+        ("n_seq", C.c_int32), ("n_tokens", C.c_int32), ("max_len", C.c_int32), ("d_out", C.c_void_p), ("d_status", C.c_void_p),
+    ]
+
+
+class san_planes(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int32), ("n_kv_heads", C.c_int32), ("n_layers", C.c_int32),
+        ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("v_stride", C.c_int64), ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p),
+        ("max_ids", C.c_int32), ("cap_len", C.c_int32),
+    ]
+
+
+class san_step_rows(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int32), ("n_heads", C.c_int32), ("d_q", C.c_void_p), ("d_ids", C.c_void_p), ("d_lens", C.c_void_p),
+        ("n_items", C.c_int32), ("max_len", C.c_int32), ("d_S", C.c_void_p), ("ld_s", C.c_int64), ("d_out", C.c_void_p),
+        ("d_status", C.c_void_p),
+    ]
+
+
+class san_mass_args(C.Structure):
+    _fields_ = [
+        ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("d_S", C.c_void_p), ("item_stride", C.c_int64),
+        ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("n_rows", C.c_int32), ("d_rows", C.c_void_p),
+        ("d_ids", C.c_void_p), ("d_lens", C.c_void_p), ("d_begin", C.c_void_p), ("n_items", C.c_int32), ("max_len", C.c_int32),
+        ("decay", C.c_float), ("d_mass", C.c_void_p), ("ld_mass", C.c_int64), ("max_ids", C.c_int32), ("d_status", C.c_void_p),
+    ]
+
+
+class san_evict_args(C.Structure):
+    _fields_ = [
+        ("d_ids", C.c_void_p), ("d_lens", C.c_void_p), ("n_items", C.c_int32), ("max_len", C.c_int32), ("n_keep", C.c_int32),
+        ("n_sink", C.c_int32), ("n_recent", C.c_int32), ("d_mass", C.c_void_p), ("ld_mass", C.c_int64), ("d_kept", C.c_void_p),
+        ("ld_kept", C.c_int64), ("d_lens_out", C.c_void_p), ("d_status", C.c_void_p),
     ]
 
 
@@ -133,6 +177,16 @@ def lib():
     L.san_prefix_attn_bytes.argtypes = [rows, pre, C.POINTER(sz)]
     L.san_prefix_attn.argtypes = [rows, pre, vp, sz, vp]
     L.san_window_block.argtypes = [i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, i32, i32, i32, vp, vp]
+    L.san_packed_block_bytes.argtypes = [C.POINTER(san_packed_args), C.POINTER(sz)]
+    L.san_packed_block.argtypes = [C.POINTER(san_packed_args), vp, sz, vp]
+    planes = C.POINTER(san_planes)
+    L.san_quant_append.argtypes = [planes, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp]
+    L.san_quant_read.argtypes = [planes, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp]
+    L.san_quant_attn_bytes.argtypes = [planes, C.POINTER(san_step_rows), C.POINTER(sz)]
+    L.san_quant_attn.argtypes = [planes, C.POINTER(san_step_rows), vp, sz, vp]
+    L.san_weight_mass.argtypes = [C.POINTER(san_mass_args), vp]
+    L.san_cache_evict_bytes.argtypes = [planes, C.POINTER(san_evict_args), C.POINTER(sz)]
+    L.san_cache_evict.argtypes = [planes, C.POINTER(san_evict_args), vp, sz, vp]
     L.san_status_string.argtypes = [i32]
     L.san_status_string.restype = C.c_char_p
     for name in EXPORTS:
@@ -421,3 +475,82 @@ def san_window_block(dtype, n_heads, n_kv_heads, n_layers, window, n_sink, d_q, 
     """Causal attention of whole sequences over a sliding window and their first rows."""
     return lib().san_window_block(dtype, n_heads, n_kv_heads, n_layers, window, n_sink, _ptr(d_q), _ptr(d_k), _ptr(d_v),
                                   _ptr(d_lens), n_seq, cap_len, max_len, _ptr(d_out), _stream(stream))
+
+
+def packed_args(**kw) -> san_packed_args:
+    """A san_packed_args block; the caller keeps the tensors alive for as long as it is used (as for all blocks here)."""
+    return _struct(san_packed_args, kw)
+
+
+def planes(**kw) -> san_planes:
+    """A san_planes block (cached rows of a block of layers)."""
+    return _struct(san_planes, kw)
+
+
+def step_rows(**kw) -> san_step_rows:
+    """A san_step_rows block (query rows of a step)."""
+    return _struct(san_step_rows, kw)
+
+
+def mass_args(**kw) -> san_mass_args:
+    """A san_mass_args block."""
+    return _struct(san_mass_args, kw)
+
+
+def evict_args(**kw) -> san_evict_args:
+    """A san_evict_args block."""
+    return _struct(san_evict_args, kw)
+
+
+def san_packed_block_bytes(args: san_packed_args):
+    """Returns (status, workspace bytes)."""
+    n = C.c_size_t(0)
+    rc = lib().san_packed_block_bytes(C.byref(args), C.byref(n))
+    return rc, n.value
+
+
+def san_packed_block(args: san_packed_args, d_workspace, workspace_bytes, stream=None) -> int:
+    """Causal attention of prompts laid end to end."""
+    return lib().san_packed_block(C.byref(args), _ptr(d_workspace), workspace_bytes, _stream(stream))
+
+
+def san_quant_append(cache: san_planes, dtype, d_k_new, d_v_new, d_ids, d_pos, d_nrows, n_items, rows_per_item, d_status=None,
+                     stream=None) -> int:
+    """Rows into a cache of four bits a number."""
+    return lib().san_quant_append(C.byref(cache), dtype, _ptr(d_k_new), _ptr(d_v_new), _ptr(d_ids), _ptr(d_pos), _ptr(d_nrows),
+                                  n_items, rows_per_item, _ptr(d_status), _stream(stream))
+
+
+def san_quant_read(cache: san_planes, dtype, d_k, d_v, d_ids, d_pos, d_nrows, n_items, rows_per_item, d_status=None, stream=None) -> int:
+    """Rows of a cache of four bits as the numbers that they stand for."""
+    return lib().san_quant_read(C.byref(cache), dtype, _ptr(d_k), _ptr(d_v), _ptr(d_ids), _ptr(d_pos), _ptr(d_nrows),
+                                n_items, rows_per_item, _ptr(d_status), _stream(stream))
+
+
+def san_quant_attn_bytes(cache: san_planes, rows: san_step_rows):
+    """Returns (status, workspace bytes)."""
+    n = C.c_size_t(0)
+    rc = lib().san_quant_attn_bytes(C.byref(cache), C.byref(rows), C.byref(n))
+    return rc, n.value
+
+
+def san_quant_attn(cache: san_planes, rows: san_step_rows, d_workspace, workspace_bytes, stream=None) -> int:
+    """One decode step of attention over a cache of four bits."""
+    return lib().san_quant_attn(C.byref(cache), C.byref(rows), _ptr(d_workspace), workspace_bytes, _stream(stream))
+
+
+def san_weight_mass(args: san_mass_args, stream=None) -> int:
+    """Adds weights to the mass of the cached rows that received them."""
+    return lib().san_weight_mass(C.byref(args), _stream(stream))
+
+
+def san_cache_evict_bytes(cache: san_planes, args: san_evict_args):
+    """Returns (status, workspace bytes)."""
+    n = C.c_size_t(0)
+    rc = lib().san_cache_evict_bytes(C.byref(cache), C.byref(args), C.byref(n))
+    return rc, n.value
+
+
+def san_cache_evict(cache: san_planes, args: san_evict_args, d_workspace, workspace_bytes, stream=None) -> int:
+    """Keeps the sinks, the newest and the heaviest rows of a cache, in place."""
+    return lib().san_cache_evict(C.byref(cache), C.byref(args), _ptr(d_workspace), workspace_bytes, _stream(stream))

@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsan_b200.so")
-SOURCES = ["san_api.cu", "san_static.cu", "san_serve.cu", "san_policy.cpp"]
+SOURCES = ["san_api.cu", "san_static.cu", "san_serve.cu", "san_quant.cu", "san_policy.cpp"]
 
 
 def _inputs():

@@ -1,12 +1,8 @@
 // Host side of the calls around the decode step of a beam decoder with long prompts: beam selection,
 // step attention behind shared prefixes and over sliding windows, windowed prompts.  Argument checks
 // and how the work is cut; the arithmetic is in san_select.cuh, san_attend.cuh and san_window.cuh.
-#include <algorithm>
-#include <cmath>
-#include <cstring>
-
 #include "san_ctx.h"
-#include "san_kernels.cuh"
+#include "san_launch.cuh"
 #include "san_select.cuh"
 #include "san_attend.cuh"
 #include "san_window.cuh"
@@ -15,35 +11,6 @@
 using namespace san;
 
 namespace {
-
-constexpr int kSms = 148;                   // the cuts are made for this GPU; any other number of SMs works
-inline long long div_up(long long a, long long b) { return (a + b - 1) / b; }
-inline int32_t cuda_status(cudaError_t e) { return e == cudaSuccess ? SAN_OK : SAN_ERR_CUDA; }
-inline bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-
-// Opt-in to dynamic shared memory above 48 KB, an attribute of a kernel on a device: done once for each (`set`, one
-// entry per device, belongs to the kernel).
-int32_t opt_in(const void* fn, int bytes, bool* set) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return SAN_ERR_CUDA;
-    if (dev >= 0 && dev < 64 && set[dev]) return SAN_OK;
-    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return SAN_ERR_CUDA;
-    if (dev >= 0 && dev < 64) set[dev] = true;
-    return SAN_OK;
-}
-
-// Launches `fn` so that its CTAs may be set up while the kernel before it on the stream still runs
-// (it waits with griddepcontrol.wait before it reads what that one wrote).
-template <typename P>
-int32_t launch_after(void (*fn)(P), dim3 grid, unsigned block, cudaStream_t st, const P& p, size_t smem = 0) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid; cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = st;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr; cfg.numAttrs = 1;
-    return cuda_status(cudaLaunchKernelEx(&cfg, fn, p));
-}
 
 // ------------------------------------------------------------------------------- beam selection
 // Steps of 8 words where that makes one wave of two (see san_select.cuh).  Parts of a row, each of whole steps: the cut with the
@@ -107,28 +74,7 @@ int32_t check_prefix(const san_cached_rows* r, const san_shared_prefix* x) {
     return SAN_OK;
 }
 
-constexpr int kOwnLeast = 4;                // tiles of own rows that are not cut
-// How one kind of units (`units` runs of up to `tiles` tiles) is cut where a warp's share of the whole call is
-// `share` tiles: warps per unit and runs of tiles.  A run of no more than 1.25 shares (or `least` tiles) is one warp's.  A longer
-// one is cut into up to four runs for a warp each, so that the warps finish together; beyond that the four
-// warps of a CTA take a run together, which leaves a quarter of the partial results.  Measured (device time): 32 prefixes of 16
-// tiles beside 1024 rows of up to 8, share 10: 48.6 us uncut, 35.9 in two runs each; 1024 runs of 17 tiles, share 15: 53.4 us
-// uncut, 58.7 by four warps each; 8 runs of 513 tiles: 13.0 us by four warps, 17.7 by one.
-// `least`: tiles below which a cut costs more than it gives (a float32 tile of eight rows is several bf16 ones' work).
-void cut_runs(int tiles, double share, int least, int* wpu, int* splits, int* span) {
-    const int most = std::max(least, (int)std::ceil(1.25 * share));
-    const int pieces = (int)div_up(tiles, most);
-    *wpu = pieces > 4 ? kAtWarps : 1;
-    *splits = pieces > 4 ? (int)div_up(pieces, kAtWarps) : pieces;
-    *span = (int)div_up(tiles, *splits);
-    *splits = (int)div_up(tiles, *span);
-}
-
 struct AttendPlan { AttendParams p; size_t ml_bytes, bytes; long long ctas, tiles, tiles_own; };
-
-// Workspace of `rows` partial results: (max, sum) and the layers' outputs of each.
-size_t partial_ml_bytes(size_t rows) { return (rows * sizeof(float2) + 255) / 256 * 256; }
-size_t partial_bytes(size_t rows, int layers) { return partial_ml_bytes(rows) + rows * layers * kDh * sizeof(float); }
 
 // Everything but the addresses.  Rows are cut into no more runs than find room in `room` bytes of workspace (a prefix's result and
 // its row's own one always stay two): a workspace made for a larger batch, which needs fewer runs, serves a smaller one.
@@ -291,10 +237,35 @@ int32_t run_attend(const san_cached_rows* r, const san_shared_prefix* x, int win
     return r->dtype == SAN_BF16 ? launch_attend<__nv_bfloat16>(a, st) : launch_attend<float>(a, st);
 }
 
-template <int LG>
-int32_t launch_window(const WindowParams& p, dim3 grid, cudaStream_t st) {
-    window_block_kernel<LG><<<grid, 128, 0, st>>>(p);
+template <int LG, bool PACKED>
+int32_t launch_window_as(const WindowParams& p, dim3 grid, cudaStream_t st) {
+    window_block_kernel<LG, PACKED><<<grid, 128, 0, st>>>(p);
     return cuda_status(cudaGetLastError());
+}
+template <bool PACKED>
+int32_t launch_window(const WindowParams& p, dim3 grid, cudaStream_t st) {
+    return p.lg == 1 ? launch_window_as<1, PACKED>(p, grid, st) : p.lg == 2 ? launch_window_as<2, PACKED>(p, grid, st) :
+           p.lg == 3 ? launch_window_as<3, PACKED>(p, grid, st) : launch_window_as<4, PACKED>(p, grid, st);
+}
+
+// ------------------------------------------------------------------------------- packed prompts
+struct PackedPlan { long long pairs, list; bool tiles; size_t bytes; };      // pairs of query tiles of all sequences at most; entries of their list
+
+int32_t plan_packed(const san_packed_args* a, PackedPlan* out) {
+    if (!a) return SAN_ERR_NULL;
+    if (a->dtype != SAN_BF16) return a->dtype == SAN_F32 ? SAN_ERR_UNSUPPORTED : SAN_ERR_DTYPE;
+    if (a->n_heads < 1 || a->n_heads > 65535 || a->n_kv_heads < 1 || a->n_heads % a->n_kv_heads != 0) return SAN_ERR_SHAPE;
+    if (a->n_layers < 1 || a->n_layers > SAN_MAX_LAYERS || a->n_seq < 0 || a->n_tokens < 0 || a->n_tokens > (1 << 28)) return SAN_ERR_SHAPE;
+    if (a->max_len < 0 || a->max_len > a->n_tokens) return SAN_ERR_SHAPE;
+    if (a->ld_q < (int64_t)a->n_heads * kDh || a->ld_k < (int64_t)a->n_kv_heads * kDh || a->ld_v < (int64_t)a->n_kv_heads * kDh) return SAN_ERR_SHAPE;
+    if (a->ld_q % 8 != 0 || a->ld_k % 8 != 0 || a->ld_v % 8 != 0) return SAN_ERR_SHAPE;
+    if (a->n_layers > 1 && (a->v_stride < 1 || a->v_stride % 8 != 0)) return SAN_ERR_SHAPE;
+    const int max_len = a->max_len ? a->max_len : a->n_tokens;
+    out->tiles = max_len >= kTileQ;
+    out->pairs = a->n_seq == 1 ? div_up(max_len, 2 * kTileQ) : a->n_tokens / (2 * kTileQ) + a->n_seq;
+    out->list = out->tiles && a->n_seq > 1 ? out->pairs : 0;
+    out->bytes = out->list ? (size_t)(1 + out->list) * sizeof(int2) : 0;
+    return SAN_OK;
 }
 
 }  // namespace
@@ -420,6 +391,7 @@ int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int
     p.v = static_cast<const __nv_bfloat16*>(d_v); p.out = static_cast<__nv_bfloat16*>(d_out);
     p.lens = d_lens; p.n_seq = n_seq; p.cap = cap_len; p.H = n_heads; p.Hk = n_kv_heads; p.group = n_heads / n_kv_heads;
     p.n_layers = n_layers; p.max_len = max_len; p.window = window; p.n_sink = n_sink;
+    p.q_ld = p.out_ld = n_heads * kDh; p.k_ld = p.v_ld = n_kv_heads * kDh;
     p.v_layer = (long long)n_seq * cap_len * n_kv_heads * kDh;
     p.out_layer = (long long)n_seq * cap_len * n_heads * kDh;
     // The tensor-core tiles take sequences of a tile and more, unless the rows that a CTA of window_block_kernel walks are
@@ -446,7 +418,59 @@ int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int
     }
     const dim3 grid((unsigned)div_up(max_len, kWinQ), (unsigned)n_heads, (unsigned)(n_seq * p.n_lg));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return p.lg == 1 ? launch_window<1>(p, grid, st) : p.lg == 2 ? launch_window<2>(p, grid, st) : p.lg == 3 ? launch_window<3>(p, grid, st) : launch_window<4>(p, grid, st);
+    return launch_window<false>(p, grid, st);
+}
+
+int32_t san_packed_block_bytes(const san_packed_args* a, size_t* workspace_bytes) {
+    if (!workspace_bytes) return SAN_ERR_NULL;
+    PackedPlan plan;
+    const int32_t rc = plan_packed(a, &plan);
+    if (rc == SAN_OK) *workspace_bytes = plan.bytes;
+    return rc;
+}
+
+int32_t san_packed_block(const san_packed_args* a, void* d_workspace, size_t workspace_bytes, void* stream) {
+    PackedPlan plan;
+    const int32_t rc = plan_packed(a, &plan);
+    if (rc != SAN_OK) return rc;
+    if (a->n_seq == 0 || a->n_tokens == 0) return SAN_OK;
+    if (!a->d_q || !a->d_k || !a->d_v || !a->d_first || !a->d_out) return SAN_ERR_NULL;
+    if (!aligned(a->d_q, 16) || !aligned(a->d_k, 16) || !aligned(a->d_v, 16) || !aligned(a->d_out, 16)) return SAN_ERR_SHAPE;
+    if (plan.bytes > 0) {
+        if (!d_workspace) return SAN_ERR_NULL;
+        if (!aligned(d_workspace, 256)) return SAN_ERR_SHAPE;
+        if (workspace_bytes < plan.bytes) return SAN_ERR_CAPACITY;
+    }
+    WindowParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.q = static_cast<const __nv_bfloat16*>(a->d_q); p.k = static_cast<const __nv_bfloat16*>(a->d_k);
+    p.v = static_cast<const __nv_bfloat16*>(a->d_v); p.out = static_cast<__nv_bfloat16*>(a->d_out);
+    p.first = a->d_first; p.n_seq = a->n_seq; p.n_tokens = a->n_tokens; p.status = a->d_status;
+    p.H = a->n_heads; p.Hk = a->n_kv_heads; p.group = a->n_heads / a->n_kv_heads; p.n_layers = a->n_layers;
+    p.max_len = a->max_len ? a->max_len : a->n_tokens;
+    p.window = p.max_len;                       // all of them; no sinks
+    p.q_ld = a->ld_q; p.k_ld = a->ld_k; p.v_ld = a->ld_v; p.out_ld = (long long)a->n_heads * kDh;
+    p.v_layer = a->v_stride; p.out_layer = (long long)a->n_tokens * p.out_ld;
+    const int at_once = plan.tiles ? kTileMaxLayers : 4;
+    p.n_lg = (int)div_up(a->n_layers, at_once);
+    p.lg = (int)div_up(a->n_layers, p.n_lg);
+    p.n_lg = (int)div_up(a->n_layers, p.lg);
+    p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)kDh));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!plan.tiles) {
+        if ((long long)a->n_seq * p.n_lg > 65535) return SAN_ERR_SHAPE;
+        return launch_window<true>(p, dim3((unsigned)div_up(p.max_len, kWinQ), (unsigned)a->n_heads, (unsigned)(a->n_seq * p.n_lg)), st);
+    }
+    const long long ctas = plan.pairs * a->n_heads * p.n_lg;
+    if (ctas > 0x7fffffffLL) return SAN_ERR_SHAPE;
+    p.pairs = (int)plan.pairs;
+    if (plan.list > 0) {
+        p.list = static_cast<const int2*>(d_workspace);
+        packed_list_kernel<<<1, 1024, 0, st>>>(p, static_cast<int2*>(d_workspace));
+        if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
+    }
+    const dim3 grid((unsigned)ctas);
+    return p.lg == 1 ? launch_tiles<TilePacked, 1>(p, grid, st) : launch_tiles<TilePacked, 2>(p, grid, st);
 }
 
 }  // extern "C"

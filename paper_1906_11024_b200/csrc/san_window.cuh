@@ -27,24 +27,48 @@ struct WindowParams {
     int n_seq, cap, H, Hk, group, n_layers, lg, n_lg, max_len, window, n_sink;
     int pairs, whole;                       // tensor-core tiles: pairs of tiles of a sequence, CTAs that take a pair
     float scale_log2e;
+    // packed sequences (san_packed_block): sequence s is the tokens first[s] .. first[s + 1] - 1
+    const int* first; const int2* list;     // list: (sequence, pair of tiles) of every CTA, the longest first, behind their number
+    long long q_ld, k_ld, v_ld, out_ld;     // elements between tokens
+    int n_tokens;
+    int* status;
 };
 
 constexpr int kWinQ = 32, kWinTile = 64, kWinSlots = 4;
+constexpr int TAG_PACKED = 12;
+
+// First token of a sequence in the buffers, and its length.  Packed sequences that do not lie within the tokens and the bound
+// have none; `report` says so.
+template <bool PACKED>
+__device__ __forceinline__ long long window_sequence(const WindowParams& p, int seq, int* len, bool report) {
+    if constexpr (!PACKED) {
+        *len = max(0, min(p.lens[seq], p.max_len));
+        return (long long)seq * p.cap;
+    } else {
+        const int a = p.first[seq], b = p.first[seq + 1];
+        const bool ok = a >= 0 && b >= a && b <= p.n_tokens && b - a <= p.max_len;
+        if (!ok && report && p.status) {
+            const bool order = a < 0 || b < a || b > p.n_tokens;
+            record_error(p.status, TAG_PACKED, seq, order ? b : b - a, order ? p.n_tokens : p.max_len);
+        }
+        *len = ok ? b - a : 0;
+        return a;
+    }
+}
 
 // Row a of (sequence, head), one layer, by one warp: the definition, over the rows that are seen.  Leaves as soon as the
 // row is known to be NaN, so that inputs full of NaN cost next to nothing.
-__device__ __noinline__ void window_row_again(const WindowParams& p, int seq, int head, int layer, int a, int lane) {
-    const long long kv = ((long long)seq * p.cap * p.Hk + head / p.group) * kDh + lane * 2;
-    const long long at = (((long long)seq * p.cap + a) * p.H + head) * kDh + lane * 2;
-    const long long step = (long long)p.Hk * kDh;
+__device__ __noinline__ void window_row_again(const WindowParams& p, long long token0, int head, int layer, int a, int lane) {
+    const long long k0 = token0 * p.k_ld + head / p.group * kDh + lane * 2, v0 = token0 * p.v_ld + head / p.group * kDh + lane * 2;
+    const long long to = (token0 + a) * p.out_ld + head * kDh + lane * 2;
     auto two = [](const __nv_bfloat16* x) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(x)); };
-    const float2 q = two(p.q + at);
+    const float2 q = two(p.q + (token0 + a) * p.q_ld + head * kDh + lane * 2);
     const int lo = max(0, a - p.window + 1), ns = min(p.n_sink, lo), n = ns + a + 1 - lo;
     float m = -INFINITY, l = 0.f, ox = 0.f, oy = 0.f;
     for (int pass = 0; pass < 2; ++pass)
         for (int i = 0; i < n; ++i) {
             const long long b = i < ns ? i : lo + i - ns;
-            const float2 k = two(p.k + kv + b * step);
+            const float2 k = two(p.k + k0 + b * p.k_ld);
             const float z = warp_sum(q.x * k.x + q.y * k.y) * p.scale_log2e;
             if (pass == 0) {
                 m = fmaxf(m, z);
@@ -55,35 +79,37 @@ __device__ __noinline__ void window_row_again(const WindowParams& p, int seq, in
             }
             const float w = exp2f(z - (m == -INFINITY ? 0.f : m));
             if (w == 0.f) continue;
-            const float2 v = two(p.v + layer * p.v_layer + kv + b * step);
+            const float2 v = two(p.v + layer * p.v_layer + v0 + b * p.v_ld);
             l += w;
             ox = fmaf(w, v.x, ox); oy = fmaf(w, v.y, oy);
             if (__all_sync(0xffffffffu, ox != ox && oy != oy)) break;        // it cannot become anything else
         }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    *reinterpret_cast<uint32_t*>(p.out + layer * p.out_layer + at) = pack_bf16(ox * inv, oy * inv);
+    *reinterpret_cast<uint32_t*>(p.out + layer * p.out_layer + to) = pack_bf16(ox * inv, oy * inv);
 }
 
-template <int LG>
+template <int LG, bool PACKED = false>
 __global__ void __launch_bounds__(128) window_block_kernel(const __grid_constant__ WindowParams p) {
     __shared__ __align__(128) char ring[kWinSlots * kWinTile * 128];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int head = blockIdx.y, seq = blockIdx.z / p.n_lg, layer0 = blockIdx.z % p.n_lg * p.lg;
     const int layers = min(p.lg, p.n_layers - layer0);
-    const int len = max(0, min(p.lens[seq], p.max_len));
+    int len;
+    const long long token0 = window_sequence<PACKED>(p, seq, &len, blockIdx.x == 0 && blockIdx.y == 0 && layer0 == 0 && threadIdx.x == 0);
     const int a0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kWinQ;        // the longest rows first
     if (a0 >= len) return;
     const int a1 = min(a0 + kWinQ, len);
     const int lo = max(0, a0 - p.window + 1), ns = min(p.n_sink, lo), n = ns + a1 - lo;
     const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(ring);
-    const char* kbase = reinterpret_cast<const char*>(p.k + ((long long)seq * p.cap * p.Hk + head / p.group) * kDh);
-    const char* vbase = reinterpret_cast<const char*>(p.v + layer0 * p.v_layer + ((long long)seq * p.cap * p.Hk + head / p.group) * kDh);
-    const long long row_bytes = (long long)p.Hk * 128;
+    const char* kbase = reinterpret_cast<const char*>(p.k + token0 * p.k_ld + head / p.group * kDh);
+    const char* vbase = reinterpret_cast<const char*>(p.v + layer0 * p.v_layer + token0 * p.v_ld + head / p.group * kDh);
+    const long long k_bytes = p.k_ld * 2, v_bytes = p.v_ld * 2;           // between rows
 
     int f_at = 0, f_plane = -1, f_slot = 0;
     auto fill = [&]() {
         if (f_at < n) {
             const char* src = f_plane < 0 ? kbase : vbase + f_plane * p.v_layer * 2;
+            const long long row_bytes = f_plane < 0 ? k_bytes : v_bytes;
             const uint32_t slot = ring_addr + f_slot * (kWinTile * 128);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -104,7 +130,7 @@ __global__ void __launch_bounds__(128) window_block_kernel(const __grid_constant
     uint32_t qb[4][2];                                                    // B: query g, dims 16 c + 2 t4 .. and 8 further on
     {
         const int a = qa0 + g;
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q + (((long long)seq * p.cap + a) * p.H + head) * kDh) + t4;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q + (token0 + a) * p.q_ld + head * kDh) + t4;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             qb[c][0] = a < a1 ? src[c * 8] : 0u;
@@ -248,7 +274,7 @@ __global__ void __launch_bounds__(128) window_block_kernel(const __grid_constant
         for (int k = 0; k < 2; ++k) {
             const int r = k * 4 + (lane >> 3), c = lane & 7, a = qa0 + r;
             if (a < a1)
-                *reinterpret_cast<uint4*>(p.out + (layer0 + y) * p.out_layer + (((long long)seq * p.cap + a) * p.H + head) * kDh + c * 8) =
+                *reinterpret_cast<uint4*>(p.out + (layer0 + y) * p.out_layer + (token0 + a) * p.out_ld + head * kDh + c * 8) =
                     *reinterpret_cast<const uint4*>(rows + r * 128 + ((c ^ r) << 4));
         }
         __syncwarp();
@@ -256,7 +282,7 @@ __global__ void __launch_bounds__(128) window_block_kernel(const __grid_constant
     for (int r = 0; r < 8; ++r) {
         const bool again = __any_sync(0xffffffffu, (2 * t4 == r && odd[0]) || (2 * t4 + 1 == r && odd[1]));
         if (again && qa0 + r < a1)
-            for (int y = 0; y < layers; ++y) window_row_again(p, seq, head, layer0 + y, qa0 + r, lane);
+            for (int y = 0; y < layers; ++y) window_row_again(p, token0, head, layer0 + y, qa0 + r, lane);
     }
 }
 
