@@ -502,9 +502,9 @@ typedef struct {
  * row d_pos[i] (0 where it is NULL) of id d_ids[i] on; the other side is in the order a projection writes it,
  *     keys [n_items][rows_per_item][n_kv_heads][64],   values [n_layers][n_items][rows_per_item][n_kv_heads][64]   of `dtype`
  * (SAN_F32 or SAN_BF16; rows beyond n are neither read nor written).
- * Of a row x:  low = min x rounded down to bf16, step = (max x - low) / 15 rounded up to bf16, n = (x - low) / step rounded to the
- * nearest, half to even (0 where step is 0), decided in 64 bits: no number is off by more than step / 2.  A row with an infinity or
- * NaN, or whose low or step no bf16 number holds, reads as NaN.  san_quant_read rounds low + step * n to `dtype`.
+ * Of a row x:  low = min x rounded down to bf16, step = (max x - low) / 15 rounded up to bf16 and, unless it is 0, to 2^-50 at least,
+ * n = (x - low) / step rounded to the nearest, half to even (0 where step is 0), decided in 64 bits: no number is off by more than
+ * step / 2.  A row with a NaN or a number of 2^40 or more reads as NaN.  san_quant_read rounds low + step * n to `dtype`.
  * An id, a number of rows or a place out of range skips the item and is reported. */
 int32_t san_quant_append(const san_planes* cache, int32_t dtype, const void* d_k_new, const void* d_v_new, const int32_t* d_ids,
                          const int32_t* d_pos, const int32_t* d_nrows, int32_t n_items, int32_t rows_per_item,
@@ -516,7 +516,7 @@ int32_t san_quant_read(const san_planes* cache, int32_t dtype, void* d_k, void* 
  * (this step's row among them; several items may read one id),
  *     S = Softmax(q . K^T / 8),   O_l = S . V_l   for every layer l of the block,
  * K and V being what the rows read as.  len = 0 gives zeros, and so does a row whose scores are all -infinity; rows behind the length are not
- * read.  A query row with an infinity or NaN gives NaN.  d_S, where it is given, receives the weights as san_attn_weights writes
+ * read.  A query row with a NaN or a number of 2^40 or more gives NaN; scales are such as san_quant_append writes.  d_S, where it is given, receives the weights as san_attn_weights writes
  * them (entries behind a row's length are left as they were): what san_weight_mass takes.
  * float32 queries are answered in float32's accuracy: the cache's codes are whole numbers, nothing else is rounded. */
 typedef struct {

@@ -4,13 +4,18 @@
 // A row of 64 numbers x is 32 bytes of codes n (dim d in byte d / 2, the even one in the low half) and a pair of bf16 numbers:
 //     low = min x, rounded down;   step = (max x - low) / 15, rounded up;   n = (x - low) / step, rounded half to even;
 // it reads as low + step n.  Rounded that way low and step cover the row, so that no number is off by more than step / 2.
+// A step is 0 or at least 2^-50; rows with a number of 2^40 or more are not held (they read as NaN, as rows with a NaN do).
 // Which code a number gets is decided as if in 64 bits: float32 where the quotient is clear of a border, doubles next to one.
 //
-// Attention.  Codes enter both products as whole numbers, which bf16 holds exactly, and a row's (step, low) is applied to its
-// score and to its weight, once for 64 numbers:
-//     q . x = step (q . n') + mid (sum of q),   sum_j S_j x_j = sum_j (S_j step_j) n'_j + sum_j S_j mid_j,
-// with n' = n - 8 and mid = low + 8 step.  So a product loses nothing to the cache's format, and float32 queries (three bf16 numbers
-// that add up to them, weights likewise) keep float32's accuracy on the tensor cores.
+// Attention.  A row is read once and its 64 codes cost five instructions per eight, because they enter the products as they lie: as
+// a bf16 number the bits 0-3 alone are n 2^-133 and the bits 4-7 alone 16 n 2^-133, exactly (subnormals and the binade above them have
+// one distance), so that one shift and four ANDs make four operands of two numbers.  The other operand brings the magnitude back: queries
+// are scaled to some 2^60 by a power of two of each row, weights are taken as 2^60 p.  A row's (step, low) is applied
+// to its score and its weight, once for 64 numbers:
+//     q . x = step (q . n) + low (sum of q),   sum_j p_j x_j = sum_j (p_j step_j) (n_j - 8) + sum_j p_j (low_j + 8 step_j),
+// the n - 8 by products with a constant -8, so that sums stay near zero, where an accumulator that cuts off does not drift.
+// So nothing is rounded for the cache's sake: bf16 rows round p, then p step to bf16; float32 rows take queries and weights as three
+// bf16 numbers that add up to them and keep float32's accuracy on the tensor cores.
 #pragma once
 
 #include <type_traits>
@@ -23,6 +28,8 @@ constexpr int TAG_QUANT = 13, TAG_QUANT_ROWS = 14;
 constexpr int kQuantRow = 32;               // bytes of codes of a row
 constexpr int kQuantTile = 64;              // positions per slot: 2 KB of codes, then their (step, low)
 constexpr int kQuantSlot = kQuantTile * (kQuantRow + 4);
+constexpr float kQuantMost = 1.0995116e12f;             // 2^40
+constexpr float kQuantLeastStep = 8.8817842e-16f;       // 2^-50
 
 // ------------------------------------------------------------------------------------------- rows in and out
 struct QuantRowsParams {
@@ -86,7 +93,7 @@ __global__ void __launch_bounds__(256) quant_append_kernel(const __grid_constant
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]);
-        finite &= fabsf(x[i]) <= 3.4028234e38f;
+        finite &= fabsf(x[i]) < kQuantMost;
     }
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) {
@@ -95,21 +102,18 @@ __global__ void __launch_bounds__(256) quant_append_kernel(const __grid_constant
     }
     const float low = bf16_down(lo);
     const double wide = ((double)hi - (double)low) / 15.0;
-    const float step = bf16_up_positive(__double2float_ru(wide));
+    const float step = wide > 0.0 ? fmaxf(bf16_up_positive(__double2float_ru(wide)), kQuantLeastStep) : 0.f;
     const unsigned group = 0xffu << (threadIdx.x & 24);
-    finite = (__ballot_sync(0xffffffffu, finite) & group) == group && fabsf(low) <= 3.4028234e38f && step <= 3.4028234e38f;
+    finite = (__ballot_sync(0xffffffffu, finite) & group) == group;
     uint32_t codes = 0;
-    // Steps without a reciprocal: everything times 2^100, which is exact (and low is that small too, since float32 numbers have no
-    // closer neighbours elsewhere).  A step of zero: codes of zero.
-    const float up = step > 1e-30f ? 1.f : 1.2676506e30f;
-    const float step1 = step * up, low1 = low * up, inv = step > 0.f ? 1.f / step1 : 0.f;
+    const float inv = step > 0.f ? 1.f / step : 0.f;        // a step of zero: codes of zero
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float x1 = x[i] * up, t = (x1 - low1) * inv;
+        const float t = (x[i] - low) * inv;
         float n = rintf(t);
         if (fabsf(fabsf(t - n) - 0.5f) < 1e-4f) {           // t is within 2e-6 of the quotient; next to a border 64 bits decide
             const float k = floorf(t);
-            const double d = (double)x1 - (double)low1, border = ((double)k + 0.5) * (double)step1;
+            const double d = (double)x[i] - (double)low, border = ((double)k + 0.5) * (double)step;
             n = d > border || (d == border && ((int)k & 1)) ? k + 1.f : k;
         }
         codes |= (uint32_t)fminf(fmaxf(n, 0.f), 15.f) << (4 * i);
@@ -169,21 +173,27 @@ __device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool full) {
 // Fills one slot with positions [begin, begin + 64) of layer `plane` (-1: keys); what lies at or behind `end` becomes zeros.
 // Value rows go to places where four lanes find rows 2 t of a block of eight in different banks: row r of eight to r / 2 + 4 (r % 2).
 __device__ __forceinline__ void quant_fill(const QuantRun& u, int begin, int end, int plane, uint32_t slot, int lane) {
-    const char* codes = plane < 0 ? u.r.k : u.r.v + plane * u.r.v_stride;
-    const char* scales = plane < 0 ? u.ks : u.vs + plane * u.s_stride;
-    const int half = lane & 1;
+    const char* codes = (plane < 0 ? u.r.k : u.r.v + plane * u.r.v_stride) + (long long)begin * kQuantRow + lane * 16;
+    const char* scales = (plane < 0 ? u.ks : u.vs + plane * u.s_stride) + (long long)begin * 4 + lane * 4;
+    const int r = lane >> 1;
+    const uint32_t to = slot + (plane < 0 ? lane * 16 : ((r & 8) | (r >> 1 & 3) | (r & 1) << 2) * kQuantRow + (lane & 1) * 16);
+    const uint32_t to_scale = slot + kQuantTile * kQuantRow + lane * 4;
+    if (begin + kQuantTile <= end) {
 #pragma unroll
-    for (int j = 0; j < kQuantTile / 16; ++j) {
-        const int r = j * 16 + (lane >> 1), pos = begin + r;
-        const int to = plane < 0 ? r : (r & ~7) | (r >> 1 & 3) | (r & 1) << 2;
-        const bool full = pos < end;
-        cp16(slot + to * kQuantRow + half * 16, codes + (long long)(full ? pos : 0) * kQuantRow + half * 16, full);
-    }
+        for (int j = 0; j < kQuantTile / 16; ++j) cp16(to + j * 16 * kQuantRow, codes + j * 16 * kQuantRow, true);
 #pragma unroll
-    for (int j = 0; j < kQuantTile / 32; ++j) {
-        const int r = j * 32 + lane, pos = begin + r;
-        const bool full = pos < end;
-        cp4(slot + kQuantTile * kQuantRow + r * 4, scales + (long long)(full ? pos : 0) * 4, full);
+        for (int j = 0; j < kQuantTile / 32; ++j) cp4(to_scale + j * 128, scales + j * 128, true);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kQuantTile / 16; ++j) {
+            const bool full = begin + j * 16 + r < end;
+            cp16(to + j * 16 * kQuantRow, full ? codes + j * 16 * kQuantRow : codes, full);
+        }
+#pragma unroll
+        for (int j = 0; j < kQuantTile / 32; ++j) {
+            const bool full = begin + j * 32 + lane < end;
+            cp4(to_scale + j * 128, full ? scales + j * 128 : scales, full);
+        }
     }
     cp_commit();
 }
@@ -214,18 +224,28 @@ template <int N> struct QuantRing {
     }
 };
 
-// Codes i and i + 4 of a word, less 8, as two bf16 numbers: 0x4300 | n is 128 + n.
-__device__ __forceinline__ uint32_t quant_two(uint32_t w, int i) {
-    const uint32_t x = (w >> (4 * i) & 0x000f000fu) | 0x43004300u;
-    uint32_t y;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(x), "r"(0x43084308u));
-    return y;
+// Four operands of two codes each from a word: bits 0-3, 4-7 (16 times as large), 8-11, 12-15 (16 times) of both halves.
+__device__ __forceinline__ void quant_four(uint32_t w, uint32_t* out) {
+    const uint32_t v = w >> 8;
+    out[0] = w & 0x000f000fu; out[1] = w & 0x00f000f0u;
+    out[2] = v & 0x000f000fu; out[3] = v & 0x00f000f0u;
+}
+__device__ __forceinline__ void quant_mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1, const float* c) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t x, uint32_t y) {
+    uint32_t z;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(z) : "r"(x), "r"(y));
+    return z;
 }
 // x as P bf16 numbers that add up to it (P = 1: its rounding).
 template <int P> __device__ __forceinline__ void quant_split(float x, float y, uint32_t* out) {
 #pragma unroll
     for (int k = 0; k < P; ++k) {
         out[k] = pack_bf16(x, y);
+        if (k + 1 == P) break;
         x -= __uint_as_float(out[k] << 16);
         y -= __uint_as_float(out[k] & 0xffff0000u);
     }
@@ -238,9 +258,9 @@ __device__ __forceinline__ void attend_warp_quant(const QuantParams& p, const Qu
     const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(smem);
     QuantRing<N> ring(u, ring_addr, lane, first, step);
     const int g = lane >> 2, t4 = lane & 3;
-    // B: query g, dims 16 t4 .. 16 t4 + 15 in the order of the codes' unpacking
+    // B: query g, dims 16 t4 .. 16 t4 + 15 in the order of the codes' unpacking, scaled to at most 2^60 and odd ones of a byte by another 1 / 16
     uint32_t qb[8][P];
-    float qs[2];                                             // sum of queries 2 t4 and 2 t4 + 1, times the scores' scale
+    float qs[2], unit[2];                                    // of queries 2 t4 and 2 t4 + 1: their sum times the scores' scale; what undoes the scaling, times it
     {
         const bool real = g < u.r.rows;
         const int head = u.r.head0 + u.r.row0 + (real ? g : 0);
@@ -259,19 +279,36 @@ __device__ __forceinline__ void attend_warp_quant(const QuantParams& p, const Qu
                 for (int i = 0; i < 4; ++i) unpack16<float>(src[i], q + 4 * i);
             }
         }
-        float sum = 0.f;
+        float sum = 0.f, most = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum = fabsf(q[i]) <= 3.4028234e38f ? sum + q[i] : NAN;
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        for (int i = 0; i < 16; ++i) {
+            sum = fabsf(q[i]) < kQuantMost ? sum + q[i] : NAN;           // a row with such a number gives NaN
+            most = fmaxf(most, fabsf(q[i]));
+        }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) qs[j] = __shfl_sync(0xffffffffu, sum, 4 * (2 * t4 + j)) * p.a.scale_log2e;
+        for (int o = 1; o < 4; o <<= 1) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        }
+        // most = 2^e (1 + ..), e within -60 .. 40: times 2^(59 - e)
+        const int e = max((int)(__float_as_uint(fminf(most, kQuantMost)) >> 23) - 127, -60);
+        const float up = __uint_as_float((uint32_t)(59 - e + 127) << 23);
+        const float down = __uint_as_float((uint32_t)(e + 74 + 127) << 23);      // 2^133 / up
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            qs[j] = __shfl_sync(0xffffffffu, sum, 4 * (2 * t4 + j)) * p.a.scale_log2e;
+            unit[j] = __shfl_sync(0xffffffffu, down, 4 * (2 * t4 + j)) * p.a.scale_log2e;
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) quant_split<P>(q[8 * h + i], q[8 * h + 4 + i], qb[4 * h + i]);
+            for (int i = 0; i < 4; ++i) {
+                const float f = i & 1 ? up * 0.0625f : up;
+                quant_split<P>(q[8 * h + i] * f, q[8 * h + 4 + i] * f, qb[4 * h + i]);
+            }
     }
-    float acc[LG][4][4], mids[LG][2];        // [layer][d]: dims 8 g + d and 8 g + 4 + d of queries 2 t4, 2 t4 + 1; sums of S mid over rows g
+    // [layer][d]: dims 8 g + d and 8 g + 4 + d of queries 2 t4, 2 t4 + 1 (odd d: 16 times), in units of 2^-73; sums of p mid in units of 2^60
+    float acc[LG][4][4], mids[LG][2];
 #pragma unroll
     for (int y = 0; y < LG; ++y) {
         mids[y][0] = mids[y][1] = 0.f;
@@ -282,36 +319,42 @@ __device__ __forceinline__ void attend_warp_quant(const QuantParams& p, const Qu
     }
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
     constexpr int kBlocks = kQuantTile / 16;
+    const float none[4] = {0.f, 0.f, 0.f, 0.f};
     for (int at = first; at < u.r.end; at += step) {
         const char* ks = smem + ring.next();
         float s[kBlocks][4];                                 // positions 16 n + g and + 8, queries 2 t4 and 2 t4 + 1
         float top[2] = {-INFINITY, -INFINITY};
-        const bool part = at + kQuantTile > u.r.end;
 #pragma unroll
         for (int n = 0; n < kBlocks; ++n) {
             const uint2 w0 = *reinterpret_cast<const uint2*>(ks + (n * 16 + g) * kQuantRow + t4 * 8);
             const uint2 w1 = *reinterpret_cast<const uint2*>(ks + (n * 16 + 8 + g) * kQuantRow + t4 * 8);
-            float dot[4] = {0.f, 0.f, 0.f, 0.f};
+            float dot[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint32_t x0 = c < 2 ? w0.x : w0.y, x1 = c < 2 ? w1.x : w1.y;
-                const int i = 2 * (c & 1), b = 4 * (c >> 1) + i;
-                const uint32_t a[4] = {quant_two(x0, i), quant_two(x1, i), quant_two(x0, i + 1), quant_two(x1, i + 1)};
+            for (int h = 0; h < 2; ++h) {
+                uint32_t x0[4], x1[4];
+                quant_four(h ? w0.y : w0.x, x0);
+                quant_four(h ? w1.y : w1.x, x1);
 #pragma unroll
-                for (int k = 0; k < P; ++k) mma_bf16(dot, a, qb[b][k], qb[b + 1][k]);
+                for (int c = 0; c < 2; ++c) {
+                    const uint32_t a[4] = {x0[2 * c], x1[2 * c], x0[2 * c + 1], x1[2 * c + 1]};
+#pragma unroll
+                    for (int k = 0; k < P; ++k) quant_mma(dot, a, qb[4 * h + 2 * c][k], qb[4 * h + 2 * c + 1][k], h + c + k == 0 ? none : dot);
+                }
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const uint32_t scale = *reinterpret_cast<const uint32_t*>(ks + kQuantTile * kQuantRow + (n * 16 + e * 8 + g) * 4);
-                const float st = __uint_as_float(scale << 16), mid = fmaf(8.f, st, __uint_as_float(scale & 0xffff0000u));
+                const float st = __uint_as_float(scale << 16), low = __uint_as_float(scale & 0xffff0000u);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    float z = fmaf(st * p.a.scale_log2e, dot[2 * e + j], mid * qs[j]);
-                    if (part && at + n * 16 + e * 8 + g >= u.r.end) z = -INFINITY;
-                    s[n][2 * e + j] = z;
-                    top[j] = fmaxf(top[j], z);
-                }
+                for (int j = 0; j < 2; ++j) s[n][2 * e + j] = fmaf(st, dot[2 * e + j] * unit[j], low * qs[j]);
             }
+        }
+        if (at + kQuantTile > u.r.end) {
+#pragma unroll
+            for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (at + n * 16 + (e >> 1) * 8 + g >= u.r.end) s[n][e] = -INFINITY;
         }
         if (p.S && u.r.layer0 == 0) {
 #pragma unroll
@@ -329,6 +372,8 @@ __device__ __forceinline__ void attend_warp_quant(const QuantParams& p, const Qu
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
+            for (int n = 0; n < kBlocks; ++n) top[j] = fmaxf(top[j], fmaxf(s[n][j], s[n][2 + j]));
+#pragma unroll
             for (int o = 4; o < 32; o <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], o));
             const float m_new = fmaxf(m[j], top[j]);
             const float base = m_new == -INFINITY ? 0.f : m_new;         // all scores -inf so far: weights 0
@@ -339,81 +384,121 @@ __device__ __forceinline__ void attend_warp_quant(const QuantParams& p, const Qu
             for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
+                    // times 2^60 by way of the argument (float32: after it, which costs the argument no bits)
                     const float z = s[n][2 * e + j] - base;
-                    s[n][2 * e + j] = P == 1 ? fast_exp2(z) : exp2f(z);
+                    s[n][2 * e + j] = P == 1 ? fast_exp2(z + 60.f) : exp2f(z) * 1.152921504606846976e18f;
                     sum += s[n][2 * e + j];
                 }
             l[j] = l[j] * alpha[j] + sum;
         }
-        if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+        // As B weights have to hold neighbouring positions: an 8 x 8 transpose.
+        uint32_t pb[P == 1 ? kBlocks : 1][2];
+        if constexpr (P == 1) {
 #pragma unroll
-            for (int y = 0; y < LG; ++y) {
-                mids[y][0] *= alpha[0]; mids[y][1] *= alpha[1];
+            for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[y][d][e] *= alpha[e & 1];
-            }
+                for (int e = 0; e < 2; ++e)
+                    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(pb[n][e]) : "r"(pack_bf16(s[n][2 * e], s[n][2 * e + 1])));
         }
 #pragma unroll
         for (int y = 0; y < LG; ++y) {
             if (y >= u.r.layers) break;
             const char* vs = smem + ring.next();
+            const char* scales = vs + kQuantTile * kQuantRow;
+            // weights times steps: bf16 rows round p and then the product (half a step each, 2^-8 relative, of independent sign)
+            uint32_t w[kBlocks][2][P];
+            float mid[4];
+            if constexpr (P == 1) {
+#pragma unroll
+                for (int n = 0; n < kBlocks; ++n) {
+                    uint32_t a[4];                           // rows g: low of positions 2 t4 .., rows g + 8: step
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint2 x = *reinterpret_cast<const uint2*>(scales + (n * 16 + e * 8 + 2 * t4) * 4);
+                        a[2 * e] = __byte_perm(x.x, x.y, 0x7632);
+                        a[2 * e + 1] = __byte_perm(x.x, x.y, 0x5410);
+                        w[n][e][0] = mul_bf16x2(pb[n][e], a[2 * e + 1]);
+                    }
+                    quant_mma(mid, a, pb[n][0], pb[n][1], n == 0 ? none : mid);
+                }
+            } else {
+                mid[0] = mid[1] = mid[2] = mid[3] = 0.f;
+#pragma unroll
+                for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t scale = *reinterpret_cast<const uint32_t*>(scales + (n * 16 + e * 8 + g) * 4);
+                        const float st = __uint_as_float(scale << 16), low = __uint_as_float(scale & 0xffff0000u);
+                        const float md = fmaf(8.f, st, low);
+                        mid[0] = fmaf(s[n][2 * e], md, mid[0]);
+                        mid[1] = fmaf(s[n][2 * e + 1], md, mid[1]);
+                        quant_split<P>(s[n][2 * e] * st, s[n][2 * e + 1] * st, w[n][e]);
+#pragma unroll
+                        for (int k = 0; k < P; ++k) asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %0;" : "+r"(w[n][e][k]));
+                    }
+            }
+            // -8 times the sum of the weights, in the units of the bits 0-3 and of the bits 4-7: where the products start
+            float start[2][4];
+            const uint32_t eight[4] = {0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u};
+#pragma unroll
+            for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+                for (int k = 0; k < P; ++k) quant_mma(start[0], eight, w[n][0][k], w[n][1][k], n + k == 0 ? none : start[0]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) start[1][e] = 16.f * start[0][e];
+            float d[4][4];
 #pragma unroll
             for (int n = 0; n < kBlocks; ++n) {
-                // Weight times step, in P bf16 numbers.  One (bf16 outputs) is off by half a step, 2^-8 relative, of independent sign
-                // over the positions.  As B they have to hold neighbouring positions: an 8 x 8 transpose.
-                uint32_t pb[2][P];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint32_t scale = *reinterpret_cast<const uint32_t*>(vs + kQuantTile * kQuantRow + (n * 16 + e * 8 + g) * 4);
-                    const float st = __uint_as_float(scale << 16), mid = fmaf(8.f, st, __uint_as_float(scale & 0xffff0000u));
-                    mids[y][0] = fmaf(s[n][2 * e], mid, mids[y][0]);
-                    mids[y][1] = fmaf(s[n][2 * e + 1], mid, mids[y][1]);
-                    quant_split<P>(s[n][2 * e] * st, s[n][2 * e + 1] * st, pb[e]);
-#pragma unroll
-                    for (int k = 0; k < P; ++k)
-                        asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %0;" : "+r"(pb[e][k]));
-                }
                 // word g of positions 2 t4, 2 t4 + 1 and 8 further on, two positions to a register
-                uint32_t lo[2], hi[2];
+                uint32_t lo[2][4], hi[2][4];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const char* at_row = vs + (n * 16 + e * 8 + t4) * kQuantRow + g * 4;
                     const uint32_t w0 = *reinterpret_cast<const uint32_t*>(at_row), w1 = *reinterpret_cast<const uint32_t*>(at_row + 4 * kQuantRow);
-                    lo[e] = __byte_perm(w0, w1, 0x5410);
-                    hi[e] = __byte_perm(w0, w1, 0x7632);
+                    quant_four(__byte_perm(w0, w1, 0x5410), lo[e]);
+                    quant_four(__byte_perm(w0, w1, 0x7632), hi[e]);
                 }
 #pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    const uint32_t a[4] = {quant_two(lo[0], d), quant_two(hi[0], d), quant_two(lo[1], d), quant_two(hi[1], d)};
+                for (int c = 0; c < 4; ++c) {
+                    const uint32_t a[4] = {lo[0][c], hi[0][c], lo[1][c], hi[1][c]};
 #pragma unroll
-                    for (int k = 0; k < P; ++k) mma_bf16(acc[y][d], a, pb[0][k], pb[1][k]);
+                    for (int k = 0; k < P; ++k) quant_mma(d[c], a, w[n][0][k], w[n][1][k], n + k == 0 ? start[c & 1] : d[c]);
                 }
             }
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[y][c][e] = fmaf(acc[y][c][e], alpha[e & 1], d[c][e]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                mids[y][j] = fmaf(mids[y][j], alpha[j], P == 1 ? fmaf(8.f, mid[2 + j], mid[j]) : mid[j]);
         }
     }
     cp_wait<0>();
     __syncwarp();
+    constexpr float kDown = 8.67361737988403547e-19f, kUp = 9.44473296573929043e21f;      // 2^-60; 2^73
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) {
             l[j] += __shfl_xor_sync(0xffffffffu, l[j], o);
+            if constexpr (P > 1)                             // (the products give every row g the whole sum)
 #pragma unroll
-            for (int y = 0; y < LG; ++y) mids[y][j] += __shfl_xor_sync(0xffffffffu, mids[y][j], o);
+                for (int y = 0; y < LG; ++y) mids[y][j] += __shfl_xor_sync(0xffffffffu, mids[y][j], o);
         }
         const int row = 2 * t4 + j;
-        if (g == 0) ml[row] = make_float2(m[j], l[j]);
+        if (g == 0) ml[row] = make_float2(m[j], l[j] * kDown);
         if (row < u.r.rows) {
             float* out = reinterpret_cast<float*>(smem) + row * kAtOutLd + g * 8;
 #pragma unroll
             for (int y = 0; y < LG; ++y)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    *reinterpret_cast<float4*>(out + y * kAtRows * kAtOutLd + h * 4) =
-                        make_float4(acc[y][0][2 * h + j] + mids[y][j], acc[y][1][2 * h + j] + mids[y][j],
-                                    acc[y][2][2 * h + j] + mids[y][j], acc[y][3][2 * h + j] + mids[y][j]);
+                for (int h = 0; h < 2; ++h) {
+                    float x[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) x[c] = fmaf(acc[y][c][2 * h + j], c & 1 ? kUp * 0.0625f : kUp, mids[y][j] * kDown);
+                    *reinterpret_cast<float4*>(out + y * kAtRows * kAtOutLd + h * 4) = make_float4(x[0], x[1], x[2], x[3]);
+                }
         }
     }
 }

@@ -57,12 +57,11 @@ def _bf16(x, up):
 def quantise_row(x):
     """64 numbers -> (codes list, step, low); step = low = NaN for a row that cannot be held."""
     x = [float(v) for v in x]
-    if not all(math.isfinite(v) for v in x):
+    if not all(abs(v) < 2.0 ** 40 for v in x):
         return [0] * DH, math.nan, math.nan
     low = _bf16(min(x), False)
-    step = _bf16((max(x) - low) / 15.0, True) if math.isfinite(low) else math.inf
-    if not (math.isfinite(low) and math.isfinite(step)):
-        return [0] * DH, math.nan, math.nan
+    step = _bf16((max(x) - low) / 15.0, True)
+    step = max(step, 2.0 ** -50) if step > 0 else step
     codes = []
     for v in x:
         t = (v - low) / step if step > 0 else 0.0
@@ -102,7 +101,8 @@ def quant_attend(q, codes, scales, dtype):
     size = (p[None, :, None] @ (whole[1:] + mid[1:].abs()[..., None]))[:, :, 0]
     bound = size * rel[None, :, None] + rounding(dtype) * out.abs() * 1.01 + 1e-30
     if dtype == torch.bfloat16:
-        bound = bound + UBF * (p[None, :, None] @ whole[1:])[:, :, 0] * 1.01                                # weights times step in bf16
+        # the weights are rounded to bf16, which goes with the numbers themselves, and so are these times the steps, which goes with n'
+        bound = bound + UBF * (p[None, :, None] @ (whole[1:] + x[1:].abs()))[:, :, 0] * 1.01
     return out, bound, p, p * rel[:, None] + 1e-37
 
 

@@ -44,7 +44,8 @@ def special_rows(dt):
     x = r(); x[63] = math.inf; rows.append(x)
     x = r(); x[0] = -math.inf; rows.append(x)
     x = r(); x[0], x[1] = big, -big; rows.append(x)                     # float32: its low is beyond bf16
-    x = r(); x[5] = 0.99 * 3.38e38; x[6] = -0.99 * 3.38e38; rows.append(x)
+    x = r(); x[5] = 1.09e12; x[6] = -1.09e12; rows.append(x)                     # below 2^40; the next is not
+    x = r(); x[9] = 1.1e12; rows.append(x)
     x = torch.zeros(DH); x[1] = 15.0; x[2:50] = torch.arange(48).float() * 0.25 + 0.5; rows.append(x)          # halves between codes
     x = torch.zeros(DH); x[0] = -2.25; x[1] = 5.25; x[2:] = 1e-12; rows.append(x)
     return torch.stack(rows).to(dt)
@@ -224,10 +225,10 @@ def test_attention_large_and_small_numbers(dtype):
     gen = torch.Generator().manual_seed(7)
     q = torch.randn(3, 4, DH, generator=gen)
     q[0] *= 30
-    q[1] *= 1e-20
+    q[1] *= 1e-10
     q = q.to(TYPES[dtype][0]).to(DEV)
-    scales[1, 0] *= 1e20
-    scales[1, 1] *= 1e-30
+    scales[1, 0] *= 1e11
+    scales[1, 1] *= 1e-12
     scales[2, 2, ..., 1] += 200
     scales[0, 2, ..., 0] = 0                                # rows of one number
     out, S, _ = attention(codes, scales, q, [0, 1, 2], [300, 299, 257], dtype, True)
