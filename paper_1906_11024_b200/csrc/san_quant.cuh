@@ -161,65 +161,84 @@ struct QuantRun {
     int item;
 };
 
-// N: slots of a warp's ring, later the place of its outputs (up to four layers of eight rows).
-template <int N> __host__ __device__ constexpr int quant_warp_bytes() { return N * kQuantSlot; }
-template <int N> __host__ __device__ constexpr int quant_smem_bytes() { return kAtWarps * (quant_warp_bytes<N>() + 2 * kAtRows * 4); }
+// A CTA takes one unit: a key head of an item, up to eight query rows, LG layers, a run of positions, in steps of one tile per warp.
+// W: warps.  Where LG divides it, warp w applies layer w % LG to the LG tiles from w / LG * LG on; 3 layers are W = 3.
+template <int LG> struct QuantWarps { static constexpr int W = LG == 3 ? 3 : 4; };
+constexpr int kQuantSlots = 4;              // of a warp's ring, later the place of its outputs
+constexpr int kQuantRing = kQuantSlots * kQuantSlot;
+template <int LG, int P, int J> __host__ __device__ constexpr int quant_weight_bytes() { return LG == 1 ? 0 : (P == 1 ? 8 : 8 * J) * 128; }       // of a tile
+template <int LG, int P, int J> __host__ __device__ constexpr int quant_smem_bytes() { return QuantWarps<LG>::W * (kQuantRing + quant_weight_bytes<LG, P, J>() + 2 * kAtRows * 4); }
+static_assert(kQuantRing >= kAtRows * kAtOutLd * 4, "room for a warp's outputs");
 
+__device__ __forceinline__ void cp16_whole(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void cp4_whole(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool full) {
     const int n = full ? 4 : 0;
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"(dst), "l"(src), "r"(n) : "memory");
 }
 
-// Fills one slot with positions [begin, begin + 64) of layer `plane` (-1: keys); what lies at or behind `end` becomes zeros.
-// Value rows go to places where four lanes find rows 2 t of a block of eight in different banks: row r of eight to r / 2 + 4 (r % 2).
-__device__ __forceinline__ void quant_fill(const QuantRun& u, int begin, int end, int plane, uint32_t slot, int lane) {
-    const char* codes = (plane < 0 ? u.r.k : u.r.v + plane * u.r.v_stride) + (long long)begin * kQuantRow + lane * 16;
-    const char* scales = (plane < 0 ? u.ks : u.vs + plane * u.s_stride) + (long long)begin * 4 + lane * 4;
-    const int r = lane >> 1;
-    const uint32_t to = slot + (plane < 0 ? lane * 16 : ((r & 8) | (r >> 1 & 3) | (r & 1) << 2) * kQuantRow + (lane & 1) * 16);
-    const uint32_t to_scale = slot + kQuantTile * kQuantRow + lane * 4;
-    if (begin + kQuantTile <= end) {
-#pragma unroll
-        for (int j = 0; j < kQuantTile / 16; ++j) cp16(to + j * 16 * kQuantRow, codes + j * 16 * kQuantRow, true);
-#pragma unroll
-        for (int j = 0; j < kQuantTile / 32; ++j) cp4(to_scale + j * 128, scales + j * 128, true);
-    } else {
-#pragma unroll
-        for (int j = 0; j < kQuantTile / 16; ++j) {
-            const bool full = begin + j * 16 + r < end;
-            cp16(to + j * 16 * kQuantRow, full ? codes + j * 16 * kQuantRow : codes, full);
-        }
-#pragma unroll
-        for (int j = 0; j < kQuantTile / 32; ++j) {
-            const bool full = begin + j * 32 + lane < end;
-            cp4(to_scale + j * 128, full ? scales + j * 128 : scales, full);
-        }
-    }
-    cp_commit();
-}
-
-template <int N> struct QuantRing {
-    const QuantRun& u; uint32_t ring; int lane, step;
-    int f_at, f_plane, f_slot, r_slot;
-    __device__ __forceinline__ QuantRing(const QuantRun& run, uint32_t smem, int ln, int first, int stp)
-        : u(run), ring(smem), lane(ln), step(stp), f_at(first), f_plane(-1), f_slot(0), r_slot(0) {
-        for (int i = 0; i < N - 1; ++i) fill();
+// Walks a warp's slots: of every step the tile of keys that it scores, then the tiles of values (of its layer) that it applies, filled
+// kQuantSlots - 1 ahead of use.  What lies at or behind `end` becomes zeros; a step has no tiles that begin there.  Value rows go to
+// places where four lanes find rows 2 t of a block of eight in different banks: row r of eight to r / 2 + 4 (r % 2).
+template <int W, int LG> struct QuantRing {
+    uint32_t ring; int lane, end;
+    int f_at, f_tile; uint32_t f_slot, r_slot;              // f_at: first position of the step; f_tile: -1 keys
+    int k_off, v_off;                                       // of the warp's tiles in a step
+    bool values;                                            // its layer is there
+    const char* k; const char* v; const char* ks; const char* vs;           // this lane's first bytes of the step
+    uint32_t v_to;                                          // where its first value row goes
+    __device__ __forceinline__ QuantRing(const QuantRun& u, uint32_t smem, int ln, int warp)
+        : ring(smem), lane(ln), end(u.r.end), f_at(u.r.begin), f_tile(-1), f_slot(0), r_slot(0) {
+        const int y = warp % LG;
+        k_off = warp * kQuantTile; v_off = warp / LG * LG * kQuantTile;
+        values = y < u.r.layers;
+        const long long at = (long long)u.r.begin * kQuantRow + lane * 16, at_scale = (long long)u.r.begin * 4 + lane * 4;
+        k = u.r.k + at; v = u.r.v + (values ? y : 0) * u.r.v_stride + at;
+        ks = u.ks + at_scale; vs = u.vs + (values ? y : 0) * u.s_stride + at_scale;
+        const int r = lane >> 1;
+        v_to = ((r & 8) | (r >> 1 & 3) | (r & 1) << 2) * kQuantRow + (lane & 1) * 16;
+        for (int i = 0; i < kQuantSlots - 1; ++i) fill();
     }
     __device__ __forceinline__ void fill() {
-        if (f_at < u.r.end) {
-            quant_fill(u, f_at, u.r.end, f_plane, ring + f_slot * kQuantSlot, lane);
-            if (++f_plane == u.r.layers) { f_plane = -1; f_at += step; }
-            f_slot = f_slot + 1 == N ? 0 : f_slot + 1;
-        } else {
-            cp_commit();
+        if (f_at < end) {
+            const int off = f_tile < 0 ? k_off : v_off + f_tile * kQuantTile, at = f_at + off;
+            const char* codes = (f_tile < 0 ? k : v) + off * kQuantRow;
+            const char* scales = (f_tile < 0 ? ks : vs) + off * 4;
+            const uint32_t slot = ring + f_slot, to = slot + (f_tile < 0 ? lane * 16 : v_to), to_scale = slot + kQuantTile * kQuantRow + lane * 4;
+            if (at + kQuantTile <= end) {
+#pragma unroll
+                for (int j = 0; j < kQuantTile / 16; ++j) cp16_whole(to + j * 16 * kQuantRow, codes + j * 16 * kQuantRow);
+#pragma unroll
+                for (int j = 0; j < kQuantTile / 32; ++j) cp4_whole(to_scale + j * 128, scales + j * 128);
+            } else if (at < end) {
+#pragma unroll
+                for (int j = 0; j < kQuantTile / 16; ++j) {
+                    const bool full = at + j * 16 + (lane >> 1) < end;
+                    cp16(to + j * 16 * kQuantRow, full ? codes + j * 16 * kQuantRow : v, full);
+                }
+#pragma unroll
+                for (int j = 0; j < kQuantTile / 32; ++j) {
+                    const bool full = at + j * 32 + lane < end;
+                    cp4(to_scale + j * 128, full ? scales + j * 128 : vs, full);
+                }
+            }
+            f_slot = f_slot + kQuantSlot == kQuantRing ? 0 : f_slot + kQuantSlot;
+            if (++f_tile == LG || !values) {
+                constexpr int step = W * kQuantTile;
+                f_tile = -1;
+                f_at += step;
+                k += step * kQuantRow; v += step * kQuantRow; ks += step * 4; vs += step * 4;
+            }
         }
+        cp_commit();                                        // behind the end an empty group keeps the count
     }
+    // Offset of the next slot in order, arrived; every lane is done with the one before it, which is refilled.
     __device__ __forceinline__ uint32_t next() {
-        cp_wait<N - 2>();
+        cp_wait<kQuantSlots - 2>();
         __syncwarp();
         fill();
-        const uint32_t s = r_slot * kQuantSlot;
-        r_slot = r_slot + 1 == N ? 0 : r_slot + 1;
+        const uint32_t s = r_slot;
+        r_slot = r_slot + kQuantSlot == kQuantRing ? 0 : r_slot + kQuantSlot;
         return s;
     }
 };
@@ -231,7 +250,7 @@ __device__ __forceinline__ void quant_four(uint32_t w, uint32_t* out) {
     out[2] = v & 0x000f000fu; out[3] = v & 0x00f000f0u;
 }
 __device__ __forceinline__ void quant_mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1, const float* c) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
                  : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
@@ -251,19 +270,27 @@ template <int P> __device__ __forceinline__ void quant_split(float x, float y, u
     }
 }
 
-// Up to eight query rows, which are the N side of both products: scores D[16 positions x 8 queries] with the codes of key rows as
-// A, outputs D[16 dims x 8 queries] with those of value rows.  P: 1 for bf16 queries, 3 for float32.
-template <int LG, int N, int P>
-__device__ __forceinline__ void attend_warp_quant(const QuantParams& p, const QuantRun& u, int first, int step, char* smem, float2* ml, int lane) {
+// Query rows, which are the N side of both products: scores D[16 positions x 8 queries] with the codes of key rows as
+// A, outputs D[16 dims x 8 queries] with those of value rows.  P: 1 for bf16 queries, 3 for float32.  J: a lane holds two neighbouring
+// columns of D.  With J = 1 only the even one is a query (up to four rows), which halves what is done to scores and weights; with
+// J = 2 both are (up to eight).
+// Every warp of the CTA calls this.  Per step: scores of the warp's own tile, the largest of all tiles (a barrier), weights, which the
+// warps share (a barrier), then the warp's layer.  So a warp holds one layer's outputs, 16 registers, and an SM holds 16 warps
+// or more: with four layers a warp (64 registers, 12 warps) instructions waited for one another half of the time.
+template <int LG, int P, int J>
+__device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRun& u, char* smem, char* shared, float* tops, float2* ml, int warp, int lane) {
+    constexpr int W = QuantWarps<LG>::W;
     const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(smem);
-    QuantRing<N> ring(u, ring_addr, lane, first, step);
+    QuantRing<W, LG> ring(u, ring_addr, lane, warp);
     const int g = lane >> 2, t4 = lane & 3;
-    // B: query g, dims 16 t4 .. 16 t4 + 15 in the order of the codes' unpacking, scaled to at most 2^60 and odd ones of a byte by another 1 / 16
+    // B: the query of column g, dims 16 t4 .. 16 t4 + 15 in the order of the codes' unpacking, scaled to at most 2^60 and odd ones of a byte by
+    // another 1 / 16
     uint32_t qb[8][P];
-    float qs[2], unit[2];                                    // of queries 2 t4 and 2 t4 + 1: their sum times the scores' scale; what undoes the scaling, times it
+    float qs[J], unit[J];                                    // of columns 2 t4 (+ 1): the query's sum times the scores' scale; what undoes the scaling, times it
     {
-        const bool real = g < u.r.rows;
-        const int head = u.r.head0 + u.r.row0 + (real ? g : 0);
+        const int row = J == 1 ? g >> 1 : g;
+        const bool real = row < u.r.rows && (J == 2 || (g & 1) == 0);
+        const int head = u.r.head0 + u.r.row0 + (real ? row : 0);
         float q[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) q[i] = 0.f;
@@ -295,7 +322,7 @@ __device__ __forceinline__ void attend_warp_quant(const QuantParams& p, const Qu
         const float up = __uint_as_float((uint32_t)(59 - e + 127) << 23);
         const float down = __uint_as_float((uint32_t)(e + 74 + 127) << 23);      // 2^133 / up
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < J; ++j) {
             qs[j] = __shfl_sync(0xffffffffu, sum, 4 * (2 * t4 + j)) * p.a.scale_log2e;
             unit[j] = __shfl_sync(0xffffffffu, down, 4 * (2 * t4 + j)) * p.a.scale_log2e;
         }
@@ -307,104 +334,150 @@ __device__ __forceinline__ void attend_warp_quant(const QuantParams& p, const Qu
                 quant_split<P>(q[8 * h + i] * f, q[8 * h + 4 + i] * f, qb[4 * h + i]);
             }
     }
-    // [layer][d]: dims 8 g + d and 8 g + 4 + d of queries 2 t4, 2 t4 + 1 (odd d: 16 times), in units of 2^-73; sums of p mid in units of 2^60
-    float acc[LG][4][4], mids[LG][2];
+    // [d]: dims 8 g + d and 8 g + 4 + d of columns 2 t4, 2 t4 + 1 (odd d: 16 times), in units of 2^-73; sums of p mid in units of 2^60
+    float acc[4][4], mids[J], m[J], l[J];
 #pragma unroll
-    for (int y = 0; y < LG; ++y) {
-        mids[y][0] = mids[y][1] = 0.f;
+    for (int j = 0; j < J; ++j) { mids[j] = 0.f; m[j] = -INFINITY; l[j] = 0.f; }
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[y][d][e] = 0.f;
-    }
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    constexpr int kBlocks = kQuantTile / 16;
+        for (int e = 0; e < 4; ++e) acc[d][e] = 0.f;
+    constexpr int kBlocks = kQuantTile / 16, kRegs = P == 1 ? 2 * kBlocks : 2 * kBlocks * J;         // weights of a lane and tile
     const float none[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int at = first; at < u.r.end; at += step) {
+    for (int at0 = u.r.begin; at0 < u.r.end; at0 += W * kQuantTile) {
+        const int at = at0 + warp * kQuantTile;
+        float s[kBlocks][2][J];                              // positions 16 n + g and + 8, columns 2 t4 (+ 1)
         const char* ks = smem + ring.next();
-        float s[kBlocks][4];                                 // positions 16 n + g and + 8, queries 2 t4 and 2 t4 + 1
-        float top[2] = {-INFINITY, -INFINITY};
+        if (at < u.r.end) {                                  // (the same in all lanes)
 #pragma unroll
-        for (int n = 0; n < kBlocks; ++n) {
-            const uint2 w0 = *reinterpret_cast<const uint2*>(ks + (n * 16 + g) * kQuantRow + t4 * 8);
-            const uint2 w1 = *reinterpret_cast<const uint2*>(ks + (n * 16 + 8 + g) * kQuantRow + t4 * 8);
-            float dot[4];
+            for (int n = 0; n < kBlocks; ++n) {
+                const uint2 w0 = *reinterpret_cast<const uint2*>(ks + (n * 16 + g) * kQuantRow + t4 * 8);
+                const uint2 w1 = *reinterpret_cast<const uint2*>(ks + (n * 16 + 8 + g) * kQuantRow + t4 * 8);
+                float dot[4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t x0[4], x1[4];
-                quant_four(h ? w0.y : w0.x, x0);
-                quant_four(h ? w1.y : w1.x, x1);
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t x0[4], x1[4];
+                    quant_four(h ? w0.y : w0.x, x0);
+                    quant_four(h ? w1.y : w1.x, x1);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const uint32_t a[4] = {x0[2 * c], x1[2 * c], x0[2 * c + 1], x1[2 * c + 1]};
+                    for (int c = 0; c < 2; ++c) {
+                        const uint32_t a[4] = {x0[2 * c], x1[2 * c], x0[2 * c + 1], x1[2 * c + 1]};
 #pragma unroll
-                    for (int k = 0; k < P; ++k) quant_mma(dot, a, qb[4 * h + 2 * c][k], qb[4 * h + 2 * c + 1][k], h + c + k == 0 ? none : dot);
+                        for (int k = 0; k < P; ++k) quant_mma(dot, a, qb[4 * h + 2 * c][k], qb[4 * h + 2 * c + 1][k], h + c + k == 0 ? none : dot);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t scale = *reinterpret_cast<const uint32_t*>(ks + kQuantTile * kQuantRow + (n * 16 + e * 8 + g) * 4);
+                    const float st = __uint_as_float(scale << 16), low = __uint_as_float(scale & 0xffff0000u);
+#pragma unroll
+                    for (int j = 0; j < J; ++j) s[n][e][j] = fmaf(st, dot[2 * e + j] * unit[j], low * qs[j]);
                 }
             }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint32_t scale = *reinterpret_cast<const uint32_t*>(ks + kQuantTile * kQuantRow + (n * 16 + e * 8 + g) * 4);
-                const float st = __uint_as_float(scale << 16), low = __uint_as_float(scale & 0xffff0000u);
-#pragma unroll
-                for (int j = 0; j < 2; ++j) s[n][2 * e + j] = fmaf(st, dot[2 * e + j] * unit[j], low * qs[j]);
-            }
-        }
-        if (at + kQuantTile > u.r.end) {
-#pragma unroll
-            for (int n = 0; n < kBlocks; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (at + n * 16 + (e >> 1) * 8 + g >= u.r.end) s[n][e] = -INFINITY;
-        }
-        if (p.S && u.r.layer0 == 0) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (2 * t4 + j >= u.r.rows) continue;
-                float* to = p.S + ((long long)u.item * p.a.H + u.r.head0 + u.r.row0 + 2 * t4 + j) * p.ld_s + at + g;
+            if (at + kQuantTile > u.r.end) {
 #pragma unroll
                 for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
-                        if (at + n * 16 + e * 8 + g < u.r.end) to[n * 16 + e * 8] = s[n][2 * e + j];
+#pragma unroll
+                        for (int j = 0; j < J; ++j)
+                            if (at + n * 16 + e * 8 + g >= u.r.end) s[n][e][j] = -INFINITY;
             }
+            if (p.S && u.r.layer0 == 0) {
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const int row = J * t4 + j;
+                    if (row >= u.r.rows) continue;
+                    float* to = p.S + ((long long)u.item * p.a.H + u.r.head0 + u.r.row0 + row) * p.ld_s + at + g;
+#pragma unroll
+                    for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if (at + n * 16 + e * 8 + g < u.r.end) to[n * 16 + e * 8] = s[n][e][j];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int j = 0; j < J; ++j) s[n][e][j] = -INFINITY;
         }
-        float alpha[2];
+        float top[J];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < J; ++j) {
+            top[j] = fmaxf(s[0][0][j], s[0][1][j]);
 #pragma unroll
-            for (int n = 0; n < kBlocks; ++n) top[j] = fmaxf(top[j], fmaxf(s[n][j], s[n][2 + j]));
+            for (int n = 1; n < kBlocks; ++n) top[j] = fmaxf(top[j], fmaxf(s[n][0][j], s[n][1][j]));
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], o));
-            const float m_new = fmaxf(m[j], top[j]);
-            const float base = m_new == -INFINITY ? 0.f : m_new;         // all scores -inf so far: weights 0
-            alpha[j] = m[j] == m_new ? 1.f : P == 1 ? fast_exp2(m[j] - base) : exp2f(m[j] - base);
-            m[j] = m_new;
+            if (g == 0) tops[warp * kAtRows + J * t4 + j] = top[j];
+        }
+        __syncthreads();                                     // (and every warp is done with the weights of the step before)
+        float alpha[J];
+        bool moved = false;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            float t = m[j];
+#pragma unroll
+            for (int w = 0; w < W; ++w) t = fmaxf(t, tops[w * kAtRows + J * t4 + j]);
+            // times 2^60 by way of the argument (float32: after it, which costs the argument no bits); all scores -inf so far: weights 0
+            const float base = (t == -INFINITY ? 0.f : t) - (P == 1 ? 60.f : 0.f);
+            alpha[j] = m[j] == t ? 1.f : P == 1 ? fast_exp2(m[j] - t) : exp2f(m[j] - t);
+            moved |= m[j] != t;
+            m[j] = t;
             float sum = 0.f;
 #pragma unroll
             for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    // times 2^60 by way of the argument (float32: after it, which costs the argument no bits)
-                    const float z = s[n][2 * e + j] - base;
-                    s[n][2 * e + j] = P == 1 ? fast_exp2(z + 60.f) : exp2f(z) * 1.152921504606846976e18f;
-                    sum += s[n][2 * e + j];
+                    s[n][e][j] = P == 1 ? fast_exp2(s[n][e][j] - base) : exp2f(s[n][e][j] - base) * 1.152921504606846976e18f;
+                    sum += s[n][e][j];
                 }
             l[j] = l[j] * alpha[j] + sum;
         }
-        // As B weights have to hold neighbouring positions: an 8 x 8 transpose.
-        uint32_t pb[P == 1 ? kBlocks : 1][2];
-        if constexpr (P == 1) {
+        // The tile's weights, as they enter the products: bf16 rows as B, which has to hold neighbouring positions (an 8 x 8 transpose).
+        uint32_t pw[kRegs];
 #pragma unroll
-            for (int n = 0; n < kBlocks; ++n)
+        for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(pb[n][e]) : "r"(pack_bf16(s[n][2 * e], s[n][2 * e + 1])));
+            for (int e = 0; e < 2; ++e) {
+                if constexpr (P == 1) {
+                    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(pw[2 * n + e]) : "r"(pack_bf16(s[n][e][0], J == 2 ? s[n][e][J - 1] : 0.f)));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < J; ++j) pw[(2 * n + e) * J + j] = __float_as_uint(s[n][e][j]);
+                }
+            }
+        if constexpr (LG > 1) {
+#pragma unroll
+            for (int i = 0; i < kRegs / 4; ++i)
+                *reinterpret_cast<uint4*>(shared + ((warp * (kRegs / 4) + i) * 32 + lane) * 16) = make_uint4(pw[4 * i], pw[4 * i + 1], pw[4 * i + 2], pw[4 * i + 3]);
         }
+        if (__any_sync(0xffffffffu, moved)) {                // seldom, once a run is under way
 #pragma unroll
-        for (int y = 0; y < LG; ++y) {
-            if (y >= u.r.layers) break;
+            for (int j = 0; j < J; ++j) {
+                mids[j] *= alpha[j];
+#pragma unroll
+                for (int d = 0; d < 4; ++d) { acc[d][j] *= alpha[j]; acc[d][2 + j] *= alpha[j]; }
+            }
+        }
+        __syncthreads();                                     // (and the tops have been read)
+        if (!ring.values) continue;
+#pragma unroll 1
+        for (int t = 0; t < LG; ++t) {
             const char* vs = smem + ring.next();
+            const int tile = warp / LG * LG + t;
+            if (at0 + tile * kQuantTile >= u.r.end) continue;
             const char* scales = vs + kQuantTile * kQuantRow;
+            if constexpr (LG > 1) {
+#pragma unroll
+                for (int i = 0; i < kRegs / 4; ++i) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(shared + ((tile * (kRegs / 4) + i) * 32 + lane) * 16);
+                    pw[4 * i] = x.x; pw[4 * i + 1] = x.y; pw[4 * i + 2] = x.z; pw[4 * i + 3] = x.w;
+                }
+            }
             // weights times steps: bf16 rows round p and then the product (half a step each, 2^-8 relative, of independent sign)
             uint32_t w[kBlocks][2][P];
             float mid[4];
@@ -417,36 +490,43 @@ __device__ __forceinline__ void attend_warp_quant(const QuantParams& p, const Qu
                         const uint2 x = *reinterpret_cast<const uint2*>(scales + (n * 16 + e * 8 + 2 * t4) * 4);
                         a[2 * e] = __byte_perm(x.x, x.y, 0x7632);
                         a[2 * e + 1] = __byte_perm(x.x, x.y, 0x5410);
-                        w[n][e][0] = mul_bf16x2(pb[n][e], a[2 * e + 1]);
+                        w[n][e][0] = mul_bf16x2(pw[2 * n + e], a[2 * e + 1]);
                     }
-                    quant_mma(mid, a, pb[n][0], pb[n][1], n == 0 ? none : mid);
+                    quant_mma(mid, a, pw[2 * n], pw[2 * n + 1], n == 0 ? none : mid);
                 }
             } else {
-                mid[0] = mid[1] = mid[2] = mid[3] = 0.f;
+                mid[0] = mid[1] = 0.f;
 #pragma unroll
                 for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const uint32_t scale = *reinterpret_cast<const uint32_t*>(scales + (n * 16 + e * 8 + g) * 4);
-                        const float st = __uint_as_float(scale << 16), low = __uint_as_float(scale & 0xffff0000u);
-                        const float md = fmaf(8.f, st, low);
-                        mid[0] = fmaf(s[n][2 * e], md, mid[0]);
-                        mid[1] = fmaf(s[n][2 * e + 1], md, mid[1]);
-                        quant_split<P>(s[n][2 * e] * st, s[n][2 * e + 1] * st, w[n][e]);
+                        const float st = __uint_as_float(scale << 16), md = fmaf(8.f, st, __uint_as_float(scale & 0xffff0000u));
+                        float x[2] = {0.f, 0.f};
 #pragma unroll
-                        for (int k = 0; k < P; ++k) asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %0;" : "+r"(w[n][e][k]));
+                        for (int j = 0; j < J; ++j) {
+                            x[j] = __uint_as_float(pw[(2 * n + e) * J + j]);
+                            mid[j] = fmaf(x[j], md, mid[j]);
+                            x[j] *= st;
+                        }
+                        quant_split<P>(x[0], x[1], w[n][e]);
+#pragma unroll
+                        for (int k = 0; k < P; ++k) asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %0;" : "+r"(w[n][e][k]));
                     }
             }
-            // -8 times the sum of the weights, in the units of the bits 0-3 and of the bits 4-7: where the products start
-            float start[2][4];
+            // -8 times the sum of the weights, in the units of the bits 0-3 (of the bits 4-7: 16 times): added first
+            float start[4];
             const uint32_t eight[4] = {0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u};
 #pragma unroll
             for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
-                for (int k = 0; k < P; ++k) quant_mma(start[0], eight, w[n][0][k], w[n][1][k], n + k == 0 ? none : start[0]);
+                for (int k = 0; k < P; ++k) quant_mma(start, eight, w[n][0][k], w[n][1][k], n + k == 0 ? none : start);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) start[1][e] = 16.f * start[0][e];
-            float d[4][4];
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int j = 0; j < J; ++j) acc[c][2 * e + j] = fmaf(start[j], c & 1 ? 16.f : 1.f, acc[c][2 * e + j]);
 #pragma unroll
             for (int n = 0; n < kBlocks; ++n) {
                 // word g of positions 2 t4, 2 t4 + 1 and 8 further on, two positions to a register
@@ -462,43 +542,32 @@ __device__ __forceinline__ void attend_warp_quant(const QuantParams& p, const Qu
                 for (int c = 0; c < 4; ++c) {
                     const uint32_t a[4] = {lo[0][c], hi[0][c], lo[1][c], hi[1][c]};
 #pragma unroll
-                    for (int k = 0; k < P; ++k) quant_mma(d[c], a, w[n][0][k], w[n][1][k], n + k == 0 ? start[c & 1] : d[c]);
+                    for (int k = 0; k < P; ++k) quant_mma(acc[c], a, w[n][0][k], w[n][1][k], acc[c]);
                 }
             }
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[y][c][e] = fmaf(acc[y][c][e], alpha[e & 1], d[c][e]);
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                mids[y][j] = fmaf(mids[y][j], alpha[j], P == 1 ? fmaf(8.f, mid[2 + j], mid[j]) : mid[j]);
+            for (int j = 0; j < J; ++j) mids[j] += P == 1 ? fmaf(8.f, mid[2 + j], mid[j]) : mid[j];
         }
     }
     cp_wait<0>();
     __syncwarp();
     constexpr float kDown = 8.67361737988403547e-19f, kUp = 9.44473296573929043e21f;      // 2^-60; 2^73
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < J; ++j) {
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) {
             l[j] += __shfl_xor_sync(0xffffffffu, l[j], o);
-            if constexpr (P > 1)                             // (the products give every row g the whole sum)
-#pragma unroll
-                for (int y = 0; y < LG; ++y) mids[y][j] += __shfl_xor_sync(0xffffffffu, mids[y][j], o);
+            if constexpr (P > 1) mids[j] += __shfl_xor_sync(0xffffffffu, mids[j], o);      // (the products give every row g the whole sum)
         }
-        const int row = 2 * t4 + j;
+        const int row = J * t4 + j;
         if (g == 0) ml[row] = make_float2(m[j], l[j] * kDown);
-        if (row < u.r.rows) {
-            float* out = reinterpret_cast<float*>(smem) + row * kAtOutLd + g * 8;
+        float* out = reinterpret_cast<float*>(smem) + row * kAtOutLd + g * 8;
 #pragma unroll
-            for (int y = 0; y < LG; ++y)
+        for (int h = 0; h < 2; ++h) {
+            float x[4];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float x[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) x[c] = fmaf(acc[y][c][2 * h + j], c & 1 ? kUp * 0.0625f : kUp, mids[y][j] * kDown);
-                    *reinterpret_cast<float4*>(out + y * kAtRows * kAtOutLd + h * 4) = make_float4(x[0], x[1], x[2], x[3]);
-                }
+            for (int c = 0; c < 4; ++c) x[c] = fmaf(acc[c][2 * h + j], c & 1 ? kUp * 0.0625f : kUp, mids[j] * kDown);
+            *reinterpret_cast<float4*>(out + h * 4) = make_float4(x[0], x[1], x[2], x[3]);
         }
     }
 }
@@ -506,10 +575,11 @@ __device__ __forceinline__ void attend_warp_quant(const QuantParams& p, const Qu
 __device__ __forceinline__ bool quant_unit(const QuantParams& p, int index, bool reporter, QuantRun* u) {
     const AttendParams& a = p.a;
     if (index >= a.o_units) return false;
+    // the first runs of all items first: those that only long items have come last, where short CTAs even out the end
     const int lg = index % a.n_lg; index /= a.n_lg;
-    const int split = index % a.o_splits; index /= a.o_splits;
     const int hk = index % a.Hk; index /= a.Hk;
-    const int tile = index % a.o_row_tiles, item = index / a.o_row_tiles;
+    const int tile = index % a.o_row_tiles; index /= a.o_row_tiles;
+    const int item = index % a.n_items, split = index / a.n_items;
     if (!own_ok(a, item)) {
         if (reporter && tile == 0 && split == 0 && hk == 0 && lg == 0) {
             const int id = a.ids[item];
@@ -538,20 +608,49 @@ __device__ __forceinline__ bool quant_unit(const QuantParams& p, int index, bool
     return true;
 }
 
-template <int LG, int N, int P>
-__global__ void __launch_bounds__(kAtWarps * 32) quant_attend_kernel(const __grid_constant__ QuantParams p) {
-    static_assert(quant_warp_bytes<N>() >= LG * kAtRows * kAtOutLd * 4, "room for a warp's outputs");
+// P, J: see attend_quant.  Registers leave room for 16 warps on an SM (bf16; 99.5 us with 20 warps and 96 registers, 95.3 with 16 and 128:
+// 128 rows of up to 4096, 4 layers).
+template <int LG, int P, int J>
+__global__ void __launch_bounds__(QuantWarps<LG>::W * 32, P == 1 ? LG == 3 ? 5 : 4 : 3) quant_attend_kernel(const __grid_constant__ QuantParams p) {
+    constexpr int W = QuantWarps<LG>::W, R = kAtRows;
     using T = typename std::conditional<P == 1, __nv_bfloat16, float>::type;
     extern __shared__ __align__(128) char attend_smem[];
+    __shared__ float tops[W * R];
     if (p.a.slots > 1 || p.S) asm volatile("griddepcontrol.launch_dependents;");
-    constexpr int R = kAtRows, WB = quant_warp_bytes<N>();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wpu = p.a.o_wpu;
-    float2* ml = reinterpret_cast<float2*>(attend_smem + kAtWarps * WB);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    char* shared = attend_smem + W * kQuantRing;
+    float2* ml = reinterpret_cast<float2*>(shared + W * quant_weight_bytes<LG, P, J>());
     QuantRun u;
-    const bool active = quant_unit(p, (int)blockIdx.x * (kAtWarps / wpu) + warp / wpu, warp % wpu == 0 && lane == 0, &u);
-    if (active)
-        attend_warp_quant<LG, N, P>(p, u, u.r.begin + (warp % wpu) * kQuantTile, wpu * kQuantTile, attend_smem + warp * WB, ml + warp * R, lane);
-    attend_finish<T, WB>(p.a, u.r, active, wpu, attend_smem, ml, warp, lane);
+    if (!quant_unit(p, (int)blockIdx.x, threadIdx.x == 0, &u)) return;
+    attend_quant<LG, P, J>(p, u, attend_smem + warp * kQuantRing, shared, tops, ml + warp * R, warp, lane);
+    __syncthreads();
+    // The warps' results: one maximum, sums of the tiles that each scored, outputs of the layer that each applied.  16 threads a row.
+    const long long n_rows = (long long)p.a.n_items * p.a.H;
+    const bool direct = p.a.slots == 1;
+    for (int i = threadIdx.x >> 4; i < u.r.rows * LG; i += W * 2) {
+        const int row = i / LG, y = i % LG, c = threadIdx.x & 15;
+        if (y >= u.r.layers) continue;
+        float l = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) l += ml[w * R + row].y;
+        const long long at = (long long)u.item * p.a.H + u.r.head0 + u.r.row0 + row;
+        if ((!direct || p.a.keep_ml) && c == 0 && y == 0 && u.r.layer0 == 0) p.a.part_ml[u.r.slot * n_rows + at] = make_float2(ml[row].x, l);
+        if (!direct && l == 0.f) continue;                   // the join does not look at it
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < W / LG; ++w) {
+            const float4 x = *reinterpret_cast<const float4*>(attend_smem + (w * LG + y) * kQuantRing + (row * kAtOutLd + c * 4) * 4);
+            o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+        }
+        if (direct) {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            T* dst = reinterpret_cast<T*>(p.a.out) + ((u.r.layer0 + y) * n_rows + at) * kDh + c * 4;
+            if constexpr (P > 1) *reinterpret_cast<float4*>(dst) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+            else *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        } else {
+            *reinterpret_cast<float4*>(p.a.part_o + (((long long)u.r.slot * p.a.n_layers + u.r.layer0 + y) * n_rows + at) * kDh + c * 4) = o;
+        }
+    }
 }
 
 // Scores to weights, where the weights are wanted: grid = (rows, parts of 2048 positions).
