@@ -544,7 +544,7 @@ int32_t san_quant_attn(const san_planes* cache, const san_step_rows* rows, void*
 typedef struct {
     int32_t n_heads, n_kv_heads;
     const float* d_S; int64_t item_stride, row_stride, head_stride;
-    int32_t n_rows; const int32_t* d_rows;
+    int32_t n_rows; const int32_t* d_rows;          /* n_rows 0 .. 2^20 */
     const int32_t* d_ids; const int32_t* d_lens; const int32_t* d_begin;
     int32_t n_items;                      /* at most 65535 */
     int32_t max_len;                      /* host bound on d_lens */

@@ -18,13 +18,15 @@ struct MassParams {
     int* status;
 };
 
-// CTA = (256 / G positions, key head, item): thread = position and every G-th of the (row, head) pairs, whose sums meet in shared
-// memory in a fixed order.
-template <int G>
-__global__ void __launch_bounds__(256) mass_kernel(const __grid_constant__ MassParams p) {
-    constexpr int W = 256 / G;
-    __shared__ float part[G > 1 ? 256 : 1];
-    const int item = blockIdx.z, hk = blockIdx.y, x = threadIdx.x % W, grp = threadIdx.x / W;
+// Bound by reading S once.  A warp sums 32 U positions, U a lane, over every G-th of the (row, query head) pairs, several pairs' loads on
+// their way at once; a CTA is 8 / G such groups of positions of one (key head, item), and the G sums of a position meet in
+// shared memory in a fixed order.  Loads of a warp are 128 bytes on end whatever the strides, so that no alignment is asked for.
+constexpr int kMassThreads = 256;
+template <int G, int U> __host__ __device__ constexpr int mass_positions() { return kMassThreads / G * U; }       // of a CTA
+template <int G, int U>
+__global__ void __launch_bounds__(kMassThreads) mass_kernel(const __grid_constant__ MassParams p) {
+    __shared__ float part[G > 1 ? kMassThreads * U : 1];
+    const int item = blockIdx.z, hk = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = warp % G;
     const int id = p.ids[item], len = p.lens[item], rows = p.rows ? p.rows[item] : p.n_rows, begin = p.begin ? p.begin[item] : len;
     const bool by_id = id < 0 || id >= p.max_ids, by_len = len < 0 || len > p.max_len, by_rows = rows < 0 || rows > p.n_rows;
     if (by_id || by_len || by_rows || begin < 0 || begin > len) {
@@ -33,24 +35,51 @@ __global__ void __launch_bounds__(256) mass_kernel(const __grid_constant__ MassP
                          by_id ? p.max_ids : by_len ? p.max_len : by_rows ? p.n_rows : len);
         return;
     }
-    const int j = blockIdx.x * W + x;
-    if ((long long)blockIdx.x * W >= len) return;
-    const bool mine = j < len;
-    float sum = 0.f;
-    if (mine) {
-        const float* S = p.S + item * p.item_stride + (long long)hk * p.group * p.head_stride + j;
-        for (int r = grp; r < rows; r += G)
-            for (int h = 0; h < p.group; ++h) sum += S[r * p.row_stride + h * p.head_stride];
+    const int base = blockIdx.x * mass_positions<G, U>();
+    if (base >= len) return;
+    const int j0 = base + warp / G * 32 * U + lane;          // this lane's positions: j0 + 32 u
+    float* to = p.mass + ((long long)id * p.Hk + hk) * p.ld + j0;
+    float old[U], sum[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        old[u] = grp == 0 && j0 + 32 * u < begin ? to[32 * u] : 0.f;
+        sum[u] = 0.f;
+    }
+    const float* S = p.S + item * p.item_stride + (long long)hk * p.group * p.head_stride + j0;
+    const int pairs = rows * p.group;
+    // pair k is row k / group, head k % group: kept as an address and a head, which go on by G pairs at a time
+    int head = grp % p.group;
+    const float* src = S + grp / p.group * p.row_stride + head * p.head_stride;
+    const int more = G % p.group;
+    const long long step = G / p.group * p.row_stride + more * p.head_stride, wrap = p.row_stride - p.group * p.head_stride;
+    constexpr int K = G > 1 ? 4 : 2;
+    for (int k0 = grp; k0 < pairs; k0 += K * G) {
+        float x[K][U];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[k][u] = k0 + k * G < pairs && j0 + 32 * u < len ? __ldcs(src + 32 * u) : 0.f;
+            src += step;
+            head += more;
+            if (head >= p.group) { head -= p.group; src += wrap; }
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int u = 0; u < U; ++u) sum[u] += x[k][u];
     }
     if constexpr (G > 1) {
-        part[threadIdx.x] = sum;
+#pragma unroll
+        for (int u = 0; u < U; ++u) part[(warp * U + u) * 32 + lane] = sum[u];
         __syncthreads();
         if (grp != 0) return;
-        for (int k = 1; k < G; ++k) sum += part[k * W + x];
+        for (int k = 1; k < G; ++k)
+#pragma unroll
+            for (int u = 0; u < U; ++u) sum[u] += part[((warp + k) * U + u) * 32 + lane];
     }
-    if (!mine) return;
-    float* to = p.mass + ((long long)id * p.Hk + hk) * p.ld + j;
-    *to = (j < begin ? p.decay * *to : 0.f) + sum;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (j0 + 32 * u < len) to[32 * u] = fmaf(p.decay, old[u], sum[u]);
 }
 
 // ------------------------------------------------------------------------------------------- eviction
@@ -61,8 +90,8 @@ struct EvictParams {
     float* mass; long long ld;
     int* kept; long long ld_kept;
     int* lens_out;
-    int Hk, n_layers, max_ids, cap, n_items, max_len, keep, sink, recent, row_bytes;
-    bool permuted;
+    int Hk, n_layers, max_ids, cap, n_items, max_len, keep, sink, recent;
+    int cluster;                            // CTAs that move the rows of one plane together
     int* list;                              // [item][key head][keep]: rows that stay
     int2* plan;                             // [item][key head]: id and first entry of the list that moves (keep: none)
     int* status;
@@ -75,29 +104,142 @@ __device__ __forceinline__ uint32_t evict_key(float x) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// CTA = (key head, item).  The least mass that stays is found digit by digit (8 bits) from counts; then one pass in order lists the rows
-// and moves the mass.
-static __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const __grid_constant__ EvictParams p) {
+// What both ways to choose begin with: the item's id (-1: skipped and reported; nothing to do where its rows all stay).
+__device__ __forceinline__ int evict_item(const EvictParams& p, int hk, int item, int* len) {
+    const long long panel = (long long)item * p.Hk + hk;
+    const int id = p.ids[item];
+    *len = p.lens[item];
+    const bool by_id = id < 0 || id >= p.max_ids;
+    if (by_id || *len < 0 || *len > p.max_len) {
+        if (threadIdx.x == 0) {
+            if (hk == 0) attend_error(p.status, TAG_EVICT, item, by_id ? id : *len, by_id ? p.max_ids : p.max_len);
+            p.plan[panel] = make_int2(-1, p.keep);
+        }
+        return -1;
+    }
+    if (*len <= p.keep) {
+        for (int i = threadIdx.x; i < *len && p.kept; i += kEvictThreads) p.kept[panel * p.ld_kept + i] = i;
+        if (threadIdx.x == 0) p.plan[panel] = make_int2(id, p.keep);
+        return -1;
+    }
+    return id;
+}
+
+// CTA = (key head, item), up to 32 R rows a warp, whose masses stay in registers (row 32 i + lane of the warp's run in register i).  The least
+// key that stays is found two bits at a time from the top: per turn three counts over all keys, by redux in each warp and one barrier.
+// Ties and places follow from the warps' counts alone.  4096 rows: 3.4 us; counting digits of 8 bits with atomics in shared memory took 18.
+template <int R>
+__global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const __grid_constant__ EvictParams p) {
+    __shared__ int4 counts[2][32];
+    const int hk = blockIdx.x, item = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int len;
+    const int id = evict_item(p, hk, item, &len);
+    asm volatile("griddepcontrol.launch_dependents;");
+    if (id < 0) return;
+    const long long panel = (long long)item * p.Hk + hk;
+    float* mass = p.mass + ((long long)id * p.Hk + hk) * p.ld;
+    const int lo = p.sink, hi = len - p.recent, want = p.keep - p.sink - p.recent;         // of rows lo .. hi - 1
+    const int run = (len + 1023) / 1024 * 32, begin = warp * run + lane;                   // a warp's rows
+    float x[R];
+    uint32_t key[R];                                        // 0: not there, or not in question
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int j = begin + 32 * i;
+        x[i] = 32 * i < run && j < len ? mass[j] : 0.f;
+        key[i] = 32 * i < run && j >= lo && j < hi ? evict_key(x[i]) : 0u;
+    }
+    uint32_t least = 0xffffffffu;                           // nothing is above it
+    if (want > 0) {
+        least = 0;
+        for (int shift = 30; shift >= 0; shift -= 2) {
+            int c[3] = {0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int t = 0; t < 3; ++t) c[t] += key[i] >= (least | (uint32_t)(t + 1) << shift);
+            const int turn = shift >> 1 & 1;
+#pragma unroll
+            for (int t = 0; t < 3; ++t) c[t] = __reduce_add_sync(0xffffffffu, c[t]);
+            if (lane == 0) counts[turn][warp] = make_int4(c[0], c[1], c[2], 0);
+            __syncthreads();
+            const int4 all = counts[turn][lane];
+            const int a = __reduce_add_sync(0xffffffffu, all.x), b = __reduce_add_sync(0xffffffffu, all.y), d = __reduce_add_sync(0xffffffffu, all.z);
+            least |= (uint32_t)(d >= want ? 3 : b >= want ? 2 : a >= want ? 1 : 0) << shift;
+        }
+    }
+    // rows that stay whatever the ties, and rows that tie
+    int sure = 0, tied = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int j = begin + 32 * i;
+        const bool forced = 32 * i < run && j < len && (j < lo || j >= hi);
+        sure += __popc(__ballot_sync(0xffffffffu, forced || key[i] > least));
+        tied += __popc(__ballot_sync(0xffffffffu, key[i] == least));
+    }
+    __syncthreads();
+    if (lane == 0) counts[0][warp] = make_int4(sure, tied, 0, 0);
+    __syncthreads();
+    const int4 mine = counts[0][lane];
+    const int ties = p.keep - __reduce_add_sync(0xffffffffu, mine.x);                       // of them that stay, the lowest first
+    int before = mine.y;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, before, o);
+        if (lane >= o) before += y;
+    }
+    before -= mine.y;
+    const int stays = mine.x + max(0, min(mine.y, ties - before));                          // of warp `lane`
+    int place = stays;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, place, o);
+        if (lane >= o) place += y;
+    }
+    int to = __shfl_sync(0xffffffffu, place - stays, warp), tie = __shfl_sync(0xffffffffu, before, warp);
+    int* list = p.list + panel * p.keep;
+    int* kept = p.kept ? p.kept + panel * p.ld_kept : nullptr;
+    const unsigned below = (1u << lane) - 1;
+    int gone = len;                                         // the first row that goes
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        if (32 * i >= run) break;
+        const int j = begin + 32 * i;
+        const bool forced = j < len && (j < lo || j >= hi), even = key[i] == least;
+        const unsigned tb = __ballot_sync(0xffffffffu, even);
+        const bool stay = forced || key[i] > least || (even && tie + __popc(tb & below) < ties);
+        const unsigned sb = __ballot_sync(0xffffffffu, stay);
+        if (stay) {
+            const int at = to + __popc(sb & below);
+            list[at] = j;
+            if (kept) kept[at] = j;
+            if (at != j) mass[at] = x[i];
+        } else if (j < len) {
+            gone = min(gone, j);
+        }
+        tie += __popc(tb);
+        to += __popc(sb);
+    }
+    gone = __reduce_min_sync(0xffffffffu, gone);
+    if (lane == 0) counts[1][warp].x = gone;
+    __syncthreads();
+    if (warp == 0) {
+        gone = __reduce_min_sync(0xffffffffu, counts[1][lane].x);
+        if (lane == 0) p.plan[panel] = make_int2(id, min(gone, p.keep));
+    }
+}
+
+// Longer ones, read again for every digit of 8 bits and once in order, 1024 rows at a time.
+static __global__ void __launch_bounds__(kEvictThreads) evict_select_long_kernel(const __grid_constant__ EvictParams p) {
     __shared__ int counts[256], warps[2][32];
     __shared__ int digit_s, above_s;
     const int hk = blockIdx.x, item = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int id = p.ids[item], len = p.lens[item];
+    int len;
+    const int id = evict_item(p, hk, item, &len);
+    asm volatile("griddepcontrol.launch_dependents;");
+    if (id < 0) return;
     const long long panel = (long long)item * p.Hk + hk;
-    if (id < 0 || id >= p.max_ids || len < 0 || len > p.max_len) {
-        if (tid == 0) {
-            const bool by_id = id < 0 || id >= p.max_ids;
-            if (hk == 0) attend_error(p.status, TAG_EVICT, item, by_id ? id : len, by_id ? p.max_ids : p.max_len);
-            p.plan[panel] = make_int2(-1, p.keep);
-        }
-        return;
-    }
     int* list = p.list + panel * p.keep;
     int* kept = p.kept ? p.kept + panel * p.ld_kept : nullptr;
-    if (len <= p.keep) {
-        for (int i = tid; i < len && kept; i += kEvictThreads) kept[i] = i;
-        if (tid == 0) p.plan[panel] = make_int2(id, p.keep);
-        return;
-    }
     float* mass = p.mass + ((long long)id * p.Hk + hk) * p.ld;
     const int lo = p.sink, hi = len - p.recent;
     int want = p.keep - p.sink - p.recent;                 // of rows lo .. hi - 1
@@ -178,51 +320,66 @@ static __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(cons
     if (tid == 0) p.plan[panel] = make_int2(id, first_moved);
 }
 
-// CTA = (plane, key head, item): rows in order, a step of them read before any is written.  Entry i of the list is row i or a later one,
-// so that a step never writes over what a later one reads.
-static __global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__ EvictParams p) {
-    const int plane = blockIdx.x, hk = blockIdx.y, item = blockIdx.z;
+// Cluster of C CTAs = (plane, key head, item): rows in order, in steps of up to 2048 pieces of 16 bytes a CTA that are read by all of the
+// cluster before any is written; the next step's reads are on their way meanwhile.  Entry i of the list is row i or a later one, so that a
+// step never writes over what a later one reads.  PIECES: of a row.
+constexpr int kMoveThreads = 256, kMoveU = 8;
+__device__ __forceinline__ void evict_together(bool cluster) {
+    if (cluster) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else {
+        __syncthreads();
+    }
+}
+template <int PIECES>
+__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ EvictParams p) {
+    constexpr int U = kMoveU, T = kMoveThreads, SU = U / PIECES > 0 ? U / PIECES : 1;      // scales of a thread and step (rows of two pieces)
+    const int C = p.cluster, plane = blockIdx.x / C, rank = blockIdx.x % C, hk = blockIdx.y, item = blockIdx.z;
     const long long panel = (long long)item * p.Hk + hk;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int2 plan = p.plan[panel];
-    if (plane == 0 && hk == 0 && threadIdx.x == 0 && plan.x >= 0) p.lens_out[item] = min(p.lens[item], p.keep);
-    if (plan.x < 0 || plan.y >= p.keep) return;
+    if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0 && plan.x >= 0) p.lens_out[item] = min(p.lens[item], p.keep);
+    if (plan.x < 0 || plan.y >= p.keep) return;             // the same for the whole cluster
     const int* list = p.list + panel * p.keep;
     const long long row0 = ((long long)plan.x * p.Hk + hk) * p.cap;
-    char* rows = (plane == 0 ? p.k : p.v + (plane - 1) * p.v_stride) + row0 * p.row_bytes;
-    const int pieces = p.row_bytes / 16, n = (p.keep - plan.y) * pieces;        // (at most 2^28 rows of 16 pieces)
-    constexpr int U = 4;
-    for (int base = 0; base < n; base += 256 * U) {
-        uint4 x[U];
+    char* rows = (plane == 0 ? p.k : p.v + (plane - 1) * p.v_stride) + row0 * (PIECES * 16);
+    uint32_t* scales = PIECES == 2 ? reinterpret_cast<uint32_t*>((plane == 0 ? p.ks : p.vs + (plane - 1) * p.s_stride) + row0 * 4) : nullptr;
+    const int step = C * T * U, n = (p.keep - plan.y) * PIECES, first = rank * T + threadIdx.x;      // pieces (2^26 rows at most)
+    auto place = [&](int row, int c) { return reinterpret_cast<uint4*>(rows + (long long)row * (PIECES * 16) + (PIECES == 8 ? c ^ (row & 7) : c) * 16); };
+    uint4 x[U], next[U];
+    uint32_t sx[SU], snext[SU];
+    auto read = [&](int base, uint4 (&to)[U], uint32_t (&sto)[SU]) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i = base + u * 256 + threadIdx.x;
-            if (i >= n) continue;
-            const int to = plan.y + i / pieces, c = i % pieces, from = list[to];
-            x[u] = *reinterpret_cast<const uint4*>(rows + (long long)from * p.row_bytes + (p.permuted ? c ^ (from & 7) : c) * 16);
+            const int i = base + u * C * T + first;
+            if (i < n) to[u] = *place(list[plan.y + i / PIECES], i % PIECES);
         }
-        __syncthreads();
+        if constexpr (PIECES == 2) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = base + u * 256 + threadIdx.x;
-            if (i >= n) continue;
-            const int to = plan.y + i / pieces, c = i % pieces;
-            *reinterpret_cast<uint4*>(rows + (long long)to * p.row_bytes + (p.permuted ? c ^ (to & 7) : c) * 16) = x[u];
+            for (int u = 0; u < SU; ++u) {
+                const int i = base / PIECES + u * C * T + first;
+                if (i < n / PIECES) sto[u] = scales[list[plan.y + i]];
+            }
         }
-    }
-    if (!p.ks) return;
-    uint32_t* scales = reinterpret_cast<uint32_t*>((plane == 0 ? p.ks : p.vs + (plane - 1) * p.s_stride) + row0 * 4);
-    for (int base = plan.y; base < p.keep; base += 256 * U) {
-        uint32_t x[U];
+    };
+    read(0, x, sx);
+    for (int base = 0; base < n; base += step) {
+        if (base + step < n) read(base + step, next, snext);
+        evict_together(C > 1);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int to = base + u * 256 + threadIdx.x;
-            if (to < p.keep) x[u] = scales[list[to]];
+            const int i = base + u * C * T + first;
+            if (i < n) *place(plan.y + i / PIECES, i % PIECES) = x[u];
+            x[u] = next[u];
         }
-        __syncthreads();
+        if constexpr (PIECES == 2) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int to = base + u * 256 + threadIdx.x;
-            if (to < p.keep) scales[to] = x[u];
+            for (int u = 0; u < SU; ++u) {
+                const int i = base / PIECES + u * C * T + first;
+                if (i < n / PIECES) scales[plan.y + i] = sx[u];
+                sx[u] = snext[u];
+            }
         }
     }
 }

@@ -140,6 +140,12 @@ int32_t launch_quant_rows(const QuantPlan& a, cudaStream_t st) {
     return a.p.a.group <= 4 ? launch_quant_layers<P, 1>(a, st) : launch_quant_layers<P, 2>(a, st);
 }
 
+template <int G, int U>
+int32_t launch_mass(const MassParams& p, cudaStream_t st) {
+    mass_kernel<G, U><<<dim3((unsigned)div_up(p.max_len, mass_positions<G, U>()), (unsigned)p.Hk, (unsigned)p.n_items), kMassThreads, 0, st>>>(p);
+    return cuda_status(cudaGetLastError());
+}
+
 int32_t check_evict(const san_planes* c, const san_evict_args* a) {
     const int32_t rc = check_planes(c, false);
     if (rc != SAN_OK) return rc;
@@ -148,6 +154,19 @@ int32_t check_evict(const san_planes* c, const san_evict_args* a) {
     if (a->n_keep < 1 || a->n_keep > (1 << 26) || a->n_sink < 0 || a->n_recent < 0 || (long long)a->n_sink + a->n_recent > a->n_keep) return SAN_ERR_SHAPE;
     if (a->ld_mass < (a->max_len ? a->max_len : c->cap_len) || (a->d_kept && a->ld_kept < a->n_keep)) return SAN_ERR_SHAPE;
     return SAN_OK;
+}
+template <int PIECES>
+int32_t launch_move(const EvictParams& p, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((1 + p.n_layers) * p.cluster), (unsigned)p.Hk, (unsigned)p.n_items);
+    cfg.blockDim = dim3(kMoveThreads); cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)p.cluster; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    return cuda_status(cudaLaunchKernelEx(&cfg, evict_move_kernel<PIECES>, p));
 }
 size_t evict_plan_bytes(const san_planes* c, const san_evict_args* a) {
     return ((size_t)a->n_items * c->n_kv_heads * sizeof(int2) + 255) / 256 * 256;
@@ -211,7 +230,7 @@ int32_t san_quant_attn(const san_planes* cache, const san_step_rows* rows, void*
 int32_t san_weight_mass(const san_mass_args* a, void* stream) {
     if (!a) return SAN_ERR_NULL;
     if (a->n_heads < 1 || a->n_heads > 1024 || a->n_kv_heads < 1 || a->n_heads % a->n_kv_heads != 0) return SAN_ERR_SHAPE;
-    if (a->n_rows < 0 || a->n_items < 0 || a->n_items > 65535 || a->max_ids < 1 || a->max_len < 0 || a->max_len > (1 << 28)) return SAN_ERR_SHAPE;
+    if (a->n_rows < 0 || a->n_rows > (1 << 20) || a->n_items < 0 || a->n_items > 65535 || a->max_ids < 1 || a->max_len < 0 || a->max_len > (1 << 28)) return SAN_ERR_SHAPE;
     if (a->ld_mass < a->max_len || !std::isfinite(a->decay)) return SAN_ERR_SHAPE;
     if (a->n_items == 0 || a->max_len == 0) return SAN_OK;
     if (!a->d_S || !a->d_ids || !a->d_lens || !a->d_mass) return SAN_ERR_NULL;
@@ -223,11 +242,10 @@ int32_t san_weight_mass(const san_mass_args* a, void* stream) {
     p.n_rows = a->n_rows; p.H = a->n_heads; p.Hk = a->n_kv_heads; p.group = p.H / p.Hk; p.n_items = a->n_items; p.max_ids = a->max_ids;
     p.max_len = a->max_len; p.decay = a->decay; p.status = a->d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool tall = a->n_rows >= 16;
-    const dim3 grid((unsigned)div_up(a->max_len, tall ? 32 : 256), (unsigned)p.Hk, (unsigned)p.n_items);
-    if (tall) mass_kernel<8><<<grid, 256, 0, st>>>(p);
-    else mass_kernel<1><<<grid, 256, 0, st>>>(p);
-    return cuda_status(cudaGetLastError());
+    // Eight warps share a position's pairs where there are many; short rows are cut into more CTAs where there would not be two an SM.
+    if ((long long)a->n_rows * p.group < 16) return launch_mass<1, 8>(p, st);
+    const long long wide = div_up(a->max_len, mass_positions<8, 4>()) * p.Hk * p.n_items;
+    return wide >= 2 * kSms ? launch_mass<8, 4>(p, st) : launch_mass<8, 1>(p, st);
 }
 
 int32_t san_cache_evict_bytes(const san_planes* cache, const san_evict_args* a, size_t* workspace_bytes) {
@@ -248,9 +266,8 @@ int32_t san_cache_evict(const san_planes* cache, const san_evict_args* a, void* 
     const bool q4 = cache->dtype == SAN_Q4;
     EvictParams p;
     std::memset(&p, 0, sizeof(p));
-    p.row_bytes = q4 ? kQuantRow : kDh * (cache->dtype == SAN_BF16 ? 2 : 4);
-    p.permuted = cache->dtype == SAN_BF16;
-    p.k = static_cast<char*>(cache->d_k); p.v = static_cast<char*>(cache->d_v); p.v_stride = cache->v_stride / kDh * p.row_bytes;
+    const int row_bytes = q4 ? kQuantRow : kDh * (cache->dtype == SAN_BF16 ? 2 : 4);
+    p.k = static_cast<char*>(cache->d_k); p.v = static_cast<char*>(cache->d_v); p.v_stride = cache->v_stride / kDh * row_bytes;
     if (q4) {
         p.ks = static_cast<char*>(cache->d_k_scale); p.vs = static_cast<char*>(cache->d_v_scale);
         p.s_stride = cache->v_stride / kDh * 4;
@@ -262,10 +279,16 @@ int32_t san_cache_evict(const san_planes* cache, const san_evict_args* a, void* 
     p.plan = static_cast<int2*>(d_workspace);
     p.list = reinterpret_cast<int*>(static_cast<char*>(d_workspace) + evict_plan_bytes(cache, a));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    evict_select_kernel<<<dim3((unsigned)p.Hk, (unsigned)p.n_items), kEvictThreads, 0, st>>>(p);
+    const dim3 panels((unsigned)p.Hk, (unsigned)p.n_items);
+    if (p.max_len <= 4 * 1024) evict_select_kernel<4><<<panels, kEvictThreads, 0, st>>>(p);
+    else if (p.max_len <= 16 * 1024) evict_select_kernel<16><<<panels, kEvictThreads, 0, st>>>(p);
+    else evict_select_long_kernel<<<panels, kEvictThreads, 0, st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
-    evict_move_kernel<<<dim3((unsigned)(1 + p.n_layers), (unsigned)p.Hk, (unsigned)p.n_items), 256, 0, st>>>(p);
-    return cuda_status(cudaGetLastError());
+    // A plane's rows are moved by as many CTAs as have something to do in a step, up to eight, where there are too few planes for the SMs.
+    const long long pieces = (long long)p.keep * (row_bytes / 16), planes = (long long)(1 + p.n_layers) * p.Hk * p.n_items;
+    p.cluster = 1;
+    while (p.cluster < 8 && planes * p.cluster < 4 * kSms && (long long)p.cluster * kMoveThreads * kMoveU < pieces) p.cluster *= 2;
+    return q4 ? launch_move<2>(p, st) : cache->dtype == SAN_BF16 ? launch_move<8>(p, st) : launch_move<16>(p, st);
 }
 
 }  // extern "C"
