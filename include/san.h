@@ -503,9 +503,10 @@ typedef struct {
  *     keys [n_items][rows_per_item][n_kv_heads][64],   values [n_layers][n_items][rows_per_item][n_kv_heads][64]   of `dtype`
  * (SAN_F32 or SAN_BF16; rows beyond n are neither read nor written).
  * Of a row x:  low = min x rounded down to bf16, step = (max x - low) / 15 rounded up to bf16 and, unless it is 0, to 2^-50 at least,
- * n = (x - low) / step rounded to the nearest, half to even (0 where step is 0), decided in 64 bits: no number is off by more than
+ * n = (x - low) / step rounded to the nearest, half to even (0 where step is 0), of the exact quotients: no number is off by more than
  * step / 2.  A row with a NaN or a number of 2^40 or more reads as NaN.  san_quant_read rounds low + step * n to `dtype`.
- * An id, a number of rows or a place out of range skips the item and is reported. */
+ * An id, a number of rows or a place out of range skips the item and is reported.  (1 + n_layers) * n_items * rows_per_item *
+ * n_kv_heads is below 2^31. */
 int32_t san_quant_append(const san_planes* cache, int32_t dtype, const void* d_k_new, const void* d_v_new, const int32_t* d_ids,
                          const int32_t* d_pos, const int32_t* d_nrows, int32_t n_items, int32_t rows_per_item,
                          int32_t* d_status, void* stream);

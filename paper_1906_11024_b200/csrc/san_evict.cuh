@@ -125,12 +125,55 @@ __device__ __forceinline__ int evict_item(const EvictParams& p, int hk, int item
     return id;
 }
 
-// CTA = (key head, item), up to 32 R rows a warp, whose masses stay in registers (row 32 i + lane of the warp's run in register i).  The least
-// key that stays is found two bits at a time from the top: per turn three counts over all keys, by redux in each warp and one barrier.
-// Ties and places follow from the warps' counts alone.  4096 rows: 3.4 us; counting digits of 8 bits with atomics in shared memory took 18.
+// The least key that stays, and how many rows above it, from counts of one digit of 8 bits after the other: four sets of counts, one for every
+// fourth warp, which halves what atomics on the same count wait for one another (masses share their exponents).  Every thread of the CTA calls
+// this; `each(f)` calls f with the thread's keys (0: not in question).  `want`: of them, 1 or more.
+template <class Each>
+__device__ __forceinline__ uint32_t evict_least(int want, int (&counts)[256][4], int* found, Each each) {
+    const int tid = threadIdx.x, lane = tid & 31, set = tid >> 5 & 3;
+    uint32_t prefix = 0, known = 0;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int i = tid; i < 1024; i += kEvictThreads) (&counts[0][0])[i] = 0;
+        __syncthreads();
+        each([&](uint32_t key) { if (key != 0 && (key & known) == prefix) atomicAdd(&counts[key >> shift & 255][set], 1); });
+        __syncthreads();
+        if (tid < 32) {                                     // the digit at which the count from above reaches `want`
+            int mine[8], sum = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int4 c = *reinterpret_cast<const int4*>(counts[255 - (lane * 8 + k)]);
+                mine[k] = c.x + c.y + c.z + c.w;
+                sum += mine[k];
+            }
+            int before = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, before, o);
+                if (lane >= o) before += y;
+            }
+            before -= sum;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (before < want && before + mine[k] >= want) { found[0] = 255 - (lane * 8 + k); found[1] = before; }
+                before += mine[k];
+            }
+        }
+        __syncthreads();
+        prefix |= (uint32_t)found[0] << shift;
+        known |= 255u << shift;
+        want -= found[1];
+    }
+    return prefix;
+}
+
+// CTA = (key head, item), up to 32 R rows a warp, whose masses stay in registers (row 32 i + lane of the warp's run in register i): read once,
+// and places follow from the warps' counts alone.  Instructions bound it, all of one SM: of a cache of 8 heads and 4096 rows 11 us cold (18 with the counts of every 1024
+// rows added up by every thread, 15 with the key found by comparisons, two bits a turn).
 template <int R>
 __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const __grid_constant__ EvictParams p) {
-    __shared__ int4 counts[2][32];
+    __shared__ __align__(16) int digits[256][4];
+    __shared__ int2 counts[32];
+    __shared__ int found[2], first_gone[32];
     const int hk = blockIdx.x, item = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int len;
     const int id = evict_item(p, hk, item, &len);
@@ -149,24 +192,11 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const __gri
         key[i] = 32 * i < run && j >= lo && j < hi ? evict_key(x[i]) : 0u;
     }
     uint32_t least = 0xffffffffu;                           // nothing is above it
-    if (want > 0) {
-        least = 0;
-        for (int shift = 30; shift >= 0; shift -= 2) {
-            int c[3] = {0, 0, 0};
+    if (want > 0)
+        least = evict_least(want, digits, found, [&](auto f) {
 #pragma unroll
-            for (int i = 0; i < R; ++i)
-#pragma unroll
-                for (int t = 0; t < 3; ++t) c[t] += key[i] >= (least | (uint32_t)(t + 1) << shift);
-            const int turn = shift >> 1 & 1;
-#pragma unroll
-            for (int t = 0; t < 3; ++t) c[t] = __reduce_add_sync(0xffffffffu, c[t]);
-            if (lane == 0) counts[turn][warp] = make_int4(c[0], c[1], c[2], 0);
-            __syncthreads();
-            const int4 all = counts[turn][lane];
-            const int a = __reduce_add_sync(0xffffffffu, all.x), b = __reduce_add_sync(0xffffffffu, all.y), d = __reduce_add_sync(0xffffffffu, all.z);
-            least |= (uint32_t)(d >= want ? 3 : b >= want ? 2 : a >= want ? 1 : 0) << shift;
-        }
-    }
+            for (int i = 0; i < R; ++i) f(key[i]);
+        });
     // rows that stay whatever the ties, and rows that tie
     int sure = 0, tied = 0;
 #pragma unroll
@@ -176,10 +206,9 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const __gri
         sure += __popc(__ballot_sync(0xffffffffu, forced || key[i] > least));
         tied += __popc(__ballot_sync(0xffffffffu, key[i] == least));
     }
+    if (lane == 0) counts[warp] = make_int2(sure, tied);
     __syncthreads();
-    if (lane == 0) counts[0][warp] = make_int4(sure, tied, 0, 0);
-    __syncthreads();
-    const int4 mine = counts[0][lane];
+    const int2 mine = counts[lane];
     const int ties = p.keep - __reduce_add_sync(0xffffffffu, mine.x);                       // of them that stay, the lowest first
     int before = mine.y;
 #pragma unroll
@@ -220,18 +249,18 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const __gri
         to += __popc(sb);
     }
     gone = __reduce_min_sync(0xffffffffu, gone);
-    if (lane == 0) counts[1][warp].x = gone;
+    if (lane == 0) first_gone[warp] = gone;
     __syncthreads();
     if (warp == 0) {
-        gone = __reduce_min_sync(0xffffffffu, counts[1][lane].x);
+        gone = __reduce_min_sync(0xffffffffu, first_gone[lane]);
         if (lane == 0) p.plan[panel] = make_int2(id, min(gone, p.keep));
     }
 }
 
 // Longer ones, read again for every digit of 8 bits and once in order, 1024 rows at a time.
 static __global__ void __launch_bounds__(kEvictThreads) evict_select_long_kernel(const __grid_constant__ EvictParams p) {
-    __shared__ int counts[256], warps[2][32];
-    __shared__ int digit_s, above_s;
+    __shared__ __align__(16) int digits[256][4];
+    __shared__ int found[2], warps[2][32];
     const int hk = blockIdx.x, item = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int len;
     const int id = evict_item(p, hk, item, &len);
@@ -242,47 +271,26 @@ static __global__ void __launch_bounds__(kEvictThreads) evict_select_long_kernel
     int* kept = p.kept ? p.kept + panel * p.ld_kept : nullptr;
     float* mass = p.mass + ((long long)id * p.Hk + hk) * p.ld;
     const int lo = p.sink, hi = len - p.recent;
-    int want = p.keep - p.sink - p.recent;                 // of rows lo .. hi - 1
-    uint32_t prefix = 0, known = 0;                         // digits of the least key that stays
+    const int want = p.keep - p.sink - p.recent;           // of rows lo .. hi - 1
+    uint32_t prefix = 0xffffffffu;                          // the least key that stays
     int ties = 0;                                           // rows of that key that stay, the lowest first
     if (want > 0) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < 256; i += kEvictThreads) counts[i] = 0;
-            __syncthreads();
-            for (int j = lo + tid; j < hi; j += kEvictThreads) {
-                const uint32_t key = evict_key(mass[j]);
-                if ((key & known) == prefix) atomicAdd(&counts[key >> shift & 255], 1);
-            }
-            __syncthreads();
-            if (warp == 0) {                                // the digit at which the count from above reaches `want`
-                int mine[8], sum = 0;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) { mine[k] = counts[255 - (lane * 8 + k)]; sum += mine[k]; }
-                int before = sum;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int y = __shfl_up_sync(0xffffffffu, before, o);
-                    if (lane >= o) before += y;
-                }
-                before -= sum;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    if (before < want && before + mine[k] >= want) { digit_s = 255 - (lane * 8 + k); above_s = before; }
-                    before += mine[k];
-                }
-            }
-            __syncthreads();
-            prefix |= (uint32_t)digit_s << shift;
-            known |= 255u << shift;
-            want -= above_s;
-        }
-        ties = want;
+        prefix = evict_least(want, digits, found, [&](auto f) {
+            for (int j = lo + tid; j < hi; j += kEvictThreads) f(evict_key(mass[j]));
+        });
+        int above = 0;
+        for (int j = lo + tid; j < hi; j += kEvictThreads) above += evict_key(mass[j]) > prefix;
+        above = __reduce_add_sync(0xffffffffu, above);
+        if (lane == 0) warps[0][warp] = above;
+        __syncthreads();
+        ties = want - __reduce_add_sync(0xffffffffu, warps[0][lane]);
+        __syncthreads();
     }
     int n_kept = 0, n_ties = 0, first_moved = p.keep;
     for (int base = 0; base < len; base += kEvictThreads) {
         const int j = base + tid;
         const float x = j < len ? mass[j] : 0.f;
-        const bool forced = j < len && (j < lo || j >= hi), open = j < len && !forced && p.keep > p.sink + p.recent;
+        const bool forced = j < len && (j < lo || j >= hi), open = j < len && !forced;
         const uint32_t key = evict_key(x);
         const bool tie = open && key == prefix;
         const unsigned tb = __ballot_sync(0xffffffffu, tie);
@@ -320,10 +328,10 @@ static __global__ void __launch_bounds__(kEvictThreads) evict_select_long_kernel
     if (tid == 0) p.plan[panel] = make_int2(id, first_moved);
 }
 
-// Cluster of C CTAs = (plane, key head, item): rows in order, in steps of up to 2048 pieces of 16 bytes a CTA that are read by all of the
+// Cluster of C CTAs = (plane, key head, item): rows in order, in steps of up to 1024 pieces of 16 bytes a CTA that are read by all of the
 // cluster before any is written; the next step's reads are on their way meanwhile.  Entry i of the list is row i or a later one, so that a
 // step never writes over what a later one reads.  PIECES: of a row.
-constexpr int kMoveThreads = 256, kMoveU = 8;
+constexpr int kMoveThreads = 512, kMoveU = 2;
 __device__ __forceinline__ void evict_together(bool cluster) {
     if (cluster) {
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");

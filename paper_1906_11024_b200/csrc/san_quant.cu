@@ -36,7 +36,7 @@ int32_t quant_rows(bool append, const san_planes* c, int32_t dtype, const void* 
     if (!k || !v || !ids) return SAN_ERR_NULL;
     if (!aligned(k, 16) || !aligned(v, 16)) return SAN_ERR_SHAPE;
     const long long all = (long long)(1 + c->n_layers) * c->n_kv_heads * n_items;
-    if (all > (1LL << 40) / rows || div_up(all * rows, 32) > 0x7fffffffLL) return SAN_ERR_SHAPE;
+    if (all > 0x7fffffffLL / rows) return SAN_ERR_SHAPE;
     QuantRowsParams p;
     std::memset(&p, 0, sizeof(p));
     p.k = static_cast<char*>(c->d_k); p.v = static_cast<char*>(c->d_v);
@@ -45,6 +45,8 @@ int32_t quant_rows(bool append, const san_planes* c, int32_t dtype, const void* 
     p.k_rows = static_cast<const char*>(k); p.v_rows = static_cast<const char*>(v);
     p.ids = ids; p.pos = pos; p.nrows = nrows; p.n_items = n_items; p.rows = rows; p.Hk = c->n_kv_heads; p.n_layers = c->n_layers;
     p.max_ids = c->max_ids; p.cap = c->cap_len; p.status = status;
+    p.all_rows = (uint32_t)(all * rows); p.layer_rows = (long long)n_items * rows * p.Hk * kDh;
+    p.by_rows.by((uint32_t)rows); p.by_heads.by((uint32_t)p.Hk); p.by_items.by((uint32_t)n_items);
     const unsigned grid = (unsigned)div_up(all * rows, 32);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (append) {
@@ -287,7 +289,7 @@ int32_t san_cache_evict(const san_planes* cache, const san_evict_args* a, void* 
     // A plane's rows are moved by as many CTAs as have something to do in a step, up to eight, where there are too few planes for the SMs.
     const long long pieces = (long long)p.keep * (row_bytes / 16), planes = (long long)(1 + p.n_layers) * p.Hk * p.n_items;
     p.cluster = 1;
-    while (p.cluster < 8 && planes * p.cluster < 4 * kSms && (long long)p.cluster * kMoveThreads * kMoveU < pieces) p.cluster *= 2;
+    while (p.cluster < 8 && planes * p.cluster < 4 * kSms && (long long)p.cluster * kMoveThreads * 2 < pieces) p.cluster *= 2;
     return q4 ? launch_move<2>(p, st) : cache->dtype == SAN_BF16 ? launch_move<8>(p, st) : launch_move<16>(p, st);
 }
 

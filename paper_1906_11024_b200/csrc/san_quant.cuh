@@ -32,12 +32,24 @@ constexpr float kQuantMost = 1.0995116e12f;             // 2^40
 constexpr float kQuantLeastStep = 8.8817842e-16f;       // 2^-50
 
 // ------------------------------------------------------------------------------------------- rows in and out
+// Quotients by a number that the host knows, of numbers below 2^31 (a quotient of 64 bits takes some 80 instructions a thread, more
+// than the row itself): with 2^shift >= d, times = ceil(2^(32 + shift) / d) - 2^32 makes (x + (x times) / 2^32) / 2^shift exact.
+struct QuantDivide {
+    uint32_t times, shift;
+    __host__ void by(uint32_t d) {
+        for (shift = 0; (1ull << shift) < d; ++shift) {}
+        times = (uint32_t)((((1ull << shift) - d) << 32) / d + 1);
+    }
+    __device__ __forceinline__ uint32_t of(uint32_t x) const { return (__umulhi(x, times) + x) >> shift; }
+};
 struct QuantRowsParams {
     char* k; char* v; char* ks; char* vs;
     long long v_stride, s_stride;           // bytes between the layers' planes of codes, of (step, low)
     const char* k_rows; const char* v_rows; // [n_items][rows][Hk][64], [layers] of those
     const int* ids; const int* pos; const int* nrows;
     int n_items, rows, Hk, n_layers, max_ids, cap;
+    uint32_t all_rows; long long layer_rows;                // of all layers; elements of a layer
+    QuantDivide by_rows, by_heads, by_items;
     int* status;
 };
 
@@ -50,12 +62,14 @@ __device__ __forceinline__ float bf16_up_positive(float x) { return __int_as_flo
 // The place of a row of eight lanes (`row`: numbered layer, item, head, position, the last the fastest; layer 0: keys): false if it is
 // none.  src: of the row's 64 numbers in elements, from the keys' or the layer's first.
 struct QuantPlace { int layer; long long src, panel; int pos; };
-__device__ __forceinline__ bool quant_place(const QuantRowsParams& p, long long row, bool reporter, QuantPlace* at) {
-    if (row >= (long long)(1 + p.n_layers) * p.n_items * p.Hk * p.rows) return false;
-    const int r = (int)(row % p.rows); row /= p.rows;
-    const int h = (int)(row % p.Hk); row /= p.Hk;
-    const int item = (int)(row % p.n_items);
-    at->layer = (int)(row / p.n_items);
+__device__ __forceinline__ bool quant_place(const QuantRowsParams& p, uint32_t row, bool reporter, QuantPlace* at) {
+    if (row >= p.all_rows) return false;
+    uint32_t up = p.by_rows.of(row);
+    const int r = (int)(row - up * p.rows);
+    row = up; up = p.by_heads.of(row);
+    const int h = (int)(row - up * p.Hk);
+    at->layer = (int)p.by_items.of(up);
+    const int item = (int)(up - at->layer * p.n_items);
     const int id = p.ids[item], pos = p.pos ? p.pos[item] : 0, n = p.nrows ? p.nrows[item] : p.rows;
     const bool by_id = id < 0 || id >= p.max_ids, by_n = n < 0 || n > p.rows;
     if (by_id || by_n || pos < 0 || pos > p.cap - n) {
@@ -63,21 +77,21 @@ __device__ __forceinline__ bool quant_place(const QuantRowsParams& p, long long 
             attend_error(p.status, TAG_QUANT_ROWS, item, by_id ? id : by_n ? n : pos, by_id ? p.max_ids : by_n ? p.rows : p.cap);
         return false;
     }
-    at->src = (((long long)item * p.rows + r) * p.Hk + h) * kDh;
+    at->src = ((long long)(item * p.rows + r) * p.Hk + h) * kDh + (at->layer > 0 ? (at->layer - 1) * p.layer_rows : 0);
     at->panel = (long long)id * p.Hk + h;
     at->pos = pos + r;
     return r < n;
 }
 
+// A row is eight lanes of eight numbers; a CTA has 32 rows, those of one head on end where there are several.
 template <typename T>
 __global__ void __launch_bounds__(256) quant_append_kernel(const __grid_constant__ QuantRowsParams p) {
     const int c = threadIdx.x & 7;                          // numbers 8 c .. 8 c + 7 of the row
     QuantPlace at;
-    const bool real = quant_place(p, (long long)blockIdx.x * 32 + (threadIdx.x >> 3), c == 0, &at);
+    const bool real = quant_place(p, blockIdx.x * 32 + (threadIdx.x >> 3), c == 0, &at);
     float x[8];
     if (real) {
         const T* src = reinterpret_cast<const T*>(at.layer == 0 ? p.k_rows : p.v_rows) + at.src + c * 8;
-        if (at.layer > 0) src += (long long)(at.layer - 1) * p.n_items * p.rows * p.Hk * kDh;
         if constexpr (sizeof(T) == 2) {
             unpack16<__nv_bfloat16>(ld16_stream(src), x);
         } else {
@@ -100,29 +114,30 @@ __global__ void __launch_bounds__(256) quant_append_kernel(const __grid_constant
         lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
         hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
     }
-    const float low = bf16_down(lo);
-    const double wide = ((double)hi - (double)low) / 15.0;
-    const float step = wide > 0.0 ? fmaxf(bf16_up_positive(__double2float_ru(wide)), kQuantLeastStep) : 0.f;
+    // Rounded up at every stage, which never passes the bf16 number that the exact quotient rounds up to (15 times that is a float32 number).
+    const float low = bf16_down(lo), wide = __fdiv_ru(__fsub_ru(hi, low), 15.f);
+    const float step = wide > 0.f ? fmaxf(bf16_up_positive(wide), kQuantLeastStep) : 0.f;
     const unsigned group = 0xffu << (threadIdx.x & 24);
     finite = (__ballot_sync(0xffffffffu, finite) & group) == group;
     uint32_t codes = 0;
     const float inv = step > 0.f ? 1.f / step : 0.f;        // a step of zero: codes of zero
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float t = (x[i] - low) * inv;
-        float n = rintf(t);
-        if (fabsf(fabsf(t - n) - 0.5f) < 1e-4f) {           // t is within 2e-6 of the quotient; next to a border 64 bits decide
+    for (int i = 7; i >= 0; --i) {
+        const float t = (x[i] - low) * inv, y = t + 12582912.f;         // the sum's low bits are t rounded half to even
+        uint32_t n = __float_as_uint(y) & 15u;
+        if (fabsf(t - (y - 12582912.f)) > 0.4999f) {        // t is within 2e-6 of the quotient; next to a border 64 bits decide
             const float k = floorf(t);
             const double d = (double)x[i] - (double)low, border = ((double)k + 0.5) * (double)step;
-            n = d > border || (d == border && ((int)k & 1)) ? k + 1.f : k;
+            n = (uint32_t)k + (d > border || (d == border && ((int)k & 1)));
         }
-        codes |= (uint32_t)fminf(fmaxf(n, 0.f), 15.f) << (4 * i);
+        codes = codes << 4 | n;
     }
     if (!real) return;
-    char* to = (at.layer == 0 ? p.k : p.v + (at.layer - 1) * p.v_stride) + (at.panel * p.cap + at.pos) * kQuantRow;
+    const long long row = at.panel * p.cap + at.pos;
+    char* to = (at.layer == 0 ? p.k : p.v + (at.layer - 1) * p.v_stride) + row * kQuantRow;
     reinterpret_cast<uint32_t*>(to)[c] = finite ? codes : 0u;
     if (c == 0) {
-        char* scale = (at.layer == 0 ? p.ks : p.vs + (at.layer - 1) * p.s_stride) + (at.panel * p.cap + at.pos) * 4;
+        char* scale = (at.layer == 0 ? p.ks : p.vs + (at.layer - 1) * p.s_stride) + row * 4;
         *reinterpret_cast<uint32_t*>(scale) = finite ? __float_as_uint(step) >> 16 | (__float_as_uint(low) & 0xffff0000u) : 0x7fc07fc0u;
     }
 }
@@ -131,7 +146,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) quant_read_kernel(const __grid_constant__ QuantRowsParams p) {
     const int c = threadIdx.x & 7;
     QuantPlace at;
-    if (!quant_place(p, (long long)blockIdx.x * 32 + (threadIdx.x >> 3), c == 0, &at)) return;
+    if (!quant_place(p, blockIdx.x * 32 + (threadIdx.x >> 3), c == 0, &at)) return;
     const long long row = at.panel * p.cap + at.pos;
     const uint32_t codes = reinterpret_cast<const uint32_t*>((at.layer == 0 ? p.k : p.v + (at.layer - 1) * p.v_stride) + row * kQuantRow)[c];
     const uint32_t scale = *reinterpret_cast<const uint32_t*>((at.layer == 0 ? p.ks : p.vs + (at.layer - 1) * p.s_stride) + row * 4);
@@ -140,7 +155,6 @@ __global__ void __launch_bounds__(256) quant_read_kernel(const __grid_constant__
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = fmaf(step, (float)(codes >> (4 * i) & 15u), low);
     T* to = reinterpret_cast<T*>(const_cast<char*>(at.layer == 0 ? p.k_rows : p.v_rows)) + at.src + c * 8;
-    if (at.layer > 0) to += (long long)(at.layer - 1) * p.n_items * p.rows * p.Hk * kDh;
     if constexpr (sizeof(T) == 2) {
         *reinterpret_cast<uint4*>(to) = pack16<__nv_bfloat16>(x);
     } else {
