@@ -68,7 +68,6 @@ struct AttendParams {
     int p_ctas;                             // CTAs of the prefix units; those of the own rows follow
     int t_lg, t_n_lg;                       // layers per unit of the tensor-core tiles (0: the prefixes are not theirs)
     int slots;                              // partial results per row; 1: units write the outputs
-    int keep_ml;                            // (max, sum) are wanted in the workspace even so
     float* part_o;                          // [slot][layer][item * H + head][64]
     float2* part_ml;                        // [slot][item * H + head]
     int* status;
@@ -107,7 +106,7 @@ __device__ __forceinline__ bool own_ok(const AttendParams& p, int item) {
 // What a unit reads: `n` positions, the first n_sink of them at 0.., the others from `lo` on.
 struct AttendRun {
     const char* k; const char* v;
-    long long row_bytes, v_row_bytes, v_stride;      // between rows (of keys, of values), between layers
+    long long row_bytes, v_stride;
     bool permuted;                          // chunk c of the row at pos sits at c ^ (pos & 7)
     int n_sink, lo, n;                      // visible rows (of the whole sequence)
     int begin, end;                         // this unit's part of them
@@ -149,13 +148,12 @@ template <typename T>
 __device__ __forceinline__ void attend_fill(const AttendRun& u, int begin, int end, int plane, uint32_t slot, int lane) {
     constexpr int RB = AttendGeom<T>::kRowBytes, CPR = RB / 16, RPI = 32 / CPR;     // chunks per row, rows per instruction
     const char* base = plane < 0 ? u.k : u.v + plane * u.v_stride;
-    const long long row_bytes = plane < 0 ? u.row_bytes : u.v_row_bytes;
     const int c_smem = lane % CPR, q = lane / CPR;
     const uint32_t dst = slot + q * RB + c_smem * 16;
     if (begin >= u.n_sink && begin + kAtTile <= end) {       // 32 rows on end
         const int pos = u.lo + begin - u.n_sink + q;
-        const char* src = base + pos * row_bytes;
-        const long long step = RPI * row_bytes;
+        const char* src = base + pos * u.row_bytes;
+        const long long step = RPI * u.row_bytes;
         int off[8 / RPI];                                    // the chunk to fetch: row j * RPI + q has 8 / RPI swizzles
 #pragma unroll
         for (int j = 0; j < 8 / RPI; ++j) {
@@ -171,7 +169,7 @@ __device__ __forceinline__ void attend_fill(const AttendRun& u, int begin, int e
             const bool full = at < end;
             const int pos = !full ? 0 : at < u.n_sink ? at : u.lo + (at - u.n_sink);
             const int c = c_smem ^ (r & 7);
-            const char* src = base + pos * row_bytes + ((u.permuted ? c ^ (pos & 7) : c) << 4);
+            const char* src = base + pos * u.row_bytes + ((u.permuted ? c ^ (pos & 7) : c) << 4);
             cp16(dst + j * RPI * RB, src, full);
         }
     }
@@ -180,8 +178,8 @@ __device__ __forceinline__ void attend_fill(const AttendRun& u, int begin, int e
 
 // Where a unit's row goes, and the meeting of the warps of a unit.  Every warp of the CTA calls this (it
 // holds CTA barriers).  In shared memory: per warp [layers][kAtRows] rows of 64 outputs, kAtOutLd floats
-// apart, at the start of its part of WB bytes, (max, sum) per row at `ml`; warps of a unit are neighbours.
-template <typename T, int WB>
+// apart, at the start of its part, (max, sum) per row at `ml`; warps of a unit are neighbours.
+template <typename T, int N>
 __device__ __forceinline__ void attend_finish(const AttendParams& p, const AttendRun& u, bool active, int wpu, char* smem,
                                               const float2* ml, int warp, int lane) {
     constexpr int R = kAtRows;
@@ -206,14 +204,14 @@ __device__ __forceinline__ void attend_finish(const AttendParams& p, const Atten
         const long long at = (long long)item * p.H + head;
         const bool direct = p.slots == 1;
         const float inv = direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-        if ((!direct || p.keep_ml) && (t & 15) == 0 && u.layer0 == 0) p.part_ml[u.slot * n_rows + at] = make_float2(m, l);
+        if (!direct && (t & 15) == 0 && u.layer0 == 0) p.part_ml[u.slot * n_rows + at] = make_float2(m, l);
         if (!direct && l == 0.f) continue;                                        // the join does not look at it
         for (int y = 0; y < u.layers; ++y) {
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < kAtWarps; ++w) {
                 if (w >= wpu || weight[w] == 0.f) continue;
-                const float4 x = *reinterpret_cast<const float4*>(smem + (w0 + w) * WB + ((y * R + i) * kAtOutLd + (t & 15) * 4) * 4);
+                const float4 x = *reinterpret_cast<const float4*>(smem + (w0 + w) * attend_warp_bytes<T, N>() + ((y * R + i) * kAtOutLd + (t & 15) * 4) * 4);
                 o.x += weight[w] * x.x; o.y += weight[w] * x.y; o.z += weight[w] * x.z; o.w += weight[w] * x.w;
             }
             const int layer = u.layer0 + y;
@@ -506,7 +504,7 @@ __device__ __forceinline__ bool attend_unit(const AttendParams& p, bool prefix, 
         u->rows = min(R, rows - u->row0);
         if (u->rows <= 0) return false;
         u->n = p.plens[g]; u->n_sink = 0; u->lo = 0;
-        u->row_bytes = u->v_row_bytes = (long long)p.Hk * RB;
+        u->row_bytes = (long long)p.Hk * RB;
         const long long at = ((long long)g * p.pcap * p.Hk + hk) * RB;
         u->k = p.pk + at;
         u->v = p.pv + at + u->layer0 * p.pv_stride;
@@ -528,7 +526,7 @@ __device__ __forceinline__ bool attend_unit(const AttendParams& p, bool prefix, 
         u->lo = p.window > 0 ? max(0, len - p.window) : 0;
         u->n_sink = min(p.n_sink, u->lo);
         u->n = u->n_sink + len - u->lo;
-        u->row_bytes = u->v_row_bytes = RB;
+        u->row_bytes = RB;
         const long long at = ((long long)p.ids[item] * p.Hk + hk) * p.cap * RB;
         u->k = p.k + at;
         u->v = p.v + at + u->layer0 * p.v_stride;
@@ -564,7 +562,7 @@ __global__ void __launch_bounds__(kAtWarps * 32) attend_kernel(const __grid_cons
             else attend_warp_f32<LG, 8, N>(p, u, first, step, smem, ml + warp * R, lane);
         }
     }
-    attend_finish<T, attend_warp_bytes<T, N>()>(p, u, active, wpu, attend_smem, ml, warp, lane);
+    attend_finish<T, N>(p, u, active, wpu, attend_smem, ml, warp, lane);
     // Beside the tensor-core tiles of the prefixes, launched before: this kernel is not over before they are, so that the
     // join, which waits for this kernel, finds both.
     if (p.t_lg > 0 && blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");

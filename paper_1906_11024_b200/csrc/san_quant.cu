@@ -105,8 +105,7 @@ int32_t plan_quant(const san_planes* c, const san_step_rows* r, size_t room, Qua
     if (rows > 0x7fffffff || runs * p.o_splits > 0x7fffffffLL) return SAN_ERR_SHAPE;
     p.o_units = (int)(runs * p.o_splits);
     p.slots = p.o_splits;
-    p.keep_ml = r->d_S != nullptr;
-    if (p.slots > 1 || p.keep_ml) out->ml_bytes = partial_ml_bytes(p.slots * rows);
+    if (p.slots > 1 || r->d_S) out->ml_bytes = partial_ml_bytes(p.slots * rows);
     out->bytes = p.slots > 1 ? partial_bytes(p.slots * rows, p.n_layers) : out->ml_bytes;
     out->ctas = p.o_units;
     p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)kDh));
@@ -200,7 +199,7 @@ int32_t san_quant_attn_bytes(const san_planes* cache, const san_step_rows* rows,
     const AttendParams& p = a.p.a;
     const long long n = rows->n_items, c = (long long)p.o_row_tiles * p.Hk * p.n_lg, most = div_up(a.tiles, kQuantStep);
     const long long partial = std::min(n * most, std::max(n, kQuantFills * kQuantCtas / c));
-    *workspace_bytes = most > 1 ? partial_bytes((size_t)partial * p.H, p.n_layers) : p.keep_ml ? partial_ml_bytes((size_t)n * p.H) : 0;
+    *workspace_bytes = most > 1 ? partial_bytes((size_t)partial * p.H, p.n_layers) : rows->d_S ? partial_ml_bytes((size_t)n * p.H) : 0;
     return SAN_OK;
 }
 

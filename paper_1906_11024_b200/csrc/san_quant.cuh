@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(256) quant_read_kernel(const __grid_constant__
 struct QuantParams {
     AttendParams a;                         // k, v: planes of codes
     const char* ks; const char* vs; long long s_stride;
-    float* S; long long ld_s;               // scores, in powers of two, until quant_weights_kernel makes them weights
+    float* S; long long ld_s;               // scores, in powers of two, until quant_weights_kernel makes them weights (by (max, sum) in the workspace)
 };
 struct QuantRun {
     AttendRun r;
@@ -607,7 +607,7 @@ __device__ __forceinline__ bool quant_unit(const QuantParams& p, int index, bool
     r.head0 = hk * a.group; r.row0 = tile * kAtRows; r.rows = min(kAtRows, a.group - r.row0);
     r.layer0 = lg * a.lg; r.layers = min(a.lg, a.n_layers - r.layer0);
     r.n = a.lens[item]; r.n_sink = 0; r.lo = 0; r.permuted = false;
-    r.row_bytes = r.v_row_bytes = kQuantRow;
+    r.row_bytes = kQuantRow;
     const long long panel = ((long long)a.ids[item] * a.Hk + hk) * a.cap;
     r.k = a.k + panel * kQuantRow;
     r.v = a.v + panel * kQuantRow + r.layer0 * a.v_stride;
@@ -648,7 +648,7 @@ __global__ void __launch_bounds__(QuantWarps<LG>::W * 32, P == 1 ? LG == 3 ? 5 :
 #pragma unroll
         for (int w = 0; w < W; ++w) l += ml[w * R + row].y;
         const long long at = (long long)u.item * p.a.H + u.r.head0 + u.r.row0 + row;
-        if ((!direct || p.a.keep_ml) && c == 0 && y == 0 && u.r.layer0 == 0) p.a.part_ml[u.r.slot * n_rows + at] = make_float2(ml[row].x, l);
+        if ((!direct || p.S) && c == 0 && y == 0 && u.r.layer0 == 0) p.a.part_ml[u.r.slot * n_rows + at] = make_float2(ml[row].x, l);
         if (!direct && l == 0.f) continue;                   // the join does not look at it
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll

@@ -7,6 +7,7 @@
 #include "san_attend.cuh"
 #include "san_window.cuh"
 #include "san_tile.cuh"
+#include "san_packed.cuh"
 
 using namespace san;
 
@@ -249,6 +250,17 @@ int32_t launch_window(const WindowParams& p, dim3 grid, cudaStream_t st) {
 }
 
 // ------------------------------------------------------------------------------- packed prompts
+template <int LG>
+int32_t launch_packed(const PackedParams& p, cudaStream_t st) {
+    constexpr int smem = pack_smem_bytes(LG);
+    static bool set[64] = {};
+    const int32_t rc = opt_in((const void*)packed_kernel<LG>, smem, set);
+    if (rc != SAN_OK) return rc;
+    const dim3 grid((unsigned)std::min<long long>(kSms, (long long)p.pairs * p.H * p.n_lg));
+    if (p.list) return launch_after(&packed_kernel<LG>, grid, kPackThreads, st, p, smem);
+    packed_kernel<LG><<<grid, kPackThreads, smem, st>>>(p);
+    return cuda_status(cudaGetLastError());
+}
 struct PackedPlan { long long pairs, list; bool tiles; size_t bytes; };      // pairs of query tiles of all sequences at most; entries of their list
 
 int32_t plan_packed(const san_packed_args* a, PackedPlan* out) {
@@ -264,7 +276,7 @@ int32_t plan_packed(const san_packed_args* a, PackedPlan* out) {
     out->tiles = max_len >= kTileQ;
     out->pairs = a->n_seq == 1 ? div_up(max_len, 2 * kTileQ) : a->n_tokens / (2 * kTileQ) + a->n_seq;
     out->list = out->tiles && a->n_seq > 1 ? out->pairs : 0;
-    out->bytes = out->list ? (size_t)(1 + out->list) * sizeof(int2) : 0;
+    out->bytes = out->list ? (size_t)(1 + out->list) * sizeof(int4) : 0;
     return SAN_OK;
 }
 
@@ -441,36 +453,42 @@ int32_t san_packed_block(const san_packed_args* a, void* d_workspace, size_t wor
         if (!aligned(d_workspace, 256)) return SAN_ERR_SHAPE;
         if (workspace_bytes < plan.bytes) return SAN_ERR_CAPACITY;
     }
-    WindowParams p;
-    std::memset(&p, 0, sizeof(p));
-    p.q = static_cast<const __nv_bfloat16*>(a->d_q); p.k = static_cast<const __nv_bfloat16*>(a->d_k);
-    p.v = static_cast<const __nv_bfloat16*>(a->d_v); p.out = static_cast<__nv_bfloat16*>(a->d_out);
-    p.first = a->d_first; p.n_seq = a->n_seq; p.n_tokens = a->n_tokens; p.status = a->d_status;
-    p.H = a->n_heads; p.Hk = a->n_kv_heads; p.group = a->n_heads / a->n_kv_heads; p.n_layers = a->n_layers;
-    p.max_len = a->max_len ? a->max_len : a->n_tokens;
-    p.window = p.max_len;                       // all of them; no sinks
-    p.q_ld = a->ld_q; p.k_ld = a->ld_k; p.v_ld = a->ld_v; p.out_ld = (long long)a->n_heads * kDh;
-    p.v_layer = a->v_stride; p.out_layer = (long long)a->n_tokens * p.out_ld;
-    const int at_once = plan.tiles ? kTileMaxLayers : 4;
-    p.n_lg = (int)div_up(a->n_layers, at_once);
-    p.lg = (int)div_up(a->n_layers, p.n_lg);
-    p.n_lg = (int)div_up(a->n_layers, p.lg);
-    p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)kDh));
+    const int max_len = a->max_len ? a->max_len : a->n_tokens, at_once = plan.tiles ? kPackLayers : 4;
+    int n_lg = (int)div_up(a->n_layers, at_once);
+    const int lg = (int)div_up(a->n_layers, n_lg);
+    n_lg = (int)div_up(a->n_layers, lg);
+    const float scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)kDh));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const auto* q = static_cast<const __nv_bfloat16*>(a->d_q);
+    const auto* k = static_cast<const __nv_bfloat16*>(a->d_k);
+    const auto* v = static_cast<const __nv_bfloat16*>(a->d_v);
+    auto* out = static_cast<__nv_bfloat16*>(a->d_out);
+    const long long out_ld = (long long)a->n_heads * kDh, out_layer = a->n_tokens * out_ld;
     if (!plan.tiles) {
-        if ((long long)a->n_seq * p.n_lg > 65535) return SAN_ERR_SHAPE;
-        return launch_window<true>(p, dim3((unsigned)div_up(p.max_len, kWinQ), (unsigned)a->n_heads, (unsigned)(a->n_seq * p.n_lg)), st);
+        if ((long long)a->n_seq * n_lg > 65535) return SAN_ERR_SHAPE;
+        WindowParams p;
+        std::memset(&p, 0, sizeof(p));
+        p.q = q; p.k = k; p.v = v; p.out = out;
+        p.first = a->d_first; p.n_seq = a->n_seq; p.n_tokens = a->n_tokens; p.status = a->d_status;
+        p.H = a->n_heads; p.Hk = a->n_kv_heads; p.group = a->n_heads / a->n_kv_heads; p.n_layers = a->n_layers; p.lg = lg; p.n_lg = n_lg;
+        p.max_len = p.window = max_len;         // all of them; no sinks
+        p.q_ld = a->ld_q; p.k_ld = a->ld_k; p.v_ld = a->ld_v; p.out_ld = out_ld; p.v_layer = a->v_stride; p.out_layer = out_layer;
+        p.scale_log2e = scale_log2e;
+        return launch_window<true>(p, dim3((unsigned)div_up(max_len, kWinQ), (unsigned)a->n_heads, (unsigned)(a->n_seq * n_lg)), st);
     }
-    const long long ctas = plan.pairs * a->n_heads * p.n_lg;
-    if (ctas > 0x7fffffffLL) return SAN_ERR_SHAPE;
-    p.pairs = (int)plan.pairs;
+    PackedParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.q = q; p.k = k; p.v = v; p.out = out;
+    p.q_ld = a->ld_q; p.k_ld = a->ld_k; p.v_ld = a->ld_v; p.out_ld = out_ld; p.v_layer = a->v_stride; p.out_layer = out_layer;
+    p.first = a->d_first; p.n_seq = a->n_seq; p.n_tokens = a->n_tokens; p.max_len = max_len; p.pairs = (int)plan.pairs;
+    p.H = a->n_heads; p.group = a->n_heads / a->n_kv_heads; p.n_layers = a->n_layers; p.lg = lg; p.n_lg = n_lg;
+    p.scale_log2e = scale_log2e; p.status = a->d_status;
     if (plan.list > 0) {
-        p.list = static_cast<const int2*>(d_workspace);
-        packed_list_kernel<<<1, 1024, 0, st>>>(p, static_cast<int2*>(d_workspace));
+        p.list = static_cast<const int4*>(d_workspace);
+        packed_list_kernel<<<1, 1024, 0, st>>>(p, static_cast<int4*>(d_workspace));
         if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
     }
-    const dim3 grid((unsigned)ctas);
-    return p.lg == 1 ? launch_tiles<TilePacked, 1>(p, grid, st) : launch_tiles<TilePacked, 2>(p, grid, st);
+    return lg == 1 ? launch_packed<1>(p, st) : launch_packed<2>(p, st);
 }
 
 }  // extern "C"

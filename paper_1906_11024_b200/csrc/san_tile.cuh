@@ -151,7 +151,7 @@ __device__ __forceinline__ float tile_max3(float a, float b, float c) {
 // What a CTA works on.  Visible keys are numbered 0 .. end - 1: the first ns of them are rows 0.., the others rows lo...
 struct TileWork {
     const char* k; const char* v;
-    long long k_bytes, v_bytes, v_stride;   // bytes between rows, between layers
+    long long row_bytes, v_stride;          // bytes between rows, between layers
     int ns, lo, begin, end;
     int rows, layer0, layers;               // query rows, up to two tiles of them
 };
@@ -182,43 +182,27 @@ struct TileRange {
     __device__ __forceinline__ bool whole(int t) const { return t >= whole_first && t < whole_end; }
 };
 
-template <class Mode, int WARPS> __device__ __noinline__ void tile_rows_again(const WindowParams& p, char* smem, const uint32_t* again_s);
+template <int WARPS> __device__ __noinline__ void tile_rows_again(const WindowParams& p, char* smem, const uint32_t* again_s);
 
 // ---- windowed prompts: CTA = (query tiles, head, sequence, layer group), longest prompts' ends first; CTAs from
-// `whole` on take one tile each of the pairs that are left (see launch_tiles of the host side).  Packed sequences have a
-// list of their pairs instead.
-template <bool PACKED> struct TileSequence {
+// `whole` on take one tile each of the pairs that are left (see launch_tiles of the host side)
+struct TileWindow {
     static constexpr int kRegs = 168;
     const WindowParams& p;
     int seq, head, a0, len;
-    long long token0;
     __device__ __forceinline__ bool work(TileWork* w) {
-        int index = blockIdx.x, half = -1, pair;
-        if constexpr (PACKED) {
-            const int layer_group = index % p.n_lg; index /= p.n_lg;
-            head = index % p.H; index /= p.H;
-            w->layer0 = layer_group * p.lg;
-            if (p.list) {
-                if (index >= p.list[0].x) return false;
-                const int2 e = p.list[1 + index];
-                seq = e.x; pair = e.y;
-            } else {                                                    // one sequence: nothing to sort
-                seq = 0; pair = p.pairs - 1 - index;
-            }
-            token0 = window_sequence<true>(p, seq, &len, !p.list && blockIdx.x == 0 && threadIdx.x == 0);
-        } else {
-            if (index >= p.whole) {
-                half = (index - p.whole) & 1;
-                index = p.whole + (index - p.whole) / 2;
-            }
-            const int layer_group = index % p.n_lg; index /= p.n_lg;
-            head = index % p.H; index /= p.H;
-            seq = index % p.n_seq;
-            pair = p.pairs - 1 - index / p.n_seq;
-            w->layer0 = layer_group * p.lg;
-            token0 = window_sequence<false>(p, seq, &len, false);
+        int index = blockIdx.x, half = -1;
+        if (index >= p.whole) {
+            half = (index - p.whole) & 1;
+            index = p.whole + (index - p.whole) / 2;
         }
+        const int layer_group = index % p.n_lg; index /= p.n_lg;
+        head = index % p.H; index /= p.H;
+        seq = index % p.n_seq;
+        const int pair = p.pairs - 1 - index / p.n_seq;
+        w->layer0 = layer_group * p.lg;
         w->layers = min(p.lg, p.n_layers - w->layer0);
+        len = max(0, min(p.lens[seq], p.max_len));
         a0 = pair * 2 * kTileQ + (half > 0 ? kTileQ : 0);
         if (a0 >= len) return false;
         w->rows = min(half < 0 ? 2 * kTileQ : kTileQ, len - a0);
@@ -226,14 +210,15 @@ template <bool PACKED> struct TileSequence {
         w->ns = min(p.n_sink, w->lo);
         w->begin = 0;
         w->end = w->ns + a0 + w->rows - w->lo;
-        w->k_bytes = p.k_ld * 2; w->v_bytes = p.v_ld * 2;
+        const long long at = ((long long)seq * p.cap * p.Hk + head / p.group) * 128;
+        w->row_bytes = (long long)p.Hk * 128;
         w->v_stride = p.v_layer * 2;
-        w->k = reinterpret_cast<const char*>(p.k + token0 * p.k_ld + head / p.group * kDh);
-        w->v = reinterpret_cast<const char*>(p.v + token0 * p.v_ld + head / p.group * kDh) + w->layer0 * w->v_stride;
+        w->k = reinterpret_cast<const char*>(p.k) + at;
+        w->v = reinterpret_cast<const char*>(p.v) + at + w->layer0 * w->v_stride;
         return true;
     }
     __device__ __forceinline__ const uint4* query(int i) const {
-        return reinterpret_cast<const uint4*>(p.q + (token0 + a0 + i) * p.q_ld + head * kDh);
+        return reinterpret_cast<const uint4*>(p.q + (((long long)seq * p.cap + a0 + i) * p.H + head) * kDh);
     }
     __device__ __forceinline__ TileRange range(const TileWork& w, int x) const {
         const int first = a0 + x * kTileQ, last = min(first + kTileQ, a0 + w.rows) - 1;      // rows of the tile
@@ -258,7 +243,7 @@ template <bool PACKED> struct TileSequence {
         const bool mine = i < w.rows;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         bool odd = false;
-        __nv_bfloat16* dst = p.out + (token0 + a0 + i) * p.out_ld + head * kDh;
+        __nv_bfloat16* dst = p.out + (((long long)seq * p.cap + a0 + i) * p.H + head) * kDh;
 #pragma unroll
         for (int y = 0; y < LG; ++y) {
             if (y >= w.layers) break;
@@ -284,72 +269,27 @@ template <bool PACKED> struct TileSequence {
     template <int WARPS> __device__ __forceinline__ void again(char* smem, const uint32_t* again_s) const {
         uint32_t any = 0;
         for (int k = 0; k < 2 * kTileQ / 32; ++k) any |= again_s[k];
-        if (any) tile_rows_again<TileSequence, WARPS>(p, smem, again_s);
+        if (any) tile_rows_again<WARPS>(p, smem, again_s);
     }
-    __device__ __forceinline__ void failed() const {
-        if constexpr (PACKED) {
-            if (p.status && atomicCAS(&p.status[0], 0, (int)SAN_ERR_TIMEOUT) == 0) { p.status[1] = TAG_PACKED; p.status[2] = seq; }
-        }
-    }
+    __device__ __forceinline__ void failed() const {}
 };
-using TileWindow = TileSequence<false>;
-using TilePacked = TileSequence<true>;
-
-// The list of packed sequences' pairs of tiles, those with the most keys first: entry i + 1 is pair .y of sequence .x, entry 0 has
-// their number.  One CTA: pairs are counted by their place in the sequence (all beyond 2047 together), the counts summed from
-// above.  Sequences that are not in order have no pairs (and are reported).
-constexpr int kPackedBins = 2048;
-static __global__ void __launch_bounds__(1024) packed_list_kernel(const __grid_constant__ WindowParams p, int2* list) {
-    __shared__ int bins[kPackedBins], sums[32];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    bins[tid] = bins[tid + 1024] = 0;
-    __syncthreads();
-    for (int s = tid; s < p.n_seq; s += 1024) {
-        int len;
-        window_sequence<true>(p, s, &len, true);
-        for (int i = 0; i * 2 * kTileQ < len; ++i) atomicAdd(&bins[min(i, kPackedBins - 1)], 1);
-    }
-    __syncthreads();
-    const int hi = kPackedBins - 1 - 2 * tid, a = bins[hi], b = bins[hi - 1];
-    int before = a + b;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, before, o);
-        if (lane >= o) before += y;
-    }
-    if (lane == 31) sums[warp] = before;
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) before += sums[w];
-    if (tid == 1023) list[0] = make_int2(min(before, p.pairs), 0);
-    bins[hi] = before - a - b;
-    bins[hi - 1] = before - b;
-    __syncthreads();
-    for (int s = tid; s < p.n_seq; s += 1024) {
-        int len;
-        window_sequence<true>(p, s, &len, false);
-        for (int i = 0; i * 2 * kTileQ < len; ++i) {
-            const int at = atomicAdd(&bins[min(i, kPackedBins - 1)], 1);
-            if (at < p.pairs) list[1 + at] = make_int2(s, i);       // more than there can be: sequences that overlap
-            else if (p.status) record_error(p.status, TAG_PACKED, s, at, p.pairs);
-        }
-    }
-}
 
 // Row a of (sequence, head), one layer, by one warp: over the rows that are seen and no others, as a row of a decode step.
 constexpr int kAgainBytes = 2 * kAtTile * 128;                          // of shared memory for a warp
-__device__ __forceinline__ void tile_row_again(const WindowParams& p, long long token0, int head, int layer, int a, char* smem, int lane) {
+__device__ __forceinline__ void tile_row_again(const WindowParams& p, int seq, int head, int layer, int a, char* smem, int lane) {
     struct { const char* q; int H, group; float scale_log2e; } rows;
-    rows.q = reinterpret_cast<const char*>(p.q + (token0 + a) * p.q_ld + head * kDh);      // the row itself: item and head 0
-    rows.H = 1; rows.group = 1; rows.scale_log2e = p.scale_log2e;
+    rows.q = reinterpret_cast<const char*>(p.q + (long long)seq * p.cap * p.H * kDh);
+    rows.H = p.H; rows.group = 1; rows.scale_log2e = p.scale_log2e;
+    const long long kv = ((long long)seq * p.cap * p.Hk + head / p.group) * kDh;
     AttendRun u;
-    u.k = reinterpret_cast<const char*>(p.k + token0 * p.k_ld + head / p.group * kDh);
-    u.v = reinterpret_cast<const char*>(p.v + layer * p.v_layer + token0 * p.v_ld + head / p.group * kDh);
-    u.row_bytes = p.k_ld * 2; u.v_row_bytes = p.v_ld * 2; u.v_stride = 0; u.permuted = false;
+    u.k = reinterpret_cast<const char*>(p.k + kv);
+    u.v = reinterpret_cast<const char*>(p.v + layer * p.v_layer + kv);
+    u.row_bytes = (long long)p.Hk * 128; u.v_stride = 0; u.permuted = false;
     u.lo = max(0, a - p.window + 1);
     u.n_sink = min(p.n_sink, u.lo);
     u.n = u.n_sink + a + 1 - u.lo;
     u.begin = 0; u.end = u.n;
-    u.item0 = 0; u.row0 = 0; u.rows = 1; u.head0 = 0;
+    u.item0 = a; u.row0 = 0; u.rows = 1; u.head0 = head;
     u.layer0 = layer; u.layers = 1; u.slot = 0;
     float2* ml = reinterpret_cast<float2*>(smem + kAtTile * 128);
     __syncwarp();                                                       // the row before has been written
@@ -357,7 +297,7 @@ __device__ __forceinline__ void tile_row_again(const WindowParams& p, long long 
     __syncwarp();
     const float l = ml[0].y, inv = l == 0.f ? 0.f : 1.f / l;
     const float2 o = *reinterpret_cast<const float2*>(smem + lane * 8);
-    *reinterpret_cast<uint32_t*>(p.out + layer * p.out_layer + (token0 + a) * p.out_ld + head * kDh + lane * 2) = pack_bf16(o.x * inv, o.y * inv);
+    *reinterpret_cast<uint32_t*>(p.out + layer * p.out_layer + (((long long)seq * p.cap + a) * p.H + head) * kDh + lane * 2) = pack_bf16(o.x * inv, o.y * inv);
 }
 
 // All threads of a CTA that is done: rows that came out as NaN (again_s, a bit for each) are computed again where a value that
@@ -365,9 +305,9 @@ __device__ __forceinline__ void tile_row_again(const WindowParams& p, long long 
 // are NaN by what they see stay: with one NaN among the sinks those are all rows of a prompt.  2 x 8192 positions, window 1024, 8
 // heads, 2 layers: 105 us; with a NaN value among the sinks 0.16 ms, in the middle 1.4, in every row 4.5 (one position
 // after the other for every row that is NaN took 198, 52 and 198).
-template <class Mode, int WARPS> __device__ __noinline__ void tile_rows_again(const WindowParams& p, char* smem, const uint32_t* again_s) {
+template <int WARPS> __device__ __noinline__ void tile_rows_again(const WindowParams& p, char* smem, const uint32_t* again_s) {
     static_assert(WARPS <= kTileThreads / 32, "warps");
-    Mode mode{p};
+    TileWindow mode{p};
     TileWork w;
     mode.work(&w);
     bool spoiled = false;
@@ -380,7 +320,7 @@ template <class Mode, int WARPS> __device__ __noinline__ void tile_rows_again(co
             for (int i = threadIdx.x; i < w.layers * kTileK * 8; i += kTileThreads) {
                 const int n = t * kTileK + (i >> 3) % kTileK, y = i / (kTileK * 8), b = n < w.ns ? n : w.lo + n - w.ns;
                 if (n >= w.end || (b <= first && (b < p.n_sink || b > last - p.window))) continue;      // none, or seen by all
-                const uint4 v = *reinterpret_cast<const uint4*>(w.v + y * w.v_stride + b * w.v_bytes + (i & 7) * 16);
+                const uint4 v = *reinterpret_cast<const uint4*>(w.v + y * w.v_stride + b * w.row_bytes + (i & 7) * 16);
                 const uint32_t e = 0x7f80u;                             // an exponent of all ones: no finite number
                 for (const uint32_t z : {v.x, v.y, v.z, v.w}) spoiled |= (z & e) == e || (z >> 16 & e) == e;
             }
@@ -392,7 +332,7 @@ template <class Mode, int WARPS> __device__ __noinline__ void tile_rows_again(co
     for (int k = 0; k < 2 * kTileQ / 32; ++k)
         for (uint32_t rows = again_s[k]; rows; rows &= rows - 1, ++n)
             for (int y = 0; y < w.layers && n % WARPS == warp; ++y)
-                tile_row_again(p, mode.token0, mode.head, w.layer0 + y, mode.a0 + 32 * k + __ffs(rows) - 1, smem + warp * kAgainBytes, lane);
+                tile_row_again(p, mode.seq, mode.head, w.layer0 + y, mode.a0 + 32 * k + __ffs(rows) - 1, smem + warp * kAgainBytes, lane);
 }
 
 // ---- shared prefixes: units as in attend_unit, 128 query rows and runs of p_span chunks
@@ -421,7 +361,7 @@ struct TilePrefix {
         w->begin = min(split * p.p_span * kTileK, p.plens[g]);
         w->end = min(w->begin + p.p_span * kTileK, p.plens[g]);
         const long long at = ((long long)g * p.pcap * p.Hk + hk) * 128;
-        w->k_bytes = w->v_bytes = (long long)p.Hk * 128;
+        w->row_bytes = (long long)p.Hk * 128;
         w->v_stride = p.pv_stride;
         w->k = p.pk + at;
         w->v = p.pv + at + w->layer0 * p.pv_stride;
@@ -562,11 +502,11 @@ __global__ void __maxnreg__(Mode::kRegs) tile_kernel(const __grid_constant__ Par
         static_assert(kTileLoaders == 96, "rows of a thread");
         const int r0 = (threadIdx.x - 2 * kTileQ) >> 3, c = threadIdx.x & 7;
         const uint32_t sw0 = (uint32_t)(r0 * 128 + ((c ^ (r0 & 7)) << 4)), sw1 = (uint32_t)(r0 * 128 + ((c ^ ((r0 + 4) & 7)) << 4));
-        auto copy = [&](const char* src, long long row_bytes, uint32_t dst, int c0) {
-            const long long step = 12 * row_bytes;
+        const long long step = 12 * w.row_bytes;
+        auto copy = [&](const char* src, uint32_t dst, int c0) {
             const int first = c0 + r0;
             if (c0 >= w.ns && c0 + kTileK <= w.end) {                   // rows on end
-                const char* at = src + (long long)(w.lo + first - w.ns) * row_bytes + (c << 4);
+                const char* at = src + (long long)(w.lo + first - w.ns) * w.row_bytes + (c << 4);
 #pragma unroll
                 for (int j = 0; j < kRows; ++j, at += step)
                     if (r0 + 12 * j < kTileK) cp16(dst + (uint32_t)(j * 12 * 128) + (j & 1 ? sw1 : sw0), at, true);
@@ -576,7 +516,7 @@ __global__ void __maxnreg__(Mode::kRegs) tile_kernel(const __grid_constant__ Par
                     const int n = first + j * 12;
                     const bool full = n < w.end;
                     const int pos = !full ? 0 : n < w.ns ? n : w.lo + n - w.ns;
-                    if (r0 + 12 * j < kTileK) cp16(dst + (uint32_t)(j * 12 * 128) + (j & 1 ? sw1 : sw0), src + pos * row_bytes + (c << 4), full);
+                    if (r0 + 12 * j < kTileK) cp16(dst + (uint32_t)(j * 12 * 128) + (j & 1 ? sw1 : sw0), src + pos * w.row_bytes + (c << 4), full);
                 }
             }
         };
@@ -587,10 +527,10 @@ __global__ void __maxnreg__(Mode::kRegs) tile_kernel(const __grid_constant__ Par
         for (int t = 0; t < chunks; ++t) {
             const int c0 = w.begin + t * kTileK, ks = t % kTileKSlots, vs = t % kTileVSlots;
             if (t >= kTileKSlots && !tile_wait(&k_free[ks], (uint32_t)(t / kTileKSlots - 1) & 1u, dead)) break;
-            copy(w.k, w.k_bytes, aK + (uint32_t)ks * (kTileK * 128), c0);
+            copy(w.k, aK + (uint32_t)ks * (kTileK * 128), c0);
             landed(&k_full[ks]);
             if (t >= kTileVSlots && !tile_wait(&v_free[vs], (uint32_t)(t / kTileVSlots - 1) & 1u, dead)) break;
-            for (int y = 0; y < w.layers; ++y) copy(w.v + y * w.v_stride, w.v_bytes, aV + (uint32_t)(vs * LG + y) * (kTileK * 128), c0);
+            for (int y = 0; y < w.layers; ++y) copy(w.v + y * w.v_stride, aV + (uint32_t)(vs * LG + y) * (kTileK * 128), c0);
             landed(&v_full[vs]);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");

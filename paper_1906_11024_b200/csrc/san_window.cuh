@@ -28,7 +28,7 @@ struct WindowParams {
     int pairs, whole;                       // tensor-core tiles: pairs of tiles of a sequence, CTAs that take a pair
     float scale_log2e;
     // packed sequences (san_packed_block): sequence s is the tokens first[s] .. first[s + 1] - 1
-    const int* first; const int2* list;     // list: (sequence, pair of tiles) of every CTA, the longest first, behind their number
+    const int* first;
     long long q_ld, k_ld, v_ld, out_ld;     // elements between tokens
     int n_tokens;
     int* status;
