@@ -103,6 +103,7 @@ int32_t plan_quant(const san_planes* c, const san_step_rows* r, size_t room, Qua
         p.o_splits = (int)div_up(tiles, p.o_span);
     }
     if (rows > 0x7fffffff || runs * p.o_splits > 0x7fffffffLL) return SAN_ERR_SHAPE;
+    if ((long long)rows * (p.n_layers + div_up(p.max_len, kQuantWeights)) > 0x7fffffffLL) return SAN_ERR_SHAPE;
     p.o_units = (int)(runs * p.o_splits);
     p.slots = p.o_splits;
     if (p.slots > 1 || r->d_S) out->ml_bytes = partial_ml_bytes(p.slots * rows);
@@ -121,15 +122,14 @@ int32_t launch_quant(const QuantPlan& a, cudaStream_t st) {
     if (rc != SAN_OK) return rc;
     quant_attend_kernel<LG, P, J><<<(unsigned)a.ctas, QuantWarps<LG>::W * 32, smem, st>>>(a.p);
     if (cudaGetLastError() != cudaSuccess) return SAN_ERR_CUDA;
-    const long long rows = (long long)a.p.a.n_items * a.p.a.H;
-    if (a.p.a.slots > 1) {
-        const int groups = a.p.a.slots <= 6 ? 1 : a.p.a.slots <= 12 ? 4 : 16;
-        const dim3 grid((unsigned)div_up(rows, 16 / groups), (unsigned)a.p.a.n_layers);
-        rc = launch_after(groups == 1 ? &attend_join_kernel<T, 1> : groups == 4 ? &attend_join_kernel<T, 4> : &attend_join_kernel<T, 16>, grid, 256, st, a.p.a);
-        if (rc != SAN_OK) return rc;
-    }
-    if (!a.p.S) return SAN_OK;
-    return launch_after(&quant_weights_kernel, dim3((unsigned)rows, (unsigned)div_up(a.p.a.max_len, kQuantWeights)), 256, st, a.p);
+    if (a.p.a.slots == 1 && !a.p.S) return SAN_OK;
+    const int slots = a.p.a.slots, groups = slots <= 6 ? 1 : slots <= 12 ? 4 : 16;
+    QuantParams p = a.p;
+    const long long rows = (long long)p.a.n_items * p.a.H;
+    p.join_ctas = slots > 1 ? (int)(div_up(rows, 16 / groups) * p.a.n_layers) : 0;
+    p.parts = p.S ? (int)div_up(p.a.max_len, kQuantWeights) : 0;
+    const dim3 grid((unsigned)(p.join_ctas + rows * p.parts));
+    return launch_after(groups == 1 ? &quant_finish_kernel<T, 1> : groups == 4 ? &quant_finish_kernel<T, 4> : &quant_finish_kernel<T, 16>, grid, 256, st, p);
 }
 template <int P, int J>
 int32_t launch_quant_layers(const QuantPlan& a, cudaStream_t st) {

@@ -57,7 +57,16 @@ __device__ __forceinline__ float bf16_down(float x) {       // of a finite x: th
     const int b = __float_as_int(x);
     return __int_as_float((b >= 0 ? b : b + 0xffff) & 0xffff0000);
 }
-__device__ __forceinline__ float bf16_up_positive(float x) { return __int_as_float((__float_as_int(x) + 0xffff) & 0xffff0000); }
+__device__ __forceinline__ float quant_min3(float a, float b, float c) {        // NaN if one is
+    float d;
+    asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float quant_max3(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 
 // The place of a row of eight lanes (`row`: numbered layer, item, head, position, the last the fastest; layer 0: keys): false if it is
 // none.  src: of the row's 64 numbers in elements, from the keys' or the layer's first.
@@ -102,43 +111,51 @@ __global__ void __launch_bounds__(256) quant_append_kernel(const __grid_constant
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = 0.f;
     }
-    float lo = x[0], hi = x[0];
-    bool finite = true;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]);
-        finite &= fabsf(x[i]) < kQuantMost;
-    }
+    float lo = quant_min3(x[0], x[1], x[2]), hi = quant_max3(x[0], x[1], x[2]);
+    lo = quant_min3(quant_min3(lo, x[3], x[4]), x[5], quant_min3(x[6], x[7], lo));
+    hi = quant_max3(quant_max3(hi, x[3], x[4]), x[5], quant_max3(x[6], x[7], hi));
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        lo = quant_min3(lo, lo, __shfl_xor_sync(0xffffffffu, lo, o));
+        hi = quant_max3(hi, hi, __shfl_xor_sync(0xffffffffu, hi, o));
     }
-    // Rounded up at every stage, which never passes the bf16 number that the exact quotient rounds up to (15 times that is a float32 number).
-    const float low = bf16_down(lo), wide = __fdiv_ru(__fsub_ru(hi, low), 15.f);
-    const float step = wide > 0.f ? fmaxf(bf16_up_positive(wide), kQuantLeastStep) : 0.f;
-    const unsigned group = 0xffu << (threadIdx.x & 24);
-    finite = (__ballot_sync(0xffffffffu, finite) & group) == group;
+    const bool held = -lo < kQuantMost && hi < kQuantMost;  // (false for NaN)
+    // step: the least bf16 number b with 15 b >= hi - low.  The product is exact, and the difference may be rounded up, since 15 b is a
+    // float32 number.  A product with a little less than 1 / 15, cut off, is that, the one below or two below.
+    const float low = bf16_down(lo), wide = __fsub_ru(hi, low);
+    float step = __int_as_float(__float_as_int(wide * 0.0666666627f) & 0xffff0000);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (15.f * step < wide) step = __int_as_float(__float_as_int(step) + 0x10000);
+    step = wide > 0.f ? fmaxf(step, kQuantLeastStep) : 0.f;
+    const float inv = step > 0.f ? __fdividef(1.f, step) : 0.f;         // a step of zero: codes of zero
     uint32_t codes = 0;
-    const float inv = step > 0.f ? 1.f / step : 0.f;        // a step of zero: codes of zero
+    float off = 0.f;                                        // the furthest from a whole number
 #pragma unroll
     for (int i = 7; i >= 0; --i) {
         const float t = (x[i] - low) * inv, y = t + 12582912.f;         // the sum's low bits are t rounded half to even
-        uint32_t n = __float_as_uint(y) & 15u;
-        if (fabsf(t - (y - 12582912.f)) > 0.4999f) {        // t is within 2e-6 of the quotient; next to a border 64 bits decide
-            const float k = floorf(t);
-            const double d = (double)x[i] - (double)low, border = ((double)k + 0.5) * (double)step;
-            n = (uint32_t)k + (d > border || (d == border && ((int)k & 1)));
+        off = fmaxf(off, fabsf(t - (y - 12582912.f)));
+        codes = codes << 4 | (__float_as_uint(y) & 15u);
+    }
+    if (off > 0.4999f && held) {                            // t is within 1e-5 of the quotient; next to a border 64 bits decide
+        codes = 0;
+#pragma unroll
+        for (int i = 7; i >= 0; --i) {
+            const double d = (double)x[i] - (double)low;
+            const float k = fminf(floorf((x[i] - low) * inv), 15.f);
+            // k may be one too large or too small itself where the quotient is a whole number
+            const double border = ((double)k + 0.5) * (double)step;
+            const uint32_t n = (uint32_t)k + (d > border || (d == border && ((int)k & 1)));
+            codes = codes << 4 | min(n, 15u);
         }
-        codes = codes << 4 | n;
     }
     if (!real) return;
     const long long row = at.panel * p.cap + at.pos;
     char* to = (at.layer == 0 ? p.k : p.v + (at.layer - 1) * p.v_stride) + row * kQuantRow;
-    reinterpret_cast<uint32_t*>(to)[c] = finite ? codes : 0u;
+    reinterpret_cast<uint32_t*>(to)[c] = held ? codes : 0u;
     if (c == 0) {
         char* scale = (at.layer == 0 ? p.ks : p.vs + (at.layer - 1) * p.s_stride) + row * 4;
-        *reinterpret_cast<uint32_t*>(scale) = finite ? __float_as_uint(step) >> 16 | (__float_as_uint(low) & 0xffff0000u) : 0x7fc07fc0u;
+        *reinterpret_cast<uint32_t*>(scale) = held ? __float_as_uint(step) >> 16 | (__float_as_uint(low) & 0xffff0000u) : 0x7fc07fc0u;
     }
 }
 
@@ -167,7 +184,8 @@ __global__ void __launch_bounds__(256) quant_read_kernel(const __grid_constant__
 struct QuantParams {
     AttendParams a;                         // k, v: planes of codes
     const char* ks; const char* vs; long long s_stride;
-    float* S; long long ld_s;               // scores, in powers of two, until quant_weights_kernel makes them weights (by (max, sum) in the workspace)
+    float* S; long long ld_s;               // scores, in powers of two, until quant_finish_kernel makes them weights (by (max, sum) in the workspace)
+    int join_ctas, parts;                   // of quant_finish_kernel: CTAs that join partial results, parts of a row of S
 };
 struct QuantRun {
     AttendRun r;
@@ -667,26 +685,76 @@ __global__ void __launch_bounds__(QuantWarps<LG>::W * 32, P == 1 ? LG == 3 ? 5 :
     }
 }
 
-// Scores to weights, where the weights are wanted: grid = (rows, parts of 2048 positions).
+// Behind the runs of all units: partial results of a row and layer added up (16 threads for its outputs, four each, times G groups
+// that take every G-th result), and scores made weights where they are wanted (a CTA for 2048 positions of a row), side by side.
 constexpr int kQuantWeights = 2048;
-static __global__ void __launch_bounds__(256) quant_weights_kernel(const __grid_constant__ QuantParams p) {
-    const long long at = blockIdx.x, n_rows = (long long)p.a.n_items * p.a.H;
-    const int item = (int)(at / p.a.H);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (!own_ok(p.a, item)) return;
-    const int begin = blockIdx.y * kQuantWeights, end = min(begin + kQuantWeights, p.a.lens[item]);
-    if (begin >= end) return;
-    float m = -INFINITY, l = 0.f;
-    for (int s = 0; s < p.a.slots; ++s) {
-        const float2 x = __ldcg(p.a.part_ml + s * n_rows + at);
-        if (x.y == 0.f) continue;
-        const float m_new = fmaxf(m, x.x);
-        l = l * (m == m_new ? 1.f : exp2f(m - m_new)) + x.y * (x.x == m_new ? 1.f : exp2f(x.x - m_new));
-        m = m_new;
+template <typename T, int G>
+__global__ void __launch_bounds__(256) quant_finish_kernel(const __grid_constant__ QuantParams p) {
+    __shared__ float4 s_o[G > 1 ? 256 : 1];
+    __shared__ float2 s_ml[G > 1 ? 256 : 1];
+    const AttendParams& a = p.a;
+    const long long n_rows = (long long)a.n_items * a.H;
+    if (blockIdx.x >= (unsigned)p.join_ctas) {
+        const unsigned index = blockIdx.x - p.join_ctas;
+        const long long at = index / p.parts;
+        const int item = (int)(at / a.H), begin = (int)(index % p.parts) * kQuantWeights;
+        const bool good = own_ok(a, item);
+        const int end = good ? min(begin + kQuantWeights, a.lens[item]) : 0;
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (begin >= end) return;
+        float m = -INFINITY, l = 0.f;
+        for (int s = 0; s < a.slots; ++s) {
+            const float2 x = __ldcg(a.part_ml + s * n_rows + at);
+            if (x.y == 0.f) continue;
+            const float m_new = fmaxf(m, x.x);
+            l = l * (m == m_new ? 1.f : exp2f(m - m_new)) + x.y * (x.x == m_new ? 1.f : exp2f(x.x - m_new));
+            m = m_new;
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l, base = m == -INFINITY ? 0.f : m;
+        float* S = p.S + at * p.ld_s;
+        constexpr int K = 4;
+        for (int j0 = begin + threadIdx.x; j0 < end; j0 += K * 256) {
+            float x[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k) x[k] = j0 + k * 256 < end ? S[j0 + k * 256] : 0.f;
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (j0 + k * 256 < end) S[j0 + k * 256] = exp2f(x[k] - base) * inv;
+        }
+        return;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l, base = m == -INFINITY ? 0.f : m;
-    float* S = p.S + at * p.ld_s;
-    for (int j = begin + threadIdx.x; j < end; j += 256) S[j] = exp2f(S[j] - base) * inv;
+    const int per_layer = p.join_ctas / a.n_layers, layer = blockIdx.x / per_layer;
+    const int c = threadIdx.x & 15, grp = threadIdx.x / 16 % G;
+    const long long at = (long long)(blockIdx.x % per_layer) * (16 / G) + threadIdx.x / (16 * G);
+    const bool mine = at < n_rows && own_ok(a, (int)(at / a.H));
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float2 x, float4 v) {
+        if (x.y == 0.f) return;                              // nothing seen there: its outputs were not written
+        const float m_new = fmaxf(m, x.x);
+        const float f = m == m_new ? 1.f : exp2f(m - m_new), b = x.x == m_new ? 1.f : exp2f(x.x - m_new);
+        l = l * f + x.y * b;
+        o.x = o.x * f + v.x * b; o.y = o.y * f + v.y * b; o.z = o.z * f + v.z * b; o.w = o.w * f + v.w * b;
+        m = m_new;
+    };
+    if (mine) {
+#pragma unroll 4
+        for (int s = grp; s < a.slots; s += G)
+            add(__ldcg(a.part_ml + s * n_rows + at), __ldcg(reinterpret_cast<const float4*>(a.part_o + (((long long)s * a.n_layers + layer) * n_rows + at) * kDh + c * 4)));
+    }
+    if constexpr (G > 1) {
+        s_o[threadIdx.x] = o;
+        s_ml[threadIdx.x] = make_float2(m, l);
+        __syncthreads();
+        if (grp != 0) return;
+        for (int k = 1; k < G; ++k) add(s_ml[threadIdx.x + k * 16], s_o[threadIdx.x + k * 16]);
+    }
+    if (!mine) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* dst = reinterpret_cast<T*>(a.out) + ((long long)layer * n_rows + at) * kDh + c * 4;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(dst) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    else *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
 }
 
 }  // namespace san
