@@ -116,7 +116,7 @@ int32_t plan_quant(const san_planes* c, const san_step_rows* r, size_t room, Qua
 template <int LG, int P, int J>
 int32_t launch_quant(const QuantPlan& a, cudaStream_t st) {
     using T = typename std::conditional<P == 1, __nv_bfloat16, float>::type;
-    constexpr int smem = quant_smem_bytes<LG, P, J>();
+    constexpr int smem = quant_smem_bytes<LG, J>();
     static bool set[64] = {};
     int32_t rc = opt_in((const void*)quant_attend_kernel<LG, P, J>, smem, set);
     if (rc != SAN_OK) return rc;

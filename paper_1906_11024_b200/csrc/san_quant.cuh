@@ -13,9 +13,9 @@
 // are scaled to some 2^60 by a power of two of each row, weights are taken as 2^60 p.  A row's (step, low) is applied
 // to its score and its weight, once for 64 numbers:
 //     q . x = step (q . n) + low (sum of q),   sum_j p_j x_j = sum_j (p_j step_j) (n_j - 8) + sum_j p_j (low_j + 8 step_j),
-// the n - 8 by products with a constant -8, so that sums stay near zero, where an accumulator that cuts off does not drift.
-// So nothing is rounded for the cache's sake: bf16 rows round p, then p step to bf16; float32 rows take queries and weights as three
-// bf16 numbers that add up to them and keep float32's accuracy on the tensor cores.
+// the -8 by a product with a constant, so that sums stay near zero, where an accumulator that cuts off does not drift.  Nothing is rounded for
+// the cache's sake: bf16 rows round p step to bf16; float32 rows take queries and weights as three bf16 numbers that add up to
+// them and keep float32's accuracy on the tensor cores.
 #pragma once
 
 #include <type_traits>
@@ -198,8 +198,8 @@ struct QuantRun {
 template <int LG> struct QuantWarps { static constexpr int W = LG == 3 ? 3 : 4; };
 constexpr int kQuantSlots = 4;              // of a warp's ring, later the place of its outputs
 constexpr int kQuantRing = kQuantSlots * kQuantSlot;
-template <int LG, int P, int J> __host__ __device__ constexpr int quant_weight_bytes() { return LG == 1 ? 0 : (P == 1 ? 8 : 8 * J) * 128; }       // of a tile
-template <int LG, int P, int J> __host__ __device__ constexpr int quant_smem_bytes() { return QuantWarps<LG>::W * (kQuantRing + quant_weight_bytes<LG, P, J>() + 2 * kAtRows * 4); }
+template <int LG, int J> __host__ __device__ constexpr int quant_weight_bytes() { return LG == 1 ? 0 : 8 * J * 128; }       // of a tile
+template <int LG, int J> __host__ __device__ constexpr int quant_smem_bytes() { return QuantWarps<LG>::W * (kQuantRing + quant_weight_bytes<LG, J>() + 2 * kAtRows * 4); }
 static_assert(kQuantRing >= kAtRows * kAtOutLd * 4, "room for a warp's outputs");
 
 __device__ __forceinline__ void cp16_whole(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory"); }
@@ -281,15 +281,24 @@ __device__ __forceinline__ void quant_four(uint32_t w, uint32_t* out) {
     out[0] = w & 0x000f000fu; out[1] = w & 0x00f000f0u;
     out[2] = v & 0x000f000fu; out[3] = v & 0x00f000f0u;
 }
+// The same of value rows.  float32 rows (P = 3) take the codes less 8, as ordinary numbers (0x4300 | n is 128 + n): their sums stay small
+// throughout, while sums of codes have the size of 8 times the weights until -8 has been added, and an accumulator that cuts off is off by
+// 2^-24 of that at every step (6.8e-6 of the outputs in all; bf16 outputs are rounded by some hundred times that).
+template <int P> __device__ __forceinline__ void quant_codes(uint32_t w, uint32_t* out) {
+    if constexpr (P == 1) {
+        quant_four(w, out);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = (w >> (4 * i) & 0x000f000fu) | 0x43004300u;
+            asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(out[i]) : "r"(x), "r"(0x43084308u));
+        }
+    }
+}
 __device__ __forceinline__ void quant_mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1, const float* c) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
                  : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
-}
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t x, uint32_t y) {
-    uint32_t z;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(z) : "r"(x), "r"(y));
-    return z;
 }
 // x as P bf16 numbers that add up to it (P = 1: its rounding).
 template <int P> __device__ __forceinline__ void quant_split(float x, float y, uint32_t* out) {
@@ -366,7 +375,8 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
                 quant_split<P>(q[8 * h + i] * f, q[8 * h + 4 + i] * f, qb[4 * h + i]);
             }
     }
-    // [d]: dims 8 g + d and 8 g + 4 + d of columns 2 t4, 2 t4 + 1 (odd d: 16 times), in units of 2^-73; sums of p mid in units of 2^60
+    // [d]: dims 8 g + d and 8 g + 4 + d of columns 2 t4, 2 t4 + 1: bf16 in units of 2^-73 (odd d: 16 times), float32 of 2^60; this lane's part of
+    // the sums of p mid in units of 2^60
     float acc[4][4], mids[J], m[J], l[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) { mids[j] = 0.f; m[j] = -INFINITY; l[j] = 0.f; }
@@ -374,7 +384,7 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
     for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[d][e] = 0.f;
-    constexpr int kBlocks = kQuantTile / 16, kRegs = P == 1 ? 2 * kBlocks : 2 * kBlocks * J;         // weights of a lane and tile
+    constexpr int kBlocks = kQuantTile / 16, kRegs = 2 * kBlocks * J;       // weights of a lane and tile
     const float none[4] = {0.f, 0.f, 0.f, 0.f};
     for (int at0 = u.r.begin; at0 < u.r.end; at0 += W * kQuantTile) {
         const int at = at0 + warp * kQuantTile;
@@ -386,18 +396,17 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
                 const uint2 w0 = *reinterpret_cast<const uint2*>(ks + (n * 16 + g) * kQuantRow + t4 * 8);
                 const uint2 w1 = *reinterpret_cast<const uint2*>(ks + (n * 16 + 8 + g) * kQuantRow + t4 * 8);
                 float dot[4];
+                uint32_t x0[8], x1[8];
+                quant_four(w0.x, x0); quant_four(w0.y, x0 + 4);
+                quant_four(w1.x, x1); quant_four(w1.y, x1 + 4);
+                // the smallest parts of the queries first: an accumulator cuts off what lies below its own last bit
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t x0[4], x1[4];
-                    quant_four(h ? w0.y : w0.x, x0);
-                    quant_four(h ? w1.y : w1.x, x1);
+                for (int k = P - 1; k >= 0; --k)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const uint32_t a[4] = {x0[2 * c], x1[2 * c], x0[2 * c + 1], x1[2 * c + 1]};
-#pragma unroll
-                        for (int k = 0; k < P; ++k) quant_mma(dot, a, qb[4 * h + 2 * c][k], qb[4 * h + 2 * c + 1][k], h + c + k == 0 ? none : dot);
+                    for (int c = 0; c < 8; c += 2) {
+                        const uint32_t a[4] = {x0[c], x1[c], x0[c + 1], x1[c + 1]};
+                        quant_mma(dot, a, qb[c][k], qb[c + 1][k], k == P - 1 && c == 0 ? none : dot);
                     }
-                }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const uint32_t scale = *reinterpret_cast<const uint32_t*>(ks + kQuantTile * kQuantRow + (n * 16 + e * 8 + g) * 4);
@@ -469,23 +478,17 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
                 }
             l[j] = l[j] * alpha[j] + sum;
         }
-        // The tile's weights, as they enter the products: bf16 rows as B, which has to hold neighbouring positions (an 8 x 8 transpose).
-        uint32_t pw[kRegs];
+        float pw[kRegs];                                     // the tile's weights
 #pragma unroll
         for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                if constexpr (P == 1) {
-                    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(pw[2 * n + e]) : "r"(pack_bf16(s[n][e][0], J == 2 ? s[n][e][J - 1] : 0.f)));
-                } else {
+            for (int e = 0; e < 2; ++e)
 #pragma unroll
-                    for (int j = 0; j < J; ++j) pw[(2 * n + e) * J + j] = __float_as_uint(s[n][e][j]);
-                }
-            }
+                for (int j = 0; j < J; ++j) pw[(2 * n + e) * J + j] = s[n][e][j];
         if constexpr (LG > 1) {
 #pragma unroll
             for (int i = 0; i < kRegs / 4; ++i)
-                *reinterpret_cast<uint4*>(shared + ((warp * (kRegs / 4) + i) * 32 + lane) * 16) = make_uint4(pw[4 * i], pw[4 * i + 1], pw[4 * i + 2], pw[4 * i + 3]);
+                *reinterpret_cast<float4*>(shared + ((warp * (kRegs / 4) + i) * 32 + lane) * 16) = make_float4(pw[4 * i], pw[4 * i + 1], pw[4 * i + 2], pw[4 * i + 3]);
         }
         if (__any_sync(0xffffffffu, moved)) {                // seldom, once a run is under way
 #pragma unroll
@@ -506,59 +509,45 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
             if constexpr (LG > 1) {
 #pragma unroll
                 for (int i = 0; i < kRegs / 4; ++i) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(shared + ((tile * (kRegs / 4) + i) * 32 + lane) * 16);
+                    const float4 x = *reinterpret_cast<const float4*>(shared + ((tile * (kRegs / 4) + i) * 32 + lane) * 16);
                     pw[4 * i] = x.x; pw[4 * i + 1] = x.y; pw[4 * i + 2] = x.z; pw[4 * i + 3] = x.w;
                 }
             }
-            // weights times steps: bf16 rows round p and then the product (half a step each, 2^-8 relative, of independent sign)
+            // Weights times steps, as B, which has to hold neighbouring positions (an 8 x 8 transpose): bf16 rows round them, by half a step
+            // (2^-8 relative) at most, of independent sign; what they are taken with is within 8 steps of 0, not the number itself.
             uint32_t w[kBlocks][2][P];
-            float mid[4];
-            if constexpr (P == 1) {
-#pragma unroll
-                for (int n = 0; n < kBlocks; ++n) {
-                    uint32_t a[4];                           // rows g: low of positions 2 t4 .., rows g + 8: step
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint2 x = *reinterpret_cast<const uint2*>(scales + (n * 16 + e * 8 + 2 * t4) * 4);
-                        a[2 * e] = __byte_perm(x.x, x.y, 0x7632);
-                        a[2 * e + 1] = __byte_perm(x.x, x.y, 0x5410);
-                        w[n][e][0] = mul_bf16x2(pw[2 * n + e], a[2 * e + 1]);
-                    }
-                    quant_mma(mid, a, pw[2 * n], pw[2 * n + 1], n == 0 ? none : mid);
-                }
-            } else {
-                mid[0] = mid[1] = 0.f;
-#pragma unroll
-                for (int n = 0; n < kBlocks; ++n)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint32_t scale = *reinterpret_cast<const uint32_t*>(scales + (n * 16 + e * 8 + g) * 4);
-                        const float st = __uint_as_float(scale << 16), md = fmaf(8.f, st, __uint_as_float(scale & 0xffff0000u));
-                        float x[2] = {0.f, 0.f};
-#pragma unroll
-                        for (int j = 0; j < J; ++j) {
-                            x[j] = __uint_as_float(pw[(2 * n + e) * J + j]);
-                            mid[j] = fmaf(x[j], md, mid[j]);
-                            x[j] *= st;
-                        }
-                        quant_split<P>(x[0], x[1], w[n][e]);
-#pragma unroll
-                        for (int k = 0; k < P; ++k) asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %0;" : "+r"(w[n][e][k]));
-                    }
-            }
-            // -8 times the sum of the weights, in the units of the bits 0-3 (of the bits 4-7: 16 times): added first
-            float start[4];
-            const uint32_t eight[4] = {0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u};
 #pragma unroll
             for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
-                for (int k = 0; k < P; ++k) quant_mma(start, eight, w[n][0][k], w[n][1][k], n + k == 0 ? none : start);
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t scale = *reinterpret_cast<const uint32_t*>(scales + (n * 16 + e * 8 + g) * 4);
+                    const float st = __uint_as_float(scale << 16), md = fmaf(8.f, st, __uint_as_float(scale & 0xffff0000u));
+                    float x[2] = {0.f, 0.f};
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+                    for (int j = 0; j < J; ++j) {
+                        x[j] = pw[(2 * n + e) * J + j];
+                        mids[j] = fmaf(x[j], md, mids[j]);
+                        x[j] *= st;
+                    }
+                    quant_split<P>(x[0], x[1], w[n][e]);
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
+                    for (int k = 0; k < P; ++k) asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %0;" : "+r"(w[n][e][k]));
+                }
+            if constexpr (P == 1) {
+                // -8 times the sum of the weights, in the units of the bits 0-3 (of the bits 4-7: 16 times): added first
+                float start[4];
+                const uint32_t eight[4] = {0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u};
 #pragma unroll
-                    for (int j = 0; j < J; ++j) acc[c][2 * e + j] = fmaf(start[j], c & 1 ? 16.f : 1.f, acc[c][2 * e + j]);
+                for (int n = 0; n < kBlocks; ++n) quant_mma(start, eight, w[n][0][0], w[n][1][0], n == 0 ? none : start);
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+#pragma unroll
+                        for (int j = 0; j < J; ++j) acc[c][2 * e + j] = fmaf(start[j], c & 1 ? 16.f : 1.f, acc[c][2 * e + j]);
+            }
+            // float32 rows add a tile's sums to those of the run in float32, rounded: an accumulator would cut off at every product of a long run
+            float part[4][4];
 #pragma unroll
             for (int n = 0; n < kBlocks; ++n) {
                 // word g of positions 2 t4, 2 t4 + 1 and 8 further on, two positions to a register
@@ -567,18 +556,28 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
                 for (int e = 0; e < 2; ++e) {
                     const char* at_row = vs + (n * 16 + e * 8 + t4) * kQuantRow + g * 4;
                     const uint32_t w0 = *reinterpret_cast<const uint32_t*>(at_row), w1 = *reinterpret_cast<const uint32_t*>(at_row + 4 * kQuantRow);
-                    quant_four(__byte_perm(w0, w1, 0x5410), lo[e]);
-                    quant_four(__byte_perm(w0, w1, 0x7632), hi[e]);
+                    quant_codes<P>(__byte_perm(w0, w1, 0x5410), lo[e]);
+                    quant_codes<P>(__byte_perm(w0, w1, 0x7632), hi[e]);
                 }
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const uint32_t a[4] = {lo[0][c], hi[0][c], lo[1][c], hi[1][c]};
+                    if constexpr (P == 1) {
+                        quant_mma(acc[c], a, w[n][0][0], w[n][1][0], acc[c]);
+                    } else {
 #pragma unroll
-                    for (int k = 0; k < P; ++k) quant_mma(acc[c], a, w[n][0][k], w[n][1][k], acc[c]);
+                        for (int k = P - 1; k >= 0; --k) quant_mma(part[c], a, w[n][0][k], w[n][1][k], n == 0 && k == P - 1 ? none : part[c]);
+                    }
                 }
             }
+            if constexpr (P > 1) {
 #pragma unroll
-            for (int j = 0; j < J; ++j) mids[j] += P == 1 ? fmaf(8.f, mid[2 + j], mid[j]) : mid[j];
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+#pragma unroll
+                        for (int j = 0; j < J; ++j) acc[c][2 * e + j] += part[c][2 * e + j];
+            }
         }
     }
     cp_wait<0>();
@@ -589,7 +588,7 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) {
             l[j] += __shfl_xor_sync(0xffffffffu, l[j], o);
-            if constexpr (P > 1) mids[j] += __shfl_xor_sync(0xffffffffu, mids[j], o);      // (the products give every row g the whole sum)
+            mids[j] += __shfl_xor_sync(0xffffffffu, mids[j], o);
         }
         const int row = J * t4 + j;
         if (g == 0) ml[row] = make_float2(m[j], l[j] * kDown);
@@ -598,7 +597,7 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
         for (int h = 0; h < 2; ++h) {
             float x[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) x[c] = fmaf(acc[c][2 * h + j], c & 1 ? kUp * 0.0625f : kUp, mids[j] * kDown);
+            for (int c = 0; c < 4; ++c) x[c] = fmaf(acc[c][2 * h + j], P > 1 ? kDown : c & 1 ? kUp * 0.0625f : kUp, mids[j] * kDown);
             *reinterpret_cast<float4*>(out + h * 4) = make_float4(x[0], x[1], x[2], x[3]);
         }
     }
@@ -651,7 +650,7 @@ __global__ void __launch_bounds__(QuantWarps<LG>::W * 32, P == 1 ? LG == 3 ? 5 :
     if (p.a.slots > 1 || p.S) asm volatile("griddepcontrol.launch_dependents;");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     char* shared = attend_smem + W * kQuantRing;
-    float2* ml = reinterpret_cast<float2*>(shared + W * quant_weight_bytes<LG, P, J>());
+    float2* ml = reinterpret_cast<float2*>(shared + W * quant_weight_bytes<LG, J>());
     QuantRun u;
     if (!quant_unit(p, (int)blockIdx.x, threadIdx.x == 0, &u)) return;
     attend_quant<LG, P, J>(p, u, attend_smem + warp * kQuantRing, shared, tops, ml + warp * R, warp, lane);

@@ -101,8 +101,7 @@ def quant_attend(q, codes, scales, dtype):
     size = (p[None, :, None] @ (whole[1:] + mid[1:].abs()[..., None]))[:, :, 0]
     bound = size * rel[None, :, None] + rounding(dtype) * out.abs() * 1.01 + 1e-30
     if dtype == torch.bfloat16:
-        # the weights are rounded to bf16, which goes with the numbers themselves, and so are these times the steps, which goes with n'
-        bound = bound + UBF * (p[None, :, None] @ (whole[1:] + x[1:].abs()))[:, :, 0] * 1.01
+        bound = bound + UBF * (p[None, :, None] @ whole[1:])[:, :, 0] * 1.01                                # weights times step in bf16
     return out, bound, p, p * rel[:, None] + 1e-37
 
 
