@@ -476,6 +476,7 @@ int32_t san_packed_block(const san_packed_args* a, void* d_workspace, size_t wor
         p.scale_log2e = scale_log2e;
         return launch_window<true>(p, dim3((unsigned)div_up(max_len, kWinQ), (unsigned)a->n_heads, (unsigned)(a->n_seq * n_lg)), st);
     }
+    if (plan.pairs * a->n_heads * n_lg > 0x7fffffffLL) return SAN_ERR_SHAPE;
     PackedParams p;
     std::memset(&p, 0, sizeof(p));
     p.q = q; p.k = k; p.v = v; p.out = out;

@@ -185,11 +185,35 @@ def test_evict(n, Hk, L, cap, n_keep, sink, recent, lens, kind, fmt):
 
 
 @pytest.mark.parametrize("fmt", ["q4", "bf16"])
-def test_evict_long(fmt):
+@pytest.mark.parametrize("kind", ["random", "ties", "odd"])
+@pytest.mark.parametrize("lens,n_keep", [([49999], 20000), ([16384, 4097], 4096), ([4096, 4095], 1500), ([16385], 16384)])
+def test_evict_long(fmt, kind, lens, n_keep):
+    """The bounds at which rows are chosen another way, and one row past them."""
     gen = torch.Generator().manual_seed(1)
-    rows, mass = stored(fmt, gen, 1, 1, 2, 50000), masses("random", gen, 1, 2, 50000)
-    got = evict(fmt, rows, mass, [0], [49999], 20000, 4, 1000, max_len=49999)
-    check(fmt, rows, mass, [0], [49999], 20000, 4, 1000, got)
+    n, cap = len(lens), max(lens) + 1
+    rows, mass = stored(fmt, gen, 1, n, 2, cap), masses(kind, gen, n, 2, cap)
+    got = evict(fmt, rows, mass, list(range(n)), lens, n_keep, 4, 1000, max_len=max(lens))
+    check(fmt, rows, mass, list(range(n)), lens, n_keep, 4, 1000, got)
+
+
+def test_evict_two_streams_with_workspaces_of_their_own():
+    gen = torch.Generator().manual_seed(9)
+    sets = []
+    for fmt, n, Hk, L, cap, n_keep in (("bf16", 9, 4, 3, 700, 300), ("q4", 2, 2, 1, 5000, 2000)):
+        rows, mass = stored(fmt, gen, L, n, Hk, cap), masses("random", gen, n, Hk, cap)
+        dev = [(to_planes(x) if fmt == "bf16" else x).to(DEV) for x in rows]
+        lens = [cap - 7 * i for i in range(n)]
+        dm, ids, dl, out = mass.to(DEV), i32(list(range(n))), i32(lens), torch.zeros(n, dtype=torch.int32, device=DEV)
+        p = planes_of(fmt, dev)
+        a = B.evict_args(d_ids=ids, d_lens=dl, n_items=n, n_keep=n_keep, n_sink=2, n_recent=9, d_mass=dm, ld_mass=cap, d_lens_out=out)
+        nb = B.san_cache_evict_bytes(p, a)[1]
+        sets.append((p, a, torch.empty(nb, dtype=torch.uint8, device=DEV), nb, torch.cuda.Stream(), (fmt, rows, mass, list(range(n)), lens, n_keep, 2, 9), dev, dm, out, ids, dl))
+    torch.cuda.synchronize()
+    for p, a, ws, nb, stream, *_ in sets:
+        B.check(B.san_cache_evict(p, a, ws, nb, stream))
+    torch.cuda.synchronize()
+    for *_, about, dev, dm, out, ids, dl in sets:
+        check(*about, (dev, dm, out, None, None))
 
 
 @pytest.mark.parametrize("fmt", ["q4", "bf16", "f32"])
