@@ -140,6 +140,21 @@ def test_what_is_not_seen_does_not_matter(t, value):
         assert bool(out[:, a:5 + t, :2].isnan().all(-1)[:, up].all()) and bool(up.any())
 
 
+@pytest.mark.parametrize("lens", [[700, 90], [60, 100]])
+@pytest.mark.parametrize("shape", ["rising", "falling", "steps", "one", "far"])
+def test_scores_that_move_along_a_sequence(lens, shape):
+    """Maxima that a row meets late, early, at some tokens alone, and scores too far apart for one scale."""
+    x = make(lens, 4, 2, 2, seed=16)
+    N = x["N"]
+    at = torch.arange(N, device=DEV).float()
+    up = {"rising": at / 40, "falling": (N - at) / 40, "steps": (at // 64 % 3) * 9, "one": (at % 97 == 13) * 40.0, "far": (at // 50) * 60}[shape]
+    x["q"][..., 0] = 8.0                                    # a score of its own for every token: q.k / 8 = up + the rest
+    x["k"][..., 0] = up[:, None].bfloat16()
+    call(x)
+    check(x)
+    assert int(x["status"][0]) == 0
+
+
 @pytest.mark.parametrize("t", [50, 300])
 def test_scores_of_minus_infinity_give_zeros(t):
     x = make([t, 20], 2, 2, 1, seed=8)
