@@ -60,9 +60,9 @@ int32_t quant_rows(bool append, const san_planes* c, int32_t dtype, const void* 
 }
 
 // ------------------------------------------------------------------------------- step attention
-constexpr int kQuantCtas = kSms * 4;                 // on the GPU at once
+constexpr int kQuantCtas = kSms * 4;                 // on the GPU at once, or nearly
 constexpr int kQuantStep = 4;                        // tiles of a step (four warps)
-constexpr int kQuantFills = 8, kQuantSteps = 3;      // see plan_quant
+constexpr int kQuantFills = 6, kQuantSteps = 3;      // see plan_quant
 struct QuantPlan { QuantParams p; size_t ml_bytes, bytes; long long ctas, tiles; };
 
 // Everything but the addresses.  Rows are cut into no more runs than find room in `room` bytes of workspace: one made for a larger batch,
@@ -87,9 +87,9 @@ int32_t plan_quant(const san_planes* c, const san_step_rows* r, size_t room, Qua
     p.n_lg = (int)div_up(p.n_layers, p.lg);
     p.o_row_tiles = (int)div_up(p.group, kAtRows);
     const long long runs = (long long)r->n_items * p.o_row_tiles * p.Hk * p.n_lg, tiles = std::max<long long>(1, div_up(p.max_len, kQuantTile));
-    // Runs of equal length, of whole steps: as many as give every SM one, and where a run keeps three steps, as many as fill the GPU eight
+    // Runs of equal length, of whole steps: as many as give every SM one, and where a run keeps three steps, as many as fill the GPU six
     // times, which evens out items of different lengths.  Measured: 4 units of 500 tiles 11.8 us in 125 runs each, 11.1 in 63, 10.4 in 32;
-    // 1024 units of up to 64 tiles 110 us in one run each, 103 in 4, 100 in 5 or 8.
+    // 1024 units of up to 64 tiles 90.5 us in 3 runs each, 92.2 in 4, and one run each takes a tenth more.
     const long long units = std::max<long long>(runs, 1), even = std::min<long long>(kQuantFills * kQuantCtas / units, tiles / (kQuantSteps * kQuantStep));
     const long long pieces = std::max<long long>(1, std::min<long long>(div_up(tiles, kQuantStep), std::max<long long>(kSms / units, even)));
     p.o_span = (int)(div_up(div_up(tiles, pieces), kQuantStep) * kQuantStep);
@@ -194,8 +194,8 @@ int32_t san_quant_attn_bytes(const san_planes* cache, const san_step_rows* rows,
     QuantPlan a;
     const int32_t rc = plan_quant(cache, rows, SIZE_MAX, &a);
     if (rc != SAN_OK) return rc;
-    // What any smaller batch or bound needs as well: n items of c units each are cut into at most 8 C / (n c) pieces (C CTAs on the GPU), so
-    // that all items together have at most 8 C / c, or one each.
+    // What any smaller batch or bound needs as well: n items of c units each are cut into at most 6 C / (n c) pieces (C CTAs on the GPU), so
+    // that all items together have at most 6 C / c, or one each.
     const AttendParams& p = a.p.a;
     const long long n = rows->n_items, c = (long long)p.o_row_tiles * p.Hk * p.n_lg, most = div_up(a.tiles, kQuantStep);
     const long long partial = std::min(n * most, std::max(n, kQuantFills * kQuantCtas / c));

@@ -209,40 +209,42 @@ __device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool full) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"(dst), "l"(src), "r"(n) : "memory");
 }
 
-// Walks a warp's slots: of every step the tile of keys that it scores, then the tiles of values (of its layer) that it applies, filled
-// kQuantSlots - 1 ahead of use.  What lies at or behind `end` becomes zeros; a step has no tiles that begin there.  Value rows go to
+// Walks a warp's slots: of every step the tile of keys that it scores (item 0), then the tiles of values of its layer that it applies (items 1 ..
+// LG), filled three ahead of use, into the place of the one used before.  Which comes when is known to the compiler, so that a fill is
+// its copies and little else.  What lies at or behind `end` becomes zeros; tiles that begin there are not copied.  Value rows go to
 // places where four lanes find rows 2 t of a block of eight in different banks: row r of eight to r / 2 + 4 (r % 2).
 template <int W, int LG> struct QuantRing {
-    uint32_t ring; int lane, end;
-    int f_at, f_tile; uint32_t f_slot, r_slot;              // f_at: first position of the step; f_tile: -1 keys
-    int k_off, v_off;                                       // of the warp's tiles in a step
+    static constexpr int kAhead = kQuantSlots - 1, kItems = LG + 1, kStep = W * kQuantTile;
+    uint32_t ring, slot;                                    // slot: of the next item
+    int lane, end, k_at, v_at;                              // positions of the warp's tiles of keys and of values in the step that is worked on
     bool values;                                            // its layer is there
-    const char* k; const char* v; const char* ks; const char* vs;           // this lane's first bytes of the step
+    const char* k; const char* v; const char* ks; const char* vs;           // this lane's first bytes of them
     uint32_t v_to;                                          // where its first value row goes
-    __device__ __forceinline__ QuantRing(const QuantRun& u, uint32_t smem, int ln, int warp)
-        : ring(smem), lane(ln), end(u.r.end), f_at(u.r.begin), f_tile(-1), f_slot(0), r_slot(0) {
+    __device__ __forceinline__ QuantRing(const QuantRun& u, uint32_t smem, int ln, int warp) : ring(smem), slot(0), lane(ln), end(u.r.end) {
         const int y = warp % LG;
-        k_off = warp * kQuantTile; v_off = warp / LG * LG * kQuantTile;
         values = y < u.r.layers;
-        const long long at = (long long)u.r.begin * kQuantRow + lane * 16, at_scale = (long long)u.r.begin * 4 + lane * 4;
-        k = u.r.k + at; v = u.r.v + (values ? y : 0) * u.r.v_stride + at;
-        ks = u.ks + at_scale; vs = u.vs + (values ? y : 0) * u.s_stride + at_scale;
+        k_at = u.r.begin + warp * kQuantTile; v_at = u.r.begin + warp / LG * LG * kQuantTile;
+        k = u.r.k + (long long)k_at * kQuantRow + lane * 16; ks = u.ks + (long long)k_at * 4 + lane * 4;
+        v = u.r.v + (values ? y : 0) * u.r.v_stride + (long long)v_at * kQuantRow + lane * 16;
+        vs = u.vs + (values ? y : 0) * u.s_stride + (long long)v_at * 4 + lane * 4;
         const int r = lane >> 1;
         v_to = ((r & 8) | (r >> 1 & 3) | (r & 1) << 2) * kQuantRow + (lane & 1) * 16;
-        for (int i = 0; i < kQuantSlots - 1; ++i) fill();
+        fill<0>(0); fill<1>(kQuantSlot); fill<2>(2 * kQuantSlot);
     }
-    __device__ __forceinline__ void fill() {
-        if (f_at < end) {
-            const int off = f_tile < 0 ? k_off : v_off + f_tile * kQuantTile, at = f_at + off;
-            const char* codes = (f_tile < 0 ? k : v) + off * kQuantRow;
-            const char* scales = (f_tile < 0 ? ks : vs) + off * 4;
-            const uint32_t slot = ring + f_slot, to = slot + (f_tile < 0 ? lane * 16 : v_to), to_scale = slot + kQuantTile * kQuantRow + lane * 4;
+    // Item ITEM of this step (ITEM >= kItems: of a later one).
+    template <int ITEM> __device__ __forceinline__ void fill(uint32_t to_slot) {
+        constexpr int later = ITEM / kItems * kStep, item = ITEM % kItems, off = later + (item > 0 ? (item - 1) * kQuantTile : 0);
+        const int at = (item == 0 ? k_at : v_at) + off;
+        if (at < end && (item == 0 || values)) {
+            const char* codes = (item == 0 ? k : v) + off * kQuantRow;
+            const char* scales = (item == 0 ? ks : vs) + off * 4;
+            const uint32_t to = ring + to_slot + (item == 0 ? lane * 16 : v_to), to_scale = ring + to_slot + kQuantTile * kQuantRow + lane * 4;
             if (at + kQuantTile <= end) {
 #pragma unroll
                 for (int j = 0; j < kQuantTile / 16; ++j) cp16_whole(to + j * 16 * kQuantRow, codes + j * 16 * kQuantRow);
 #pragma unroll
                 for (int j = 0; j < kQuantTile / 32; ++j) cp4_whole(to_scale + j * 128, scales + j * 128);
-            } else if (at < end) {
+            } else {
 #pragma unroll
                 for (int j = 0; j < kQuantTile / 16; ++j) {
                     const bool full = at + j * 16 + (lane >> 1) < end;
@@ -254,24 +256,21 @@ template <int W, int LG> struct QuantRing {
                     cp4(to_scale + j * 128, full ? scales + j * 128 : vs, full);
                 }
             }
-            f_slot = f_slot + kQuantSlot == kQuantRing ? 0 : f_slot + kQuantSlot;
-            if (++f_tile == LG || !values) {
-                constexpr int step = W * kQuantTile;
-                f_tile = -1;
-                f_at += step;
-                k += step * kQuantRow; v += step * kQuantRow; ks += step * 4; vs += step * 4;
-            }
         }
-        cp_commit();                                        // behind the end an empty group keeps the count
+        cp_commit();                                        // where nothing was copied an empty group keeps the count
     }
-    // Offset of the next slot in order, arrived; every lane is done with the one before it, which is refilled.
-    __device__ __forceinline__ uint32_t next() {
-        cp_wait<kQuantSlots - 2>();
+    // Offset of item ITEM's slot, arrived; every lane is done with the one before it, which is refilled.
+    template <int ITEM> __device__ __forceinline__ uint32_t next() {
+        cp_wait<kAhead - 1>();
         __syncwarp();
-        fill();
-        const uint32_t s = r_slot;
-        r_slot = r_slot + kQuantSlot == kQuantRing ? 0 : r_slot + kQuantSlot;
+        const uint32_t s = slot;
+        fill<ITEM + kAhead>(s == 0 ? kAhead * kQuantSlot : s - kQuantSlot);
+        slot = s == kAhead * kQuantSlot ? 0 : s + kQuantSlot;
         return s;
+    }
+    __device__ __forceinline__ void step() {
+        k_at += kStep; v_at += kStep;
+        k += kStep * kQuantRow; v += kStep * kQuantRow; ks += kStep * 4; vs += kStep * 4;
     }
 };
 
@@ -389,7 +388,7 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
     for (int at0 = u.r.begin; at0 < u.r.end; at0 += W * kQuantTile) {
         const int at = at0 + warp * kQuantTile;
         float s[kBlocks][2][J];                              // positions 16 n + g and + 8, columns 2 t4 (+ 1)
-        const char* ks = smem + ring.next();
+        const char* ks = smem + ring.template next<0>();
         if (at < u.r.end) {                                  // (the same in all lanes)
 #pragma unroll
             for (int n = 0; n < kBlocks; ++n) {
@@ -499,12 +498,8 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
             }
         }
         __syncthreads();                                     // (and the tops have been read)
-        if (!ring.values) continue;
-#pragma unroll 1
-        for (int t = 0; t < LG; ++t) {
-            const char* vs = smem + ring.next();
-            const int tile = warp / LG * LG + t;
-            if (at0 + tile * kQuantTile >= u.r.end) continue;
+        auto apply = [&](const char* vs, int tile) {
+            if (!ring.values || at0 + tile * kQuantTile >= u.r.end) return;
             const char* scales = vs + kQuantTile * kQuantRow;
             if constexpr (LG > 1) {
 #pragma unroll
@@ -533,18 +528,12 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
 #pragma unroll
                     for (int k = 0; k < P; ++k) asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %0;" : "+r"(w[n][e][k]));
                 }
+            // -8 times the sum of the weights, in the units of the bits 0-3 (of the bits 4-7: 16 times)
+            float start[4];
             if constexpr (P == 1) {
-                // -8 times the sum of the weights, in the units of the bits 0-3 (of the bits 4-7: 16 times): added first
-                float start[4];
                 const uint32_t eight[4] = {0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u};
 #pragma unroll
                 for (int n = 0; n < kBlocks; ++n) quant_mma(start, eight, w[n][0][0], w[n][1][0], n == 0 ? none : start);
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-#pragma unroll
-                        for (int j = 0; j < J; ++j) acc[c][2 * e + j] = fmaf(start[j], c & 1 ? 16.f : 1.f, acc[c][2 * e + j]);
             }
             // float32 rows add a tile's sums to those of the run in float32, rounded: an accumulator would cut off at every product of a long run
             float part[4][4];
@@ -570,15 +559,19 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
                     }
                 }
             }
-            if constexpr (P > 1) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < 4; ++c)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
+                for (int e = 0; e < 2; ++e)
 #pragma unroll
-                        for (int j = 0; j < J; ++j) acc[c][2 * e + j] += part[c][2 * e + j];
-            }
-        }
+                    for (int j = 0; j < J; ++j) acc[c][2 * e + j] = P > 1 ? acc[c][2 * e + j] + part[c][2 * e + j] : fmaf(start[j], c & 1 ? 16.f : 1.f, acc[c][2 * e + j]);
+        };
+        const int tile0 = warp / LG * LG;
+        apply(smem + ring.template next<1>(), tile0);
+        if constexpr (LG > 1) apply(smem + ring.template next<2>(), tile0 + 1);
+        if constexpr (LG > 2) apply(smem + ring.template next<3>(), tile0 + 2);
+        if constexpr (LG > 3) apply(smem + ring.template next<4>(), tile0 + 3);
+        ring.step();
     }
     cp_wait<0>();
     __syncwarp();
@@ -639,10 +632,9 @@ __device__ __forceinline__ bool quant_unit(const QuantParams& p, int index, bool
     return true;
 }
 
-// P, J: see attend_quant.  Registers leave room for 16 warps on an SM (bf16; 99.5 us with 20 warps and 96 registers, 95.3 with 16 and 128:
-// 128 rows of up to 4096, 4 layers).
+// P, J: see attend_quant.  Registers leave room for 20 warps on an SM (bf16; 128 rows of up to 4096, 4 layers: 92.9 us, 96.5 with 16 warps).
 template <int LG, int P, int J>
-__global__ void __launch_bounds__(QuantWarps<LG>::W * 32, P == 1 ? LG == 3 ? 5 : 4 : 3) quant_attend_kernel(const __grid_constant__ QuantParams p) {
+__global__ void __launch_bounds__(QuantWarps<LG>::W * 32, P == 1 ? LG == 3 ? 6 : 5 : 3) quant_attend_kernel(const __grid_constant__ QuantParams p) {
     constexpr int W = QuantWarps<LG>::W, R = kAtRows;
     using T = typename std::conditional<P == 1, __nv_bfloat16, float>::type;
     extern __shared__ __align__(128) char attend_smem[];
