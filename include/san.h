@@ -15,11 +15,12 @@
  *  - Every function returns a status (SAN_OK = 0).  Nothing throws or traps, and no kernel
  *    spins on another kernel, CTA or rank.  The only device-side waits are a CTA's waits for
  *    its OWN asynchronous copies or tensor-core operations (mbarrier waits in the kernels
- *    behind san_decode_step, san_full_block, san_window_block and san_prefix_attn) and the end of
+ *    behind san_decode_step, san_full_block, san_window_block, san_prefix_attn and san_packed_block), the CTAs of a
+ *    cluster meeting one another (san_cache_evict) and the end of
  *    the kernel before on the same stream; an mbarrier wait gives up after about a second and makes
  *    the kernel stop early.  san_decode_step reports it as SAN_ERR_TIMEOUT through
  *    san_device_status, which then also clears the context's split-row tickets so that later
- *    steps start clean; san_prefix_attn reports it in its status words (its rows' outputs are then
+ *    steps start clean; san_prefix_attn and san_packed_block report it in their status words (their outputs are then
  *    undefined); san_full_block and san_window_block have no status word, and a tile whose wait
  *    ran out leaves its output rows unwritten.
  *  - All `d_` pointers are DEVICE pointers owned by the caller; all others are HOST
@@ -36,8 +37,8 @@
  *  - Element type is SAN_F32 or SAN_BF16 for q/k/v/x/outputs; S, where it is given or taken, is
  *    always float32; products, sums and the softmax are float32.  d_head must be 64.  Of bf16 inputs the
  *    weights enter their product with the values in bf16 (at most half a step off, 2^-8 relative; their sum is that of
- *    the float32 ones) in san_window_block, san_window_attn, san_prefix_attn, the 128-query tiles of
- *    san_full_block and kernels 2 and 3 of san_decode_step (san_step_kernel_select): outputs are off by 1.2 to 1.4
+ *    the float32 ones) in san_window_block, san_window_attn, san_prefix_attn, san_packed_block, san_quant_attn (there
+ *    times a row's step), the 128-query tiles of san_full_block and kernels 2 and 3 of san_decode_step (san_step_kernel_select): outputs are off by 1.2 to 1.4
  *    times what their own rounding alone is.  The per-warp step kernel and the 64-query tiles of san_full_block
  *    add what the rounding of a weight left as a second bf16 number.
  *  - Sequences are numbered 0 .. max_sent*beam-1; sequence s belongs to sentence
@@ -502,7 +503,7 @@ typedef struct {
 /* Rows into a cache of four bits, and back as numbers.  Item i's rows are n = d_nrows[i] (rows_per_item where d_nrows is NULL) from
  * row d_pos[i] (0 where it is NULL) of id d_ids[i] on; the other side is in the order a projection writes it,
  *     keys [n_items][rows_per_item][n_kv_heads][64],   values [n_layers][n_items][rows_per_item][n_kv_heads][64]   of `dtype`
- * (SAN_F32 or SAN_BF16; rows beyond n are neither read nor written).
+ * (SAN_F32 or SAN_BF16; rows beyond n are neither read nor written; rows_per_item may be more than cap_len where d_nrows is given).
  * Of a row x:  low = min x rounded down to bf16, step = (max x - low) / 15 rounded up to bf16 and, unless it is 0, to 2^-50 at least,
  * n = (x - low) / step rounded to the nearest, half to even (0 where step is 0), of the exact quotients: no number is off by more than
  * step / 2.  A row with a NaN or a number of 2^40 or more reads as NaN.  san_quant_read rounds low + step * n to `dtype`.

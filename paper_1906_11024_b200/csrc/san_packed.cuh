@@ -15,6 +15,12 @@
 //                outputs of this one.  MMAs of a thread complete in order, so that scores never replace weights that have not been read.
 //                The tiles share keys and values and nothing else, so that one may be at its exponentials while the other is not.
 // Tensor memory: a tile of 128 rows has 256 columns: scores twice (64 each, weights over them) and up to two layers' outputs.
+// What bounds it: the softmax warps.  A chunk (256 rows x 64 keys) takes some 1500 clocks, of which a warp is at its exponentials for 700 to 850 (two
+// warps to an SM quarter, whose 16 exponentials a clock and SM they share), at maxima for 250, waiting for scores 200; an item's end takes 2500 to 4000.
+// 48 prompts of 1 to 4096 tokens, 16 heads over 4 key heads: 235 us (296 with a CTA for an item, 16 softmax warps and two threads a row
+// 345, since their meeting took 500 clocks a chunk); two of some 8000 tokens, 8 heads, 2 layers: 199 us = 940 TFLOP/s (247, 296).
+// Tried and not faster: no look for a chunk's maximum while sums stay small (273 and 235 us: the scores stay live), the second tile started
+// later, weights stored in two halves.
 // Every wait is bounded: one that runs out raises a flag that ends the CTA's other waits; the CTA frees its tensor memory, reports, and
 // leaves what it has not written.
 #pragma once
@@ -115,7 +121,9 @@ __device__ __forceinline__ float pack_max3(float a, float b, float c) {         
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-constexpr int kPackPoly = 2;                                            // of eight pairs
+// Of eight pairs of exponentials.  48 prompts of 1 to 4096 tokens and two of some 8000 (see the kernel): 250 and 218 us with none, 245 and 210 with
+// one, 241 and 205 with two, 248 and 212 with three.
+constexpr int kPackPoly = 2;
 
 // What a CTA works on, and which comes next.
 struct PackedItem {

@@ -30,7 +30,7 @@ int32_t quant_rows(bool append, const san_planes* c, int32_t dtype, const void* 
     int32_t rc = check_planes(c, true);
     if (rc != SAN_OK) return rc;
     if (dtype != SAN_F32 && dtype != SAN_BF16) return SAN_ERR_DTYPE;
-    if (n_items < 0 || rows < 1 || rows > c->cap_len) return SAN_ERR_SHAPE;
+    if (n_items < 0 || rows < 1 || (!nrows && rows > c->cap_len)) return SAN_ERR_SHAPE;
     if (n_items == 0) return SAN_OK;
     if ((rc = check_plane_pointers(c)) != SAN_OK) return rc;
     if (!k || !v || !ids) return SAN_ERR_NULL;

@@ -134,6 +134,36 @@ def test_rows_bad_items_are_skipped_and_reported():
                 assert bool((out_k[bad[0]] == -9.0).all()) and not bool((out_k[good] == -9.0).any())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_wider_than_the_cache(dtype):
+    """Buffers padded to more rows than the cache has: counts say what is real; more than the cache has room for is reported."""
+    dt, code = TYPES[dtype]
+    n, R, Hk, L, cap = 3, 70, 2, 2, 23
+    gen = torch.Generator().manual_seed(9)
+    k, v = (torch.randn(*s, generator=gen).to(dt).to(DEV) for s in ((n, R, Hk, DH), (L, n, R, Hk, DH)))
+    ids, nrows = i32([2, 0, 1]), i32([23, 24, 11])
+    codes, scales = cache(3, Hk, L, cap, fill=0x5B)
+    p, status = planes(codes, scales), torch.zeros(8, dtype=torch.int32, device=DEV)
+    B.check(B.san_quant_append(p, code, k, v, ids, None, nrows, n, R, status))
+    back_k, back_v = torch.full_like(k, -9.0), torch.full_like(v, -9.0)
+    B.check(B.san_quant_read(p, code, back_k, back_v, ids, None, nrows, n, R))
+    torch.cuda.synchronize()
+    assert status.tolist()[:5] == [B.SAN_ERR_DEVICE_CHECK, 14, 1, 0, 23]
+    hc, hs = codes.cpu(), scales.cpu()
+    assert bool((hc[:, 0] == 0x5B).all()) and bool((hc[:, 1, :, 11:] == 0x5B).all())
+    for i, b, m in ((0, 2, 23), (2, 1, 11)):
+        for y, x in enumerate([k.cpu(), *v.cpu()]):
+            got = (back_k if y == 0 else back_v[y - 1])[i].cpu()
+            for r in range(m):
+                for h in range(Hk):
+                    want, step, low = quantise_row(x[i, r, h].double().tolist())
+                    assert hc[y, b, h, r].tolist() == pack(want) and hs[y, b, h, r].double().tolist() == [step, low]
+            want = numbers(hc[y, b, :, :m], hs[y, b, :, :m]).transpose(0, 1)
+            assert bool(((got[:m].double() - want).abs() <= want.abs() * (2.0 ** -24 + (2.0 ** -8 * 1.01 if dtype == "bf16" else 0))).all())
+            assert bool((got[m:] == -9.0).all())
+    assert bool((back_k[1] == -9.0).all()) and bool((back_v[:, 1] == -9.0).all())
+
+
 # ------------------------------------------------------------------------------------------- attention
 def filled(n_ids, Hk, L, cap, seed=0):
     gen = torch.Generator(device=DEV).manual_seed(seed)

@@ -75,6 +75,15 @@ def test_quant_rows_refusals(call):
         assert _rows(call, **kw) == status, kw
 
 
+def test_quant_rows_wider_than_the_cache():
+    """With counts of their own the items' rows may lie further apart than the cache is long."""
+    for call in (B.san_quant_append, B.san_quant_read):
+        got = call(_planes(), B.SAN_BF16, FAKE, FAKE, FAKE, None, FAKE, 0, 101, None, stream=0)
+        assert got == B.SAN_OK
+        assert call(_planes(), B.SAN_BF16, None, FAKE, FAKE, None, FAKE, 3, 101, None, stream=0) == B.SAN_ERR_NULL
+        assert call(_planes(), B.SAN_BF16, FAKE, FAKE, FAKE, None, FAKE, 3, 0x7fffffff, None, stream=0) == B.SAN_ERR_SHAPE
+
+
 def _step(**kw):
     a = dict(dtype=B.SAN_BF16, n_heads=8, d_q=FAKE, d_ids=FAKE, d_lens=FAKE, n_items=4, max_len=0, d_out=FAKE)
     return B.step_rows(**(a | kw))
