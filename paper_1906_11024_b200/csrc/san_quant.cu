@@ -47,7 +47,7 @@ int32_t quant_rows(bool append, const san_planes* c, int32_t dtype, const void* 
     p.max_ids = c->max_ids; p.cap = c->cap_len; p.status = status;
     p.all_rows = (uint32_t)(all * rows); p.layer_rows = (long long)n_items * rows * p.Hk * kDh;
     p.by_rows.by((uint32_t)rows); p.by_heads.by((uint32_t)p.Hk); p.by_items.by((uint32_t)n_items);
-    const unsigned grid = (unsigned)div_up(all * rows, 32);
+    const unsigned grid = (unsigned)div_up(all * rows, kQuantCtaRows);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (append) {
         if (dtype == SAN_BF16) quant_append_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(p);

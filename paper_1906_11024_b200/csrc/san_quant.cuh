@@ -42,6 +42,7 @@ struct QuantDivide {
     }
     __device__ __forceinline__ uint32_t of(uint32_t x) const { return (__umulhi(x, times) + x) >> shift; }
 };
+constexpr int kQuantCtaRows = 64;           // of 256 threads, four lanes a row
 struct QuantRowsParams {
     char* k; char* v; char* ks; char* vs;
     long long v_stride, s_stride;           // bytes between the layers' planes of codes, of (step, low)
@@ -68,7 +69,7 @@ __device__ __forceinline__ float quant_max3(float a, float b, float c) {
     return d;
 }
 
-// The place of a row of eight lanes (`row`: numbered layer, item, head, position, the last the fastest; layer 0: keys): false if it is
+// The place of a row (`row`: numbered layer, item, head, position, the last the fastest; layer 0: keys): false if it is
 // none.  src: of the row's 64 numbers in elements, from the keys' or the layer's first.
 struct QuantPlace { int layer; long long src, panel; int pos; };
 __device__ __forceinline__ bool quant_place(const QuantRowsParams& p, uint32_t row, bool reporter, QuantPlace* at) {
@@ -92,30 +93,38 @@ __device__ __forceinline__ bool quant_place(const QuantRowsParams& p, uint32_t r
     return r < n;
 }
 
-// A row is eight lanes of eight numbers; a CTA has 32 rows, those of one head on end where there are several.
+// A row is four lanes of sixteen numbers; a CTA has 64 rows, those of one head on end where there are several.
 template <typename T>
-__global__ void __launch_bounds__(256) quant_append_kernel(const __grid_constant__ QuantRowsParams p) {
-    const int c = threadIdx.x & 7;                          // numbers 8 c .. 8 c + 7 of the row
+__global__ void __launch_bounds__(256, 5) quant_append_kernel(const __grid_constant__ QuantRowsParams p) {
+    const int c = threadIdx.x & 3;                          // numbers 8 c .. 8 c + 7 of the row and of its second half
     QuantPlace at;
-    const bool real = quant_place(p, blockIdx.x * 32 + (threadIdx.x >> 3), c == 0, &at);
-    float x[8];
+    const bool real = quant_place(p, blockIdx.x * kQuantCtaRows + (threadIdx.x >> 2), c == 0, &at);
+    float x[16];
     if (real) {
         const T* src = reinterpret_cast<const T*>(at.layer == 0 ? p.k_rows : p.v_rows) + at.src + c * 8;
-        if constexpr (sizeof(T) == 2) {
-            unpack16<__nv_bfloat16>(ld16_stream(src), x);
-        } else {
-            unpack16<float>(ld16_stream(src), x);
-            unpack16<float>(ld16_stream(src + 4), x + 4);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (sizeof(T) == 2) {
+                unpack16<__nv_bfloat16>(ld16_stream(src + 32 * h), x + 8 * h);
+            } else {
+                unpack16<float>(ld16_stream(src + 32 * h), x + 8 * h);
+                unpack16<float>(ld16_stream(src + 32 * h + 4), x + 8 * h + 4);
+            }
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        for (int i = 0; i < 16; ++i) x[i] = 0.f;
     }
-    float lo = quant_min3(x[0], x[1], x[2]), hi = quant_max3(x[0], x[1], x[2]);
-    lo = quant_min3(quant_min3(lo, x[3], x[4]), x[5], quant_min3(x[6], x[7], lo));
-    hi = quant_max3(quant_max3(hi, x[3], x[4]), x[5], quant_max3(x[6], x[7], hi));
+    float lo = x[0], hi = x[0];
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
+    for (int i = 1; i < 15; i += 2) {
+        lo = quant_min3(lo, x[i], x[i + 1]);
+        hi = quant_max3(hi, x[i], x[i + 1]);
+    }
+    lo = quant_min3(lo, lo, x[15]);
+    hi = quant_max3(hi, hi, x[15]);
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
         lo = quant_min3(lo, lo, __shfl_xor_sync(0xffffffffu, lo, o));
         hi = quant_max3(hi, hi, __shfl_xor_sync(0xffffffffu, hi, o));
     }
@@ -129,30 +138,31 @@ __global__ void __launch_bounds__(256) quant_append_kernel(const __grid_constant
         if (15.f * step < wide) step = __int_as_float(__float_as_int(step) + 0x10000);
     step = wide > 0.f ? fmaxf(step, kQuantLeastStep) : 0.f;
     const float inv = step > 0.f ? __fdividef(1.f, step) : 0.f;         // a step of zero: codes of zero
-    uint32_t codes = 0;
+    uint32_t codes[2] = {0u, 0u};
     float off = 0.f;                                        // the furthest from a whole number
 #pragma unroll
-    for (int i = 7; i >= 0; --i) {
+    for (int i = 15; i >= 0; --i) {
         const float t = (x[i] - low) * inv, y = t + 12582912.f;         // the sum's low bits are t rounded half to even
         off = fmaxf(off, fabsf(t - (y - 12582912.f)));
-        codes = codes << 4 | (__float_as_uint(y) & 15u);
+        codes[i >> 3] = codes[i >> 3] << 4 | (__float_as_uint(y) & 15u);
     }
     if (off > 0.4999f && held) {                            // t is within 1e-5 of the quotient; next to a border 64 bits decide
-        codes = 0;
+        codes[0] = codes[1] = 0u;
 #pragma unroll
-        for (int i = 7; i >= 0; --i) {
+        for (int i = 15; i >= 0; --i) {
             const double d = (double)x[i] - (double)low;
             const float k = fminf(floorf((x[i] - low) * inv), 15.f);
             // k may be one too large or too small itself where the quotient is a whole number
             const double border = ((double)k + 0.5) * (double)step;
             const uint32_t n = (uint32_t)k + (d > border || (d == border && ((int)k & 1)));
-            codes = codes << 4 | min(n, 15u);
+            codes[i >> 3] = codes[i >> 3] << 4 | min(n, 15u);
         }
     }
     if (!real) return;
     const long long row = at.panel * p.cap + at.pos;
     char* to = (at.layer == 0 ? p.k : p.v + (at.layer - 1) * p.v_stride) + row * kQuantRow;
-    reinterpret_cast<uint32_t*>(to)[c] = held ? codes : 0u;
+    reinterpret_cast<uint32_t*>(to)[c] = held ? codes[0] : 0u;
+    reinterpret_cast<uint32_t*>(to)[c + 4] = held ? codes[1] : 0u;
     if (c == 0) {
         char* scale = (at.layer == 0 ? p.ks : p.vs + (at.layer - 1) * p.s_stride) + row * 4;
         *reinterpret_cast<uint32_t*>(scale) = held ? __float_as_uint(step) >> 16 | (__float_as_uint(low) & 0xffff0000u) : 0x7fc07fc0u;
@@ -161,22 +171,33 @@ __global__ void __launch_bounds__(256) quant_append_kernel(const __grid_constant
 
 template <typename T>
 __global__ void __launch_bounds__(256) quant_read_kernel(const __grid_constant__ QuantRowsParams p) {
-    const int c = threadIdx.x & 7;
+    const int c = threadIdx.x & 3;
     QuantPlace at;
-    if (!quant_place(p, blockIdx.x * 32 + (threadIdx.x >> 3), c == 0, &at)) return;
+    if (!quant_place(p, blockIdx.x * kQuantCtaRows + (threadIdx.x >> 2), c == 0, &at)) return;
     const long long row = at.panel * p.cap + at.pos;
-    const uint32_t codes = reinterpret_cast<const uint32_t*>((at.layer == 0 ? p.k : p.v + (at.layer - 1) * p.v_stride) + row * kQuantRow)[c];
+    const char* codes = (at.layer == 0 ? p.k : p.v + (at.layer - 1) * p.v_stride) + row * kQuantRow;
     const uint32_t scale = *reinterpret_cast<const uint32_t*>((at.layer == 0 ? p.ks : p.vs + (at.layer - 1) * p.s_stride) + row * 4);
     const float step = __uint_as_float(scale << 16), low = __uint_as_float(scale & 0xffff0000u);
-    float x[8];
+    T* to = reinterpret_cast<T*>(const_cast<char*>(at.layer == 0 ? p.k_rows : p.v_rows)) + at.src;
+    // 16 bytes at a time, four lanes side by side.
+    constexpr int N = 16 / sizeof(T);                       // numbers
+    uint32_t words[16 / N];
+    if constexpr (N == 8) {
+        for (int i = 0; i < 2; ++i) words[i] = reinterpret_cast<const uint32_t*>(codes)[c + 4 * i];
+    } else {                                                // the lane's 16 bits of each of four pairs of words
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = fmaf(step, (float)(codes >> (4 * i) & 15u), low);
-    T* to = reinterpret_cast<T*>(const_cast<char*>(at.layer == 0 ? p.k_rows : p.v_rows)) + at.src + c * 8;
-    if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<uint4*>(to) = pack16<__nv_bfloat16>(x);
-    } else {
-        *reinterpret_cast<uint4*>(to) = pack16<float>(x);
-        *reinterpret_cast<uint4*>(to + 4) = pack16<float>(x + 4);
+        for (int i = 0; i < 2; ++i) {
+            const uint4 half = reinterpret_cast<const uint4*>(codes)[i];
+            words[2 * i] = (c < 2 ? half.x : half.y) >> 16 * (c & 1);
+            words[2 * i + 1] = (c < 2 ? half.z : half.w) >> 16 * (c & 1);
+        }
+    }
+#pragma unroll
+    for (int w = 0; w < 16 / N; ++w) {
+        float x[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = fmaf(step, (float)(words[w] >> (4 * i) & 15u), low);
+        *reinterpret_cast<uint4*>(to + (4 * w + c) * N) = pack16<T>(x);
     }
 }
 
