@@ -69,6 +69,24 @@ __device__ __forceinline__ float quant_max3(float a, float b, float c) {
     return d;
 }
 
+// Two float32 numbers in one instruction.
+__device__ __forceinline__ unsigned long long quant_pair(float x, float y) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void quant_unpair(unsigned long long r, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(r)); }
+__device__ __forceinline__ unsigned long long quant_add2(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ unsigned long long quant_fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+
 // The place of a row (`row`: numbered layer, item, head, position, the last the fastest; layer 0: keys): false if it is
 // none.  src: of the row's 64 numbers in elements, from the keys' or the layer's first.
 struct QuantPlace { int layer; long long src, panel; int pos; };
@@ -138,14 +156,22 @@ __global__ void __launch_bounds__(256, 5) quant_append_kernel(const __grid_const
         if (15.f * step < wide) step = __int_as_float(__float_as_int(step) + 0x10000);
     step = wide > 0.f ? fmaxf(step, kQuantLeastStep) : 0.f;
     const float inv = step > 0.f ? __fdividef(1.f, step) : 0.f;         // a step of zero: codes of zero
+    constexpr float kWhole = 12582912.f;                    // 1.5 2^23
+    const unsigned long long low2 = quant_pair(-low, -low), inv2 = quant_pair(inv, inv), zero2 = quant_pair(0.f, 0.f), most2 = quant_pair(kWhole, kWhole);
     uint32_t codes[2] = {0u, 0u};
     float off = 0.f;                                        // the furthest from a whole number
 #pragma unroll
-    for (int i = 15; i >= 0; --i) {
-        const float t = (x[i] - low) * inv, y = t + 12582912.f;         // the sum's low bits are t rounded half to even
-        off = fmaxf(off, fabsf(t - (y - 12582912.f)));
-        codes[i >> 3] = codes[i >> 3] << 4 | (__float_as_uint(y) & 15u);
+    for (int i = 14; i >= 0; i -= 2) {                      // two numbers in one instruction
+        const unsigned long long t = quant_fma2(quant_add2(quant_pair(x[i], x[i + 1]), low2), inv2, zero2);
+        const unsigned long long y = quant_add2(t, most2);               // the sums' low bits are t rounded half to even
+        float a, b;
+        quant_unpair(quant_fma2(quant_add2(y, quant_pair(-kWhole, -kWhole)), quant_pair(-1.f, -1.f), t), a, b);
+        off = quant_max3(off, fabsf(a), fabsf(b));
+        quant_unpair(y, a, b);
+        codes[i >> 3] = (codes[i >> 3] * 16 + __float_as_uint(b)) * 16 + __float_as_uint(a);
     }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) codes[h] -= 0x4b400000u * 0x11111111u;  // the bits of kWhole, eight times
     if (off > 0.4999f && held) {                            // t is within 1e-5 of the quotient; next to a border 64 bits decide
         codes[0] = codes[1] = 0u;
 #pragma unroll
