@@ -20,7 +20,7 @@
 // 48 prompts of 1 to 4096 tokens, 16 heads over 4 key heads: 235 us (296 with a CTA for an item, 16 softmax warps and two threads a row
 // 345, since their meeting took 500 clocks a chunk); two of some 8000 tokens, 8 heads, 2 layers: 199 us = 940 TFLOP/s (247, 296).
 // Tried and not faster: no look for a chunk's maximum while sums stay small (273 and 235 us: the scores stay live), the second tile started
-// later, weights stored in two halves.
+// later, weights stored in two halves, the next chunk's scores read and looked through between the halves of this one's exponentials (291 and 254).
 // Every wait is bounded: one that runs out raises a flag that ends the CTA's other waits; the CTA frees its tensor memory, reports, and
 // leaves what it has not written.
 #pragma once
