@@ -260,8 +260,8 @@ __device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool full) {
 
 // Walks a warp's slots: of every step the tile of keys that it scores (item 0), then the tiles of values of its layer that it applies (items 1 ..
 // LG), filled three ahead of use, into the place of the one used before.  Which comes when is known to the compiler, so that a fill is
-// its copies and little else.  What lies at or behind `end` becomes zeros; tiles that begin there are not copied.  Value rows go to
-// places where four lanes find rows 2 t of a block of eight in different banks: row r of eight to r / 2 + 4 (r % 2).
+// its copies and little else.  What lies at or behind `end` becomes zeros; tiles that begin there are not copied.  The halves of rows
+// 4 .. 7 of eight change places, so that a half of eight rows is in different banks.
 template <int W, int LG> struct QuantRing {
     static constexpr int kAhead = kQuantSlots - 1, kItems = LG + 1, kStep = W * kQuantTile;
     uint32_t ring, slot;                                    // slot: of the next item
@@ -277,7 +277,7 @@ template <int W, int LG> struct QuantRing {
         v = u.r.v + (values ? y : 0) * u.r.v_stride + (long long)v_at * kQuantRow + lane * 16;
         vs = u.vs + (values ? y : 0) * u.s_stride + (long long)v_at * 4 + lane * 4;
         const int r = lane >> 1;
-        v_to = ((r & 8) | (r >> 1 & 3) | (r & 1) << 2) * kQuantRow + (lane & 1) * 16;
+        v_to = r * kQuantRow + ((lane ^ r >> 2) & 1) * 16;
         fill<0>(0); fill<1>(kQuantSlot); fill<2>(2 * kQuantSlot);
     }
     // Item ITEM of this step (ITEM >= kItems: of a later one).
@@ -423,7 +423,7 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
                 quant_split<P>(q[8 * h + i] * f, q[8 * h + 4 + i] * f, qb[4 * h + i]);
             }
     }
-    // [d]: dims 8 g + d and 8 g + 4 + d of columns 2 t4, 2 t4 + 1: bf16 in units of 2^-73 (odd d: 16 times), float32 of 2^60; this lane's part of
+    // [d]: dims 4 g + d and 32 + 4 g + d of columns 2 t4, 2 t4 + 1: bf16 in units of 2^-73 (odd d: 16 times), float32 of 2^60; this lane's part of
     // the sums of p mid in units of 2^60
     float acc[4][4], mids[J], m[J], l[J];
 #pragma unroll
@@ -432,6 +432,8 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
     for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[d][e] = 0.f;
+    // the row's half that this lane names of 16 positions: eight lanes each for those of 0 .. 7, then of 8 .. 15
+    const uint32_t row_at = ((lane >> 4) * 8 + (lane & 7)) * kQuantRow + ((lane >> 3 ^ lane >> 2) & 1) * 16;
     constexpr int kBlocks = kQuantTile / 16, kRegs = 2 * kBlocks * J;       // weights of a lane and tile
     const float none[4] = {0.f, 0.f, 0.f, 0.f};
     for (int at0 = u.r.begin; at0 < u.r.end; at0 += W * kQuantTile) {
@@ -550,6 +552,7 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
         auto apply = [&](const char* vs, int tile) {
             if (!ring.values || at0 + tile * kQuantTile >= u.r.end) return;
             const char* scales = vs + kQuantTile * kQuantRow;
+            const uint32_t rows = ring_addr + (uint32_t)(vs - smem) + row_at;
             if constexpr (LG > 1) {
 #pragma unroll
                 for (int i = 0; i < kRegs / 4; ++i) {
@@ -588,14 +591,14 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
             float part[4][4];
 #pragma unroll
             for (int n = 0; n < kBlocks; ++n) {
-                // word g of positions 2 t4, 2 t4 + 1 and 8 further on, two positions to a register
-                uint32_t lo[2][4], hi[2][4];
+                // four codes each of positions 2 t4 and 2 t4 + 1 (and 8 further on) in a register: dims 4 g .. and 32 + 4 g ..
+                uint32_t lo[2][4], hi[2][4], x[4];
+                asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
+                             : "r"(rows + n * 16 * kQuantRow) : "memory");
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const char* at_row = vs + (n * 16 + e * 8 + t4) * kQuantRow + g * 4;
-                    const uint32_t w0 = *reinterpret_cast<const uint32_t*>(at_row), w1 = *reinterpret_cast<const uint32_t*>(at_row + 4 * kQuantRow);
-                    quant_codes<P>(__byte_perm(w0, w1, 0x5410), lo[e]);
-                    quant_codes<P>(__byte_perm(w0, w1, 0x7632), hi[e]);
+                    quant_codes<P>(x[2 * e], lo[e]);
+                    quant_codes<P>(x[2 * e + 1], hi[e]);
                 }
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
@@ -634,13 +637,13 @@ __device__ __forceinline__ void attend_quant(const QuantParams& p, const QuantRu
         }
         const int row = J * t4 + j;
         if (g == 0) ml[row] = make_float2(m[j], l[j] * kDown);
-        float* out = reinterpret_cast<float*>(smem) + row * kAtOutLd + g * 8;
+        float* out = reinterpret_cast<float*>(smem) + row * kAtOutLd + g * 4;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             float x[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) x[c] = fmaf(acc[c][2 * h + j], P > 1 ? kDown : c & 1 ? kUp * 0.0625f : kUp, mids[j] * kDown);
-            *reinterpret_cast<float4*>(out + h * 4) = make_float4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<float4*>(out + h * 32) = make_float4(x[0], x[1], x[2], x[3]);
         }
     }
 }
