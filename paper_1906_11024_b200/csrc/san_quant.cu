@@ -88,8 +88,8 @@ int32_t plan_quant(const san_planes* c, const san_step_rows* r, size_t room, Qua
     p.o_row_tiles = (int)div_up(p.group, kAtRows);
     const long long runs = (long long)r->n_items * p.o_row_tiles * p.Hk * p.n_lg, tiles = std::max<long long>(1, div_up(p.max_len, kQuantTile));
     // Runs of equal length, of whole steps: as many as give every SM one, and where a run keeps three steps, as many as fill the GPU six
-    // times, which evens out items of different lengths.  Measured: 4 units of 500 tiles 11.8 us in 125 runs each, 11.1 in 63, 10.4 in 32;
-    // 1024 units of up to 64 tiles 90.5 us in 3 runs each, 92.2 in 4, and one run each takes a tenth more.
+    // times, which evens out items of different lengths.  Measured: 4 units of 500 tiles 11.8 us in 125 runs each, 11.1 in 63, 10.4 in 32 (10.0
+    // by now); 1024 units of up to 64 tiles 90.5 us in 3 runs each (81.7 by now), 92.2 in 4, and one run each takes a tenth more.
     const long long units = std::max<long long>(runs, 1), even = std::min<long long>(kQuantFills * kQuantCtas / units, tiles / (kQuantSteps * kQuantStep));
     const long long pieces = std::max<long long>(1, std::min<long long>(div_up(tiles, kQuantStep), std::max<long long>(kSms / units, even)));
     p.o_span = (int)(div_up(div_up(tiles, pieces), kQuantStep) * kQuantStep);
