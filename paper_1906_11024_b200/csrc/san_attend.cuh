@@ -106,7 +106,7 @@ __device__ __forceinline__ bool own_ok(const AttendParams& p, int item) {
 // What a unit reads: `n` positions, the first n_sink of them at 0.., the others from `lo` on.
 struct AttendRun {
     const char* k; const char* v;
-    long long row_bytes, v_stride;
+    long long row_bytes, v_row_bytes, v_stride;                 // between rows of keys, of values; between the layers' values
     bool permuted;                          // chunk c of the row at pos sits at c ^ (pos & 7)
     int n_sink, lo, n;                      // visible rows (of the whole sequence)
     int begin, end;                         // this unit's part of them
@@ -148,12 +148,13 @@ template <typename T>
 __device__ __forceinline__ void attend_fill(const AttendRun& u, int begin, int end, int plane, uint32_t slot, int lane) {
     constexpr int RB = AttendGeom<T>::kRowBytes, CPR = RB / 16, RPI = 32 / CPR;     // chunks per row, rows per instruction
     const char* base = plane < 0 ? u.k : u.v + plane * u.v_stride;
+    const long long row_bytes = plane < 0 ? u.row_bytes : u.v_row_bytes;
     const int c_smem = lane % CPR, q = lane / CPR;
     const uint32_t dst = slot + q * RB + c_smem * 16;
     if (begin >= u.n_sink && begin + kAtTile <= end) {       // 32 rows on end
         const int pos = u.lo + begin - u.n_sink + q;
-        const char* src = base + pos * u.row_bytes;
-        const long long step = RPI * u.row_bytes;
+        const char* src = base + pos * row_bytes;
+        const long long step = RPI * row_bytes;
         int off[8 / RPI];                                    // the chunk to fetch: row j * RPI + q has 8 / RPI swizzles
 #pragma unroll
         for (int j = 0; j < 8 / RPI; ++j) {
@@ -169,7 +170,7 @@ __device__ __forceinline__ void attend_fill(const AttendRun& u, int begin, int e
             const bool full = at < end;
             const int pos = !full ? 0 : at < u.n_sink ? at : u.lo + (at - u.n_sink);
             const int c = c_smem ^ (r & 7);
-            const char* src = base + pos * u.row_bytes + ((u.permuted ? c ^ (pos & 7) : c) << 4);
+            const char* src = base + pos * row_bytes + ((u.permuted ? c ^ (pos & 7) : c) << 4);
             cp16(dst + j * RPI * RB, src, full);
         }
     }
@@ -504,7 +505,7 @@ __device__ __forceinline__ bool attend_unit(const AttendParams& p, bool prefix, 
         u->rows = min(R, rows - u->row0);
         if (u->rows <= 0) return false;
         u->n = p.plens[g]; u->n_sink = 0; u->lo = 0;
-        u->row_bytes = (long long)p.Hk * RB;
+        u->row_bytes = u->v_row_bytes = (long long)p.Hk * RB;
         const long long at = ((long long)g * p.pcap * p.Hk + hk) * RB;
         u->k = p.pk + at;
         u->v = p.pv + at + u->layer0 * p.pv_stride;
@@ -526,7 +527,7 @@ __device__ __forceinline__ bool attend_unit(const AttendParams& p, bool prefix, 
         u->lo = p.window > 0 ? max(0, len - p.window) : 0;
         u->n_sink = min(p.n_sink, u->lo);
         u->n = u->n_sink + len - u->lo;
-        u->row_bytes = RB;
+        u->row_bytes = u->v_row_bytes = RB;
         const long long at = ((long long)p.ids[item] * p.Hk + hk) * p.cap * RB;
         u->k = p.k + at;
         u->v = p.v + at + u->layer0 * p.v_stride;

@@ -181,7 +181,7 @@ __device__ __forceinline__ void packed_row_again(const PackedParams& p, const Pa
     AttendRun u;
     u.v = reinterpret_cast<const char*>(p.v + layer * p.v_layer + (long long)w.token0 * p.v_ld + w.head / p.group * kDh);
     u.k = reinterpret_cast<const char*>(p.k + (long long)w.token0 * p.k_ld + w.head / p.group * kDh);
-    u.row_bytes = p.k_ld * 2; u.v_stride = 0; u.permuted = false;
+    u.row_bytes = p.k_ld * 2; u.v_row_bytes = p.v_ld * 2; u.v_stride = 0; u.permuted = false;
     u.lo = 0; u.n_sink = 0; u.n = a + 1; u.begin = 0; u.end = a + 1;
     u.item0 = 0; u.row0 = 0; u.rows = 1; u.head0 = 0; u.layer0 = layer; u.layers = 1; u.slot = 0;
     float2* ml = reinterpret_cast<float2*>(smem + kAtTile * 128);

@@ -669,7 +669,7 @@ __device__ __forceinline__ bool quant_unit(const QuantParams& p, int index, bool
     r.head0 = hk * a.group; r.row0 = tile * kAtRows; r.rows = min(kAtRows, a.group - r.row0);
     r.layer0 = lg * a.lg; r.layers = min(a.lg, a.n_layers - r.layer0);
     r.n = a.lens[item]; r.n_sink = 0; r.lo = 0; r.permuted = false;
-    r.row_bytes = kQuantRow;
+    r.row_bytes = r.v_row_bytes = kQuantRow;
     const long long panel = ((long long)a.ids[item] * a.Hk + hk) * a.cap;
     r.k = a.k + panel * kQuantRow;
     r.v = a.v + panel * kQuantRow + r.layer0 * a.v_stride;

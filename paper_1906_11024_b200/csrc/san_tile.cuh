@@ -284,7 +284,7 @@ __device__ __forceinline__ void tile_row_again(const WindowParams& p, int seq, i
     AttendRun u;
     u.k = reinterpret_cast<const char*>(p.k + kv);
     u.v = reinterpret_cast<const char*>(p.v + layer * p.v_layer + kv);
-    u.row_bytes = (long long)p.Hk * 128; u.v_stride = 0; u.permuted = false;
+    u.row_bytes = u.v_row_bytes = (long long)p.Hk * 128; u.v_stride = 0; u.permuted = false;
     u.lo = max(0, a - p.window + 1);
     u.n_sink = min(p.n_sink, u.lo);
     u.n = u.n_sink + a + 1 - u.lo;

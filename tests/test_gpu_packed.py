@@ -255,3 +255,34 @@ def test_offsets_past_32_bits():
         x.update(q=q, k=k, v=v[None])
         call(x, v_stride=8, max_len=max(x["lens"]))
         check(x)
+
+
+@pytest.mark.parametrize("lens", [[700, 90, 1000], [60, 100]])
+@pytest.mark.parametrize("layout", [None, "fused", "apart", "wide keys", "wide values"])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_values_that_are_not_seen_at_all_distances(lens, layout, value):
+    """Rows that are computed again beside a bad value read keys and values each at their own distance."""
+    H, Hk, L = 4, 2, 3
+    x = make(lens, H, Hk, L, seed=17, ld=layout if layout in ("fused", "apart") else None)
+    N = x["N"]
+    if layout in ("wide keys", "wide values"):              # (with room behind the other, so that a wrong distance stays in its buffer)
+        wide, tight = ("k", "v") if layout == "wide keys" else ("v", "k")
+        room_for = torch.zeros(L * N * (Hk + 20) * DH, dtype=BF, device=DEV)
+        room_for.normal_()
+        x[tight] = room_for[:x[tight].numel()].view(x[tight].shape).copy_(x[tight])
+        far = torch.randn(*x[wide].shape[:-2], Hk + 20, DH, device=DEV).to(BF)
+        far[..., 7:7 + Hk, :] = x[wide]
+        x[wide] = far[..., 7:7 + Hk, :]
+    first = x["first"].tolist()
+    wants = [packed(x["q"][a:a + t], x["k"][a:a + t], x["v"][:, a:a + t], BF) for a, t in zip(first, lens)]
+    bad = [(s, b) for s, t in enumerate(lens) for b in (1, t // 3, t - 1)]
+    for s, b in bad:                                        # one dim of key head 0, in one layer
+        x["v"][1, first[s] + b, 0, 3] = value
+    call(x)
+    assert int(x["status"][0]) == 0
+    for s, (a, t) in enumerate(zip(first, lens)):
+        out, (want, bound) = x["out"][:, a:a + t], wants[s]
+        sees = torch.zeros_like(out, dtype=torch.bool)
+        sees[1, 1:, :H // Hk, 3] = True
+        assert bool((((out.double() - want).abs() <= bound) | sees).all()), s
+        assert not bool(out[sees].isfinite().any())
