@@ -550,7 +550,7 @@ typedef struct {
     int32_t n_rows; const int32_t* d_rows;          /* n_rows 0 .. 2^20 */
     const int32_t* d_ids; const int32_t* d_lens; const int32_t* d_begin;
     int32_t n_items;                      /* at most 65535 */
-    int32_t max_len;                      /* host bound on d_lens */
+    int32_t max_len;                      /* host bound on d_lens, at most 2^28 (0 = ld_mass) */
     float decay;                          /* finite */
     float* d_mass; int64_t ld_mass;       /* [max_ids][n_kv_heads][ld_mass], ld_mass >= max_len */
     int32_t max_ids;

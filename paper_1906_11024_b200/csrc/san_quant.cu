@@ -233,7 +233,9 @@ int32_t san_weight_mass(const san_mass_args* a, void* stream) {
     if (a->n_heads < 1 || a->n_heads > 1024 || a->n_kv_heads < 1 || a->n_heads % a->n_kv_heads != 0) return SAN_ERR_SHAPE;
     if (a->n_rows < 0 || a->n_rows > (1 << 20) || a->n_items < 0 || a->n_items > 65535 || a->max_ids < 1 || a->max_len < 0 || a->max_len > (1 << 28)) return SAN_ERR_SHAPE;
     if (a->ld_mass < a->max_len || !std::isfinite(a->decay)) return SAN_ERR_SHAPE;
-    if (a->n_items == 0 || a->max_len == 0) return SAN_OK;
+    if (a->max_len == 0 && a->ld_mass > (1 << 28)) return SAN_ERR_SHAPE;
+    const int max_len = a->max_len ? a->max_len : (int)a->ld_mass;
+    if (a->n_items == 0 || max_len == 0) return SAN_OK;
     if (!a->d_S || !a->d_ids || !a->d_lens || !a->d_mass) return SAN_ERR_NULL;
     if (!aligned(a->d_S, 4) || !aligned(a->d_mass, 4)) return SAN_ERR_SHAPE;
     MassParams p;
@@ -241,11 +243,11 @@ int32_t san_weight_mass(const san_mass_args* a, void* stream) {
     p.S = a->d_S; p.item_stride = a->item_stride; p.row_stride = a->row_stride; p.head_stride = a->head_stride;
     p.mass = a->d_mass; p.ld = a->ld_mass; p.rows = a->d_rows; p.ids = a->d_ids; p.lens = a->d_lens; p.begin = a->d_begin;
     p.n_rows = a->n_rows; p.H = a->n_heads; p.Hk = a->n_kv_heads; p.group = p.H / p.Hk; p.n_items = a->n_items; p.max_ids = a->max_ids;
-    p.max_len = a->max_len; p.decay = a->decay; p.status = a->d_status;
+    p.max_len = max_len; p.decay = a->decay; p.status = a->d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     // Eight warps share a position's pairs where there are many; short rows are cut into more CTAs where there would not be two an SM.
     if ((long long)a->n_rows * p.group < 16) return launch_mass<1, 8>(p, st);
-    const long long wide = div_up(a->max_len, mass_positions<8, 4>()) * p.Hk * p.n_items;
+    const long long wide = div_up(max_len, mass_positions<8, 4>()) * p.Hk * p.n_items;
     return wide >= 2 * kSms ? launch_mass<8, 4>(p, st) : launch_mass<8, 1>(p, st);
 }
 

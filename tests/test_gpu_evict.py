@@ -271,3 +271,25 @@ def test_evict_offsets_past_32_bits():
     torch.cuda.synchronize()
     at = keep(mass[-1, 0].tolist(), cap, 5000, 4, 50)
     assert int(a[1][0]) == 5000 and torch.equal(dev[:, -1, 0, :5000].cpu(), to_planes(rows[0][:, :, :, at])[:, 0, 0])
+
+
+@pytest.mark.parametrize("R", [1, 40])
+def test_mass_without_a_bound(R):
+    """max_len 0: whatever the mass holds; a longer length is reported."""
+    n, H, Hk, ld = 3, 4, 2, 70
+    S = torch.rand(n, R, H, ld, device=DEV)
+    mass = torch.rand(n, Hk, ld, device=DEV)
+    old, lens = mass.clone(), [70, 71, 33]
+    status, a = torch.zeros(8, dtype=torch.int32, device=DEV), [i32([2, 0, 1]), i32(lens)]
+    B.check(B.san_weight_mass(B.mass_args(n_heads=H, n_kv_heads=Hk, d_S=S, item_stride=R * H * ld, row_stride=H * ld, head_stride=ld, n_rows=R,
+                                          d_ids=a[0], d_lens=a[1], n_items=n, max_len=0, decay=1.0, d_mass=mass, ld_mass=ld, max_ids=n, d_status=status)))
+    torch.cuda.synchronize()
+    assert status.tolist()[:5] == [B.SAN_ERR_DEVICE_CHECK, 15, 1, 71, 70]
+    want, bound = old.double(), torch.zeros(n, Hk, ld, dtype=torch.float64, device=DEV)
+    for i, b in ((0, 2), (2, 1)):
+        t = lens[i]
+        got = S[i, :, :, :t].double().view(R, Hk, H // Hk, t).sum((0, 2))
+        want[b, :, :t] += got
+        # terms of one sign in any order, the old mass and the addition
+        bound[b, :, :t] = U32 * ((H // Hk * R + 1) * got + 3 * (old[b, :, :t] + got)) + 1e-37
+    assert bool(((mass.double() - want).abs() <= bound).all())

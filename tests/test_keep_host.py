@@ -165,3 +165,11 @@ def test_evict_refusals():
     assert B.san_cache_evict(_planes(), _evict(), FAKE, n - 1, stream=0) == B.SAN_ERR_CAPACITY
     assert B.lib().san_cache_evict(None, None, None, 0, None) == B.SAN_ERR_NULL
     assert B.lib().san_cache_evict_bytes(_planes(), _evict(), None) == B.SAN_ERR_NULL
+
+
+def test_mass_bound_of_zero_is_the_mass_itself():
+    """As in the other calls: no bound given is the bound of the buffer, not "no rows"."""
+    assert B.san_weight_mass(_mass(max_len=0, d_S=None), stream=0) == B.SAN_ERR_NULL
+    assert B.san_weight_mass(_mass(max_len=0, ld_mass=(1 << 28) + 1), stream=0) == B.SAN_ERR_SHAPE
+    assert B.san_weight_mass(_mass(max_len=0, ld_mass=0, d_S=None), stream=0) == B.SAN_OK         # a mass of no rows
+    assert B.san_weight_mass(_mass(max_len=0, ld_mass=-1), stream=0) == B.SAN_ERR_SHAPE
