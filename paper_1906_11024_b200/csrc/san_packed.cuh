@@ -173,40 +173,77 @@ struct PackedWalk {
     }
 };
 
-// Row a of an item's head, one layer, by one warp: over the tokens that it sees, as a row of a decode step.
-__device__ __forceinline__ void packed_row_again(const PackedParams& p, const PackedItem& w, int layer, int a, char* smem, int lane) {
+// Row a of an item's head, its layers, by one warp: over the tokens that it sees, as a row of a decode step, kPackAgain of them at a time. A sum that
+// is NaN ends it: nothing makes the row anything else.
+constexpr int kPackAgain = 4096;
+__device__ __forceinline__ void packed_row_again(const PackedParams& p, const PackedItem& w, int a, char* smem, int lane) {
     struct { const char* q; int H, group; float scale_log2e; } row;
     row.q = reinterpret_cast<const char*>(p.q + (long long)(w.token0 + a) * p.q_ld + w.head * kDh);
     row.H = 1; row.group = 1; row.scale_log2e = p.scale_log2e;
     AttendRun u;
-    u.v = reinterpret_cast<const char*>(p.v + layer * p.v_layer + (long long)w.token0 * p.v_ld + w.head / p.group * kDh);
+    u.v = reinterpret_cast<const char*>(p.v + w.layer0 * p.v_layer + (long long)w.token0 * p.v_ld + w.head / p.group * kDh);
     u.k = reinterpret_cast<const char*>(p.k + (long long)w.token0 * p.k_ld + w.head / p.group * kDh);
-    u.row_bytes = p.k_ld * 2; u.v_row_bytes = p.v_ld * 2; u.v_stride = 0; u.permuted = false;
-    u.lo = 0; u.n_sink = 0; u.n = a + 1; u.begin = 0; u.end = a + 1;
-    u.item0 = 0; u.row0 = 0; u.rows = 1; u.head0 = 0; u.layer0 = layer; u.layers = 1; u.slot = 0;
+    u.row_bytes = p.k_ld * 2; u.v_row_bytes = p.v_ld * 2; u.v_stride = p.v_layer * 2; u.permuted = false;
+    u.lo = 0; u.n_sink = 0; u.n = a + 1;
+    u.item0 = 0; u.row0 = 0; u.rows = 1; u.head0 = 0; u.layer0 = w.layer0; u.layers = w.layers; u.slot = 0;
+    static_assert((kPackLayers - 1) * kAtRows * kAtOutLd * 4 + kDh * 4 <= kAtTile * 128, "the row's outputs, then (max, sum), in the ring's place");
     float2* ml = reinterpret_cast<float2*>(smem + kAtTile * 128);
-    __syncwarp();
-    attend_warp_bf16<1, 2>(row, u, 0, kAtTile, smem, ml, lane);
-    __syncwarp();
-    const float l = ml[0].y, inv = l == 0.f ? 0.f : 1.f / l;
-    const float2 o = *reinterpret_cast<const float2*>(smem + lane * 8);
-    *reinterpret_cast<uint32_t*>(p.out + layer * p.out_layer + (long long)(w.token0 + a) * p.out_ld + w.head * kDh + lane * 2) = pack_bf16(o.x * inv, o.y * inv);
+    float m = -INFINITY, l = 0.f;
+    float2 o[kPackLayers];
+#pragma unroll
+    for (int y = 0; y < kPackLayers; ++y) o[y] = make_float2(0.f, 0.f);
+    for (u.begin = 0; u.begin <= a; u.begin += kPackAgain) {
+        u.end = min(u.begin + kPackAgain, a + 1);
+        __syncwarp();
+        attend_warp_bf16<kPackLayers, 2>(row, u, u.begin, kAtTile, smem, ml, lane);
+        __syncwarp();
+        const float2 x = ml[0];
+        const float m_new = fmaxf(m, x.x), f = m == m_new ? 1.f : exp2f(m - m_new), b = x.x == m_new ? 1.f : exp2f(x.x - m_new);
+        l = l * f + x.y * b;
+        m = m_new;
+#pragma unroll
+        for (int y = 0; y < kPackLayers; ++y) {
+            if (y >= w.layers) break;
+            const float2 v = *reinterpret_cast<const float2*>(smem + y * (kAtRows * kAtOutLd * 4) + lane * 8);
+            o[y] = make_float2(o[y].x * f + v.x * b, o[y].y * f + v.y * b);
+        }
+        if (l != l) break;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int y = 0; y < kPackLayers; ++y) {
+        if (y >= w.layers) break;
+        *reinterpret_cast<uint32_t*>(p.out + (w.layer0 + y) * p.out_layer + (long long)(w.token0 + a) * p.out_ld + w.head * kDh + lane * 2) = pack_bf16(o[y].x * inv, o[y].y * inv);
+    }
 }
 
-// Rows of a warp's 32 that came out as NaN (`odd`, a bit for each): computed again where a value that was multiplied by a weight of zero can be
-// the cause, which only tokens behind the tile's first row can hold.
-__device__ __noinline__ void packed_again(const PackedParams& p, const PackedItem& w, int x, int quarter, uint32_t odd, char* smem, int lane) {
-    const int first = w.a0 + x * kTileQ, last = w.a0 + min((x + 1) * kTileQ, w.rows) - 1;
-    bool spoiled = false;
+// Rows of a warp's 32 in the tile x of an item that came out as NaN: computed again where a value that was multiplied by a weight of zero can be
+// the cause, which only later tokens of the tile can hold.  The outputs, which this warp has written, are read for them.
+__device__ __noinline__ void packed_again(const PackedParams& p, const PackedItem& w, int x, int quarter, char* smem, int lane) {
+    const int first = w.a0 + x * kTileQ, last = w.a0 + min((x + 1) * kTileQ, w.rows) - 1, row0 = first + 32 * quarter;
+    uint32_t odd = 0;                                       // a bit for each
+    for (int r = 0; r < 32 && row0 + r <= last; ++r) {
+        bool nan = false;
+        for (int y = 0; y < w.layers; ++y) {
+            const uint32_t z = *reinterpret_cast<const uint32_t*>(p.out + (w.layer0 + y) * p.out_layer + (long long)(w.token0 + row0 + r) * p.out_ld + w.head * kDh + lane * 2);
+            nan |= (z & 0x7fffu) > 0x7f80u || (z >> 16 & 0x7fffu) > 0x7f80u;
+        }
+        if (__any_sync(0xffffffffu, nan)) odd |= 1u << r;
+    }
+    if (odd == 0) return;
+    int bad = 0;                                            // the last token of the tile with such a value
     for (int i = lane; i < w.layers * (last - first) * 8; i += 32) {
         const int b = first + 1 + (i >> 3) % (last - first), y = i / ((last - first) * 8);
         const uint4 v = *reinterpret_cast<const uint4*>(p.v + (w.layer0 + y) * p.v_layer + (long long)(w.token0 + b) * p.v_ld + w.head / p.group * kDh + (i & 7) * 8);
         const uint32_t e = 0x7f80u;                         // an exponent of all ones: no finite number
-        for (const uint32_t z : {v.x, v.y, v.z, v.w}) spoiled |= (z & e) == e || (z >> 16 & e) == e;
+        for (const uint32_t z : {v.x, v.y, v.z, v.w})
+            if ((z & e) == e || (z >> 16 & e) == e) bad = max(bad, b);
     }
-    if (!__any_sync(0xffffffffu, spoiled)) return;
-    for (; odd; odd &= odd - 1)
-        for (int y = 0; y < w.layers; ++y) packed_row_again(p, w, w.layer0 + y, first + 32 * quarter + __ffs(odd) - 1, smem, lane);
+    bad = __reduce_max_sync(0xffffffffu, bad);
+    for (; odd; odd &= odd - 1) {
+        const int a = row0 + __ffs(odd) - 1;
+        if (a < bad) packed_row_again(p, w, a, smem, lane);  // later ones see it
+    }
 }
 
 template <int LG>
@@ -217,7 +254,7 @@ __global__ void __launch_bounds__(kPackThreads, 1) packed_kernel(const __grid_co
     __shared__ __align__(8) uint64_t q_full[2], q_free[2], k_full[kTileKSlots], k_free[kTileKSlots], v_full[kTileVSlots], v_free[kTileVSlots];
     __shared__ __align__(8) uint64_t s_full[2][2], p_full[2][2], pv_done[2][2], o_free[2];
     __shared__ uint32_t tmem_s;
-    __shared__ int dead_s;
+    __shared__ int dead_s, again_s[2 * kTileQ / 32];                    // again: rows of a softmax warp came out as NaN
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int* dead = &dead_s;
     char* sQ = pack_smem + ((1024u - (tile_u32(pack_smem) & 1023u)) & 1023u);
@@ -365,6 +402,7 @@ __global__ void __launch_bounds__(kPackThreads, 1) packed_kernel(const __grid_co
         const unsigned long long sc2 = tile_pair(sc, sc);
         int count = 0;                                                  // chunks of all items
         bool ok = true;
+        if (lane == 0) again_s[warp] = 0;
         // The outputs of the tile's chunk n are complete.  Two barriers in turn, as for scores and weights, because a wait
         // names a phase by its parity: the outputs of chunk n - 2 were complete before the scores of chunk n.
         auto outputs = [&](int n) -> bool { return tile_wait_warp(&pv_done[x][n & 1], (uint32_t)(n >> 1) & 1u, dead); };
@@ -474,10 +512,16 @@ __global__ void __launch_bounds__(kPackThreads, 1) packed_kernel(const __grid_co
                     *reinterpret_cast<uint4*>(dst + (r - (lane >> 3)) * p.out_ld) = *reinterpret_cast<const uint4*>(mine + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
                 __syncwarp();
             }
-            const uint32_t bits = __ballot_sync(0xffffffffu, odd && lane < left);
-            if (bits != 0) packed_again(p, w, x, quarter, bits, mine, lane);
+            if (__any_sync(0xffffffffu, odd && lane < left) && lane == 0) again_s[warp] = 1;
         }
         if (!ok && lane == 0 && p.status && atomicCAS(&p.status[0], 0, (int)SAN_ERR_TIMEOUT) == 0) { p.status[1] = TAG_PACKED; p.status[2] = w.seq; }
+        // Behind all items, when no wait is under way any more: a row of a long sequence may take longer than a wait may last.
+        __syncwarp();
+        if (ok && again_s[warp]) {
+            PackedItem item;
+            for (PackedWalk items(p); items.next(&item);)
+                if (item.chunks(x) > 0) packed_again(p, item, x, quarter, mine, lane);
+        }
     }
     tile_before_sync();
     __syncthreads();

@@ -286,3 +286,25 @@ def test_values_that_are_not_seen_at_all_distances(lens, layout, value):
         sees[1, 1:, :H // Hk, 3] = True
         assert bool((((out.double() - want).abs() <= bound) | sees).all()), s
         assert not bool(out[sees].isfinite().any())
+
+
+def test_rows_computed_again_may_take_longer_than_a_wait():
+    """A bad value at the end of a sequence so long that the rows before it, computed again, take a second and more."""
+    N, L = 1_300_000, 2
+    x = make([N], 1, 1, L, seed=18)
+    x["q"] *= 3                                             # few keys have most of a row's weight
+    x["v"][1, N - 1, 0, 3] = math.nan
+    call(x)
+    assert int(x["status"][0]) == 0
+    out = x["out"][:, :, 0]
+    rows = list(range(N - 129, N - 1, 9)) + [0, 1, 127, 128, 255, N // 3, N // 2 + 1]
+    for a in rows:
+        q, k, v = x["q"][a, 0].double(), x["k"][:a + 1, 0].double(), x["v"][:, :a + 1, 0].double()
+        p = torch.softmax(k @ q / 8.0, 0)
+        want, size = p @ v, p @ v.abs()
+        # as in keep_helpers.packed, but that sums are made of products of 16 keys at once, added up one after the other
+        dz = 70 * 2.0 ** -23 * float((k.abs() @ q.abs()).max()) / 8.0
+        bound = size * (4 * dz + 2.0 ** -20 + 2 * (a / 8 + 16) * 2.0 ** -23 + 2 * 2.0 ** -8) + 2.0 ** -8 * want.abs() + 1e-30
+        assert bool(((out[:, a].double() - want).abs() <= bound).all()), a
+    assert bool(out[:, :N - 1].isfinite().all()) and bool((out[:, ::997] != -7.0).any(-1).all())
+    assert bool(out[0, N - 1].isfinite().all()) and bool(out[1, N - 1, 3].isnan())
