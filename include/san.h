@@ -478,9 +478,10 @@ typedef struct {
     const void* d_k; int64_t ld_k;        /* [n_tokens][n_kv_heads][64] */
     const void* d_v; int64_t ld_v; int64_t v_stride;        /* [n_layers] of those, v_stride elements apart (a multiple of 8) */
     const int32_t* d_first;               /* [n_seq + 1], ascending */
-    int32_t n_seq, n_tokens;
+    int32_t n_seq, n_tokens;              /* 2^28 each at most */
     int32_t max_len;                      /* host bound on the lengths (0 = n_tokens); kernels are chosen by it: below 128
-                                             n_seq times the layers' groups of four is at most 65535 */
+                                             n_seq times the layers' groups of four is at most 65535, from there on (n_tokens / 256 + n_seq) *
+                                             n_heads times the groups of two below 2^31 */
     void* d_out;                          /* [n_layers][n_tokens][n_heads][64] */
     int32_t* d_status;                    /* optional */
 } san_packed_args;

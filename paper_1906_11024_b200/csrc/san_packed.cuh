@@ -60,18 +60,20 @@ __device__ __forceinline__ int packed_sequence(const PackedParams& p, int seq, i
 
 // The list of all sequences' pairs of tiles, those with the most keys first: entry i + 1 is (first token, length, pair, sequence), entry 0
 // has their number.  One CTA: pairs are counted by their place in the sequence (all beyond 2047 together), the counts summed from
-// above.  Sequences that are not in order have no pairs (and are reported).
+// above.  Sequences that are not in order have no pairs (and are reported).  A thread's sequences have no more pairs than the tokens and one each, unless
+// they overlap: it counts no more, so that no sum passes 31 bits (2^28 tokens and sequences at most) and no call takes forever.
 constexpr int kPackedBins = 2048;
 static __global__ void __launch_bounds__(1024) packed_list_kernel(const __grid_constant__ PackedParams p, int4* list) {
     __shared__ int bins[kPackedBins], sums[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     asm volatile("griddepcontrol.launch_dependents;");                  // packed_kernel sets itself up meanwhile
+    const int most = p.n_tokens / (2 * kTileQ) + (p.n_seq + 1023) / 1024;
     bins[tid] = bins[tid + 1024] = 0;
     __syncthreads();
-    for (int s = tid; s < p.n_seq; s += 1024) {
+    for (int s = tid, n = 0; s < p.n_seq; s += 1024) {
         int len;
         packed_sequence(p, s, &len, true);
-        for (int i = 0; i * 2 * kTileQ < len; ++i) atomicAdd(&bins[min(i, kPackedBins - 1)], 1);
+        for (int i = 0; i * 2 * kTileQ < len && n < most; ++i, ++n) atomicAdd(&bins[min(i, kPackedBins - 1)], 1);
     }
     __syncthreads();
     const int hi = kPackedBins - 1 - 2 * tid, a = bins[hi], b = bins[hi - 1];
@@ -88,13 +90,14 @@ static __global__ void __launch_bounds__(1024) packed_list_kernel(const __grid_c
     bins[hi] = before - a - b;
     bins[hi - 1] = before - b;
     __syncthreads();
-    for (int s = tid; s < p.n_seq; s += 1024) {
+    for (int s = tid, n = 0; s < p.n_seq; s += 1024) {
         int len;
         const int token0 = packed_sequence(p, s, &len, false);
-        for (int i = 0; i * 2 * kTileQ < len; ++i) {
-            const int at = atomicAdd(&bins[min(i, kPackedBins - 1)], 1);
-            if (at < p.pairs) list[1 + at] = make_int4(token0, len, i, s);      // more than there can be: sequences that overlap
-            else if (p.status) record_error(p.status, TAG_PACKED, s, at, p.pairs);
+        for (int i = 0; i * 2 * kTileQ < len; ++i, ++n) {
+            const int at = n < most ? atomicAdd(&bins[min(i, kPackedBins - 1)], 1) : p.pairs;
+            if (at < p.pairs) { list[1 + at] = make_int4(token0, len, i, s); continue; }
+            if (p.status) record_error(p.status, TAG_PACKED, s, at, p.pairs);   // more than there can be: sequences that overlap
+            if (n >= most) return;                                              // (no barrier follows)
         }
     }
 }

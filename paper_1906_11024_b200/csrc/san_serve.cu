@@ -267,7 +267,7 @@ int32_t plan_packed(const san_packed_args* a, PackedPlan* out) {
     if (!a) return SAN_ERR_NULL;
     if (a->dtype != SAN_BF16) return a->dtype == SAN_F32 ? SAN_ERR_UNSUPPORTED : SAN_ERR_DTYPE;
     if (a->n_heads < 1 || a->n_heads > 65535 || a->n_kv_heads < 1 || a->n_heads % a->n_kv_heads != 0) return SAN_ERR_SHAPE;
-    if (a->n_layers < 1 || a->n_layers > SAN_MAX_LAYERS || a->n_seq < 0 || a->n_tokens < 0 || a->n_tokens > (1 << 28)) return SAN_ERR_SHAPE;
+    if (a->n_layers < 1 || a->n_layers > SAN_MAX_LAYERS || a->n_seq < 0 || a->n_seq > (1 << 28) || a->n_tokens < 0 || a->n_tokens > (1 << 28)) return SAN_ERR_SHAPE;
     if (a->max_len < 0 || a->max_len > a->n_tokens) return SAN_ERR_SHAPE;
     if (a->ld_q < (int64_t)a->n_heads * kDh || a->ld_k < (int64_t)a->n_kv_heads * kDh || a->ld_v < (int64_t)a->n_kv_heads * kDh) return SAN_ERR_SHAPE;
     if (a->ld_q % 8 != 0 || a->ld_k % 8 != 0 || a->ld_v % 8 != 0) return SAN_ERR_SHAPE;

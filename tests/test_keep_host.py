@@ -173,3 +173,13 @@ def test_mass_bound_of_zero_is_the_mass_itself():
     assert B.san_weight_mass(_mass(max_len=0, ld_mass=(1 << 28) + 1), stream=0) == B.SAN_ERR_SHAPE
     assert B.san_weight_mass(_mass(max_len=0, ld_mass=0, d_S=None), stream=0) == B.SAN_OK         # a mass of no rows
     assert B.san_weight_mass(_mass(max_len=0, ld_mass=-1), stream=0) == B.SAN_ERR_SHAPE
+
+
+def test_packed_more_sequences_than_are_counted():
+    """Counts of tiles are 31 bits: n_tokens / 256 + n_seq was formed in as many and came out negative."""
+    for n_seq, n_tokens in (((1 << 28) + 1, 1000), (0x7fffffff, 1000), (0x7fffffff, 1 << 28)):
+        a = _packed(n_seq=n_seq, n_tokens=n_tokens, n_heads=1, n_kv_heads=1, n_layers=1)
+        assert B.san_packed_block_bytes(a)[0] == B.SAN_ERR_SHAPE
+        assert B.san_packed_block(a, FAKE, BIG, stream=0) == B.SAN_ERR_SHAPE
+    rc, n = B.san_packed_block_bytes(_packed(n_seq=1 << 28, n_tokens=1 << 28))
+    assert rc == B.SAN_OK and n == 16 * (1 + (1 << 20) + (1 << 28))
