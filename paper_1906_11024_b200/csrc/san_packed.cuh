@@ -222,7 +222,7 @@ __device__ __forceinline__ void packed_row_again(const PackedParams& p, const Pa
 
 // Rows of a warp's 32 in the tile x of an item that came out as NaN: computed again where a value that was multiplied by a weight of zero can be
 // the cause, which only later tokens of the tile can hold.  The outputs, which this warp has written, are read for them.
-__device__ __noinline__ void packed_again(const PackedParams& p, const PackedItem& w, int x, int quarter, char* smem, int lane) {
+__device__ __forceinline__ void packed_again(const PackedParams& p, const PackedItem& w, int x, int quarter, char* smem, int lane) {
     const int first = w.a0 + x * kTileQ, last = w.a0 + min((x + 1) * kTileQ, w.rows) - 1, row0 = first + 32 * quarter;
     uint32_t odd = 0;                                       // a bit for each
     for (int r = 0; r < 32 && row0 + r <= last; ++r) {
@@ -247,6 +247,13 @@ __device__ __noinline__ void packed_again(const PackedParams& p, const PackedIte
         const int a = row0 + __ffs(odd) - 1;
         if (a < bad) packed_row_again(p, w, a, smem, lane);  // later ones see it
     }
+}
+
+// The same for all items of the CTA.
+__device__ __noinline__ void packed_items_again(const PackedParams& p, int x, int quarter, char* smem, int lane) {
+    PackedItem w;
+    for (PackedWalk walk(p); walk.next(&w);)
+        if (w.chunks(x) > 0) packed_again(p, w, x, quarter, smem, lane);
 }
 
 template <int LG>
@@ -515,16 +522,12 @@ __global__ void __launch_bounds__(kPackThreads, 1) packed_kernel(const __grid_co
                     *reinterpret_cast<uint4*>(dst + (r - (lane >> 3)) * p.out_ld) = *reinterpret_cast<const uint4*>(mine + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
                 __syncwarp();
             }
-            if (__any_sync(0xffffffffu, odd && lane < left) && lane == 0) again_s[warp] = 1;
+            if (odd && lane < left) again_s[warp] = 1;
         }
         if (!ok && lane == 0 && p.status && atomicCAS(&p.status[0], 0, (int)SAN_ERR_TIMEOUT) == 0) { p.status[1] = TAG_PACKED; p.status[2] = w.seq; }
         // Behind all items, when no wait is under way any more: a row of a long sequence may take longer than a wait may last.
         __syncwarp();
-        if (ok && again_s[warp]) {
-            PackedItem item;
-            for (PackedWalk items(p); items.next(&item);)
-                if (item.chunks(x) > 0) packed_again(p, item, x, quarter, mine, lane);
-        }
+        if (ok && again_s[warp]) packed_items_again(p, x, quarter, mine, lane);
     }
     tile_before_sync();
     __syncthreads();
