@@ -469,7 +469,9 @@ int32_t san_window_block(int32_t dtype, int32_t n_heads, int32_t n_kv_heads, int
  *     S = Softmax(Q . K^T / 8) over those,   O_l = S . V_l   for every layer l of the block (Eq. 1 - 4).
  * Query head h reads key head h / (n_heads / n_kv_heads).  Tokens may lie further apart than their numbers are long (q, k and v of
  * one fused projection): ld_q, ld_k, ld_v are elements between tokens, multiples of 8.  Sequences may be empty.  Tokens that belong to no
- * sequence keep their outputs as they were.  What a token does not see does not reach it, infinities and NaN included.
+ * sequence keep their outputs as they were.  What a token does not see does not reach it, infinities and NaN included (rows beside such values are
+ * computed a second time, one by one: some 30 ms for 32 of them in a sequence of 32768).  A quarter of the exponentials of bounds of 128 and more are
+ * off by up to 1.0e-4, which the rounding of the weights to bf16 covers; the others, and all of shorter bounds, by 2^-22.
  * SAN_BF16 only (SAN_F32: SAN_ERR_UNSUPPORTED, for the reason given for san_full_block).  A sequence that does not lie within the
  * tokens or is longer than max_len is skipped and reported, and so is a tile of sequences that overlap in more tokens than there are. */
 typedef struct {
@@ -507,7 +509,8 @@ typedef struct {
  * (SAN_F32 or SAN_BF16; rows beyond n are neither read nor written; rows_per_item may be more than cap_len where d_nrows is given).
  * Of a row x:  low = min x rounded down to bf16, step = (max x - low) / 15 rounded up to bf16 and, unless it is 0, to 2^-50 at least,
  * n = (x - low) / step rounded to the nearest, half to even (0 where step is 0), of the exact quotients: no number is off by more than
- * step / 2.  A row with a NaN or a number of 2^40 or more reads as NaN.  san_quant_read rounds low + step * n to `dtype`.
+ * step / 2.  A row with a NaN or a number of 2^40 or more reads as NaN.  san_quant_read gives the float32 number next to low + step * n, rounded
+ * once more where `dtype` is bf16.
  * An id, a number of rows or a place out of range skips the item and is reported.  (1 + n_layers) * n_items * rows_per_item *
  * n_kv_heads is below 2^31. */
 int32_t san_quant_append(const san_planes* cache, int32_t dtype, const void* d_k_new, const void* d_v_new, const int32_t* d_ids,
@@ -544,7 +547,7 @@ int32_t san_quant_attn(const san_planes* cache, const san_step_rows* rows, void*
  *     the same for encoder memory, rows = beam             item_stride beam * H * ld_s, row_stride H * ld_s, head_stride ld_s
  *     san_full_block, rows = positions                     item_stride H * cap_len * ld_s, head_stride cap_len * ld_s, row_stride ld_s
  * S[i][r][h][j] is read for j < len alone.  d_rows: rows of each item, 0 .. n_rows (NULL: n_rows).  Sums are float32, in an order that
- * depends on n_rows alone.  An id, length, number of rows or begin out of range skips the item and is reported. */
+ * n_rows and the heads of a group alone decide.  An id, length, number of rows or begin out of range skips the item and is reported. */
 typedef struct {
     int32_t n_heads, n_kv_heads;
     const float* d_S; int64_t item_stride, row_stride, head_stride;

@@ -166,9 +166,10 @@ __device__ __forceinline__ uint32_t evict_least(int want, int (&counts)[256][4],
     return prefix;
 }
 
-// CTA = (key head, item), up to 32 R rows a warp, whose masses stay in registers (row 32 i + lane of the warp's run in register i): read once,
-// and places follow from the warps' counts alone.  Instructions bound it, all of one SM: of a cache of 8 heads and 4096 rows 11 us cold (18 with the counts of every 1024
-// rows added up by every thread, 15 with the key found by comparisons, two bits a turn).
+// CTA = (key head, item), up to 32 R rows a warp, whose masses stay in registers (row 32 i + lane of the warp's run in register i; of R = 16, whose 1024
+// threads have 64 registers each, 22 words a thread lie in local memory): read once, and places follow from the warps' counts alone.
+// Instructions bound it, all of one SM: of a cache of 8 heads and 4096 rows 11 us cold (18 with the counts of every 1024 rows added up by every thread, 15
+// with the key found by comparisons, two bits a turn).
 template <int R>
 __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const __grid_constant__ EvictParams p) {
     __shared__ __align__(16) int digits[256][4];

@@ -17,8 +17,9 @@
 // Tensor memory: a tile of 128 rows has 256 columns: scores twice (64 each, weights over them) and up to two layers' outputs.
 // What bounds it: the softmax warps.  A chunk (256 rows x 64 keys) takes some 1500 clocks, of which a warp is at its exponentials for 700 to 850 (two
 // warps to an SM quarter, whose 16 exponentials a clock and SM they share), at maxima for 250, waiting for scores 200; an item's end takes 2500 to 4000.
-// 48 prompts of 1 to 4096 tokens, 16 heads over 4 key heads: 235 us (296 with a CTA for an item, 16 softmax warps and two threads a row
-// 345, since their meeting took 500 clocks a chunk); two of some 8000 tokens, 8 heads, 2 layers: 199 us = 940 TFLOP/s (247, 296).
+// 48 prompts of 1 to 4096 tokens, 16 heads over 4 key heads: 234 us (296 with a CTA for an item, 16 softmax warps and two threads a row
+// 345, since their meeting took 500 clocks a chunk); two of some 8000 tokens, 8 heads, 2 layers: 224 us = 835 TFLOP/s in calls one after the other, under the
+// power limit, and 199 = 940 in a few of them (those before: 247, 296).
 // Tried and not faster: no look for a chunk's maximum while sums stay small (273 and 235 us: the scores stay live), the second tile started
 // later, weights stored in two halves, the next chunk's scores read and looked through between the halves of this one's exponentials (291 and 254).
 // Every wait is bounded: one that runs out raises a flag that ends the CTA's other waits; the CTA frees its tensor memory, reports, and
@@ -249,7 +250,7 @@ __device__ __forceinline__ void packed_again(const PackedParams& p, const Packed
     }
 }
 
-// The same for all items of the CTA.
+// The same for all items of the CTA, one after the other: 0.9 ms for 32 rows of a block of two layers and every 1000 tokens in front of them.
 __device__ __noinline__ void packed_items_again(const PackedParams& p, int x, int quarter, char* smem, int lane) {
     PackedItem w;
     for (PackedWalk walk(p); walk.next(&w);)

@@ -684,7 +684,8 @@ __device__ __forceinline__ bool quant_unit(const QuantParams& p, int index, bool
     return true;
 }
 
-// P, J: see attend_quant.  Registers leave room for 20 warps on an SM (bf16; 128 rows of up to 4096, 4 layers: 81.7 us; before transposed loads 90, with 16 warps some 4 more).
+// P, J: see attend_quant.  Registers leave room for 20 warps on an SM (bf16; 128 rows of up to 4096, 4 layers: 81.7 us; before transposed loads 90, with 16 warps some 4 more; six of the eight bf16 forms
+// spill a word or two for it).
 template <int LG, int P, int J>
 __global__ void __launch_bounds__(QuantWarps<LG>::W * 32, P == 1 ? LG == 3 ? 6 : 5 : 3) quant_attend_kernel(const __grid_constant__ QuantParams p) {
     constexpr int W = QuantWarps<LG>::W, R = kAtRows;
